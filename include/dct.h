@@ -584,6 +584,127 @@ DCT_API dct_status_t dct_dp_drift_check(
     uint32_t* flag_out, dct_stream_t stream);
 
 /*
+ * Layer norm -- what stands in front of a model split of a Transformer: its output rows are what
+ * dct_mp_topk_pack_fwd packs, its parameter gradients (fp32, summed over the batch) are what the DCT-DP calls
+ * compress.  With mu and var the mean and the (biased) variance of a row's d elements and r = 1/sqrt(var + eps):
+ *   h = (x - mu) r,   y = h * weight + bias
+ *   g = dy * weight,  dx = r (g - mean(g) - h mean(g h)),   dweight = sum_rows dy h,   dbias = sum_rows dy
+ *
+ *   x, dy      [rows, ld] / [rows, ld_dy] row-major, dtype fp32 or bf16; only the first d columns of a row count.
+ *   y, dx      [rows, ld_y] / [rows, ld_dx], dtype of x.  y may be x itself, dx may be x or dy itself (same
+ *              address and stride); any other overlap is refused.
+ *   weight, bias  [d], param_dtype fp32 or bf16; NULL is all ones / all zeros.
+ *   mean, rstd [rows] fp32: mu and r, written by the forward call (there each may be NULL) and read by the
+ *              backward call.
+ *   dweight, dbias  [d] fp32, each may be NULL.  The sums run in a fixed order: equal inputs, equal bits.
+ *   eps        finite, >= 0.
+ *   workspace  (backward) >= dct_layer_norm_bwd_workspace_bytes(rows, d), 256-byte aligned; its contents need not
+ *              be preserved.  Not looked at if dweight and dbias are both NULL.
+ * 1 <= d <= 65536; rows may be 0 (nothing is read or written but dweight and dbias, which become zero).
+ * All arithmetic is fp32, rounded once into y / dx.  A row with NaN or infinities gives NaN, and is not looked for.
+ * Any width, stride and address gives the same result; rows on 16-byte boundaries are the fast case.
+ */
+DCT_API dct_status_t dct_layer_norm_fwd(
+    const void* x, dct_dtype_t dtype, uint32_t rows, uint32_t d, uint32_t ld,
+    const void* weight, const void* bias, dct_dtype_t param_dtype, float eps,
+    void* y, uint32_t ld_y, float* mean_out, float* rstd_out, dct_stream_t stream);
+DCT_API size_t dct_layer_norm_bwd_workspace_bytes(uint32_t rows, uint32_t d);
+DCT_API dct_status_t dct_layer_norm_bwd(
+    const void* dy, uint32_t ld_dy, const void* x, dct_dtype_t dtype, uint32_t rows, uint32_t d, uint32_t ld,
+    const void* weight, dct_dtype_t param_dtype, const float* mean, const float* rstd,
+    void* dx, uint32_t ld_dx, float* dweight, float* dbias,
+    void* workspace, size_t workspace_bytes, dct_stream_t stream);
+
+/* Limits of the calls on rows of logits. */
+#define DCT_LM_MAX_VOCAB 1048576u      /* columns of a row */
+#define DCT_LM_MAX_TOP 256u            /* alternatives dct_lm_logprobs_fwd returns per row */
+#define DCT_LM_MAX_TEACHER_TOP 1024u   /* teacher slots per row dct_lm_distill takes */
+
+/*
+ * dct_lm_logprobs_fwd -- log-probabilities of given tokens, the entropy of the distribution and its most likely
+ * columns, from one pass over the logits.  With z = x * inv_temperature, m = max z and s = log sum exp(z - m):
+ *   log p_j = z_j - m - s,    entropy = -sum p_j log p_j.
+ * For a teacher's batch (top_ids, top_logprobs) is the message dct_lm_distill takes.
+ *
+ *   logits     [rows, ld] row-major, fp32 or bf16; only the first `vocab` columns of a row count.
+ *   tokens     [rows] int32 or NULL.  A negative token asks for nothing: its logprob is 0.
+ *   logprob_out [rows] fp32: log p of the row's token (NULL exactly when tokens is NULL).
+ *   entropy_out [rows] fp32 or NULL.
+ *   stats_out  [rows, 2] fp32 or NULL: m and s of each row, what the backward call takes.
+ *   top        0 <= top <= min(vocab, DCT_LM_MAX_TOP); 0: top_ids and top_logprobs are not looked at.
+ *   top_ids    [rows, top] int32: the columns of the `top` largest logits, best first, equal logits (-0 and +0
+ *              among them) by the lower column.
+ *   top_logprobs [rows, top] fp32: their log p.
+ *   result     device block or NULL; status is DCT_OK, or DCT_ERR_BAD_MASK if a token was >= vocab (it is then
+ *              treated like a negative one).  With NULL no extra work is enqueued for it.
+ * 1 <= vocab <= DCT_LM_MAX_VOCAB; rows may be 0; inv_temperature is finite and > 0.
+ * A masked column holds -inf (log p = -inf, no weight anywhere) or the type's lowest value.  A row that is -inf
+ * throughout has no distribution: m = -inf, s = 0, log p = -inf, entropy 0.  A row with a NaN or +inf gets NaN for
+ * all of its computed values; its top_ids are still in order, NaN after everything else.
+ * Sums are fp32 (any width, stride and address; rows on 16-byte boundaries are the fast case).  Columns outside
+ * the row that share a 16-byte unit with its ends may be read, never used.
+ */
+DCT_API dct_status_t dct_lm_logprobs_fwd(
+    const void* logits, dct_dtype_t dtype, uint32_t rows, uint32_t vocab, uint32_t ld, float inv_temperature,
+    const int32_t* tokens, uint32_t top,
+    float* logprob_out, float* entropy_out, float* stats_out, int32_t* top_ids, float* top_logprobs,
+    dct_result_t* result, dct_stream_t stream);
+
+/*
+ * dct_lm_logprobs_bwd -- the gradient of sum_i (grad_logprob[i] logprob[i] + grad_entropy[i] entropy[i]) at the logits:
+ *   grad_j = inv_temperature * ( a (1[j == token] - p_j) - c p_j (log p_j + entropy) )
+ * with a = grad_logprob[i] (0 for a token < 0 or >= vocab) and c = grad_entropy[i].
+ *
+ *   stats, entropy  from dct_lm_logprobs_fwd on the same logits and temperature.
+ *   grad_logprob    [rows] fp32 or NULL for zeros (tokens may then be NULL).
+ *   grad_entropy    [rows] fp32 or NULL for zeros (entropy may then be NULL).
+ *   grad_logits     [rows, ld_grad], dtype of logits: the first `vocab` columns of each row are written.  It may be
+ *                   logits itself (same address and stride); any other overlap is refused.
+ * A column with p = 0 gets a 1[j == token]; a row without a distribution (m = -inf) gets zeros.
+ */
+DCT_API dct_status_t dct_lm_logprobs_bwd(
+    const void* logits, dct_dtype_t dtype, uint32_t rows, uint32_t vocab, uint32_t ld, float inv_temperature,
+    const int32_t* tokens, const float* stats, const float* entropy,
+    const float* grad_logprob, const float* grad_entropy,
+    void* grad_logits, uint32_t ld_grad, dct_stream_t stream);
+
+typedef enum {
+  DCT_DISTILL_RENORM = 0, /* the teacher's slots are its whole distribution: q = softmax over the slots */
+  DCT_DISTILL_TAIL   = 1  /* q = exp(log-prob); what is missing to 1 is one more class, held against all other columns */
+} dct_distill_mode_t;
+
+/*
+ * dct_lm_distill -- distillation from a teacher's top log-probabilities: the loss of every row and, in the same
+ * call, its gradient at the student's logits.  With p the student's softmax(logits * inv_temperature), i_k and t_k the
+ * teacher's columns and log-probabilities (taken at the temperature the teacher used) of a row's `top` slots:
+ *   RENORM: q = softmax(t);  loss = sum_k q_k (log q_k - log p_{i_k});  dloss/dz_j = p_j - sum_{k: i_k = j} q_k
+ *   TAIL:   q = exp(t), q_r = max(0, 1 - sum q), p_r = sum of p over the columns no slot names;
+ *           loss = sum_k q_k (log q_k - log p_{i_k}) + q_r (log q_r - log p_r);
+ *           dloss/dz_j = p_j - sum_{k: i_k = j} q_k for a column some slot names, p_j (1 - q_r / p_r) for the others
+ *   grad_logits_j = grad_loss * inv_temperature * dloss/dz_j
+ * (q log q = 0 at q = 0; a slot with q = 0 adds nothing; the q_r term is left out where p_r = 0.)
+ *
+ *   teacher_ids       [rows, top] int32, any order.  A negative id is an empty slot.  A column named by several
+ *                     slots has the sum of their q.
+ *   teacher_logprobs  [rows, top] fp32.  In RENORM mode a common offset does not matter: logits / T serve as well.
+ *   top               1 <= top <= DCT_LM_MAX_TEACHER_TOP.
+ *   grad_loss         [rows] fp32 or NULL for ones: the gradient that arrives at each row's loss (0 for padding).
+ *   loss_out          [rows] fp32 or NULL.
+ *   grad_logits       [rows, ld_grad], dtype of logits, or NULL for the loss alone.  May be logits itself (same address
+ *                     and stride); any other overlap is refused.  One of loss_out and grad_logits must be given.
+ *   result            device block or NULL; status is DCT_OK, or DCT_ERR_BAD_MASK if an id was >= vocab (that slot
+ *                     counts as empty).
+ * A RENORM row without a slot that has weight, and a row of logits that is -inf throughout, has loss 0 and gradient 0.
+ * A named column with q > 0 and p = 0 makes the loss +inf (the gradient stays finite).  A row with NaN or +inf in its
+ * logits, or NaN in its teacher's values, gives NaN.  Vocabulary, strides, alignment and rows as in dct_lm_logprobs_fwd.
+ */
+DCT_API dct_status_t dct_lm_distill(
+    const void* logits, dct_dtype_t dtype, uint32_t rows, uint32_t vocab, uint32_t ld, float inv_temperature,
+    const int32_t* teacher_ids, const float* teacher_logprobs, uint32_t top, dct_distill_mode_t mode,
+    const float* grad_loss, float* loss_out, void* grad_logits, uint32_t ld_grad,
+    dct_result_t* result, dct_stream_t stream);
+
+/*
  * TEST-ONLY knobs, exported for the library's own test-suite and not part of the production interface: two
  * process-wide words (atomics) that every later call reads once.  A build with -DDCT_NO_TEST_HOOKS turns the
  * call into a no-op.  spin_limit is the

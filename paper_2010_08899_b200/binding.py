@@ -19,6 +19,7 @@ from . import build as _build
 DCT_OK, DCT_ERR_INVALID_ARG, DCT_ERR_WORKSPACE, DCT_ERR_UNSUPPORTED = 0, 1, 2, 3
 DCT_ERR_CUDA, DCT_ERR_CAPACITY, DCT_ERR_TIMEOUT, DCT_ERR_BAD_MASK = 4, 5, 6, 7
 DCT_F32, DCT_BF16 = 0, 1
+DCT_DISTILL_RENORM, DCT_DISTILL_TAIL = 0, 1
 
 RESULT_BYTES = 40          # sizeof(dct_result_t)
 
@@ -38,9 +39,12 @@ EXPORTED_SYMBOLS = (
     "dct_threshold_select_shard_pass", "dct_threshold_select_shard_advance",
     "dct_threshold_select_shard_sampled_workspace_bytes", "dct_threshold_select_shard_sampled_begin",
     "dct_threshold_select_shard_sampled_pass", "dct_threshold_select_shard_sampled_advance",
+    "dct_layer_norm_fwd", "dct_layer_norm_bwd", "dct_layer_norm_bwd_workspace_bytes",
+    "dct_lm_logprobs_fwd", "dct_lm_logprobs_bwd", "dct_lm_distill",
 )
 
 _vp, _u64, _u32, _sz, _int = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_size_t, ctypes.c_int
+_f32 = ctypes.c_float
 _lib = None
 
 
@@ -131,6 +135,19 @@ def lib() -> ctypes.CDLL:
     L.dct_threshold_select_shard_sampled_pass.argtypes = [_vp, _vp, _u64, _u32, _vp, _vp, _vp]
     L.dct_threshold_select_shard_sampled_advance.restype = _int
     L.dct_threshold_select_shard_sampled_advance.argtypes = [_vp, _u32, _vp, _vp, _vp, _vp]
+    L.dct_layer_norm_fwd.restype = _int
+    L.dct_layer_norm_fwd.argtypes = [_vp, _int, _u32, _u32, _u32, _vp, _vp, _int, _f32, _vp, _u32, _vp, _vp, _vp]
+    L.dct_layer_norm_bwd_workspace_bytes.restype = _sz
+    L.dct_layer_norm_bwd_workspace_bytes.argtypes = [_u32, _u32]
+    L.dct_layer_norm_bwd.restype = _int
+    L.dct_layer_norm_bwd.argtypes = [_vp, _u32, _vp, _int, _u32, _u32, _u32, _vp, _int, _vp, _vp, _vp, _u32, _vp, _vp,
+                                     _vp, _sz, _vp]
+    L.dct_lm_logprobs_fwd.restype = _int
+    L.dct_lm_logprobs_fwd.argtypes = [_vp, _int, _u32, _u32, _u32, _f32, _vp, _u32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+    L.dct_lm_logprobs_bwd.restype = _int
+    L.dct_lm_logprobs_bwd.argtypes = [_vp, _int, _u32, _u32, _u32, _f32, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _vp]
+    L.dct_lm_distill.restype = _int
+    L.dct_lm_distill.argtypes = [_vp, _int, _u32, _u32, _u32, _f32, _vp, _vp, _u32, _int, _vp, _vp, _vp, _u32, _vp, _vp]
     L.dct_debug_configure.restype = None
     L.dct_debug_configure.argtypes = [_u32, _u32]
     _lib = L
@@ -662,3 +679,113 @@ def dct_threshold_select_sharded(grad, residual, n_local, k_global, tau_out, res
 
     sharded_select_rounds(local_histogram, advance, all_reduce_sum)
     return False
+
+
+# --------------------------------------------------------------------------------------------
+# layer norm, and the calls on rows of logits
+# --------------------------------------------------------------------------------------------
+
+DCT_LM_MAX_VOCAB, DCT_LM_MAX_TOP, DCT_LM_MAX_TEACHER_TOP = 1 << 20, 256, 1024
+
+
+def _need_opt(t: Optional[torch.Tensor], dtype, name: str, count: int):
+    """An optional buffer: type, place and at least ``count`` elements."""
+    if t is not None:
+        _need(t, dtype, name)
+        if t.numel() < count:
+            raise ValueError(f"{name}: smaller than {count} elements")
+
+
+def _need_rows(t: torch.Tensor, dtype, name: str, rows: int, d: int, ld: int):
+    """A matrix buffer of ``rows`` rows, ``ld`` elements apart, of which the first ``d`` count."""
+    _need(t, dtype, name)
+    if rows >= 1 and ld >= d and t.numel() < (rows - 1) * ld + d:
+        raise ValueError(f"{name}: smaller than rows x ld")
+
+
+def dct_layer_norm_fwd(x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out=None, rstd_out=None, stream=None) -> None:
+    code = _dtype_code(x)
+    _need_rows(x, x.dtype, "x", rows, d, ld)
+    _need_rows(y, x.dtype, "y", rows, d, ld_y)
+    param = weight if weight is not None else bias
+    pcode = DCT_F32 if param is None else _dtype_code(param)
+    _need_opt(weight, None if param is None else param.dtype, "weight", d)
+    _need_opt(bias, None if param is None else param.dtype, "bias", d)
+    _need_opt(mean_out, torch.float32, "mean_out", rows)
+    _need_opt(rstd_out, torch.float32, "rstd_out", rows)
+    _check("dct_layer_norm_fwd",
+           lib().dct_layer_norm_fwd(_p(x), code, rows, d, ld, _p(weight), _p(bias), pcode, eps, _p(y), ld_y,
+                                    _p(mean_out), _p(rstd_out), _stream(stream)))
+
+
+def dct_layer_norm_bwd_workspace_bytes(rows: int, d: int) -> int:
+    return lib().dct_layer_norm_bwd_workspace_bytes(rows, d)
+
+
+def dct_layer_norm_bwd(dy, ld_dy, x, rows, d, ld, weight, mean, rstd, dx, ld_dx, dweight=None, dbias=None,
+                       workspace=None, stream=None) -> None:
+    code = _dtype_code(x)
+    _need_rows(x, x.dtype, "x", rows, d, ld)
+    _need_rows(dy, x.dtype, "dy", rows, d, ld_dy)
+    _need_rows(dx, x.dtype, "dx", rows, d, ld_dx)
+    pcode = DCT_F32 if weight is None else _dtype_code(weight)
+    _need_opt(weight, None if weight is None else weight.dtype, "weight", d)
+    _need_opt(mean, torch.float32, "mean", rows)
+    _need_opt(rstd, torch.float32, "rstd", rows)
+    _need_opt(dweight, torch.float32, "dweight", d)
+    _need_opt(dbias, torch.float32, "dbias", d)
+    _need_opt(workspace, torch.uint8, "workspace", 0)
+    _check("dct_layer_norm_bwd",
+           lib().dct_layer_norm_bwd(_p(dy), ld_dy, _p(x), code, rows, d, ld, _p(weight), pcode, _p(mean), _p(rstd),
+                                    _p(dx), ld_dx, _p(dweight), _p(dbias), _p(workspace),
+                                    0 if workspace is None else workspace.numel(), _stream(stream)))
+
+
+def dct_lm_logprobs_fwd(logits, rows, vocab, ld, inv_temperature, tokens, top, logprob_out=None, entropy_out=None,
+                        stats_out=None, top_ids=None, top_logprobs=None, result=None, stream=None) -> None:
+    code = _dtype_code(logits)
+    _need_rows(logits, logits.dtype, "logits", rows, vocab, ld)
+    _need_opt(tokens, torch.int32, "tokens", rows)
+    _need_opt(logprob_out, torch.float32, "logprob_out", rows)
+    _need_opt(entropy_out, torch.float32, "entropy_out", rows)
+    _need_opt(stats_out, torch.float32, "stats_out", 2 * rows)
+    _need_opt(top_ids, torch.int32, "top_ids", rows * top)
+    _need_opt(top_logprobs, torch.float32, "top_logprobs", rows * top)
+    _need_opt(result, torch.int64, "result", RESULT_BYTES // 8)
+    _check("dct_lm_logprobs_fwd",
+           lib().dct_lm_logprobs_fwd(_p(logits), code, rows, vocab, ld, inv_temperature, _p(tokens), top,
+                                     _p(logprob_out), _p(entropy_out), _p(stats_out), _p(top_ids), _p(top_logprobs),
+                                     _p(result), _stream(stream)))
+
+
+def dct_lm_logprobs_bwd(logits, rows, vocab, ld, inv_temperature, tokens, stats, entropy, grad_logprob, grad_entropy,
+                        grad_logits, ld_grad, stream=None) -> None:
+    code = _dtype_code(logits)
+    _need_rows(logits, logits.dtype, "logits", rows, vocab, ld)
+    _need_rows(grad_logits, logits.dtype, "grad_logits", rows, vocab, ld_grad)
+    _need_opt(tokens, torch.int32, "tokens", rows)
+    _need_opt(stats, torch.float32, "stats", 2 * rows)
+    _need_opt(entropy, torch.float32, "entropy", rows)
+    _need_opt(grad_logprob, torch.float32, "grad_logprob", rows)
+    _need_opt(grad_entropy, torch.float32, "grad_entropy", rows)
+    _check("dct_lm_logprobs_bwd",
+           lib().dct_lm_logprobs_bwd(_p(logits), code, rows, vocab, ld, inv_temperature, _p(tokens), _p(stats),
+                                     _p(entropy), _p(grad_logprob), _p(grad_entropy), _p(grad_logits), ld_grad,
+                                     _stream(stream)))
+
+
+def dct_lm_distill(logits, rows, vocab, ld, inv_temperature, teacher_ids, teacher_logprobs, top, mode, grad_loss=None,
+                   loss_out=None, grad_logits=None, ld_grad=0, result=None, stream=None) -> None:
+    code = _dtype_code(logits)
+    _need_rows(logits, logits.dtype, "logits", rows, vocab, ld)
+    _need_opt(teacher_ids, torch.int32, "teacher_ids", rows * top)
+    _need_opt(teacher_logprobs, torch.float32, "teacher_logprobs", rows * top)
+    _need_opt(grad_loss, torch.float32, "grad_loss", rows)
+    _need_opt(loss_out, torch.float32, "loss_out", rows)
+    if grad_logits is not None:
+        _need_rows(grad_logits, logits.dtype, "grad_logits", rows, vocab, ld_grad)
+    _need_opt(result, torch.int64, "result", RESULT_BYTES // 8)
+    _check("dct_lm_distill",
+           lib().dct_lm_distill(_p(logits), code, rows, vocab, ld, inv_temperature, _p(teacher_ids),
+                                _p(teacher_logprobs), top, mode, _p(grad_loss), _p(loss_out), _p(grad_logits), ld_grad,
+                                _p(result), _stream(stream)))
