@@ -58,7 +58,292 @@ __device__ __forceinline__ uint32_t cta_count(uint32_t v, uint32_t* scratch) {
     return v;
 }
 
+// A row as 16-byte units ----------------------------------------------------------------------------------------
+// A row starts and ends anywhere; it is read in whole 16-byte units from the boundary at or before its first element
+// (the unit lies in the same page, so the elements outside the row are readable), and what lies outside the row
+// is replaced before it is used.
+
+constexpr float kLog2E = 1.4426950408889634f;
+
+__device__ __forceinline__ float exp2_fast(float x) {            // 2^x within 2 ulp; results below 2^-126 are 0
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// two fp32 in a 64-bit register: one instruction for both
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+template <typename T> struct Unit {};
+template <> struct Unit<float> {
+    static constexpr int kElems = 4;
+    static constexpr uint32_t kMinusInf = 0xFF800000u;
+    __device__ static __forceinline__ float get(const uint4& v, int i) {
+        return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w);
+    }
+    __device__ static __forceinline__ void set(uint4& v, int i, float x) {
+        const uint32_t u = __float_as_uint(x);
+        if (i == 0) v.x = u; else if (i == 1) v.y = u; else if (i == 2) v.z = u; else v.w = u;
+    }
+    // the largest element, NaN only if all are
+    __device__ static __forceinline__ float best(const uint4& a, const uint4& b, const uint4& c, const uint4& d) {
+        const float p = fmaxf(fmaxf(fmaxf(get(a, 0), get(a, 1)), fmaxf(get(a, 2), get(a, 3))),
+                              fmaxf(fmaxf(get(b, 0), get(b, 1)), fmaxf(get(b, 2), get(b, 3))));
+        const float q = fmaxf(fmaxf(fmaxf(get(c, 0), get(c, 1)), fmaxf(get(c, 2), get(c, 3))),
+                              fmaxf(fmaxf(get(d, 0), get(d, 1)), fmaxf(get(d, 2), get(d, 3))));
+        return fmaxf(p, q);
+    }
+};
+template <> struct Unit<__nv_bfloat16> {
+    static constexpr int kElems = 8;
+    static constexpr uint32_t kMinusInf = 0xFF80FF80u;
+    __device__ static __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+    __device__ static __forceinline__ float get(const uint4& v, int i) {
+        const uint32_t w = word(v, i >> 1);
+        return __uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16);
+    }
+    __device__ static __forceinline__ void set(uint4& v, int i, float x) {
+        const uint32_t u = __bfloat16_as_ushort(__float2bfloat16_rn(x));
+        uint32_t w = word(v, i >> 1);
+        w = i & 1 ? (w & 0xFFFFu) | u << 16 : (w & 0xFFFF0000u) | u;
+        if (i >> 1 == 0) v.x = w; else if (i >> 1 == 1) v.y = w; else if (i >> 1 == 2) v.z = w; else v.w = w;
+    }
+    __device__ static __forceinline__ __nv_bfloat162 pair(uint32_t w) { return *reinterpret_cast<__nv_bfloat162*>(&w); }
+    __device__ static __forceinline__ __nv_bfloat162 best2(const uint4& v) {
+        return __hmax2(__hmax2(pair(v.x), pair(v.y)), __hmax2(pair(v.z), pair(v.w)));
+    }
+    __device__ static __forceinline__ float best(const uint4& a, const uint4& b, const uint4& c, const uint4& d) {
+        const __nv_bfloat162 m = __hmax2(__hmax2(best2(a), best2(b)), __hmax2(best2(c), best2(d)));
+        return fmaxf(__low2float(m), __high2float(m));
+    }
+};
+
+__device__ __forceinline__ uint4 ld_unit(const uint4* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void st_unit(void* p, const uint4& v) {
+    asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ float max_nan(float a, float b) {     // NaN if either is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+template <typename T> struct RowView {
+    static constexpr uint32_t kElems = Unit<T>::kElems;
+    const uint4* base;       // the boundary at or before the first element
+    uint32_t lead;           // elements of the first unit that lie before the row
+    uint32_t units;
+    uint32_t width;          // elements of the row
+
+    __device__ __forceinline__ RowView(const T* row, uint32_t width_) : width(width_) {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(row);
+        lead = static_cast<uint32_t>(a & 15u) / static_cast<uint32_t>(sizeof(T));
+        base = reinterpret_cast<const uint4*>(a & ~static_cast<uintptr_t>(15));
+        units = (lead + width + kElems - 1) / kElems;
+    }
+    // column of element i of unit u; >= width (as unsigned) outside the row
+    __device__ __forceinline__ uint32_t column(uint32_t u, uint32_t i) const { return u * kElems + i - lead; }
+    __device__ __forceinline__ bool at_an_end(uint32_t u) const { return u == 0 || u + 1 == units; }
+    // -inf in the place of what lies outside the row (only the first and the last unit can hold such elements)
+    __device__ __forceinline__ void mask(uint4& v, uint32_t u) const {
+        if (at_an_end(u)) {
+#pragma unroll
+            for (uint32_t i = 0; i < kElems; ++i)
+                if (column(u, i) >= width) Unit<T>::set(v, i, minus_inf());
+        }
+    }
+};
+
+// Writes unit u of a row laid out as `row`, element by element where the unit holds anything else, too (or everywhere, if
+// the output row sits differently against the 16-byte boundaries: `aligned` is false then).
+template <typename T>
+__device__ __forceinline__ void store_unit(const RowView<T>& row, T* out, uint32_t u, const float (&g)[Unit<T>::kElems], bool aligned) {
+    constexpr uint32_t E = Unit<T>::kElems;
+    if (aligned && !row.at_an_end(u)) {
+        uint4 v;
+        if constexpr (sizeof(T) == 4) {
+            v = make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
+        } else {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(g[2 * i], g[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            v = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        st_unit(out + row.column(u, 0), v);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < E; ++i) {
+            const uint32_t col = row.column(u, i);
+            if (col < row.width) out[col] = from_f32<T>(g[i]);
+        }
+    }
+}
+inline __device__ bool same_boundary(const void* a, const void* b) {      // alike against the 16-byte boundaries
+    return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
+}
+
+// One thread's share of sum exp(z - ref) and sum exp(z - ref) (z - ref) over a row, z = x inv_t, with a reference of
+// its own that is at most kSlack below the largest z so far: the sums are rescaled only when a batch exceeds it by more.
+// z - ref is formed exactly but for one rounding (a product with log2 e folded into the logits would lose the digits
+// in which large logits differ), so log p of any column is (z - m) - log sum to fp32 accuracy.
+struct RowSums {
+    static constexpr float kSlack = 2.0f;
+    float ref, s, st;
+    __device__ __forceinline__ RowSums() : ref(minus_inf()), s(0.0f), st(0.0f) {}
+
+    __device__ __forceinline__ void rebase(float to) {
+        if (ref != minus_inf()) {
+            // (a reference of the type's lowest value is too far off for s * d; from -1e4 on f is 0 all the same)
+            const float d = max_nan(__fadd_rn(ref, -to), -1.0e4f), f = exp2_fast(__fmul_rn(d, kLog2E));
+            st = __fmul_rn(f, fmaf(s, d, st));
+            s = __fmul_rn(f, s);
+        }
+        ref = to;
+    }
+    // best: the batch's largest element
+    template <typename T, bool kMoment> __device__ __forceinline__ void add(const uint4 (&v)[4], float best, float inv_t) {
+        constexpr int E = Unit<T>::kElems;
+        const float zb = __fmul_rn(best, inv_t);
+        if (!(zb <= __fadd_rn(ref, kSlack)) && zb > minus_inf()) rebase(zb);
+        if (ref == minus_inf()) {        // nothing but -inf and NaN so far
+            float any = 0.0f;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < E; ++i) any = __fadd_rn(any, Unit<T>::get(v[u], i));
+            if (any != any) s = any;
+            return;
+        }
+        const uint64_t t_scale = pack2(inv_t, inv_t), shift = pack2(-ref, -ref), to_log2 = pack2(kLog2E, kLog2E);
+        uint64_t sb = 0, stb = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < E; i += 2) {
+                const uint64_t t = fma2(pack2(Unit<T>::get(v[u], i), Unit<T>::get(v[u], i + 1)), t_scale, shift);
+                float y0, y1;
+                unpack2(mul2(t, to_log2), y0, y1);
+                const uint64_t e = pack2(exp2_fast(y0), exp2_fast(y1));
+                sb = add2(sb, e);
+                if (kMoment) stb = fma2(e, t, stb);
+            }
+        float a, b;
+        unpack2(sb, a, b);
+        s = __fadd_rn(s, __fadd_rn(a, b));
+        if (kMoment) {
+            unpack2(stb, a, b);
+            float sum = __fadd_rn(a, b);
+            if (sum != sum) {            // 0 * -inf at masked columns: leave those out
+                sum = 0.0f;
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int i = 0; i < E; ++i) {
+                        const float t = fmaf(Unit<T>::get(v[u], i), inv_t, -ref);
+                        const float e = exp2_fast(__fmul_rn(t, kLog2E));
+                        if (e != 0.0f) sum = fmaf(e, t, sum);
+                    }
+            }
+            st = __fadd_rn(st, sum);
+        }
+    }
+    // the same sums relative to m (the row's largest z)
+    __device__ __forceinline__ void finish(float m) {
+        if (s == 0.0f) {
+            st = 0.0f;
+        } else {
+            rebase(m);
+        }
+        ref = m;
+    }
+};
+
+// Clusters of CTAs -------------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+// every CTA of the cluster has arrived, and what each wrote to its shared memory before is visible to all
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t remote_smem(const void* p, uint32_t rank) {      // p's counterpart in CTA `rank`
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ float ld_remote_f32(uint32_t a) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t ld_remote_u32(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint64_t ld_remote_u64(uint32_t a) {
+    uint64_t v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
+    return v;
+}
+
 // Host side ---------------------------------------------------------------------------------------------------
+
+// launches `kernel` in clusters of `cluster` CTAs
+template <typename... Params, typename... Args>
+cudaError_t launch_clusters(void (*kernel)(Params...), unsigned grid, unsigned block, unsigned cluster, size_t smem,
+                            cudaStream_t stream, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute shape = {};
+    shape.id = cudaLaunchAttributeClusterDimension;
+    shape.val.clusterDim.x = cluster;
+    shape.val.clusterDim.y = 1;
+    shape.val.clusterDim.z = 1;
+    cfg.attrs = &shape;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
 
 inline size_t element_size(dct_dtype_t t) { return t == DCT_F32 ? 4 : 2; }
 inline bool known_dtype(dct_dtype_t t) { return t == DCT_F32 || t == DCT_BF16; }
