@@ -688,34 +688,33 @@ def dct_threshold_select_sharded(grad, residual, n_local, k_global, tau_out, res
 DCT_LM_MAX_VOCAB, DCT_LM_MAX_TOP, DCT_LM_MAX_TEACHER_TOP = 1 << 20, 256, 1024
 
 
-def _need_opt(t: Optional[torch.Tensor], dtype, name: str, count: int):
-    """An optional buffer: type, place and at least ``count`` elements."""
-    if t is not None:
+def _buf(t: Optional[torch.Tensor], dtype, name: str, count: int):
+    """The address of an optional buffer (None if absent) after the checks of type, place and at least ``count``
+    elements.  One call per argument: these calls also run once per decoded token, where the host's time counts."""
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
         _need(t, dtype, name)
-        if t.numel() < count:
-            raise ValueError(f"{name}: smaller than {count} elements")
+    if t.numel() < count:
+        raise ValueError(f"{name}: smaller than {count} elements")
+    return t.data_ptr()
 
 
-def _need_rows(t: torch.Tensor, dtype, name: str, rows: int, d: int, ld: int):
-    """A matrix buffer of ``rows`` rows, ``ld`` elements apart, of which the first ``d`` count."""
-    _need(t, dtype, name)
-    if rows >= 1 and ld >= d and t.numel() < (rows - 1) * ld + d:
-        raise ValueError(f"{name}: smaller than rows x ld")
+def _span(rows: int, d: int, ld: int) -> int:
+    """Elements from the first to one past the last of ``rows`` rows, ``ld`` apart, of which the first ``d`` count."""
+    return (rows - 1) * ld + d if rows >= 1 and ld >= d else 0
 
 
 def dct_layer_norm_fwd(x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out=None, rstd_out=None, stream=None) -> None:
-    code = _dtype_code(x)
-    _need_rows(x, x.dtype, "x", rows, d, ld)
-    _need_rows(y, x.dtype, "y", rows, d, ld_y)
+    code, dt = _dtype_code(x), x.dtype
     param = weight if weight is not None else bias
-    pcode = DCT_F32 if param is None else _dtype_code(param)
-    _need_opt(weight, None if param is None else param.dtype, "weight", d)
-    _need_opt(bias, None if param is None else param.dtype, "bias", d)
-    _need_opt(mean_out, torch.float32, "mean_out", rows)
-    _need_opt(rstd_out, torch.float32, "rstd_out", rows)
-    _check("dct_layer_norm_fwd",
-           lib().dct_layer_norm_fwd(_p(x), code, rows, d, ld, _p(weight), _p(bias), pcode, eps, _p(y), ld_y,
-                                    _p(mean_out), _p(rstd_out), _stream(stream)))
+    pcode, pdt = (DCT_F32, None) if param is None else (_dtype_code(param), param.dtype)
+    f32 = torch.float32
+    status = lib().dct_layer_norm_fwd(
+        _buf(x, dt, "x", _span(rows, d, ld)), code, rows, d, ld, _buf(weight, pdt, "weight", d), _buf(bias, pdt, "bias", d),
+        pcode, eps, _buf(y, dt, "y", _span(rows, d, ld_y)), ld_y, _buf(mean_out, f32, "mean_out", rows),
+        _buf(rstd_out, f32, "rstd_out", rows), _stream(stream))
+    _check("dct_layer_norm_fwd", status)
 
 
 def dct_layer_norm_bwd_workspace_bytes(rows: int, d: int) -> int:
@@ -724,68 +723,47 @@ def dct_layer_norm_bwd_workspace_bytes(rows: int, d: int) -> int:
 
 def dct_layer_norm_bwd(dy, ld_dy, x, rows, d, ld, weight, mean, rstd, dx, ld_dx, dweight=None, dbias=None,
                        workspace=None, stream=None) -> None:
-    code = _dtype_code(x)
-    _need_rows(x, x.dtype, "x", rows, d, ld)
-    _need_rows(dy, x.dtype, "dy", rows, d, ld_dy)
-    _need_rows(dx, x.dtype, "dx", rows, d, ld_dx)
-    pcode = DCT_F32 if weight is None else _dtype_code(weight)
-    _need_opt(weight, None if weight is None else weight.dtype, "weight", d)
-    _need_opt(mean, torch.float32, "mean", rows)
-    _need_opt(rstd, torch.float32, "rstd", rows)
-    _need_opt(dweight, torch.float32, "dweight", d)
-    _need_opt(dbias, torch.float32, "dbias", d)
-    _need_opt(workspace, torch.uint8, "workspace", 0)
-    _check("dct_layer_norm_bwd",
-           lib().dct_layer_norm_bwd(_p(dy), ld_dy, _p(x), code, rows, d, ld, _p(weight), pcode, _p(mean), _p(rstd),
-                                    _p(dx), ld_dx, _p(dweight), _p(dbias), _p(workspace),
-                                    0 if workspace is None else workspace.numel(), _stream(stream)))
+    code, dt, f32 = _dtype_code(x), x.dtype, torch.float32
+    pcode, pdt = (DCT_F32, None) if weight is None else (_dtype_code(weight), weight.dtype)
+    status = lib().dct_layer_norm_bwd(
+        _buf(dy, dt, "dy", _span(rows, d, ld_dy)), ld_dy, _buf(x, dt, "x", _span(rows, d, ld)), code, rows, d, ld,
+        _buf(weight, pdt, "weight", d), pcode, _buf(mean, f32, "mean", rows), _buf(rstd, f32, "rstd", rows),
+        _buf(dx, dt, "dx", _span(rows, d, ld_dx)), ld_dx, _buf(dweight, f32, "dweight", d), _buf(dbias, f32, "dbias", d),
+        _buf(workspace, torch.uint8, "workspace", 0), 0 if workspace is None else workspace.numel(), _stream(stream))
+    _check("dct_layer_norm_bwd", status)
 
 
 def dct_lm_logprobs_fwd(logits, rows, vocab, ld, inv_temperature, tokens, top, logprob_out=None, entropy_out=None,
                         stats_out=None, top_ids=None, top_logprobs=None, result=None, stream=None) -> None:
-    code = _dtype_code(logits)
-    _need_rows(logits, logits.dtype, "logits", rows, vocab, ld)
-    _need_opt(tokens, torch.int32, "tokens", rows)
-    _need_opt(logprob_out, torch.float32, "logprob_out", rows)
-    _need_opt(entropy_out, torch.float32, "entropy_out", rows)
-    _need_opt(stats_out, torch.float32, "stats_out", 2 * rows)
-    _need_opt(top_ids, torch.int32, "top_ids", rows * top)
-    _need_opt(top_logprobs, torch.float32, "top_logprobs", rows * top)
-    _need_opt(result, torch.int64, "result", RESULT_BYTES // 8)
-    _check("dct_lm_logprobs_fwd",
-           lib().dct_lm_logprobs_fwd(_p(logits), code, rows, vocab, ld, inv_temperature, _p(tokens), top,
-                                     _p(logprob_out), _p(entropy_out), _p(stats_out), _p(top_ids), _p(top_logprobs),
-                                     _p(result), _stream(stream)))
+    code, f32, i32 = _dtype_code(logits), torch.float32, torch.int32
+    status = lib().dct_lm_logprobs_fwd(
+        _buf(logits, logits.dtype, "logits", _span(rows, vocab, ld)), code, rows, vocab, ld, inv_temperature,
+        _buf(tokens, i32, "tokens", rows), top, _buf(logprob_out, f32, "logprob_out", rows),
+        _buf(entropy_out, f32, "entropy_out", rows), _buf(stats_out, f32, "stats_out", 2 * rows),
+        _buf(top_ids, i32, "top_ids", rows * top), _buf(top_logprobs, f32, "top_logprobs", rows * top),
+        _buf(result, torch.int64, "result", RESULT_BYTES // 8), _stream(stream))
+    _check("dct_lm_logprobs_fwd", status)
 
 
 def dct_lm_logprobs_bwd(logits, rows, vocab, ld, inv_temperature, tokens, stats, entropy, grad_logprob, grad_entropy,
                         grad_logits, ld_grad, stream=None) -> None:
-    code = _dtype_code(logits)
-    _need_rows(logits, logits.dtype, "logits", rows, vocab, ld)
-    _need_rows(grad_logits, logits.dtype, "grad_logits", rows, vocab, ld_grad)
-    _need_opt(tokens, torch.int32, "tokens", rows)
-    _need_opt(stats, torch.float32, "stats", 2 * rows)
-    _need_opt(entropy, torch.float32, "entropy", rows)
-    _need_opt(grad_logprob, torch.float32, "grad_logprob", rows)
-    _need_opt(grad_entropy, torch.float32, "grad_entropy", rows)
-    _check("dct_lm_logprobs_bwd",
-           lib().dct_lm_logprobs_bwd(_p(logits), code, rows, vocab, ld, inv_temperature, _p(tokens), _p(stats),
-                                     _p(entropy), _p(grad_logprob), _p(grad_entropy), _p(grad_logits), ld_grad,
-                                     _stream(stream)))
+    code, dt, f32 = _dtype_code(logits), logits.dtype, torch.float32
+    status = lib().dct_lm_logprobs_bwd(
+        _buf(logits, dt, "logits", _span(rows, vocab, ld)), code, rows, vocab, ld, inv_temperature,
+        _buf(tokens, torch.int32, "tokens", rows), _buf(stats, f32, "stats", 2 * rows),
+        _buf(entropy, f32, "entropy", rows), _buf(grad_logprob, f32, "grad_logprob", rows),
+        _buf(grad_entropy, f32, "grad_entropy", rows),
+        _buf(grad_logits, dt, "grad_logits", _span(rows, vocab, ld_grad)), ld_grad, _stream(stream))
+    _check("dct_lm_logprobs_bwd", status)
 
 
 def dct_lm_distill(logits, rows, vocab, ld, inv_temperature, teacher_ids, teacher_logprobs, top, mode, grad_loss=None,
                    loss_out=None, grad_logits=None, ld_grad=0, result=None, stream=None) -> None:
-    code = _dtype_code(logits)
-    _need_rows(logits, logits.dtype, "logits", rows, vocab, ld)
-    _need_opt(teacher_ids, torch.int32, "teacher_ids", rows * top)
-    _need_opt(teacher_logprobs, torch.float32, "teacher_logprobs", rows * top)
-    _need_opt(grad_loss, torch.float32, "grad_loss", rows)
-    _need_opt(loss_out, torch.float32, "loss_out", rows)
-    if grad_logits is not None:
-        _need_rows(grad_logits, logits.dtype, "grad_logits", rows, vocab, ld_grad)
-    _need_opt(result, torch.int64, "result", RESULT_BYTES // 8)
-    _check("dct_lm_distill",
-           lib().dct_lm_distill(_p(logits), code, rows, vocab, ld, inv_temperature, _p(teacher_ids),
-                                _p(teacher_logprobs), top, mode, _p(grad_loss), _p(loss_out), _p(grad_logits), ld_grad,
-                                _p(result), _stream(stream)))
+    code, dt, f32 = _dtype_code(logits), logits.dtype, torch.float32
+    status = lib().dct_lm_distill(
+        _buf(logits, dt, "logits", _span(rows, vocab, ld)), code, rows, vocab, ld, inv_temperature,
+        _buf(teacher_ids, torch.int32, "teacher_ids", rows * top), _buf(teacher_logprobs, f32, "teacher_logprobs", rows * top),
+        top, mode, _buf(grad_loss, f32, "grad_loss", rows), _buf(loss_out, f32, "loss_out", rows),
+        _buf(grad_logits, dt, "grad_logits", _span(rows, vocab, ld_grad)), ld_grad,
+        _buf(result, torch.int64, "result", RESULT_BYTES // 8), _stream(stream))
+    _check("dct_lm_distill", status)

@@ -31,9 +31,10 @@ template <uint32_t kThreads> struct LogProbShared {
     float group_max[kMaxima];
     uint64_t candidates[kCandidates];
     uint64_t best[DCT_LM_MAX_TOP];
-    float scratch[32];
+    uint16_t hits[kMaxima];
+    float slots[96];
     uint32_t counts[32];
-    uint32_t counter;
+    uint32_t counter, hit_count;
     SlicePart part;
 };
 
@@ -65,24 +66,33 @@ template <typename T, uint32_t kThreads> struct Selector {
         return static_cast<uint64_t>(key) << 32 | (0xFFFFFFFFu - col);
     }
     // candidates := the slice's columns with key >= bound (> bound if strict); returns how many there are, of which the
-    // first kCandidates found are stored
+    // first kCandidates found are stored.  The groups whose maximum reaches the bound are listed first and their units
+    // then dealt out over all threads: every load is independent of the others.
     __device__ uint32_t collect(uint32_t bound, bool strict) {
         __syncthreads();
-        if (threadIdx.x == 0) sh.counter = 0;
+        if (threadIdx.x == 0) sh.counter = sh.hit_count = 0;
         __syncthreads();
-        const uint32_t span = per_group * 4 * kThreads;
-        uint32_t g = 0;
-        for (uint32_t first = u0; first < u1; first += span, ++g) {
-            const uint32_t top_key = order_key(sh.group_max[g * kThreads + threadIdx.x]);
-            if (strict ? top_key <= bound : top_key < bound) continue;
-            const uint32_t end = min(u1, first + span);
-            for (uint32_t u = first + threadIdx.x; u < end; u += kThreads)
-                each_element(u, [&](uint32_t key, uint32_t col) {
-                    if (strict ? key > bound : key >= bound) {
-                        const uint32_t at = atomicAdd(&sh.counter, 1u);
-                        if (at < kCandidates) sh.candidates[at] = entry(key, col);
-                    }
-                });
+        const uint32_t low = strict ? bound + 1 : bound;          // (bound = 0xFFFFFFFF is no element's key)
+        const uint32_t span = per_group * 4 * kThreads, groups = (u1 - u0 + span - 1) / span;
+        for (uint32_t g = 0; g < groups; ++g)
+            if (order_key(sh.group_max[g * kThreads + threadIdx.x]) >= low)
+                sh.hits[atomicAdd(&sh.hit_count, 1u)] = static_cast<uint16_t>(g * kThreads + threadIdx.x);
+        __syncthreads();
+        const uint32_t in_group = per_group * 4, items = sh.hit_count * in_group;
+        for (uint32_t item = threadIdx.x; item < items; item += kThreads) {
+            const uint32_t hit = sh.hits[item / in_group];
+            const uint32_t u = u0 + (hit / kThreads * in_group + item % in_group) * kThreads + hit % kThreads;
+            if (u >= u1) continue;
+            const uint4 v = ld_unit(row.base + u);
+            if (low > 1 && order_key(Unit<T>::best(v, v, v, v)) < low) continue;
+#pragma unroll
+            for (uint32_t i = 0; i < E; ++i) {
+                const uint32_t col = row.column(u, i), key = order_key(Unit<T>::get(v, i));
+                if (key >= low && col < row.width) {
+                    const uint32_t at = atomicAdd(&sh.counter, 1u);
+                    if (at < kCandidates) sh.candidates[at] = entry(key, col);
+                }
+            }
         }
         __syncthreads();
         return sh.counter;
@@ -161,12 +171,12 @@ template <typename T, uint32_t kThreads> struct Selector {
             __syncthreads();
             if (lane_id() == 0) {
                 sh.counts[threadIdx.x >> 5] = hi;
-                sh.scratch[threadIdx.x >> 5] = __uint_as_float(lo);
+                sh.slots[threadIdx.x >> 5] = __uint_as_float(lo);
             }
             __syncthreads();
             for (uint32_t w = 0; w < kThreads / 32; ++w) {
                 hi = max(hi, sh.counts[w]);
-                lo = min(lo, __float_as_uint(sh.scratch[w]));
+                lo = min(lo, __float_as_uint(sh.slots[w]));
             }
             // at least kk threads reach lo, fewer reach hi + 1; a few more than kk are as good as kk
             while (lo < hi) {
@@ -174,7 +184,7 @@ template <typename T, uint32_t kThreads> struct Selector {
                 const uint32_t c = __syncthreads_count(key >= mid);
                 if (c >= kk) lo = mid;
                 else hi = mid - 1;
-                if (c >= kk && c <= kk + kk / 8 + 2) break;
+                if (c >= kk && c <= kk + kk / 4 + 2) break;
             }
             bound = lo;
         }
@@ -238,17 +248,8 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
         for (uint32_t b = 0; b < batches; ++b) {
             const uint32_t first = u0 + b * 4 * kThreads + tid;
             uint4 v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t u = first + i * kThreads;
-                v[i] = make_uint4(Unit<T>::kMinusInf, Unit<T>::kMinusInf, Unit<T>::kMinusInf, Unit<T>::kMinusInf);
-                if (u < u1) v[i] = ld_unit(row.base + u);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t u = first + i * kThreads;
-                if (u < u1) row.mask(v[i], u);
-            }
+            load_batch<T, kThreads>(v, row, first, u1);
+            mask_batch<T, kThreads>(v, row, first, u1);
             const float best = Unit<T>::best(v[0], v[1], v[2], v[3]);
             sums.add<T, true>(v, best, a.inv_t);
             group_max = fmaxf(group_max, best);
@@ -261,10 +262,8 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
             }
         }
         // the slice's sums, relative to its largest z
-        float m = __fmul_rn(cta_join<MaxOp>(thread_max, sh.scratch), a.inv_t);
-        sums.finish(m);
-        float s = cta_join<SumOp>(sums.s, sh.scratch);
-        float st = cta_join<SumOp>(sums.st, sh.scratch);
+        sums.join_cta(__fmul_rn(thread_max, a.inv_t), sh.slots);
+        float m = sums.ref, s = sums.s, st = sums.st;
 
         uint32_t kept = 0;
         if (a.top) {

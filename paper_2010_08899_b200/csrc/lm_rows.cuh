@@ -277,16 +277,65 @@ struct RowSums {
             st = __fadd_rn(st, sum);
         }
     }
-    // the same sums relative to m (the row's largest z)
+    // the same sums relative to m (the largest z of whatever is joined; -inf if that is all there is)
     __device__ __forceinline__ void finish(float m) {
-        if (s == 0.0f) {
-            st = 0.0f;
-        } else {
-            rebase(m);
-        }
+        if (s == 0.0f) st = 0.0f;
+        else rebase(m);
         ref = m;
     }
+    // joins `lanes` (a power of two) neighbouring lanes: all get the sums of all; the order is fixed
+    __device__ __forceinline__ void join_lanes(float m, int lanes) {
+        for (int o = lanes / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        finish(m);
+        for (int o = lanes / 2; o > 0; o >>= 1) {
+            s = __fadd_rn(s, __shfl_xor_sync(0xFFFFFFFFu, s, o));
+            st = __fadd_rn(st, __shfl_xor_sync(0xFFFFFFFFu, st, o));
+        }
+    }
+    // joins the CTA's threads with one barrier.  m: the largest z this thread has met.  slots: 3 x 32 floats that nothing
+    // else uses before the next barrier.
+    __device__ __forceinline__ void join_cta(float m, float* slots) {
+        join_lanes(m, 32);
+        const uint32_t warps = blockDim.x >> 5, lane = lane_id();
+        if (lane == 0) {
+            slots[threadIdx.x >> 5] = ref;
+            slots[32 + (threadIdx.x >> 5)] = s;
+            slots[64 + (threadIdx.x >> 5)] = st;
+        }
+        __syncthreads();
+        const uint32_t w = lane & (warps - 1);                 // (warps is a power of two)
+        ref = slots[w];
+        s = slots[32 + w];
+        st = slots[64 + w];
+        join_lanes(ref, static_cast<int>(warps));
+    }
 };
+
+// A thread's units first, first + kThreads, ... of a slice that ends at u1: loaded without looking at bounds where all
+// threads' units lie inside, -inf beyond the slice; and the row's ends masked in the batches that can hold them.
+template <typename T, uint32_t kThreads>
+__device__ __forceinline__ void load_batch(uint4 (&v)[4], const RowView<T>& row, uint32_t first, uint32_t u1) {
+    if (first - threadIdx.x + 4 * kThreads <= u1) {            // the same for the whole CTA
+        const uint4* p = row.base + first;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = ld_unit(p + i * kThreads);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = make_uint4(Unit<T>::kMinusInf, Unit<T>::kMinusInf, Unit<T>::kMinusInf, Unit<T>::kMinusInf);
+            if (first + i * kThreads < u1) v[i] = ld_unit(row.base + first + i * kThreads);
+        }
+    }
+}
+template <typename T, uint32_t kThreads>
+__device__ __forceinline__ void mask_batch(uint4 (&v)[4], const RowView<T>& row, uint32_t first, uint32_t u1) {
+    const uint32_t batch = first - threadIdx.x;
+    if (batch == 0 || batch + 4 * kThreads >= row.units) {     // the same for the whole CTA
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (first + i * kThreads < u1) row.mask(v[i], first + i * kThreads);
+    }
+}
 
 // Clusters of CTAs -------------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {
