@@ -5,13 +5,11 @@ namespace dct {
 namespace {
 
 constexpr uint32_t kMaxCluster = 8u;
-constexpr uint32_t kMaxima = 4096u;           // noted maxima of a CTA (16 for each of 256 threads)
-constexpr uint32_t kCandidates = 2048u;       // columns the selection holds at a time
-constexpr uint32_t kRankable = 512u;          // ... and the most it puts in order by counting
+constexpr uint32_t kRankable = 512u;          // the most columns the selection puts in order
 
 struct LogProbArgs {
     uint32_t rows, vocab, ld;
-    float inv_t;
+    float inv_t, c;                 // 1 / T and log2 e / T
     const int32_t* tokens;
     uint32_t top;
     float *logprob_out, *entropy_out, *stats_out;
@@ -20,22 +18,20 @@ struct LogProbArgs {
     dct_result_t* result;
 };
 
-// What one CTA knows of its slice of the row, read by the others of its cluster.
-struct SlicePart {
-    float m, s, st;
-    uint32_t kept;
-};
-
 template <uint32_t kThreads> struct LogProbShared {
-    static constexpr uint32_t kGroups = kMaxima / kThreads;
-    float group_max[kMaxima];
+    static constexpr uint32_t kWarps = kThreads / 32;
+    static constexpr uint32_t kGroups = kThreads > 256 ? 8 : 16;                   // maxima a thread notes
+    static constexpr uint32_t kCandidates = kThreads > 128 ? 2048 : 1024;          // columns the selection holds
+    float group_max[kGroups * kThreads];
     uint64_t candidates[kCandidates];
     uint64_t best[DCT_LM_MAX_TOP];
-    uint16_t hits[kMaxima];
-    float slots[96];
+    float thread_max[kThreads];
+    uint16_t hits[kGroups * kThreads];
+    RowPart warp_part[2][kWarps];      // by turns, row by row
+    RowPart part;                      // this CTA's slice
+    float m, logsum;                   // of the whole row
     uint32_t counts[32];
-    uint32_t counter, hit_count;
-    SlicePart part;
+    uint32_t counter, hit_count, bound, kept;
 };
 
 __device__ __forceinline__ float value_of_key(uint32_t key) {       // the inverse of order_key
@@ -46,12 +42,13 @@ __device__ __forceinline__ float value_of_key(uint32_t key) {       // the inver
 // While the row streams by, every thread notes the largest element of each batch of units it reads.  The kk-th
 // largest of the threads' own maxima is a bound that at least kk columns reach and, for kk well below the number of
 // threads, not many more do (T ln(T / (T - kk)) for columns in no particular order); only batches whose noted maximum reaches it
-// are read again, and of them the elements that reach it are put in order by counting.
+// are read again, and of them the elements that reach it are put in order.
 template <typename T, uint32_t kThreads> struct Selector {
     static constexpr uint32_t E = Unit<T>::kElems;
-    const RowView<T>& row;
+    static constexpr uint32_t kCandidates = LogProbShared<kThreads>::kCandidates;
+    RowView<T> row;
     uint32_t u0, u1;                // the slice's units
-    uint32_t per_group;             // batches per noted maximum
+    uint32_t group_shift;           // log2 of the batches per noted maximum
     LogProbShared<kThreads>& sh;
 
     template <typename F> __device__ __forceinline__ void each_element(uint32_t u, F&& f) const {
@@ -65,57 +62,118 @@ template <typename T, uint32_t kThreads> struct Selector {
     __device__ __forceinline__ static uint64_t entry(uint32_t key, uint32_t col) {
         return static_cast<uint64_t>(key) << 32 | (0xFFFFFFFFu - col);
     }
-    // candidates := the slice's columns with key >= bound (> bound if strict); returns how many there are, of which the
-    // first kCandidates found are stored.  The groups whose maximum reaches the bound are listed first and their units
-    // then dealt out over all threads: every load is independent of the others.
-    __device__ uint32_t collect(uint32_t bound, bool strict) {
-        __syncthreads();
+    // By one warp, from the threads' maxima: a key that at least kk of them reach, and not many more if that can be had
+    // (0 if fewer than kk threads have a unit).
+    __device__ __forceinline__ uint32_t find_bound(uint32_t kk) const {
+        constexpr uint32_t N = kThreads / 32;
+        const uint32_t units = u1 - u0;
+        if (min(units, kThreads) < kk) return 0;
+        uint32_t key[N], lo = 0xFFFFFFFFu, hi = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) {
+            const uint32_t t = i * 32 + lane_id();
+            key[i] = t < units ? order_key(sh.thread_max[t]) : 0u;
+            lo = min(lo, key[i]);
+            hi = max(hi, key[i]);
+        }
+        lo = __reduce_min_sync(0xFFFFFFFFu, lo);
+        hi = __reduce_max_sync(0xFFFFFFFFu, hi);
+        // at least kk threads reach lo, fewer reach hi + 1; a few more than kk are as good as kk
+        while (lo < hi) {
+            const uint32_t mid = lo + (hi - lo) / 2 + 1;
+            uint32_t n = 0;
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i) n += key[i] >= mid;
+            n = __reduce_add_sync(0xFFFFFFFFu, n);
+            if (n >= kk) lo = mid;
+            else hi = mid - 1;
+            if (n >= kk && n <= kk + kk / 8 + 1) break;
+        }
+        return lo;
+    }
+    // candidates := the slice's columns with key >= low; returns how many there are, of which the first kCandidates
+    // found are stored.  The groups whose maximum reaches the bound are listed first; their units are then dealt out over all
+    // threads.
+    __device__ __forceinline__ uint32_t collect(uint32_t low) const {
         if (threadIdx.x == 0) sh.counter = sh.hit_count = 0;
         __syncthreads();
-        const uint32_t low = strict ? bound + 1 : bound;          // (bound = 0xFFFFFFFF is no element's key)
-        const uint32_t span = per_group * 4 * kThreads, groups = (u1 - u0 + span - 1) / span;
-        for (uint32_t g = 0; g < groups; ++g)
-            if (order_key(sh.group_max[g * kThreads + threadIdx.x]) >= low)
-                sh.hits[atomicAdd(&sh.hit_count, 1u)] = static_cast<uint16_t>(g * kThreads + threadIdx.x);
+        const uint32_t group_units = 4u << group_shift, span = group_units * kThreads;
+        // (the order of floats and of keys is the same from -inf up; below that, everything is a candidate)
+        const bool all = low <= 0x007FFFFFu;
+        const float low_value = value_of_key(low);
+        const uint32_t groups = (u1 - u0 + span - 1) / span;
+        uint32_t mine = 0;
+        for (uint32_t g = 0; g < groups; ++g) mine += all || sh.group_max[g * kThreads + threadIdx.x] >= low_value;
+        if (mine) {
+            uint32_t at = atomicAdd(&sh.hit_count, mine);
+            for (uint32_t g = 0; g < groups; ++g)
+                if (all || sh.group_max[g * kThreads + threadIdx.x] >= low_value)
+                    sh.hits[at++] = static_cast<uint16_t>(g * kThreads + threadIdx.x);
+        }
         __syncthreads();
-        const uint32_t in_group = per_group * 4, items = sh.hit_count * in_group;
-        for (uint32_t item = threadIdx.x; item < items; item += kThreads) {
-            const uint32_t hit = sh.hits[item / in_group];
-            const uint32_t u = u0 + (hit / kThreads * in_group + item % in_group) * kThreads + hit % kThreads;
-            if (u >= u1) continue;
-            const uint4 v = ld_unit(row.base + u);
-            if (low > 1 && order_key(Unit<T>::best(v, v, v, v)) < low) continue;
+        const uint32_t unit_shift = group_shift + 2, items = sh.hit_count << unit_shift;
+        for (uint32_t item0 = threadIdx.x; item0 < items; item0 += 2 * kThreads) {
+            uint4 v[2];
+            uint32_t us[2];
 #pragma unroll
-            for (uint32_t i = 0; i < E; ++i) {
-                const uint32_t col = row.column(u, i), key = order_key(Unit<T>::get(v, i));
-                if (key >= low && col < row.width) {
-                    const uint32_t at = atomicAdd(&sh.counter, 1u);
-                    if (at < kCandidates) sh.candidates[at] = entry(key, col);
+            for (uint32_t q = 0; q < 2; ++q) {
+                const uint32_t item = item0 + q * kThreads;
+                us[q] = 0xFFFFFFFFu;
+                if (item < items) {
+                    const uint32_t slot = sh.hits[item >> unit_shift];
+                    const uint32_t u = u0 + (slot / kThreads * group_units + (item & (group_units - 1))) * kThreads + slot % kThreads;
+                    if (u < u1) {
+                        us[q] = u;
+                        v[q] = ld_unit(row.base + u);
+                    }
                 }
+            }
+#pragma unroll
+            for (uint32_t q = 0; q < 2; ++q) {
+                if (us[q] == 0xFFFFFFFFu) continue;
+                uint32_t found = 0;
+#pragma unroll
+                for (uint32_t i = 0; i < E; ++i)
+                    found |= static_cast<uint32_t>(all ? order_key(Unit<T>::get(v[q], i)) >= low : Unit<T>::get(v[q], i) >= low_value) << i;
+                if (row.ragged && row.at_an_end(us[q])) {
+#pragma unroll
+                    for (uint32_t i = 0; i < E; ++i)
+                        if (row.column(us[q], i) >= row.width) found &= ~(1u << i);
+                }
+                if (!found) continue;
+                uint32_t at = atomicAdd(&sh.counter, static_cast<uint32_t>(__popc(found)));
+#pragma unroll
+                for (uint32_t i = 0; i < E; ++i)
+                    if (found >> i & 1u) {
+                        if (at < kCandidates) sh.candidates[at] = entry(order_key(Unit<T>::get(v[q], i)), row.column(us[q], i));
+                        ++at;
+                    }
             }
         }
         __syncthreads();
-        return sh.counter;
+        const uint32_t n = sh.counter;
+        __syncthreads();                       // (the counters may be set anew)
+        return n;
     }
     // the kk-th largest key of the slice, by halving the range of keys: 32 passes
-    __device__ uint32_t kth_key(uint32_t kk) {
+    __device__ __noinline__ static uint32_t kth_key(const Selector s, uint32_t kk) {
         uint32_t lo = 0, hi = 0xFFFFFFFFu;
         while (lo < hi) {
             const uint32_t mid = lo + (hi - lo) / 2 + 1;
             uint32_t n = 0;
-            for (uint32_t u = u0 + threadIdx.x; u < u1; u += kThreads)
-                each_element(u, [&](uint32_t key, uint32_t) { n += key >= mid; });
-            if (cta_count(n, sh.counts) >= kk) lo = mid;
+            for (uint32_t u = s.u0 + threadIdx.x; u < s.u1; u += kThreads)
+                s.each_element(u, [&](uint32_t key, uint32_t) { n += key >= mid; });
+            if (cta_count(n, s.sh.counts) >= kk) lo = mid;
             else hi = mid - 1;
         }
         return lo;
     }
     // appends the lowest columns whose key is `key` until there are kk candidates
-    __device__ void fill_with_equals(uint32_t key, uint32_t have, uint32_t kk) {
-        for (uint32_t first = u0; first < u1 && have < kk; first += kThreads) {
+    __device__ __noinline__ static void fill_with_equals(const Selector s, uint32_t key, uint32_t have, uint32_t kk) {
+        for (uint32_t first = s.u0; first < s.u1 && have < kk; first += kThreads) {
             const uint32_t u = first + threadIdx.x;
             uint32_t mine = 0;
-            if (u < u1) each_element(u, [&](uint32_t k, uint32_t) { mine += k == key; });
+            if (u < s.u1) s.each_element(u, [&](uint32_t k, uint32_t) { mine += k == key; });
             uint32_t before = mine;                         // inclusive sum over the lanes
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -123,17 +181,17 @@ template <typename T, uint32_t kThreads> struct Selector {
                 if (lane_id() >= static_cast<uint32_t>(o)) before += t;
             }
             __syncthreads();
-            if (lane_id() == 31) sh.counts[threadIdx.x >> 5] = before;
+            if (lane_id() == 31) s.sh.counts[threadIdx.x >> 5] = before;
             __syncthreads();
             uint32_t at = have + before - mine, all = 0;
             for (uint32_t w = 0; w < kThreads / 32; ++w) {
-                if (w < (threadIdx.x >> 5)) at += sh.counts[w];
-                all += sh.counts[w];
+                if (w < (threadIdx.x >> 5)) at += s.sh.counts[w];
+                all += s.sh.counts[w];
             }
-            if (u < u1 && mine)
-                each_element(u, [&](uint32_t k, uint32_t col) {
+            if (u < s.u1 && mine)
+                s.each_element(u, [&](uint32_t k, uint32_t col) {
                     if (k == key) {
-                        if (at < kk) sh.candidates[at] = entry(key, col);
+                        if (at < kk) s.sh.candidates[at] = entry(key, col);
                         ++at;
                     }
                 });
@@ -142,7 +200,7 @@ template <typename T, uint32_t kThreads> struct Selector {
         __syncthreads();
     }
     // keeps the kk best of n candidates, kk < n, in no order
-    __device__ void cut(uint32_t n, uint32_t kk) {
+    __device__ __noinline__ static void cut(LogProbShared<kThreads>& sh, uint32_t n, uint32_t kk) {
         uint64_t lo = 0, hi = ~0ull;
         while (lo < hi) {
             const uint64_t mid = lo + (hi - lo) / 2 + 1;
@@ -161,188 +219,235 @@ template <typename T, uint32_t kThreads> struct Selector {
         for (uint32_t i = threadIdx.x; i < kk; i += kThreads) sh.candidates[i] = sh.best[i];
         __syncthreads();
     }
-    // best[0 .. kk) := the slice's kk best columns in order.  thread_max: the largest element of this thread's batches.
-    __device__ void run(float thread_max, uint32_t kk) {
-        const uint32_t units = u1 - u0;
-        uint32_t bound = 0;
-        if (min(units, kThreads) >= kk) {
-            const uint32_t key = threadIdx.x < units ? order_key(thread_max) : 0u;
-            uint32_t lo = __reduce_min_sync(0xFFFFFFFFu, key), hi = __reduce_max_sync(0xFFFFFFFFu, key);
-            __syncthreads();
-            if (lane_id() == 0) {
-                sh.counts[threadIdx.x >> 5] = hi;
-                sh.slots[threadIdx.x >> 5] = __uint_as_float(lo);
-            }
-            __syncthreads();
-            for (uint32_t w = 0; w < kThreads / 32; ++w) {
-                hi = max(hi, sh.counts[w]);
-                lo = min(lo, __float_as_uint(sh.slots[w]));
-            }
-            // at least kk threads reach lo, fewer reach hi + 1; a few more than kk are as good as kk
-            while (lo < hi) {
-                const uint32_t mid = lo + (hi - lo) / 2 + 1;
-                const uint32_t c = __syncthreads_count(key >= mid);
-                if (c >= kk) lo = mid;
-                else hi = mid - 1;
-                if (c >= kk && c <= kk + kk / 4 + 2) break;
-            }
-            bound = lo;
+    // best[0 .. kk) := the kk best of n <= kRankable candidates in order.  Every warp sorts runs of 32 in its registers;
+    // an entry's place is its place in its run and, by bisection, how many of every other run are better.
+    __device__ __forceinline__ void in_order(uint32_t n, uint32_t kk) const {
+        const uint32_t runs = (n + 31) / 32, lane = lane_id();
+        for (uint32_t run = threadIdx.x >> 5; run < runs; run += kThreads / 32) {
+            uint64_t key = run * 32 + lane < n ? sh.candidates[run * 32 + lane] : 0ull;
+#pragma unroll
+            for (uint32_t size = 2; size <= 32; size *= 2)
+#pragma unroll
+                for (uint32_t step = size / 2; step > 0; step /= 2) {
+                    const uint64_t other = __shfl_xor_sync(0xFFFFFFFFu, key, step);
+                    const bool keep_larger = ((lane & step) == 0) == ((lane & size) == 0 || size == 32);
+                    key = (key > other) == keep_larger ? key : other;
+                }
+            sh.candidates[run * 32 + lane] = key;                 // (kCandidates is a multiple of 32)
         }
-        uint32_t n = collect(bound, false);
-        if (n < kk) {                          // threads whose only elements lie outside the row or are NaN
-            bound = 0;
-            n = collect(bound, false);
-        }
-        if (n > kCandidates) {                 // many equal to the bound, or sorted columns
-            n = collect(bound, true);
-            if (n > kCandidates) {
-                bound = kth_key(kk);
-                n = collect(bound, true);
-            }
-            if (n < kk) {
-                fill_with_equals(bound, n, kk);
-                n = kk;
-            }
-        }
-        if (n > kRankable) {
-            cut(n, kk);
-            n = kk;
-        }
+        __syncthreads();
         for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
             const uint64_t key = sh.candidates[i];
-            uint32_t rank = 0;
-            for (uint32_t q = 0; q < n; ++q) rank += sh.candidates[q] > key;
-            if (rank < kk) sh.best[rank] = key;
+            uint32_t place = i & 31u;
+            for (uint32_t run = 0; run < runs; ++run) {
+                if (run == i / 32) continue;
+                const uint64_t* list = sh.candidates + run * 32;
+                uint32_t better = 0;
+#pragma unroll
+                for (uint32_t step = 16; step > 0; step /= 2)
+                    if (list[better + step - 1] > key) better += step;
+                place += better + (list[better] > key);
+            }
+            if (place < kk) sh.best[place] = key;
         }
         __syncthreads();
     }
+    // best[0 .. kk) := the slice's kk best columns in order.  Every thread's largest element is in thread_max.
+    __device__ __forceinline__ void run(uint32_t kk) const {
+        if (threadIdx.x < 32) {
+            const uint32_t b = find_bound(kk);
+            if (threadIdx.x == 0) sh.bound = b;
+        }
+        __syncthreads();
+        uint32_t bound = sh.bound, low = bound, n;
+        bool above = false;                    // the candidates are the columns above the bound
+        for (;;) {
+            n = collect(low);
+            if (n < kk && !above && bound != 0) {        // threads whose only elements lie outside the row or are NaN
+                bound = low = 0;
+            } else if (n > kCandidates) {                // many equal to the bound, or sorted columns
+                if (above) bound = kth_key(*this, kk);
+                above = true;
+                low = bound + 1;                         // (0xFFFFFFFF is no element's key)
+            } else {
+                break;
+            }
+        }
+        if (n < kk) {
+            fill_with_equals(*this, bound, n, kk);
+            n = kk;
+        }
+        if (n > kRankable) {
+            cut(sh, n, kk);
+            n = kk;
+        }
+        in_order(n, kk);
+    }
 };
+
+// One thread: the row's m and log sum, and the results that are numbers per row.
+template <typename T>
+__device__ __forceinline__ void write_row(const LogProbArgs& a, uint32_t row_id, const T* xr, int32_t tok, const RowPart& all,
+                                          float& m_out, float& logsum_out) {
+    const float m = __fmul_rn(all.xmax, a.inv_t);
+    const bool empty = m == minus_inf() && all.s == all.s;
+    // (s belongs to the exact product xmax / T: the rounding of m goes into the logarithm)
+    const float log_s = logf(all.s), logsum = empty ? 0.0f : log_s + fmaf(all.xmax, a.inv_t, -m);
+    m_out = m;
+    logsum_out = logsum;
+    if (a.tokens) {
+        float lp = 0.0f;
+        if (tok >= 0 && static_cast<uint32_t>(tok) < a.vocab) {
+            lp = fmaf(to_f32(xr[tok]), a.inv_t, m == minus_inf() ? 0.0f : -m) - logsum;
+        } else if (tok >= 0 && a.result) {
+            atomicMax(&a.result->status, static_cast<uint32_t>(DCT_ERR_BAD_MASK));
+        }
+        a.logprob_out[row_id] = lp;
+    }
+    if (a.entropy_out) a.entropy_out[row_id] = empty ? 0.0f : fmaf(-kLn2, all.st / all.s, log_s);
+    if (a.stats_out) {
+        a.stats_out[2 * static_cast<size_t>(row_id)] = m;
+        a.stats_out[2 * static_cast<size_t>(row_id) + 1] = logsum;
+    }
+}
 
 // A cluster of CTAs takes a row, each CTA a slice of its units; the CTAs join their sums and their ordered best columns
 // through each other's shared memory.
 template <typename T, uint32_t kThreads, bool kCluster>
-__global__ void __launch_bounds__(kThreads, 1024 / kThreads)
+__global__ void __launch_bounds__(kThreads, kThreads == 128 ? 7 : 1024 / kThreads)
 lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
+    constexpr uint32_t kWarps = kThreads / 32;
     __shared__ LogProbShared<kThreads> sh;
-    const uint32_t tid = threadIdx.x;
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = lane_id();
     const uint32_t rank = kCluster ? cluster_rank() : 0u, ctas = kCluster ? cluster_size() : 1u;
     const uint32_t clusters = gridDim.x / ctas;
-    for (uint32_t row_id = blockIdx.x / ctas; row_id < a.rows; row_id += clusters) {
+    uint32_t turn = 0;
+    for (uint32_t row_id = blockIdx.x / ctas;; turn ^= 1) {
         const T* xr = logits + static_cast<size_t>(row_id) * a.ld;
         const RowView<T> row(xr, a.vocab);
-        const uint32_t share = (row.units + ctas - 1) / ctas;
-        const uint32_t u0 = min(row.units, rank * share), u1 = min(row.units, u0 + share);
+        const Slice slice(row.units, rank, ctas);
+        const uint32_t u0 = slice.u0, u1 = slice.u1;
+        // what the row's token is like, for the thread that will write its log-probability
         int32_t tok = -1;
-        float x_tok = 0.0f;
-        if (tid == 0 && rank == 0 && a.tokens) {
-            tok = a.tokens[row_id];
-            if (tok >= 0 && static_cast<uint32_t>(tok) < a.vocab) x_tok = to_f32(xr[tok]);
-        }
+        if (a.tokens && tid == kThreads - 32) tok = a.tokens[row_id];
 
         // one pass: sums, and the largest element of every batch of four units
         RowSums sums;
-        const uint32_t batches = (u1 - u0 + 4 * kThreads - 1) / (4 * kThreads);
-        const uint32_t per_group = max(1u, (batches + sh.kGroups - 1) / sh.kGroups);
+        uint32_t group_shift = 0;
+        while ((u1 - u0 + (4 * kThreads << group_shift) - 1) / (4 * kThreads << group_shift) > sh.kGroups) ++group_shift;
         float thread_max = minus_inf(), group_max = minus_inf();
-        uint32_t in_group = 0, group = 0;
-        for (uint32_t b = 0; b < batches; ++b) {
-            const uint32_t first = u0 + b * 4 * kThreads + tid;
-            uint4 v[4];
-            load_batch<T, kThreads>(v, row, first, u1);
-            mask_batch<T, kThreads>(v, row, first, u1);
-            const float best = Unit<T>::best(v[0], v[1], v[2], v[3]);
-            sums.add<T, true>(v, best, a.inv_t);
+        uint32_t in_group = 1u << group_shift, slot = tid;
+        stream_units<T, kThreads>(row, u0, u1, [&](const uint4 (&v)[4], float best) {
+            sums.add<T, true>(v, best, a.c);
             group_max = fmaxf(group_max, best);
-            if (++in_group == per_group || b + 1 == batches) {
-                sh.group_max[group * kThreads + tid] = group_max;
+            sh.group_max[slot] = group_max;                      // (written again until the group is complete)
+            if (--in_group == 0) {
                 thread_max = fmaxf(thread_max, group_max);
                 group_max = minus_inf();
-                in_group = 0;
-                ++group;
+                in_group = 1u << group_shift;
+                slot += kThreads;
+            }
+        });
+        thread_max = fmaxf(thread_max, group_max);
+        if (a.top) sh.thread_max[tid] = thread_max;
+        const RowPart mine = sums.part(warp_max(thread_max), a.c);
+        if (lane == 0) sh.warp_part[turn][warp] = mine;
+        __syncthreads();
+
+        // the last warp joins the slice's sums (and writes the results of a row that is one slice); the first meanwhile looks
+        // for the bound of the selection
+        if (warp == kWarps - 1) {
+            RowPart all = sh.warp_part[turn][lane & (kWarps - 1)];
+            all.join_lanes(a.c, kWarps);
+            if (all.s == 0.0f && all.xmax > minus_inf()) {
+                // values so low that x c overflows: once more, slowly, from differences
+                RowPart p{all.xmax, 0.0f, 0.0f};
+                for (uint32_t u = u0 + lane; u < u1; u += 32) {
+                    const uint4 v = ld_unit(row.base + u);
+                    for (uint32_t i = 0; i < Unit<T>::kElems; ++i)
+                        if (row.column(u, i) < row.width) {
+                            const float y = __fmul_rn(__fadd_rn(Unit<T>::get(v, i), -all.xmax), a.c), e = exp2_fast(y);
+                            p.s = __fadd_rn(p.s, e);
+                            if (e != 0.0f) p.st = fmaf(e, y, p.st);
+                        }
+                }
+                p.join_lanes(a.c, 32);
+                all = p;
+            }
+            if (lane == 0) {
+                sh.part = all;
+                if (!kCluster) write_row(a, row_id, xr, tok, all, sh.m, sh.logsum);
             }
         }
-        // the slice's sums, relative to its largest z
-        sums.join_cta(__fmul_rn(thread_max, a.inv_t), sh.slots);
-        float m = sums.ref, s = sums.s, st = sums.st;
-
         uint32_t kept = 0;
         if (a.top) {
             const uint32_t columns = u1 == u0 ? 0u
                 : min(a.vocab, u1 * Unit<T>::kElems - row.lead) - (u0 == 0 ? 0u : u0 * Unit<T>::kElems - row.lead);
             kept = min(a.top, columns);
-            if (kept) Selector<T, kThreads>{row, u0, u1, per_group, sh}.run(thread_max, kept);
+            if (kept) Selector<T, kThreads>{row, u0, u1, group_shift, sh}.run(kept);
         }
 
         if (kCluster) {
-            if (tid == 0) sh.part = SlicePart{m, s, st, kept};
+            if (tid == 0) sh.kept = kept;
             cluster_barrier();
-            float all_m = minus_inf();
-            for (uint32_t c = 0; c < ctas; ++c) all_m = fmaxf(all_m, ld_remote_f32(remote_smem(&sh.part.m, c)));
-            s = st = 0.0f;
-            for (uint32_t c = 0; c < ctas; ++c) {
-                RowSums other;
-                other.ref = ld_remote_f32(remote_smem(&sh.part.m, c));
-                other.s = ld_remote_f32(remote_smem(&sh.part.s, c));
-                other.st = ld_remote_f32(remote_smem(&sh.part.st, c));
-                other.finish(all_m);
-                s = __fadd_rn(s, other.s);
-                st = __fadd_rn(st, other.st);
+            if (warp == kWarps - 1) {
+                RowPart all{minus_inf(), 0.0f, 0.0f};
+                if (lane < ctas) {
+                    all.xmax = ld_remote_f32(remote_smem(&sh.part.xmax, lane));
+                    all.s = ld_remote_f32(remote_smem(&sh.part.s, lane));
+                    all.st = ld_remote_f32(remote_smem(&sh.part.st, lane));
+                }
+                all.join_lanes(a.c, kMaxCluster);
+                if (lane == 0) {
+                    if (rank == 0) {
+                        write_row(a, row_id, xr, tok, all, sh.m, sh.logsum);
+                    } else {
+                        LogProbArgs quiet = a;
+                        quiet.tokens = nullptr;
+                        quiet.entropy_out = quiet.stats_out = nullptr;
+                        write_row(quiet, row_id, xr, tok, all, sh.m, sh.logsum);
+                    }
+                }
             }
-            m = all_m;
-        }
-        const bool empty = m == minus_inf() && s == 0.0f;
-        const float ref = m == minus_inf() ? 0.0f : m;
-        const float logsum = empty ? 0.0f : logf(s);
-        if (tid == 0 && rank == 0) {
-            if (a.tokens) {
-                const bool inside = tok >= 0 && static_cast<uint32_t>(tok) < a.vocab;
-                a.logprob_out[row_id] = inside ? fmaf(x_tok, a.inv_t, -ref) - logsum : 0.0f;
-                if (tok >= 0 && !inside && a.result) atomicMax(&a.result->status, static_cast<uint32_t>(DCT_ERR_BAD_MASK));
-            }
-            if (a.entropy_out) a.entropy_out[row_id] = empty ? 0.0f : logsum - st / s;
-            if (a.stats_out) {
-                a.stats_out[2 * static_cast<size_t>(row_id)] = m;
-                a.stats_out[2 * static_cast<size_t>(row_id) + 1] = logsum;
-            }
-        }
-        if (a.top) {
-            // a column's place: its place in its own slice's list, and how many of each other list are better
-            uint32_t starts = 0;
-            if (kCluster) {
+            if (a.top) {
                 for (uint32_t c = 0; c < ctas; ++c) {
-                    const uint32_t n = ld_remote_u32(remote_smem(&sh.part.kept, c));
+                    const uint32_t n = ld_remote_u32(remote_smem(&sh.kept, c));
                     for (uint32_t i = tid; i < n; i += kThreads)
                         sh.candidates[c * DCT_LM_MAX_TOP + i] = ld_remote_u64(remote_smem(&sh.best[i], c));
                     if (tid == 0) sh.counts[c] = n;
-                    starts += n;
                 }
                 __syncthreads();
             }
-            for (uint32_t i = tid; i < kept; i += kThreads) {
-                const uint64_t key = sh.best[i];
-                uint32_t place = i;
-                if (kCluster) {
-                    for (uint32_t c = 0; c < ctas; ++c) {
-                        if (c == rank) continue;
-                        const uint64_t* list = sh.candidates + c * DCT_LM_MAX_TOP;
-                        uint32_t lo = 0, hi = sh.counts[c];         // list[0 .. lo) are better
-                        while (lo < hi) {
-                            const uint32_t mid = (lo + hi) / 2;
-                            if (list[mid] > key) lo = mid + 1;
-                            else hi = mid;
-                        }
-                        place += lo;
+        }
+        // a column's place: its place in its own slice's list, and how many of each other list are better
+        for (uint32_t i = tid; i < kept; i += kThreads) {
+            const uint64_t key = sh.best[i];
+            uint32_t place = i;
+            if (kCluster) {
+                for (uint32_t c = 0; c < ctas; ++c) {
+                    if (c == rank) continue;
+                    const uint64_t* list = sh.candidates + c * DCT_LM_MAX_TOP;
+                    uint32_t lo = 0, hi = sh.counts[c];         // list[0 .. lo) are better
+                    while (lo < hi) {
+                        const uint32_t mid = (lo + hi) / 2;
+                        if (list[mid] > key) lo = mid + 1;
+                        else hi = mid;
                     }
-                }
-                if (place < a.top) {
-                    const size_t at = static_cast<size_t>(row_id) * a.top + place;
-                    a.top_ids[at] = static_cast<int32_t>(0xFFFFFFFFu - static_cast<uint32_t>(key));
-                    a.top_logprobs[at] = fmaf(value_of_key(static_cast<uint32_t>(key >> 32)), a.inv_t, -ref) - logsum;
+                    place += lo;
                 }
             }
+            if (place < a.top) {
+                const size_t at = static_cast<size_t>(row_id) * a.top + place;
+                a.top_ids[at] = static_cast<int32_t>(0xFFFFFFFFu - static_cast<uint32_t>(key));
+                a.top_logprobs[at] = fmaf(value_of_key(static_cast<uint32_t>(key >> 32)), a.inv_t,
+                                          sh.m == minus_inf() ? 0.0f : -sh.m) - sh.logsum;
+            }
         }
-        if (kCluster) cluster_barrier();          // nobody reads this CTA's shared memory any more
-        else __syncthreads();
+        // Nobody may read this CTA's shared memory any more when its next row begins.  (A CTA on its own needs no barrier
+        // here: the warps' parts alternate, and what else the next row writes it writes behind its first barrier.)
+        if (kCluster) cluster_barrier();
+        if (a.rows - row_id <= clusters) break;
+        row_id += clusters;
     }
 }
 
@@ -411,13 +516,17 @@ lm_logprobs_bwd_kernel(const T* logits, T* grad, const LogProbBwdArgs q) {
 }
 
 template <typename T, uint32_t kThreads>
-dct_status_t launch_logprobs_threads(const void* logits, const LogProbArgs& a, uint32_t cluster, cudaStream_t stream) {
+dct_status_t launch_logprobs_threads(const void* logits, const LogProbArgs& a, uint32_t cluster, uint32_t ctas, cudaStream_t stream) {
     const T* x = static_cast<const T*>(logits);
-    const uint32_t clusters = a.rows < (1u << 20) ? a.rows : 1u << 20;
-    if (cluster == 1)
-        lm_logprobs_kernel<T, kThreads, false><<<clusters, kThreads, 0, stream>>>(x, a);
-    else
-        DCT_CUDA_TRY(launch_clusters(lm_logprobs_kernel<T, kThreads, true>, clusters * cluster, kThreads, cluster, 0, stream, x, a));
+    const uint64_t wanted = static_cast<uint64_t>(a.rows) * cluster, room = ctas / cluster * cluster;
+    const uint32_t grid = static_cast<uint32_t>(wanted < room ? wanted : room);
+    if constexpr (kThreads > 128) {
+        if (cluster > 1) {
+            DCT_CUDA_TRY(launch_clusters(lm_logprobs_kernel<T, kThreads, true>, grid, kThreads, cluster, 0, stream, x, a));
+            return DCT_OK;
+        }
+    }
+    lm_logprobs_kernel<T, kThreads, false><<<grid, kThreads, 0, stream>>>(x, a);
     DCT_CUDA_TRY(cudaGetLastError());
     return DCT_OK;
 }
@@ -426,13 +535,23 @@ template <typename T> dct_status_t launch_logprobs(const void* logits, const Log
     const int sms = sm_count();
     if (sms <= 0) return DCT_ERR_CUDA;
     const uint32_t units = (a.vocab + Unit<T>::kElems - 1) / Unit<T>::kElems;
-    // a row goes to as many CTAs as it takes to give every SM two, while each still has a batch of four units per thread
+    const uint32_t threads = a.top > 128 ? 512 : a.top <= 64 && (units <= 1024 || a.rows >= 4u * sms) ? 128 : 256;
+    const uint32_t ctas = static_cast<uint32_t>(sms) * (threads == 128 ? 7 : 1024 / threads);
+    // A row goes to 1, 2, 4 or 8 CTAs: the number of rounds the CTAs on the chip need, times the units of a CTA's slice
+    // and about two batches' worth of work at its end.
     uint32_t cluster = 1;
-    while (cluster < kMaxCluster && static_cast<uint64_t>(a.rows) * cluster * 2 <= static_cast<uint64_t>(sms) * 2 &&
-           units / (cluster * 2) >= 1024)
-        cluster *= 2;
-    if (a.top > 128) return launch_logprobs_threads<T, 512>(logits, a, cluster, stream);
-    return launch_logprobs_threads<T, 256>(logits, a, cluster, stream);
+    uint64_t best = ~0ull;
+    for (uint32_t c = 1; c <= kMaxCluster && (c == 1 || (threads > 128 && units / c >= 512)); c *= 2) {
+        const uint64_t rounds = (static_cast<uint64_t>(a.rows) * c + ctas - 1) / ctas;
+        const uint64_t cost = rounds * (units / c + 2048);
+        if (cost < best) {
+            best = cost;
+            cluster = c;
+        }
+    }
+    if (threads == 512) return launch_logprobs_threads<T, 512>(logits, a, cluster, ctas, stream);
+    if (threads == 256) return launch_logprobs_threads<T, 256>(logits, a, cluster, ctas, stream);
+    return launch_logprobs_threads<T, 128>(logits, a, 1, ctas, stream);
 }
 
 bool refused_logits(const void* logits, dct_dtype_t dtype, uint32_t vocab, uint32_t ld, float inv_t) {
@@ -462,7 +581,7 @@ extern "C" dct_status_t dct_lm_logprobs_fwd(const void* logits, dct_dtype_t dtyp
     }
     if (result) DCT_CUDA_TRY(cudaMemsetAsync(result, 0, sizeof(dct_result_t), stream));
     if (rows == 0) return DCT_OK;
-    const LogProbArgs args{rows, vocab, ld, inv_temperature, tokens, top, logprob_out, entropy_out, stats_out, top_ids, top_logprobs, result};
+    const LogProbArgs args{rows, vocab, ld, inv_temperature, log2_scale(inv_temperature), tokens, top, logprob_out, entropy_out, stats_out, top_ids, top_logprobs, result};
     return dtype == DCT_F32 ? launch_logprobs<float>(logits, args, stream) : launch_logprobs<__nv_bfloat16>(logits, args, stream);
 }
 

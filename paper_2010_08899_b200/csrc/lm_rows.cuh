@@ -63,7 +63,7 @@ __device__ __forceinline__ uint32_t cta_count(uint32_t v, uint32_t* scratch) {
 // (the unit lies in the same page, so the elements outside the row are readable), and what lies outside the row
 // is replaced before it is used.
 
-constexpr float kLog2E = 1.4426950408889634f;
+constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_fast(float x) {            // 2^x within 2 ulp; results below 2^-126 are 0
     float y;
@@ -108,13 +108,10 @@ template <> struct Unit<float> {
         if (i == 0) v.x = u; else if (i == 1) v.y = u; else if (i == 2) v.z = u; else v.w = u;
     }
     // the largest element, NaN only if all are
-    __device__ static __forceinline__ float best(const uint4& a, const uint4& b, const uint4& c, const uint4& d) {
-        const float p = fmaxf(fmaxf(fmaxf(get(a, 0), get(a, 1)), fmaxf(get(a, 2), get(a, 3))),
-                              fmaxf(fmaxf(get(b, 0), get(b, 1)), fmaxf(get(b, 2), get(b, 3))));
-        const float q = fmaxf(fmaxf(fmaxf(get(c, 0), get(c, 1)), fmaxf(get(c, 2), get(c, 3))),
-                              fmaxf(fmaxf(get(d, 0), get(d, 1)), fmaxf(get(d, 2), get(d, 3))));
-        return fmaxf(p, q);
+    __device__ static __forceinline__ float best(const uint4& a) {
+        return fmaxf(fmaxf(get(a, 0), get(a, 1)), fmaxf(get(a, 2), get(a, 3)));
     }
+    __device__ static __forceinline__ float best(const uint4& a, const uint4& b) { return fmaxf(best(a), best(b)); }
 };
 template <> struct Unit<__nv_bfloat16> {
     static constexpr int kElems = 8;
@@ -133,6 +130,10 @@ template <> struct Unit<__nv_bfloat16> {
     __device__ static __forceinline__ __nv_bfloat162 pair(uint32_t w) { return *reinterpret_cast<__nv_bfloat162*>(&w); }
     __device__ static __forceinline__ __nv_bfloat162 best2(const uint4& v) {
         return __hmax2(__hmax2(pair(v.x), pair(v.y)), __hmax2(pair(v.z), pair(v.w)));
+    }
+    __device__ static __forceinline__ float best(const uint4& a) {
+        const __nv_bfloat162 m = best2(a);
+        return fmaxf(__low2float(m), __high2float(m));
     }
     __device__ static __forceinline__ float best(const uint4& a, const uint4& b, const uint4& c, const uint4& d) {
         const __nv_bfloat162 m = __hmax2(__hmax2(best2(a), best2(b)), __hmax2(best2(c), best2(d)));
@@ -161,12 +162,16 @@ template <typename T> struct RowView {
     uint32_t lead;           // elements of the first unit that lie before the row
     uint32_t units;
     uint32_t width;          // elements of the row
+    bool ragged;             // a unit at an end holds elements outside the row
 
-    __device__ __forceinline__ RowView(const T* row, uint32_t width_) : width(width_) {
+    __device__ __forceinline__ RowView(const T* row, uint32_t width_) { at(row, width_); }
+    __device__ __forceinline__ void at(const T* row, uint32_t width_) {
+        width = width_;
         const uintptr_t a = reinterpret_cast<uintptr_t>(row);
         lead = static_cast<uint32_t>(a & 15u) / static_cast<uint32_t>(sizeof(T));
         base = reinterpret_cast<const uint4*>(a & ~static_cast<uintptr_t>(15));
         units = (lead + width + kElems - 1) / kElems;
+        ragged = lead != 0 || width % kElems != 0;
     }
     // column of element i of unit u; >= width (as unsigned) outside the row
     __device__ __forceinline__ uint32_t column(uint32_t u, uint32_t i) const { return u * kElems + i - lead; }
@@ -212,30 +217,64 @@ inline __device__ bool same_boundary(const void* a, const void* b) {      // ali
     return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
 }
 
-// One thread's share of sum exp(z - ref) and sum exp(z - ref) (z - ref) over a row, z = x inv_t, with a reference of
-// its own that is at most kSlack below the largest z so far: the sums are rescaled only when a batch exceeds it by more.
-// z - ref is formed exactly but for one rounding (a product with log2 e folded into the logits would lose the digits
-// in which large logits differ), so log p of any column is (z - m) - log sum to fp32 accuracy.
-struct RowSums {
-    static constexpr float kSlack = 2.0f;
-    float ref, s, st;
-    __device__ __forceinline__ RowSums() : ref(minus_inf()), s(0.0f), st(0.0f) {}
+__device__ __forceinline__ float warp_max(float v) {               // NaN only if every lane's is
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(r) : "f"(v));
+    return r;
+}
 
-    __device__ __forceinline__ void rebase(float to) {
-        if (ref != minus_inf()) {
-            // (a reference of the type's lowest value is too far off for s * d; from -1e4 on f is 0 all the same)
-            const float d = max_nan(__fadd_rn(ref, -to), -1.0e4f), f = exp2_fast(__fmul_rn(d, kLog2E));
+// What is known of a part of a row: its largest x, and relative to that the sums s = sum 2^y and st = sum 2^y y with
+// y = (x - xmax) c, c = inv_t log2 e.  st / s is the mean of log2 p + log2 s.  An empty part has xmax = -inf, s = 0.
+struct RowPart {
+    float xmax, s, st;
+    // the same sums relative to a larger x
+    __device__ __forceinline__ void raise(float to, float c) {
+        if (s == 0.0f) {
+            st = 0.0f;
+        } else {
+            // (the type's lowest values are too far off for s * d; from -1e4 on the factor is 0 all the same)
+            const float d = xmax == to ? 0.0f : max_nan(__fmul_rn(__fadd_rn(xmax, -to), c), -1.0e4f), f = exp2_fast(d);
             st = __fmul_rn(f, fmaf(s, d, st));
             s = __fmul_rn(f, s);
         }
-        ref = to;
+        xmax = to;
     }
-    // best: the batch's largest element
-    template <typename T, bool kMoment> __device__ __forceinline__ void add(const uint4 (&v)[4], float best, float inv_t) {
+    // joins the parts of `lanes` (a power of two) neighbouring lanes, in a fixed order; all lanes get the result
+    __device__ __forceinline__ void join_lanes(float c, int lanes) {
+        float m = xmax;
+        for (int o = lanes / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        raise(m, c);
+        for (int o = lanes / 2; o > 0; o >>= 1) {
+            s = __fadd_rn(s, __shfl_xor_sync(0xFFFFFFFFu, s, o));
+            st = __fadd_rn(st, __shfl_xor_sync(0xFFFFFFFFu, st, o));
+        }
+    }
+};
+
+// One thread's share of sum 2^y and sum 2^y y over a row, y = x c - ref.  The reference is the warp's: the largest x c of its
+// first batch, replaced only when a batch exceeds it by kSlack, so that an element costs one product-sum, one power of
+// two and two sums.  Rounding c and ref moves nothing but the reference: what counts is (x - xmax) c, and the
+// distance of xmax c to ref is formed by one fma at the end.
+struct RowSums {
+    static constexpr float kSlack = 4.0f;
+    float ref, s, st;
+    __device__ __forceinline__ RowSums() : ref(minus_inf()), s(0.0f), st(0.0f) {}
+
+    // best: the largest of this thread's four units; all lanes of the warp take part
+    template <typename T, bool kMoment> __device__ __forceinline__ void add(const uint4 (&v)[4], float best, float c) {
         constexpr int E = Unit<T>::kElems;
-        const float zb = __fmul_rn(best, inv_t);
-        if (!(zb <= __fadd_rn(ref, kSlack)) && zb > minus_inf()) rebase(zb);
-        if (ref == minus_inf()) {        // nothing but -inf and NaN so far
+        if (__any_sync(0xFFFFFFFFu, !(__fmul_rn(best, c) <= __fadd_rn(ref, kSlack)))) {
+            const float to = __fmul_rn(warp_max(best), c);
+            if (to > ref) {
+                if (ref != minus_inf()) {
+                    const float d = max_nan(__fadd_rn(ref, -to), -1.0e4f), f = exp2_fast(d);
+                    st = __fmul_rn(f, fmaf(s, d, st));
+                    s = __fmul_rn(f, s);
+                }
+                ref = to;
+            }
+        }
+        if (ref == minus_inf()) {        // nothing but -inf and NaN so far (or values whose product with c overflows)
             float any = 0.0f;
 #pragma unroll
             for (int u = 0; u < 4; ++u)
@@ -244,98 +283,90 @@ struct RowSums {
             if (any != any) s = any;
             return;
         }
-        const uint64_t t_scale = pack2(inv_t, inv_t), shift = pack2(-ref, -ref), to_log2 = pack2(kLog2E, kLog2E);
+        const uint64_t scale = pack2(c, c), shift = pack2(-ref, -ref);
         uint64_t sb = 0, stb = 0;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int i = 0; i < E; i += 2) {
-                const uint64_t t = fma2(pack2(Unit<T>::get(v[u], i), Unit<T>::get(v[u], i + 1)), t_scale, shift);
+                const uint64_t y = fma2(pack2(Unit<T>::get(v[u], i), Unit<T>::get(v[u], i + 1)), scale, shift);
                 float y0, y1;
-                unpack2(mul2(t, to_log2), y0, y1);
+                unpack2(y, y0, y1);
                 const uint64_t e = pack2(exp2_fast(y0), exp2_fast(y1));
                 sb = add2(sb, e);
-                if (kMoment) stb = fma2(e, t, stb);
+                if (kMoment) stb = fma2(e, y, stb);
             }
-        float a, b;
-        unpack2(sb, a, b);
-        s = __fadd_rn(s, __fadd_rn(a, b));
+        float p, q;
+        unpack2(sb, p, q);
+        s = __fadd_rn(s, __fadd_rn(p, q));
         if (kMoment) {
-            unpack2(stb, a, b);
-            float sum = __fadd_rn(a, b);
+            unpack2(stb, p, q);
+            float sum = __fadd_rn(p, q);
             if (sum != sum) {            // 0 * -inf at masked columns: leave those out
                 sum = 0.0f;
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
 #pragma unroll
                     for (int i = 0; i < E; ++i) {
-                        const float t = fmaf(Unit<T>::get(v[u], i), inv_t, -ref);
-                        const float e = exp2_fast(__fmul_rn(t, kLog2E));
-                        if (e != 0.0f) sum = fmaf(e, t, sum);
+                        const float y = fmaf(Unit<T>::get(v[u], i), c, -ref), e = exp2_fast(y);
+                        if (e != 0.0f) sum = fmaf(e, y, sum);
                     }
             }
             st = __fadd_rn(st, sum);
         }
     }
-    // the same sums relative to m (the largest z of whatever is joined; -inf if that is all there is)
-    __device__ __forceinline__ void finish(float m) {
-        if (s == 0.0f) st = 0.0f;
-        else rebase(m);
-        ref = m;
-    }
-    // joins `lanes` (a power of two) neighbouring lanes: all get the sums of all; the order is fixed
-    __device__ __forceinline__ void join_lanes(float m, int lanes) {
-        for (int o = lanes / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-        finish(m);
-        for (int o = lanes / 2; o > 0; o >>= 1) {
-            s = __fadd_rn(s, __shfl_xor_sync(0xFFFFFFFFu, s, o));
-            st = __fadd_rn(st, __shfl_xor_sync(0xFFFFFFFFu, st, o));
+    // the warp's sums as a part; xmax: the warp's largest x
+    __device__ __forceinline__ RowPart part(float xmax, float c) const {
+        RowPart r{xmax, warp_join<SumOp>(s), warp_join<SumOp>(st)};
+        if (ref != minus_inf()) {
+            // |xmax c - ref| <= kSlack; the factor puts the sums where 2^y of the largest x is 1
+            const float d = fmaf(xmax, c, -ref), f = exp2_fast(-d);
+            r.st = __fmul_rn(f, fmaf(-d, r.s, r.st));
+            r.s = __fmul_rn(f, r.s);
         }
-    }
-    // joins the CTA's threads with one barrier.  m: the largest z this thread has met.  slots: 3 x 32 floats that nothing
-    // else uses before the next barrier.
-    __device__ __forceinline__ void join_cta(float m, float* slots) {
-        join_lanes(m, 32);
-        const uint32_t warps = blockDim.x >> 5, lane = lane_id();
-        if (lane == 0) {
-            slots[threadIdx.x >> 5] = ref;
-            slots[32 + (threadIdx.x >> 5)] = s;
-            slots[64 + (threadIdx.x >> 5)] = st;
-        }
-        __syncthreads();
-        const uint32_t w = lane & (warps - 1);                 // (warps is a power of two)
-        ref = slots[w];
-        s = slots[32 + w];
-        st = slots[64 + w];
-        join_lanes(ref, static_cast<int>(warps));
+        return r;
     }
 };
 
-// A thread's units first, first + kThreads, ... of a slice that ends at u1: loaded without looking at bounds where all
-// threads' units lie inside, -inf beyond the slice; and the row's ends masked in the batches that can hold them.
-template <typename T, uint32_t kThreads>
-__device__ __forceinline__ void load_batch(uint4 (&v)[4], const RowView<T>& row, uint32_t first, uint32_t u1) {
-    if (first - threadIdx.x + 4 * kThreads <= u1) {            // the same for the whole CTA
-        const uint4* p = row.base + first;
+// Streams the units [u0, u1) of a row through the CTA, in batches of four units per thread (first + tid + i kThreads).
+// each(v, best) takes the four units, -inf where there is no element, and their largest element.
+template <typename T, uint32_t kThreads, typename Each>
+__device__ __forceinline__ void stream_units(const RowView<T>& row, uint32_t u0, uint32_t u1, Each&& each) {
+    constexpr uint32_t kInf = Unit<T>::kMinusInf;
+    for (uint32_t batch = u0; batch < u1; batch += 4 * kThreads) {
+        const uint32_t first = batch + threadIdx.x;
+        uint4 v[4];
+        if (batch + 4 * kThreads <= u1) {                  // the same for the whole CTA: no bounds to look at
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = ld_unit(p + i * kThreads);
-    } else {
+            for (int i = 0; i < 4; ++i) v[i] = ld_unit(row.base + first + i * kThreads);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] = make_uint4(Unit<T>::kMinusInf, Unit<T>::kMinusInf, Unit<T>::kMinusInf, Unit<T>::kMinusInf);
-            if (first + i * kThreads < u1) v[i] = ld_unit(row.base + first + i * kThreads);
+            for (int i = 0; i < 4; ++i) {
+                v[i] = make_uint4(kInf, kInf, kInf, kInf);
+                if (first + i * kThreads < u1) v[i] = ld_unit(row.base + first + i * kThreads);
+            }
         }
-    }
-}
-template <typename T, uint32_t kThreads>
-__device__ __forceinline__ void mask_batch(uint4 (&v)[4], const RowView<T>& row, uint32_t first, uint32_t u1) {
-    const uint32_t batch = first - threadIdx.x;
-    if (batch == 0 || batch + 4 * kThreads >= row.units) {     // the same for the whole CTA
+        if (row.ragged && (batch == 0 || batch + 4 * kThreads >= row.units)) {      // can hold an end of the row
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (first + i * kThreads < u1) row.mask(v[i], first + i * kThreads);
+            for (int i = 0; i < 4; ++i)
+                if (first + i * kThreads < u1) row.mask(v[i], first + i * kThreads);
+        }
+        float best;
+        if constexpr (sizeof(T) == 4) best = fmaxf(Unit<T>::best(v[0], v[1]), Unit<T>::best(v[2], v[3]));
+        else best = Unit<T>::best(v[0], v[1], v[2], v[3]);
+        each(v, best);
     }
 }
+
+// The units of one row that one of `ctas` CTAs takes.
+struct Slice {
+    uint32_t u0, u1;
+    __device__ __forceinline__ Slice(uint32_t units, uint32_t rank, uint32_t ctas) {
+        const uint32_t share = (units + ctas - 1) / ctas;
+        u0 = min(units, rank * share);
+        u1 = min(units, u0 + share);
+    }
+};
 
 // Clusters of CTAs -------------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -411,6 +442,7 @@ inline bool in_place_or_apart(const void* in, uint32_t ld_in, const void* out, u
     return (in == out && ld_in == ld_out) ||
            !spans_overlap(in, span_bytes(rows, d, ld_in, es), out, span_bytes(rows, d, ld_out, es));
 }
+inline float log2_scale(float inv_t) { return static_cast<float>(1.4426950408889634 * inv_t); }
 inline bool usable_temperature(float inv_t) { return std::isfinite(inv_t) && inv_t > 0.0f; }
 
 }  // namespace dct
