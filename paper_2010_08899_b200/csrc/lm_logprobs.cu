@@ -20,12 +20,12 @@ struct LogProbArgs {
 
 template <uint32_t kThreads> struct LogProbShared {
     static constexpr uint32_t kWarps = kThreads / 32;
-    static constexpr uint32_t kGroups = kThreads > 256 ? 8 : 16;                   // maxima a thread notes
+    static constexpr uint32_t kGroups = 16;                                        // maxima a thread notes
     static constexpr uint32_t kCandidates = kThreads > 128 ? 2048 : 1024;          // columns the selection holds
     float group_max[kGroups * kThreads];
     uint64_t candidates[kCandidates];
     uint64_t best[DCT_LM_MAX_TOP];
-    float thread_max[kThreads];
+    float class_max[2 * kThreads];
     uint16_t hits[kGroups * kThreads];
     RowPart warp_part[2][kWarps];      // by turns, row by row
     RowPart part;                      // this CTA's slice
@@ -39,16 +39,17 @@ __device__ __forceinline__ float value_of_key(uint32_t key) {       // the inver
 }
 
 // The selection of a slice's best columns.  A column is (order key << 32 | ~column): larger is better, all distinct.
-// While the row streams by, every thread notes the largest element of each batch of units it reads.  The kk-th
-// largest of the threads' own maxima is a bound that at least kk columns reach and, for kk well below the number of
-// threads, not many more do (T ln(T / (T - kk)) for columns in no particular order); only batches whose noted maximum reaches it
-// are read again, and of them the elements that reach it are put in order.
+// While the row streams by, every thread notes the largest element of each pair of units it reads, and that of all its first
+// and all its second pairs.  The kk-th largest of these N = 2 kThreads class maxima is a bound that at least kk columns
+// reach and, for kk well below N, not many more do (N ln(N / (N - kk)) for columns in no particular order: 74 for 64 of
+// 256); only pairs of units whose noted maximum reaches it are read again, and of them the elements that reach it are put
+// in order.
 template <typename T, uint32_t kThreads> struct Selector {
     static constexpr uint32_t E = Unit<T>::kElems;
     static constexpr uint32_t kCandidates = LogProbShared<kThreads>::kCandidates;
     RowView<T> row;
     uint32_t u0, u1;                // the slice's units
-    uint32_t group_shift;           // log2 of the batches per noted maximum
+    uint32_t group_shift;           // log2 of the pairs of units per noted maximum
     LogProbShared<kThreads>& sh;
 
     template <typename F> __device__ __forceinline__ void each_element(uint32_t u, F&& f) const {
@@ -62,23 +63,24 @@ template <typename T, uint32_t kThreads> struct Selector {
     __device__ __forceinline__ static uint64_t entry(uint32_t key, uint32_t col) {
         return static_cast<uint64_t>(key) << 32 | (0xFFFFFFFFu - col);
     }
-    // By one warp, from the threads' maxima: a key that at least kk of them reach, and not many more if that can be had
-    // (0 if fewer than kk threads have a unit).
+    // By one warp, from the class maxima: a key that at least kk of them reach, and not many more if that can be had
+    // (0 if fewer than kk classes have a unit).
     __device__ __forceinline__ uint32_t find_bound(uint32_t kk) const {
-        constexpr uint32_t N = kThreads / 32;
+        constexpr uint32_t N = 2 * kThreads / 32;
         const uint32_t units = u1 - u0;
-        if (min(units, kThreads) < kk) return 0;
+        if (min(units, kThreads) + min(units - min(units, 2 * kThreads), kThreads) < kk) return 0;
         uint32_t key[N], lo = 0xFFFFFFFFu, hi = 0;
 #pragma unroll
         for (uint32_t i = 0; i < N; ++i) {
+            // (class t holds the first pairs of thread t, class kThreads + t its second ones, the first of them unit 2 kThreads + t)
             const uint32_t t = i * 32 + lane_id();
-            key[i] = t < units ? order_key(sh.thread_max[t]) : 0u;
+            key[i] = (t < kThreads ? t : t + kThreads) < units ? order_key(sh.class_max[t]) : 0u;
             lo = min(lo, key[i]);
             hi = max(hi, key[i]);
         }
         lo = __reduce_min_sync(0xFFFFFFFFu, lo);
         hi = __reduce_max_sync(0xFFFFFFFFu, hi);
-        // at least kk threads reach lo, fewer reach hi + 1; a few more than kk are as good as kk
+        // at least kk classes reach lo, fewer reach hi + 1; a few more than kk are as good as kk
         while (lo < hi) {
             const uint32_t mid = lo + (hi - lo) / 2 + 1;
             uint32_t n = 0;
@@ -97,21 +99,21 @@ template <typename T, uint32_t kThreads> struct Selector {
     __device__ __forceinline__ uint32_t collect(uint32_t low) const {
         if (threadIdx.x == 0) sh.counter = sh.hit_count = 0;
         __syncthreads();
-        const uint32_t group_units = 4u << group_shift, span = group_units * kThreads;
+        const uint32_t group_units = 2u << group_shift, span = group_units * kThreads;
         // (the order of floats and of keys is the same from -inf up; below that, everything is a candidate)
         const bool all = low <= 0x007FFFFFu;
         const float low_value = value_of_key(low);
         const uint32_t groups = (u1 - u0 + span - 1) / span;
         uint32_t mine = 0;
-        for (uint32_t g = 0; g < groups; ++g) mine += all || sh.group_max[g * kThreads + threadIdx.x] >= low_value;
+#pragma unroll
+        for (uint32_t g = 0; g < sh.kGroups; ++g)
+            mine |= static_cast<uint32_t>(g < groups && (all || sh.group_max[g * kThreads + threadIdx.x] >= low_value)) << g;
         if (mine) {
-            uint32_t at = atomicAdd(&sh.hit_count, mine);
-            for (uint32_t g = 0; g < groups; ++g)
-                if (all || sh.group_max[g * kThreads + threadIdx.x] >= low_value)
-                    sh.hits[at++] = static_cast<uint16_t>(g * kThreads + threadIdx.x);
+            uint32_t at = atomicAdd(&sh.hit_count, static_cast<uint32_t>(__popc(mine)));
+            for (; mine; mine &= mine - 1) sh.hits[at++] = static_cast<uint16_t>((__ffs(mine) - 1) * kThreads + threadIdx.x);
         }
         __syncthreads();
-        const uint32_t unit_shift = group_shift + 2, items = sh.hit_count << unit_shift;
+        const uint32_t unit_shift = group_shift + 1, items = sh.hit_count << unit_shift;
         for (uint32_t item0 = threadIdx.x; item0 < items; item0 += 2 * kThreads) {
             uint4 v[2];
             uint32_t us[2];
@@ -220,7 +222,7 @@ template <typename T, uint32_t kThreads> struct Selector {
         __syncthreads();
     }
     // best[0 .. kk) := the kk best of n <= kRankable candidates in order.  Every warp sorts runs of 32 in its registers;
-    // an entry's place is its place in its run and, by bisection, how many of every other run are better.
+    // an entry's place is how many entries of each run are better, by bisection.
     __device__ __forceinline__ void in_order(uint32_t n, uint32_t kk) const {
         const uint32_t runs = (n + 31) / 32, lane = lane_id();
         for (uint32_t run = threadIdx.x >> 5; run < runs; run += kThreads / 32) {
@@ -238,9 +240,9 @@ template <typename T, uint32_t kThreads> struct Selector {
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
             const uint64_t key = sh.candidates[i];
-            uint32_t place = i & 31u;
+            uint32_t place = 0;
+#pragma unroll 4
             for (uint32_t run = 0; run < runs; ++run) {
-                if (run == i / 32) continue;
                 const uint64_t* list = sh.candidates + run * 32;
                 uint32_t better = 0;
 #pragma unroll
@@ -252,7 +254,7 @@ template <typename T, uint32_t kThreads> struct Selector {
         }
         __syncthreads();
     }
-    // best[0 .. kk) := the slice's kk best columns in order.  Every thread's largest element is in thread_max.
+    // best[0 .. kk) := the slice's kk best columns in order.  The class maxima are in class_max.
     __device__ __forceinline__ void run(uint32_t kk) const {
         if (threadIdx.x < 32) {
             const uint32_t b = find_bound(kk);
@@ -263,7 +265,7 @@ template <typename T, uint32_t kThreads> struct Selector {
         bool above = false;                    // the candidates are the columns above the bound
         for (;;) {
             n = collect(low);
-            if (n < kk && !above && bound != 0) {        // threads whose only elements lie outside the row or are NaN
+            if (n < kk && !above && bound != 0) {        // classes whose only elements lie outside the row or are NaN
                 bound = low = 0;
             } else if (n > kCandidates) {                // many equal to the bound, or sorted columns
                 if (above) bound = kth_key(*this, kk);
@@ -314,7 +316,7 @@ __device__ __forceinline__ void write_row(const LogProbArgs& a, uint32_t row_id,
 // A cluster of CTAs takes a row, each CTA a slice of its units; the CTAs join their sums and their ordered best columns
 // through each other's shared memory.
 template <typename T, uint32_t kThreads, bool kCluster>
-__global__ void __launch_bounds__(kThreads, kThreads == 128 ? 7 : 1024 / kThreads)
+__global__ void __launch_bounds__(kThreads, kThreads == 128 ? 7 : 3)
 lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
     constexpr uint32_t kWarps = kThreads / 32;
     __shared__ LogProbShared<kThreads> sh;
@@ -334,23 +336,33 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
         // one pass: sums, and the largest element of every batch of four units
         RowSums sums;
         uint32_t group_shift = 0;
-        while ((u1 - u0 + (4 * kThreads << group_shift) - 1) / (4 * kThreads << group_shift) > sh.kGroups) ++group_shift;
-        float thread_max = minus_inf(), group_max = minus_inf();
+        while ((u1 - u0 + (2 * kThreads << group_shift) - 1) / (2 * kThreads << group_shift) > sh.kGroups) ++group_shift;
+        float max0 = minus_inf(), max1 = minus_inf(), group_max = minus_inf();
         uint32_t in_group = 1u << group_shift, slot = tid;
-        stream_units<T, kThreads>(row, u0, u1, [&](const uint4 (&v)[4], float best) {
+        stream_units<T, kThreads>(row, u0, u1, [&](const uint4 (&v)[4], float best0, float best1) {
+            const float best = fmaxf(best0, best1);
             sums.add<T, true>(v, best, a.c);
-            group_max = fmaxf(group_max, best);
-            sh.group_max[slot] = group_max;                      // (written again until the group is complete)
-            if (--in_group == 0) {
-                thread_max = fmaxf(thread_max, group_max);
-                group_max = minus_inf();
-                in_group = 1u << group_shift;
-                slot += kThreads;
+            max0 = fmaxf(max0, best0);
+            max1 = fmaxf(max1, best1);
+            if (group_shift == 0) {                                  // the same for the whole CTA
+                sh.group_max[slot] = best0;
+                if (slot + kThreads < sh.kGroups * kThreads) sh.group_max[slot + kThreads] = best1;
+                slot += 2 * kThreads;
+            } else {
+                group_max = fmaxf(group_max, best);
+                sh.group_max[slot] = group_max;                      // (written again until the group is complete)
+                if ((in_group -= 2) == 0) {
+                    group_max = minus_inf();
+                    in_group = 1u << group_shift;
+                    slot += kThreads;
+                }
             }
         });
-        thread_max = fmaxf(thread_max, group_max);
-        if (a.top) sh.thread_max[tid] = thread_max;
-        const RowPart mine = sums.part(warp_max(thread_max), a.c);
+        if (a.top) {
+            sh.class_max[tid] = max0;
+            sh.class_max[kThreads + tid] = max1;
+        }
+        const RowPart mine = sums.part(warp_max(fmaxf(max0, max1)), a.c);
         if (lane == 0) sh.warp_part[turn][warp] = mine;
         __syncthreads();
 
@@ -535,8 +547,8 @@ template <typename T> dct_status_t launch_logprobs(const void* logits, const Log
     const int sms = sm_count();
     if (sms <= 0) return DCT_ERR_CUDA;
     const uint32_t units = (a.vocab + Unit<T>::kElems - 1) / Unit<T>::kElems;
-    const uint32_t threads = a.top > 128 ? 512 : a.top <= 64 && (units <= 1024 || a.rows >= 4u * sms) ? 128 : 256;
-    const uint32_t ctas = static_cast<uint32_t>(sms) * (threads == 128 ? 7 : 1024 / threads);
+    const uint32_t threads = a.top <= 128 && (units <= 1024 || a.rows >= 4u * sms) ? 128 : 256;
+    const uint32_t ctas = static_cast<uint32_t>(sms) * (threads == 128 ? 7 : 3);
     // A row goes to 1, 2, 4 or 8 CTAs: the number of rounds the CTAs on the chip need, times the units of a CTA's slice
     // and about two batches' worth of work at its end.
     uint32_t cluster = 1;
@@ -549,7 +561,6 @@ template <typename T> dct_status_t launch_logprobs(const void* logits, const Log
             cluster = c;
         }
     }
-    if (threads == 512) return launch_logprobs_threads<T, 512>(logits, a, cluster, ctas, stream);
     if (threads == 256) return launch_logprobs_threads<T, 256>(logits, a, cluster, ctas, stream);
     return launch_logprobs_threads<T, 128>(logits, a, 1, ctas, stream);
 }

@@ -135,8 +135,8 @@ template <> struct Unit<__nv_bfloat16> {
         const __nv_bfloat162 m = best2(a);
         return fmaxf(__low2float(m), __high2float(m));
     }
-    __device__ static __forceinline__ float best(const uint4& a, const uint4& b, const uint4& c, const uint4& d) {
-        const __nv_bfloat162 m = __hmax2(__hmax2(best2(a), best2(b)), __hmax2(best2(c), best2(d)));
+    __device__ static __forceinline__ float best(const uint4& a, const uint4& b) {
+        const __nv_bfloat162 m = __hmax2(best2(a), best2(b));
         return fmaxf(__low2float(m), __high2float(m));
     }
 };
@@ -329,7 +329,8 @@ struct RowSums {
 };
 
 // Streams the units [u0, u1) of a row through the CTA, in batches of four units per thread (first + tid + i kThreads).
-// each(v, best) takes the four units, -inf where there is no element, and their largest element.
+// each(v, best0, best1) takes the four units, -inf where there is no element, and the largest element of the first two and
+// of the last two.
 template <typename T, uint32_t kThreads, typename Each>
 __device__ __forceinline__ void stream_units(const RowView<T>& row, uint32_t u0, uint32_t u1, Each&& each) {
     constexpr uint32_t kInf = Unit<T>::kMinusInf;
@@ -351,10 +352,7 @@ __device__ __forceinline__ void stream_units(const RowView<T>& row, uint32_t u0,
             for (int i = 0; i < 4; ++i)
                 if (first + i * kThreads < u1) row.mask(v[i], first + i * kThreads);
         }
-        float best;
-        if constexpr (sizeof(T) == 4) best = fmaxf(Unit<T>::best(v[0], v[1]), Unit<T>::best(v[2], v[3]));
-        else best = Unit<T>::best(v[0], v[1], v[2], v[3]);
-        each(v, best);
+        each(v, Unit<T>::best(v[0], v[1]), Unit<T>::best(v[2], v[3]));
     }
 }
 
