@@ -21,17 +21,18 @@ struct LogProbArgs {
 template <uint32_t kThreads> struct LogProbShared {
     static constexpr uint32_t kWarps = kThreads / 32;
     static constexpr uint32_t kGroups = 16;                                        // maxima a thread notes
-    static constexpr uint32_t kCandidates = kThreads > 128 ? 2048 : 1024;          // columns the selection holds
+    static constexpr uint32_t kMaxTop = kThreads;                                  // (half the classes the bound comes from)
+    static constexpr uint32_t kCandidates = 8 * kThreads;                          // columns the selection holds
     float group_max[kGroups * kThreads];
     uint64_t candidates[kCandidates];
-    uint64_t best[DCT_LM_MAX_TOP];
+    uint64_t best[kMaxTop];
     float class_max[2 * kThreads];
     uint16_t hits[kGroups * kThreads];
     RowPart warp_part[2][kWarps];      // by turns, row by row
     RowPart part;                      // this CTA's slice
     float m, logsum;                   // of the whole row
     uint32_t counts[32];
-    uint32_t counter, hit_count, bound, kept;
+    uint32_t counter, hit_count, bound;
 };
 
 __device__ __forceinline__ float value_of_key(uint32_t key) {       // the inverse of order_key
@@ -39,8 +40,8 @@ __device__ __forceinline__ float value_of_key(uint32_t key) {       // the inver
 }
 
 // The selection of a slice's best columns.  A column is (order key << 32 | ~column): larger is better, all distinct.
-// While the row streams by, every thread notes the largest element of each pair of units it reads, and that of all its first
-// and all its second pairs.  The kk-th largest of these N = 2 kThreads class maxima is a bound that at least kk columns
+// While the row streams by, every thread notes the largest element of each pair of units it reads, and that of its even and of
+// its odd units.  The kk-th largest of these N = 2 kThreads class maxima is a bound that at least kk columns
 // reach and, for kk well below N, not many more do (N ln(N / (N - kk)) for columns in no particular order: 74 for 64 of
 // 256); only pairs of units whose noted maximum reaches it are read again, and of them the elements that reach it are put
 // in order.
@@ -68,13 +69,12 @@ template <typename T, uint32_t kThreads> struct Selector {
     __device__ __forceinline__ uint32_t find_bound(uint32_t kk) const {
         constexpr uint32_t N = 2 * kThreads / 32;
         const uint32_t units = u1 - u0;
-        if (min(units, kThreads) + min(units - min(units, 2 * kThreads), kThreads) < kk) return 0;
+        if (min(units, 2 * kThreads) < kk) return 0;
         uint32_t key[N], lo = 0xFFFFFFFFu, hi = 0;
 #pragma unroll
         for (uint32_t i = 0; i < N; ++i) {
-            // (class t holds the first pairs of thread t, class kThreads + t its second ones, the first of them unit 2 kThreads + t)
-            const uint32_t t = i * 32 + lane_id();
-            key[i] = (t < kThreads ? t : t + kThreads) < units ? order_key(sh.class_max[t]) : 0u;
+            const uint32_t t = i * 32 + lane_id();           // (the class's first unit)
+            key[i] = t < units ? order_key(sh.class_max[t]) : 0u;
             lo = min(lo, key[i]);
             hi = max(hi, key[i]);
         }
@@ -103,7 +103,7 @@ template <typename T, uint32_t kThreads> struct Selector {
         // (the order of floats and of keys is the same from -inf up; below that, everything is a candidate)
         const bool all = low <= 0x007FFFFFu;
         const float low_value = value_of_key(low);
-        const uint32_t groups = (u1 - u0 + span - 1) / span;
+        const uint32_t groups = group_shift ? (u1 - u0 + span - 1) / span : (u1 - u0 + 2 * span - 1) / (2 * span) * 2;
         uint32_t mine = 0;
 #pragma unroll
         for (uint32_t g = 0; g < sh.kGroups; ++g)
@@ -123,7 +123,10 @@ template <typename T, uint32_t kThreads> struct Selector {
                 us[q] = 0xFFFFFFFFu;
                 if (item < items) {
                     const uint32_t slot = sh.hits[item >> unit_shift];
-                    const uint32_t u = u0 + (slot / kThreads * group_units + (item & (group_units - 1))) * kThreads + slot % kThreads;
+                    const uint32_t g = slot / kThreads, j = item & (group_units - 1);
+                    // (a pair is the first and third or the second and fourth unit of a batch, a larger group whole batches)
+                    const uint32_t at = group_shift ? g * group_units + j : (g >> 1) * 4 + (g & 1) + 2 * j;
+                    const uint32_t u = u0 + at * kThreads + slot % kThreads;
                     if (u < u1) {
                         us[q] = u;
                         v[q] = ld_unit(row.base + u);
@@ -316,7 +319,7 @@ __device__ __forceinline__ void write_row(const LogProbArgs& a, uint32_t row_id,
 // A cluster of CTAs takes a row, each CTA a slice of its units; the CTAs join their sums and their ordered best columns
 // through each other's shared memory.
 template <typename T, uint32_t kThreads, bool kCluster>
-__global__ void __launch_bounds__(kThreads, kThreads == 128 ? 7 : 3)
+__global__ void __launch_bounds__(kThreads, kThreads <= 128 ? 896 / kThreads : 3)
 lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
     constexpr uint32_t kWarps = kThreads / 32;
     __shared__ LogProbShared<kThreads> sh;
@@ -393,14 +396,11 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
         }
         uint32_t kept = 0;
         if (a.top) {
-            const uint32_t columns = u1 == u0 ? 0u
-                : min(a.vocab, u1 * Unit<T>::kElems - row.lead) - (u0 == 0 ? 0u : u0 * Unit<T>::kElems - row.lead);
-            kept = min(a.top, columns);
+            kept = min(a.top, slice.columns(row));
             if (kept) Selector<T, kThreads>{row, u0, u1, group_shift, sh}.run(kept);
         }
 
         if (kCluster) {
-            if (tid == 0) sh.kept = kept;
             cluster_barrier();
             if (warp == kWarps - 1) {
                 RowPart all{minus_inf(), 0.0f, 0.0f};
@@ -411,25 +411,22 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
                 }
                 all.join_lanes(a.c, kMaxCluster);
                 if (lane == 0) {
-                    if (rank == 0) {
-                        write_row(a, row_id, xr, tok, all, sh.m, sh.logsum);
-                    } else {
-                        LogProbArgs quiet = a;
-                        quiet.tokens = nullptr;
-                        quiet.entropy_out = quiet.stats_out = nullptr;
-                        write_row(quiet, row_id, xr, tok, all, sh.m, sh.logsum);
+                    LogProbArgs mine = a;
+                    if (rank != 0) {
+                        mine.tokens = nullptr;
+                        mine.entropy_out = mine.stats_out = nullptr;
                     }
+                    write_row(mine, row_id, xr, tok, all, sh.m, sh.logsum);
                 }
             }
-            if (a.top) {
-                for (uint32_t c = 0; c < ctas; ++c) {
-                    const uint32_t n = ld_remote_u32(remote_smem(&sh.kept, c));
-                    for (uint32_t i = tid; i < n; i += kThreads)
-                        sh.candidates[c * DCT_LM_MAX_TOP + i] = ld_remote_u64(remote_smem(&sh.best[i], c));
-                    if (tid == 0) sh.counts[c] = n;
-                }
-                __syncthreads();
+            // the other slices' lists, all loads at once
+            for (uint32_t item = tid; item < ctas * a.top; item += kThreads) {
+                const uint32_t c = item / a.top, i = item % a.top;
+                if (c != rank && i < min(a.top, Slice(row.units, c, ctas).columns(row)))
+                    sh.candidates[c * sh.kMaxTop + i] = ld_remote_u64(remote_smem(&sh.best[i], c));
             }
+            __syncthreads();
+            cluster_arrive();             // (waited for below: nobody reads this CTA's shared memory any more)
         }
         // a column's place: its place in its own slice's list, and how many of each other list are better
         for (uint32_t i = tid; i < kept; i += kThreads) {
@@ -438,8 +435,8 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
             if (kCluster) {
                 for (uint32_t c = 0; c < ctas; ++c) {
                     if (c == rank) continue;
-                    const uint64_t* list = sh.candidates + c * DCT_LM_MAX_TOP;
-                    uint32_t lo = 0, hi = sh.counts[c];         // list[0 .. lo) are better
+                    const uint64_t* list = sh.candidates + c * sh.kMaxTop;
+                    uint32_t lo = 0, hi = min(a.top, Slice(row.units, c, ctas).columns(row));         // list[0 .. lo) are better
                     while (lo < hi) {
                         const uint32_t mid = (lo + hi) / 2;
                         if (list[mid] > key) lo = mid + 1;
@@ -457,7 +454,7 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
         }
         // Nobody may read this CTA's shared memory any more when its next row begins.  (A CTA on its own needs no barrier
         // here: the warps' parts alternate, and what else the next row writes it writes behind its first barrier.)
-        if (kCluster) cluster_barrier();
+        if (kCluster) cluster_wait();
         if (a.rows - row_id <= clusters) break;
         row_id += clusters;
     }
@@ -547,22 +544,37 @@ template <typename T> dct_status_t launch_logprobs(const void* logits, const Log
     const int sms = sm_count();
     if (sms <= 0) return DCT_ERR_CUDA;
     const uint32_t units = (a.vocab + Unit<T>::kElems - 1) / Unit<T>::kElems;
-    const uint32_t threads = a.top <= 128 && (units <= 1024 || a.rows >= 4u * sms) ? 128 : 256;
-    const uint32_t ctas = static_cast<uint32_t>(sms) * (threads == 128 ? 7 : 3);
-    // A row goes to 1, 2, 4 or 8 CTAs: the number of rounds the CTAs on the chip need, times the units of a CTA's slice
-    // and about two batches' worth of work at its end.
-    uint32_t cluster = 1;
+    // Threads to a row's CTA, and CTAs to a row: the shape with the least estimated time, in tenths of a microsecond.  A round of
+    // CTAs takes what the end of a row costs (join, selection, order; more warps to a row make it shorter but fewer rows share
+    // it) and 0.9 us for each batch of four units per thread.  Measured at both ends: 16384 rows of 4096 bf16, top 20: 49 / 70 /
+    // 96 / 252 us with 32 / 64 / 128 / 256 threads; 1000 rows of 131072: 146 / 82 / 57 / 72; one row of 32768: 26 / 14 / 9 / 7.5.
+    // Splitting a row costs the exchange of the lists: one row of 32768 with 1 / 2 / 4 / 8 CTAs 7.5 / 8.3 / 8.2 / 10.6 us, of 131072
+    // 14.9 / 12.2 / 10.3 / 10.5, 64 rows of 131072 21.6 / 16.1 / 13.6 / 21.9.
+    // A selection wants twice as many classes as columns; where the row has many batches, more threads to it are better
+    // still (4096 rows of 32768, top 64: 79 us with 64 threads, 73 with 128; of 8192: 67 and 75).
+    uint32_t threads = 256, cluster = 1;
     uint64_t best = ~0ull;
-    for (uint32_t c = 1; c <= kMaxCluster && (c == 1 || (threads > 128 && units / c >= 512)); c *= 2) {
-        const uint64_t rounds = (static_cast<uint64_t>(a.rows) * c + ctas - 1) / ctas;
-        const uint64_t cost = rounds * (units / c + 2048);
-        if (cost < best) {
-            best = cost;
-            cluster = c;
+    for (uint32_t t = 32; t <= 256; t *= 2) {
+        if (t < 256 && (a.top > t || (a.top > t / 2 && units > 32 * t))) continue;
+        const uint64_t slots = static_cast<uint64_t>(sms) * (t <= 128 ? 896 / t : 3);
+        for (uint32_t c = 1; c <= kMaxCluster && (c == 1 || (t == 256 && units / c >= 512)); c *= 2) {
+            const uint64_t rounds = (static_cast<uint64_t>(a.rows) * c + slots - 1) / slots;
+            const uint64_t end = a.top ? (t == 32 ? 100 : t == 64 ? 70 : t == 128 ? 55 : 60) + 50 * a.top / t +
+                                             (c == 1 ? 0 : c == 2 ? 15 : c == 4 ? 25 : 45)
+                                       : (t == 32 ? 40 : t == 64 ? 30 : t == 128 ? 20 : 25) + (c > 1 ? 10 : 0);
+            const uint64_t cost = rounds * (end + 9 * ((units / c + 4 * t - 1) / (4 * t)));
+            if (cost < best) {
+                best = cost;
+                threads = t;
+                cluster = c;
+            }
         }
     }
-    if (threads == 256) return launch_logprobs_threads<T, 256>(logits, a, cluster, ctas, stream);
-    return launch_logprobs_threads<T, 128>(logits, a, 1, ctas, stream);
+    const uint32_t ctas = static_cast<uint32_t>(sms) * (threads <= 128 ? 896 / threads : 3);
+    if (threads == 32) return launch_logprobs_threads<T, 32>(logits, a, 1, ctas, stream);
+    if (threads == 64) return launch_logprobs_threads<T, 64>(logits, a, 1, ctas, stream);
+    if (threads == 128) return launch_logprobs_threads<T, 128>(logits, a, 1, ctas, stream);
+    return launch_logprobs_threads<T, 256>(logits, a, cluster, ctas, stream);
 }
 
 bool refused_logits(const void* logits, dct_dtype_t dtype, uint32_t vocab, uint32_t ld, float inv_t) {

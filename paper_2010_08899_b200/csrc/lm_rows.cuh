@@ -329,8 +329,8 @@ struct RowSums {
 };
 
 // Streams the units [u0, u1) of a row through the CTA, in batches of four units per thread (first + tid + i kThreads).
-// each(v, best0, best1) takes the four units, -inf where there is no element, and the largest element of the first two and
-// of the last two.
+// each(v, best0, best1) takes the four units, -inf where there is no element, and the largest element of the first and third
+// and of the second and fourth.
 template <typename T, uint32_t kThreads, typename Each>
 __device__ __forceinline__ void stream_units(const RowView<T>& row, uint32_t u0, uint32_t u1, Each&& each) {
     constexpr uint32_t kInf = Unit<T>::kMinusInf;
@@ -352,7 +352,7 @@ __device__ __forceinline__ void stream_units(const RowView<T>& row, uint32_t u0,
             for (int i = 0; i < 4; ++i)
                 if (first + i * kThreads < u1) row.mask(v[i], first + i * kThreads);
         }
-        each(v, Unit<T>::best(v[0], v[1]), Unit<T>::best(v[2], v[3]));
+        each(v, Unit<T>::best(v[0], v[2]), Unit<T>::best(v[1], v[3]));
     }
 }
 
@@ -363,6 +363,11 @@ struct Slice {
         const uint32_t share = (units + ctas - 1) / ctas;
         u0 = min(units, rank * share);
         u1 = min(units, u0 + share);
+    }
+    // the row's columns that lie in it
+    template <typename Row> __device__ __forceinline__ uint32_t columns(const Row& row) const {
+        if (u0 == u1) return 0;
+        return min(row.width, u1 * Row::kElems - row.lead) - (u0 == 0 ? 0u : u0 * Row::kElems - row.lead);
     }
 };
 
@@ -381,6 +386,9 @@ __device__ __forceinline__ uint32_t cluster_size() {
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
+// its two halves, for work in between that needs neither
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ uint32_t remote_smem(const void* p, uint32_t rank) {      // p's counterpart in CTA `rank`
     uint32_t a;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
