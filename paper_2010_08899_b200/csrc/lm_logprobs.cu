@@ -342,8 +342,8 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
         while ((u1 - u0 + (2 * kThreads << group_shift) - 1) / (2 * kThreads << group_shift) > sh.kGroups) ++group_shift;
         float max0 = minus_inf(), max1 = minus_inf(), group_max = minus_inf();
         uint32_t in_group = 1u << group_shift, slot = tid;
-        stream_units<T, kThreads>(row, u0, u1, [&](const uint4 (&v)[4], float best0, float best1) {
-            const float best = fmaxf(best0, best1);
+        stream_units<T, kThreads>(row, u0, u1, [&](const uint4 (&v)[4], uint32_t) {
+            const float best0 = Unit<T>::best(v[0], v[2]), best1 = Unit<T>::best(v[1], v[3]), best = fmaxf(best0, best1);
             sums.add<T, true>(v, best, a.c);
             max0 = fmaxf(max0, best0);
             max1 = fmaxf(max1, best1);
@@ -375,19 +375,7 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
             RowPart all = sh.warp_part[turn][lane & (kWarps - 1)];
             all.join_lanes(a.c, kWarps);
             if (all.s == 0.0f && all.xmax > minus_inf()) {
-                // values so low that x c overflows: once more, slowly, from differences
-                RowPart p{all.xmax, 0.0f, 0.0f};
-                for (uint32_t u = u0 + lane; u < u1; u += 32) {
-                    const uint4 v = ld_unit(row.base + u);
-                    for (uint32_t i = 0; i < Unit<T>::kElems; ++i)
-                        if (row.column(u, i) < row.width) {
-                            const float y = __fmul_rn(__fadd_rn(Unit<T>::get(v, i), -all.xmax), a.c), e = exp2_fast(y);
-                            p.s = __fadd_rn(p.s, e);
-                            if (e != 0.0f) p.st = fmaf(e, y, p.st);
-                        }
-                }
-                p.join_lanes(a.c, 32);
-                all = p;
+                all = low_part(row, u0, u1, all.xmax, a.c, [](uint32_t, uint32_t) { return true; });
             }
             if (lane == 0) {
                 sh.part = all;

@@ -150,6 +150,11 @@ __device__ __forceinline__ uint4 ld_unit(const uint4* p) {
 __device__ __forceinline__ void st_unit(void* p, const uint4& v) {
     asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+__device__ __forceinline__ void copy_word_async(void* smem, const void* global) {        // 4 bytes, both 4-byte aligned
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_addr(smem)), "l"(global) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
 __device__ __forceinline__ float max_nan(float a, float b) {     // NaN if either is
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -251,6 +256,26 @@ struct RowPart {
     }
 };
 
+// The part of a row whose values are so low that x c overflows (the type's lowest value in every column that counts): from
+// differences, by every warp on its own.  keep(u, i): whether element i of unit u counts.
+template <typename T, typename Keep>
+__device__ __noinline__ RowPart low_part(const RowView<T> row, uint32_t u0, uint32_t u1, float xmax, float c, const Keep keep) {
+    RowPart p{xmax, 0.0f, 0.0f};
+    for (uint32_t u = u0 + lane_id(); u < u1; u += 32) {
+        const uint4 v = ld_unit(row.base + u);
+#pragma unroll
+        for (uint32_t i = 0; i < Unit<T>::kElems; ++i)
+            if (row.column(u, i) < row.width && keep(u, i)) {
+                const float y = __fmul_rn(__fadd_rn(Unit<T>::get(v, i), -xmax), c), e = exp2_fast(y);
+                p.s = __fadd_rn(p.s, e);
+                if (e != 0.0f) p.st = fmaf(e, y, p.st);
+            }
+    }
+    __syncwarp();
+    p.join_lanes(c, 32);
+    return p;
+}
+
 // One thread's share of sum 2^y and sum 2^y y over a row, y = x c - ref.  The reference is the warp's: the largest x c of its
 // first batch, replaced only when a batch exceeds it by kSlack, so that an element costs one product-sum, one power of
 // two and two sums.  Rounding c and ref moves nothing but the reference: what counts is (x - xmax) c, and the
@@ -329,8 +354,7 @@ struct RowSums {
 };
 
 // Streams the units [u0, u1) of a row through the CTA, in batches of four units per thread (first + tid + i kThreads).
-// each(v, best0, best1) takes the four units, -inf where there is no element, and the largest element of the first and third
-// and of the second and fourth.
+// each(v, first) takes the four units, -inf where there is no element of the row or the slice, and the first one's number.
 template <typename T, uint32_t kThreads, typename Each>
 __device__ __forceinline__ void stream_units(const RowView<T>& row, uint32_t u0, uint32_t u1, Each&& each) {
     constexpr uint32_t kInf = Unit<T>::kMinusInf;
@@ -352,7 +376,7 @@ __device__ __forceinline__ void stream_units(const RowView<T>& row, uint32_t u0,
             for (int i = 0; i < 4; ++i)
                 if (first + i * kThreads < u1) row.mask(v[i], first + i * kThreads);
         }
-        each(v, Unit<T>::best(v[0], v[2]), Unit<T>::best(v[1], v[3]));
+        each(v, first);
     }
 }
 
