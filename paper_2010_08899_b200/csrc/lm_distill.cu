@@ -14,7 +14,7 @@ struct DistillArgs {
     uint32_t top;
     const float* grad_loss;
     float* loss_out;
-    uint32_t ld_grad, mark_words;
+    uint32_t ld_grad, chunks, mark_words, spin_limit;      // of a CTA's slice at most; polls a wait may take
     dct_result_t* result;
 };
 
@@ -28,28 +28,48 @@ __device__ __forceinline__ void add_value(RowPart& p, float v) {
     }
 }
 
-// A row's cluster of CTAs reads its logits twice: for the sums, and, when those are joined, for the gradient; the second time
-// they come from L2, as few enough rows are under way.  The teacher's slots of the next row, and the logits that this row's
-// slots name, are fetched while the row streams by.  `marks` has a bit for every element of the slice's units that a
-// slot names.  kTail: those are left out of the sums, so that the remainder is summed and not a difference.  The gradient is
-// first written as if no column were named, and the named ones once more afterwards.
+// A row belongs to a cluster of CTAs, a slice of it to each, and a slice's chunks of 128 units (2 KiB) in turn to the CTA's
+// warps.  The logits are needed twice, for the sums and, when those are joined, for the gradient.  kStaged: a warp fetches
+// its chunks by bulk copies into shared memory, works on them twice and, as it lets go of each, asks for the next row's, so
+// that they cross the memory bus once and are under way while other work is done; otherwise (slices beyond shared memory)
+// they are loaded twice.  The teacher's slots of the next row, and the logits that this row's slots name, are fetched while the
+// row streams by.  `marks` has a bit for every element of the slice's units that a slot names.  kTail: those are left out of
+// the sums, so that the remainder is summed and not a difference.  The gradient is first written as if no column were named,
+// and the named ones once more afterwards.
 // Slot i belongs to thread i mod kThreads throughout.
-template <typename T, uint32_t kThreads, bool kTail, bool kCluster>
+constexpr uint32_t kChunkUnits = 128u, kChunkBytes = 16u * kChunkUnits;
+constexpr uint32_t kMaxChunksPerWarp = 16u;
+constexpr uint32_t kStagedLimit = 200u * 1024u;            // shared memory of an SM that slices may fill
+
+template <typename T, uint32_t kThreads, bool kTail, bool kCluster, bool kStaged>
 __global__ void __launch_bounds__(kThreads, 768 / kThreads)
 lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
     constexpr uint32_t E = Unit<T>::kElems, kWarps = kThreads / 32;
-    extern __shared__ __align__(16) uint32_t dynamic[];
+    extern __shared__ __align__(128) uint32_t dynamic[];
     __shared__ RowPart student_parts[kWarps], teacher_parts[kWarps], named_parts[kWarps], slice_part, slice_named;
     __shared__ float loss_parts[kWarps];
-    __shared__ uint32_t repeated_flag;
-    uint32_t* const marks = dynamic;
+    __shared__ uint32_t repeated_flag, gave_up;
+    __shared__ uint64_t arrived[kStaged ? kWarps * kMaxChunksPerWarp : 1];
+    uint4* const stage = reinterpret_cast<uint4*>(dynamic);
+    uint32_t* const marks = dynamic + (kStaged ? a.chunks * (kChunkBytes / 4) : 0);
     int32_t* const ids_by_turn = reinterpret_cast<int32_t*>(marks + a.mark_words);       // two rows
     float* const t_by_turn = reinterpret_cast<float*>(ids_by_turn + 2 * a.top);           // two rows
     uint32_t* const z_words = reinterpret_cast<uint32_t*>(t_by_turn + 2 * a.top);
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = lane_id();
     const uint32_t rank = kCluster ? cluster_rank() : 0u, ctas = kCluster ? cluster_size() : 1u;
     const uint32_t clusters = gridDim.x / ctas;
+    uint32_t phases = 0, missed = 0;       // the parity each of this warp's barriers is waited for with; copies given up on
 
+    // (staged) asks for chunk k of a row's slice
+    auto fetch_chunk = [&](const RowView<T>& of_row, const Slice& of_slice, uint32_t k) {
+        const uint32_t first = of_slice.u0 + k * kChunkUnits;
+        if (lane == 0 && first < of_slice.u1 && !*const_cast<volatile uint32_t*>(&gave_up)) {
+            const uint32_t bytes = 16u * min(kChunkUnits, of_slice.u1 - first);
+            uint64_t* bar = &arrived[warp * kMaxChunksPerWarp + k / kWarps];
+            mbar_arrive_expect_tx(bar, bytes);
+            bulk_load(stage + k * kChunkUnits, of_row.base + first, bytes, bar);
+        }
+    };
     auto fetch_slots = [&](uint32_t of_row, uint32_t turn) {
         const size_t at = static_cast<size_t>(of_row) * a.top;
         for (uint32_t i = tid; i < a.top; i += kThreads) {
@@ -58,10 +78,21 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         }
     };
     uint32_t row_id = blockIdx.x / ctas;
+    if (tid == 0) repeated_flag = gave_up = 0;
+    __syncthreads();
+    if (kStaged) {
+        if (lane == 0) {
+            for (uint32_t j = 0; j < kMaxChunksPerWarp; ++j) mbar_init(&arrived[warp * kMaxChunksPerWarp + j], 1);
+            mbar_init_fence();
+            fence_proxy_async_smem();
+        }
+        __syncwarp();
+        const RowView<T> row(logits + static_cast<size_t>(row_id) * a.ld, a.vocab);
+        for (uint32_t k = warp; k < a.chunks; k += kWarps) fetch_chunk(row, Slice(row.units, rank, ctas), k);
+    }
     fetch_slots(row_id, 0);
     copy_commit();
     for (uint32_t w = tid; w < a.mark_words; w += kThreads) marks[w] = 0;
-    if (tid == 0) repeated_flag = 0;
     for (uint32_t turn = 0;; turn ^= 1) {
         const T* xr = logits + static_cast<size_t>(row_id) * a.ld;
         const RowView<T> row(xr, a.vocab);
@@ -92,6 +123,8 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         }
         copy_commit();
         const bool more = a.rows - row_id > clusters;
+        const RowView<T> next_row(logits + static_cast<size_t>(more ? row_id + clusters : row_id) * a.ld, a.vocab);
+        const Slice next_slice(next_row.units, rank, ctas);
         if (more) fetch_slots(row_id + clusters, turn ^ 1);
         copy_commit();
         if (bad && a.result && rank == 0) atomicMax(&a.result->status, static_cast<uint32_t>(DCT_ERR_BAD_MASK));
@@ -104,11 +137,32 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         };
         RowSums sums;
         float x_best = minus_inf();
-        stream_units<T, kThreads>(row, u0, u1, [&](uint4 (&v)[4], uint32_t first) {
+        for (uint32_t k = warp; u0 + k * kChunkUnits < u1; k += kWarps) {
+            const uint32_t first = u0 + k * kChunkUnits + lane;
+            uint4 v[4];
+            if (kStaged) {
+                const uint32_t j = k / kWarps;
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&arrived[warp * kMaxChunksPerWarp + j], phases >> j & 1u, a.spin_limit, &gave_up))) {
+                    *const_cast<volatile uint32_t*>(&gave_up) = 1;       // this row and the rest become NaN
+                    missed |= 1u << j;
+                } else {
+                    phases ^= 1u << j;
+                }
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                v[i] = make_uint4(Unit<T>::kMinusInf, Unit<T>::kMinusInf, Unit<T>::kMinusInf, Unit<T>::kMinusInf);
+                if (first + 32 * i < u1) v[i] = kStaged ? stage[k * kChunkUnits + lane + 32 * i] : ld_unit(row.base + first + 32 * i);
+            }
+            if (row.ragged && (first < kChunkUnits || first - lane + kChunkUnits >= row.units)) {      // can hold an end of the row
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i)
+                    if (first + 32 * i < u1) row.mask(v[i], first + 32 * i);
+            }
             if (kTail) {
 #pragma unroll
                 for (uint32_t i = 0; i < 4; ++i) {
-                    const uint32_t u = first + i * kThreads, bits = u < u1 ? marked(u) : 0u;
+                    const uint32_t u = first + 32 * i, bits = u < u1 ? marked(u) : 0u;
                     if (bits) {
 #pragma unroll
                         for (uint32_t e = 0; e < E; ++e)
@@ -116,10 +170,14 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                     }
                 }
             }
+            if (kStaged && !grad) {
+                __syncwarp();                              // every lane has its units
+                if (more) fetch_chunk(next_row, next_slice, k);
+            }
             const float best = fmaxf(Unit<T>::best(v[0], v[2]), Unit<T>::best(v[1], v[3]));
             x_best = fmaxf(x_best, best);
             sums.add<T, false>(v, best, a.c);
-        });
+        }
         const RowPart mine = sums.part(warp_max(x_best), a.c);
 
         // the slots: the teacher's values, and (kTail) the student's at the slice's named columns, each column once
@@ -212,7 +270,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         } else {
             log_norm = teacher.xmax + logf(teacher.s);
         }
-        const bool broken = log_total != log_total || teacher.s != teacher.s;
+        const bool broken = log_total != log_total || teacher.s != teacher.s || gave_up;
         const bool nothing = (!broken && z_max == minus_inf()) || (!kTail && teacher.s == 0.0f);
         const bool remainder = kTail && student.s != 0.0f;
         auto log_p = [&](uint32_t i) { return fmaf(logit(i), a.inv_t, -z_max) - log_total; };
@@ -240,15 +298,19 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             if (nothing) factor = 0.0f;
             const float x_ref = student.xmax == minus_inf() ? 0.0f : -student.xmax;
             const uint64_t shift = pack2(x_ref, x_ref), by_c = pack2(a.c, a.c), by_factor = pack2(factor, factor);
-            for (uint32_t batch = u0; batch < u1; batch += 4 * kThreads) {
-                const uint32_t first = batch + tid;
+            for (uint32_t k = warp; u0 + k * kChunkUnits < u1; k += kWarps) {
+                const uint32_t first = u0 + k * kChunkUnits + lane;
                 uint4 v[4];
 #pragma unroll
                 for (uint32_t i = 0; i < 4; ++i)
-                    if (first + i * kThreads < u1) v[i] = ld_unit(row.base + first + i * kThreads);
+                    if (first + 32 * i < u1) v[i] = kStaged ? stage[k * kChunkUnits + lane + 32 * i] : ld_unit(row.base + first + 32 * i);
+                if (kStaged) {
+                    __syncwarp();                          // every lane has its units
+                    if (more) fetch_chunk(next_row, next_slice, k);
+                }
 #pragma unroll
                 for (uint32_t i = 0; i < 4; ++i) {
-                    const uint32_t u = first + i * kThreads;
+                    const uint32_t u = first + 32 * i;
                     if (u >= u1) break;
                     float g[E];
 #pragma unroll
@@ -267,6 +329,10 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                 }
             }
         }
+        // (a row may have a chunk more than the one before it)
+        if (kStaged && more)
+            for (uint32_t k = warp; k < a.chunks; k += kWarps)
+                if (u0 + k * kChunkUnits >= u1) fetch_chunk(next_row, next_slice, k);
         __syncthreads();                                   // the gradient is written, the loss' parts are there
 
         if (a.loss_out && rank == 0 && warp == 0) {
@@ -285,49 +351,73 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                     if (ids[k] == ids[i]) q += expf(log_q(k));
             out[ids[i]] = from_f32<T>(broken ? __uint_as_float(0x7FFFFFFFu) : (expf(log_p(i)) - q) * scale);
         }
-        if (tid == 0) repeated_flag = 0;
+        if (tid == 0) {
+            repeated_flag = 0;
+            if (gave_up && a.result) atomicMax(&a.result->status, static_cast<uint32_t>(DCT_ERR_TIMEOUT));
+        }
         if (kCluster) cluster_wait();
         if (!more) break;
         row_id += clusters;
     }
+    // no copy may land in the shared memory of a CTA that is gone
+    if (kStaged && missed && lane == 0)
+        for (uint32_t j = 0; j < kMaxChunksPerWarp; ++j)
+            for (uint32_t i = 0; (missed >> j & 1u) && i < a.spin_limit; ++i)
+                if (mbar_try_wait(&arrived[warp * kMaxChunksPerWarp + j], phases >> j & 1u)) break;
 }
 
-template <typename T, uint32_t kThreads, bool kTail>
-dct_status_t launch_distill_threads(const void* logits, void* grad, DistillArgs a, uint32_t cluster, cudaStream_t stream) {
+template <typename T, uint32_t kThreads, bool kTail, bool kCluster, bool kStaged>
+dct_status_t launch_distill_shape(const void* logits, void* grad, const DistillArgs& a, uint32_t cluster, cudaStream_t stream) {
     const int sms = sm_count();
     if (sms <= 0) return DCT_ERR_CUDA;
-    const uint32_t units = a.vocab / Unit<T>::kElems + 2, share = (units + cluster - 1) / cluster;
-    a.mark_words = ((share * Unit<T>::kElems + 31) / 32 + 3) & ~3u;
-    const size_t smem = 4 * static_cast<size_t>(a.mark_words) + 20 * static_cast<size_t>(a.top);
-    const T* x = static_cast<const T*>(logits);
-    T* g = static_cast<T*>(grad);
-    const uint64_t wanted = static_cast<uint64_t>(a.rows) * cluster;
-    const uint32_t room = static_cast<uint32_t>(sms) * (768 / kThreads) / cluster * cluster;
-    const uint32_t grid = static_cast<uint32_t>(wanted < room ? wanted : room);
-    if (cluster > 1) {
-        auto kernel = lm_distill_kernel<T, kThreads, kTail, true>;
-        if (smem > 32 * 1024)
-            DCT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-        DCT_CUDA_TRY(launch_clusters(kernel, grid, kThreads, cluster, smem, stream, x, g, a));
-        return DCT_OK;
-    }
-    auto kernel = lm_distill_kernel<T, kThreads, kTail, false>;
+    const size_t smem = (kStaged ? static_cast<size_t>(a.chunks) * kChunkBytes : 0) + 4 * static_cast<size_t>(a.mark_words) +
+                        20 * static_cast<size_t>(a.top);
+    auto kernel = lm_distill_kernel<T, kThreads, kTail, kCluster, kStaged>;
     if (smem > 32 * 1024)
         DCT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-    kernel<<<grid, kThreads, smem, stream>>>(x, g, a);
-    DCT_CUDA_TRY(cudaGetLastError());
+    uint32_t per_sm = static_cast<uint32_t>((227 * 1024) / (smem + 3 * 1024));
+    per_sm = per_sm < 1 ? 1 : per_sm < 768 / kThreads ? per_sm : 768 / kThreads;
+    const T* x = static_cast<const T*>(logits);
+    T* g = static_cast<T*>(grad);
+    uint32_t at_once = static_cast<uint32_t>(sms) * per_sm;
+    if (kCluster) {
+        static std::atomic<uint32_t> kept[768 / kThreads + 1][3];
+        const dct_status_t st = clusters_at_once(kernel, kThreads, cluster, smem, kept[per_sm], &at_once);
+        if (st != DCT_OK) return st;
+    }
+    const uint32_t grid = (a.rows < at_once ? a.rows : at_once) * cluster;
+    if (kCluster) {
+        DCT_CUDA_TRY(launch_clusters(kernel, grid, kThreads, cluster, smem, stream, x, g, a));
+    } else {
+        kernel<<<grid, kThreads, smem, stream>>>(x, g, a);
+        DCT_CUDA_TRY(cudaGetLastError());
+    }
     return DCT_OK;
 }
 
 template <typename T, bool kTail>
-dct_status_t launch_distill(const void* logits, void* grad, const DistillArgs& a, cudaStream_t stream) {
+dct_status_t launch_distill(const void* logits, void* grad, DistillArgs a, cudaStream_t stream) {
     const int sms = sm_count();
     if (sms <= 0) return DCT_ERR_CUDA;
-    const uint32_t units = a.vocab / Unit<T>::kElems + 2;
+    const uint32_t units = a.vocab / Unit<T>::kElems + 2, chunks = (units + kChunkUnits - 1) / kChunkUnits;
+    // Slices of at most about 66 KiB leave room for three CTAs of eight warps on an SM; few rows are split further, while each
+    // CTA still has a chunk per warp.
     uint32_t cluster = 1;
-    while (cluster < kMaxCluster && static_cast<uint64_t>(a.rows) * cluster * 2 <= 3ull * sms && units / (cluster * 2) >= 512) cluster *= 2;
-    while (cluster < kMaxCluster && units / cluster > 16384) cluster *= 2;
-    return launch_distill_threads<T, 256, kTail>(logits, grad, a, cluster, stream);
+    while (cluster < kMaxCluster && (chunks > 34 * cluster || (static_cast<uint64_t>(a.rows) * cluster * 2 <= 3ull * sms && chunks >= 16 * cluster)))
+        cluster *= 2;
+    const uint32_t share = (units + cluster - 1) / cluster;
+    a.chunks = (share + kChunkUnits - 1) / kChunkUnits;
+    a.mark_words = ((share * Unit<T>::kElems + 31) / 32 + 3) & ~3u;
+    a.spin_limit = debug_config().spin_limit;
+    const bool staged = static_cast<size_t>(a.chunks) * kChunkBytes + 4 * a.mark_words + 20 * a.top <= kStagedLimit &&
+                        a.chunks <= 8 * kMaxChunksPerWarp;
+    if (!staged) return launch_distill_shape<T, 256, kTail, true, false>(logits, grad, a, cluster, stream);
+    if (cluster > 1) return launch_distill_shape<T, 256, kTail, true, true>(logits, grad, a, cluster, stream);
+    // about four chunks to a warp
+    if (a.chunks <= 5) return launch_distill_shape<T, 32, kTail, false, true>(logits, grad, a, 1, stream);
+    if (a.chunks <= 10) return launch_distill_shape<T, 64, kTail, false, true>(logits, grad, a, 1, stream);
+    if (a.chunks <= 20) return launch_distill_shape<T, 128, kTail, false, true>(logits, grad, a, 1, stream);
+    return launch_distill_shape<T, 256, kTail, false, true>(logits, grad, a, 1, stream);
 }
 
 }  // namespace
@@ -357,7 +447,7 @@ extern "C" dct_status_t dct_lm_distill(const void* logits, dct_dtype_t dtype, ui
     if (result) DCT_CUDA_TRY(cudaMemsetAsync(result, 0, sizeof(dct_result_t), stream));
     if (rows == 0) return DCT_OK;
     const DistillArgs args{rows, vocab, ld, inv_temperature, log2_scale(inv_temperature), teacher_ids, teacher_logprobs, top,
-                           grad_loss, loss_out, ld_grad, 0, result};
+                           grad_loss, loss_out, ld_grad, 0, 0, 0, result};
     auto launch = dtype == DCT_F32
         ? (mode == DCT_DISTILL_TAIL ? launch_distill<float, true> : launch_distill<float, false>)
         : (mode == DCT_DISTILL_TAIL ? launch_distill<__nv_bfloat16, true> : launch_distill<__nv_bfloat16, false>);

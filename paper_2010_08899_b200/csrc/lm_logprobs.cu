@@ -515,15 +515,18 @@ lm_logprobs_bwd_kernel(const T* logits, T* grad, const LogProbBwdArgs q) {
 template <typename T, uint32_t kThreads>
 dct_status_t launch_logprobs_threads(const void* logits, const LogProbArgs& a, uint32_t cluster, uint32_t ctas, cudaStream_t stream) {
     const T* x = static_cast<const T*>(logits);
-    const uint64_t wanted = static_cast<uint64_t>(a.rows) * cluster, room = ctas / cluster * cluster;
-    const uint32_t grid = static_cast<uint32_t>(wanted < room ? wanted : room);
-    if constexpr (kThreads > 128) {
+    if constexpr (kThreads == 256) {
         if (cluster > 1) {
-            DCT_CUDA_TRY(launch_clusters(lm_logprobs_kernel<T, kThreads, true>, grid, kThreads, cluster, 0, stream, x, a));
+            static std::atomic<uint32_t> kept[3];
+            auto kernel = lm_logprobs_kernel<T, kThreads, true>;
+            uint32_t at_once = 1;
+            const dct_status_t st = clusters_at_once(kernel, kThreads, cluster, 0, kept, &at_once);
+            if (st != DCT_OK) return st;
+            DCT_CUDA_TRY(launch_clusters(kernel, (a.rows < at_once ? a.rows : at_once) * cluster, kThreads, cluster, 0, stream, x, a));
             return DCT_OK;
         }
     }
-    lm_logprobs_kernel<T, kThreads, false><<<grid, kThreads, 0, stream>>>(x, a);
+    lm_logprobs_kernel<T, kThreads, false><<<a.rows < ctas ? a.rows : ctas, kThreads, 0, stream>>>(x, a);
     DCT_CUDA_TRY(cudaGetLastError());
     return DCT_OK;
 }

@@ -1,6 +1,7 @@
 // Pieces shared by the layer norm and by the calls on rows of logits: element types, sums over a CTA in a fixed
 // order, the order of logits, and the host's argument checks.
 #pragma once
+#include <atomic>
 #include <cmath>
 
 #include "common.cuh"
@@ -435,6 +436,35 @@ __device__ __forceinline__ uint64_t ld_remote_u64(uint32_t a) {
 }
 
 // Host side ---------------------------------------------------------------------------------------------------
+
+// How many clusters of `cluster` (2, 4 or 8) CTAs the current device holds at a time.  A GPC's SMs are no multiple of a cluster, so
+// this is less than the CTAs that fit divided by the cluster; a persistent grid of more would run its last clusters after
+// all others.  kept: one word per cluster size, zero at first, for launches that differ in nothing that matters here.
+template <typename... Params>
+inline dct_status_t clusters_at_once(void (*kernel)(Params...), unsigned block, unsigned cluster, size_t smem,
+                                     std::atomic<uint32_t> (&kept)[3], uint32_t* out) {
+    std::atomic<uint32_t>& word = kept[cluster == 2 ? 0 : cluster == 4 ? 1 : 2];
+    uint32_t n = word.load(std::memory_order_relaxed);
+    if (n == 0) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(cluster);
+        cfg.blockDim = dim3(block);
+        cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute shape = {};
+        shape.id = cudaLaunchAttributeClusterDimension;
+        shape.val.clusterDim.x = cluster;
+        shape.val.clusterDim.y = 1;
+        shape.val.clusterDim.z = 1;
+        cfg.attrs = &shape;
+        cfg.numAttrs = 1;
+        int found = 0;
+        DCT_CUDA_TRY(cudaOccupancyMaxActiveClusters(&found, kernel, &cfg));
+        n = found > 0 ? static_cast<uint32_t>(found) : 1u;
+        word.store(n, std::memory_order_relaxed);
+    }
+    *out = n;
+    return DCT_OK;
+}
 
 // launches `kernel` in clusters of `cluster` CTAs
 template <typename... Params, typename... Args>
