@@ -46,9 +46,9 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads)
 lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
     constexpr uint32_t E = Unit<T>::kElems, kWarps = kThreads / 32;
     extern __shared__ __align__(128) uint32_t dynamic[];
-    __shared__ RowPart student_parts[kWarps], teacher_parts[kWarps], named_parts[kWarps], slice_part, slice_named;
+    __shared__ RowPart student_parts[kWarps], named_parts[kWarps], slice_part, slice_named;
     __shared__ float loss_parts[kWarps];
-    __shared__ uint32_t repeated_flag, gave_up;
+    __shared__ uint32_t repeated_flag, weight_flag, nan_flag, gave_up;      // of the row's slots; a wait ran out
     __shared__ uint64_t arrived[kStaged ? kWarps * kMaxChunksPerWarp : 1];
     uint4* const stage = reinterpret_cast<uint4*>(dynamic);
     uint32_t* const marks = dynamic + (kStaged ? a.chunks * (kChunkBytes / 4) : 0);
@@ -78,7 +78,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         }
     };
     uint32_t row_id = blockIdx.x / ctas;
-    if (tid == 0) repeated_flag = gave_up = 0;
+    if (tid == 0) repeated_flag = weight_flag = nan_flag = gave_up = 0;
     __syncthreads();
     if (kStaged) {
         if (lane == 0) {
@@ -100,6 +100,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         const uint32_t u0 = slice.u0, u1 = slice.u1;
         const int32_t* ids = ids_by_turn + turn * a.top;
         const float* t_s = t_by_turn + turn * a.top;
+        const float scale = __fmul_rn(a.grad_loss ? __ldg(a.grad_loss + row_id) : 1.0f, a.inv_t);
         copy_wait<0>();
         __syncthreads();                                   // the last row's marks are gone, its numbers are read
 
@@ -114,6 +115,8 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                 bad |= ids[i] >= 0;
                 continue;
             }
+            if (t_s[i] > minus_inf()) weight_flag = 1;
+            if (t_s[i] != t_s[i]) nan_flag = 1;
             const uintptr_t x = reinterpret_cast<uintptr_t>(xr + ids[i]);
             copy_word_async(z_words + i, reinterpret_cast<const void*>(x & ~static_cast<uintptr_t>(3)));
             if (in_slice(i)) {
@@ -131,9 +134,11 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         if (kTail) __syncthreads();                        // all marks are set
 
         // first reading: the student's sums
-        auto marked = [&](uint32_t u) {
-            const uint32_t at = (u - u0) * E;
-            return marks[at >> 5] >> (at & 31) & ((1u << E) - 1);
+        // (a unit's marks: a byte of bf16, half a byte of fp32)
+        auto marked = [&](uint32_t u) -> uint32_t {
+            const uint8_t* bytes = reinterpret_cast<const uint8_t*>(marks);
+            if (sizeof(T) == 2) return bytes[u - u0];
+            return bytes[(u - u0) >> 1] >> ((u - u0) & 1u) * 4 & 15u;
         };
         RowSums sums;
         float x_best = minus_inf();
@@ -149,10 +154,16 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                     phases ^= 1u << j;
                 }
             }
+            const uint4* from = kStaged ? stage + k * kChunkUnits + lane : row.base + first;
+            if (first - lane + kChunkUnits <= u1) {        // a whole chunk
 #pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) {
-                v[i] = make_uint4(Unit<T>::kMinusInf, Unit<T>::kMinusInf, Unit<T>::kMinusInf, Unit<T>::kMinusInf);
-                if (first + 32 * i < u1) v[i] = kStaged ? stage[k * kChunkUnits + lane + 32 * i] : ld_unit(row.base + first + 32 * i);
+                for (uint32_t i = 0; i < 4; ++i) v[i] = kStaged ? from[32 * i] : ld_unit(from + 32 * i);
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    v[i] = make_uint4(Unit<T>::kMinusInf, Unit<T>::kMinusInf, Unit<T>::kMinusInf, Unit<T>::kMinusInf);
+                    if (first + 32 * i < u1) v[i] = kStaged ? from[32 * i] : ld_unit(from + 32 * i);
+                }
             }
             if (row.ragged && (first < kChunkUnits || first - lane + kChunkUnits >= row.units)) {      // can hold an end of the row
 #pragma unroll
@@ -160,14 +171,15 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                     if (first + 32 * i < u1) row.mask(v[i], first + 32 * i);
             }
             if (kTail) {
+                uint32_t bits[4];
 #pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    const uint32_t u = first + 32 * i, bits = u < u1 ? marked(u) : 0u;
-                    if (bits) {
+                for (uint32_t i = 0; i < 4; ++i) bits[i] = marked(min(first + 32 * i, u1 - 1));
+                if (bits[0] | bits[1] | bits[2] | bits[3]) {
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i)
 #pragma unroll
                         for (uint32_t e = 0; e < E; ++e)
-                            if (bits >> e & 1u) Unit<T>::set(v[i], e, minus_inf());
-                    }
+                            if (bits[i] >> e & 1u) Unit<T>::set(v[i], e, minus_inf());
                 }
             }
             if (kStaged && !grad) {
@@ -178,7 +190,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             x_best = fmaxf(x_best, best);
             sums.add<T, false>(v, best, a.c);
         }
-        const RowPart mine = sums.part(warp_max(x_best), a.c);
+        const RowPart mine = sums.part<false>(warp_max(x_best), a.c);
 
         // the slots: the teacher's values, and (kTail) the student's at the slice's named columns, each column once
         copy_wait<1>();
@@ -192,36 +204,30 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                 if (ids[k] == ids[i]) return false;
             return true;
         };
-        RowPart teacher{minus_inf(), 0.0f, 0.0f}, named{minus_inf(), 0.0f, 0.0f};
+        RowPart named{minus_inf(), 0.0f, 0.0f};
         float q_sum = 0.0f;
-        {
-            const bool repeated = kTail && repeated_flag != 0;
+        if (kTail) {
+            const bool repeated = repeated_flag != 0;
             for (uint32_t i = tid; i < a.top; i += kThreads) {
                 if (!inside(i)) continue;
-                if (kTail) {
-                    q_sum += expf(t_s[i]);
-                    if (in_slice(i) && (!repeated || first_of_its_column(i))) add_value(named, __fmul_rn(logit(i), a.inv_t));
-                } else {
-                    add_value(teacher, t_s[i]);
-                }
+                q_sum += expf(t_s[i]);
+                if (in_slice(i) && (!repeated || first_of_its_column(i))) add_value(named, __fmul_rn(logit(i), a.inv_t));
             }
-        }
-        if (kTail) {
             q_sum = warp_join<SumOp>(q_sum);
-            named.join_lanes(kLog2E, 32);
-        } else {
-            teacher.join_lanes(kLog2E, 32);
+            named.join_lanes<32, false>(kLog2E);
         }
         if (lane == 0) {
             student_parts[warp] = mine;
-            teacher_parts[warp] = kTail ? RowPart{0.0f, q_sum, 0.0f} : teacher;
-            if (kTail) named_parts[warp] = named;
+            if (kTail) {
+                named.st = q_sum;
+                named_parts[warp] = named;
+            }
         }
         __syncthreads();
 
         // every warp joins the parts of all
         RowPart student = student_parts[lane & (kWarps - 1)];
-        student.join_lanes(a.c, kWarps);
+        student.join_lanes<kWarps, false>(a.c);
         if (student.s == 0.0f && student.xmax > minus_inf())
             student = low_part(row, u0, u1, student.xmax, a.c, [=](uint32_t u, uint32_t i) {
                 const uint32_t at = (u - u0) * E + i;
@@ -229,7 +235,11 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             });
         if (kTail) {
             named = named_parts[lane & (kWarps - 1)];
-            named.join_lanes(kLog2E, kWarps);
+            q_sum = named.st;
+#pragma unroll
+            for (uint32_t o = kWarps / 2; o > 0; o >>= 1) q_sum = __fadd_rn(q_sum, __shfl_xor_sync(0xFFFFFFFFu, q_sum, o));
+            named.st = 0.0f;
+            named.join_lanes<kWarps, false>(kLog2E);
         }
         if (kCluster) {
             if (tid == 0) {
@@ -247,13 +257,20 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                     named.s = ld_remote_f32(remote_smem(&slice_named.s, c));
                 }
             }
-            student.join_lanes(a.c, kMaxCluster);
-            if (kTail) named.join_lanes(kLog2E, kMaxCluster);
+            student.join_lanes<kMaxCluster, false>(a.c);
+            if (kTail) named.join_lanes<kMaxCluster, false>(kLog2E);
             cluster_arrive();                              // (waited for at the end of the row)
         }
-        teacher = teacher_parts[lane & (kWarps - 1)];
-        teacher.join_lanes(kLog2E, kWarps);                // (kTail: all xmax are 0, s becomes the sum of q)
+        // the norm of the teacher's values: the warps that have slots find it for themselves
+        RowPart teacher{minus_inf(), 0.0f, 0.0f};
+        if (!kTail && warp * 32 < a.top) {
+            for (uint32_t i = lane; i < a.top; i += 32)
+                if (inside(i)) add_value(teacher, t_s[i]);
+            __syncwarp();
+            teacher.join_lanes<32, false>(kLog2E);
+        }
         const bool repeated = repeated_flag != 0;
+        const bool no_teacher = !kTail && !weight_flag && !nan_flag;
 
         // log Z = z_max + log_total; the streamed columns' share p_streamed of the student's distribution (1 unless kTail)
         const float z_streamed = __fmul_rn(student.xmax, a.inv_t), exact_rest = fmaf(student.xmax, a.inv_t, -z_streamed);
@@ -266,12 +283,12 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             if (student.s != 0.0f) total += expf((z_streamed - z_max) + log_s);
             log_total = logf(total);
             log_streamed = (z_streamed - z_max) + (log_s - log_total);
-            q_rest = teacher.s > 1.0f ? 0.0f : 1.0f - teacher.s;
+            q_rest = q_sum > 1.0f ? 0.0f : 1.0f - q_sum;
         } else {
             log_norm = teacher.xmax + logf(teacher.s);
         }
-        const bool broken = log_total != log_total || teacher.s != teacher.s || gave_up;
-        const bool nothing = (!broken && z_max == minus_inf()) || (!kTail && teacher.s == 0.0f);
+        const bool broken = log_total != log_total || nan_flag || gave_up;
+        const bool nothing = (!broken && z_max == minus_inf()) || no_teacher;
         const bool remainder = kTail && student.s != 0.0f;
         auto log_p = [&](uint32_t i) { return fmaf(logit(i), a.inv_t, -z_max) - log_total; };
         auto log_q = [&](uint32_t i) { return t_s[i] - log_norm; };
@@ -288,45 +305,57 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             if (lane == 0) loss_parts[warp] = loss;
         }
         T* out = grad + static_cast<size_t>(row_id) * a.ld_grad;
-        const float scale = __fmul_rn(a.grad_loss ? a.grad_loss[row_id] : 1.0f, a.inv_t);
         if (grad) {
             // second reading: 2^((x - xmax) c) times one factor
             const bool aligned = same_boundary(xr, out);
             float factor = scale / student.s;
             if (kTail) factor = remainder ? factor * (expf(log_streamed) - q_rest) : 0.0f;
             if (broken) factor = __uint_as_float(0x7FFFFFFFu);
-            if (nothing) factor = 0.0f;
-            const float x_ref = student.xmax == minus_inf() ? 0.0f : -student.xmax;
-            const uint64_t shift = pack2(x_ref, x_ref), by_c = pack2(a.c, a.c), by_factor = pack2(factor, factor);
-            for (uint32_t k = warp; u0 + k * kChunkUnits < u1; k += kWarps) {
-                const uint32_t first = u0 + k * kChunkUnits + lane;
-                uint4 v[4];
+            auto write_chunks = [&](auto&& two) {
+                for (uint32_t k = warp; u0 + k * kChunkUnits < u1; k += kWarps) {
+                    const uint32_t first = u0 + k * kChunkUnits + lane;
+                    uint4 v[4];
+                    const uint4* from = kStaged ? stage + k * kChunkUnits + lane : row.base + first;
+                    // (a whole chunk inside the row, laid out alike: no unit needs a look)
+                    const bool whole = aligned && first - lane + kChunkUnits <= u1 &&
+                                       (!row.ragged || (first >= kChunkUnits && first - lane + kChunkUnits < row.units));
 #pragma unroll
-                for (uint32_t i = 0; i < 4; ++i)
-                    if (first + 32 * i < u1) v[i] = kStaged ? stage[k * kChunkUnits + lane + 32 * i] : ld_unit(row.base + first + 32 * i);
-                if (kStaged) {
-                    __syncwarp();                          // every lane has its units
-                    if (more) fetch_chunk(next_row, next_slice, k);
-                }
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    const uint32_t u = first + 32 * i;
-                    if (u >= u1) break;
-                    float g[E];
-#pragma unroll
-                    for (uint32_t e = 0; e < E; e += 2) {
-                        float y0, y1;
-                        unpack2(mul2(add2(pack2(Unit<T>::get(v[i], e), Unit<T>::get(v[i], e + 1)), shift), by_c), y0, y1);
-                        // (a named column may be far above the others that the factor belongs to: written again below)
-                        if (kTail) {
-                            y0 = fminf(y0, 64.0f);
-                            y1 = fminf(y1, 64.0f);
-                        }
-                        unpack2(mul2(pack2(exp2_fast(y0), exp2_fast(y1)), by_factor), g[e], g[e + 1]);
-                        if (nothing) g[e] = g[e + 1] = 0.0f;            // whatever the logits are
+                    for (uint32_t i = 0; i < 4; ++i)
+                        if (whole || first + 32 * i < u1) v[i] = kStaged ? from[32 * i] : ld_unit(from + 32 * i);
+                    if (kStaged) {
+                        __syncwarp();                      // every lane has its units
+                        if (more) fetch_chunk(next_row, next_slice, k);
                     }
-                    store_unit(row, out, u, g, aligned);
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        float g[E];
+#pragma unroll
+                        for (uint32_t e = 0; e < E; e += 2)
+                            unpack2(two(pack2(Unit<T>::get(v[i], e), Unit<T>::get(v[i], e + 1))), g[e], g[e + 1]);
+                        if (whole) st_unit(out + row.column(first + 32 * i, 0), Unit<T>::pack(g));
+                        else if (first + 32 * i < u1) store_unit(row, out, first + 32 * i, g, aligned);
+                    }
                 }
+            };
+            const float ref = __fmul_rn(student.xmax, a.c);
+            const uint64_t by_c = pack2(a.c, a.c);
+            // (a named column may be far above the others, whose factor this is: it is written again below)
+            auto powers = [&](uint64_t y) {
+                float y0, y1;
+                unpack2(y, y0, y1);
+                return kTail ? pack2(exp2_fast(fminf(y0, 64.0f)), exp2_fast(fminf(y1, 64.0f))) : pack2(exp2_fast(y0), exp2_fast(y1));
+            };
+            if (nothing) {                                 // whatever the logits are
+                write_chunks([](uint64_t) { return 0ull; });
+            } else if (fabsf(ref) <= 3.0e38f) {
+                // x c - ref instead of (x - xmax) c, what xmax c is off ref by goes into the factor
+                factor *= exp2_fast(-fmaf(student.xmax, a.c, -ref));
+                const uint64_t shift = pack2(-ref, -ref), by_factor = pack2(factor, factor);
+                write_chunks([&](uint64_t x) { return mul2(powers(fma2(x, by_c, shift)), by_factor); });
+            } else {                                       // values whose product with c overflows, or none but -inf
+                const float x_ref = student.xmax == minus_inf() ? 0.0f : -student.xmax;
+                const uint64_t shift = pack2(x_ref, x_ref), by_factor = pack2(factor, factor);
+                write_chunks([&](uint64_t x) { return mul2(powers(mul2(add2(x, shift), by_c)), by_factor); });
             }
         }
         // (a row may have a chunk more than the one before it)
@@ -352,7 +381,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             out[ids[i]] = from_f32<T>(broken ? __uint_as_float(0x7FFFFFFFu) : (expf(log_p(i)) - q) * scale);
         }
         if (tid == 0) {
-            repeated_flag = 0;
+            repeated_flag = weight_flag = nan_flag = 0;
             if (gave_up && a.result) atomicMax(&a.result->status, static_cast<uint32_t>(DCT_ERR_TIMEOUT));
         }
         if (kCluster) cluster_wait();

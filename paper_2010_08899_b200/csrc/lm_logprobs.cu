@@ -365,7 +365,7 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
             sh.class_max[tid] = max0;
             sh.class_max[kThreads + tid] = max1;
         }
-        const RowPart mine = sums.part(warp_max(fmaxf(max0, max1)), a.c);
+        const RowPart mine = sums.part<true>(warp_max(fmaxf(max0, max1)), a.c);
         if (lane == 0) sh.warp_part[turn][warp] = mine;
         __syncthreads();
 
@@ -373,7 +373,7 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
         // for the bound of the selection
         if (warp == kWarps - 1) {
             RowPart all = sh.warp_part[turn][lane & (kWarps - 1)];
-            all.join_lanes(a.c, kWarps);
+            all.join_lanes<kWarps, true>(a.c);
             if (all.s == 0.0f && all.xmax > minus_inf()) {
                 all = low_part(row, u0, u1, all.xmax, a.c, [](uint32_t, uint32_t) { return true; });
             }
@@ -392,12 +392,13 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
             cluster_barrier();
             if (warp == kWarps - 1) {
                 RowPart all{minus_inf(), 0.0f, 0.0f};
-                if (lane < ctas) {
-                    all.xmax = ld_remote_f32(remote_smem(&sh.part.xmax, lane));
-                    all.s = ld_remote_f32(remote_smem(&sh.part.s, lane));
-                    all.st = ld_remote_f32(remote_smem(&sh.part.st, lane));
+                const uint32_t c = lane & (kMaxCluster - 1);
+                if (c < ctas) {
+                    all.xmax = ld_remote_f32(remote_smem(&sh.part.xmax, c));
+                    all.s = ld_remote_f32(remote_smem(&sh.part.s, c));
+                    all.st = ld_remote_f32(remote_smem(&sh.part.st, c));
                 }
-                all.join_lanes(a.c, kMaxCluster);
+                all.join_lanes<kMaxCluster, true>(a.c);
                 if (lane == 0) {
                     LogProbArgs mine = a;
                     if (rank != 0) {

@@ -108,6 +108,9 @@ template <> struct Unit<float> {
         const uint32_t u = __float_as_uint(x);
         if (i == 0) v.x = u; else if (i == 1) v.y = u; else if (i == 2) v.z = u; else v.w = u;
     }
+    __device__ static __forceinline__ uint4 pack(const float (&g)[4]) {
+        return make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
+    }
     // the largest element, NaN only if all are
     __device__ static __forceinline__ float best(const uint4& a) {
         return fmaxf(fmaxf(get(a, 0), get(a, 1)), fmaxf(get(a, 2), get(a, 3)));
@@ -127,6 +130,15 @@ template <> struct Unit<__nv_bfloat16> {
         uint32_t w = word(v, i >> 1);
         w = i & 1 ? (w & 0xFFFFu) | u << 16 : (w & 0xFFFF0000u) | u;
         if (i >> 1 == 0) v.x = w; else if (i >> 1 == 1) v.y = w; else if (i >> 1 == 2) v.z = w; else v.w = w;
+    }
+    __device__ static __forceinline__ uint4 pack(const float (&g)[8]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(g[2 * i], g[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
     __device__ static __forceinline__ __nv_bfloat162 pair(uint32_t w) { return *reinterpret_cast<__nv_bfloat162*>(&w); }
     __device__ static __forceinline__ __nv_bfloat162 best2(const uint4& v) {
@@ -198,19 +210,7 @@ template <typename T>
 __device__ __forceinline__ void store_unit(const RowView<T>& row, T* out, uint32_t u, const float (&g)[Unit<T>::kElems], bool aligned) {
     constexpr uint32_t E = Unit<T>::kElems;
     if (aligned && !row.at_an_end(u)) {
-        uint4 v;
-        if constexpr (sizeof(T) == 4) {
-            v = make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
-        } else {
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(g[2 * i], g[2 * i + 1]);
-                w[i] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            v = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        st_unit(out + row.column(u, 0), v);
+        st_unit(out + row.column(u, 0), Unit<T>::pack(g));
     } else {
 #pragma unroll
         for (uint32_t i = 0; i < E; ++i) {
@@ -245,14 +245,14 @@ struct RowPart {
         }
         xmax = to;
     }
-    // joins the parts of `lanes` (a power of two) neighbouring lanes, in a fixed order; all lanes get the result
-    __device__ __forceinline__ void join_lanes(float c, int lanes) {
-        float m = xmax;
-        for (int o = lanes / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-        raise(m, c);
-        for (int o = lanes / 2; o > 0; o >>= 1) {
+    // joins the parts of kLanes (a power of two) neighbouring lanes, in a fixed order; all lanes get the result.  (Every group of
+    // kLanes lanes holds the same parts, so the warp's largest x is the group's.)
+    template <int kLanes, bool kMoment> __device__ __forceinline__ void join_lanes(float c) {
+        raise(kLanes == 1 ? xmax : warp_max(xmax), c);
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o >>= 1) {
             s = __fadd_rn(s, __shfl_xor_sync(0xFFFFFFFFu, s, o));
-            st = __fadd_rn(st, __shfl_xor_sync(0xFFFFFFFFu, st, o));
+            if (kMoment) st = __fadd_rn(st, __shfl_xor_sync(0xFFFFFFFFu, st, o));
         }
     }
 };
@@ -273,7 +273,7 @@ __device__ __noinline__ RowPart low_part(const RowView<T> row, uint32_t u0, uint
             }
     }
     __syncwarp();
-    p.join_lanes(c, 32);
+    p.join_lanes<32, true>(c);
     return p;
 }
 
@@ -342,8 +342,8 @@ struct RowSums {
         }
     }
     // the warp's sums as a part; xmax: the warp's largest x
-    __device__ __forceinline__ RowPart part(float xmax, float c) const {
-        RowPart r{xmax, warp_join<SumOp>(s), warp_join<SumOp>(st)};
+    template <bool kMoment> __device__ __forceinline__ RowPart part(float xmax, float c) const {
+        RowPart r{xmax, warp_join<SumOp>(s), kMoment ? warp_join<SumOp>(st) : 0.0f};
         if (ref != minus_inf()) {
             // |xmax c - ref| <= kSlack; the factor puts the sums where 2^y of the largest x is 1
             const float d = fmaf(xmax, c, -ref), f = exp2_fast(-d);
