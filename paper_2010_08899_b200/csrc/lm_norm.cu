@@ -6,7 +6,434 @@ namespace {
 
 constexpr uint32_t kNormMaxWidth = 65536u;
 constexpr uint32_t kNormThreads = 256u;
-constexpr uint32_t kNormMaxParts = 592u;
+constexpr uint32_t kMaxParts = 148u * 4u;        // CTAs that leave partial sums of the parameter gradients, at most
+
+// Rows as units of 16 bytes counted from the row's own first element.  Where a row does not start on a 16-byte boundary, a unit is
+// put together from the two aligned pieces it lies in; these are inside the row but for the bytes next to its ends, which share
+// a 16-byte piece (and so a page) with it.
+
+// the 16 bytes that start `by` bytes into a, b (by = 0, 2, ... 14)
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, uint32_t by) {
+    uint32_t w0 = a.x, w1 = a.y, w2 = a.z, w3 = a.w, w4 = b.x, w5 = b.y, w6 = b.z;
+    const uint32_t w7 = b.w;
+    if (by & 8u) { w0 = w2; w1 = w3; w2 = w4; w3 = w5; w4 = w6; w5 = w7; }
+    if (by & 4u) { w0 = w1; w1 = w2; w2 = w3; w3 = w4; w4 = w5; }
+    const uint32_t bits = (by & 2u) * 8u;
+    return make_uint4(__funnelshift_r(w0, w1, bits), __funnelshift_r(w1, w2, bits), __funnelshift_r(w2, w3, bits),
+                      __funnelshift_r(w3, w4, bits));
+}
+
+template <typename T> struct NormRow {
+    const uint4* base;         // the boundary at or before the row's first element
+    uint32_t off;              // bytes from there to it
+    uint32_t pieces;           // aligned pieces that hold a part of the row
+    __device__ __forceinline__ NormRow(const T* row, uint32_t d) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(row);
+        off = static_cast<uint32_t>(at & 15u);
+        base = reinterpret_cast<const uint4*>(at & ~static_cast<uintptr_t>(15));
+        pieces = (off + d * static_cast<uint32_t>(sizeof(T)) + 15) / 16;
+    }
+};
+// unit u of a row whose aligned pieces are at `pieces_at` (in global or shared memory, read by ld): elements past the row's end
+// are whatever lies there
+template <typename Ld>
+__device__ __forceinline__ uint4 norm_unit(uint32_t u, uint32_t off, uint32_t pieces, Ld&& ld) {
+    if (off == 0) return ld(u);
+    const uint4 a = ld(u), b = u + 1 < pieces ? ld(u + 1) : make_uint4(0, 0, 0, 0);
+    return shifted(a, b, off);
+}
+// the unit's elements in pairs; those at and past `left` (elements of the row from the unit's first on) become `fill`
+template <typename T>
+__device__ __forceinline__ void unit_pairs(const uint4& v, uint32_t left, float fill, uint64_t (&x)[Unit<T>::kElems / 2]) {
+    constexpr uint32_t E = Unit<T>::kElems;
+#pragma unroll
+    for (uint32_t e = 0; e < E; e += 2) x[e / 2] = pack2(Unit<T>::get(v, e), Unit<T>::get(v, e + 1));
+    if (left < E) {
+#pragma unroll
+        for (uint32_t e = 0; e < E; e += 2) {
+            float p, q;
+            unpack2(x[e / 2], p, q);
+            x[e / 2] = pack2(e < left ? p : fill, e + 1 < left ? q : fill);
+        }
+    }
+}
+// kE parameters from column `col` on as pairs, `fill` past the end or without an array
+template <typename P, uint32_t kE>
+__device__ __forceinline__ void param_pairs(const P* params, uint32_t col, uint32_t d, float fill, uint64_t (&x)[kE / 2]) {
+    if (!params || col + kE > d || (reinterpret_cast<uintptr_t>(params) & 15u) != 0) {
+#pragma unroll
+        for (uint32_t e = 0; e < kE; e += 2)
+            x[e / 2] = pack2(params && col + e < d ? to_f32(params[col + e]) : fill,
+                             params && col + e + 1 < d ? to_f32(params[col + e + 1]) : fill);
+        return;
+    }
+    if constexpr (kE * sizeof(P) >= 16) {
+#pragma unroll
+        for (uint32_t q = 0; q < kE * sizeof(P) / 16; ++q) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(params + col) + q);
+#pragma unroll
+            for (uint32_t e = 0; e < Unit<P>::kElems; e += 2)
+                x[q * Unit<P>::kElems / 2 + e / 2] = pack2(Unit<P>::get(v, e), Unit<P>::get(v, e + 1));
+        }
+    } else {
+        const uint2 v = __ldg(reinterpret_cast<const uint2*>(params + col));           // four bf16
+        const uint4 w = make_uint4(v.x, v.y, 0, 0);
+#pragma unroll
+        for (uint32_t e = 0; e < kE; e += 2) x[e / 2] = pack2(Unit<P>::get(w, e), Unit<P>::get(w, e + 1));
+    }
+}
+
+// A group of threads works on one row: a warp (kGroup = 32) or the CTA.
+template <uint32_t kGroup> __device__ __forceinline__ void group_sync() {
+    if (kGroup == 32) __syncwarp();
+    else __syncthreads();
+}
+// sums of a and b over the group, the same in every thread.  slots: 2 x 2 x 32 floats of the group, `turn` alternates from call to
+// call (so that one barrier is enough).
+template <uint32_t kGroup>
+__device__ __forceinline__ void group_sums(float& a, float& b, float* slots, uint32_t turn) {
+    a = warp_join<SumOp>(a);
+    b = warp_join<SumOp>(b);
+    if (kGroup == 32) return;
+    float* s = slots + (turn & 1u) * 64;
+    const uint32_t warps = kGroup / 32, lane = lane_id();
+    if (lane == 0) {
+        s[threadIdx.x >> 5] = a;
+        s[32 + (threadIdx.x >> 5)] = b;
+    }
+    __syncthreads();
+    a = s[lane & (warps - 1)];
+    b = s[32 + (lane & (warps - 1))];
+#pragma unroll
+    for (uint32_t o = warps / 2; o > 0; o >>= 1) {
+        a = __fadd_rn(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
+        b = __fadd_rn(b, __shfl_xor_sync(0xFFFFFFFFu, b, o));
+    }
+}
+
+// A row of d results of a group.  A row on a 16-byte boundary is written unit by unit; another one by way of shared memory
+// (`image`: a unit for every unit of the row), from which the aligned pieces of the row are put together.
+template <typename T, uint32_t kGroup> struct RowWriter {
+    static constexpr uint32_t E = Unit<T>::kElems;
+    T* row;
+    uint32_t d, off;
+    uint4* image;
+    __device__ __forceinline__ RowWriter(T* row_, uint32_t d_, uint4* image_)
+        : row(row_), d(d_), off(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row_) & 15u)), image(image_) {
+        if (off) group_sync<kGroup>();             // the last row's image is read
+    }
+    __device__ __forceinline__ void put(uint32_t u, const uint4& v) {
+        if (off) {
+            if (u * E < d) image[u] = v;
+        } else if (u * E + E <= d) {
+            st_unit(row + u * E, v);
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < E; ++e)
+                if (u * E + e < d) row[u * E + e] = from_f32<T>(Unit<T>::get(v, e));           // (exact: it is a T already)
+        }
+    }
+    __device__ __forceinline__ void finish(uint32_t lane) {
+        if (!off) return;
+        group_sync<kGroup>();
+        // piece j holds the row's bytes from 16 j - off on
+        const uint32_t bytes = d * static_cast<uint32_t>(sizeof(T)), pieces = (off + bytes + 15) / 16, units = (d + E - 1) / E;
+        uint8_t* base = reinterpret_cast<uint8_t*>(row) - off;
+        for (uint32_t j = lane; j < pieces; j += kGroup) {
+            const uint4 zero = make_uint4(0, 0, 0, 0);
+            const uint4 v = shifted(j > 0 ? image[j - 1] : zero, j < units ? image[j] : zero, 16 - off);
+            if (j > 0 && 16 * j + 16 <= off + bytes) {
+                st_unit(base + 16 * j, v);
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < E; ++e) {
+                    const uint32_t at = 16 * j + e * static_cast<uint32_t>(sizeof(T));       // from base
+                    if (at >= off && at < off + bytes) *reinterpret_cast<T*>(base + at) = from_f32<T>(Unit<T>::get(v, e));
+                }
+            }
+        }
+    }
+};
+template <typename T> __device__ __forceinline__ uint4 pack_unit(const uint64_t (&x)[Unit<T>::kElems / 2]) {
+    float g[Unit<T>::kElems];
+#pragma unroll
+    for (uint32_t e = 0; e < Unit<T>::kElems; e += 2) unpack2(x[e / 2], g[e], g[e + 1]);
+    return Unit<T>::pack(g);
+}
+
+// Forward: the row is read once into registers; the variance is that of the deviations from the mean.
+template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits>
+__global__ void __launch_bounds__(kThreads, (kUnits == 4 ? 896 : 1280) / kThreads)
+norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* __restrict__ weight,
+                      const P* __restrict__ bias, float eps, T* y, uint32_t ld_y, float* __restrict__ mean_out,
+                      float* __restrict__ rstd_out) {
+    constexpr uint32_t E = Unit<T>::kElems, kGroups = kThreads / kGroup;
+    extern __shared__ __align__(16) uint4 images[];
+    __shared__ float slots[128];
+    const uint32_t lane = threadIdx.x % kGroup, group = threadIdx.x / kGroup, units = (d + E - 1) / E;
+    uint4* image = images + group * units;
+    uint32_t turn = 0;
+    for (uint64_t row = static_cast<uint64_t>(blockIdx.x) * kGroups + group; row < rows;
+         row += static_cast<uint64_t>(gridDim.x) * kGroups) {
+        const NormRow<T> in(x + row * ld, d);
+        uint64_t v[kUnits][E / 2];
+        uint64_t sum = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kUnits; ++i) {
+            const uint32_t u = lane + i * kGroup;
+            uint4 raw = make_uint4(0, 0, 0, 0);
+            if (u < units) raw = norm_unit(u, in.off, in.pieces, [&](uint32_t p) { return ld_unit(in.base + p); });
+            unit_pairs<T>(raw, u < units ? d - u * E : 0u, 0.0f, v[i]);
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) sum = add2(sum, v[i][q]);
+        }
+        float s0, s1, none = 0.0f;
+        unpack2(sum, s0, s1);
+        float total = __fadd_rn(s0, s1);
+        group_sums<kGroup>(total, none, slots, turn++);
+        const float mean = total / static_cast<float>(d);
+        const uint64_t minus_mean = pack2(-mean, -mean);
+        uint64_t squares = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kUnits; ++i) {
+            const uint32_t u = lane + i * kGroup, left = u < units ? d - u * E : 0u;
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) v[i][q] = add2(v[i][q], minus_mean);
+            if (left < E) {                        // what is past the end does not deviate
+#pragma unroll
+                for (uint32_t q = 0; q < E / 2; ++q) {
+                    float p0, p1;
+                    unpack2(v[i][q], p0, p1);
+                    v[i][q] = pack2(2 * q < left ? p0 : 0.0f, 2 * q + 1 < left ? p1 : 0.0f);
+                }
+            }
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) squares = fma2(v[i][q], v[i][q], squares);
+        }
+        unpack2(squares, s0, s1);
+        float deviation = __fadd_rn(s0, s1);
+        group_sums<kGroup>(deviation, none, slots, turn++);
+        const float rstd = 1.0f / sqrtf(deviation / static_cast<float>(d) + eps);
+        const uint64_t by_rstd = pack2(rstd, rstd);
+        RowWriter<T, kGroup> out(y + row * ld_y, d, image);
+#pragma unroll
+        for (uint32_t i = 0; i < kUnits; ++i) {
+            const uint32_t col = (lane + i * kGroup) * E;
+            uint64_t w[E / 2], b[E / 2];
+            param_pairs<P, E>(weight, col, d, 1.0f, w);
+            param_pairs<P, E>(bias, col, d, 0.0f, b);
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) v[i][q] = fma2(mul2(v[i][q], by_rstd), w[q], b[q]);
+            out.put(lane + i * kGroup, pack_unit<T>(v[i]));
+        }
+        out.finish(lane);
+        if (lane == 0) {
+            if (mean_out) mean_out[row] = mean;
+            if (rstd_out) rstd_out[row] = rstd;
+        }
+    }
+}
+
+// Backward: a group's rows come through a ring of bulk copies (x and dy of a row to a slot); the row is taken into registers, added to
+// the group's columns of the parameter gradients, summed over, and dx is written from the registers while the slot is
+// filled again.
+constexpr uint32_t kRing = 3u;
+
+template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits>
+__global__ void __launch_bounds__(kThreads, 512 / kThreads)
+norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, uint32_t d, uint32_t ld,
+                      const P* __restrict__ weight, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
+                      uint32_t ld_dx, float* __restrict__ parts, uint32_t slot_units, uint32_t spin_limit) {
+    constexpr uint32_t E = Unit<T>::kElems, kGroups = kThreads / kGroup;
+    extern __shared__ __align__(128) uint4 ring[];        // per group: kRing slots of (x, dy), and the image of an unaligned dx
+    __shared__ float slots[128];
+    __shared__ uint64_t full[kGroups][kRing];
+    __shared__ uint32_t gave_up;
+    const uint32_t lane = threadIdx.x % kGroup, group = threadIdx.x / kGroup, units = (d + E - 1) / E;
+    uint4* const mine = ring + group * (2 * kRing + 1) * slot_units;
+    uint4* const image = mine + 2 * kRing * slot_units;
+    const uint64_t stride = static_cast<uint64_t>(gridDim.x) * kGroups;
+    const uint64_t first = static_cast<uint64_t>(blockIdx.x) * kGroups + group;
+
+    if (threadIdx.x == 0) gave_up = 0;
+    if (lane == 0) {
+        for (uint32_t s = 0; s < kRing; ++s) mbar_init(&full[group][s], 1);
+        mbar_init_fence();
+        fence_proxy_async_smem();
+    }
+    __syncthreads();
+    auto fetch = [&](uint64_t row, uint32_t slot) {          // by one thread
+        if (row >= rows || *const_cast<volatile uint32_t*>(&gave_up)) return;
+        const NormRow<T> a(x + row * ld, d), b(dy + row * ld_dy, d);
+        mbar_arrive_expect_tx(&full[group][slot], 16 * (a.pieces + b.pieces));
+        bulk_load(mine + 2 * slot * slot_units, a.base, 16 * a.pieces, &full[group][slot]);
+        bulk_load(mine + (2 * slot + 1) * slot_units, b.base, 16 * b.pieces, &full[group][slot]);
+    };
+    if (lane == 0)
+        for (uint32_t s = 0; s < kRing; ++s) fetch(first + s * stride, s);
+
+    uint64_t w[kUnits][E / 2], dw[kUnits][E / 2], db[kUnits][E / 2];
+#pragma unroll
+    for (uint32_t i = 0; i < kUnits; ++i) {
+        param_pairs<P, E>(weight, (lane + i * kGroup) * E, d, 1.0f, w[i]);
+#pragma unroll
+        for (uint32_t q = 0; q < E / 2; ++q) dw[i][q] = db[i][q] = 0;
+    }
+    uint32_t slot = 0, phase = 0, turn = 0;
+    bool missed = false;
+    float mu = first < rows ? mean[first] : 0.0f, r = first < rows ? rstd[first] : 0.0f;
+    for (uint64_t row = first; row < rows; row += stride) {
+        const uint64_t next = row + stride;
+        const float next_mu = next < rows ? mean[next] : 0.0f, next_r = next < rows ? rstd[next] : 0.0f;
+        const NormRow<T> ax(x + row * ld, d), ay(dy + row * ld_dy, d);
+        if (!mbar_wait_bounded(&full[group][slot], phase, spin_limit, &gave_up)) {
+            *const_cast<volatile uint32_t*>(&gave_up) = 1;
+            missed = true;
+        }
+        if (missed) r = __uint_as_float(0x7FFFFFFFu);      // what the group writes from here on is NaN
+        const uint64_t minus_mu = pack2(-mu, -mu), by_r = pack2(r, r);
+        uint64_t h[kUnits][E / 2], g[kUnits][E / 2], sum_g = 0, sum_gh = 0;
+        const uint4* sx = mine + 2 * slot * slot_units;
+        const uint4* sy = sx + slot_units;
+#pragma unroll
+        for (uint32_t i = 0; i < kUnits; ++i) {
+            const uint32_t u = lane + i * kGroup, left = u < units ? d - u * E : 0u;
+            uint4 raw_x = make_uint4(0, 0, 0, 0), raw_y = raw_x;
+            if (u < units) {
+                raw_x = norm_unit(u, ax.off, ax.pieces, [&](uint32_t p) { return sx[p]; });
+                raw_y = norm_unit(u, ay.off, ay.pieces, [&](uint32_t p) { return sy[p]; });
+            }
+            unit_pairs<T>(raw_x, left, 0.0f, h[i]);
+            unit_pairs<T>(raw_y, left, 0.0f, g[i]);
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) {
+                h[i][q] = mul2(add2(h[i][q], minus_mu), by_r);
+                dw[i][q] = fma2(g[i][q], h[i][q], dw[i][q]);
+                db[i][q] = add2(db[i][q], g[i][q]);
+                g[i][q] = mul2(g[i][q], w[i][q]);
+                sum_g = add2(sum_g, g[i][q]);
+                sum_gh = fma2(g[i][q], h[i][q], sum_gh);
+            }
+        }
+        float p, q0, a, b;
+        unpack2(sum_g, p, q0);
+        a = __fadd_rn(p, q0);
+        unpack2(sum_gh, p, q0);
+        b = __fadd_rn(p, q0);
+        group_sums<kGroup>(a, b, slots, turn++);
+        if (kGroup == 32) __syncwarp();
+        // every thread has its part of the row: the slot is free
+        if (lane == 0) fetch(row + kRing * stride, slot);
+        const float m1 = a / static_cast<float>(d), m2 = b / static_cast<float>(d);
+        const uint64_t minus_m1 = pack2(-m1, -m1), minus_m2 = pack2(-m2, -m2);
+        RowWriter<T, kGroup> out(dx + row * ld_dx, d, image);
+#pragma unroll
+        for (uint32_t i = 0; i < kUnits; ++i) {
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q)
+                g[i][q] = mul2(by_r, fma2(h[i][q], minus_m2, add2(g[i][q], minus_m1)));
+            out.put(lane + i * kGroup, pack_unit<T>(g[i]));
+        }
+        out.finish(lane);
+        mu = next_mu;
+        r = next_r;
+        if (++slot == kRing) {
+            slot = 0;
+            phase ^= 1u;
+        }
+    }
+    // no copy may land in the shared memory of a CTA that is gone, nor in what is used below
+    if (missed)
+        for (uint32_t s = 0; s < kRing; ++s)
+            for (uint32_t i = 0; i < spin_limit; ++i)
+                if (mbar_try_wait(&full[group][s], phase)) break;
+    if (!parts) return;
+    // the groups' sums, one group after the other (a wait that ran out: NaN)
+    float* cta = parts + static_cast<size_t>(blockIdx.x) * 2 * d;
+    const float broken = gave_up ? __uint_as_float(0x7FFFFFFFu) : 0.0f;
+    if (kGroups == 1) {
+#pragma unroll
+        for (uint32_t i = 0; i < kUnits; ++i)
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) {
+                const uint32_t col = (lane + i * kGroup) * E + 2 * q;
+                float w0, w1, b0, b1;
+                unpack2(dw[i][q], w0, w1);
+                unpack2(db[i][q], b0, b1);
+                if (col < d) {
+                    cta[col] = w0 + broken;
+                    cta[d + col] = b0 + broken;
+                }
+                if (col + 1 < d) {
+                    cta[col + 1] = w1 + broken;
+                    cta[d + col + 1] = b1 + broken;
+                }
+            }
+        return;
+    }
+    float* sums = reinterpret_cast<float*>(ring);          // [2][units * E]; every copy has arrived and been used
+    const uint32_t width = units * E;
+    for (uint32_t turn_of = 0; turn_of < kGroups; ++turn_of) {
+        __syncthreads();
+        if (group == turn_of) {
+#pragma unroll
+            for (uint32_t i = 0; i < kUnits; ++i)
+                if (lane + i * kGroup < units) {
+#pragma unroll
+                    for (uint32_t q = 0; q < E / 2; ++q) {
+                        const uint32_t col = (lane + i * kGroup) * E + 2 * q;
+                        float w0, w1, b0, b1;
+                        unpack2(dw[i][q], w0, w1);
+                        unpack2(db[i][q], b0, b1);
+                        if (turn_of) {
+                            w0 = __fadd_rn(sums[col], w0);
+                            w1 = __fadd_rn(sums[col + 1], w1);
+                            b0 = __fadd_rn(sums[width + col], b0);
+                            b1 = __fadd_rn(sums[width + col + 1], b1);
+                        }
+                        sums[col] = w0;
+                        sums[col + 1] = w1;
+                        sums[width + col] = b0;
+                        sums[width + col + 1] = b1;
+                    }
+                }
+        }
+    }
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < d; c += kThreads) {
+        cta[c] = sums[c] + broken;
+        cta[d + c] = sums[width + c] + broken;
+    }
+}
+
+// dweight, dbias from the CTAs' partial sums: 32 columns to a CTA, 8 runs of partial sums to a column
+__global__ void __launch_bounds__(256)
+norm_param_join_kernel(const float* __restrict__ parts, uint32_t num, uint32_t d, float* __restrict__ dweight,
+                       float* __restrict__ dbias) {
+    __shared__ float s[2][8][33];
+    chain_wait_previous();
+    const uint32_t lane = threadIdx.x & 31u, run = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+    float w = 0.0f, b = 0.0f;
+    if (col < d) {
+#pragma unroll 4
+        for (uint32_t i = run; i < num; i += 8) {
+            const float* p = parts + static_cast<size_t>(i) * 2 * d;
+            w = __fadd_rn(w, p[col]);
+            b = __fadd_rn(b, p[d + col]);
+        }
+    }
+    s[0][run][lane] = w;
+    s[1][run][lane] = b;
+    __syncthreads();
+    if (run < 2 && col < d) {
+        float v = s[run][0][lane];
+        for (uint32_t i = 1; i < 8; ++i) v = __fadd_rn(v, s[run][i][lane]);
+        float* out = run == 0 ? dweight : dbias;
+        if (out) out[col] = v;
+    }
+}
+
+// Rows too wide for a CTA's registers ---------------------------------------------------------------------------
 
 template <typename T, typename P>
 __global__ void __launch_bounds__(kNormThreads)
@@ -57,20 +484,6 @@ norm_param_parts_kernel(const T* __restrict__ dy, uint32_t ld_dy, const T* __res
     p[d + j] = db;
 }
 
-__global__ void __launch_bounds__(kNormThreads)
-norm_param_sum_kernel(const float* __restrict__ parts, uint32_t num, uint32_t d, float* __restrict__ dweight,
-                      float* __restrict__ dbias) {
-    const uint32_t j = blockIdx.x * kNormThreads + threadIdx.x;
-    if (j >= d) return;
-    float dw = 0.0f, db = 0.0f;
-    for (uint32_t i = 0; i < num; ++i) {
-        dw += parts[static_cast<size_t>(i) * 2 * d + j];
-        db += parts[static_cast<size_t>(i) * 2 * d + d + j];
-    }
-    if (dweight) dweight[j] = dw;
-    if (dbias) dbias[j] = db;
-}
-
 template <typename T, typename P>
 __global__ void __launch_bounds__(kNormThreads)
 norm_bwd_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, uint32_t d, uint32_t ld,
@@ -97,35 +510,100 @@ norm_bwd_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, uint32_t
     }
 }
 
-uint32_t norm_parts(uint32_t rows) { return rows < kNormMaxParts ? (rows ? rows : 1) : kNormMaxParts; }
+uint32_t norm_parts(uint32_t rows) { return rows < kMaxParts ? (rows ? rows : 1) : kMaxParts; }
 
-template <typename T, typename P>
-dct_status_t launch_norm_fwd(const void* x, uint32_t rows, uint32_t d, uint32_t ld, const void* weight, const void* bias,
-                             float eps, void* y, uint32_t ld_y, float* mean_out, float* rstd_out, cudaStream_t stream) {
-    const uint32_t grid = rows < 4096u ? rows : 4096u;
-    norm_fwd_kernel<T, P><<<grid, kNormThreads, 0, stream>>>(static_cast<const T*>(x), rows, d, ld,
-                                                             static_cast<const P*>(weight), static_cast<const P*>(bias),
-                                                             eps, static_cast<T*>(y), ld_y, mean_out, rstd_out);
+template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits>
+dct_status_t launch_fwd_units(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* weight, const P* bias, float eps, T* y,
+                              uint32_t ld_y, float* mean_out, float* rstd_out, cudaStream_t stream) {
+    constexpr uint32_t kGroups = kThreads / kGroup, E = Unit<T>::kElems;
+    auto kernel = norm_fwd_units_kernel<T, P, kGroup, kThreads, kUnits>;
+    // an image only if some row of y does not start on a boundary
+    const bool aligned = aligned_to(y, 16) && (rows == 1 || static_cast<size_t>(ld_y) * sizeof(T) % 16 == 0);
+    const size_t smem = aligned ? 0 : static_cast<size_t>(kGroups) * ((d + E - 1) / E) * 16;
+    if (smem > 40 * 1024)
+        DCT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    const uint64_t ctas = (static_cast<uint64_t>(rows) + kGroups - 1) / kGroups;
+    kernel<<<static_cast<uint32_t>(ctas < (1u << 30) ? ctas : 1u << 30), kThreads, smem, stream>>>(
+        x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out);
     DCT_CUDA_TRY(cudaGetLastError());
     return DCT_OK;
 }
 
 template <typename T, typename P>
-dct_status_t launch_norm_bwd(const void* dy, uint32_t ld_dy, const void* x, uint32_t rows, uint32_t d, uint32_t ld,
-                             const void* weight, const float* mean, const float* rstd, void* dx, uint32_t ld_dx,
+dct_status_t launch_norm_fwd(const void* x_, uint32_t rows, uint32_t d, uint32_t ld, const void* weight_, const void* bias_,
+                             float eps, void* y_, uint32_t ld_y, float* mean_out, float* rstd_out, cudaStream_t stream) {
+    const T* x = static_cast<const T*>(x_);
+    T* y = static_cast<T*>(y_);
+    const P *weight = static_cast<const P*>(weight_), *bias = static_cast<const P*>(bias_);
+    const uint32_t units = (d + Unit<T>::kElems - 1) / Unit<T>::kElems;
+    auto go = [&](auto launch) { return launch(x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out, stream); };
+    if (units <= 32) return go(launch_fwd_units<T, P, 32, 128, 1>);
+    if (units <= 64) return go(launch_fwd_units<T, P, 32, 128, 2>);
+    if (units <= 128) return go(launch_fwd_units<T, P, 32, 128, 4>);
+    if (units <= 256) return go(launch_fwd_units<T, P, 128, 128, 2>);
+    if (units <= 512) return go(launch_fwd_units<T, P, 128, 128, 4>);
+    if (units <= 1024) return go(launch_fwd_units<T, P, 256, 256, 4>);
+    if (units <= 2048) return go(launch_fwd_units<T, P, 512, 512, 4>);
+    const uint32_t grid = rows < 4096u ? rows : 4096u;
+    norm_fwd_kernel<T, P><<<grid, kNormThreads, 0, stream>>>(x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out);
+    DCT_CUDA_TRY(cudaGetLastError());
+    return DCT_OK;
+}
+
+dct_status_t launch_param_join(const float* parts, uint32_t num, uint32_t d, float* dweight, float* dbias, cudaStream_t stream) {
+    DCT_CUDA_TRY(launch_chained(norm_param_join_kernel, (d + 31) / 32, 256, stream, parts, num, d, dweight, dbias));
+    return DCT_OK;
+}
+
+template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits>
+dct_status_t launch_bwd_units(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* weight,
+                              const float* mean, const float* rstd, T* dx, uint32_t ld_dx, float* dweight, float* dbias,
+                              float* parts, cudaStream_t stream) {
+    constexpr uint32_t kGroups = kThreads / kGroup, E = Unit<T>::kElems;
+    const int sms = sm_count();
+    if (sms <= 0) return DCT_ERR_CUDA;
+    auto kernel = norm_bwd_units_kernel<T, P, kGroup, kThreads, kUnits>;
+    const uint32_t slot_units = (d + E - 1) / E + 1;       // (an unaligned row touches one piece more)
+    const size_t smem = static_cast<size_t>(kGroups) * (2 * kRing + 1) * slot_units * 16;
+    if (smem > 40 * 1024)
+        DCT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    const uint64_t wanted = (static_cast<uint64_t>(rows) + kGroups - 1) / kGroups;
+    uint64_t room = static_cast<uint64_t>(sms) * (512 / kThreads);
+    if (room > kMaxParts) room = kMaxParts;
+    const uint32_t grid = static_cast<uint32_t>(wanted < room ? wanted : room);
+    const bool params = dweight || dbias;
+    kernel<<<grid, kThreads, smem, stream>>>(dy, ld_dy, x, rows, d, ld, weight, mean, rstd, dx, ld_dx,
+                                             params ? parts : nullptr, slot_units, debug_config().spin_limit);
+    DCT_CUDA_TRY(cudaGetLastError());
+    return params ? launch_param_join(parts, grid, d, dweight, dbias, stream) : DCT_OK;
+}
+
+template <typename T, typename P>
+dct_status_t launch_norm_bwd(const void* dy_, uint32_t ld_dy, const void* x_, uint32_t rows, uint32_t d, uint32_t ld,
+                             const void* weight_, const float* mean, const float* rstd, void* dx_, uint32_t ld_dx,
                              float* dweight, float* dbias, float* parts, cudaStream_t stream) {
+    const T *dy = static_cast<const T*>(dy_), *x = static_cast<const T*>(x_);
+    T* dx = static_cast<T*>(dx_);
+    const P* weight = static_cast<const P*>(weight_);
+    const uint32_t units = (d + Unit<T>::kElems - 1) / Unit<T>::kElems;
+    auto go = [&](auto launch) { return launch(dy, ld_dy, x, rows, d, ld, weight, mean, rstd, dx, ld_dx, dweight, dbias, parts, stream); };
+    if (units <= 32) return go(launch_bwd_units<T, P, 32, 128, 1>);
+    if (units <= 64) return go(launch_bwd_units<T, P, 32, 128, 2>);
+    if (units <= 128) return go(launch_bwd_units<T, P, sizeof(T) == 4 ? 32 : 128, 128, sizeof(T) == 4 ? 4 : 1>);
+    if (units <= 256) return go(launch_bwd_units<T, P, 256, 256, 1>);
+    if (units <= 512) return go(launch_bwd_units<T, P, 256, 256, 2>);
+    if (units <= 1024) return go(launch_bwd_units<T, P, 512, 512, 2>);
+    if constexpr (sizeof(T) == 4)
+        if (units <= 2048) return go(launch_bwd_units<T, P, 512, 512, 4>);
     if (dweight || dbias) {        // before dx, which may take the place of dy or x
         const uint32_t cols = (d + kNormThreads - 1) / kNormThreads, num = norm_parts(rows);
-        norm_param_parts_kernel<T><<<dim3(cols, num), kNormThreads, 0, stream>>>(
-            static_cast<const T*>(dy), ld_dy, static_cast<const T*>(x), rows, d, ld, mean, rstd, parts);
+        norm_param_parts_kernel<T><<<dim3(cols, num), kNormThreads, 0, stream>>>(dy, ld_dy, x, rows, d, ld, mean, rstd, parts);
         DCT_CUDA_TRY(cudaGetLastError());
-        norm_param_sum_kernel<<<cols, kNormThreads, 0, stream>>>(parts, num, d, dweight, dbias);
-        DCT_CUDA_TRY(cudaGetLastError());
+        const dct_status_t st = launch_param_join(parts, num, d, dweight, dbias, stream);
+        if (st != DCT_OK) return st;
     }
     const uint32_t grid = rows < 4096u ? rows : 4096u;
-    norm_bwd_kernel<T, P><<<grid, kNormThreads, 0, stream>>>(static_cast<const T*>(dy), ld_dy, static_cast<const T*>(x),
-                                                             rows, d, ld, static_cast<const P*>(weight), mean, rstd,
-                                                             static_cast<T*>(dx), ld_dx);
+    norm_bwd_kernel<T, P><<<grid, kNormThreads, 0, stream>>>(dy, ld_dy, x, rows, d, ld, weight, mean, rstd, dx, ld_dx);
     DCT_CUDA_TRY(cudaGetLastError());
     return DCT_OK;
 }
