@@ -34,13 +34,19 @@ template <typename T> struct NormRow {
         pieces = (off + d * static_cast<uint32_t>(sizeof(T)) + 15) / 16;
     }
 };
-// unit u of a row whose aligned pieces are at `pieces_at` (in global or shared memory, read by ld): elements past the row's end
-// are whatever lies there
-template <typename Ld>
-__device__ __forceinline__ uint4 norm_unit(uint32_t u, uint32_t off, uint32_t pieces, Ld&& ld) {
-    if (off == 0) return ld(u);
-    const uint4 a = ld(u), b = u + 1 < pieces ? ld(u + 1) : make_uint4(0, 0, 0, 0);
-    return shifted(a, b, off);
+// units lane, lane + kGroup, ... of a row whose aligned pieces ld reads (from global or shared memory), all loads before any use;
+// elements past the row's end are whatever lies there.  kWhole, here and below: the group's lanes hold exactly the row's units, all
+// of them whole, and every row starts on a 16-byte boundary.
+template <uint32_t kGroup, uint32_t kUnits, bool kWhole, typename Ld>
+__device__ __forceinline__ void load_units(uint4 (&v)[kUnits], uint32_t lane, uint32_t units, uint32_t off, uint32_t pieces, Ld&& ld) {
+#pragma unroll
+    for (uint32_t i = 0; i < kUnits; ++i) v[i] = ld(kWhole ? lane + i * kGroup : min(lane + i * kGroup, units - 1));
+    if (kWhole || off == 0) return;
+    uint4 b[kUnits];
+#pragma unroll
+    for (uint32_t i = 0; i < kUnits; ++i) b[i] = ld(min(lane + i * kGroup + 1, pieces - 1));     // (a last piece again: not used)
+#pragma unroll
+    for (uint32_t i = 0; i < kUnits; ++i) v[i] = shifted(v[i], b[i], off);
 }
 // the unit's elements in pairs; those at and past `left` (elements of the row from the unit's first on) become `fill`
 template <typename T>
@@ -57,10 +63,14 @@ __device__ __forceinline__ void unit_pairs(const uint4& v, uint32_t left, float 
         }
     }
 }
-// kE parameters from column `col` on as pairs, `fill` past the end or without an array
+// kE parameters from column `col` on as pairs, `fill` past the end or without an array.  whole: there is an array on a 16-byte
+// boundary and every unit of the row is whole; vector: the former alone (both the same for all threads)
 template <typename P, uint32_t kE>
-__device__ __forceinline__ void param_pairs(const P* params, uint32_t col, uint32_t d, float fill, uint64_t (&x)[kE / 2]) {
-    if (!params || col + kE > d || (reinterpret_cast<uintptr_t>(params) & 15u) != 0) {
+__device__ __forceinline__ void param_pairs(const P* params, bool whole, bool vector, uint32_t col, uint32_t d, float fill,
+                                            uint64_t (&x)[kE / 2]) {
+    if (whole) {
+        col = min(col, d - kE);
+    } else if (!vector || col + kE > d) {
 #pragma unroll
         for (uint32_t e = 0; e < kE; e += 2)
             x[e / 2] = pack2(params && col + e < d ? to_f32(params[col + e]) : fill,
@@ -81,6 +91,10 @@ __device__ __forceinline__ void param_pairs(const P* params, uint32_t col, uint3
 #pragma unroll
         for (uint32_t e = 0; e < kE; e += 2) x[e / 2] = pack2(Unit<P>::get(w, e), Unit<P>::get(w, e + 1));
     }
+}
+
+template <typename P> __device__ __forceinline__ bool vector_params(const P* params) {
+    return params && (reinterpret_cast<uintptr_t>(params) & 15u) == 0;
 }
 
 // A group of threads works on one row: a warp (kGroup = 32) or the CTA.
@@ -111,21 +125,33 @@ __device__ __forceinline__ void group_sums(float& a, float& b, float* slots, uin
     }
 }
 
+template <uint32_t kGroup> __device__ __forceinline__ void group_sum(float& a, float* slots, uint32_t turn) {
+    a = warp_join<SumOp>(a);
+    if (kGroup == 32) return;
+    float* s = slots + (turn & 1u) * 64;
+    const uint32_t warps = kGroup / 32, lane = lane_id();
+    if (lane == 0) s[threadIdx.x >> 5] = a;
+    __syncthreads();
+    a = s[lane & (warps - 1)];
+#pragma unroll
+    for (uint32_t o = warps / 2; o > 0; o >>= 1) a = __fadd_rn(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
+}
+
 // A row of d results of a group.  A row on a 16-byte boundary is written unit by unit; another one by way of shared memory
 // (`image`: a unit for every unit of the row), from which the aligned pieces of the row are put together.
-template <typename T, uint32_t kGroup> struct RowWriter {
+template <typename T, uint32_t kGroup, bool kWhole> struct RowWriter {
     static constexpr uint32_t E = Unit<T>::kElems;
     T* row;
     uint32_t d, off;
     uint4* image;
     __device__ __forceinline__ RowWriter(T* row_, uint32_t d_, uint4* image_)
-        : row(row_), d(d_), off(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row_) & 15u)), image(image_) {
+        : row(row_), d(d_), off(kWhole ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row_) & 15u)), image(image_) {
         if (off) group_sync<kGroup>();             // the last row's image is read
     }
     __device__ __forceinline__ void put(uint32_t u, const uint4& v) {
         if (off) {
             if (u * E < d) image[u] = v;
-        } else if (u * E + E <= d) {
+        } else if (kWhole || u * E + E <= d) {
             st_unit(row + u * E, v);
         } else {
 #pragma unroll
@@ -163,7 +189,7 @@ template <typename T> __device__ __forceinline__ uint4 pack_unit(const uint64_t 
 
 // Forward: the row is read once into registers; the variance is that of the deviations from the mean.
 template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits>
-__global__ void __launch_bounds__(kThreads, (kUnits == 4 ? 896 : 1280) / kThreads)
+__global__ void __launch_bounds__(kThreads)
 norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* __restrict__ weight,
                       const P* __restrict__ bias, float eps, T* y, uint32_t ld_y, float* __restrict__ mean_out,
                       float* __restrict__ rstd_out) {
@@ -172,25 +198,26 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
     __shared__ float slots[128];
     const uint32_t lane = threadIdx.x % kGroup, group = threadIdx.x / kGroup, units = (d + E - 1) / E;
     uint4* image = images + group * units;
+    const bool vec_w = vector_params(weight), vec_b = vector_params(bias), whole = d % E == 0;
     uint32_t turn = 0;
     for (uint64_t row = static_cast<uint64_t>(blockIdx.x) * kGroups + group; row < rows;
          row += static_cast<uint64_t>(gridDim.x) * kGroups) {
         const NormRow<T> in(x + row * ld, d);
+        uint4 raw[kUnits];
+        load_units<kGroup, kUnits, false>(raw, lane, units, in.off, in.pieces, [&](uint32_t p) { return ld_unit(in.base + p); });
         uint64_t v[kUnits][E / 2];
         uint64_t sum = 0;
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
             const uint32_t u = lane + i * kGroup;
-            uint4 raw = make_uint4(0, 0, 0, 0);
-            if (u < units) raw = norm_unit(u, in.off, in.pieces, [&](uint32_t p) { return ld_unit(in.base + p); });
-            unit_pairs<T>(raw, u < units ? d - u * E : 0u, 0.0f, v[i]);
+            unit_pairs<T>(raw[i], u < units ? d - u * E : 0u, 0.0f, v[i]);
 #pragma unroll
             for (uint32_t q = 0; q < E / 2; ++q) sum = add2(sum, v[i][q]);
         }
-        float s0, s1, none = 0.0f;
+        float s0, s1;
         unpack2(sum, s0, s1);
         float total = __fadd_rn(s0, s1);
-        group_sums<kGroup>(total, none, slots, turn++);
+        group_sum<kGroup>(total, slots, turn++);
         const float mean = total / static_cast<float>(d);
         const uint64_t minus_mean = pack2(-mean, -mean);
         uint64_t squares = 0;
@@ -212,16 +239,16 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
         }
         unpack2(squares, s0, s1);
         float deviation = __fadd_rn(s0, s1);
-        group_sums<kGroup>(deviation, none, slots, turn++);
+        group_sum<kGroup>(deviation, slots, turn++);
         const float rstd = 1.0f / sqrtf(deviation / static_cast<float>(d) + eps);
         const uint64_t by_rstd = pack2(rstd, rstd);
-        RowWriter<T, kGroup> out(y + row * ld_y, d, image);
+        RowWriter<T, kGroup, false> out(y + row * ld_y, d, image);
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
             const uint32_t col = (lane + i * kGroup) * E;
             uint64_t w[E / 2], b[E / 2];
-            param_pairs<P, E>(weight, col, d, 1.0f, w);
-            param_pairs<P, E>(bias, col, d, 0.0f, b);
+            param_pairs<P, E>(weight, vec_w && whole, vec_w, col, d, 1.0f, w);
+            param_pairs<P, E>(bias, vec_b && whole, vec_b, col, d, 0.0f, b);
 #pragma unroll
             for (uint32_t q = 0; q < E / 2; ++q) v[i][q] = fma2(mul2(v[i][q], by_rstd), w[q], b[q]);
             out.put(lane + i * kGroup, pack_unit<T>(v[i]));
@@ -234,16 +261,168 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
     }
 }
 
+// Forward by the same rules for as many rows as a grid that stays has groups for: the rows come through a ring of bulk copies,
+// kRing ahead of the one being worked on, and the parameters lie in shared memory, so that a row's only waits are its two sums.
+constexpr uint32_t kRing = 3u;
+
+// the parameters as they lie in shared memory: 16-byte pieces (fp32 where a unit's bf16 parameters would be less than that),
+// piece q of unit u at [q][u]
+template <typename P, uint32_t kE> struct ParamImage {
+    static constexpr bool kWide = kE * sizeof(P) < 16;
+    static constexpr uint32_t kPieces = kWide ? 1 : kE * sizeof(P) / 16;
+    static constexpr uint32_t kPerPiece = kE / kPieces;
+    __device__ __forceinline__ static void fill(uint4* image, const P* params, uint32_t d, uint32_t units, float none) {
+        for (uint32_t i = threadIdx.x; i < kPieces * units; i += blockDim.x) {
+            const uint32_t col = i % units * kE + i / units * kPerPiece;
+            float v[kPerPiece];
+#pragma unroll
+            for (uint32_t e = 0; e < kPerPiece; ++e) v[e] = params && col + e < d ? to_f32(params[col + e]) : none;
+            if constexpr (kPerPiece == 4) image[i] = Unit<float>::pack(v);
+            else image[i] = Unit<__nv_bfloat16>::pack(v);                   // (exact: bf16 already)
+        }
+    }
+    __device__ __forceinline__ static void pairs(const uint4* image, uint32_t u, uint32_t units, uint64_t (&x)[kE / 2]) {
+#pragma unroll
+        for (uint32_t q = 0; q < kPieces; ++q) {
+            const uint4 v = image[q * units + u];
+#pragma unroll
+            for (uint32_t e = 0; e < kPerPiece; e += 2) {
+                if constexpr (kPerPiece == 4) x[(q * kPerPiece + e) / 2] = pack2(Unit<float>::get(v, e), Unit<float>::get(v, e + 1));
+                else x[(q * kPerPiece + e) / 2] = pack2(Unit<__nv_bfloat16>::get(v, e), Unit<__nv_bfloat16>::get(v, e + 1));
+            }
+        }
+    }
+};
+
+// CTAs of the forward kernel an SM's registers are asked to hold
+template <uint32_t kThreads, uint32_t kUnits> constexpr uint32_t fwd_ctas() { return (kUnits == 4 ? 512 : 1024) / kThreads; }
+
+template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits, bool kWhole>
+__global__ void __launch_bounds__(kThreads, fwd_ctas<kThreads, kUnits>())
+norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* __restrict__ weight,
+                     const P* __restrict__ bias, float eps, T* y, uint32_t ld_y, float* __restrict__ mean_out,
+                     float* __restrict__ rstd_out, uint32_t slot_units, float per_column, uint32_t spin_limit) {
+    constexpr uint32_t E = Unit<T>::kElems, kGroups = kThreads / kGroup;
+    using Image = ParamImage<P, E>;
+    extern __shared__ __align__(128) uint4 shared[];       // parameters; per group kRing slots and the image of an unaligned y
+    __shared__ float slots[128];
+    __shared__ uint64_t full[kGroups][kRing];
+    __shared__ uint32_t gave_up;
+    constexpr uint32_t kAll = kGroup * kUnits;             // units the group's lanes hold
+    const uint32_t lane = threadIdx.x % kGroup, group = threadIdx.x / kGroup, units = (d + E - 1) / E;
+    uint4 *const weights = shared, *const biases = shared + Image::kPieces * kAll;
+    uint4* const mine = shared + 2 * Image::kPieces * kAll + group * (kRing + 1) * slot_units;
+    uint4* const image = mine + kRing * slot_units;
+    const uint64_t stride = static_cast<uint64_t>(gridDim.x) * kGroups;
+    const uint64_t first = static_cast<uint64_t>(blockIdx.x) * kGroups + group;
+
+    if (threadIdx.x == 0) gave_up = 0;
+    if (lane == 0) {
+        for (uint32_t s = 0; s < kRing; ++s) mbar_init(&full[group][s], 1);
+        mbar_init_fence();
+        fence_proxy_async_smem();
+    }
+    __syncthreads();
+    auto fetch = [&](uint64_t row, uint32_t slot) {          // by one thread
+        if (row >= rows || *const_cast<volatile uint32_t*>(&gave_up)) return;
+        const NormRow<T> a(x + row * ld, d);
+        mbar_arrive_expect_tx(&full[group][slot], 16 * a.pieces);
+        bulk_load(mine + slot * slot_units, a.base, 16 * a.pieces, &full[group][slot]);
+    };
+    if (lane == 0)
+        for (uint32_t s = 0; s < kRing; ++s) fetch(first + s * stride, s);
+    Image::fill(weights, weight, d, kAll, 1.0f);
+    Image::fill(biases, bias, d, kAll, 0.0f);
+    __syncthreads();
+
+    uint32_t slot = 0, phase = 0, turn = 0;
+    bool missed = false;
+    const T* x_row = x + first * ld;
+    T* y_row = y + first * ld_y;
+    for (uint64_t row = first; row < rows; row += stride, x_row += stride * ld, y_row += stride * ld_y) {
+        const NormRow<T> in(x_row, d);
+        if (!mbar_wait_bounded(&full[group][slot], phase, spin_limit, &gave_up)) {
+            *const_cast<volatile uint32_t*>(&gave_up) = 1;
+            missed = true;
+        }
+        uint4 raw[kUnits];
+        const uint4* from = mine + slot * slot_units;
+        load_units<kGroup, kUnits, kWhole>(raw, lane, units, in.off, in.pieces, [&](uint32_t p) { return from[p]; });
+        uint64_t v[kUnits][E / 2];
+        uint64_t sum = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kUnits; ++i) {
+            const uint32_t u = lane + i * kGroup;
+            unit_pairs<T>(raw[i], kWhole ? E : u < units ? d - u * E : 0u, 0.0f, v[i]);
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) sum = add2(sum, v[i][q]);
+        }
+        float s0, s1, total;
+        unpack2(sum, s0, s1);
+        total = __fadd_rn(s0, s1);
+        group_sum<kGroup>(total, slots, turn++);
+        if (kGroup == 32) __syncwarp();
+        if (lane == 0) fetch(row + kRing * stride, slot);      // every thread has its part of the row: the slot is free
+        const float mean = __fmul_rn(total, per_column);
+        const uint64_t minus_mean = pack2(-mean, -mean);
+        uint64_t squares = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kUnits; ++i) {
+            const uint32_t u = lane + i * kGroup, left = kWhole ? E : u < units ? d - u * E : 0u;
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) v[i][q] = add2(v[i][q], minus_mean);
+            if (left < E) {                        // what is past the end does not deviate
+#pragma unroll
+                for (uint32_t q = 0; q < E / 2; ++q) {
+                    float p0, p1;
+                    unpack2(v[i][q], p0, p1);
+                    v[i][q] = pack2(2 * q < left ? p0 : 0.0f, 2 * q + 1 < left ? p1 : 0.0f);
+                }
+            }
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) squares = fma2(v[i][q], v[i][q], squares);
+        }
+        unpack2(squares, s0, s1);
+        float deviation = __fadd_rn(s0, s1);
+        group_sum<kGroup>(deviation, slots, turn++);
+        float rstd = rsqrtf(fmaf(deviation, per_column, eps));
+        if (missed) rstd = __uint_as_float(0x7FFFFFFFu);       // what the group writes from here on is NaN
+        const uint64_t by_rstd = pack2(rstd, rstd);
+        RowWriter<T, kGroup, kWhole> out(y_row, d, image);
+#pragma unroll
+        for (uint32_t i = 0; i < kUnits; ++i) {
+            uint64_t w[E / 2], b[E / 2];
+            Image::pairs(weights, lane + i * kGroup, kAll, w);
+            Image::pairs(biases, lane + i * kGroup, kAll, b);
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) v[i][q] = fma2(mul2(v[i][q], by_rstd), w[q], b[q]);
+            out.put(lane + i * kGroup, pack_unit<T>(v[i]));
+        }
+        out.finish(lane);
+        if (lane == 0) {
+            if (mean_out) mean_out[row] = mean;
+            if (rstd_out) rstd_out[row] = rstd;
+        }
+        if (++slot == kRing) {
+            slot = 0;
+            phase ^= 1u;
+        }
+    }
+    // no copy may land in the shared memory of a CTA that is gone
+    if (missed)
+        for (uint32_t s = 0; s < kRing; ++s)
+            for (uint32_t i = 0; i < spin_limit; ++i)
+                if (mbar_try_wait(&full[group][s], phase)) break;
+}
+
 // Backward: a group's rows come through a ring of bulk copies (x and dy of a row to a slot); the row is taken into registers, added to
 // the group's columns of the parameter gradients, summed over, and dx is written from the registers while the slot is
 // filled again.
-constexpr uint32_t kRing = 3u;
-
-template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits>
+template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits, bool kWhole>
 __global__ void __launch_bounds__(kThreads, 512 / kThreads)
 norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, uint32_t d, uint32_t ld,
                       const P* __restrict__ weight, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
-                      uint32_t ld_dx, float* __restrict__ parts, uint32_t slot_units, uint32_t spin_limit) {
+                      uint32_t ld_dx, float* __restrict__ parts, uint32_t slot_units, float per_column, uint32_t spin_limit) {
     constexpr uint32_t E = Unit<T>::kElems, kGroups = kThreads / kGroup;
     extern __shared__ __align__(128) uint4 ring[];        // per group: kRing slots of (x, dy), and the image of an unaligned dx
     __shared__ float slots[128];
@@ -255,6 +434,7 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
     const uint64_t stride = static_cast<uint64_t>(gridDim.x) * kGroups;
     const uint64_t first = static_cast<uint64_t>(blockIdx.x) * kGroups + group;
 
+    chain_release_next();                  // the CTAs that join the partial sums may come and wait
     if (threadIdx.x == 0) gave_up = 0;
     if (lane == 0) {
         for (uint32_t s = 0; s < kRing; ++s) mbar_init(&full[group][s], 1);
@@ -275,17 +455,19 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
     uint64_t w[kUnits][E / 2], dw[kUnits][E / 2], db[kUnits][E / 2];
 #pragma unroll
     for (uint32_t i = 0; i < kUnits; ++i) {
-        param_pairs<P, E>(weight, (lane + i * kGroup) * E, d, 1.0f, w[i]);
+        param_pairs<P, E>(weight, false, vector_params(weight), (lane + i * kGroup) * E, d, 1.0f, w[i]);
 #pragma unroll
         for (uint32_t q = 0; q < E / 2; ++q) dw[i][q] = db[i][q] = 0;
     }
     uint32_t slot = 0, phase = 0, turn = 0;
     bool missed = false;
     float mu = first < rows ? mean[first] : 0.0f, r = first < rows ? rstd[first] : 0.0f;
-    for (uint64_t row = first; row < rows; row += stride) {
+    const T *x_row = x + first * ld, *dy_row = dy + first * ld_dy;
+    T* dx_row = dx + first * ld_dx;
+    for (uint64_t row = first; row < rows; row += stride, x_row += stride * ld, dy_row += stride * ld_dy, dx_row += stride * ld_dx) {
         const uint64_t next = row + stride;
         const float next_mu = next < rows ? mean[next] : 0.0f, next_r = next < rows ? rstd[next] : 0.0f;
-        const NormRow<T> ax(x + row * ld, d), ay(dy + row * ld_dy, d);
+        const NormRow<T> ax(x_row, d), ay(dy_row, d);
         if (!mbar_wait_bounded(&full[group][slot], phase, spin_limit, &gave_up)) {
             *const_cast<volatile uint32_t*>(&gave_up) = 1;
             missed = true;
@@ -295,16 +477,14 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
         uint64_t h[kUnits][E / 2], g[kUnits][E / 2], sum_g = 0, sum_gh = 0;
         const uint4* sx = mine + 2 * slot * slot_units;
         const uint4* sy = sx + slot_units;
+        uint4 raw_x[kUnits], raw_y[kUnits];
+        load_units<kGroup, kUnits, kWhole>(raw_x, lane, units, ax.off, ax.pieces, [&](uint32_t p) { return sx[p]; });
+        load_units<kGroup, kUnits, kWhole>(raw_y, lane, units, ay.off, ay.pieces, [&](uint32_t p) { return sy[p]; });
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
-            const uint32_t u = lane + i * kGroup, left = u < units ? d - u * E : 0u;
-            uint4 raw_x = make_uint4(0, 0, 0, 0), raw_y = raw_x;
-            if (u < units) {
-                raw_x = norm_unit(u, ax.off, ax.pieces, [&](uint32_t p) { return sx[p]; });
-                raw_y = norm_unit(u, ay.off, ay.pieces, [&](uint32_t p) { return sy[p]; });
-            }
-            unit_pairs<T>(raw_x, left, 0.0f, h[i]);
-            unit_pairs<T>(raw_y, left, 0.0f, g[i]);
+            const uint32_t u = lane + i * kGroup, left = kWhole ? E : u < units ? d - u * E : 0u;
+            unit_pairs<T>(raw_x[i], left, 0.0f, h[i]);
+            unit_pairs<T>(raw_y[i], left, 0.0f, g[i]);
 #pragma unroll
             for (uint32_t q = 0; q < E / 2; ++q) {
                 h[i][q] = mul2(add2(h[i][q], minus_mu), by_r);
@@ -324,9 +504,9 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
         if (kGroup == 32) __syncwarp();
         // every thread has its part of the row: the slot is free
         if (lane == 0) fetch(row + kRing * stride, slot);
-        const float m1 = a / static_cast<float>(d), m2 = b / static_cast<float>(d);
+        const float m1 = __fmul_rn(a, per_column), m2 = __fmul_rn(b, per_column);
         const uint64_t minus_m1 = pack2(-m1, -m1), minus_m2 = pack2(-m2, -m2);
-        RowWriter<T, kGroup> out(dx + row * ld_dx, d, image);
+        RowWriter<T, kGroup, kWhole> out(dx_row, d, image);
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
 #pragma unroll
@@ -348,88 +528,76 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
             for (uint32_t i = 0; i < spin_limit; ++i)
                 if (mbar_try_wait(&full[group][s], phase)) break;
     if (!parts) return;
-    // the groups' sums, one group after the other (a wait that ran out: NaN)
-    float* cta = parts + static_cast<size_t>(blockIdx.x) * 2 * d;
-    const float broken = gave_up ? __uint_as_float(0x7FFFFFFFu) : 0.0f;
-    if (kGroups == 1) {
-#pragma unroll
-        for (uint32_t i = 0; i < kUnits; ++i)
-#pragma unroll
-            for (uint32_t q = 0; q < E / 2; ++q) {
-                const uint32_t col = (lane + i * kGroup) * E + 2 * q;
-                float w0, w1, b0, b1;
-                unpack2(dw[i][q], w0, w1);
-                unpack2(db[i][q], b0, b1);
-                if (col < d) {
-                    cta[col] = w0 + broken;
-                    cta[d + col] = b0 + broken;
-                }
-                if (col + 1 < d) {
-                    cta[col + 1] = w1 + broken;
-                    cta[d + col + 1] = b1 + broken;
-                }
-            }
-        return;
-    }
-    float* sums = reinterpret_cast<float*>(ring);          // [2][units * E]; every copy has arrived and been used
+    // the CTA's partial sums: dweight, then dbias, `width` apart (a wait that ran out: NaN)
     const uint32_t width = units * E;
-    for (uint32_t turn_of = 0; turn_of < kGroups; ++turn_of) {
-        __syncthreads();
-        if (group == turn_of) {
+    float* cta = parts + static_cast<size_t>(blockIdx.x) * 2 * width;
+    const float broken = gave_up ? __uint_as_float(0x7FFFFFFFu) : 0.0f;
+    float* to = cta;
+    if (kGroups > 1) {
+        __syncthreads();                                   // every copy has arrived and been used
+        to = reinterpret_cast<float*>(ring) + group * 2 * width;
+    }
 #pragma unroll
-            for (uint32_t i = 0; i < kUnits; ++i)
-                if (lane + i * kGroup < units) {
+    for (uint32_t i = 0; i < kUnits; ++i) {
+        const uint32_t u = lane + i * kGroup;
+        if (u >= units) break;
 #pragma unroll
-                    for (uint32_t q = 0; q < E / 2; ++q) {
-                        const uint32_t col = (lane + i * kGroup) * E + 2 * q;
-                        float w0, w1, b0, b1;
-                        unpack2(dw[i][q], w0, w1);
-                        unpack2(db[i][q], b0, b1);
-                        if (turn_of) {
-                            w0 = __fadd_rn(sums[col], w0);
-                            w1 = __fadd_rn(sums[col + 1], w1);
-                            b0 = __fadd_rn(sums[width + col], b0);
-                            b1 = __fadd_rn(sums[width + col + 1], b1);
-                        }
-                        sums[col] = w0;
-                        sums[col + 1] = w1;
-                        sums[width + col] = b0;
-                        sums[width + col + 1] = b1;
-                    }
-                }
+        for (uint32_t q = 0; q < E / 2; q += 2) {
+            float4 v, t;
+            unpack2(dw[i][q], v.x, v.y);
+            unpack2(dw[i][q + 1], v.z, v.w);
+            unpack2(db[i][q], t.x, t.y);
+            unpack2(db[i][q + 1], t.z, t.w);
+            v.x += broken;
+            t.x += broken;
+            *reinterpret_cast<float4*>(to + u * E + 2 * q) = v;
+            *reinterpret_cast<float4*>(to + width + u * E + 2 * q) = t;
         }
     }
-    __syncthreads();
-    for (uint32_t c = threadIdx.x; c < d; c += kThreads) {
-        cta[c] = sums[c] + broken;
-        cta[d + c] = sums[width + c] + broken;
+    if (kGroups > 1) {
+        __syncthreads();
+        const float4* from = reinterpret_cast<const float4*>(ring);
+        for (uint32_t c = threadIdx.x; c < 2 * width / 4; c += kThreads) {
+            float4 v = from[c];
+#pragma unroll
+            for (uint32_t k = 1; k < kGroups; ++k) {
+                const float4 t = from[c + k * (2 * width / 4)];
+                v.x = __fadd_rn(v.x, t.x);
+                v.y = __fadd_rn(v.y, t.y);
+                v.z = __fadd_rn(v.z, t.z);
+                v.w = __fadd_rn(v.w, t.w);
+            }
+            reinterpret_cast<float4*>(cta)[c] = v;
+        }
     }
 }
 
-// dweight, dbias from the CTAs' partial sums: 32 columns to a CTA, 8 runs of partial sums to a column
-__global__ void __launch_bounds__(256)
-norm_param_join_kernel(const float* __restrict__ parts, uint32_t num, uint32_t d, float* __restrict__ dweight,
-                       float* __restrict__ dbias) {
-    __shared__ float s[2][8][33];
+// dweight, dbias from the CTAs' partial sums: 32 columns to a CTA, a run of partial sums to each of its warps
+constexpr uint32_t kJoinRuns = 32u;
+__global__ void __launch_bounds__(32 * kJoinRuns)
+norm_param_join_kernel(const float* __restrict__ parts, uint32_t num, uint32_t d, uint32_t width,
+                       float* __restrict__ dweight, float* __restrict__ dbias) {
+    __shared__ float s[2][kJoinRuns][33];
     chain_wait_previous();
     const uint32_t lane = threadIdx.x & 31u, run = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
     float w = 0.0f, b = 0.0f;
     if (col < d) {
-#pragma unroll 4
-        for (uint32_t i = run; i < num; i += 8) {
-            const float* p = parts + static_cast<size_t>(i) * 2 * d;
-            w = __fadd_rn(w, p[col]);
-            b = __fadd_rn(b, p[d + col]);
+#pragma unroll 5
+        for (uint32_t i = run; i < num; i += kJoinRuns) {
+            const float* p = parts + static_cast<size_t>(i) * 2 * width;
+            w = __fadd_rn(w, __ldcg(p + col));
+            b = __fadd_rn(b, __ldcg(p + width + col));
         }
     }
     s[0][run][lane] = w;
     s[1][run][lane] = b;
     __syncthreads();
-    if (run < 2 && col < d) {
-        float v = s[run][0][lane];
-        for (uint32_t i = 1; i < 8; ++i) v = __fadd_rn(v, s[run][i][lane]);
-        float* out = run == 0 ? dweight : dbias;
-        if (out) out[col] = v;
+    // warp r adds up column r of this CTA's: dweight, then dbias
+    float v = warp_join<SumOp>(s[0][lane][run]), u = warp_join<SumOp>(s[1][lane][run]);
+    const uint32_t mine = blockIdx.x * 32 + run;
+    if (lane == 0 && mine < d) {
+        if (dweight) dweight[mine] = v;
+        if (dbias) dbias[mine] = u;
     }
 }
 
@@ -510,6 +678,11 @@ norm_bwd_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, uint32_t
     }
 }
 
+// every row of a matrix starts on a 16-byte boundary
+bool on_boundaries(const void* p, uint32_t rows, uint32_t ld, size_t es) {
+    return aligned_to(p, 16) && (rows == 1 || static_cast<size_t>(ld) * es % 16 == 0);
+}
+
 uint32_t norm_parts(uint32_t rows) { return rows < kMaxParts ? (rows ? rows : 1) : kMaxParts; }
 
 template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits>
@@ -518,13 +691,34 @@ dct_status_t launch_fwd_units(const T* x, uint32_t rows, uint32_t d, uint32_t ld
     constexpr uint32_t kGroups = kThreads / kGroup, E = Unit<T>::kElems;
     auto kernel = norm_fwd_units_kernel<T, P, kGroup, kThreads, kUnits>;
     // an image only if some row of y does not start on a boundary
-    const bool aligned = aligned_to(y, 16) && (rows == 1 || static_cast<size_t>(ld_y) * sizeof(T) % 16 == 0);
-    const size_t smem = aligned ? 0 : static_cast<size_t>(kGroups) * ((d + E - 1) / E) * 16;
+    const size_t smem = on_boundaries(y, rows, ld_y, sizeof(T)) ? 0 : static_cast<size_t>(kGroups) * ((d + E - 1) / E) * 16;
     if (smem > 40 * 1024)
         DCT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
     const uint64_t ctas = (static_cast<uint64_t>(rows) + kGroups - 1) / kGroups;
     kernel<<<static_cast<uint32_t>(ctas < (1u << 30) ? ctas : 1u << 30), kThreads, smem, stream>>>(
         x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out);
+    DCT_CUDA_TRY(cudaGetLastError());
+    return DCT_OK;
+}
+
+template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits>
+dct_status_t launch_fwd_ring(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* weight, const P* bias, float eps, T* y,
+                             uint32_t ld_y, float* mean_out, float* rstd_out, cudaStream_t stream) {
+    constexpr uint32_t kGroups = kThreads / kGroup, E = Unit<T>::kElems;
+    const int sms = sm_count();
+    if (sms <= 0) return DCT_ERR_CUDA;
+    const bool whole = d == E * kGroup * kUnits && on_boundaries(x, rows, ld, sizeof(T)) && on_boundaries(y, rows, ld_y, sizeof(T));
+    auto kernel = whole ? norm_fwd_ring_kernel<T, P, kGroup, kThreads, kUnits, true> : norm_fwd_ring_kernel<T, P, kGroup, kThreads, kUnits, false>;
+    const uint32_t slot_units = (d + E - 1) / E + 1;       // (an unaligned row touches one piece more)
+    const size_t smem = 16 * (2 * static_cast<size_t>(ParamImage<P, E>::kPieces) * kGroup * kUnits +
+                              static_cast<size_t>(kGroups) * (kRing + 1) * slot_units);
+    if (smem > 40 * 1024)
+        DCT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    uint32_t per_sm = static_cast<uint32_t>(227 * 1024 / (smem + 2048));
+    per_sm = per_sm < 1 ? 1 : per_sm < fwd_ctas<kThreads, kUnits>() ? per_sm : fwd_ctas<kThreads, kUnits>();
+    const uint64_t wanted = (static_cast<uint64_t>(rows) + kGroups - 1) / kGroups, room = static_cast<uint64_t>(sms) * per_sm;
+    kernel<<<static_cast<uint32_t>(wanted < room ? wanted : room), kThreads, smem, stream>>>(
+        x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out, slot_units, 1.0f / static_cast<float>(d), debug_config().spin_limit);
     DCT_CUDA_TRY(cudaGetLastError());
     return DCT_OK;
 }
@@ -537,21 +731,25 @@ dct_status_t launch_norm_fwd(const void* x_, uint32_t rows, uint32_t d, uint32_t
     const P *weight = static_cast<const P*>(weight_), *bias = static_cast<const P*>(bias_);
     const uint32_t units = (d + Unit<T>::kElems - 1) / Unit<T>::kElems;
     auto go = [&](auto launch) { return launch(x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out, stream); };
-    if (units <= 32) return go(launch_fwd_units<T, P, 32, 128, 1>);
-    if (units <= 64) return go(launch_fwd_units<T, P, 32, 128, 2>);
-    if (units <= 128) return go(launch_fwd_units<T, P, 32, 128, 4>);
-    if (units <= 256) return go(launch_fwd_units<T, P, 128, 128, 2>);
-    if (units <= 512) return go(launch_fwd_units<T, P, 128, 128, 4>);
-    if (units <= 1024) return go(launch_fwd_units<T, P, 256, 256, 4>);
-    if (units <= 2048) return go(launch_fwd_units<T, P, 512, 512, 4>);
+    if (units <= 32) return go(launch_fwd_ring<T, P, 32, 256, 1>);
+    if (units <= 64) return go(launch_fwd_ring<T, P, 32, 256, 2>);
+    if (units <= 128) return go(launch_fwd_ring<T, P, 32, 256, 4>);
+    if (units <= 256) return go(launch_fwd_ring<T, P, 128, 128, 2>);
+    if (units <= 512) return go(launch_fwd_ring<T, P, 256, 256, 2>);
+    if (units <= 1024) return go(launch_fwd_ring<T, P, 256, 256, 4>);
+    if (units <= 2048) {
+        // (the ring and both arrays of parameters fit an SM's shared memory unless fp32 parameters come with bf16 rows)
+        if constexpr (sizeof(P) <= sizeof(T)) return go(launch_fwd_ring<T, P, 512, 512, 4>);
+        else return go(launch_fwd_units<T, P, 512, 512, 4>);
+    }
     const uint32_t grid = rows < 4096u ? rows : 4096u;
     norm_fwd_kernel<T, P><<<grid, kNormThreads, 0, stream>>>(x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out);
     DCT_CUDA_TRY(cudaGetLastError());
     return DCT_OK;
 }
 
-dct_status_t launch_param_join(const float* parts, uint32_t num, uint32_t d, float* dweight, float* dbias, cudaStream_t stream) {
-    DCT_CUDA_TRY(launch_chained(norm_param_join_kernel, (d + 31) / 32, 256, stream, parts, num, d, dweight, dbias));
+dct_status_t launch_param_join(const float* parts, uint32_t num, uint32_t d, uint32_t width, float* dweight, float* dbias, cudaStream_t stream) {
+    DCT_CUDA_TRY(launch_chained(norm_param_join_kernel, (d + 31) / 32, 32 * kJoinRuns, stream, parts, num, d, width, dweight, dbias));
     return DCT_OK;
 }
 
@@ -562,7 +760,9 @@ dct_status_t launch_bwd_units(const T* dy, uint32_t ld_dy, const T* x, uint32_t 
     constexpr uint32_t kGroups = kThreads / kGroup, E = Unit<T>::kElems;
     const int sms = sm_count();
     if (sms <= 0) return DCT_ERR_CUDA;
-    auto kernel = norm_bwd_units_kernel<T, P, kGroup, kThreads, kUnits>;
+    const bool whole = d == E * kGroup * kUnits && on_boundaries(x, rows, ld, sizeof(T)) &&
+                       on_boundaries(dy, rows, ld_dy, sizeof(T)) && on_boundaries(dx, rows, ld_dx, sizeof(T));
+    auto kernel = whole ? norm_bwd_units_kernel<T, P, kGroup, kThreads, kUnits, true> : norm_bwd_units_kernel<T, P, kGroup, kThreads, kUnits, false>;
     const uint32_t slot_units = (d + E - 1) / E + 1;       // (an unaligned row touches one piece more)
     const size_t smem = static_cast<size_t>(kGroups) * (2 * kRing + 1) * slot_units * 16;
     if (smem > 40 * 1024)
@@ -573,9 +773,9 @@ dct_status_t launch_bwd_units(const T* dy, uint32_t ld_dy, const T* x, uint32_t 
     const uint32_t grid = static_cast<uint32_t>(wanted < room ? wanted : room);
     const bool params = dweight || dbias;
     kernel<<<grid, kThreads, smem, stream>>>(dy, ld_dy, x, rows, d, ld, weight, mean, rstd, dx, ld_dx,
-                                             params ? parts : nullptr, slot_units, debug_config().spin_limit);
+                                             params ? parts : nullptr, slot_units, 1.0f / static_cast<float>(d), debug_config().spin_limit);
     DCT_CUDA_TRY(cudaGetLastError());
-    return params ? launch_param_join(parts, grid, d, dweight, dbias, stream) : DCT_OK;
+    return params ? launch_param_join(parts, grid, d, (d + E - 1) / E * E, dweight, dbias, stream) : DCT_OK;
 }
 
 template <typename T, typename P>
@@ -587,9 +787,12 @@ dct_status_t launch_norm_bwd(const void* dy_, uint32_t ld_dy, const void* x_, ui
     const P* weight = static_cast<const P*>(weight_);
     const uint32_t units = (d + Unit<T>::kElems - 1) / Unit<T>::kElems;
     auto go = [&](auto launch) { return launch(dy, ld_dy, x, rows, d, ld, weight, mean, rstd, dx, ld_dx, dweight, dbias, parts, stream); };
-    if (units <= 32) return go(launch_bwd_units<T, P, 32, 128, 1>);
-    if (units <= 64) return go(launch_bwd_units<T, P, 32, 128, 2>);
-    if (units <= 128) return go(launch_bwd_units<T, P, sizeof(T) == 4 ? 32 : 128, 128, sizeof(T) == 4 ? 4 : 1>);
+    if (units <= 32) return go(launch_bwd_units<T, P, 32, 256, 1>);
+    if (units <= 64) return go(launch_bwd_units<T, P, 32, 256, 2>);
+    if (units <= 128) {
+        if constexpr (sizeof(T) == 4) return go(launch_bwd_units<T, P, 32, 256, 4>);
+        else return go(launch_bwd_units<T, P, 128, 128, 1>);
+    }
     if (units <= 256) return go(launch_bwd_units<T, P, 256, 256, 1>);
     if (units <= 512) return go(launch_bwd_units<T, P, 256, 256, 2>);
     if (units <= 1024) return go(launch_bwd_units<T, P, 512, 512, 2>);
@@ -599,7 +802,7 @@ dct_status_t launch_norm_bwd(const void* dy_, uint32_t ld_dy, const void* x_, ui
         const uint32_t cols = (d + kNormThreads - 1) / kNormThreads, num = norm_parts(rows);
         norm_param_parts_kernel<T><<<dim3(cols, num), kNormThreads, 0, stream>>>(dy, ld_dy, x, rows, d, ld, mean, rstd, parts);
         DCT_CUDA_TRY(cudaGetLastError());
-        const dct_status_t st = launch_param_join(parts, num, d, dweight, dbias, stream);
+        const dct_status_t st = launch_param_join(parts, num, d, d, dweight, dbias, stream);
         if (st != DCT_OK) return st;
     }
     const uint32_t grid = rows < 4096u ? rows : 4096u;
@@ -639,7 +842,7 @@ extern "C" dct_status_t dct_layer_norm_fwd(const void* x, dct_dtype_t dtype, uin
 
 extern "C" size_t dct_layer_norm_bwd_workspace_bytes(uint32_t rows, uint32_t d) {
     if (d == 0 || d > kNormMaxWidth) return 0;
-    return (static_cast<size_t>(norm_parts(rows)) * 2 * d * sizeof(float) + 255) & ~static_cast<size_t>(255);
+    return (static_cast<size_t>(norm_parts(rows)) * 2 * ((d + 7) / 8 * 8) * sizeof(float) + 255) & ~static_cast<size_t>(255);
 }
 
 extern "C" dct_status_t dct_layer_norm_bwd(const void* dy, uint32_t ld_dy, const void* x, dct_dtype_t dtype,
