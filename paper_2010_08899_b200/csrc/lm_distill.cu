@@ -402,8 +402,9 @@ dct_status_t launch_distill_shape(const void* logits, void* grad, const DistillA
     const size_t smem = (kStaged ? static_cast<size_t>(a.chunks) * kChunkBytes : 0) + 4 * static_cast<size_t>(a.mark_words) +
                         20 * static_cast<size_t>(a.top);
     auto kernel = lm_distill_kernel<T, kThreads, kTail, kCluster, kStaged>;
-    if (smem > 32 * 1024)
-        DCT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    static std::atomic<uint32_t> allowed[64];
+    const dct_status_t allowed_st = allow_shared(kernel, smem, allowed);
+    if (allowed_st != DCT_OK) return allowed_st;
     uint32_t per_sm = static_cast<uint32_t>((227 * 1024) / (smem + 3 * 1024));
     per_sm = per_sm < 1 ? 1 : per_sm < 768 / kThreads ? per_sm : 768 / kThreads;
     const T* x = static_cast<const T*>(logits);

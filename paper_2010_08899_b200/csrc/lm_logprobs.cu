@@ -32,7 +32,7 @@ template <uint32_t kThreads> struct LogProbShared {
     RowPart part;                      // this CTA's slice
     float m, logsum;                   // of the whole row
     uint32_t counts[32];
-    uint32_t counter, hit_count, bound;
+    uint32_t counter, hit_count, bound, tied;
 };
 
 __device__ __forceinline__ float value_of_key(uint32_t key) {       // the inverse of order_key
@@ -65,10 +65,11 @@ template <typename T, uint32_t kThreads> struct Selector {
         return static_cast<uint64_t>(key) << 32 | (0xFFFFFFFFu - col);
     }
     // By one warp, from the class maxima: a key that at least kk of them reach, and not many more if that can be had
-    // (0 if fewer than kk classes have a unit).
-    __device__ __forceinline__ uint32_t find_bound(uint32_t kk) const {
+    // (0 if fewer than kk classes have a unit).  tied: many more of them equal it.
+    __device__ __forceinline__ uint32_t find_bound(uint32_t kk, bool& tied) const {
         constexpr uint32_t N = 2 * kThreads / 32;
         const uint32_t units = u1 - u0;
+        tied = false;
         if (min(units, 2 * kThreads) < kk) return 0;
         uint32_t key[N], lo = 0xFFFFFFFFu, hi = 0;
 #pragma unroll
@@ -89,8 +90,12 @@ template <typename T, uint32_t kThreads> struct Selector {
             n = __reduce_add_sync(0xFFFFFFFFu, n);
             if (n >= kk) lo = mid;
             else hi = mid - 1;
-            if (n >= kk && n <= kk + kk / 8 + 1) break;
+            if (n >= kk && n <= kk + kk / 8 + 1) return lo;
         }
+        uint32_t n = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) n += key[i] >= lo;
+        tied = __reduce_add_sync(0xFFFFFFFFu, n) > 2 * kk + 8;
         return lo;
     }
     // candidates := the slice's columns with key >= low; returns how many there are, of which the first kCandidates
@@ -173,8 +178,8 @@ template <typename T, uint32_t kThreads> struct Selector {
         }
         return lo;
     }
-    // appends the lowest columns whose key is `key` until there are kk candidates
-    __device__ __noinline__ static void fill_with_equals(const Selector s, uint32_t key, uint32_t have, uint32_t kk) {
+    // appends the lowest columns whose key is `key` until there are kk candidates; returns how many there are then
+    __device__ __noinline__ static uint32_t fill_with_equals(const Selector s, uint32_t key, uint32_t have, uint32_t kk) {
         for (uint32_t first = s.u0; first < s.u1 && have < kk; first += kThreads) {
             const uint32_t u = first + threadIdx.x;
             uint32_t mine = 0;
@@ -203,6 +208,7 @@ template <typename T, uint32_t kThreads> struct Selector {
             have += all;
         }
         __syncthreads();
+        return min(have, kk);
     }
     // keeps the kk best of n candidates, kk < n, in no order
     __device__ __noinline__ static void cut(LogProbShared<kThreads>& sh, uint32_t n, uint32_t kk) {
@@ -260,12 +266,17 @@ template <typename T, uint32_t kThreads> struct Selector {
     // best[0 .. kk) := the slice's kk best columns in order.  The class maxima are in class_max.
     __device__ __forceinline__ void run(uint32_t kk) const {
         if (threadIdx.x < 32) {
-            const uint32_t b = find_bound(kk);
-            if (threadIdx.x == 0) sh.bound = b;
+            bool tied;
+            const uint32_t b = find_bound(kk, tied);
+            if (threadIdx.x == 0) {
+                sh.bound = b;
+                sh.tied = tied;
+            }
         }
         __syncthreads();
-        uint32_t bound = sh.bound, low = bound, n;
-        bool above = false;                    // the candidates are the columns above the bound
+        // (rows that a mask leaves little of: the columns that equal the bound are too many to look at, their lowest few will do)
+        bool above = sh.tied;                  // the candidates are the columns above the bound
+        uint32_t bound = sh.bound, low = bound + above, n;
         for (;;) {
             n = collect(low);
             if (n < kk && !above && bound != 0) {        // classes whose only elements lie outside the row or are NaN
@@ -279,7 +290,8 @@ template <typename T, uint32_t kThreads> struct Selector {
             }
         }
         if (n < kk) {
-            fill_with_equals(*this, bound, n, kk);
+            n = fill_with_equals(*this, bound, n, kk);
+            if (n < kk) fill_with_equals(*this, 0, n, kk);       // NaN: some class of the bound had nothing else
             n = kk;
         }
         if (n > kRankable) {

@@ -692,8 +692,9 @@ dct_status_t launch_fwd_units(const T* x, uint32_t rows, uint32_t d, uint32_t ld
     auto kernel = norm_fwd_units_kernel<T, P, kGroup, kThreads, kUnits>;
     // an image only if some row of y does not start on a boundary
     const size_t smem = on_boundaries(y, rows, ld_y, sizeof(T)) ? 0 : static_cast<size_t>(kGroups) * ((d + E - 1) / E) * 16;
-    if (smem > 40 * 1024)
-        DCT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    static std::atomic<uint32_t> allowed[64];
+    const dct_status_t allowed_st = allow_shared(kernel, smem, allowed);
+    if (allowed_st != DCT_OK) return allowed_st;
     const uint64_t ctas = (static_cast<uint64_t>(rows) + kGroups - 1) / kGroups;
     kernel<<<static_cast<uint32_t>(ctas < (1u << 30) ? ctas : 1u << 30), kThreads, smem, stream>>>(
         x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out);
@@ -712,8 +713,9 @@ dct_status_t launch_fwd_ring(const T* x, uint32_t rows, uint32_t d, uint32_t ld,
     const uint32_t slot_units = (d + E - 1) / E + 1;       // (an unaligned row touches one piece more)
     const size_t smem = 16 * (2 * static_cast<size_t>(ParamImage<P, E>::kPieces) * kGroup * kUnits +
                               static_cast<size_t>(kGroups) * (kRing + 1) * slot_units);
-    if (smem > 40 * 1024)
-        DCT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    static std::atomic<uint32_t> allowed[2][64];
+    const dct_status_t allowed_st = allow_shared(kernel, smem, allowed[whole]);
+    if (allowed_st != DCT_OK) return allowed_st;
     uint32_t per_sm = static_cast<uint32_t>(227 * 1024 / (smem + 2048));
     per_sm = per_sm < 1 ? 1 : per_sm < fwd_ctas<kThreads, kUnits>() ? per_sm : fwd_ctas<kThreads, kUnits>();
     const uint64_t wanted = (static_cast<uint64_t>(rows) + kGroups - 1) / kGroups, room = static_cast<uint64_t>(sms) * per_sm;
@@ -765,8 +767,9 @@ dct_status_t launch_bwd_units(const T* dy, uint32_t ld_dy, const T* x, uint32_t 
     auto kernel = whole ? norm_bwd_units_kernel<T, P, kGroup, kThreads, kUnits, true> : norm_bwd_units_kernel<T, P, kGroup, kThreads, kUnits, false>;
     const uint32_t slot_units = (d + E - 1) / E + 1;       // (an unaligned row touches one piece more)
     const size_t smem = static_cast<size_t>(kGroups) * (2 * kRing + 1) * slot_units * 16;
-    if (smem > 40 * 1024)
-        DCT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    static std::atomic<uint32_t> allowed[2][64];
+    const dct_status_t allowed_st = allow_shared(kernel, smem, allowed[whole]);
+    if (allowed_st != DCT_OK) return allowed_st;
     const uint64_t wanted = (static_cast<uint64_t>(rows) + kGroups - 1) / kGroups;
     uint64_t room = static_cast<uint64_t>(sms) * (512 / kThreads);
     if (room > kMaxParts) room = kMaxParts;

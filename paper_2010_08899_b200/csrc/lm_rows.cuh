@@ -284,11 +284,35 @@ __device__ __noinline__ RowPart low_part(const RowView<T> row, uint32_t u0, uint
 struct RowSums {
     static constexpr float kSlack = 4.0f;
     float ref, s, st;
-    __device__ __forceinline__ RowSums() : ref(minus_inf()), s(0.0f), st(0.0f) {}
+    bool masked;                   // this thread has met -inf beside numbers
+    __device__ __forceinline__ RowSums() : ref(minus_inf()), s(0.0f), st(0.0f), masked(false) {}
 
+    // sums over four units.  kClamp: y at least -200, so that a masked column (2^y = 0, y = -inf) adds 0 to the moment and not NaN
+    template <typename T, bool kMoment, bool kClamp>
+    __device__ __forceinline__ void batch(const uint4 (&v)[4], float c, float& sum, float& moment) const {
+        constexpr int E = Unit<T>::kElems;
+        const uint64_t scale = pack2(c, c), shift = pack2(-ref, -ref);
+        uint64_t sb = 0, stb = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < E; i += 2) {
+                uint64_t y = fma2(pack2(Unit<T>::get(v[u], i), Unit<T>::get(v[u], i + 1)), scale, shift);
+                float y0, y1;
+                unpack2(y, y0, y1);
+                if (kClamp) y = pack2(y0 = max_nan(y0, -200.0f), y1 = max_nan(y1, -200.0f));
+                const uint64_t e = pack2(exp2_fast(y0), exp2_fast(y1));
+                sb = add2(sb, e);
+                if (kMoment) stb = fma2(e, y, stb);
+            }
+        float p, q;
+        unpack2(sb, p, q);
+        sum = __fadd_rn(p, q);
+        unpack2(stb, p, q);
+        moment = __fadd_rn(p, q);
+    }
     // best: the largest of this thread's four units; all lanes of the warp take part
     template <typename T, bool kMoment> __device__ __forceinline__ void add(const uint4 (&v)[4], float best, float c) {
-        constexpr int E = Unit<T>::kElems;
         if (__any_sync(0xFFFFFFFFu, !(__fmul_rn(best, c) <= __fadd_rn(ref, kSlack)))) {
             const float to = __fmul_rn(warp_max(best), c);
             if (to > ref) {
@@ -305,41 +329,22 @@ struct RowSums {
 #pragma unroll
             for (int u = 0; u < 4; ++u)
 #pragma unroll
-                for (int i = 0; i < E; ++i) any = __fadd_rn(any, Unit<T>::get(v[u], i));
+                for (int i = 0; i < Unit<T>::kElems; ++i) any = __fadd_rn(any, Unit<T>::get(v[u], i));
             if (any != any) s = any;
             return;
         }
-        const uint64_t scale = pack2(c, c), shift = pack2(-ref, -ref);
-        uint64_t sb = 0, stb = 0;
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int i = 0; i < E; i += 2) {
-                const uint64_t y = fma2(pack2(Unit<T>::get(v[u], i), Unit<T>::get(v[u], i + 1)), scale, shift);
-                float y0, y1;
-                unpack2(y, y0, y1);
-                const uint64_t e = pack2(exp2_fast(y0), exp2_fast(y1));
-                sb = add2(sb, e);
-                if (kMoment) stb = fma2(e, y, stb);
+        float sum, moment = 0.0f;
+        if (!kMoment) {
+            batch<T, false, false>(v, c, sum, moment);
+        } else {
+            if (!masked) {
+                batch<T, true, false>(v, c, sum, moment);
+                masked = moment != moment;
             }
-        float p, q;
-        unpack2(sb, p, q);
-        s = __fadd_rn(s, __fadd_rn(p, q));
-        if (kMoment) {
-            unpack2(stb, p, q);
-            float sum = __fadd_rn(p, q);
-            if (sum != sum) {            // 0 * -inf at masked columns: leave those out
-                sum = 0.0f;
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-#pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        const float y = fmaf(Unit<T>::get(v[u], i), c, -ref), e = exp2_fast(y);
-                        if (e != 0.0f) sum = fmaf(e, y, sum);
-                    }
-            }
-            st = __fadd_rn(st, sum);
+            if (masked) batch<T, true, true>(v, c, sum, moment);
         }
+        s = __fadd_rn(s, sum);
+        if (kMoment) st = __fadd_rn(st, moment);
     }
     // the warp's sums as a part; xmax: the warp's largest x
     template <bool kMoment> __device__ __forceinline__ RowPart part(float xmax, float c) const {
@@ -502,6 +507,20 @@ inline bool in_place_or_apart(const void* in, uint32_t ld_in, const void* out, u
     return (in == out && ld_in == ld_out) ||
            !spans_overlap(in, span_bytes(rows, d, ld_in, es), out, span_bytes(rows, d, ld_out, es));
 }
+// lets `kernel` have `bytes` of dynamic shared memory, once per device and amount.  (Without asking it has 48 KiB, of which static
+// shared memory is a part: asked for from well below that.)  allowed: zeros at first, the kernel's own.
+template <typename... Params>
+inline dct_status_t allow_shared(void (*kernel)(Params...), size_t bytes, std::atomic<uint32_t> (&allowed)[64]) {
+    if (bytes <= 32 * 1024) return DCT_OK;
+    int dev = 0;
+    DCT_CUDA_TRY(cudaGetDevice(&dev));
+    std::atomic<uint32_t>* word = dev >= 0 && dev < 64 ? &allowed[dev] : nullptr;
+    if (word && word->load(std::memory_order_relaxed) >= bytes) return DCT_OK;
+    DCT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
+    if (word) word->store(static_cast<uint32_t>(bytes), std::memory_order_relaxed);
+    return DCT_OK;
+}
+
 inline float log2_scale(float inv_t) { return static_cast<float>(1.4426950408889634 * inv_t); }
 inline bool usable_temperature(float inv_t) { return std::isfinite(inv_t) && inv_t > 0.0f; }
 
