@@ -95,6 +95,17 @@ def mp_gradients(rows: int, d: int, seed: int, dtype=torch.float32, device="cpu"
     return x.to(dtype).contiguous()
 
 
+def lm_logits(rows: int, vocab: int, seed: int, dtype=torch.float32, device="cpu") -> torch.Tensor:
+    """Logits [rows, vocab] as a language model gives them: a unigram slope over the columns in random order, Gaussian
+    noise, and one favoured column per row."""
+    g = _gen(seed, device)
+    slope = -0.7 * torch.log(torch.randperm(vocab, generator=g, device=device).float() + 1.0)
+    x = torch.randn(rows, vocab, generator=g, device=device) * 2.0 + slope
+    target = torch.randint(0, vocab, (rows, 1), generator=g, device=device)
+    x.scatter_add_(1, target, 4.0 + 8.0 * torch.rand(rows, 1, generator=g, device=device))
+    return x.to(dtype).contiguous()
+
+
 def quantize_mantissa(x: torch.Tensor, keep_bits: int) -> torch.Tensor:
     """Round-toward-zero fp32 values to ``keep_bits`` mantissa bits: a cheap way to force many ties."""
     assert x.dtype == torch.float32

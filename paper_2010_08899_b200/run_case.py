@@ -14,6 +14,11 @@ A small command-line driver for profiling and quick timing of a single kernel at
     python -m paper_2010_08899_b200.run_case mp_fwd_sweep --dtype bf16    (a table: row widths x sparsity levels)
     python -m paper_2010_08899_b200.run_case dp_sweep                     (a table: vector sizes x densities)
     python -m paper_2010_08899_b200.run_case receiver_sweep               (backward pack, unpack, decompress over shapes)
+    python -m paper_2010_08899_b200.run_case norm_fwd --rows 16384 --d 4096 --dtype bf16      (layer norm; norm_bwd)
+    python -m paper_2010_08899_b200.run_case logprobs --rows 4096 --d 32768 --k 64 --dtype bf16
+    python -m paper_2010_08899_b200.run_case logprobs_bwd / distill / distill_tail            (same arguments)
+    python -m paper_2010_08899_b200.run_case student_step --rows 1024 --d 512 --vocab 32768 --k 64
+                                                                 (a split student learns from a teacher: all of it together)
 
 It prints the mean device time per call (CUDA events) and the algorithmic GB/s.
 """
@@ -165,14 +170,77 @@ def receiver_sweep(args, dev, stream):
               f"{ms_a:7.4f} ({(8 * n + 8 * cnt) / ms_a / 1e9:5.2f})", flush=True)
 
 
+def lm_call(args, dev):
+    """One call of the layer norm or of an operator on rows of logits (--d columns, --k alternatives or teacher slots) on
+    three sets of inputs by turns, and the bytes it cannot do without."""
+    rows, d, k = args.rows, args.d, args.k or 20
+    dt = torch.float32 if args.dtype == "f32" else torch.bfloat16
+    es = 4 if args.dtype == "f32" else 2
+    new = lambda *shape, t=torch.float32: torch.empty(*shape, dtype=t, device=dev)
+    if args.entry.startswith("norm"):
+        x = [inputs.mp_gradients(rows, d, 510 + j, dtype=dt, device=dev) for j in range(3)]
+        out = [torch.empty_like(x[0]) for _ in range(3)]
+        w, b, mean, rstd = torch.ones(d, device=dev), torch.zeros(d, device=dev), new(rows), new(rows)
+        fwd = lambda i: B.dct_layer_norm_fwd(x[i % 3], rows, d, d, w, b, 1e-5, out[i % 3], d, mean, rstd)
+        if args.entry == "norm_fwd":
+            return fwd, 2 * rows * d * es
+        fwd(0)
+        dy = [inputs.mp_gradients(rows, d, 520 + j, dtype=dt, device=dev) for j in range(3)]
+        dw, db = new(d), new(d)
+        ws = B.new_workspace(B.dct_layer_norm_bwd_workspace_bytes(rows, d), dev)
+        return (lambda i: B.dct_layer_norm_bwd(dy[i % 3], d, x[i % 3], rows, d, d, w, mean, rstd, out[i % 3], d, dw, db, ws),
+                3 * rows * d * es)
+    x = [inputs.lm_logits(rows, d, 530 + j, dtype=dt, device=dev) for j in range(3)]
+    grad = [torch.empty_like(x[0]) for _ in range(3)]
+    tokens = torch.arange(rows, dtype=torch.int32, device=dev) % d
+    lp, ent, stats = new(rows), new(rows), new(rows, 2)
+    ids, lps = new(rows, k, t=torch.int32), new(rows, k)
+    fwd = lambda i: B.dct_lm_logprobs_fwd(x[i % 3], rows, d, d, 1.0, tokens, k, lp, ent, stats, ids, lps)
+    if args.entry == "logprobs":
+        return fwd, rows * d * es
+    fwd(0)
+    if args.entry == "logprobs_bwd":
+        a = torch.ones(rows, device=dev)
+        return (lambda i: B.dct_lm_logprobs_bwd(x[0], rows, d, d, 1.0, tokens, stats, ent, a, a, grad[i % 3], d),
+                2 * rows * d * es)
+    mode = B.DCT_DISTILL_TAIL if args.entry == "distill_tail" else B.DCT_DISTILL_RENORM
+    loss = new(rows)
+    return (lambda i: B.dct_lm_distill(x[i % 3], rows, d, d, 1.0, ids, lps, k, mode, None, loss, grad[i % 3], d),
+            2 * rows * d * es)
+
+
+def student_step(args, dev, stream):
+    """A student (layer norm, split with DCT-MP, projection) learns from a teacher's top log-probabilities, its gradient sent
+    by DCT-DP: --iters steps on one batch of --rows rows of --d features and --vocab columns, --k slots per row."""
+    from .student import Student
+    rows, d, vocab, top = args.rows, args.d, args.vocab, args.k or 64
+    dt = torch.float32 if args.dtype == "f32" else torch.bfloat16
+    s = Student(d, vocab, rows, keep=B.k_from_sparsity(d, 75, 100), top=top, dtype=dt, device=dev, lr=20.0)
+    hidden = inputs.mp_gradients(rows, d, 551, dtype=dt, device=dev)
+    teacher = inputs.lm_logits(rows, vocab, 552, dtype=dt, device=dev)
+    tokens = teacher.argmax(1).to(torch.int32)
+    for i in range(max(2, args.iters)):
+        a = torch.cuda.Event(enable_timing=True)
+        b = torch.cuda.Event(enable_timing=True)
+        a.record(stream)
+        r = s.step(hidden, teacher)
+        b.record(stream)
+        b.synchronize()
+        lp, ent, _, _ = s.score(hidden, tokens)
+        print(f"step {i}: loss {float(r.loss.mean()):.4f}, {B.read_result(r.sent).count} of {s.params.numel()} gradients sent, "
+              f"{a.elapsed_time(b):.3f} ms; afterwards log p of the teacher's choice {float(lp.mean()):.4f}, entropy {float(ent.mean()):.4f}")
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("entry", choices=["select", "compress", "select_compress", "compress_layers", "decompress", "mp_fwd", "mp_bwd", "mp_unpack",
-                                     "select_multi", "threshold_mean", "mp_fwd_sweep", "dp_sweep", "receiver_sweep"])
+                                     "select_multi", "threshold_mean", "mp_fwd_sweep", "dp_sweep", "receiver_sweep",
+                                     "norm_fwd", "norm_bwd", "logprobs", "logprobs_bwd", "distill", "distill_tail", "student_step"])
     ap.add_argument("--n", type=int, default=1 << 28)
     ap.add_argument("--k", type=int, default=0, help="survivor target (default: 0.01 %% of n, or 5 %% of d)")
     ap.add_argument("--rows", type=int, default=16384)
     ap.add_argument("--d", type=int, default=4096)
+    ap.add_argument("--vocab", type=int, default=32768, help="student_step: columns of the logits")
     ap.add_argument("--dtype", choices=["f32", "bf16"], default="bf16")
     ap.add_argument("--dist", choices=["mixture", "gaussian", "dlrm"], default="mixture")
     ap.add_argument("--iters", type=int, default=3)
@@ -205,6 +273,8 @@ def main():
         return dp_sweep(args, dev, stream)
     if args.entry == "receiver_sweep":
         return receiver_sweep(args, dev, stream)
+    if args.entry == "student_step":
+        return student_step(args, dev, stream)
     gen = {"mixture": inputs.dp_mixture, "gaussian": inputs.dp_gaussian, "dlrm": inputs.dp_dlrm_like}[args.dist]
 
     if args.entry == "compress_layers":
@@ -331,6 +401,8 @@ def main():
                 call = lambda i: B.dct_dp_decompress(idx, val, packed, cap, dense, n, False, res2)
                 reset = lambda: None
                 nbytes = 4 * n + 8 * count       # clear the dense vector, read the packed pairs
+    elif args.entry in ("norm_fwd", "norm_bwd", "logprobs", "logprobs_bwd", "distill", "distill_tail"):
+        call, nbytes = lm_call(args, dev)
     else:
         rows, d = args.rows, args.d
         k = args.k or B.k_from_sparsity(d, 95, 100)
