@@ -6,7 +6,7 @@ namespace {
 
 constexpr uint32_t kNormMaxWidth = 65536u;
 constexpr uint32_t kNormThreads = 256u;
-constexpr uint32_t kMaxParts = 148u * 4u;        // CTAs that leave partial sums of the parameter gradients, at most
+constexpr uint32_t kMaxParts = 148u * 6u;        // CTAs that leave partial sums of the parameter gradients, at most
 
 // Rows as units of 16 bytes counted from the row's own first element.  Where a row does not start on a 16-byte boundary, a unit is
 // put together from the two aligned pieces it lies in; these are inside the row but for the bytes next to its ends, which share
@@ -34,19 +34,27 @@ template <typename T> struct NormRow {
         pieces = (off + d * static_cast<uint32_t>(sizeof(T)) + 15) / 16;
     }
 };
-// units lane, lane + kGroup, ... of a row whose aligned pieces ld reads (from global or shared memory), all loads before any use;
+// A group of threads works on one row: a warp (kGroup = 32), or the CTA (kGroup = 0; as many warps as the row's width wants, up to 16).
+template <uint32_t kGroup> __device__ __forceinline__ uint32_t group_size() { return kGroup ? kGroup : blockDim.x; }
+template <uint32_t kGroup> __device__ __forceinline__ void group_sync() {
+    if (kGroup == 32) __syncwarp();
+    else __syncthreads();
+}
+// units lane, lane + group size, ... of a row whose aligned pieces ld reads (from global or shared memory), all loads before any use;
 // elements past the row's end are whatever lies there.  kWhole, here and below: the group's lanes hold exactly the row's units, all
 // of them whole, and every row starts on a 16-byte boundary.
 template <uint32_t kGroup, uint32_t kUnits, bool kWhole, typename Ld>
 __device__ __forceinline__ void load_units(uint4 (&v)[kUnits], uint32_t lane, uint32_t units, uint32_t off, uint32_t pieces, Ld&& ld) {
 #pragma unroll
-    for (uint32_t i = 0; i < kUnits; ++i) v[i] = ld(kWhole ? lane + i * kGroup : min(lane + i * kGroup, units - 1));
-    if (kWhole || off == 0) return;
-    uint4 b[kUnits];
+    for (uint32_t i = 0; i < kUnits; ++i) v[i] = ld(kWhole ? lane + i * group_size<kGroup>() : min(lane + i * group_size<kGroup>(), units - 1));
+    if constexpr (!kWhole) {
+        if (off == 0) return;
+        uint4 b[kUnits];
 #pragma unroll
-    for (uint32_t i = 0; i < kUnits; ++i) b[i] = ld(min(lane + i * kGroup + 1, pieces - 1));     // (a last piece again: not used)
+        for (uint32_t i = 0; i < kUnits; ++i) b[i] = ld(min(lane + i * group_size<kGroup>() + 1, pieces - 1));     // (a last piece again: not used)
 #pragma unroll
-    for (uint32_t i = 0; i < kUnits; ++i) v[i] = shifted(v[i], b[i], off);
+        for (uint32_t i = 0; i < kUnits; ++i) v[i] = shifted(v[i], b[i], off);
+    }
 }
 // the unit's elements in pairs; those at and past `left` (elements of the row from the unit's first on) become `fill`
 template <typename T>
@@ -97,11 +105,6 @@ template <typename P> __device__ __forceinline__ bool vector_params(const P* par
     return params && (reinterpret_cast<uintptr_t>(params) & 15u) == 0;
 }
 
-// A group of threads works on one row: a warp (kGroup = 32) or the CTA.
-template <uint32_t kGroup> __device__ __forceinline__ void group_sync() {
-    if (kGroup == 32) __syncwarp();
-    else __syncthreads();
-}
 // sums of a and b over the group, the same in every thread.  slots: 2 x 2 x 32 floats of the group, `turn` alternates from call to
 // call (so that one barrier is enough).
 template <uint32_t kGroup>
@@ -110,31 +113,30 @@ __device__ __forceinline__ void group_sums(float& a, float& b, float* slots, uin
     b = warp_join<SumOp>(b);
     if (kGroup == 32) return;
     float* s = slots + (turn & 1u) * 64;
-    const uint32_t warps = kGroup / 32, lane = lane_id();
+    const uint32_t warps = blockDim.x / 32, lane = lane_id(), w = lane & 15u;
     if (lane == 0) {
         s[threadIdx.x >> 5] = a;
         s[32 + (threadIdx.x >> 5)] = b;
     }
     __syncthreads();
-    a = s[lane & (warps - 1)];
-    b = s[32 + (lane & (warps - 1))];
+    a = w < warps ? s[w] : 0.0f;
+    b = w < warps ? s[32 + w] : 0.0f;
 #pragma unroll
-    for (uint32_t o = warps / 2; o > 0; o >>= 1) {
+    for (uint32_t o = 8; o > 0; o >>= 1) {
         a = __fadd_rn(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
         b = __fadd_rn(b, __shfl_xor_sync(0xFFFFFFFFu, b, o));
     }
 }
-
 template <uint32_t kGroup> __device__ __forceinline__ void group_sum(float& a, float* slots, uint32_t turn) {
     a = warp_join<SumOp>(a);
     if (kGroup == 32) return;
     float* s = slots + (turn & 1u) * 64;
-    const uint32_t warps = kGroup / 32, lane = lane_id();
+    const uint32_t warps = blockDim.x / 32, lane = lane_id(), w = lane & 15u;
     if (lane == 0) s[threadIdx.x >> 5] = a;
     __syncthreads();
-    a = s[lane & (warps - 1)];
+    a = w < warps ? s[w] : 0.0f;
 #pragma unroll
-    for (uint32_t o = warps / 2; o > 0; o >>= 1) a = __fadd_rn(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
+    for (uint32_t o = 8; o > 0; o >>= 1) a = __fadd_rn(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
 }
 
 // A row of d results of a group.  A row on a 16-byte boundary is written unit by unit; another one by way of shared memory
@@ -165,7 +167,7 @@ template <typename T, uint32_t kGroup, bool kWhole> struct RowWriter {
         // piece j holds the row's bytes from 16 j - off on
         const uint32_t bytes = d * static_cast<uint32_t>(sizeof(T)), pieces = (off + bytes + 15) / 16, units = (d + E - 1) / E;
         uint8_t* base = reinterpret_cast<uint8_t*>(row) - off;
-        for (uint32_t j = lane; j < pieces; j += kGroup) {
+        for (uint32_t j = lane; j < pieces; j += group_size<kGroup>()) {
             const uint4 zero = make_uint4(0, 0, 0, 0);
             const uint4 v = shifted(j > 0 ? image[j - 1] : zero, j < units ? image[j] : zero, 16 - off);
             if (j > 0 && 16 * j + 16 <= off + bytes) {
@@ -193,10 +195,10 @@ __global__ void __launch_bounds__(kThreads)
 norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* __restrict__ weight,
                       const P* __restrict__ bias, float eps, T* y, uint32_t ld_y, float* __restrict__ mean_out,
                       float* __restrict__ rstd_out) {
-    constexpr uint32_t E = Unit<T>::kElems, kGroups = kThreads / kGroup;
+    constexpr uint32_t E = Unit<T>::kElems, kGroups = kGroup ? kThreads / kGroup : 1;
     extern __shared__ __align__(16) uint4 images[];
     __shared__ float slots[128];
-    const uint32_t lane = threadIdx.x % kGroup, group = threadIdx.x / kGroup, units = (d + E - 1) / E;
+    const uint32_t lane = kGroup ? threadIdx.x % 32 : threadIdx.x, group = kGroup ? threadIdx.x / 32 : 0, units = (d + E - 1) / E;
     uint4* image = images + group * units;
     const bool vec_w = vector_params(weight), vec_b = vector_params(bias), whole = d % E == 0;
     uint32_t turn = 0;
@@ -209,7 +211,7 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
         uint64_t sum = 0;
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
-            const uint32_t u = lane + i * kGroup;
+            const uint32_t u = lane + i * group_size<kGroup>();
             unit_pairs<T>(raw[i], u < units ? d - u * E : 0u, 0.0f, v[i]);
 #pragma unroll
             for (uint32_t q = 0; q < E / 2; ++q) sum = add2(sum, v[i][q]);
@@ -223,7 +225,7 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
         uint64_t squares = 0;
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
-            const uint32_t u = lane + i * kGroup, left = u < units ? d - u * E : 0u;
+            const uint32_t u = lane + i * group_size<kGroup>(), left = u < units ? d - u * E : 0u;
 #pragma unroll
             for (uint32_t q = 0; q < E / 2; ++q) v[i][q] = add2(v[i][q], minus_mean);
             if (left < E) {                        // what is past the end does not deviate
@@ -245,13 +247,13 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
         RowWriter<T, kGroup, false> out(y + row * ld_y, d, image);
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
-            const uint32_t col = (lane + i * kGroup) * E;
+            const uint32_t col = (lane + i * group_size<kGroup>()) * E;
             uint64_t w[E / 2], b[E / 2];
             param_pairs<P, E>(weight, vec_w && whole, vec_w, col, d, 1.0f, w);
             param_pairs<P, E>(bias, vec_b && whole, vec_b, col, d, 0.0f, b);
 #pragma unroll
             for (uint32_t q = 0; q < E / 2; ++q) v[i][q] = fma2(mul2(v[i][q], by_rstd), w[q], b[q]);
-            out.put(lane + i * kGroup, pack_unit<T>(v[i]));
+            out.put(lane + i * group_size<kGroup>(), pack_unit<T>(v[i]));
         }
         out.finish(lane);
         if (lane == 0) {
@@ -262,8 +264,9 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
 }
 
 // Forward by the same rules for as many rows as a grid that stays has groups for: the rows come through a ring of bulk copies,
-// kRing ahead of the one being worked on, and the parameters lie in shared memory, so that a row's only waits are its two sums.
-constexpr uint32_t kRing = 3u;
+// kFwdRing ahead of the one being worked on, and the parameters lie in shared memory, so that a row's only waits are its two sums.
+// (more rows on their way make the reads outrun the writes, and both slower: 16384 rows of 4096 fp32 with 2 / 3 / 4: 88 / 96 / 107 us)
+constexpr uint32_t kFwdRing = 2u;
 
 // the parameters as they lie in shared memory: 16-byte pieces (fp32 where a unit's bf16 parameters would be less than that),
 // piece q of unit u at [q][u]
@@ -302,23 +305,23 @@ __global__ void __launch_bounds__(kThreads, fwd_ctas<kThreads, kUnits>())
 norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* __restrict__ weight,
                      const P* __restrict__ bias, float eps, T* y, uint32_t ld_y, float* __restrict__ mean_out,
                      float* __restrict__ rstd_out, uint32_t slot_units, float per_column, uint32_t spin_limit) {
-    constexpr uint32_t E = Unit<T>::kElems, kGroups = kThreads / kGroup;
+    constexpr uint32_t E = Unit<T>::kElems, kGroups = kGroup ? kThreads / kGroup : 1;
     using Image = ParamImage<P, E>;
-    extern __shared__ __align__(128) uint4 shared[];       // parameters; per group kRing slots and the image of an unaligned y
+    extern __shared__ __align__(128) uint4 shared[];       // parameters; per group kFwdRing slots and the image of an unaligned y
     __shared__ float slots[128];
-    __shared__ uint64_t full[kGroups][kRing];
+    __shared__ uint64_t full[kGroups][kFwdRing];
     __shared__ uint32_t gave_up;
-    constexpr uint32_t kAll = kGroup * kUnits;             // units the group's lanes hold
-    const uint32_t lane = threadIdx.x % kGroup, group = threadIdx.x / kGroup, units = (d + E - 1) / E;
-    uint4 *const weights = shared, *const biases = shared + Image::kPieces * kAll;
-    uint4* const mine = shared + 2 * Image::kPieces * kAll + group * (kRing + 1) * slot_units;
-    uint4* const image = mine + kRing * slot_units;
+    const uint32_t all = group_size<kGroup>() * kUnits;    // units the group's lanes hold
+    const uint32_t lane = kGroup ? threadIdx.x % 32 : threadIdx.x, group = kGroup ? threadIdx.x / 32 : 0, units = (d + E - 1) / E;
+    uint4 *const weights = shared, *const biases = shared + Image::kPieces * all;
+    uint4* const mine = shared + 2 * Image::kPieces * all + group * (kFwdRing + 1) * slot_units;
+    uint4* const image = mine + kFwdRing * slot_units;
     const uint64_t stride = static_cast<uint64_t>(gridDim.x) * kGroups;
     const uint64_t first = static_cast<uint64_t>(blockIdx.x) * kGroups + group;
 
     if (threadIdx.x == 0) gave_up = 0;
     if (lane == 0) {
-        for (uint32_t s = 0; s < kRing; ++s) mbar_init(&full[group][s], 1);
+        for (uint32_t s = 0; s < kFwdRing; ++s) mbar_init(&full[group][s], 1);
         mbar_init_fence();
         fence_proxy_async_smem();
     }
@@ -330,9 +333,9 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
         bulk_load(mine + slot * slot_units, a.base, 16 * a.pieces, &full[group][slot]);
     };
     if (lane == 0)
-        for (uint32_t s = 0; s < kRing; ++s) fetch(first + s * stride, s);
-    Image::fill(weights, weight, d, kAll, 1.0f);
-    Image::fill(biases, bias, d, kAll, 0.0f);
+        for (uint32_t s = 0; s < kFwdRing; ++s) fetch(first + s * stride, s);
+    Image::fill(weights, weight, d, all, 1.0f);
+    Image::fill(biases, bias, d, all, 0.0f);
     __syncthreads();
 
     uint32_t slot = 0, phase = 0, turn = 0;
@@ -352,7 +355,7 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
         uint64_t sum = 0;
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
-            const uint32_t u = lane + i * kGroup;
+            const uint32_t u = lane + i * group_size<kGroup>();
             unit_pairs<T>(raw[i], kWhole ? E : u < units ? d - u * E : 0u, 0.0f, v[i]);
 #pragma unroll
             for (uint32_t q = 0; q < E / 2; ++q) sum = add2(sum, v[i][q]);
@@ -362,13 +365,13 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
         total = __fadd_rn(s0, s1);
         group_sum<kGroup>(total, slots, turn++);
         if (kGroup == 32) __syncwarp();
-        if (lane == 0) fetch(row + kRing * stride, slot);      // every thread has its part of the row: the slot is free
+        if (lane == 0) fetch(row + kFwdRing * stride, slot);      // every thread has its part of the row: the slot is free
         const float mean = __fmul_rn(total, per_column);
         const uint64_t minus_mean = pack2(-mean, -mean);
         uint64_t squares = 0;
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
-            const uint32_t u = lane + i * kGroup, left = kWhole ? E : u < units ? d - u * E : 0u;
+            const uint32_t u = lane + i * group_size<kGroup>(), left = kWhole ? E : u < units ? d - u * E : 0u;
 #pragma unroll
             for (uint32_t q = 0; q < E / 2; ++q) v[i][q] = add2(v[i][q], minus_mean);
             if (left < E) {                        // what is past the end does not deviate
@@ -392,25 +395,25 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
             uint64_t w[E / 2], b[E / 2];
-            Image::pairs(weights, lane + i * kGroup, kAll, w);
-            Image::pairs(biases, lane + i * kGroup, kAll, b);
+            Image::pairs(weights, lane + i * group_size<kGroup>(), all, w);
+            Image::pairs(biases, lane + i * group_size<kGroup>(), all, b);
 #pragma unroll
             for (uint32_t q = 0; q < E / 2; ++q) v[i][q] = fma2(mul2(v[i][q], by_rstd), w[q], b[q]);
-            out.put(lane + i * kGroup, pack_unit<T>(v[i]));
+            out.put(lane + i * group_size<kGroup>(), pack_unit<T>(v[i]));
         }
         out.finish(lane);
         if (lane == 0) {
             if (mean_out) mean_out[row] = mean;
             if (rstd_out) rstd_out[row] = rstd;
         }
-        if (++slot == kRing) {
+        if (++slot == kFwdRing) {
             slot = 0;
             phase ^= 1u;
         }
     }
     // no copy may land in the shared memory of a CTA that is gone
     if (missed)
-        for (uint32_t s = 0; s < kRing; ++s)
+        for (uint32_t s = 0; s < kFwdRing; ++s)
             for (uint32_t i = 0; i < spin_limit; ++i)
                 if (mbar_try_wait(&full[group][s], phase)) break;
 }
@@ -418,17 +421,24 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
 // Backward: a group's rows come through a ring of bulk copies (x and dy of a row to a slot); the row is taken into registers, added to
 // the group's columns of the parameter gradients, summed over, and dx is written from the registers while the slot is
 // filled again.
+// (2 / 3 / 4 rows ahead: 73 / 68 / 69 us for 16384 rows of 4096 bf16)
+constexpr uint32_t kRing = 3u;
+// CTAs of the backward kernel an SM's registers are asked to hold
+template <uint32_t kThreads, uint32_t kUnits> constexpr uint32_t bwd_ctas() {
+    return kUnits == 1 ? 768 / kThreads : kThreads <= 320 ? 640 / kThreads : 1;
+}
+
 template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits, bool kWhole>
-__global__ void __launch_bounds__(kThreads, 512 / kThreads)
+__global__ void __launch_bounds__(kThreads, bwd_ctas<kThreads, kUnits>())
 norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, uint32_t d, uint32_t ld,
                       const P* __restrict__ weight, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
                       uint32_t ld_dx, float* __restrict__ parts, uint32_t slot_units, float per_column, uint32_t spin_limit) {
-    constexpr uint32_t E = Unit<T>::kElems, kGroups = kThreads / kGroup;
+    constexpr uint32_t E = Unit<T>::kElems, kGroups = kGroup ? kThreads / kGroup : 1;
     extern __shared__ __align__(128) uint4 ring[];        // per group: kRing slots of (x, dy), and the image of an unaligned dx
     __shared__ float slots[128];
     __shared__ uint64_t full[kGroups][kRing];
     __shared__ uint32_t gave_up;
-    const uint32_t lane = threadIdx.x % kGroup, group = threadIdx.x / kGroup, units = (d + E - 1) / E;
+    const uint32_t lane = kGroup ? threadIdx.x % 32 : threadIdx.x, group = kGroup ? threadIdx.x / 32 : 0, units = (d + E - 1) / E;
     uint4* const mine = ring + group * (2 * kRing + 1) * slot_units;
     uint4* const image = mine + 2 * kRing * slot_units;
     const uint64_t stride = static_cast<uint64_t>(gridDim.x) * kGroups;
@@ -455,7 +465,7 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
     uint64_t w[kUnits][E / 2], dw[kUnits][E / 2], db[kUnits][E / 2];
 #pragma unroll
     for (uint32_t i = 0; i < kUnits; ++i) {
-        param_pairs<P, E>(weight, false, vector_params(weight), (lane + i * kGroup) * E, d, 1.0f, w[i]);
+        param_pairs<P, E>(weight, false, vector_params(weight), (lane + i * group_size<kGroup>()) * E, d, 1.0f, w[i]);
 #pragma unroll
         for (uint32_t q = 0; q < E / 2; ++q) dw[i][q] = db[i][q] = 0;
     }
@@ -482,7 +492,7 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
         load_units<kGroup, kUnits, kWhole>(raw_y, lane, units, ay.off, ay.pieces, [&](uint32_t p) { return sy[p]; });
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
-            const uint32_t u = lane + i * kGroup, left = kWhole ? E : u < units ? d - u * E : 0u;
+            const uint32_t u = lane + i * group_size<kGroup>(), left = kWhole ? E : u < units ? d - u * E : 0u;
             unit_pairs<T>(raw_x[i], left, 0.0f, h[i]);
             unit_pairs<T>(raw_y[i], left, 0.0f, g[i]);
 #pragma unroll
@@ -512,7 +522,7 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
 #pragma unroll
             for (uint32_t q = 0; q < E / 2; ++q)
                 g[i][q] = mul2(by_r, fma2(h[i][q], minus_m2, add2(g[i][q], minus_m1)));
-            out.put(lane + i * kGroup, pack_unit<T>(g[i]));
+            out.put(lane + i * group_size<kGroup>(), pack_unit<T>(g[i]));
         }
         out.finish(lane);
         mu = next_mu;
@@ -539,7 +549,7 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
     }
 #pragma unroll
     for (uint32_t i = 0; i < kUnits; ++i) {
-        const uint32_t u = lane + i * kGroup;
+        const uint32_t u = lane + i * group_size<kGroup>();
         if (u >= units) break;
 #pragma unroll
         for (uint32_t q = 0; q < E / 2; q += 2) {
@@ -678,17 +688,24 @@ norm_bwd_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, uint32_t
     }
 }
 
+// warps that hold `units` with `each` to a lane
+uint32_t warps_for(uint32_t units, uint32_t each) { return (units + 32 * each - 1) / (32 * each); }
 // every row of a matrix starts on a 16-byte boundary
 bool on_boundaries(const void* p, uint32_t rows, uint32_t ld, size_t es) {
     return aligned_to(p, 16) && (rows == 1 || static_cast<size_t>(ld) * es % 16 == 0);
 }
 
-uint32_t norm_parts(uint32_t rows) { return rows < kMaxParts ? (rows ? rows : 1) : kMaxParts; }
+// CTAs that may leave partial sums (the general kernels' rows are so wide that fewer do)
+uint32_t norm_parts(uint32_t rows, uint32_t d) {
+    const uint32_t most = d <= 8192 ? kMaxParts : 148u;
+    return rows < most ? (rows ? rows : 1) : most;
+}
 
 template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits>
 dct_status_t launch_fwd_units(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* weight, const P* bias, float eps, T* y,
                               uint32_t ld_y, float* mean_out, float* rstd_out, cudaStream_t stream) {
-    constexpr uint32_t kGroups = kThreads / kGroup, E = Unit<T>::kElems;
+    constexpr uint32_t kGroups = kGroup ? kThreads / kGroup : 1, E = Unit<T>::kElems;
+    const uint32_t threads = kGroup ? kThreads : warps_for((d + E - 1) / E, kUnits) * 32;
     auto kernel = norm_fwd_units_kernel<T, P, kGroup, kThreads, kUnits>;
     // an image only if some row of y does not start on a boundary
     const size_t smem = on_boundaries(y, rows, ld_y, sizeof(T)) ? 0 : static_cast<size_t>(kGroups) * ((d + E - 1) / E) * 16;
@@ -696,7 +713,7 @@ dct_status_t launch_fwd_units(const T* x, uint32_t rows, uint32_t d, uint32_t ld
     const dct_status_t allowed_st = allow_shared(kernel, smem, allowed);
     if (allowed_st != DCT_OK) return allowed_st;
     const uint64_t ctas = (static_cast<uint64_t>(rows) + kGroups - 1) / kGroups;
-    kernel<<<static_cast<uint32_t>(ctas < (1u << 30) ? ctas : 1u << 30), kThreads, smem, stream>>>(
+    kernel<<<static_cast<uint32_t>(ctas < (1u << 30) ? ctas : 1u << 30), threads, smem, stream>>>(
         x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out);
     DCT_CUDA_TRY(cudaGetLastError());
     return DCT_OK;
@@ -705,21 +722,23 @@ dct_status_t launch_fwd_units(const T* x, uint32_t rows, uint32_t d, uint32_t ld
 template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits>
 dct_status_t launch_fwd_ring(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* weight, const P* bias, float eps, T* y,
                              uint32_t ld_y, float* mean_out, float* rstd_out, cudaStream_t stream) {
-    constexpr uint32_t kGroups = kThreads / kGroup, E = Unit<T>::kElems;
+    constexpr uint32_t kGroups = kGroup ? kThreads / kGroup : 1, E = Unit<T>::kElems;
     const int sms = sm_count();
     if (sms <= 0) return DCT_ERR_CUDA;
-    const bool whole = d == E * kGroup * kUnits && on_boundaries(x, rows, ld, sizeof(T)) && on_boundaries(y, rows, ld_y, sizeof(T));
+    const uint32_t threads = kGroup ? kThreads : warps_for((d + E - 1) / E, kUnits) * 32, all = (kGroup ? kGroup : threads) * kUnits;
+    const bool whole = d == E * all && on_boundaries(x, rows, ld, sizeof(T)) && on_boundaries(y, rows, ld_y, sizeof(T));
     auto kernel = whole ? norm_fwd_ring_kernel<T, P, kGroup, kThreads, kUnits, true> : norm_fwd_ring_kernel<T, P, kGroup, kThreads, kUnits, false>;
     const uint32_t slot_units = (d + E - 1) / E + 1;       // (an unaligned row touches one piece more)
-    const size_t smem = 16 * (2 * static_cast<size_t>(ParamImage<P, E>::kPieces) * kGroup * kUnits +
-                              static_cast<size_t>(kGroups) * (kRing + 1) * slot_units);
+    const size_t smem = 16 * (2 * static_cast<size_t>(ParamImage<P, E>::kPieces) * all +
+                              static_cast<size_t>(kGroups) * (kFwdRing + 1) * slot_units);
     static std::atomic<uint32_t> allowed[2][64];
     const dct_status_t allowed_st = allow_shared(kernel, smem, allowed[whole]);
     if (allowed_st != DCT_OK) return allowed_st;
     uint32_t per_sm = static_cast<uint32_t>(227 * 1024 / (smem + 2048));
-    per_sm = per_sm < 1 ? 1 : per_sm < fwd_ctas<kThreads, kUnits>() ? per_sm : fwd_ctas<kThreads, kUnits>();
+    const uint32_t by_registers = fwd_ctas<kThreads, kUnits>() * kThreads / threads;
+    per_sm = per_sm < 1 ? 1 : per_sm < by_registers ? per_sm : by_registers;
     const uint64_t wanted = (static_cast<uint64_t>(rows) + kGroups - 1) / kGroups, room = static_cast<uint64_t>(sms) * per_sm;
-    kernel<<<static_cast<uint32_t>(wanted < room ? wanted : room), kThreads, smem, stream>>>(
+    kernel<<<static_cast<uint32_t>(wanted < room ? wanted : room), threads, smem, stream>>>(
         x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out, slot_units, 1.0f / static_cast<float>(d), debug_config().spin_limit);
     DCT_CUDA_TRY(cudaGetLastError());
     return DCT_OK;
@@ -736,13 +755,12 @@ dct_status_t launch_norm_fwd(const void* x_, uint32_t rows, uint32_t d, uint32_t
     if (units <= 32) return go(launch_fwd_ring<T, P, 32, 256, 1>);
     if (units <= 64) return go(launch_fwd_ring<T, P, 32, 256, 2>);
     if (units <= 128) return go(launch_fwd_ring<T, P, 32, 256, 4>);
-    if (units <= 256) return go(launch_fwd_ring<T, P, 128, 128, 2>);
-    if (units <= 512) return go(launch_fwd_ring<T, P, 256, 256, 2>);
-    if (units <= 1024) return go(launch_fwd_ring<T, P, 256, 256, 4>);
+    if (units <= 512) return go(launch_fwd_ring<T, P, 0, 256, 2>);
+    if (units <= 1024) return go(launch_fwd_ring<T, P, 0, 256, 4>);
     if (units <= 2048) {
         // (the ring and both arrays of parameters fit an SM's shared memory unless fp32 parameters come with bf16 rows)
-        if constexpr (sizeof(P) <= sizeof(T)) return go(launch_fwd_ring<T, P, 512, 512, 4>);
-        else return go(launch_fwd_units<T, P, 512, 512, 4>);
+        if constexpr (sizeof(P) <= sizeof(T)) return go(launch_fwd_ring<T, P, 0, 512, 4>);
+        else return go(launch_fwd_units<T, P, 0, 512, 4>);
     }
     const uint32_t grid = rows < 4096u ? rows : 4096u;
     norm_fwd_kernel<T, P><<<grid, kNormThreads, 0, stream>>>(x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out);
@@ -759,10 +777,11 @@ template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t k
 dct_status_t launch_bwd_units(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* weight,
                               const float* mean, const float* rstd, T* dx, uint32_t ld_dx, float* dweight, float* dbias,
                               float* parts, cudaStream_t stream) {
-    constexpr uint32_t kGroups = kThreads / kGroup, E = Unit<T>::kElems;
+    constexpr uint32_t kGroups = kGroup ? kThreads / kGroup : 1, E = Unit<T>::kElems;
     const int sms = sm_count();
     if (sms <= 0) return DCT_ERR_CUDA;
-    const bool whole = d == E * kGroup * kUnits && on_boundaries(x, rows, ld, sizeof(T)) &&
+    const uint32_t threads = kGroup ? kThreads : warps_for((d + E - 1) / E, kUnits) * 32;
+    const bool whole = d == E * (kGroup ? kGroup : threads) * kUnits && on_boundaries(x, rows, ld, sizeof(T)) &&
                        on_boundaries(dy, rows, ld_dy, sizeof(T)) && on_boundaries(dx, rows, ld_dx, sizeof(T));
     auto kernel = whole ? norm_bwd_units_kernel<T, P, kGroup, kThreads, kUnits, true> : norm_bwd_units_kernel<T, P, kGroup, kThreads, kUnits, false>;
     const uint32_t slot_units = (d + E - 1) / E + 1;       // (an unaligned row touches one piece more)
@@ -771,11 +790,11 @@ dct_status_t launch_bwd_units(const T* dy, uint32_t ld_dy, const T* x, uint32_t 
     const dct_status_t allowed_st = allow_shared(kernel, smem, allowed[whole]);
     if (allowed_st != DCT_OK) return allowed_st;
     const uint64_t wanted = (static_cast<uint64_t>(rows) + kGroups - 1) / kGroups;
-    uint64_t room = static_cast<uint64_t>(sms) * (512 / kThreads);
+    uint64_t room = static_cast<uint64_t>(sms) * (bwd_ctas<kThreads, kUnits>() * kThreads / threads);
     if (room > kMaxParts) room = kMaxParts;
     const uint32_t grid = static_cast<uint32_t>(wanted < room ? wanted : room);
     const bool params = dweight || dbias;
-    kernel<<<grid, kThreads, smem, stream>>>(dy, ld_dy, x, rows, d, ld, weight, mean, rstd, dx, ld_dx,
+    kernel<<<grid, threads, smem, stream>>>(dy, ld_dy, x, rows, d, ld, weight, mean, rstd, dx, ld_dx,
                                              params ? parts : nullptr, slot_units, 1.0f / static_cast<float>(d), debug_config().spin_limit);
     DCT_CUDA_TRY(cudaGetLastError());
     return params ? launch_param_join(parts, grid, d, (d + E - 1) / E * E, dweight, dbias, stream) : DCT_OK;
@@ -794,15 +813,16 @@ dct_status_t launch_norm_bwd(const void* dy_, uint32_t ld_dy, const void* x_, ui
     if (units <= 64) return go(launch_bwd_units<T, P, 32, 256, 2>);
     if (units <= 128) {
         if constexpr (sizeof(T) == 4) return go(launch_bwd_units<T, P, 32, 256, 4>);
-        else return go(launch_bwd_units<T, P, 128, 128, 1>);
+        else return go(launch_bwd_units<T, P, 0, 128, 1>);
     }
-    if (units <= 256) return go(launch_bwd_units<T, P, 256, 256, 1>);
-    if (units <= 512) return go(launch_bwd_units<T, P, 256, 256, 2>);
-    if (units <= 1024) return go(launch_bwd_units<T, P, 512, 512, 2>);
+    if (units <= 256) return go(launch_bwd_units<T, P, 0, 256, 1>);
+    if (units <= 512) return go(launch_bwd_units<T, P, 0, 256, 2>);
+    if (units <= 640) return go(launch_bwd_units<T, P, 0, 320, 2>);
+    if (units <= 1024) return go(launch_bwd_units<T, P, 0, 512, 2>);
     if constexpr (sizeof(T) == 4)
-        if (units <= 2048) return go(launch_bwd_units<T, P, 512, 512, 4>);
+        if (units <= 2048) return go(launch_bwd_units<T, P, 0, 512, 4>);
     if (dweight || dbias) {        // before dx, which may take the place of dy or x
-        const uint32_t cols = (d + kNormThreads - 1) / kNormThreads, num = norm_parts(rows);
+        const uint32_t cols = (d + kNormThreads - 1) / kNormThreads, num = norm_parts(rows, d);
         norm_param_parts_kernel<T><<<dim3(cols, num), kNormThreads, 0, stream>>>(dy, ld_dy, x, rows, d, ld, mean, rstd, parts);
         DCT_CUDA_TRY(cudaGetLastError());
         const dct_status_t st = launch_param_join(parts, num, d, d, dweight, dbias, stream);
@@ -845,7 +865,7 @@ extern "C" dct_status_t dct_layer_norm_fwd(const void* x, dct_dtype_t dtype, uin
 
 extern "C" size_t dct_layer_norm_bwd_workspace_bytes(uint32_t rows, uint32_t d) {
     if (d == 0 || d > kNormMaxWidth) return 0;
-    return (static_cast<size_t>(norm_parts(rows)) * 2 * ((d + 7) / 8 * 8) * sizeof(float) + 255) & ~static_cast<size_t>(255);
+    return (static_cast<size_t>(norm_parts(rows, d)) * 2 * ((d + 7) / 8 * 8) * sizeof(float) + 255) & ~static_cast<size_t>(255);
 }
 
 extern "C" dct_status_t dct_layer_norm_bwd(const void* dy, uint32_t ld_dy, const void* x, dct_dtype_t dtype,
