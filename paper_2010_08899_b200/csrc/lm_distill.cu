@@ -31,15 +31,17 @@ __device__ __forceinline__ void add_value(RowPart& p, float v) {
 // A row belongs to a cluster of CTAs, a slice of it to each, and a slice's chunks of 128 units (2 KiB) in turn to the CTA's
 // warps.  The logits are needed twice, for the sums and, when those are joined, for the gradient.  kStaged: a warp fetches
 // its chunks by bulk copies into shared memory, works on them twice and, as it lets go of each, asks for the next row's, so
-// that they cross the memory bus once and are under way while other work is done; otherwise (slices beyond shared memory)
-// they are loaded twice.  The teacher's slots of the next row, and the logits that this row's slots name, are fetched while the
+// that they cross the memory bus once and are under way while other work is done; otherwise (slices that would leave an SM one CTA)
+// they are loaded twice, the second time from L2.  The teacher's slots of the next row, and the logits that this row's slots name, are fetched while the
 // row streams by.  `marks` has a bit for every element of the slice's units that a slot names.  kTail: those are left out of
 // the sums, so that the remainder is summed and not a difference.  The gradient is first written as if no column were named,
 // and the named ones once more afterwards.
 // Slot i belongs to thread i mod kThreads throughout.
 constexpr uint32_t kChunkUnits = 128u, kChunkBytes = 16u * kChunkUnits;
 constexpr uint32_t kMaxChunksPerWarp = 16u;
-constexpr uint32_t kStagedLimit = 200u * 1024u;            // shared memory of an SM that slices may fill
+// shared memory of a CTA that a staged slice may take: three CTAs to an SM.  (With one, loading twice is faster: 256 rows of 262144
+// fp32, 8 CTAs to a row, 195 us staged and 152 loaded twice; rows of 32768 bf16 154 us loaded twice and 117 staged.)
+constexpr uint32_t kStagedLimit = 90u * 1024u;
 
 template <typename T, uint32_t kThreads, bool kTail, bool kCluster, bool kStaged>
 __global__ void __launch_bounds__(kThreads, 768 / kThreads)
