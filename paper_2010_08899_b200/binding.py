@@ -163,13 +163,13 @@ def _p(t: Optional[torch.Tensor]):
 
 
 # the current stream's handle without the Stream object around it (3 us of every call)
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        if _raw_stream is not None and torch.cuda.is_initialized():
-            return _raw_stream(torch.cuda.current_device())
+        if _raw_stream is not None and _device is not None:
+            return _raw_stream(_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -185,11 +185,13 @@ def _need(t: torch.Tensor, dtype, name: str, cuda: bool = True):
         raise ValueError(f"{name}: must be a host tensor")
 
 
+_DTYPE_CODES = {torch.float32: DCT_F32, torch.bfloat16: DCT_BF16}
+
+
 def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
-        return DCT_F32
-    if t.dtype == torch.bfloat16:
-        return DCT_BF16
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is not None:
+        return code
     raise TypeError(f"unsupported dtype {t.dtype}: float32 or bfloat16")
 
 
