@@ -139,20 +139,38 @@ template <uint32_t kGroup> __device__ __forceinline__ void group_sum(float& a, f
     for (uint32_t o = 8; o > 0; o >>= 1) a = __fadd_rn(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
 }
 
-// A row of d results of a group.  A row on a 16-byte boundary is written unit by unit; another one by way of shared memory
-// (`image`: a unit for every unit of the row), from which the aligned pieces of the row are put together.
+// A row of d results of a group.  A row on a 16-byte boundary is written unit by unit; another one is laid out in shared memory as it
+// lies against the boundaries (`image`) and its whole aligned pieces are stored by one bulk copy.  Two images take turns: a copy
+// has read one by the time the row after the next writes it.
 template <typename T, uint32_t kGroup, bool kWhole> struct RowWriter {
     static constexpr uint32_t E = Unit<T>::kElems;
     T* row;
     uint32_t d, off;
-    uint4* image;
-    __device__ __forceinline__ RowWriter(T* row_, uint32_t d_, uint4* image_)
-        : row(row_), d(d_), off(kWhole ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row_) & 15u)), image(image_) {
-        if (off) group_sync<kGroup>();             // the last row's image is read
-    }
+    uint32_t* image;
+    __device__ __forceinline__ RowWriter(T* row_, uint32_t d_, uint4* images, uint32_t image_units, uint32_t turn)
+        : row(row_), d(d_), off(kWhole ? 0u : static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row_) & 15u)),
+          image(reinterpret_cast<uint32_t*>(images + (turn & 1u) * image_units)) {}
+    // by all lanes of a warp, for neighbouring units
     __device__ __forceinline__ void put(uint32_t u, const uint4& v) {
         if (off) {
-            if (u * E < d) image[u] = v;
+            uint32_t* to = image + off / 4 + 4 * u;
+            const bool mine = u * E < d;
+            if (off & 2u) {          // bf16 half a word off: a word holds the end of one pair and the start of the next
+                const uint32_t before = __shfl_up_sync(0xFFFFFFFFu, v.w, 1);
+                if (mine) {
+                    if (lane_id() == 0) reinterpret_cast<uint16_t*>(to)[1] = static_cast<uint16_t>(v.x);
+                    else to[0] = __funnelshift_r(before, v.x, 16);
+                    to[1] = __funnelshift_r(v.x, v.y, 16);
+                    to[2] = __funnelshift_r(v.y, v.z, 16);
+                    to[3] = __funnelshift_r(v.z, v.w, 16);
+                    if (lane_id() == 31 || (u + 1) * E >= d) reinterpret_cast<uint16_t*>(to + 4)[0] = static_cast<uint16_t>(v.w >> 16);
+                }
+            } else if (mine) {
+                to[0] = v.x;
+                to[1] = v.y;
+                to[2] = v.z;
+                to[3] = v.w;
+            }
         } else if (kWhole || u * E + E <= d) {
             st_unit(row + u * E, v);
         } else {
@@ -162,24 +180,33 @@ template <typename T, uint32_t kGroup, bool kWhole> struct RowWriter {
         }
     }
     __device__ __forceinline__ void finish(uint32_t lane) {
-        if (!off) return;
-        group_sync<kGroup>();
-        // piece j holds the row's bytes from 16 j - off on
-        const uint32_t bytes = d * static_cast<uint32_t>(sizeof(T)), pieces = (off + bytes + 15) / 16, units = (d + E - 1) / E;
-        uint8_t* base = reinterpret_cast<uint8_t*>(row) - off;
-        for (uint32_t j = lane; j < pieces; j += group_size<kGroup>()) {
-            const uint4 zero = make_uint4(0, 0, 0, 0);
-            const uint4 v = shifted(j > 0 ? image[j - 1] : zero, j < units ? image[j] : zero, 16 - off);
-            if (j > 0 && 16 * j + 16 <= off + bytes) {
-                st_unit(base + 16 * j, v);
-            } else {
-#pragma unroll
-                for (uint32_t e = 0; e < E; ++e) {
-                    const uint32_t at = 16 * j + e * static_cast<uint32_t>(sizeof(T));       // from base
-                    if (at >= off && at < off + bytes) *reinterpret_cast<T*>(base + at) = from_f32<T>(Unit<T>::get(v, e));
-                }
+        if (kWhole) return;
+        if (!off) {                  // nothing to copy, but its turn passes
+            if (lane == 0) {
+                bulk_commit();
+                bulk_wait_read<1>();
             }
+            return;
         }
+        fence_proxy_async_smem();
+        group_sync<kGroup>();
+        const uint32_t end = off + d * static_cast<uint32_t>(sizeof(T)), whole_end = end / 16;      // pieces [1, whole_end) are whole
+        uint8_t* base = reinterpret_cast<uint8_t*>(row) - off;
+        if (lane == 0) {
+            if (whole_end > 1) bulk_store(base + 16, image + 4, 16 * (whole_end - 1));
+            bulk_commit();
+            bulk_wait_read<1>();
+        }
+        // the first piece's elements, and those past the last whole one
+        const T* elements = reinterpret_cast<const T*>(image);
+        if (lane < 2 * E) {
+            const uint32_t e = lane < E ? lane : max(whole_end, 1u) * E + lane - E, at = e * static_cast<uint32_t>(sizeof(T));
+            if (at >= off && at < end) *reinterpret_cast<T*>(base + at) = elements[e];
+        }
+    }
+    // before the shared memory is given up
+    __device__ static __forceinline__ void drain(uint32_t lane) {
+        if (!kWhole && lane == 0) bulk_wait_read<0>();
     }
 };
 template <typename T> __device__ __forceinline__ uint4 pack_unit(const uint64_t (&x)[Unit<T>::kElems / 2]) {
@@ -199,7 +226,7 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
     extern __shared__ __align__(16) uint4 images[];
     __shared__ float slots[128];
     const uint32_t lane = kGroup ? threadIdx.x % 32 : threadIdx.x, group = kGroup ? threadIdx.x / 32 : 0, units = (d + E - 1) / E;
-    uint4* image = images + group * units;
+    uint4* image = images + group * 2 * (units + 2);
     const bool vec_w = vector_params(weight), vec_b = vector_params(bias), whole = d % E == 0;
     uint32_t turn = 0;
     for (uint64_t row = static_cast<uint64_t>(blockIdx.x) * kGroups + group; row < rows;
@@ -244,7 +271,7 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
         group_sum<kGroup>(deviation, slots, turn++);
         const float rstd = 1.0f / sqrtf(deviation / static_cast<float>(d) + eps);
         const uint64_t by_rstd = pack2(rstd, rstd);
-        RowWriter<T, kGroup, false> out(y + row * ld_y, d, image);
+        RowWriter<T, kGroup, false> out(y + row * ld_y, d, image, units + 2, turn / 2);
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
             const uint32_t col = (lane + i * group_size<kGroup>()) * E;
@@ -261,6 +288,7 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
             if (rstd_out) rstd_out[row] = rstd;
         }
     }
+    RowWriter<T, kGroup, false>::drain(lane);
 }
 
 // Forward by the same rules for as many rows as a grid that stays has groups for: the rows come through a ring of bulk copies,
@@ -307,14 +335,14 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
                      float* __restrict__ rstd_out, uint32_t slot_units, float per_column, uint32_t spin_limit) {
     constexpr uint32_t E = Unit<T>::kElems, kGroups = kGroup ? kThreads / kGroup : 1;
     using Image = ParamImage<P, E>;
-    extern __shared__ __align__(128) uint4 shared[];       // parameters; per group kFwdRing slots and the image of an unaligned y
+    extern __shared__ __align__(128) uint4 shared[];       // parameters; per group its slots and two images of an unaligned y
     __shared__ float slots[128];
     __shared__ uint64_t full[kGroups][kFwdRing];
     __shared__ uint32_t gave_up;
     const uint32_t all = group_size<kGroup>() * kUnits;    // units the group's lanes hold
     const uint32_t lane = kGroup ? threadIdx.x % 32 : threadIdx.x, group = kGroup ? threadIdx.x / 32 : 0, units = (d + E - 1) / E;
     uint4 *const weights = shared, *const biases = shared + Image::kPieces * all;
-    uint4* const mine = shared + 2 * Image::kPieces * all + group * (kFwdRing + 1) * slot_units;
+    uint4* const mine = shared + 2 * Image::kPieces * all + group * (kFwdRing + (kWhole ? 0 : 2)) * slot_units;
     uint4* const image = mine + kFwdRing * slot_units;
     const uint64_t stride = static_cast<uint64_t>(gridDim.x) * kGroups;
     const uint64_t first = static_cast<uint64_t>(blockIdx.x) * kGroups + group;
@@ -391,7 +419,7 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
         float rstd = rsqrtf(fmaf(deviation, per_column, eps));
         if (missed) rstd = __uint_as_float(0x7FFFFFFFu);       // what the group writes from here on is NaN
         const uint64_t by_rstd = pack2(rstd, rstd);
-        RowWriter<T, kGroup, kWhole> out(y_row, d, image);
+        RowWriter<T, kGroup, kWhole> out(y_row, d, image, slot_units, turn / 2);
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
             uint64_t w[E / 2], b[E / 2];
@@ -411,6 +439,7 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
             phase ^= 1u;
         }
     }
+    RowWriter<T, kGroup, kWhole>::drain(lane);
     // no copy may land in the shared memory of a CTA that is gone
     if (missed)
         for (uint32_t s = 0; s < kFwdRing; ++s)
@@ -434,12 +463,12 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
                       const P* __restrict__ weight, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
                       uint32_t ld_dx, float* __restrict__ parts, uint32_t slot_units, float per_column, uint32_t spin_limit) {
     constexpr uint32_t E = Unit<T>::kElems, kGroups = kGroup ? kThreads / kGroup : 1;
-    extern __shared__ __align__(128) uint4 ring[];        // per group: kRing slots of (x, dy), and the image of an unaligned dx
+    extern __shared__ __align__(128) uint4 ring[];        // per group: kRing slots of (x, dy), and two images of an unaligned dx
     __shared__ float slots[128];
     __shared__ uint64_t full[kGroups][kRing];
     __shared__ uint32_t gave_up;
     const uint32_t lane = kGroup ? threadIdx.x % 32 : threadIdx.x, group = kGroup ? threadIdx.x / 32 : 0, units = (d + E - 1) / E;
-    uint4* const mine = ring + group * (2 * kRing + 1) * slot_units;
+    uint4* const mine = ring + group * (2 * kRing + (kWhole ? 0 : 2)) * slot_units;
     uint4* const image = mine + 2 * kRing * slot_units;
     const uint64_t stride = static_cast<uint64_t>(gridDim.x) * kGroups;
     const uint64_t first = static_cast<uint64_t>(blockIdx.x) * kGroups + group;
@@ -516,7 +545,7 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
         if (lane == 0) fetch(row + kRing * stride, slot);
         const float m1 = __fmul_rn(a, per_column), m2 = __fmul_rn(b, per_column);
         const uint64_t minus_m1 = pack2(-m1, -m1), minus_m2 = pack2(-m2, -m2);
-        RowWriter<T, kGroup, kWhole> out(dx_row, d, image);
+        RowWriter<T, kGroup, kWhole> out(dx_row, d, image, slot_units, turn);
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
 #pragma unroll
@@ -532,6 +561,7 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
             phase ^= 1u;
         }
     }
+    RowWriter<T, kGroup, kWhole>::drain(lane);
     // no copy may land in the shared memory of a CTA that is gone, nor in what is used below
     if (missed)
         for (uint32_t s = 0; s < kRing; ++s)
@@ -708,7 +738,7 @@ dct_status_t launch_fwd_units(const T* x, uint32_t rows, uint32_t d, uint32_t ld
     const uint32_t threads = kGroup ? kThreads : warps_for((d + E - 1) / E, kUnits) * 32;
     auto kernel = norm_fwd_units_kernel<T, P, kGroup, kThreads, kUnits>;
     // an image only if some row of y does not start on a boundary
-    const size_t smem = on_boundaries(y, rows, ld_y, sizeof(T)) ? 0 : static_cast<size_t>(kGroups) * ((d + E - 1) / E) * 16;
+    const size_t smem = on_boundaries(y, rows, ld_y, sizeof(T)) ? 0 : static_cast<size_t>(kGroups) * 2 * ((d + E - 1) / E + 2) * 16;
     static std::atomic<uint32_t> allowed[64];
     const dct_status_t allowed_st = allow_shared(kernel, smem, allowed);
     if (allowed_st != DCT_OK) return allowed_st;
@@ -728,9 +758,9 @@ dct_status_t launch_fwd_ring(const T* x, uint32_t rows, uint32_t d, uint32_t ld,
     const uint32_t threads = kGroup ? kThreads : warps_for((d + E - 1) / E, kUnits) * 32, all = (kGroup ? kGroup : threads) * kUnits;
     const bool whole = d == E * all && on_boundaries(x, rows, ld, sizeof(T)) && on_boundaries(y, rows, ld_y, sizeof(T));
     auto kernel = whole ? norm_fwd_ring_kernel<T, P, kGroup, kThreads, kUnits, true> : norm_fwd_ring_kernel<T, P, kGroup, kThreads, kUnits, false>;
-    const uint32_t slot_units = (d + E - 1) / E + 1;       // (an unaligned row touches one piece more)
+    const uint32_t slot_units = (d + E - 1) / E + 2;       // (an unaligned row touches one piece more; its image half a word beyond)
     const size_t smem = 16 * (2 * static_cast<size_t>(ParamImage<P, E>::kPieces) * all +
-                              static_cast<size_t>(kGroups) * (kFwdRing + 1) * slot_units);
+                              static_cast<size_t>(kGroups) * (kFwdRing + (whole ? 0 : 2)) * slot_units);
     static std::atomic<uint32_t> allowed[2][64];
     const dct_status_t allowed_st = allow_shared(kernel, smem, allowed[whole]);
     if (allowed_st != DCT_OK) return allowed_st;
@@ -784,8 +814,8 @@ dct_status_t launch_bwd_units(const T* dy, uint32_t ld_dy, const T* x, uint32_t 
     const bool whole = d == E * (kGroup ? kGroup : threads) * kUnits && on_boundaries(x, rows, ld, sizeof(T)) &&
                        on_boundaries(dy, rows, ld_dy, sizeof(T)) && on_boundaries(dx, rows, ld_dx, sizeof(T));
     auto kernel = whole ? norm_bwd_units_kernel<T, P, kGroup, kThreads, kUnits, true> : norm_bwd_units_kernel<T, P, kGroup, kThreads, kUnits, false>;
-    const uint32_t slot_units = (d + E - 1) / E + 1;       // (an unaligned row touches one piece more)
-    const size_t smem = static_cast<size_t>(kGroups) * (2 * kRing + 1) * slot_units * 16;
+    const uint32_t slot_units = (d + E - 1) / E + 2;       // (an unaligned row touches one piece more; its image half a word beyond)
+    const size_t smem = static_cast<size_t>(kGroups) * (2 * kRing + (whole ? 0 : 2)) * slot_units * 16;
     static std::atomic<uint32_t> allowed[2][64];
     const dct_status_t allowed_st = allow_shared(kernel, smem, allowed[whole]);
     if (allowed_st != DCT_OK) return allowed_st;
