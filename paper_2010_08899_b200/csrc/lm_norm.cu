@@ -291,6 +291,187 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
     RowWriter<T, kGroup, false>::drain(lane);
 }
 
+// Narrow rows: a unit to a lane and 32 / kLanes rows to a warp, four such sets of rows at a time.  With a warp to a row the work
+// that every row costs (its sums, its addresses) would be most of all there is: 65536 rows of 128 bf16 25 us that way.
+constexpr uint32_t kSets = 4u;
+
+template <uint32_t kLanes> __device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+    for (uint32_t o = kLanes / 2; o > 0; o >>= 1) v = __fadd_rn(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    return v;
+}
+// unit u of a row that starts `off` bytes into the piece at base
+__device__ __forceinline__ uint4 load_narrow(const uint4* base, uint32_t off, uint32_t pieces, uint32_t u) {
+    uint4 v = ld_unit(base + min(u, pieces - 1));
+    if (off) v = shifted(v, ld_unit(base + min(u + 1, pieces - 1)), off);
+    return v;
+}
+// `left` elements of the row from the unit's first on
+template <typename T> __device__ __forceinline__ void store_narrow(T* to, const uint4& v, uint32_t left) {
+    constexpr uint32_t E = Unit<T>::kElems;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(to);
+    if (left >= E && (at & 15u) == 0) {
+        st_unit(to, v);
+    } else if (left >= E && (at & 3u) == 0) {
+        uint32_t* words = reinterpret_cast<uint32_t*>(to);
+        words[0] = v.x;
+        words[1] = v.y;
+        words[2] = v.z;
+        words[3] = v.w;
+    } else {
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e)
+            if (e < left) to[e] = from_f32<T>(Unit<T>::get(v, e));         // (exact: it is a T already)
+    }
+}
+
+template <typename T, typename P, uint32_t kLanes>
+__global__ void __launch_bounds__(256)
+norm_fwd_narrow_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* __restrict__ weight,
+                       const P* __restrict__ bias, float eps, T* y, uint32_t ld_y, float* __restrict__ mean_out,
+                       float* __restrict__ rstd_out, float per_column) {
+    constexpr uint32_t E = Unit<T>::kElems, kRows = 32 / kLanes;
+    const uint32_t sub = lane_id() % kLanes, col = sub * E, left = col < d ? d - col : 0u;
+    uint64_t w[E / 2], b[E / 2];
+    param_pairs<P, E>(weight, false, vector_params(weight), col, d, 1.0f, w);
+    param_pairs<P, E>(bias, false, vector_params(bias), col, d, 0.0f, b);
+    const uint64_t warps = static_cast<uint64_t>(gridDim.x) * 8, warp = static_cast<uint64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    for (uint64_t first = warp * kRows * kSets; first < rows; first += warps * kRows * kSets) {
+        uint4 raw[kSets];
+#pragma unroll
+        for (uint32_t s = 0; s < kSets; ++s) {
+            const uint64_t row = min(first + s * kRows + lane_id() / kLanes, static_cast<uint64_t>(rows) - 1);
+            const NormRow<T> in(x + row * ld, d);
+            raw[s] = load_narrow(in.base, in.off, in.pieces, sub);
+        }
+#pragma unroll
+        for (uint32_t s = 0; s < kSets; ++s) {
+            const uint64_t row = first + s * kRows + lane_id() / kLanes;
+            uint64_t v[E / 2], sum = 0, squares = 0;
+            unit_pairs<T>(raw[s], left, 0.0f, v);
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) sum = add2(sum, v[q]);
+            float p0, p1;
+            unpack2(sum, p0, p1);
+            const float mean = __fmul_rn(lanes_sum<kLanes>(__fadd_rn(p0, p1)), per_column);
+            const uint64_t minus_mean = pack2(-mean, -mean);
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) {
+                v[q] = add2(v[q], minus_mean);
+                if (left < E) {                    // what is past the end does not deviate
+                    unpack2(v[q], p0, p1);
+                    v[q] = pack2(2 * q < left ? p0 : 0.0f, 2 * q + 1 < left ? p1 : 0.0f);
+                }
+                squares = fma2(v[q], v[q], squares);
+            }
+            unpack2(squares, p0, p1);
+            const float rstd = rsqrtf(fmaf(lanes_sum<kLanes>(__fadd_rn(p0, p1)), per_column, eps));
+            const uint64_t by_rstd = pack2(rstd, rstd);
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) v[q] = fma2(mul2(v[q], by_rstd), w[q], b[q]);
+            if (row < rows) {
+                if (left) store_narrow(y + row * ld_y + col, pack_unit<T>(v), left);
+                if (sub == 0) {
+                    if (mean_out) mean_out[row] = mean;
+                    if (rstd_out) rstd_out[row] = rstd;
+                }
+            }
+        }
+    }
+}
+
+template <typename T, typename P, uint32_t kLanes>
+__global__ void __launch_bounds__(256)
+norm_bwd_narrow_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, uint32_t d, uint32_t ld,
+                       const P* __restrict__ weight, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
+                       uint32_t ld_dx, float* __restrict__ parts, float per_column) {
+    constexpr uint32_t E = Unit<T>::kElems, kRows = 32 / kLanes;
+    __shared__ float4 sums[8][2][kLanes * E / 4];
+    chain_release_next();                  // the CTAs that join the partial sums may come and wait
+    const uint32_t sub = lane_id() % kLanes, col = sub * E, left = col < d ? d - col : 0u;
+    uint64_t w[E / 2], dw[E / 2], db[E / 2];
+    param_pairs<P, E>(weight, false, vector_params(weight), col, d, 1.0f, w);
+#pragma unroll
+    for (uint32_t q = 0; q < E / 2; ++q) dw[q] = db[q] = 0;
+    const uint64_t warps = static_cast<uint64_t>(gridDim.x) * 8, warp = static_cast<uint64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    for (uint64_t first = warp * kRows * kSets; first < rows; first += warps * kRows * kSets) {
+        uint4 raw_x[kSets], raw_y[kSets];
+        float mu[kSets], r[kSets];
+#pragma unroll
+        for (uint32_t s = 0; s < kSets; ++s) {
+            const uint64_t row = min(first + s * kRows + lane_id() / kLanes, static_cast<uint64_t>(rows) - 1);
+            const NormRow<T> in_x(x + row * ld, d), in_y(dy + row * ld_dy, d);
+            raw_x[s] = load_narrow(in_x.base, in_x.off, in_x.pieces, sub);
+            raw_y[s] = load_narrow(in_y.base, in_y.off, in_y.pieces, sub);
+            mu[s] = mean[row];
+            r[s] = rstd[row];
+        }
+#pragma unroll
+        for (uint32_t s = 0; s < kSets; ++s) {
+            const uint64_t row = first + s * kRows + lane_id() / kLanes;
+            const bool inside = row < rows;
+            const uint64_t minus_mu = pack2(-mu[s], -mu[s]), by_r = pack2(r[s], r[s]);
+            uint64_t h[E / 2], g[E / 2], sum_g = 0, sum_gh = 0;
+            unit_pairs<T>(raw_x[s], left, 0.0f, h);
+            unit_pairs<T>(raw_y[s], inside ? left : 0u, 0.0f, g);           // (a row again at the end adds nothing)
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) {
+                h[q] = mul2(add2(h[q], minus_mu), by_r);
+                if (inside) dw[q] = fma2(g[q], h[q], dw[q]);
+                db[q] = add2(db[q], g[q]);
+                g[q] = mul2(g[q], w[q]);
+                sum_g = add2(sum_g, g[q]);
+                sum_gh = fma2(g[q], h[q], sum_gh);
+            }
+            float p0, p1;
+            unpack2(sum_g, p0, p1);
+            const float m1 = __fmul_rn(lanes_sum<kLanes>(__fadd_rn(p0, p1)), per_column);
+            unpack2(sum_gh, p0, p1);
+            const float m2 = __fmul_rn(lanes_sum<kLanes>(__fadd_rn(p0, p1)), per_column);
+            const uint64_t minus_m1 = pack2(-m1, -m1), minus_m2 = pack2(-m2, -m2);
+#pragma unroll
+            for (uint32_t q = 0; q < E / 2; ++q) g[q] = mul2(by_r, fma2(h[q], minus_m2, add2(g[q], minus_m1)));
+            if (inside && left) store_narrow(dx + row * ld_dx + col, pack_unit<T>(g), left);
+        }
+    }
+    if (!parts) return;
+    // the warp's sums over its rows' places, then the CTA's over its warps
+    float v[2][E];
+#pragma unroll
+    for (uint32_t q = 0; q < E / 2; ++q) {
+        unpack2(dw[q], v[0][2 * q], v[0][2 * q + 1]);
+        unpack2(db[q], v[1][2 * q], v[1][2 * q + 1]);
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) {
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e)
+#pragma unroll
+            for (uint32_t o = 16; o >= kLanes; o >>= 1) v[k][e] = __fadd_rn(v[k][e], __shfl_xor_sync(0xFFFFFFFFu, v[k][e], o));
+        if (lane_id() < kLanes) {
+#pragma unroll
+            for (uint32_t e = 0; e < E; e += 4)
+                sums[threadIdx.x >> 5][k][(col + e) / 4] = make_float4(v[k][e], v[k][e + 1], v[k][e + 2], v[k][e + 3]);
+        }
+    }
+    __syncthreads();
+    const uint32_t width = (d + E - 1) / E * E;
+    float4* cta = reinterpret_cast<float4*>(parts + static_cast<size_t>(blockIdx.x) * 2 * width);
+    for (uint32_t i = threadIdx.x; i < 2 * width / 4; i += 256) {
+        const uint32_t k = i / (width / 4), c = i % (width / 4);
+        float4 t = sums[0][k][c];
+#pragma unroll
+        for (uint32_t n = 1; n < 8; ++n) {
+            const float4 o = sums[n][k][c];
+            t.x = __fadd_rn(t.x, o.x);
+            t.y = __fadd_rn(t.y, o.y);
+            t.z = __fadd_rn(t.z, o.z);
+            t.w = __fadd_rn(t.w, o.w);
+        }
+        cta[i] = t;
+    }
+}
+
 // Forward by the same rules for as many rows as a grid that stays has groups for: the rows come through a ring of bulk copies,
 // kFwdRing ahead of the one being worked on, and the parameters lie in shared memory, so that a row's only waits are its two sums.
 // (more rows on their way make the reads outrun the writes, and both slower: 16384 rows of 4096 fp32 with 2 / 3 / 4: 88 / 96 / 107 us)
@@ -774,6 +955,19 @@ dct_status_t launch_fwd_ring(const T* x, uint32_t rows, uint32_t d, uint32_t ld,
     return DCT_OK;
 }
 
+template <typename T, typename P, uint32_t kLanes>
+dct_status_t launch_fwd_narrow(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* weight, const P* bias, float eps, T* y,
+                               uint32_t ld_y, float* mean_out, float* rstd_out, cudaStream_t stream) {
+    const int sms = sm_count();
+    if (sms <= 0) return DCT_ERR_CUDA;
+    constexpr uint32_t per_cta = 8 * (32 / kLanes) * kSets;
+    const uint64_t wanted = (static_cast<uint64_t>(rows) + per_cta - 1) / per_cta, room = static_cast<uint64_t>(sms) * 16;
+    norm_fwd_narrow_kernel<T, P, kLanes><<<static_cast<uint32_t>(wanted < room ? wanted : room), 256, 0, stream>>>(
+        x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out, 1.0f / static_cast<float>(d));
+    DCT_CUDA_TRY(cudaGetLastError());
+    return DCT_OK;
+}
+
 template <typename T, typename P>
 dct_status_t launch_norm_fwd(const void* x_, uint32_t rows, uint32_t d, uint32_t ld, const void* weight_, const void* bias_,
                              float eps, void* y_, uint32_t ld_y, float* mean_out, float* rstd_out, cudaStream_t stream) {
@@ -782,7 +976,13 @@ dct_status_t launch_norm_fwd(const void* x_, uint32_t rows, uint32_t d, uint32_t
     const P *weight = static_cast<const P*>(weight_), *bias = static_cast<const P*>(bias_);
     const uint32_t units = (d + Unit<T>::kElems - 1) / Unit<T>::kElems;
     auto go = [&](auto launch) { return launch(x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out, stream); };
-    if (units <= 32) return go(launch_fwd_ring<T, P, 32, 256, 1>);
+    if (units <= 8) return go(launch_fwd_narrow<T, P, 8>);
+    if (units <= 16) return go(launch_fwd_narrow<T, P, 16>);
+    if (units <= 32) {
+        // (rows of exactly 32 units on boundaries: 17 us by the ring, 20 by this, for 65536 rows of 256 bf16; of 200: 27 and 22)
+        const bool whole = d == 32 * Unit<T>::kElems && on_boundaries(x, rows, ld, sizeof(T)) && on_boundaries(y, rows, ld_y, sizeof(T));
+        return whole ? go(launch_fwd_ring<T, P, 32, 256, 1>) : go(launch_fwd_narrow<T, P, 32>);
+    }
     if (units <= 64) return go(launch_fwd_ring<T, P, 32, 256, 2>);
     if (units <= 128) return go(launch_fwd_ring<T, P, 32, 256, 4>);
     if (units <= 512) return go(launch_fwd_ring<T, P, 0, 256, 2>);
@@ -830,6 +1030,24 @@ dct_status_t launch_bwd_units(const T* dy, uint32_t ld_dy, const T* x, uint32_t 
     return params ? launch_param_join(parts, grid, d, (d + E - 1) / E * E, dweight, dbias, stream) : DCT_OK;
 }
 
+template <typename T, typename P, uint32_t kLanes>
+dct_status_t launch_bwd_narrow(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* weight,
+                               const float* mean, const float* rstd, T* dx, uint32_t ld_dx, float* dweight, float* dbias,
+                               float* parts, cudaStream_t stream) {
+    const int sms = sm_count();
+    if (sms <= 0) return DCT_ERR_CUDA;
+    constexpr uint32_t per_cta = 8 * (32 / kLanes) * kSets, E = Unit<T>::kElems;
+    const uint64_t wanted = (static_cast<uint64_t>(rows) + per_cta - 1) / per_cta;
+    uint64_t room = static_cast<uint64_t>(sms) * 3;
+    if (room > norm_parts(rows, d)) room = norm_parts(rows, d);
+    const uint32_t grid = static_cast<uint32_t>(wanted < room ? wanted : room);
+    const bool params = dweight || dbias;
+    norm_bwd_narrow_kernel<T, P, kLanes><<<grid, 256, 0, stream>>>(dy, ld_dy, x, rows, d, ld, weight, mean, rstd, dx, ld_dx,
+                                                                   params ? parts : nullptr, 1.0f / static_cast<float>(d));
+    DCT_CUDA_TRY(cudaGetLastError());
+    return params ? launch_param_join(parts, grid, d, (d + E - 1) / E * E, dweight, dbias, stream) : DCT_OK;
+}
+
 template <typename T, typename P>
 dct_status_t launch_norm_bwd(const void* dy_, uint32_t ld_dy, const void* x_, uint32_t rows, uint32_t d, uint32_t ld,
                              const void* weight_, const float* mean, const float* rstd, void* dx_, uint32_t ld_dx,
@@ -839,7 +1057,13 @@ dct_status_t launch_norm_bwd(const void* dy_, uint32_t ld_dy, const void* x_, ui
     const P* weight = static_cast<const P*>(weight_);
     const uint32_t units = (d + Unit<T>::kElems - 1) / Unit<T>::kElems;
     auto go = [&](auto launch) { return launch(dy, ld_dy, x, rows, d, ld, weight, mean, rstd, dx, ld_dx, dweight, dbias, parts, stream); };
-    if (units <= 32) return go(launch_bwd_units<T, P, 32, 256, 1>);
+    if (units <= 8) return go(launch_bwd_narrow<T, P, 8>);
+    if (units <= 16) return go(launch_bwd_narrow<T, P, 16>);
+    if (units <= 32) {
+        const bool whole = d == 32 * Unit<T>::kElems && on_boundaries(x, rows, ld, sizeof(T)) &&
+                           on_boundaries(dy, rows, ld_dy, sizeof(T)) && on_boundaries(dx, rows, ld_dx, sizeof(T));
+        return whole ? go(launch_bwd_units<T, P, 32, 256, 1>) : go(launch_bwd_narrow<T, P, 32>);
+    }
     if (units <= 64) return go(launch_bwd_units<T, P, 32, 256, 2>);
     if (units <= 128) {
         if constexpr (sizeof(T) == 4) return go(launch_bwd_units<T, P, 32, 256, 4>);
