@@ -331,7 +331,7 @@ __device__ __forceinline__ void write_row(const LogProbArgs& a, uint32_t row_id,
 // A cluster of CTAs takes a row, each CTA a slice of its units; the CTAs join their sums and their ordered best columns
 // through each other's shared memory.
 template <typename T, uint32_t kThreads, bool kCluster>
-__global__ void __launch_bounds__(kThreads, kThreads <= 128 ? 896 / kThreads : 3)
+__global__ void __launch_bounds__(kThreads, kThreads <= 128 ? 1024 / kThreads : 4)
 lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
     constexpr uint32_t kWarps = kThreads / 32;
     __shared__ LogProbShared<kThreads> sh;
@@ -560,7 +560,7 @@ template <typename T> dct_status_t launch_logprobs(const void* logits, const Log
     uint64_t best = ~0ull;
     for (uint32_t t = 32; t <= 256; t *= 2) {
         if (t < 256 && (a.top > t || (a.top > t / 2 && units > 32 * t))) continue;
-        const uint64_t slots = static_cast<uint64_t>(sms) * (t <= 128 ? 896 / t : 3);
+        const uint64_t slots = static_cast<uint64_t>(sms) * (t <= 128 ? 1024 / t : 4);
         for (uint32_t c = 1; c <= kMaxCluster && (c == 1 || (t == 256 && units / c >= 512)); c *= 2) {
             const uint64_t rounds = (static_cast<uint64_t>(a.rows) * c + slots - 1) / slots;
             const uint64_t end = a.top ? (t == 32 ? 100 : t == 64 ? 70 : t == 128 ? 55 : 60) + 50 * a.top / t +
@@ -574,7 +574,7 @@ template <typename T> dct_status_t launch_logprobs(const void* logits, const Log
             }
         }
     }
-    const uint32_t ctas = static_cast<uint32_t>(sms) * (threads <= 128 ? 896 / threads : 3);
+    const uint32_t ctas = static_cast<uint32_t>(sms) * (threads <= 128 ? 1024 / threads : 4);
     if (threads == 32) return launch_logprobs_threads<T, 32>(logits, a, 1, ctas, stream);
     if (threads == 64) return launch_logprobs_threads<T, 64>(logits, a, 1, ctas, stream);
     if (threads == 128) return launch_logprobs_threads<T, 128>(logits, a, 1, ctas, stream);
