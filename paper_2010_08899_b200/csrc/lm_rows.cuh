@@ -284,7 +284,7 @@ __device__ __noinline__ RowPart low_part(const RowView<T> row, uint32_t u0, uint
 struct RowSums {
     static constexpr float kSlack = 4.0f;
     float ref, s, st;
-    bool masked;                   // this thread has met -inf beside numbers
+    bool masked;                   // several of the warp's lanes met -inf beside numbers in the last batch
     __device__ __forceinline__ RowSums() : ref(minus_inf()), s(0.0f), st(0.0f), masked(false) {}
 
     // sums over four units.  kClamp: y at least -200, so that a masked column (2^y = 0, y = -inf) adds 0 to the moment and not NaN
@@ -337,11 +337,11 @@ struct RowSums {
         if (!kMoment) {
             batch<T, false, false>(v, c, sum, moment);
         } else {
-            if (!masked) {
-                batch<T, true, false>(v, c, sum, moment);
-                masked = moment != moment;
-            }
-            if (masked) batch<T, true, true>(v, c, sum, moment);
+            // (the ends of a row put -inf into one lane's units of one batch: no reason to clamp from there on)
+            if (!masked) batch<T, true, false>(v, c, sum, moment);
+            const bool clamp = masked || moment != moment;
+            masked = __popc(__ballot_sync(0xFFFFFFFFu, clamp)) >= 8;
+            if (clamp) batch<T, true, true>(v, c, sum, moment);
         }
         s = __fadd_rn(s, sum);
         if (kMoment) st = __fadd_rn(st, moment);
