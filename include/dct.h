@@ -602,7 +602,10 @@ DCT_API dct_status_t dct_dp_drift_check(
  *              be preserved.  Not looked at if dweight and dbias are both NULL.
  * 1 <= d <= 65536; rows may be 0 (nothing is read or written but dweight and dbias, which become zero).
  * All arithmetic is fp32, rounded once into y / dx.  A row with NaN or infinities gives NaN, and is not looked for.
- * Any width, stride and address gives the same result; rows on 16-byte boundaries are the fast case.
+ * Any width, stride and address gives the same result; rows on 16-byte boundaries are the fast case.  Rows of up to 32 KiB
+ * (backward: 16 KiB of bf16, 32 KiB of fp32) are read once; wider ones several times.  Should a bounded wait for an
+ * asynchronous copy give up (not seen in practice), the rows concerned and the parameters' gradients become NaN.
+ * (The paper trains a Transformer with its own layer norms; it prescribes nothing for this or the calls below.)
  */
 DCT_API dct_status_t dct_layer_norm_fwd(
     const void* x, dct_dtype_t dtype, uint32_t rows, uint32_t d, uint32_t ld,
@@ -638,11 +641,12 @@ DCT_API dct_status_t dct_layer_norm_bwd(
  *   result     device block or NULL; status is DCT_OK, or DCT_ERR_BAD_MASK if a token was >= vocab (it is then
  *              treated like a negative one).  With NULL no extra work is enqueued for it.
  * 1 <= vocab <= DCT_LM_MAX_VOCAB; rows may be 0; inv_temperature is finite and > 0.
- * A masked column holds -inf (log p = -inf, no weight anywhere) or the type's lowest value.  A row that is -inf
+ * z has to stay within fp32's range.  A masked column holds -inf (log p = -inf, no weight anywhere) or the type's lowest value.  A row that is -inf
  * throughout has no distribution: m = -inf, s = 0, log p = -inf, entropy 0.  A row with a NaN or +inf gets NaN for
  * all of its computed values; its top_ids are still in order, NaN after everything else.
- * Sums are fp32 (any width, stride and address; rows on 16-byte boundaries are the fast case).  Columns outside
- * the row that share a 16-byte unit with its ends may be read, never used.
+ * Sums are fp32, in a fixed order for given sizes and alignment (any width, stride and address; rows on 16-byte
+ * boundaries are the fast case).  Columns outside the row that share a 16-byte unit with its ends may be read, never
+ * used.
  */
 DCT_API dct_status_t dct_lm_logprobs_fwd(
     const void* logits, dct_dtype_t dtype, uint32_t rows, uint32_t vocab, uint32_t ld, float inv_temperature,
@@ -693,7 +697,8 @@ typedef enum {
  *   grad_logits       [rows, ld_grad], dtype of logits, or NULL for the loss alone.  May be logits itself (same address
  *                     and stride); any other overlap is refused.  One of loss_out and grad_logits must be given.
  *   result            device block or NULL; status is DCT_OK, or DCT_ERR_BAD_MASK if an id was >= vocab (that slot
- *                     counts as empty).
+ *                     counts as empty), or DCT_ERR_TIMEOUT if a bounded wait for an asynchronous copy gave up (not
+ *                     seen in practice; loss and gradient of the rows concerned are then NaN).
  * A RENORM row without a slot that has weight, and a row of logits that is -inf throughout, has loss 0 and gradient 0.
  * A named column with q > 0 and p = 0 makes the loss +inf (the gradient stays finite).  A row with NaN or +inf in its
  * logits, or NaN in its teacher's values, gives NaN.  Vocabulary, strides, alignment and rows as in dct_lm_logprobs_fwd.

@@ -37,6 +37,13 @@ __device__ __forceinline__ void add_value(RowPart& p, float v) {
 // the sums, so that the remainder is summed and not a difference.  The gradient is first written as if no column were named,
 // and the named ones once more afterwards.
 // Slot i belongs to thread i mod kThreads throughout.
+// With y_j = (x_j - xmax) c and S = sum 2^y over the streamed columns:
+//   RENORM: gradient of a column 2^y (scale / S), a named one's less its q scale;
+//   TAIL:   of a column that is not named 2^y (p_r - q_r) scale / S, with p_r the streamed columns' share of the whole: the
+//           factor p_j (1 - q_r / p_r) without the quotient, which overflows where the remainder is tiny.
+// What bounds it: instructions.  An element takes two powers of two (the special function unit is 55 % busy) and 17 instructions of
+// its thread in all, at 24 warps to an SM since the rows take the shared memory; reading and writing 2^27 bf16 logits alone would
+// take 82 us.  4096 rows of 32768 bf16, 64 slots: 116 us (4.6 TB/s; every logit is read from DRAM once), fp32 232 us (4.6).
 constexpr uint32_t kChunkUnits = 128u, kChunkBytes = 16u * kChunkUnits;
 constexpr uint32_t kMaxChunksPerWarp = 16u;
 // shared memory of a CTA that a staged slice may take: three CTAs to an SM.  (With one, loading twice is faster: 256 rows of 262144

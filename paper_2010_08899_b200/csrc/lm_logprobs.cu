@@ -328,8 +328,14 @@ __device__ __forceinline__ void write_row(const LogProbArgs& a, uint32_t row_id,
     }
 }
 
+// log p_j = z_j - m - s, entropy = s - mean of (z - m), and the `top` best columns, from one reading of the logits.
 // A cluster of CTAs takes a row, each CTA a slice of its units; the CTAs join their sums and their ordered best columns
 // through each other's shared memory.
+// What bounds it: without alternatives reading, 4096 rows of 32768 bf16 in 50 us (5.4 TB/s), fp32 in 88 us (6.1 TB/s).  With 64
+// alternatives bf16 takes 71 us: 10 instructions per element and thread in all, and after the reading the selection's short phases
+// one after the other (bound, list, some 80 pairs read again, order), which only other CTAs on the SM fill.  So it is the
+// number of warps that counts: 32 to an SM 71 us, 28 73 us, 20 with a batch loaded ahead into registers 88 us; bringing the next row
+// into L2 during the selection made it 77, as the selection's own random reads waited longer.
 template <typename T, uint32_t kThreads, bool kCluster>
 __global__ void __launch_bounds__(kThreads, kThreads <= 128 ? 1024 / kThreads : 4)
 lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
@@ -461,7 +467,9 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
     }
 }
 
-// Elementwise: a CTA takes four units per thread of one row.
+// grad_j = (1 / T) (a (1[j = token] - p_j) - c p_j (log p_j + entropy)), elementwise: a CTA takes four units per thread of one
+// row.  p comes from the saved m and log sum, so no row is summed again; the product with log2 e is a step of its own here (log p
+// itself is needed to fp32 accuracy).  Memory bound: 1023 rows of 50021 fp32 at a stride of 50048 in 68 us, 6.0 TB/s.
 constexpr uint32_t kBwdThreads = 256u, kBwdUnits = 4u;
 
 struct LogProbBwdArgs {
@@ -550,12 +558,12 @@ template <typename T> dct_status_t launch_logprobs(const void* logits, const Log
     const uint32_t units = (a.vocab + Unit<T>::kElems - 1) / Unit<T>::kElems;
     // Threads to a row's CTA, and CTAs to a row: the shape with the least estimated time, in tenths of a microsecond.  A round of
     // CTAs takes what the end of a row costs (join, selection, order; more warps to a row make it shorter but fewer rows share
-    // it) and 0.9 us for each batch of four units per thread.  Measured at both ends: 16384 rows of 4096 bf16, top 20: 49 / 70 /
-    // 96 / 252 us with 32 / 64 / 128 / 256 threads; 1000 rows of 131072: 146 / 82 / 57 / 72; one row of 32768: 26 / 14 / 9 / 7.5.
-    // Splitting a row costs the exchange of the lists: one row of 32768 with 1 / 2 / 4 / 8 CTAs 7.5 / 8.3 / 8.2 / 10.6 us, of 131072
-    // 14.9 / 12.2 / 10.3 / 10.5, 64 rows of 131072 21.6 / 16.1 / 13.6 / 21.9.
+    // it) and 0.9 us for each batch of four units per thread.  Measured at both ends: 16384 rows of 4096 bf16, top 20: 46 / 66 /
+    // 89 / 217 us with 32 / 64 / 128 / 256 threads; 1000 rows of 131072: 137 / 82 / 56 / 63; one row of 32768: 23 / 15 / 10 / 7.8.
+    // Splitting a row costs the exchange of the lists: one row of 32768 with 1 / 2 / 4 / 8 CTAs 7.8 / 8.4 / 8.3 / 10.6 us, of 131072
+    // 16.3 / 12.9 / 10.6 / 10.5, 64 rows of 131072 22.6 / 17.3 / 14.2 / 14.7.
     // A selection wants twice as many classes as columns; where the row has many batches, more threads to it are better
-    // still (4096 rows of 32768, top 64: 79 us with 64 threads, 73 with 128; of 8192: 67 and 75).
+    // still (4096 rows of 32768, top 64: 79 us with 64 threads, 71 with 128; 8192 of 8192: 61 and 71).
     uint32_t threads = 256, cluster = 1;
     uint64_t best = ~0ull;
     for (uint32_t t = 32; t <= 256; t *= 2) {
