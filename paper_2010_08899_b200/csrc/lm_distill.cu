@@ -55,7 +55,11 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads)
 lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
     constexpr uint32_t E = Unit<T>::kElems, kWarps = kThreads / 32;
     extern __shared__ __align__(128) uint32_t dynamic[];
-    __shared__ RowPart student_parts[kWarps], named_parts[kWarps], slice_part, slice_named;
+    __shared__ RowPart student_parts[kWarps], named_parts[kWarps];
+    // the sums of the cluster's slices: every CTA pushes its own to all, two rows in turn.  (A row's numbers arrive only after every CTA
+    // has had the last row's, so two places are enough, and no barrier has to wait for the gradient's stores.)
+    __shared__ __align__(16) float4 pushed[kCluster ? 2 : 1][kMaxCluster];
+    __shared__ uint64_t joined[2];
     __shared__ float loss_parts[kWarps];
     __shared__ uint32_t repeated_flag, weight_flag, nan_flag, gave_up;      // of the row's slots; a wait ran out
     __shared__ uint64_t arrived[kStaged ? kWarps * kMaxChunksPerWarp : 1];
@@ -67,7 +71,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = lane_id();
     const uint32_t rank = kCluster ? cluster_rank() : 0u, ctas = kCluster ? cluster_size() : 1u;
     const uint32_t clusters = gridDim.x / ctas;
-    uint32_t phases = 0, missed = 0;       // the parity each of this warp's barriers is waited for with; copies given up on
+    uint32_t phases = 0, join_phases = 0, missed = 0;       // the parity each of this warp's barriers is waited for with; copies given up on
 
     // (staged) asks for chunk k of a row's slice
     auto fetch_chunk = [&](const RowView<T>& of_row, const Slice& of_slice, uint32_t k) {
@@ -98,6 +102,14 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         __syncwarp();
         const RowView<T> row(logits + static_cast<size_t>(row_id) * a.ld, a.vocab);
         for (uint32_t k = warp; k < a.chunks; k += kWarps) fetch_chunk(row, Slice(row.units, rank, ctas), k);
+    }
+    if (kCluster) {
+        if (tid == 0) {
+            mbar_init(&joined[0], 1);
+            mbar_init(&joined[1], 1);
+            mbar_init_fence();
+        }
+        cluster_arrive();                                  // (waited for before the first push)
     }
     fetch_slots(row_id, 0);
     copy_commit();
@@ -163,6 +175,19 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                     phases ^= 1u << j;
                 }
             }
+            if (kTail && kStaged) {                        // -inf at this thread's named columns, for both readings
+                uint32_t bits = 0;
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) bits |= marked(min(first + 32 * i, u1 - 1)) << E * i;
+                if (bits) {
+                    do {
+                        const uint32_t at = __ffs(bits) - 1;
+                        reinterpret_cast<T*>(stage + k * kChunkUnits + lane + at / E * 32)[at % E] = from_f32<T>(minus_inf());
+                        bits &= bits - 1;
+                    } while (bits);
+                    if (!grad) fence_proxy_async_smem();   // the next row's copy comes after this
+                }
+            }
             const uint4* from = kStaged ? stage + k * kChunkUnits + lane : row.base + first;
             if (first - lane + kChunkUnits <= u1) {        // a whole chunk
 #pragma unroll
@@ -179,7 +204,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                 for (uint32_t i = 0; i < 4; ++i)
                     if (first + 32 * i < u1) row.mask(v[i], first + 32 * i);
             }
-            if (kTail) {
+            if (kTail && !kStaged) {
                 uint32_t bits[4];
 #pragma unroll
                 for (uint32_t i = 0; i < 4; ++i) bits[i] = marked(min(first + 32 * i, u1 - 1));
@@ -199,6 +224,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             x_best = fmaxf(x_best, best);
             sums.add<T, false>(v, best, a.c);
         }
+        if (kTail && kStaged && grad) fence_proxy_async_smem();      // the next row's copies come after what was written to `stage`
         const RowPart mine = sums.part<false>(warp_max(x_best), a.c);
 
         // the slots: the teacher's values, and (kTail) the student's at the slice's named columns, each column once
@@ -251,24 +277,28 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             named.join_lanes<kWarps, false>(kLog2E);
         }
         if (kCluster) {
-            if (tid == 0) {
-                slice_part = student;
-                slice_named = named;
+            if (row_id == blockIdx.x / ctas) cluster_wait();         // (the first row) every CTA's mbarriers are there
+            if (warp == 0) {
+                if (lane == 0 && !gave_up) mbar_arrive_expect_tx(&joined[turn], 16 * ctas);
+                __syncwarp();
+                if (lane < ctas)
+                    push_remote(remote_smem(&pushed[turn][rank], lane), student.xmax, gave_up ? __uint_as_float(0x7FFFFFFFu) : student.s,
+                                named.xmax, named.s, remote_smem(&joined[turn], lane));
             }
-            cluster_barrier();
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&joined[turn], join_phases >> turn & 1u, a.spin_limit, &gave_up)))
+                *const_cast<volatile uint32_t*>(&gave_up) = 1;
+            join_phases ^= 1u << turn;
             const uint32_t c = lane & (kMaxCluster - 1);
             student = named = RowPart{minus_inf(), 0.0f, 0.0f};
             if (c < ctas) {
-                student.xmax = ld_remote_f32(remote_smem(&slice_part.xmax, c));
-                student.s = ld_remote_f32(remote_smem(&slice_part.s, c));
-                if (kTail) {
-                    named.xmax = ld_remote_f32(remote_smem(&slice_named.xmax, c));
-                    named.s = ld_remote_f32(remote_smem(&slice_named.s, c));
-                }
+                const float4 of = pushed[turn][c];
+                student.xmax = of.x;
+                student.s = of.y;
+                named.xmax = of.z;
+                named.s = of.w;
             }
             student.join_lanes<kMaxCluster, false>(a.c);
             if (kTail) named.join_lanes<kMaxCluster, false>(kLog2E);
-            cluster_arrive();                              // (waited for at the end of the row)
         }
         // the norm of the teacher's values: the warps that have slots find it for themselves
         RowPart teacher{minus_inf(), 0.0f, 0.0f};
@@ -348,11 +378,11 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             };
             const float ref = __fmul_rn(student.xmax, a.c);
             const uint64_t by_c = pack2(a.c, a.c);
-            // (a named column may be far above the others, whose factor this is: it is written again below)
+            // (a named column may be far above the others, whose factor this is: it is written again below; staged, it is -inf by now)
             auto powers = [&](uint64_t y) {
                 float y0, y1;
                 unpack2(y, y0, y1);
-                return kTail ? pack2(exp2_fast(fminf(y0, 64.0f)), exp2_fast(fminf(y1, 64.0f))) : pack2(exp2_fast(y0), exp2_fast(y1));
+                return kTail && !kStaged ? pack2(exp2_fast(fminf(y0, 64.0f)), exp2_fast(fminf(y1, 64.0f))) : pack2(exp2_fast(y0), exp2_fast(y1));
             };
             if (nothing) {                                 // whatever the logits are
                 write_chunks([](uint64_t) { return 0ull; });
@@ -393,7 +423,6 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             repeated_flag = weight_flag = nan_flag = 0;
             if (gave_up && a.result) atomicMax(&a.result->status, static_cast<uint32_t>(DCT_ERR_TIMEOUT));
         }
-        if (kCluster) cluster_wait();
         if (!more) break;
         row_id += clusters;
     }
@@ -402,6 +431,10 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         for (uint32_t j = 0; j < kMaxChunksPerWarp; ++j)
             for (uint32_t i = 0; (missed >> j & 1u) && i < a.spin_limit; ++i)
                 if (mbar_try_wait(&arrived[warp * kMaxChunksPerWarp + j], phases >> j & 1u)) break;
+    if (kCluster) {                                        // the same for what the cluster pushes, should a wait have run out
+        cluster_barrier();
+        if (gave_up) __nanosleep(1000000u);
+    }
 }
 
 template <typename T, uint32_t kThreads, bool kTail, bool kCluster, bool kStaged>

@@ -439,6 +439,11 @@ __device__ __forceinline__ uint64_t ld_remote_u64(uint32_t a) {
     asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
     return v;
 }
+// four values into another CTA's shared memory (16-byte aligned), counted there on that CTA's mbarrier; both by remote_smem
+__device__ __forceinline__ void push_remote(uint32_t to, float x, float y, float z, float w, uint32_t bar) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                 ::"r"(to), "f"(x), "f"(y), "f"(z), "f"(w), "r"(bar) : "memory");
+}
 
 // Host side ---------------------------------------------------------------------------------------------------
 
