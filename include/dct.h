@@ -639,7 +639,8 @@ DCT_API dct_status_t dct_layer_norm_bwd(
  *              among them) by the lower column.
  *   top_logprobs [rows, top] fp32: their log p.
  *   result     device block or NULL; status is DCT_OK, or DCT_ERR_BAD_MASK if a token was >= vocab (it is then
- *              treated like a negative one).  With NULL no extra work is enqueued for it.
+ *              treated like a negative one), or DCT_ERR_TIMEOUT if a bounded wait between the CTAs of a row gave up (not
+ *              seen in practice; that row's numbers are NaN).  With NULL no extra work is enqueued for it.
  * 1 <= vocab <= DCT_LM_MAX_VOCAB; rows may be 0; inv_temperature is finite and > 0.
  * z has to stay within fp32's range.  A masked column holds -inf (log p = -inf, no weight anywhere) or the type's lowest value.  A row that is -inf
  * throughout has no distribution: m = -inf, s = 0, log p = -inf, entropy 0.  A row with a NaN or +inf gets NaN for

@@ -16,6 +16,7 @@ struct LogProbArgs {
     int32_t* top_ids;
     float* top_logprobs;
     dct_result_t* result;
+    uint32_t spin_limit;            // polls a wait for the cluster's other CTAs may take
 };
 
 template <uint32_t kThreads> struct LogProbShared {
@@ -27,12 +28,11 @@ template <uint32_t kThreads> struct LogProbShared {
     uint64_t candidates[kCandidates];
     uint64_t best[kMaxTop];
     float class_max[2 * kThreads];
-    uint16_t hits[kGroups * kThreads];
+    alignas(4) uint16_t hits[kGroups * kThreads];
     RowPart warp_part[2][kWarps];      // by turns, row by row
-    RowPart part;                      // this CTA's slice
     float m, logsum;                   // of the whole row
     uint32_t counts[32];
-    uint32_t counter, hit_count, bound, tied;
+    uint32_t counter, hit_count, bound, tied, gave_up;
 };
 
 __device__ __forceinline__ float value_of_key(uint32_t key) {       // the inverse of order_key
@@ -81,7 +81,8 @@ template <typename T, uint32_t kThreads> struct Selector {
         }
         lo = __reduce_min_sync(0xFFFFFFFFu, lo);
         hi = __reduce_max_sync(0xFFFFFFFFu, hi);
-        // at least kk classes reach lo, fewer reach hi + 1; a few more than kk are as good as kk
+        // at least kk classes reach lo, fewer reach hi + 1; a few more than kk are as good as kk.  (Counting the range into 256 parts
+        // instead of halving it: no difference for many rows, 0.3 us more for one row, whose code is not in the caches yet.)
         while (lo < hi) {
             const uint32_t mid = lo + (hi - lo) / 2 + 1;
             uint32_t n = 0;
@@ -302,9 +303,9 @@ template <typename T, uint32_t kThreads> struct Selector {
     }
 };
 
-// One thread: the row's m and log sum, and the results that are numbers per row.
-template <typename T>
-__device__ __forceinline__ void write_row(const LogProbArgs& a, uint32_t row_id, const T* xr, int32_t tok, const RowPart& all,
+// One thread: the row's m and log sum, and the results that are numbers per row.  x: the logit of the token (any number if that is
+// none of the row's).
+__device__ __forceinline__ void write_row(const LogProbArgs& a, uint32_t row_id, float x, int32_t tok, const RowPart& all,
                                           float& m_out, float& logsum_out) {
     const float m = __fmul_rn(all.xmax, a.inv_t);
     const bool empty = m == minus_inf() && all.s == all.s;
@@ -315,7 +316,7 @@ __device__ __forceinline__ void write_row(const LogProbArgs& a, uint32_t row_id,
     if (a.tokens) {
         float lp = 0.0f;
         if (tok >= 0 && static_cast<uint32_t>(tok) < a.vocab) {
-            lp = fmaf(to_f32(xr[tok]), a.inv_t, m == minus_inf() ? 0.0f : -m) - logsum;
+            lp = fmaf(x, a.inv_t, m == minus_inf() ? 0.0f : -m) - logsum;
         } else if (tok >= 0 && a.result) {
             atomicMax(&a.result->status, static_cast<uint32_t>(DCT_ERR_BAD_MASK));
         }
@@ -344,6 +345,19 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = lane_id();
     const uint32_t rank = kCluster ? cluster_rank() : 0u, ctas = kCluster ? cluster_size() : 1u;
     const uint32_t clusters = gridDim.x / ctas;
+    // kCluster: every CTA pushes the sums of its slice, and its best columns in order, to all.  (Nobody pushes a row's before all
+    // have read the last row's: that is what the cluster's barrier is for.  It is met long before it is waited for.)
+    extern __shared__ __align__(16) uint64_t lists[];                  // [ctas][top]
+    __shared__ __align__(16) float4 pushed[kMaxCluster];
+    __shared__ uint64_t joined;
+    if (kCluster) {
+        if (tid == 0) {
+            sh.gave_up = 0;
+            mbar_init(&joined, 1);
+            mbar_init_fence();
+        }
+        cluster_arrive();
+    }
     uint32_t turn = 0;
     for (uint32_t row_id = blockIdx.x / ctas;; turn ^= 1) {
         const T* xr = logits + static_cast<size_t>(row_id) * a.ld;
@@ -387,6 +401,17 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
         if (lane == 0) sh.warp_part[turn][warp] = mine;
         __syncthreads();
 
+        float x_tok = 0.0f;
+        if (tid == kThreads - 32 && tok >= 0 && static_cast<uint32_t>(tok) < a.vocab) x_tok = to_f32(xr[tok]);
+        if (kCluster) {
+            cluster_wait();
+            if (tid == 0 && !sh.gave_up) {
+                uint32_t listed = 0;
+                for (uint32_t c = 0; c < ctas; ++c)
+                    if (c != rank) listed += min(a.top, Slice(row.units, c, ctas).columns(row));
+                mbar_arrive_expect_tx(&joined, 16 * ctas + 8 * listed);
+            }
+        }
         // the last warp joins the slice's sums (and writes the results of a row that is one slice); the first meanwhile looks
         // for the bound of the selection
         if (warp == kWarps - 1) {
@@ -395,9 +420,10 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
             if (all.s == 0.0f && all.xmax > minus_inf()) {
                 all = low_part(row, u0, u1, all.xmax, a.c, [](uint32_t, uint32_t) { return true; });
             }
-            if (lane == 0) {
-                sh.part = all;
-                if (!kCluster) write_row(a, row_id, xr, tok, all, sh.m, sh.logsum);
+            if (kCluster) {
+                if (lane < ctas) push_remote(remote_smem(&pushed[rank], lane), all.xmax, all.s, all.st, 0.0f, remote_smem(&joined, lane));
+            } else if (lane == 0) {
+                write_row(a, row_id, x_tok, tok, all, sh.m, sh.logsum);
             }
         }
         uint32_t kept = 0;
@@ -406,15 +432,22 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
             if (kept) Selector<T, kThreads>{row, u0, u1, group_shift, sh}.run(kept);
         }
 
+        uint32_t* const places = reinterpret_cast<uint32_t*>(sh.hits);      // no longer in use
         if (kCluster) {
-            cluster_barrier();
+            for (uint32_t item = tid; item < ctas * kept; item += kThreads) {
+                const uint32_t c = item / kept, i = item % kept;
+                if (c != rank) push_remote(remote_smem(&lists[rank * a.top + i], c), sh.best[i], remote_smem(&joined, c));
+            }
+            for (uint32_t i = tid; i < kept; i += kThreads) places[i] = i;
+            const bool here = mbar_wait_bounded(&joined, turn, a.spin_limit, &sh.gave_up);
+            if (!here) *const_cast<volatile uint32_t*>(&sh.gave_up) = 1;         // this row and the rest become NaN
+            __syncthreads();
             if (warp == kWarps - 1) {
                 RowPart all{minus_inf(), 0.0f, 0.0f};
                 const uint32_t c = lane & (kMaxCluster - 1);
                 if (c < ctas) {
-                    all.xmax = ld_remote_f32(remote_smem(&sh.part.xmax, c));
-                    all.s = ld_remote_f32(remote_smem(&sh.part.s, c));
-                    all.st = ld_remote_f32(remote_smem(&sh.part.st, c));
+                    const float4 of = pushed[c];
+                    all = RowPart{of.x, sh.gave_up ? __uint_as_float(0x7FFFFFFFu) : of.y, of.z};
                 }
                 all.join_lanes<kMaxCluster, true>(a.c);
                 if (lane == 0) {
@@ -423,35 +456,29 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
                         mine.tokens = nullptr;
                         mine.entropy_out = mine.stats_out = nullptr;
                     }
-                    write_row(mine, row_id, xr, tok, all, sh.m, sh.logsum);
+                    if (sh.gave_up && a.result) atomicMax(&a.result->status, static_cast<uint32_t>(DCT_ERR_TIMEOUT));
+                    write_row(mine, row_id, x_tok, tok, all, sh.m, sh.logsum);
                 }
             }
-            // the other slices' lists, all loads at once
-            for (uint32_t item = tid; item < ctas * a.top; item += kThreads) {
-                const uint32_t c = item / a.top, i = item % a.top;
-                if (c != rank && i < min(a.top, Slice(row.units, c, ctas).columns(row)))
-                    sh.candidates[c * sh.kMaxTop + i] = ld_remote_u64(remote_smem(&sh.best[i], c));
+            // a column's place: its place in its own slice's list, and how many of each other list are better
+            for (uint32_t item = tid; item < ctas * kept; item += kThreads) {
+                const uint32_t c = item / kept, i = item % kept;
+                if (c == rank) continue;
+                const uint64_t key = sh.best[i], *list = lists + c * a.top;
+                uint32_t lo = 0, hi = min(a.top, Slice(row.units, c, ctas).columns(row));         // list[0 .. lo) are better
+                while (lo < hi) {
+                    const uint32_t mid = (lo + hi) / 2;
+                    if (list[mid] > key) lo = mid + 1;
+                    else hi = mid;
+                }
+                if (lo) atomicAdd(&places[i], lo);
             }
             __syncthreads();
-            cluster_arrive();             // (waited for below: nobody reads this CTA's shared memory any more)
+            cluster_arrive();             // what the others pushed has been read
         }
-        // a column's place: its place in its own slice's list, and how many of each other list are better
         for (uint32_t i = tid; i < kept; i += kThreads) {
             const uint64_t key = sh.best[i];
-            uint32_t place = i;
-            if (kCluster) {
-                for (uint32_t c = 0; c < ctas; ++c) {
-                    if (c == rank) continue;
-                    const uint64_t* list = sh.candidates + c * sh.kMaxTop;
-                    uint32_t lo = 0, hi = min(a.top, Slice(row.units, c, ctas).columns(row));         // list[0 .. lo) are better
-                    while (lo < hi) {
-                        const uint32_t mid = (lo + hi) / 2;
-                        if (list[mid] > key) lo = mid + 1;
-                        else hi = mid;
-                    }
-                    place += lo;
-                }
-            }
+            const uint32_t place = kCluster ? places[i] : i;
             if (place < a.top) {
                 const size_t at = static_cast<size_t>(row_id) * a.top + place;
                 a.top_ids[at] = static_cast<int32_t>(0xFFFFFFFFu - static_cast<uint32_t>(key));
@@ -459,11 +486,13 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
                                           sh.m == minus_inf() ? 0.0f : -sh.m) - sh.logsum;
             }
         }
-        // Nobody may read this CTA's shared memory any more when its next row begins.  (A CTA on its own needs no barrier
-        // here: the warps' parts alternate, and what else the next row writes it writes behind its first barrier.)
-        if (kCluster) cluster_wait();
+        // (No barrier: the warps' parts alternate, and what else the next row writes it writes behind its first barrier.)
         if (a.rows - row_id <= clusters) break;
         row_id += clusters;
+    }
+    if (kCluster) {                       // nobody pushes to a CTA that is gone
+        cluster_wait();
+        if (sh.gave_up) __nanosleep(1000000u);
     }
 }
 
@@ -538,12 +567,16 @@ dct_status_t launch_logprobs_threads(const void* logits, const LogProbArgs& a, u
     const T* x = static_cast<const T*>(logits);
     if constexpr (kThreads == 256) {
         if (cluster > 1) {
-            static std::atomic<uint32_t> kept[3];
+            static std::atomic<uint32_t> allowed[64], kept[2][3];
             auto kernel = lm_logprobs_kernel<T, kThreads, true>;
-            uint32_t at_once = 1;
-            const dct_status_t st = clusters_at_once(kernel, kThreads, cluster, 0, kept, &at_once);
+            const bool many = a.top > 128;            // room for the lists: 8 CTAs' of 128 columns leave four CTAs to an SM
+            const size_t smem = static_cast<size_t>(cluster) * (many ? 256 : 128) * sizeof(uint64_t);
+            dct_status_t st = allow_shared(kernel, smem, allowed, 0);
             if (st != DCT_OK) return st;
-            DCT_CUDA_TRY(launch_clusters(kernel, (a.rows < at_once ? a.rows : at_once) * cluster, kThreads, cluster, 0, stream, x, a));
+            uint32_t at_once = 1;
+            st = clusters_at_once(kernel, kThreads, cluster, smem, kept[many], &at_once);
+            if (st != DCT_OK) return st;
+            DCT_CUDA_TRY(launch_clusters(kernel, (a.rows < at_once ? a.rows : at_once) * cluster, kThreads, cluster, smem, stream, x, a));
             return DCT_OK;
         }
     }
@@ -616,7 +649,8 @@ extern "C" dct_status_t dct_lm_logprobs_fwd(const void* logits, dct_dtype_t dtyp
     }
     if (result) DCT_CUDA_TRY(cudaMemsetAsync(result, 0, sizeof(dct_result_t), stream));
     if (rows == 0) return DCT_OK;
-    const LogProbArgs args{rows, vocab, ld, inv_temperature, log2_scale(inv_temperature), tokens, top, logprob_out, entropy_out, stats_out, top_ids, top_logprobs, result};
+    const LogProbArgs args{rows, vocab, ld, inv_temperature, log2_scale(inv_temperature), tokens, top, logprob_out, entropy_out, stats_out, top_ids, top_logprobs, result,
+                           debug_config().spin_limit};
     return dtype == DCT_F32 ? launch_logprobs<float>(logits, args, stream) : launch_logprobs<__nv_bfloat16>(logits, args, stream);
 }
 

@@ -425,25 +425,13 @@ __device__ __forceinline__ uint32_t remote_smem(const void* p, uint32_t rank) { 
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
     return a;
 }
-__device__ __forceinline__ float ld_remote_f32(uint32_t a) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint32_t ld_remote_u32(uint32_t a) {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint64_t ld_remote_u64(uint32_t a) {
-    uint64_t v;
-    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
-    return v;
-}
 // four values into another CTA's shared memory (16-byte aligned), counted there on that CTA's mbarrier; both by remote_smem
 __device__ __forceinline__ void push_remote(uint32_t to, float x, float y, float z, float w, uint32_t bar) {
     asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
                  ::"r"(to), "f"(x), "f"(y), "f"(z), "f"(w), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void push_remote(uint32_t to, uint64_t x, uint32_t bar) {          // 8-byte aligned
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(to), "l"(x), "r"(bar) : "memory");
 }
 
 // Host side ---------------------------------------------------------------------------------------------------
@@ -513,11 +501,11 @@ inline bool in_place_or_apart(const void* in, uint32_t ld_in, const void* out, u
     return (in == out && ld_in == ld_out) ||
            !spans_overlap(in, span_bytes(rows, d, ld_in, es), out, span_bytes(rows, d, ld_out, es));
 }
-// lets `kernel` have `bytes` of dynamic shared memory, once per device and amount.  (Without asking it has 48 KiB, of which static
-// shared memory is a part: asked for from well below that.)  allowed: zeros at first, the kernel's own.
+// lets `kernel` have `bytes` of dynamic shared memory, once per device and amount.  Without asking it has 48 KiB, of which static
+// shared memory is a part: `unasked` of them are had anyway.  allowed: zeros at first, the kernel's own.
 template <typename... Params>
-inline dct_status_t allow_shared(void (*kernel)(Params...), size_t bytes, std::atomic<uint32_t> (&allowed)[64]) {
-    if (bytes <= 32 * 1024) return DCT_OK;
+inline dct_status_t allow_shared(void (*kernel)(Params...), size_t bytes, std::atomic<uint32_t> (&allowed)[64], size_t unasked = 32 * 1024) {
+    if (bytes <= unasked) return DCT_OK;
     int dev = 0;
     DCT_CUDA_TRY(cudaGetDevice(&dev));
     std::atomic<uint32_t>* word = dev >= 0 && dev < 64 ? &allowed[dev] : nullptr;
