@@ -593,8 +593,9 @@ template <typename T> dct_status_t launch_logprobs(const void* logits, const Log
     // CTAs takes what the end of a row costs (join, selection, order; more warps to a row make it shorter but fewer rows share
     // it) and 0.9 us for each batch of four units per thread.  Measured at both ends: 16384 rows of 4096 bf16, top 20: 46 / 66 /
     // 89 / 217 us with 32 / 64 / 128 / 256 threads; 1000 rows of 131072: 137 / 82 / 56 / 63; one row of 32768: 23 / 15 / 10 / 7.8.
-    // Splitting a row costs the exchange of the lists: one row of 32768 with 1 / 2 / 4 / 8 CTAs 7.8 / 8.4 / 8.3 / 10.6 us, of 131072
-    // 16.3 / 12.9 / 10.6 / 10.5, 64 rows of 131072 22.6 / 17.3 / 14.2 / 14.7.
+    // Splitting a row costs the exchange of the lists, and the more CTAs share an SM the longer their ends take: one row of 32768
+    // with 1 / 2 / 4 / 8 CTAs 7.8 / 8.2 / 7.3 / 8.6 us, 100 rows 10.0 / 8.9 / 10.5 / 18.4; one row of 131072 16.6 / 12.6 / 9.5 / 8.4, 64 rows
+    // 22.0 / 16.8 / 13.5 / 12.4; 8 rows of 131072 with the top 256 23.0 / 17.7 / 16.0 / 17.5.
     // A selection wants twice as many classes as columns; where the row has many batches, more threads to it are better
     // still (4096 rows of 32768, top 64: 79 us with 64 threads, 71 with 128; 8192 of 8192: 61 and 71).
     uint32_t threads = 256, cluster = 1;
@@ -603,9 +604,11 @@ template <typename T> dct_status_t launch_logprobs(const void* logits, const Log
         if (t < 256 && (a.top > t || (a.top > t / 2 && units > 32 * t))) continue;
         const uint64_t slots = static_cast<uint64_t>(sms) * (t <= 128 ? 1024 / t : 4);
         for (uint32_t c = 1; c <= kMaxCluster && (c == 1 || (t == 256 && units / c >= 512)); c *= 2) {
-            const uint64_t rounds = (static_cast<uint64_t>(a.rows) * c + slots - 1) / slots;
-            const uint64_t end = a.top ? (t == 32 ? 100 : t == 64 ? 70 : t == 128 ? 55 : 60) + 50 * a.top / t +
-                                             (c == 1 ? 0 : c == 2 ? 15 : c == 4 ? 25 : 45)
+            const uint64_t fit = c == 1 ? slots : slots * 7 / 8;              // (a GPC's SMs are no multiple of a cluster)
+            const uint64_t rounds = (static_cast<uint64_t>(a.rows) * c + fit - 1) / fit;
+            const uint64_t shared = t < 256 ? 0 : 4ull * a.rows * c >= 16ull * sms ? 16 : 4ull * a.rows * c / sms;
+            const uint64_t end = a.top ? (t == 32 ? 100 : t == 64 ? 70 : t == 128 ? 55 : 60) + 50 * a.top / t + shared +
+                                             (c == 1 ? 0 : (c == 2 ? 13 : c == 4 ? 19 : 27) + a.top * c / 64)
                                        : (t == 32 ? 40 : t == 64 ? 30 : t == 128 ? 20 : 25) + (c > 1 ? 10 : 0);
             const uint64_t cost = rounds * (end + 9 * ((units / c + 4 * t - 1) / (4 * t)));
             if (cost < best) {
