@@ -175,17 +175,13 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                     phases ^= 1u << j;
                 }
             }
-            if (kTail && kStaged) {                        // -inf at this thread's named columns, for both readings
-                uint32_t bits = 0;
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) bits |= marked(min(first + 32 * i, u1 - 1)) << E * i;
-                if (bits) {
-                    do {
-                        const uint32_t at = __ffs(bits) - 1;
-                        reinterpret_cast<T*>(stage + k * kChunkUnits + lane + at / E * 32)[at % E] = from_f32<T>(minus_inf());
-                        bits &= bits - 1;
-                    } while (bits);
+            if (kTail && kStaged) {                        // -inf at the named columns, for both readings; a word of marks to a lane
+                const uint32_t w = k * (4 * E) + lane;
+                uint32_t bits = lane < 4 * E && w < a.mark_words ? marks[w] : 0u;
+                if (__any_sync(0xFFFFFFFFu, bits)) {
+                    for (; bits; bits &= bits - 1) reinterpret_cast<T*>(stage)[32 * w + __ffs(bits) - 1] = from_f32<T>(minus_inf());
                     if (!grad) fence_proxy_async_smem();   // the next row's copy comes after this
+                    __syncwarp();
                 }
             }
             const uint4* from = kStaged ? stage + k * kChunkUnits + lane : row.base + first;
