@@ -43,7 +43,8 @@ __device__ __forceinline__ void add_value(RowPart& p, float v) {
 //           factor p_j (1 - q_r / p_r) without the quotient, which overflows where the remainder is tiny.
 // What bounds it: instructions.  An element takes two powers of two (the special function unit is 55 % busy) and 17 instructions of
 // its thread in all, at 24 warps to an SM since the rows take the shared memory; reading and writing 2^27 bf16 logits alone would
-// take 82 us.  4096 rows of 32768 bf16, 64 slots: 116 us (4.6 TB/s; every logit is read from DRAM once), fp32 232 us (4.6).
+// take 82 us.  4096 rows of 32768 bf16, 64 slots: 114 us (4.7 TB/s; every logit is read from DRAM once), fp32 200 us (5.4);
+// 1024 rows of 131072 bf16, 128 slots and the remainder (21 instructions): 147 us (3.7 TB/s).
 constexpr uint32_t kChunkUnits = 128u, kChunkBytes = 16u * kChunkUnits;
 constexpr uint32_t kMaxChunksPerWarp = 16u;
 // shared memory of a CTA that a staged slice may take: three CTAs to an SM.  (With one, loading twice is faster: 256 rows of 262144

@@ -6,9 +6,9 @@
 //   up to 2048   a CTA to a row (bf16 backward up to 1024)             } rows through a ring of bulk copies
 //   beyond       a CTA to a row that is read again for every sum (norm_fwd_kernel, norm_bwd_kernel, norm_param_parts_kernel);
 //                bf16 rows of 1025 to 2048 units with fp32 parameters go forward in registers without a ring (norm_fwd_units_kernel)
-// Memory bound: 2 and 3 times the matrix cross the bus.  16384 rows of 4096 bf16: forward 46 us (5.9 TB/s), backward 69 us with
-// the parameters' gradients (5.9 TB/s) and 62 us without; fp32 forward 89 us (6.0), backward 122 us (6.6).  Rows off the
-// 16-byte boundaries are bound by instructions: 16384 rows of 4095 bf16 72 and 102 us.
+// Memory bound: 2 and 3 times the matrix cross the bus.  16384 rows of 4096 bf16: forward 46 us (5.9 TB/s), backward 67 us with
+// the parameters' gradients (6.0 TB/s) and 62 us without; fp32 forward 89 us (6.0), backward 122 us (6.6).  Rows off the
+// 16-byte boundaries are bound by instructions: 16384 rows of 4095 bf16 72 and 100 us.
 #include "lm_rows.cuh"
 
 namespace dct {
@@ -806,9 +806,9 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
 }
 
 // dweight, dbias from the CTAs' partial sums, in a fixed order: 32 columns to a CTA, a run of partial sums to each of its warps.
-// Its launch overlaps the backward kernel; what it adds is the partial sums' way through L2 (16384 rows of 4096: 6.5 us)
-constexpr uint32_t kJoinRuns = 32u;
-__global__ void __launch_bounds__(32 * kJoinRuns)
+// Its launch overlaps the backward kernel; what it adds is the partial sums' way through L2 (16384 rows of 4096: 5.5 us)
+constexpr uint32_t kJoinRuns = 32u, kJoinBatch = 5u;      // (ten would take the registers of an SM's second CTA)
+__global__ void __launch_bounds__(32 * kJoinRuns, 2)
 norm_param_join_kernel(const float* __restrict__ parts, uint32_t num, uint32_t d, uint32_t width,
                        float* __restrict__ dweight, float* __restrict__ dbias) {
     __shared__ float s[2][kJoinRuns][33];
@@ -816,11 +816,20 @@ norm_param_join_kernel(const float* __restrict__ parts, uint32_t num, uint32_t d
     const uint32_t lane = threadIdx.x & 31u, run = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
     float w = 0.0f, b = 0.0f;
     if (col < d) {
-#pragma unroll 5
-        for (uint32_t i = run; i < num; i += kJoinRuns) {
-            const float* p = parts + static_cast<size_t>(i) * 2 * width;
-            w = __fadd_rn(w, __ldcg(p + col));
-            b = __fadd_rn(b, __ldcg(p + width + col));
+        for (uint32_t first = run; first < num; first += kJoinBatch * kJoinRuns) {
+            float ws[kJoinBatch], bs[kJoinBatch];
+#pragma unroll
+            for (uint32_t k = 0; k < kJoinBatch; ++k) {
+                const uint32_t i = first + k * kJoinRuns;
+                const float* p = parts + static_cast<size_t>(i) * 2 * width + col;
+                ws[k] = i < num ? __ldcg(p) : 0.0f;
+                bs[k] = i < num ? __ldcg(p + width) : 0.0f;
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < kJoinBatch; ++k) {
+                w = __fadd_rn(w, ws[k]);
+                b = __fadd_rn(b, bs[k]);
+            }
         }
     }
     s[0][run][lane] = w;
