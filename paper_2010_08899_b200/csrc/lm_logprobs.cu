@@ -81,6 +81,20 @@ template <typename T, uint32_t kThreads> struct Selector {
         }
         lo = __reduce_min_sync(0xFFFFFFFFu, lo);
         hi = __reduce_max_sync(0xFFFFFFFFu, hi);
+        // A mask (-inf, the type's lowest value, classes that have no unit) leaves many classes at the least key: the rest is the range, or,
+        // if it is fewer than kk, that key is the bound.  (37 rows of 50021 fp32 with twenty columns left: 12.9 us without this, 11.7 with)
+        for (uint32_t turn = 0; turn < 2 && lo < order_key(-1.0e30f) && lo < hi; ++turn) {
+            uint32_t n = 0, next = 0xFFFFFFFFu;
+#pragma unroll
+            for (uint32_t i = 0; i < N; ++i) {
+                n += key[i] > lo;
+                if (key[i] > lo) next = min(next, key[i]);
+            }
+            n = __reduce_add_sync(0xFFFFFFFFu, n);
+            next = __reduce_min_sync(0xFFFFFFFFu, next);
+            if (n < kk) hi = lo;
+            else lo = next;
+        }
         // at least kk classes reach lo, fewer reach hi + 1; a few more than kk are as good as kk.  (Counting the range into 256 parts
         // instead of halving it: no difference for many rows, 0.3 us more for one row, whose code is not in the caches yet.)
         while (lo < hi) {

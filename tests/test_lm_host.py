@@ -37,7 +37,7 @@ def test_layer_norm_forward_refusals(p):
 
 
 def test_layer_norm_backward_refusals(p):
-    ok = dict(dy=p, ld_dy=8, x=p + 1024, dtype=0, rows=2, d=8, ld=8, w=p + 2048, pd=0, mean=p + 3072, rstd=p + 3584, dx=p + 4096,
+    ok = dict(dy=p, ld_dy=8, x=p + 1024, dtype=0, rows=2, d=8, ld=8, w=p + 2048, pd=0, mean=p + 3328, rstd=p + 3584, dx=p + 4096,
               ld_dx=8, dw=p + 5120, db=p + 6144, ws=p + 8192, nbytes=1 << 15, stream=None)
     call = lambda **c: B.lib().dct_layer_norm_bwd(*_with(ok, **c))
     for change in (dict(dy=None), dict(x=None), dict(mean=None), dict(rstd=None), dict(dx=None), dict(d=0), dict(ld=7),
@@ -55,7 +55,7 @@ def test_layer_norm_backward_refusals(p):
 
 
 def test_logprobs_forward_refusals(p):
-    ok = dict(x=p, dtype=0, rows=2, vocab=8, ld=8, inv_t=1.0, tok=p + 1024, top=2, lp=p + 2048, ent=p + 3072, st=p + 4096,
+    ok = dict(x=p, dtype=0, rows=2, vocab=8, ld=8, inv_t=1.0, tok=p + 1024, top=2, lp=p + 2048, ent=p + 3328, st=p + 4096,
               ids=p + 5120, tlp=p + 6144, res=None, stream=None)
     call = lambda **c: B.lib().dct_lm_logprobs_fwd(*_with(ok, **c))
     for change in (dict(x=None), dict(vocab=0), dict(vocab=(1 << 20) + 1, ld=(1 << 20) + 1), dict(ld=7), dict(inv_t=0.0),
@@ -69,7 +69,7 @@ def test_logprobs_forward_refusals(p):
 
 
 def test_logprobs_backward_refusals(p):
-    ok = dict(x=p, dtype=1, rows=2, vocab=8, ld=8, inv_t=1.0, tok=p + 1024, st=p + 2048, ent=p + 3072, glp=p + 4096, gent=p + 5120,
+    ok = dict(x=p, dtype=1, rows=2, vocab=8, ld=8, inv_t=1.0, tok=p + 1024, st=p + 2048, ent=p + 3328, glp=p + 4096, gent=p + 5120,
               g=p + 6144, ld_g=8, stream=None)
     call = lambda **c: B.lib().dct_lm_logprobs_bwd(*_with(ok, **c))
     for change in (dict(x=None), dict(st=None), dict(g=None), dict(tok=None), dict(ent=None), dict(vocab=0), dict(ld=7),
@@ -81,7 +81,7 @@ def test_logprobs_backward_refusals(p):
 
 
 def test_distill_refusals(p):
-    ok = dict(x=p, dtype=0, rows=2, vocab=8, ld=8, inv_t=1.0, ids=p + 1024, t=p + 2048, top=2, mode=0, gl=p + 3072, loss=p + 4096,
+    ok = dict(x=p, dtype=0, rows=2, vocab=8, ld=8, inv_t=1.0, ids=p + 1024, t=p + 2048, top=2, mode=0, gl=p + 3328, loss=p + 4096,
               g=p + 5120, ld_g=8, res=None, stream=None)
     call = lambda **c: B.lib().dct_lm_distill(*_with(ok, **c))
     for change in (dict(x=None), dict(ids=None), dict(t=None), dict(loss=None, g=None), dict(top=0), dict(top=1025), dict(vocab=0),
