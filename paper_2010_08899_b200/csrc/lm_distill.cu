@@ -41,14 +41,14 @@ __device__ __forceinline__ void add_value(RowPart& p, float v) {
 //   RENORM: gradient of a column 2^y (scale / S), a named one's less its q scale;
 //   TAIL:   of a column that is not named 2^y (p_r - q_r) scale / S, with p_r the streamed columns' share of the whole: the
 //           factor p_j (1 - q_r / p_r) without the quotient, which overflows where the remainder is tiny.
-// What bounds it: instructions.  An element takes two powers of two (the special function unit is 55 % busy) and 17 instructions of
-// its thread in all, at 24 warps to an SM since the rows take the shared memory; reading and writing 2^27 bf16 logits alone would
-// take 82 us.  4096 rows of 32768 bf16, 64 slots: 114 us (4.7 TB/s; every logit is read from DRAM once), fp32 200 us (5.4);
-// 1024 rows of 131072 bf16, 128 slots and the remainder (21 instructions): 147 us (3.7 TB/s).
+// What bounds it: instructions.  An element takes two powers of two and some 16 instructions of its thread in all, at 24 warps to an SM
+// since the rows take the shared memory; reading and writing 2^27 bf16 logits alone would take 82 us.  4096 rows of 32768 bf16, 64
+// slots: 111 us (4.8 TB/s; every logit is read from DRAM once), fp32 206 us (5.2); 1024 rows of 131072 bf16, 128 slots and the
+// remainder: 142 us (3.8 TB/s).
 constexpr uint32_t kChunkUnits = 128u, kChunkBytes = 16u * kChunkUnits;
 constexpr uint32_t kMaxChunksPerWarp = 16u;
 // shared memory of a CTA that a staged slice may take: three CTAs to an SM.  (With one, loading twice is faster: 256 rows of 262144
-// fp32, 8 CTAs to a row, 195 us staged and 152 loaded twice; rows of 32768 bf16 154 us loaded twice and 117 staged.)
+// fp32, 8 CTAs to a row, 195 us staged and 152 loaded twice; rows of 32768 bf16 154 us loaded twice and 111 staged.)
 constexpr uint32_t kStagedLimit = 90u * 1024u;
 
 template <typename T, uint32_t kThreads, bool kTail, bool kCluster, bool kStaged>
@@ -69,7 +69,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
     int32_t* const ids_by_turn = reinterpret_cast<int32_t*>(marks + a.mark_words);       // two rows
     float* const t_by_turn = reinterpret_cast<float*>(ids_by_turn + 2 * a.top);           // two rows
     uint32_t* const z_words = reinterpret_cast<uint32_t*>(t_by_turn + 2 * a.top);
-    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = lane_id();
+    const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = lane_id();
     const uint32_t rank = kCluster ? cluster_rank() : 0u, ctas = kCluster ? cluster_size() : 1u;
     const uint32_t clusters = gridDim.x / ctas;
     uint32_t phases = 0, join_phases = 0, missed = 0;       // the parity each of this warp's barriers is waited for with; copies given up on
@@ -348,28 +348,44 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             if (kTail) factor = remainder ? factor * (expf(log_streamed) - q_rest) : 0.0f;
             if (broken) factor = __uint_as_float(0x7FFFFFFFu);
             auto write_chunks = [&](auto&& two) {
+                auto gradient = [&](const uint4& unit, float (&g)[E]) {
+#pragma unroll
+                    for (uint32_t e = 0; e < E; e += 2)
+                        unpack2(two(pack2(Unit<T>::get(unit, e), Unit<T>::get(unit, e + 1))), g[e], g[e + 1]);
+                };
                 for (uint32_t k = warp; u0 + k * kChunkUnits < u1; k += kWarps) {
-                    const uint32_t first = u0 + k * kChunkUnits + lane;
+                    const uint32_t start = u0 + k * kChunkUnits, first = start + lane;
                     uint4 v[4];
                     const uint4* from = kStaged ? stage + k * kChunkUnits + lane : row.base + first;
-                    // (a whole chunk inside the row, laid out alike: no unit needs a look)
-                    const bool whole = aligned && first - lane + kChunkUnits <= u1 &&
-                                       (!row.ragged || (first >= kChunkUnits && first - lane + kChunkUnits < row.units));
+                    if (aligned && start + kChunkUnits <= u1 && (!row.ragged || (start >= kChunkUnits && start + kChunkUnits < row.units))) {
+                        // a whole chunk inside the row, laid out alike: no unit needs a look
+#pragma unroll
+                        for (uint32_t i = 0; i < 4; ++i) v[i] = kStaged ? from[32 * i] : ld_unit(from + 32 * i);
+                        if (kStaged) {
+                            __syncwarp();                  // every lane has its units
+                            if (more) fetch_chunk(next_row, next_slice, k);
+                        }
+                        T* const to = out + row.column(first, 0);
+#pragma unroll
+                        for (uint32_t i = 0; i < 4; ++i) {
+                            float g[E];
+                            gradient(v[i], g);
+                            st_unit(to + 32 * i * E, Unit<T>::pack(g));
+                        }
+                        continue;
+                    }
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i)
-                        if (whole || first + 32 * i < u1) v[i] = kStaged ? from[32 * i] : ld_unit(from + 32 * i);
+                        if (first + 32 * i < u1) v[i] = kStaged ? from[32 * i] : ld_unit(from + 32 * i);
                     if (kStaged) {
-                        __syncwarp();                      // every lane has its units
+                        __syncwarp();
                         if (more) fetch_chunk(next_row, next_slice, k);
                     }
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i) {
                         float g[E];
-#pragma unroll
-                        for (uint32_t e = 0; e < E; e += 2)
-                            unpack2(two(pack2(Unit<T>::get(v[i], e), Unit<T>::get(v[i], e + 1))), g[e], g[e + 1]);
-                        if (whole) st_unit(out + row.column(first + 32 * i, 0), Unit<T>::pack(g));
-                        else if (first + 32 * i < u1) store_unit(row, out, first + 32 * i, g, aligned);
+                        gradient(v[i], g);
+                        if (first + 32 * i < u1) store_unit(row, out, first + 32 * i, g, aligned);
                     }
                 }
             };
