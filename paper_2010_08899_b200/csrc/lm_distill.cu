@@ -48,7 +48,7 @@ __device__ __forceinline__ void add_value(RowPart& p, float v) {
 constexpr uint32_t kChunkUnits = 128u, kChunkBytes = 16u * kChunkUnits;
 constexpr uint32_t kMaxChunksPerWarp = 16u;
 // shared memory of a CTA that a staged slice may take: three CTAs to an SM.  (With one, loading twice is faster: 256 rows of 262144
-// fp32, 8 CTAs to a row, 195 us staged and 152 loaded twice; rows of 32768 bf16 154 us loaded twice and 111 staged.)
+// fp32, 8 CTAs to a row, 195 us staged and 138 loaded twice; rows of 32768 bf16 154 us loaded twice and 111 staged.)
 constexpr uint32_t kStagedLimit = 90u * 1024u;
 
 template <typename T, uint32_t kThreads, bool kTail, bool kCluster, bool kStaged>
@@ -370,7 +370,9 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                         for (uint32_t i = 0; i < 4; ++i) {
                             float g[E];
                             gradient(v[i], g);
-                            st_unit(to + 32 * i * E, Unit<T>::pack(g));
+                            // (rows that are loaded twice had better keep L2: 146 and 138 us for 256 rows of 262144 fp32)
+                            if (kStaged) st_unit(to + 32 * i * E, Unit<T>::pack(g));
+                            else st_unit_stream(to + 32 * i * E, Unit<T>::pack(g));
                         }
                         continue;
                     }

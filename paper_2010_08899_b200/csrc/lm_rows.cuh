@@ -163,6 +163,9 @@ __device__ __forceinline__ uint4 ld_unit(const uint4* p) {
 __device__ __forceinline__ void st_unit(void* p, const uint4& v) {
     asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+__device__ __forceinline__ void st_unit_stream(void* p, const uint4& v) {        // the first to leave L2
+    asm volatile("st.global.cs.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 __device__ __forceinline__ void copy_word_async(void* smem, const void* global) {        // 4 bytes, both 4-byte aligned
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_addr(smem)), "l"(global) : "memory");
 }
