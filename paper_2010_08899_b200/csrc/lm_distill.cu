@@ -260,11 +260,19 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         // every warp joins the parts of all
         RowPart student = student_parts[lane & (kWarps - 1)];
         student.join_lanes<kWarps, false>(a.c);
-        if (student.s == 0.0f && student.xmax > minus_inf())
-            student = low_part(row, u0, u1, student.xmax, a.c, [=](uint32_t u, uint32_t i) {
+        // (the same for the whole CTA.  The warps read the slice again, a share each, and no warp goes on to write a gradient, which may
+        // take the logits' place, before all have read theirs)
+        if (student.s == 0.0f && student.xmax > minus_inf()) {
+            const RowPart share = low_part(row, u0 + warp * 32, kThreads, u1, student.xmax, a.c, [=](uint32_t u, uint32_t i) {
                 const uint32_t at = (u - u0) * E + i;
                 return !kTail || !(marks[at >> 5] >> (at & 31) & 1u);
             });
+            __syncthreads();                               // the parts of the first reading have been read
+            if (lane == 0) student_parts[warp] = share;
+            __syncthreads();
+            student = student_parts[lane & (kWarps - 1)];
+            student.join_lanes<kWarps, false>(a.c);
+        }
         if (kTail) {
             named = named_parts[lane & (kWarps - 1)];
             q_sum = named.st;

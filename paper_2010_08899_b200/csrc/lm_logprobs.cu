@@ -432,7 +432,7 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
             RowPart all = sh.warp_part[turn][lane & (kWarps - 1)];
             all.join_lanes<kWarps, true>(a.c);
             if (all.s == 0.0f && all.xmax > minus_inf()) {
-                all = low_part(row, u0, u1, all.xmax, a.c, [](uint32_t, uint32_t) { return true; });
+                all = low_part(row, u0, 32, u1, all.xmax, a.c, [](uint32_t, uint32_t) { return true; });
             }
             if (kCluster) {
                 if (lane < ctas) push_remote(remote_smem(&pushed[rank], lane), all.xmax, all.s, all.st, 0.0f, remote_smem(&joined, lane));

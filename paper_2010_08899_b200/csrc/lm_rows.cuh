@@ -260,12 +260,12 @@ struct RowPart {
     }
 };
 
-// The part of a row whose values are so low that x c overflows (the type's lowest value in every column that counts): from
-// differences, by every warp on its own.  keep(u, i): whether element i of unit u counts.
+// One warp's share of the part of a row whose values are so low that x c overflows (the type's lowest value in every column that
+// counts), from differences: the units first + lane, `step` on, below u1.  keep(u, i): whether element i of unit u counts.
 template <typename T, typename Keep>
-__device__ __noinline__ RowPart low_part(const RowView<T> row, uint32_t u0, uint32_t u1, float xmax, float c, const Keep keep) {
+__device__ __noinline__ RowPart low_part(const RowView<T> row, uint32_t first, uint32_t step, uint32_t u1, float xmax, float c, const Keep keep) {
     RowPart p{xmax, 0.0f, 0.0f};
-    for (uint32_t u = u0 + lane_id(); u < u1; u += 32) {
+    for (uint32_t u = first + lane_id(); u < u1; u += step) {
         const uint4 v = ld_unit(row.base + u);
 #pragma unroll
         for (uint32_t i = 0; i < Unit<T>::kElems; ++i)
