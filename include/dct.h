@@ -642,9 +642,11 @@ DCT_API dct_status_t dct_layer_norm_bwd(
  *              treated like a negative one), or DCT_ERR_TIMEOUT if a bounded wait between the CTAs of a row gave up (not
  *              seen in practice; that row's numbers are NaN).  With NULL no extra work is enqueued for it.
  * 1 <= vocab <= DCT_LM_MAX_VOCAB; rows may be 0; inv_temperature is finite and > 0.
- * z has to stay within fp32's range.  A masked column holds -inf (log p = -inf, no weight anywhere) or the type's lowest
- * value.  A row that is -inf throughout has no distribution: m = -inf, s = 0, log p = -inf, entropy 0.  A row with a NaN
- * or +inf gets NaN for all of its computed values; its top_ids are still in order, NaN after everything else.
+ * z has to stay within fp32's range; in a row whose largest |z| is 2^26 or more it is the product rounded to fp32, otherwise the
+ * exact one.  A masked column holds -inf (log p = -inf, no weight anywhere) or a value far below the rest (-1e9, the type's
+ * lowest); a row that holds nothing but one such value is uniform.  A row that is -inf throughout has no distribution:
+ * m = -inf, s = 0, log p = -inf, entropy 0.  A row with a NaN or +inf gets NaN for all of its computed values; its top_ids are
+ * still in order, NaN after everything else.
  * Sums are fp32, in a fixed order for given sizes and alignment (any width, stride and address; rows on 16-byte
  * boundaries are the fast case).  Columns outside the row that share a 16-byte unit with its ends may be read, never
  * used.

@@ -8,7 +8,7 @@ constexpr uint32_t kMaxCluster = 8u;
 
 struct DistillArgs {
     uint32_t rows, vocab, ld;
-    float inv_t, c;                 // 1 / T and log2 e / T
+    Scale by;
     const int32_t* ids;
     const float* lps;
     uint32_t top;
@@ -122,7 +122,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         const uint32_t u0 = slice.u0, u1 = slice.u1;
         const int32_t* ids = ids_by_turn + turn * a.top;
         const float* t_s = t_by_turn + turn * a.top;
-        const float scale = __fmul_rn(a.grad_loss ? __ldg(a.grad_loss + row_id) : 1.0f, a.inv_t);
+        const float scale = __fmul_rn(a.grad_loss ? __ldg(a.grad_loss + row_id) : 1.0f, a.by.inv_t);
         copy_wait<0>();
         __syncthreads();                                   // the last row's marks are gone, its numbers are read
 
@@ -219,10 +219,10 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             }
             const float best = fmaxf(Unit<T>::best(v[0], v[2]), Unit<T>::best(v[1], v[3]));
             x_best = fmaxf(x_best, best);
-            sums.add<T, false>(v, best, a.c);
+            sums.add<T, false>(v, best, a.by.c);
         }
         if (kTail && kStaged && grad) fence_proxy_async_smem();      // the next row's copies come after what was written to `stage`
-        const RowPart mine = sums.part<false>(warp_max(x_best), a.c);
+        const RowPart mine = sums.part<false>(warp_max(x_best), a.by.c);
 
         // the slots: the teacher's values, and (kTail) the student's at the slice's named columns, each column once
         copy_wait<1>();
@@ -243,7 +243,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             for (uint32_t i = tid; i < a.top; i += kThreads) {
                 if (!inside(i)) continue;
                 q_sum += expf(t_s[i]);
-                if (in_slice(i) && (!repeated || first_of_its_column(i))) add_value(named, __fmul_rn(logit(i), a.inv_t));
+                if (in_slice(i) && (!repeated || first_of_its_column(i))) add_value(named, __fmul_rn(logit(i), a.by.inv_t));
             }
             q_sum = warp_join<SumOp>(q_sum);
             named.join_lanes<32, false>(kLog2E);
@@ -259,11 +259,11 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
 
         // every warp joins the parts of all
         RowPart student = student_parts[lane & (kWarps - 1)];
-        student.join_lanes<kWarps, false>(a.c);
+        student.join_lanes<kWarps, false>(a.by.c);
         // (the same for the whole CTA.  The warps read the slice again, a share each, and no warp goes on to write a gradient, which may
         // take the logits' place, before all have read theirs)
-        if (student.s == 0.0f && student.xmax > minus_inf()) {
-            const RowPart share = low_part(row, u0 + warp * 32, kThreads, u1, student.xmax, a.c, [=](uint32_t u, uint32_t i) {
+        if (student.xmax > minus_inf() && far_off(__fmul_rn(student.xmax, a.by.inv_t))) {
+            const RowPart share = far_part(row, u0 + warp * 32, kThreads, u1, student.xmax, a.by, [=](uint32_t u, uint32_t i) {
                 const uint32_t at = (u - u0) * E + i;
                 return !kTail || !(marks[at >> 5] >> (at & 31) & 1u);
             });
@@ -271,7 +271,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             if (lane == 0) student_parts[warp] = share;
             __syncthreads();
             student = student_parts[lane & (kWarps - 1)];
-            student.join_lanes<kWarps, false>(a.c);
+            student.join_lanes<kWarps, false>(a.by.c);
         }
         if (kTail) {
             named = named_parts[lane & (kWarps - 1)];
@@ -302,7 +302,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                 named.xmax = of.z;
                 named.s = of.w;
             }
-            student.join_lanes<kMaxCluster, false>(a.c);
+            student.join_slices<kMaxCluster, false>(a.by);
             if (kTail) named.join_lanes<kMaxCluster, false>(kLog2E);
         }
         // the norm of the teacher's values: the warps that have slots find it for themselves
@@ -317,8 +317,8 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         const bool no_teacher = !kTail && !weight_flag && !nan_flag;
 
         // log Z = z_max + log_total; the streamed columns' share p_streamed of the student's distribution (1 unless kTail)
-        const float z_streamed = __fmul_rn(student.xmax, a.inv_t), exact_rest = fmaf(student.xmax, a.inv_t, -z_streamed);
-        float z_max = z_streamed, log_total = logf(student.s) + (student.xmax > minus_inf() ? exact_rest : 0.0f);
+        const float z_streamed = __fmul_rn(student.xmax, a.by.inv_t);
+        float z_max = z_streamed, log_total = logf(student.s) + beyond_max(student.xmax, a.by.inv_t, z_streamed);
         float log_streamed = 0.0f, q_rest = 0.0f, log_norm = 0.0f;
         if (kTail) {
             const float log_s = log_total;
@@ -334,7 +334,10 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         const bool broken = log_total != log_total || nan_flag || gave_up;
         const bool nothing = (!broken && z_max == minus_inf()) || no_teacher;
         const bool remainder = kTail && student.s != 0.0f;
-        auto log_p = [&](uint32_t i) { return fmaf(logit(i), a.inv_t, -z_max) - log_total; };
+        const bool far = far_off(z_max);
+        auto log_p = [&](uint32_t i) {                     // (as less_max: a row without a number is not asked for its log p)
+            return (far ? __fadd_rn(__fmul_rn(logit(i), a.by.inv_t), -z_max) : fmaf(logit(i), a.by.inv_t, -z_max)) - log_total;
+        };
         auto log_q = [&](uint32_t i) { return t_s[i] - log_norm; };
 
         if (a.loss_out && rank == 0) {
@@ -399,8 +402,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                     }
                 }
             };
-            const float ref = __fmul_rn(student.xmax, a.c);
-            const uint64_t by_c = pack2(a.c, a.c);
+            const float ref = __fmul_rn(student.xmax, a.by.c);
             // (a named column may be far above the others, whose factor this is: it is written again below; staged, it is -inf by now)
             auto powers = [&](uint64_t y) {
                 float y0, y1;
@@ -409,15 +411,32 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             };
             if (nothing) {                                 // whatever the logits are
                 write_chunks([](uint64_t) { return 0ull; });
-            } else if (fabsf(ref) <= 3.0e38f) {
+            } else if (!far_off(z_streamed)) {
                 // x c - ref instead of (x - xmax) c, what xmax c is off ref by goes into the factor
-                factor *= exp2_fast(-fmaf(student.xmax, a.c, -ref));
-                const uint64_t shift = pack2(-ref, -ref), by_factor = pack2(factor, factor);
+                factor *= exp2_fast(-fmaf(student.xmax, a.by.c, -ref));
+                const uint64_t by_c = pack2(a.by.c, a.by.c), shift = pack2(-ref, -ref), by_factor = pack2(factor, factor);
                 write_chunks([&](uint64_t x) { return mul2(powers(fma2(x, by_c, shift)), by_factor); });
-            } else {                                       // values whose product with c overflows, or none but -inf
-                const float x_ref = student.xmax == minus_inf() ? 0.0f : -student.xmax;
-                const uint64_t shift = pack2(x_ref, x_ref), by_factor = pack2(factor, factor);
-                write_chunks([&](uint64_t x) { return mul2(powers(mul2(add2(x, shift), by_c)), by_factor); });
+            } else {                                       // (or none but -inf)
+                // (rare: one unit after the other, to keep it out of the other rows' registers)
+                const float less = z_streamed == minus_inf() ? 0.0f : -z_streamed;
+                for (uint32_t k = warp; u0 + k * kChunkUnits < u1; k += kWarps) {
+#pragma unroll 1
+                    for (uint32_t i = lane; i < kChunkUnits && u0 + k * kChunkUnits + i < u1; i += 32) {
+                        const uint32_t u = u0 + k * kChunkUnits + i;
+                        const uint4 unit = kStaged ? stage[k * kChunkUnits + i] : ld_unit(row.base + u);
+                        float g[E];
+#pragma unroll
+                        for (uint32_t e = 0; e < E; ++e) {
+                            const float y = __fmul_rn(__fadd_rn(__fmul_rn(Unit<T>::get(unit, e), a.by.inv_t), less), kLog2E);
+                            g[e] = __fmul_rn(exp2_fast(kTail && !kStaged ? fminf(y, 64.0f) : y), factor);
+                        }
+                        store_unit(row, out, u, g, aligned);
+                    }
+                    if (kStaged) {
+                        __syncwarp();
+                        if (more) fetch_chunk(next_row, next_slice, k);
+                    }
+                }
             }
         }
         // (a row may have a chunk more than the one before it)
@@ -541,7 +560,7 @@ extern "C" dct_status_t dct_lm_distill(const void* logits, dct_dtype_t dtype, ui
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     if (result) DCT_CUDA_TRY(cudaMemsetAsync(result, 0, sizeof(dct_result_t), stream));
     if (rows == 0) return DCT_OK;
-    const DistillArgs args{rows, vocab, ld, inv_temperature, log2_scale(inv_temperature), teacher_ids, teacher_logprobs, top,
+    const DistillArgs args{rows, vocab, ld, Scale{inv_temperature, log2_scale(inv_temperature)}, teacher_ids, teacher_logprobs, top,
                            grad_loss, loss_out, ld_grad, 0, 0, 0, result};
     auto launch = dtype == DCT_F32
         ? (mode == DCT_DISTILL_TAIL ? launch_distill<float, true> : launch_distill<float, false>)

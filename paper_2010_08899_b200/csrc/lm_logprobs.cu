@@ -9,7 +9,7 @@ constexpr uint32_t kRankable = 512u;          // the most columns the selection 
 
 struct LogProbArgs {
     uint32_t rows, vocab, ld;
-    float inv_t, c;                 // 1 / T and log2 e / T
+    Scale by;
     const int32_t* tokens;
     uint32_t top;
     float *logprob_out, *entropy_out, *stats_out;
@@ -321,16 +321,16 @@ template <typename T, uint32_t kThreads> struct Selector {
 // none of the row's).
 __device__ __forceinline__ void write_row(const LogProbArgs& a, uint32_t row_id, float x, int32_t tok, const RowPart& all,
                                           float& m_out, float& logsum_out) {
-    const float m = __fmul_rn(all.xmax, a.inv_t);
+    const float m = __fmul_rn(all.xmax, a.by.inv_t);
     const bool empty = m == minus_inf() && all.s == all.s;
     // (s belongs to the exact product xmax / T: the rounding of m goes into the logarithm)
-    const float log_s = logf(all.s), logsum = empty ? 0.0f : log_s + fmaf(all.xmax, a.inv_t, -m);
+    const float log_s = logf(all.s), logsum = empty ? 0.0f : log_s + beyond_max(all.xmax, a.by.inv_t, m);
     m_out = m;
     logsum_out = logsum;
     if (a.tokens) {
         float lp = 0.0f;
         if (tok >= 0 && static_cast<uint32_t>(tok) < a.vocab) {
-            lp = fmaf(x, a.inv_t, m == minus_inf() ? 0.0f : -m) - logsum;
+            lp = less_max(x, a.by.inv_t, m) - logsum;
         } else if (tok >= 0 && a.result) {
             atomicMax(&a.result->status, static_cast<uint32_t>(DCT_ERR_BAD_MASK));
         }
@@ -390,7 +390,7 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
         uint32_t in_group = 1u << group_shift, slot = tid;
         stream_units<T, kThreads>(row, u0, u1, [&](const uint4 (&v)[4], uint32_t) {
             const float best0 = Unit<T>::best(v[0], v[2]), best1 = Unit<T>::best(v[1], v[3]), best = fmaxf(best0, best1);
-            sums.add<T, true>(v, best, a.c);
+            sums.add<T, true>(v, best, a.by.c);
             max0 = fmaxf(max0, best0);
             max1 = fmaxf(max1, best1);
             if (group_shift == 0) {                                  // the same for the whole CTA
@@ -411,7 +411,7 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
             sh.class_max[tid] = max0;
             sh.class_max[kThreads + tid] = max1;
         }
-        const RowPart mine = sums.part<true>(warp_max(fmaxf(max0, max1)), a.c);
+        const RowPart mine = sums.part<true>(warp_max(fmaxf(max0, max1)), a.by.c);
         if (lane == 0) sh.warp_part[turn][warp] = mine;
         __syncthreads();
 
@@ -430,10 +430,9 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
         // for the bound of the selection
         if (warp == kWarps - 1) {
             RowPart all = sh.warp_part[turn][lane & (kWarps - 1)];
-            all.join_lanes<kWarps, true>(a.c);
-            if (all.s == 0.0f && all.xmax > minus_inf()) {
-                all = low_part(row, u0, 32, u1, all.xmax, a.c, [](uint32_t, uint32_t) { return true; });
-            }
+            all.join_lanes<kWarps, true>(a.by.c);
+            if (all.xmax > minus_inf() && far_off(__fmul_rn(all.xmax, a.by.inv_t)))
+                all = far_part(row, u0, 32, u1, all.xmax, a.by, [](uint32_t, uint32_t) { return true; });
             if (kCluster) {
                 if (lane < ctas) push_remote(remote_smem(&pushed[rank], lane), all.xmax, all.s, all.st, 0.0f, remote_smem(&joined, lane));
             } else if (lane == 0) {
@@ -463,7 +462,7 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
                     const float4 of = pushed[c];
                     all = RowPart{of.x, sh.gave_up ? __uint_as_float(0x7FFFFFFFu) : of.y, of.z};
                 }
-                all.join_lanes<kMaxCluster, true>(a.c);
+                all.join_slices<kMaxCluster, true>(a.by);
                 if (lane == 0) {
                     LogProbArgs mine = a;
                     if (rank != 0) {
@@ -496,8 +495,7 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
             if (place < a.top) {
                 const size_t at = static_cast<size_t>(row_id) * a.top + place;
                 a.top_ids[at] = static_cast<int32_t>(0xFFFFFFFFu - static_cast<uint32_t>(key));
-                a.top_logprobs[at] = fmaf(value_of_key(static_cast<uint32_t>(key >> 32)), a.inv_t,
-                                          sh.m == minus_inf() ? 0.0f : -sh.m) - sh.logsum;
+                a.top_logprobs[at] = less_max(value_of_key(static_cast<uint32_t>(key >> 32)), a.by.inv_t, sh.m) - sh.logsum;
             }
         }
         // (No barrier: the warps' parts alternate, and what else the next row writes it writes behind its first barrier.)
@@ -549,6 +547,9 @@ lm_logprobs_bwd_kernel(const T* logits, T* grad, const LogProbBwdArgs q) {
         const float a = asked ? q.grad_logprob[row_id] : 0.0f;
         const float c = q.grad_entropy ? q.grad_entropy[row_id] : 0.0f, h = q.grad_entropy ? q.entropy[row_id] : 0.0f;
         const uint32_t tok_at = asked ? static_cast<uint32_t>(tok) + row.lead : 0xFFFFFFFFu;
+        // z - m as the forward call forms it: the product with 1 / T by the fma, or (rows far off) rounded before it; the other factor is 1
+        const float before = far_off(ref) ? q.inv_t : 1.0f, within = far_off(ref) ? 1.0f : q.inv_t;
+        const uint64_t first_scale = pack2(before, before), then_scale = pack2(within, within);
         const uint64_t scale = pack2(q.inv_t, q.inv_t), shift = pack2(-ref, -ref), less = pack2(-logsum, -logsum);
         const uint64_t to_log2 = pack2(kLog2E, kLog2E), plus = pack2(h, h), minus_c = pack2(-c, -c), minus_a = pack2(-a, -a);
 #pragma unroll
@@ -559,7 +560,8 @@ lm_logprobs_bwd_kernel(const T* logits, T* grad, const LogProbBwdArgs q) {
 #pragma unroll
             for (uint32_t e = 0; e < E; e += 2) {
                 float l0, l1, y0, y1;
-                unpack2(add2(fma2(pack2(Unit<T>::get(v[i], e), Unit<T>::get(v[i], e + 1)), scale, shift), less), l0, l1);
+                const uint64_t x = mul2(pack2(Unit<T>::get(v[i], e), Unit<T>::get(v[i], e + 1)), first_scale);
+                unpack2(add2(fma2(x, then_scale, shift), less), l0, l1);
                 // (a column without weight: its log p may be -inf, and 0 * -inf is not 0)
                 const uint64_t lp = pack2(max_nan(l0, -1.0e4f), max_nan(l1, -1.0e4f));
                 unpack2(mul2(lp, to_log2), y0, y1);
@@ -666,7 +668,7 @@ extern "C" dct_status_t dct_lm_logprobs_fwd(const void* logits, dct_dtype_t dtyp
     }
     if (result) DCT_CUDA_TRY(cudaMemsetAsync(result, 0, sizeof(dct_result_t), stream));
     if (rows == 0) return DCT_OK;
-    const LogProbArgs args{rows, vocab, ld, inv_temperature, log2_scale(inv_temperature), tokens, top, logprob_out, entropy_out, stats_out, top_ids, top_logprobs, result,
+    const LogProbArgs args{rows, vocab, ld, Scale{inv_temperature, log2_scale(inv_temperature)}, tokens, top, logprob_out, entropy_out, stats_out, top_ids, top_logprobs, result,
                            debug_config().spin_limit};
     return dtype == DCT_F32 ? launch_logprobs<float>(logits, args, stream) : launch_logprobs<__nv_bfloat16>(logits, args, stream);
 }

@@ -232,58 +232,90 @@ __device__ __forceinline__ float warp_max(float v) {               // NaN only i
     return r;
 }
 
+// 1 / T and log2 e / T
+struct Scale {
+    float inv_t, c;
+};
+
+// Rows whose largest z = x / T lies 2^26 or more from zero (a mask's value throughout, as a rule) are far off.  The exact z is then up to
+// 2 and more away from the nearest fp32 number, and for the masks in use, -1e9 to the type's lowest value, so far that 2^z
+// relative to that number overflows.  z there is the product rounded to fp32 everywhere: in the largest, in the sums, in log p and in the gradients.
+// Below that, z enters as the exact product (one fma).
+constexpr float kFar = 67108864.0f, kFarLog2 = 2.0f * kFar;          // (kFarLog2 > log2 e kFar)
+__device__ __forceinline__ bool far_off(float z) { return !(fabsf(z) < kFar); }            // infinities and NaN, too
+// z - m; m: the row's largest z, rounded (-inf, a row without a number: z itself)
+__device__ __forceinline__ float less_max(float x, float inv_t, float m) {
+    if (m == minus_inf()) m = 0.0f;
+    return far_off(m) ? __fadd_rn(__fmul_rn(x, inv_t), -m) : fmaf(x, inv_t, -m);
+}
+// what the exact largest z is beyond m
+__device__ __forceinline__ float beyond_max(float xmax, float inv_t, float m) { return far_off(m) ? 0.0f : fmaf(xmax, inv_t, -m); }
+
 // What is known of a part of a row: its largest x, and relative to that the sums s = sum 2^y and st = sum 2^y y with
-// y = (x - xmax) c, c = inv_t log2 e.  st / s is the mean of log2 p + log2 s.  An empty part has xmax = -inf, s = 0.
+// y = (x - xmax) c, c = log2 e / T.  st / s is the mean of log2 p + log2 s.  An empty part has xmax = -inf, s = 0.
 struct RowPart {
     float xmax, s, st;
-    // the same sums relative to a larger x
-    __device__ __forceinline__ void raise(float to, float c) {
+    // the same sums relative to a larger x, which is `apart` (binary powers) above this one
+    __device__ __forceinline__ void raise(float to, float apart) {
         if (s == 0.0f) {
             st = 0.0f;
         } else {
-            // (the type's lowest values are too far off for s * d; from -1e4 on the factor is 0 all the same)
-            const float d = xmax == to ? 0.0f : max_nan(__fmul_rn(__fadd_rn(xmax, -to), c), -1.0e4f), f = exp2_fast(d);
+            // (from -1e4 on the factor is 0, and no difference may be so large that s * d overflows)
+            const float d = xmax == to ? 0.0f : max_nan(apart, -1.0e4f), f = exp2_fast(d);
             st = __fmul_rn(f, fmaf(s, d, st));
             s = __fmul_rn(f, s);
         }
         xmax = to;
     }
-    // joins the parts of kLanes (a power of two) neighbouring lanes, in a fixed order; all lanes get the result.  (Every group of
-    // kLanes lanes holds the same parts, so the warp's largest x is the group's.)
-    template <int kLanes, bool kMoment> __device__ __forceinline__ void join_lanes(float c) {
-        raise(kLanes == 1 ? xmax : warp_max(xmax), c);
+    template <int kLanes, bool kMoment> __device__ __forceinline__ void add_lanes() {
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o >>= 1) {
             s = __fadd_rn(s, __shfl_xor_sync(0xFFFFFFFFu, s, o));
             if (kMoment) st = __fadd_rn(st, __shfl_xor_sync(0xFFFFFFFFu, st, o));
         }
     }
+    // joins the parts of kLanes (a power of two) neighbouring lanes, in a fixed order; all lanes get the result.  (Every group of
+    // kLanes lanes holds the same parts, so the warp's largest x is the group's.)
+    template <int kLanes, bool kMoment> __device__ __forceinline__ void join_lanes(float c) {
+        const float to = kLanes == 1 ? xmax : warp_max(xmax);
+        raise(to, __fmul_rn(__fadd_rn(xmax, -to), c));
+        add_lanes<kLanes, kMoment>();
+    }
+    // the same for whole slices of a row, each summed as its own largest x asks for
+    template <int kLanes, bool kMoment> __device__ __forceinline__ void join_slices(const Scale& by) {
+        const float to = warp_max(xmax), z = __fmul_rn(to, by.inv_t);
+        raise(to, far_off(z) && z > minus_inf() ? __fmul_rn(__fadd_rn(__fmul_rn(xmax, by.inv_t), -z), kLog2E) : __fmul_rn(__fadd_rn(xmax, -to), by.c));
+        add_lanes<kLanes, kMoment>();
+    }
 };
 
-// One warp's share of the part of a row whose values are so low that x c overflows (the type's lowest value in every column that
-// counts), from differences: the units first + lane, `step` on, below u1.  keep(u, i): whether element i of unit u counts.
+// One warp's share of the part of a row whose largest z is far off, from z as rounded: the units first + lane, `step` on, below u1.
+// keep(u, i): whether element i of unit u counts.
 template <typename T, typename Keep>
-__device__ __noinline__ RowPart low_part(const RowView<T> row, uint32_t first, uint32_t step, uint32_t u1, float xmax, float c, const Keep keep) {
+__device__ __noinline__ RowPart far_part(const RowView<T> row, uint32_t first, uint32_t step, uint32_t u1, float xmax, const Scale by, const Keep keep) {
     RowPart p{xmax, 0.0f, 0.0f};
+    const float m = __fmul_rn(xmax, by.inv_t), less = m == minus_inf() ? 0.0f : -m;
     for (uint32_t u = first + lane_id(); u < u1; u += step) {
         const uint4 v = ld_unit(row.base + u);
 #pragma unroll
         for (uint32_t i = 0; i < Unit<T>::kElems; ++i)
             if (row.column(u, i) < row.width && keep(u, i)) {
-                const float y = __fmul_rn(__fadd_rn(Unit<T>::get(v, i), -xmax), c), e = exp2_fast(y);
+                const float y = __fmul_rn(__fadd_rn(__fmul_rn(Unit<T>::get(v, i), by.inv_t), less), kLog2E), e = exp2_fast(y);
                 p.s = __fadd_rn(p.s, e);
                 if (e != 0.0f) p.st = fmaf(e, y, p.st);
             }
     }
     __syncwarp();
-    p.join_lanes<32, true>(c);
+    p.join_lanes<32, true>(by.c);          // (alike in their xmax)
     return p;
 }
 
 // One thread's share of sum 2^y and sum 2^y y over a row, y = x c - ref.  The reference is the warp's: the largest x c of its
 // first batch, replaced only when a batch exceeds it by kSlack, so that an element costs one product-sum, one power of
 // two and two sums.  Rounding c and ref moves nothing but the reference: what counts is (x - xmax) c, and the
-// distance of xmax c to ref is formed by one fma at the end.
+// distance of xmax c to ref is formed by one fma at the end.  A reference is below kFarLog2 in size, so that no y exceeds kSlack by more
+// than the 4 its rounding can be off.  Batches whose largest x is further down add nothing; where it is all the row has, or
+// where there is one further up, the row is far off and these sums are not used.
 struct RowSums {
     static constexpr float kSlack = 4.0f;
     float ref, s, st;
@@ -318,7 +350,7 @@ struct RowSums {
     template <typename T, bool kMoment> __device__ __forceinline__ void add(const uint4 (&v)[4], float best, float c) {
         if (__any_sync(0xFFFFFFFFu, !(__fmul_rn(best, c) <= __fadd_rn(ref, kSlack)))) {
             const float to = __fmul_rn(warp_max(best), c);
-            if (to > ref) {
+            if (to > ref && fabsf(to) < kFarLog2) {
                 if (ref != minus_inf()) {
                     const float d = max_nan(__fadd_rn(ref, -to), -1.0e4f), f = exp2_fast(d);
                     st = __fmul_rn(f, fmaf(s, d, st));
@@ -327,7 +359,7 @@ struct RowSums {
                 ref = to;
             }
         }
-        if (ref == minus_inf()) {        // nothing but -inf and NaN so far (or values whose product with c overflows)
+        if (ref == minus_inf()) {        // nothing but -inf, NaN and values far off so far
             float any = 0.0f;
 #pragma unroll
             for (int u = 0; u < 4; ++u)
@@ -353,7 +385,7 @@ struct RowSums {
     template <bool kMoment> __device__ __forceinline__ RowPart part(float xmax, float c) const {
         RowPart r{xmax, warp_join<SumOp>(s), kMoment ? warp_join<SumOp>(st) : 0.0f};
         if (ref != minus_inf()) {
-            // |xmax c - ref| <= kSlack; the factor puts the sums where 2^y of the largest x is 1
+            // |xmax c - ref| <= kSlack + 4; the factor puts the sums where 2^y of the largest x is 1
             const float d = fmaf(xmax, c, -ref), f = exp2_fast(-d);
             r.st = __fmul_rn(f, fmaf(-d, r.s, r.st));
             r.s = __fmul_rn(f, r.s);

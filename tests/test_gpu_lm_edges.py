@@ -7,7 +7,8 @@ import torch
 from oracle import lm
 from paper_2010_08899_b200 import binding as B
 
-from .test_gpu_lm import DEV, DT, U, chain, close, f64, half_step, teacher_of, vec
+from . import test_gpu_lm as base
+from .test_gpu_lm import DEV, DT, U, chain, check_distill, check_logprobs, close, f64, half_step, logits, vec
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +50,116 @@ def test_distill_of_lowest_rows_in_place(dtype, vocab, rows, top, tail):
     q = np.zeros((rows, vocab))
     np.put_along_axis(q, ids.numpy().astype(np.int64), np.exp(f64(t)), 1)
     close(f64(apart).reshape(rows, vocab)[even], o.grad, c * (4 / vocab + 4 * q[even]) + half_step(dt) * 1.01 * np.abs(o.grad))
+
+
+def masked_rows(rows, vocab, fill, dt, seed):
+    """Logits masked by a finite value in several manners, row by row in turn, and which rows hold nothing above it."""
+    x, _ = logits(rows, vocab, seed, dt)
+    fill = torch.tensor(fill).to(dt)
+    col = torch.arange(vocab)
+    gen = torch.Generator().manual_seed(seed + 1)
+    for i in range(rows):
+        kind = i % 7
+        if kind == 0:
+            x[i] = fill                                                      # throughout
+        elif kind == 1:
+            x[i, :vocab // 2] = fill                                         # what is read first
+        elif kind == 2:
+            x[i, :vocab - 2] = fill                                          # all but the last two
+        elif kind == 3:
+            x[i, 2:] = fill
+        elif kind == 4:
+            x[i] = torch.where((torch.rand(vocab, generator=gen) < 0.1) | (col == 1), x[i], fill)
+        elif kind == 5:
+            x[i] = torch.where(col % 3 == 0, fill, torch.tensor(float("-inf"), dtype=dt))      # a mask upon a mask
+        else:
+            x[i, vocab // 3:] = fill
+    return x, torch.tensor([i % 7 in (0, 5) for i in range(rows)])
+
+
+def from_their_largest(x):
+    """The same distributions with the rows' largest value at 0 where it is far off."""
+    top = x.max(axis=1, keepdims=True)
+    with np.errstate(invalid="ignore"):
+        return np.where(np.isfinite(top) & (top < -1e9), x - top, x)
+
+
+FILLS = ["lowest", -1e10, -1e30]
+FAR_SHAPES = [(7, 70, 7), (210, 1000, 20), (420, 4099, 9), (7, 40003, 20), (7, 200001, 5)]
+
+
+@pytest.mark.parametrize("rows,vocab,top", FAR_SHAPES)
+@pytest.mark.parametrize("inv_t", [1.0, 0.5, 0.6])
+@pytest.mark.parametrize("fill", FILLS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logprobs_of_finite_masks(dtype, fill, inv_t, rows, vocab, top):
+    dt = DT[dtype]
+    x, whole = masked_rows(rows, vocab, torch.finfo(dt).min if fill == "lowest" else fill, dt, vocab)
+    tokens = torch.arange(rows, dtype=torch.int32) * 7919 % vocab
+    tokens[whole] -= tokens[whole] % 3                                       # (a column that the mask upon the mask leaves)
+    flat, stats, ent, _ = check_logprobs(x, inv_t, tokens, top, vocab, 0, dt)
+    # rows that the mask covers, against the uniform distribution they are
+    lp, ids, tlp = vec(rows), vec(rows * top, torch.int32), vec(rows * top)
+    B.dct_lm_logprobs_fwd(flat, rows, vocab, vocab, inv_t, tokens.to(DEV), top, lp, None, None, ids, tlp)
+    inv, w = float(np.float32(inv_t)), whole.numpy()
+    xs = from_their_largest(f64(x))
+    o = lm.log_probs(xs, inv)
+    c = U * (64 + chain(vocab))
+    tol = c * (1 + np.abs(o.logsum))[w]
+    want = o.logp[np.arange(rows), tokens.numpy()]
+    close(f64(lp[:rows])[w], want[w], tol + 8 * U * np.abs(want[w]))
+    close(f64(ent)[w], o.entropy[w], (c + 16 * U) * (12 + o.entropy[w]))
+    st = f64(stats).reshape(rows, 2)
+    close(st[w, 1], o.logsum[w], tol)
+    at = ids[:rows * top].cpu().numpy().reshape(rows, top).astype(np.int64)
+    best = np.take_along_axis(o.logp, at, 1)
+    size = np.where(np.isfinite(best), np.abs(best), 0.0)
+    close(f64(tlp[:rows * top]).reshape(rows, top)[w], best[w], tol[:, None] + 8 * U * size[w])
+
+    gen = torch.Generator().manual_seed(3)
+    a, b = torch.randn(rows, generator=gen), torch.randn(rows, generator=gen)
+    g = torch.empty(rows * vocab, dtype=dt, device=DEV)
+    B.dct_lm_logprobs_bwd(flat, rows, vocab, vocab, inv_t, tokens.to(DEV), stats, ent, a.to(DEV), b.to(DEV), g, vocab)
+    m = np.where(w, 0.0, st[:, 0])
+    want = lm.log_probs_bwd(xs, inv, tokens.numpy(), m, st[:, 1], f64(ent), f64(a), f64(b))
+    with np.errstate(invalid="ignore"):
+        lpx = np.maximum(xs * inv - m[:, None] - st[:, 1:], -1e4)
+    p = np.exp(lpx)
+    rel = U * (32 + 8 * np.abs(lpx) + 4 * (np.abs(m) + np.abs(st[:, 1]))[:, None])
+    tol = inv * rel * p * (np.abs(f64(a)) + np.abs(f64(b)))[:, None] * (1 + np.abs(lpx) + f64(ent)[:, None]) + half_step(dt) * np.abs(want) * 1.01
+    tol[np.arange(rows), tokens.numpy()] += inv * 4 * U * np.abs(f64(a))
+    close(f64(g).reshape(rows, vocab), want, tol + 1e-37)
+
+
+def check_distill_of_masked(dtype, fill, inv_t, rows, vocab, top, tail, monkeypatch):
+    """check_distill with the oracle given the far rows from their largest value on: the same distributions, with tolerances that
+    do not grow with the mask."""
+    dt = DT[dtype]
+    x, _ = masked_rows(rows, vocab, torch.finfo(dt).min if fill == "lowest" else fill, dt, vocab + 5)
+    gen = torch.Generator().manual_seed(13)
+    ids = torch.stack([torch.randperm(vocab - 2, generator=gen)[:top] for _ in range(rows)]).to(torch.int32) + 1
+    ids[torch.arange(rows) % 7 == 5] = ids[torch.arange(rows) % 7 == 5] // 3 * 3      # (named twice or more, some of them)
+    t = torch.log_softmax(2.0 * torch.randn(rows, top, generator=gen), 1) - 0.25
+    distill, log_probs = lm.distill, lm.log_probs
+    monkeypatch.setattr(lm, "distill", lambda z, *rest: distill(from_their_largest(z), *rest))
+    monkeypatch.setattr(lm, "log_probs", lambda z, *rest: log_probs(from_their_largest(z), *rest))
+    # (a teacher whose whole mass lies on columns at fp32's lowest value: the exact loss is fp32's largest number, and a sum that is
+    # within its tolerance may round to infinity)
+    most = float(np.finfo(np.float32).max)
+    monkeypatch.setattr(base, "close", lambda got, want, tol: close(np.where(np.isposinf(got) & np.isfinite(want) & (want + tol >= most), most, got), want, tol))
+    check_distill(x, inv_t, ids, t, tail, torch.rand(rows, generator=gen) + 0.5, vocab, 0, dt)
+
+
+@pytest.mark.parametrize("rows,vocab,top", FAR_SHAPES)
+@pytest.mark.parametrize("inv_t", [1.0, 0.5, 0.6])
+@pytest.mark.parametrize("fill", FILLS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill_of_finite_masks(dtype, fill, inv_t, rows, vocab, top, tail, monkeypatch):
+    check_distill_of_masked(dtype, fill, inv_t, rows, vocab, top, tail, monkeypatch)
+
+
+@pytest.mark.parametrize("fill", FILLS)
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill_of_finite_masks_in_rows_loaded_twice(fill, tail, monkeypatch):
+    check_distill_of_masked("bf16", fill, 0.6, 230, 32768, 1024, tail, monkeypatch)
