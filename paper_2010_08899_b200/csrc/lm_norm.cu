@@ -17,6 +17,7 @@ namespace {
 constexpr uint32_t kNormMaxWidth = 65536u;
 constexpr uint32_t kNormThreads = 256u;
 constexpr uint32_t kMaxParts = 148u * 6u;        // CTAs that leave partial sums of the parameter gradients, at most
+constexpr size_t kMostShared = 226 * 1024;       // dynamic shared memory a CTA may ask for: 227 KiB less what it holds statically
 
 // Rows as units of 16 bytes counted from the row's own first element.  Where a row does not start on a 16-byte boundary, a unit is
 // put together from the two aligned pieces it lies in; these are inside the row but for the bytes next to its ends, which share
@@ -520,6 +521,11 @@ template <typename P, uint32_t kE> struct ParamImage {
 // CTAs of the forward kernel an SM's registers are asked to hold
 template <uint32_t kThreads, uint32_t kUnits> constexpr uint32_t fwd_ctas() { return (kUnits == 4 ? 512 : 1024) / kThreads; }
 
+// shared memory of a CTA of it: the parameters for `all` units; per group its slots and two images of an unaligned y
+template <typename P, uint32_t kE, uint32_t kGroups> constexpr size_t fwd_shared(uint32_t all, uint32_t slot_units, bool whole) {
+    return 16 * (2 * static_cast<size_t>(ParamImage<P, kE>::kPieces) * all + static_cast<size_t>(kGroups) * (kFwdRing + (whole ? 0 : 2)) * slot_units);
+}
+
 template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits, bool kWhole>
 __global__ void __launch_bounds__(kThreads, fwd_ctas<kThreads, kUnits>())
 norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* __restrict__ weight,
@@ -643,8 +649,14 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
 // A group's rows come through a ring of bulk copies (x and dy of a row to a slot); the row is taken into registers, added to
 // the group's columns of the parameter gradients, summed over, and dx is written from the registers while the slot is
 // filled again.
-// (2 / 3 / 4 rows ahead: 73 / 68 / 69 us for 16384 rows of 4096 bf16)
-constexpr uint32_t kRing = 3u;
+// (2 / 3 / 4 rows ahead: 73 / 68 / 69 us for 16384 rows of 4096 bf16.  Rows of more than 16 KiB go two ahead: with three, beside the images
+// that an unaligned dx needs, slots of 32 KiB would not fit a CTA, and where they do, it is slower: 8192 rows of 8192 fp32 133 us with
+// two and 137 with three, of 7000 108 and 118.)
+template <uint32_t kThreads, uint32_t kUnits> constexpr uint32_t kBwdRing = kThreads * kUnits > 1024 ? 2 : 3;
+// shared memory of a backward CTA whose rows span slot_units pieces at most: per group the slots of (x, dy) and two images of an unaligned dx
+template <uint32_t kGroups, uint32_t kThreads, uint32_t kUnits, bool kWhole> constexpr size_t bwd_shared(uint32_t slot_units) {
+    return static_cast<size_t>(kGroups) * (2 * kBwdRing<kThreads, kUnits> + (kWhole ? 0 : 2)) * slot_units * 16;
+}
 // CTAs of the backward kernel an SM's registers are asked to hold
 template <uint32_t kThreads, uint32_t kUnits> constexpr uint32_t bwd_ctas() {
     return kUnits == 1 ? 768 / kThreads : kThreads <= 320 ? 640 / kThreads : 1;
@@ -655,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, bwd_ctas<kThreads, kUnits>())
 norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, uint32_t d, uint32_t ld,
                       const P* __restrict__ weight, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
                       uint32_t ld_dx, float* __restrict__ parts, uint32_t slot_units, float per_column, uint32_t spin_limit) {
-    constexpr uint32_t E = Unit<T>::kElems, kGroups = kGroup ? kThreads / kGroup : 1;
+    constexpr uint32_t E = Unit<T>::kElems, kGroups = kGroup ? kThreads / kGroup : 1, kRing = kBwdRing<kThreads, kUnits>;
     extern __shared__ __align__(128) uint4 ring[];        // per group: kRing slots of (x, dy), and two images of an unaligned dx
     __shared__ float slots[128];
     __shared__ uint64_t full[kGroups][kRing];
@@ -962,8 +974,9 @@ dct_status_t launch_fwd_ring(const T* x, uint32_t rows, uint32_t d, uint32_t ld,
     const bool whole = d == E * all && on_boundaries(x, rows, ld, sizeof(T)) && on_boundaries(y, rows, ld_y, sizeof(T));
     auto kernel = whole ? norm_fwd_ring_kernel<T, P, kGroup, kThreads, kUnits, true> : norm_fwd_ring_kernel<T, P, kGroup, kThreads, kUnits, false>;
     const uint32_t slot_units = (d + E - 1) / E + 2;       // (an unaligned row touches one piece more; its image half a word beyond)
-    const size_t smem = 16 * (2 * static_cast<size_t>(ParamImage<P, E>::kPieces) * all +
-                              static_cast<size_t>(kGroups) * (kFwdRing + (whole ? 0 : 2)) * slot_units);
+    const size_t smem = fwd_shared<P, E, kGroups>(all, slot_units, whole);
+    constexpr uint32_t kMostUnits = (kGroup ? kGroup : kThreads) * kUnits;
+    static_assert(fwd_shared<P, E, kGroups>(kMostUnits, kMostUnits + 2, false) <= kMostShared, "a width of this kernel would be refused at launch");
     static std::atomic<uint32_t> allowed[2][64];
     const dct_status_t allowed_st = allow_shared(kernel, smem, allowed[whole]);
     if (allowed_st != DCT_OK) return allowed_st;
@@ -1037,7 +1050,10 @@ dct_status_t launch_bwd_units(const T* dy, uint32_t ld_dy, const T* x, uint32_t 
                        on_boundaries(dy, rows, ld_dy, sizeof(T)) && on_boundaries(dx, rows, ld_dx, sizeof(T));
     auto kernel = whole ? norm_bwd_units_kernel<T, P, kGroup, kThreads, kUnits, true> : norm_bwd_units_kernel<T, P, kGroup, kThreads, kUnits, false>;
     const uint32_t slot_units = (d + E - 1) / E + 2;       // (an unaligned row touches one piece more; its image half a word beyond)
-    const size_t smem = static_cast<size_t>(kGroups) * (2 * kRing + (whole ? 0 : 2)) * slot_units * 16;
+    const size_t smem = whole ? bwd_shared<kGroups, kThreads, kUnits, true>(slot_units) : bwd_shared<kGroups, kThreads, kUnits, false>(slot_units);
+    constexpr uint32_t kMostUnits = (kGroup ? kGroup : kThreads) * kUnits + 2;
+    static_assert(bwd_shared<kGroups, kThreads, kUnits, true>(kMostUnits) <= kMostShared && bwd_shared<kGroups, kThreads, kUnits, false>(kMostUnits) <= kMostShared,
+                  "a width of this kernel would be refused at launch");
     static std::atomic<uint32_t> allowed[2][64];
     const dct_status_t allowed_st = allow_shared(kernel, smem, allowed[whole]);
     if (allowed_st != DCT_OK) return allowed_st;

@@ -163,3 +163,12 @@ def test_distill_of_finite_masks(dtype, fill, inv_t, rows, vocab, top, tail, mon
 @pytest.mark.parametrize("tail", [False, True])
 def test_distill_of_finite_masks_in_rows_loaded_twice(fill, tail, monkeypatch):
     check_distill_of_masked("bf16", fill, 0.6, 230, 32768, 1024, tail, monkeypatch)
+
+
+@pytest.mark.parametrize("rows,d,ld,offset", [(3, 7236, 7236, 0), (3, 7237, 7237, 0), (5, 7500, 7500, 0), (310, 7680, 7680, 0), (4, 7680, 7681, 0),
+                                              (310, 8000, 8000, 0), (4, 8191, 8191, 0), (4, 8192, 8197, 0), (4, 8192, 8192, 1),
+                                              (3, 4097, 4097, 0), (3, 5000, 5001, 1)])
+@pytest.mark.parametrize("dtype,pdtype", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")])
+def test_layer_norm_of_wide_rows_in_a_ring(rows, d, ld, offset, dtype, pdtype):
+    """Widths at which the slots of a CTA come near what it may have of shared memory."""
+    base.test_layer_norm(rows, d, ld, offset, dtype, pdtype)
