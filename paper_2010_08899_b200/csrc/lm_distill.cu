@@ -494,8 +494,8 @@ dct_status_t launch_distill_shape(const void* logits, void* grad, const DistillA
     const T* x = static_cast<const T*>(logits);
     T* g = static_cast<T*>(grad);
     uint32_t at_once = static_cast<uint32_t>(sms) * per_sm;
-    if (kCluster) {
-        static std::atomic<uint32_t> kept[768 / kThreads + 1][3];
+    if (kCluster && cluster > 1) {
+        static ClusterCounts kept[768 / kThreads + 1];
         const dct_status_t st = clusters_at_once(kernel, kThreads, cluster, smem, kept[per_sm], &at_once);
         if (st != DCT_OK) return st;
     }

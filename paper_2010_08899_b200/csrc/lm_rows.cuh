@@ -5,6 +5,7 @@
 #include <cmath>
 
 #include "common.cuh"
+#include "launch_words.h"
 
 namespace dct {
 
@@ -471,15 +472,23 @@ __device__ __forceinline__ void push_remote(uint32_t to, uint64_t x, uint32_t ba
 
 // Host side ---------------------------------------------------------------------------------------------------
 
+// the current device, as an index into what is kept per device
+inline dct_status_t current_device(int* out) {
+    DCT_CUDA_TRY(cudaGetDevice(out));
+    return *out >= 0 && *out < kMaxDevices ? DCT_OK : DCT_ERR_CUDA;
+}
+
 // How many clusters of `cluster` (2, 4 or 8) CTAs the current device holds at a time.  A GPC's SMs are no multiple of a cluster, so
 // this is less than the CTAs that fit divided by the cluster; a persistent grid of more would run its last clusters after
-// all others.  kept: one word per cluster size, zero at first, for launches that differ in nothing that matters here.
+// all others.
 template <typename... Params>
 inline dct_status_t clusters_at_once(void (*kernel)(Params...), unsigned block, unsigned cluster, size_t smem,
-                                     std::atomic<uint32_t> (&kept)[3], uint32_t* out) {
-    std::atomic<uint32_t>& word = kept[cluster == 2 ? 0 : cluster == 4 ? 1 : 2];
-    uint32_t n = word.load(std::memory_order_relaxed);
-    if (n == 0) {
+                                     ClusterCounts& kept, uint32_t* out) {
+    int dev = 0;
+    const dct_status_t st = current_device(&dev);
+    if (st != DCT_OK) return st;
+    cudaError_t error = cudaSuccess;
+    *out = kept.get(dev, cluster, [&]() -> uint32_t {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(cluster);
         cfg.blockDim = dim3(block);
@@ -492,11 +501,10 @@ inline dct_status_t clusters_at_once(void (*kernel)(Params...), unsigned block, 
         cfg.attrs = &shape;
         cfg.numAttrs = 1;
         int found = 0;
-        DCT_CUDA_TRY(cudaOccupancyMaxActiveClusters(&found, kernel, &cfg));
-        n = found > 0 ? static_cast<uint32_t>(found) : 1u;
-        word.store(n, std::memory_order_relaxed);
-    }
-    *out = n;
+        error = cudaOccupancyMaxActiveClusters(&found, kernel, &cfg);
+        return error != cudaSuccess ? 0u : found > 0 ? static_cast<uint32_t>(found) : 1u;
+    });
+    DCT_CUDA_TRY(error);
     return DCT_OK;
 }
 

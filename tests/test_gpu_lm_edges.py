@@ -1,5 +1,8 @@
 """Further edges of the layer norm and of the calls on rows of logits: masks, widths and shapes at which a choice of
 kernel or of arithmetic changes.  Tolerances as in test_gpu_lm.py."""
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -8,6 +11,7 @@ from oracle import lm
 from paper_2010_08899_b200 import binding as B
 
 from . import test_gpu_lm as base
+from .conftest import ROOT
 from .test_gpu_lm import DEV, DT, U, chain, check_distill, check_logprobs, close, f64, half_step, logits, vec
 
 pytestmark = pytest.mark.gpu
@@ -172,3 +176,33 @@ def test_distill_of_finite_masks_in_rows_loaded_twice(fill, tail, monkeypatch):
 def test_layer_norm_of_wide_rows_in_a_ring(rows, d, ld, offset, dtype, pdtype):
     """Widths at which the slots of a CTA come near what it may have of shared memory."""
     base.test_layer_norm(rows, d, ld, offset, dtype, pdtype)
+
+
+ORDER = """
+import sys, torch
+from paper_2010_08899_b200 import binding as B
+
+def step(rows, vocab, top, times):
+    x = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
+    ids = torch.arange(rows * top, dtype=torch.int32, device="cuda") % vocab
+    t, loss, g = torch.zeros(rows * top, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(x)
+    ends = [torch.cuda.Event(enable_timing=True) for _ in range(times + 1)]
+    for e in ends:
+        e.record()
+        B.dct_lm_distill(x, rows, vocab, vocab, 1.0, ids, t, top, B.DCT_DISTILL_RENORM, None, loss, g, vocab)
+    torch.cuda.synchronize()
+    took = sorted(a.elapsed_time(b) for a, b in zip(ends[2:], ends[3:]))
+    return took[len(took) // 2]
+
+if sys.argv[1] == "after":
+    step(256, 524288, 64, 3)           # the same kernel with eight CTAs to a row
+print(step(4096, 32768, 1024, 12))
+"""
+
+
+def test_time_of_a_call_does_not_depend_on_the_calls_before():
+    """A persistent grid of one CTA to a row is as large after a call whose rows were split as in a new process (a grid of the other
+    shape's size takes several times as long)."""
+    took = [float(subprocess.run([sys.executable, "-c", ORDER, word], cwd=ROOT, capture_output=True, text=True, check=True, timeout=300).stdout)
+            for word in ("before", "after")]
+    assert took[1] < 1.5 * took[0]
