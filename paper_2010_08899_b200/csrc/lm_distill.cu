@@ -486,7 +486,7 @@ dct_status_t launch_distill_shape(const void* logits, void* grad, const DistillA
     const size_t smem = (kStaged ? static_cast<size_t>(a.chunks) * kChunkBytes : 0) + 4 * static_cast<size_t>(a.mark_words) +
                         20 * static_cast<size_t>(a.top);
     auto kernel = lm_distill_kernel<T, kThreads, kTail, kCluster, kStaged>;
-    static std::atomic<uint32_t> allowed[64];
+    static SharedLimit allowed;
     const dct_status_t allowed_st = allow_shared(kernel, smem, allowed);
     if (allowed_st != DCT_OK) return allowed_st;
     uint32_t per_sm = static_cast<uint32_t>((227 * 1024) / (smem + 3 * 1024));

@@ -583,7 +583,7 @@ dct_status_t launch_logprobs_threads(const void* logits, const LogProbArgs& a, u
     const T* x = static_cast<const T*>(logits);
     if constexpr (kThreads == 256) {
         if (cluster > 1) {
-            static std::atomic<uint32_t> allowed[64];
+            static SharedLimit allowed;
             static ClusterCounts kept[2];
             auto kernel = lm_logprobs_kernel<T, kThreads, true>;
             const bool many = a.top > 128;            // room for the lists: 8 CTAs' of 128 columns leave four CTAs to an SM

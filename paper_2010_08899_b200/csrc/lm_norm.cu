@@ -954,7 +954,7 @@ dct_status_t launch_fwd_units(const T* x, uint32_t rows, uint32_t d, uint32_t ld
     auto kernel = norm_fwd_units_kernel<T, P, kGroup, kThreads, kUnits>;
     // an image only if some row of y does not start on a boundary
     const size_t smem = on_boundaries(y, rows, ld_y, sizeof(T)) ? 0 : static_cast<size_t>(kGroups) * 2 * ((d + E - 1) / E + 2) * 16;
-    static std::atomic<uint32_t> allowed[64];
+    static SharedLimit allowed;
     const dct_status_t allowed_st = allow_shared(kernel, smem, allowed);
     if (allowed_st != DCT_OK) return allowed_st;
     const uint64_t ctas = (static_cast<uint64_t>(rows) + kGroups - 1) / kGroups;
@@ -977,7 +977,7 @@ dct_status_t launch_fwd_ring(const T* x, uint32_t rows, uint32_t d, uint32_t ld,
     const size_t smem = fwd_shared<P, E, kGroups>(all, slot_units, whole);
     constexpr uint32_t kMostUnits = (kGroup ? kGroup : kThreads) * kUnits;
     static_assert(fwd_shared<P, E, kGroups>(kMostUnits, kMostUnits + 2, false) <= kMostShared, "a width of this kernel would be refused at launch");
-    static std::atomic<uint32_t> allowed[2][64];
+    static SharedLimit allowed[2];
     const dct_status_t allowed_st = allow_shared(kernel, smem, allowed[whole]);
     if (allowed_st != DCT_OK) return allowed_st;
     uint32_t per_sm = static_cast<uint32_t>(227 * 1024 / (smem + 2048));
@@ -1054,7 +1054,7 @@ dct_status_t launch_bwd_units(const T* dy, uint32_t ld_dy, const T* x, uint32_t 
     constexpr uint32_t kMostUnits = (kGroup ? kGroup : kThreads) * kUnits + 2;
     static_assert(bwd_shared<kGroups, kThreads, kUnits, true>(kMostUnits) <= kMostShared && bwd_shared<kGroups, kThreads, kUnits, false>(kMostUnits) <= kMostShared,
                   "a width of this kernel would be refused at launch");
-    static std::atomic<uint32_t> allowed[2][64];
+    static SharedLimit allowed[2];
     const dct_status_t allowed_st = allow_shared(kernel, smem, allowed[whole]);
     if (allowed_st != DCT_OK) return allowed_st;
     const uint64_t wanted = (static_cast<uint64_t>(rows) + kGroups - 1) / kGroups;

@@ -1,7 +1,6 @@
 // Pieces shared by the layer norm and by the calls on rows of logits: element types, sums over a CTA in a fixed
 // order, the order of logits, and the host's argument checks.
 #pragma once
-#include <atomic>
 #include <cmath>
 
 #include "common.cuh"
@@ -544,17 +543,17 @@ inline bool in_place_or_apart(const void* in, uint32_t ld_in, const void* out, u
     return (in == out && ld_in == ld_out) ||
            !spans_overlap(in, span_bytes(rows, d, ld_in, es), out, span_bytes(rows, d, ld_out, es));
 }
-// lets `kernel` have `bytes` of dynamic shared memory, once per device and amount.  Without asking it has 48 KiB, of which static
-// shared memory is a part: `unasked` of them are had anyway.  allowed: zeros at first, the kernel's own.
+// lets `kernel` have `bytes` of dynamic shared memory.  Without asking it has 48 KiB, of which static
+// shared memory is a part: `unasked` of them are had anyway.  allowed: the kernel's own.
 template <typename... Params>
-inline dct_status_t allow_shared(void (*kernel)(Params...), size_t bytes, std::atomic<uint32_t> (&allowed)[64], size_t unasked = 32 * 1024) {
+inline dct_status_t allow_shared(void (*kernel)(Params...), size_t bytes, SharedLimit& allowed, size_t unasked = 32 * 1024) {
     if (bytes <= unasked) return DCT_OK;
     int dev = 0;
-    DCT_CUDA_TRY(cudaGetDevice(&dev));
-    std::atomic<uint32_t>* word = dev >= 0 && dev < 64 ? &allowed[dev] : nullptr;
-    if (word && word->load(std::memory_order_relaxed) >= bytes) return DCT_OK;
-    DCT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
-    if (word) word->store(static_cast<uint32_t>(bytes), std::memory_order_relaxed);
+    const dct_status_t st = current_device(&dev);
+    if (st != DCT_OK) return st;
+    DCT_CUDA_TRY(static_cast<cudaError_t>(allowed.raise(dev, static_cast<uint32_t>(bytes), [&](uint32_t most) {
+        return static_cast<int>(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most)));
+    })));
     return DCT_OK;
 }
 
