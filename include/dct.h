@@ -640,7 +640,7 @@ DCT_API dct_status_t dct_layer_norm_bwd(
  *   top_logprobs [rows, top] fp32: their log p.
  *   result     device block or NULL; status is DCT_OK, or DCT_ERR_BAD_MASK if a token was >= vocab (it is then
  *              treated like a negative one), or DCT_ERR_TIMEOUT if a bounded wait between the CTAs of a row gave up (not
- *              seen in practice; that row's numbers are NaN).  With NULL no extra work is enqueued for it.
+ *              seen in practice; every sum and log p that depends on it is NaN).  With NULL no extra work is enqueued for it.
  * 1 <= vocab <= DCT_LM_MAX_VOCAB; rows may be 0; inv_temperature is finite and > 0.
  * z has to stay within fp32's range; in a row whose largest |z| is 2^26 or more it is the product rounded to fp32, otherwise the
  * exact one.  A masked column holds -inf (log p = -inf, no weight anywhere) or a value far below the rest (-1e9, the type's

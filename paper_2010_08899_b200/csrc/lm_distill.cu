@@ -72,12 +72,13 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
     const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = lane_id();
     const uint32_t rank = kCluster ? cluster_rank() : 0u, ctas = kCluster ? cluster_size() : 1u;
     const uint32_t clusters = gridDim.x / ctas;
-    uint32_t phases = 0, join_phases = 0, missed = 0;       // the parity each of this warp's barriers is waited for with; copies given up on
+    uint32_t phases = 0, join_phases = 0;       // the parity each of this warp's barriers is waited for with
+    bool stuck = false, join_stuck = false;     // a copy, the cluster's sums did not come at all: no more are waited for
 
     // (staged) asks for chunk k of a row's slice
     auto fetch_chunk = [&](const RowView<T>& of_row, const Slice& of_slice, uint32_t k) {
         const uint32_t first = of_slice.u0 + k * kChunkUnits;
-        if (lane == 0 && first < of_slice.u1 && !*const_cast<volatile uint32_t*>(&gave_up)) {
+        if (lane == 0 && first < of_slice.u1 && !stuck) {
             const uint32_t bytes = 16u * min(kChunkUnits, of_slice.u1 - first);
             uint64_t* bar = &arrived[warp * kMaxChunksPerWarp + k / kWarps];
             mbar_arrive_expect_tx(bar, bytes);
@@ -169,12 +170,12 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             uint4 v[4];
             if (kStaged) {
                 const uint32_t j = k / kWarps;
-                if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&arrived[warp * kMaxChunksPerWarp + j], phases >> j & 1u, a.spin_limit, &gave_up))) {
+                uint64_t* const bar = &arrived[warp * kMaxChunksPerWarp + j];
+                if (stuck || !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, phases >> j & 1u, a.spin_limit, &gave_up))) {
                     *const_cast<volatile uint32_t*>(&gave_up) = 1;       // this row and the rest become NaN
-                    missed |= 1u << j;
-                } else {
-                    phases ^= 1u << j;
+                    if (!stuck) stuck = !__all_sync(0xFFFFFFFFu, mbar_drain(bar, phases >> j & 1u));
                 }
+                phases ^= 1u << j;
             }
             if (kTail && kStaged) {                        // -inf at the named columns, for both readings; a word of marks to a lane
                 const uint32_t w = k * (4 * E) + lane;
@@ -284,14 +285,16 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         if (kCluster) {
             if (row_id == blockIdx.x / ctas) cluster_wait();         // (the first row) every CTA's mbarriers are there
             if (warp == 0) {
-                if (lane == 0 && !gave_up) mbar_arrive_expect_tx(&joined[turn], 16 * ctas);
+                if (lane == 0 && !join_stuck) mbar_arrive_expect_tx(&joined[turn], 16 * ctas);
                 __syncwarp();
                 if (lane < ctas)
                     push_remote(remote_smem(&pushed[turn][rank], lane), student.xmax, gave_up ? __uint_as_float(0x7FFFFFFFu) : student.s,
                                 named.xmax, named.s, remote_smem(&joined[turn], lane));
             }
-            if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&joined[turn], join_phases >> turn & 1u, a.spin_limit, &gave_up)))
+            if (join_stuck || !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&joined[turn], join_phases >> turn & 1u, a.spin_limit, &gave_up))) {
                 *const_cast<volatile uint32_t*>(&gave_up) = 1;
+                if (!join_stuck) join_stuck = !__all_sync(0xFFFFFFFFu, mbar_drain(&joined[turn], join_phases >> turn & 1u));
+            }
             join_phases ^= 1u << turn;
             const uint32_t c = lane & (kMaxCluster - 1);
             student = named = RowPart{minus_inf(), 0.0f, 0.0f};
@@ -349,7 +352,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                 }
             if (remainder && tid == 0 && q_rest != 0.0f) loss = fmaf(q_rest, logf(q_rest) - log_streamed, loss);
             loss = warp_join<SumOp>(loss);
-            if (lane == 0) loss_parts[warp] = loss;
+            if (lane == 0) loss_parts[warp] = broken ? __uint_as_float(0x7FFFFFFFu) : loss;
         }
         T* out = grad + static_cast<size_t>(row_id) * a.ld_grad;
         if (grad) {
@@ -468,14 +471,9 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         if (!more) break;
         row_id += clusters;
     }
-    // no copy may land in the shared memory of a CTA that is gone
-    if (kStaged && missed && lane == 0)
-        for (uint32_t j = 0; j < kMaxChunksPerWarp; ++j)
-            for (uint32_t i = 0; (missed >> j & 1u) && i < a.spin_limit; ++i)
-                if (mbar_try_wait(&arrived[warp * kMaxChunksPerWarp + j], phases >> j & 1u)) break;
-    if (kCluster) {                                        // the same for what the cluster pushes, should a wait have run out
+    if (kCluster) {                                        // nobody pushes to a CTA that is gone
         cluster_barrier();
-        if (gave_up) __nanosleep(1000000u);
+        if (join_stuck) __nanosleep(1000000u);
     }
 }
 

@@ -373,6 +373,7 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
         cluster_arrive();
     }
     uint32_t turn = 0;
+    bool stuck = false;                   // the others' numbers did not come at all
     for (uint32_t row_id = blockIdx.x / ctas;; turn ^= 1) {
         const T* xr = logits + static_cast<size_t>(row_id) * a.ld;
         const RowView<T> row(xr, a.vocab);
@@ -419,7 +420,7 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
         if (tid == kThreads - 32 && tok >= 0 && static_cast<uint32_t>(tok) < a.vocab) x_tok = to_f32(xr[tok]);
         if (kCluster) {
             cluster_wait();
-            if (tid == 0 && !sh.gave_up) {
+            if (tid == 0 && !stuck) {
                 uint32_t listed = 0;
                 for (uint32_t c = 0; c < ctas; ++c)
                     if (c != rank) listed += min(a.top, Slice(row.units, c, ctas).columns(row));
@@ -452,8 +453,10 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
                 if (c != rank) push_remote(remote_smem(&lists[rank * a.top + i], c), sh.best[i], remote_smem(&joined, c));
             }
             for (uint32_t i = tid; i < kept; i += kThreads) places[i] = i;
-            const bool here = mbar_wait_bounded(&joined, turn, a.spin_limit, &sh.gave_up);
-            if (!here) *const_cast<volatile uint32_t*>(&sh.gave_up) = 1;         // this row and the rest become NaN
+            if (stuck || !mbar_wait_bounded(&joined, turn, a.spin_limit, &sh.gave_up)) {
+                *const_cast<volatile uint32_t*>(&sh.gave_up) = 1;                // this row and the rest become NaN
+                if (!stuck) stuck = !mbar_drain(&joined, turn);
+            }
             __syncthreads();
             if (warp == kWarps - 1) {
                 RowPart all{minus_inf(), 0.0f, 0.0f};
@@ -504,7 +507,7 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
     }
     if (kCluster) {                       // nobody pushes to a CTA that is gone
         cluster_wait();
-        if (sh.gave_up) __nanosleep(1000000u);
+        if (stuck) __nanosleep(1000000u);
     }
 }
 

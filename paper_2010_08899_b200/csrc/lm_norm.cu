@@ -518,6 +518,25 @@ template <typename P, uint32_t kE> struct ParamImage {
     }
 };
 
+// What a CTA knows of its waits for rows of a ring.  gave_up: a bounded wait ran out, and that row is NaN; stuck: its copy did not come at
+// all, no more are asked for and what is left is NaN.
+struct RingWaits {
+    uint32_t gave_up, stuck;
+    __device__ __forceinline__ bool is_stuck() const { return *const_cast<const volatile uint32_t*>(&stuck); }
+    // false: what lies in the slot is not to be used
+    __device__ __forceinline__ bool row_is_here(uint64_t* full, uint32_t phase, uint32_t spin_limit) {
+        if (mbar_wait_bounded(full, phase, spin_limit, &gave_up)) return true;
+        *const_cast<volatile uint32_t*>(&gave_up) = 1;
+        if (!is_stuck() && !mbar_drain(full, phase)) *const_cast<volatile uint32_t*>(&stuck) = 1;
+        return false;
+    }
+};
+// Before the shared memory of a CTA that is stuck is given up or used for something else: by the thread that asked for the
+// copies, in whichever phase they are.
+template <uint32_t kRows> static __device__ __noinline__ void drain_ring(uint64_t* full) {
+    for (uint32_t i = 0; i < 2 * kRows; ++i) mbar_drain(&full[i / 2], i & 1u);
+}
+
 // CTAs of the forward kernel an SM's registers are asked to hold
 template <uint32_t kThreads, uint32_t kUnits> constexpr uint32_t fwd_ctas() { return (kUnits == 4 ? 512 : 1024) / kThreads; }
 
@@ -536,7 +555,7 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
     extern __shared__ __align__(128) uint4 shared[];       // parameters; per group its slots and two images of an unaligned y
     __shared__ float slots[128];
     __shared__ uint64_t full[kGroups][kFwdRing];
-    __shared__ uint32_t gave_up;
+    __shared__ RingWaits waits;
     const uint32_t all = group_size<kGroup>() * kUnits;    // units the group's lanes hold
     const uint32_t lane = kGroup ? threadIdx.x % 32 : threadIdx.x, group = kGroup ? threadIdx.x / 32 : 0, units = (d + E - 1) / E;
     uint4 *const weights = shared, *const biases = shared + Image::kPieces * all;
@@ -545,7 +564,7 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
     const uint64_t stride = static_cast<uint64_t>(gridDim.x) * kGroups;
     const uint64_t first = static_cast<uint64_t>(blockIdx.x) * kGroups + group;
 
-    if (threadIdx.x == 0) gave_up = 0;
+    if (threadIdx.x == 0) waits = RingWaits{0, 0};
     if (lane == 0) {
         for (uint32_t s = 0; s < kFwdRing; ++s) mbar_init(&full[group][s], 1);
         mbar_init_fence();
@@ -553,7 +572,7 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
     }
     __syncthreads();
     auto fetch = [&](uint64_t row, uint32_t slot) {          // by one thread
-        if (row >= rows || *const_cast<volatile uint32_t*>(&gave_up)) return;
+        if (row >= rows || waits.is_stuck()) return;
         const NormRow<T> a(x + row * ld, d);
         mbar_arrive_expect_tx(&full[group][slot], 16 * a.pieces);
         bulk_load(mine + slot * slot_units, a.base, 16 * a.pieces, &full[group][slot]);
@@ -565,15 +584,12 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
     __syncthreads();
 
     uint32_t slot = 0, phase = 0, turn = 0;
-    bool missed = false;
     const T* x_row = x + first * ld;
     T* y_row = y + first * ld_y;
     for (uint64_t row = first; row < rows; row += stride, x_row += stride * ld, y_row += stride * ld_y) {
         const NormRow<T> in(x_row, d);
-        if (!mbar_wait_bounded(&full[group][slot], phase, spin_limit, &gave_up)) {
-            *const_cast<volatile uint32_t*>(&gave_up) = 1;
-            missed = true;
-        }
+        // (a thread that misses the row makes its sum NaN, and with it all the group writes of it)
+        const bool missed = !waits.row_is_here(&full[group][slot], phase, spin_limit);
         uint4 raw[kUnits];
         const uint4* from = mine + slot * slot_units;
         load_units<kGroup, kUnits, kWhole>(raw, lane, units, in.off, in.pieces, [&](uint32_t p) { return from[p]; });
@@ -588,7 +604,7 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
         }
         float s0, s1, total;
         unpack2(sum, s0, s1);
-        total = __fadd_rn(s0, s1);
+        total = missed ? __uint_as_float(0x7FFFFFFFu) : __fadd_rn(s0, s1);
         group_sum<kGroup>(total, slots, turn++);
         if (kGroup == 32) __syncwarp();
         if (lane == 0) fetch(row + kFwdRing * stride, slot);      // every thread has its part of the row: the slot is free
@@ -614,8 +630,7 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
         unpack2(squares, s0, s1);
         float deviation = __fadd_rn(s0, s1);
         group_sum<kGroup>(deviation, slots, turn++);
-        float rstd = rsqrtf(fmaf(deviation, per_column, eps));
-        if (missed) rstd = __uint_as_float(0x7FFFFFFFu);       // what the group writes from here on is NaN
+        const float rstd = rsqrtf(fmaf(deviation, per_column, eps));
         const uint64_t by_rstd = pack2(rstd, rstd);
         RowWriter<T, kGroup, kWhole> out(y_row, d, image, slot_units, turn / 2);
 #pragma unroll
@@ -638,11 +653,7 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
         }
     }
     RowWriter<T, kGroup, kWhole>::drain(lane);
-    // no copy may land in the shared memory of a CTA that is gone
-    if (missed)
-        for (uint32_t s = 0; s < kFwdRing; ++s)
-            for (uint32_t i = 0; i < spin_limit; ++i)
-                if (mbar_try_wait(&full[group][s], phase)) break;
+    if (lane == 0 && waits.is_stuck()) drain_ring<kFwdRing>(full[group]);
 }
 
 // Backward: dx = r (g - mean(g) - h mean(g h)) with g = dy w, h = (x - mu) r; dweight = sum dy h, dbias = sum dy.
@@ -671,7 +682,7 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
     extern __shared__ __align__(128) uint4 ring[];        // per group: kRing slots of (x, dy), and two images of an unaligned dx
     __shared__ float slots[128];
     __shared__ uint64_t full[kGroups][kRing];
-    __shared__ uint32_t gave_up;
+    __shared__ RingWaits waits;
     const uint32_t lane = kGroup ? threadIdx.x % 32 : threadIdx.x, group = kGroup ? threadIdx.x / 32 : 0, units = (d + E - 1) / E;
     uint4* const mine = ring + group * (2 * kRing + (kWhole ? 0 : 2)) * slot_units;
     uint4* const image = mine + 2 * kRing * slot_units;
@@ -679,7 +690,7 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
     const uint64_t first = static_cast<uint64_t>(blockIdx.x) * kGroups + group;
 
     chain_release_next();                  // the CTAs that join the partial sums may come and wait
-    if (threadIdx.x == 0) gave_up = 0;
+    if (threadIdx.x == 0) waits = RingWaits{0, 0};
     if (lane == 0) {
         for (uint32_t s = 0; s < kRing; ++s) mbar_init(&full[group][s], 1);
         mbar_init_fence();
@@ -687,7 +698,7 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
     }
     __syncthreads();
     auto fetch = [&](uint64_t row, uint32_t slot) {          // by one thread
-        if (row >= rows || *const_cast<volatile uint32_t*>(&gave_up)) return;
+        if (row >= rows || waits.is_stuck()) return;
         const NormRow<T> a(x + row * ld, d), b(dy + row * ld_dy, d);
         mbar_arrive_expect_tx(&full[group][slot], 16 * (a.pieces + b.pieces));
         bulk_load(mine + 2 * slot * slot_units, a.base, 16 * a.pieces, &full[group][slot]);
@@ -704,7 +715,6 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
         for (uint32_t q = 0; q < E / 2; ++q) dw[i][q] = db[i][q] = 0;
     }
     uint32_t slot = 0, phase = 0, turn = 0;
-    bool missed = false;
     float mu = first < rows ? mean[first] : 0.0f, r = first < rows ? rstd[first] : 0.0f;
     const T *x_row = x + first * ld, *dy_row = dy + first * ld_dy;
     T* dx_row = dx + first * ld_dx;
@@ -712,11 +722,8 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
         const uint64_t next = row + stride;
         const float next_mu = next < rows ? mean[next] : 0.0f, next_r = next < rows ? rstd[next] : 0.0f;
         const NormRow<T> ax(x_row, d), ay(dy_row, d);
-        if (!mbar_wait_bounded(&full[group][slot], phase, spin_limit, &gave_up)) {
-            *const_cast<volatile uint32_t*>(&gave_up) = 1;
-            missed = true;
-        }
-        if (missed) r = __uint_as_float(0x7FFFFFFFu);      // what the group writes from here on is NaN
+        // (a thread that misses the row makes its h NaN, and with it the sum of g h: all the group writes of it)
+        if (!waits.row_is_here(&full[group][slot], phase, spin_limit)) r = __uint_as_float(0x7FFFFFFFu);
         const uint64_t minus_mu = pack2(-mu, -mu), by_r = pack2(r, r);
         uint64_t h[kUnits][E / 2], g[kUnits][E / 2], sum_g = 0, sum_gh = 0;
         const uint4* sx = mine + 2 * slot * slot_units;
@@ -767,21 +774,15 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
         }
     }
     RowWriter<T, kGroup, kWhole>::drain(lane);
-    // no copy may land in the shared memory of a CTA that is gone, nor in what is used below
-    if (missed)
-        for (uint32_t s = 0; s < kRing; ++s)
-            for (uint32_t i = 0; i < spin_limit; ++i)
-                if (mbar_try_wait(&full[group][s], phase)) break;
+    if (lane == 0 && waits.is_stuck()) drain_ring<kRing>(full[group]);
     if (!parts) return;
+    __syncthreads();                                       // every copy has arrived and been used, a wait that ran out is known
     // the CTA's partial sums: dweight, then dbias, `width` apart (a wait that ran out: NaN)
     const uint32_t width = units * E;
     float* cta = parts + static_cast<size_t>(blockIdx.x) * 2 * width;
-    const float broken = gave_up ? __uint_as_float(0x7FFFFFFFu) : 0.0f;
+    const float broken = waits.gave_up ? __uint_as_float(0x7FFFFFFFu) : 0.0f;
     float* to = cta;
-    if (kGroups > 1) {
-        __syncthreads();                                   // every copy has arrived and been used
-        to = reinterpret_cast<float*>(ring) + group * 2 * width;
-    }
+    if (kGroups > 1) to = reinterpret_cast<float*>(ring) + group * 2 * width;
 #pragma unroll
     for (uint32_t i = 0; i < kUnits; ++i) {
         const uint32_t u = lane + i * group_size<kGroup>();
@@ -793,8 +794,8 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
             unpack2(dw[i][q + 1], v.z, v.w);
             unpack2(db[i][q], t.x, t.y);
             unpack2(db[i][q + 1], t.z, t.w);
-            v.x += broken;
-            t.x += broken;
+            v = make_float4(v.x + broken, v.y + broken, v.z + broken, v.w + broken);
+            t = make_float4(t.x + broken, t.y + broken, t.z + broken, t.w + broken);
             *reinterpret_cast<float4*>(to + u * E + 2 * q) = v;
             *reinterpret_cast<float4*>(to + width + u * E + 2 * q) = t;
         }

@@ -436,6 +436,20 @@ struct Slice {
     }
 };
 
+// After a bounded wait that ran out (what depends on it becomes NaN): waits for the same phase once more, for up to a second by the
+// clock and whatever the first limit was, so that nothing is on its way when shared memory is used again or given up, and the
+// barrier is in step with its copies.  False if that ran out, too.
+__device__ __forceinline__ bool mbar_drain(uint64_t* bar, uint32_t parity) {
+    uint64_t start, now;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(start));
+    for (uint32_t i = 0; i < 1u << 24; ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+        if (now - start > 1000000000ull) break;
+    }
+    return false;
+}
+
 // Clusters of CTAs -------------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;

@@ -206,3 +206,75 @@ def test_time_of_a_call_does_not_depend_on_the_calls_before():
     took = [float(subprocess.run([sys.executable, "-c", ORDER, word], cwd=ROOT, capture_output=True, text=True, check=True, timeout=300).stdout)
             for word in ("before", "after")]
     assert took[1] < 1.5 * took[0]
+
+
+@pytest.fixture
+def waits_run_out():
+    """Every bounded wait gives up before its first poll.  (The kernels then wait again, with a limit of their own, before they go on.)"""
+    B.dct_debug_configure(spin_limit=0)
+    yield
+    B.dct_debug_configure()
+
+
+@pytest.mark.parametrize("rows,d,ld", [(1500, 256, 256), (700, 512, 512), (701, 509, 509), (301, 1000, 1000), (1200, 1024, 1024), (601, 4096, 4096),
+                                       (600, 4095, 4095), (450, 8192, 8192), (450, 8000, 8001)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layer_norm_whose_waits_run_out(dtype, rows, d, ld, waits_run_out):
+    """A wait for a row that gave up leaves no finite number: not in the row, not in its statistics, not in the parameters' gradients."""
+    dt = DT[dtype]
+    x = torch.randn(rows, ld, device=DEV).to(dt)
+    y, mean, rstd = torch.zeros(rows, ld, dtype=dt, device=DEV), vec(rows), vec(rows)
+    B.dct_layer_norm_fwd(x, rows, d, ld, None, None, 1e-5, y, ld, mean, rstd)
+    assert bool(y[:, :d].isnan().all()) and bool((y[:, d:] == 0).all())
+    assert bool(mean[:rows].isnan().all()) and bool(rstd[:rows].isnan().all())
+    ones, zeros = torch.ones(rows, device=DEV), torch.zeros(rows, device=DEV)
+    dx, dw, db = torch.zeros(rows, ld, dtype=dt, device=DEV), vec(d), vec(d)
+    ws = B.new_workspace(B.dct_layer_norm_bwd_workspace_bytes(rows, d))
+    B.dct_layer_norm_bwd(x, ld, x, rows, d, ld, None, zeros, ones, dx, ld, dw, db, ws)
+    assert bool(dx[:, :d].isnan().all()) and bool((dx[:, d:] == 0).all())
+    assert bool(dw[:d].isnan().all()) and bool(db[:d].isnan().all())
+    # and nothing of it is left behind
+    B.dct_debug_configure()
+    B.dct_layer_norm_fwd(x, rows, d, ld, None, None, 1e-5, y, ld, mean, rstd)
+    B.dct_layer_norm_bwd(x, ld, x, rows, d, ld, None, zeros, ones, dx, ld, dw, db, ws)
+    for t in (y, mean[:rows], rstd[:rows], dx, dw[:d], db[:d]):
+        assert bool(t.isfinite().all())
+
+
+@pytest.mark.parametrize("rows,vocab,top", [(700, 1500, 4), (700, 4000, 4), (500, 16000, 4), (500, 32768, 4), (40, 60000, 4), (230, 32768, 1024), (3, 400000, 16)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill_whose_waits_run_out(dtype, rows, vocab, top, tail, waits_run_out):
+    dt = DT[dtype]
+    x = torch.randn(rows, vocab, device=DEV).to(dt)
+    ids = (torch.arange(rows * top, device=DEV) % vocab).to(torch.int32)
+    t = torch.full((rows * top,), -np.log(2.0 * top), device=DEV)
+    loss, g, res = vec(rows), torch.zeros_like(x), B.new_result()
+    mode = B.DCT_DISTILL_TAIL if tail else B.DCT_DISTILL_RENORM
+    B.dct_lm_distill(x, rows, vocab, vocab, 1.0, ids, t, top, mode, None, loss, g, vocab, res)
+    assert B.read_result(res).status == B.DCT_ERR_TIMEOUT
+    assert bool(loss[:rows].isnan().all()) and bool(g.isnan().all())
+    B.dct_lm_distill(x, rows, vocab, vocab, 1.0, ids, t, top, mode, None, loss, None, 0, res)
+    assert B.read_result(res).status == B.DCT_ERR_TIMEOUT and bool(loss[:rows].isnan().all())
+    B.dct_debug_configure()
+    B.dct_lm_distill(x, rows, vocab, vocab, 1.0, ids, t, top, mode, None, loss, g, vocab, res)
+    assert B.read_result(res).status == B.DCT_OK
+    assert bool(loss[:rows].isfinite().all()) and bool(g.isfinite().all())
+
+
+@pytest.mark.parametrize("rows,vocab", [(1, 131072), (90, 131072), (150, 65536)])
+def test_logprobs_whose_waits_run_out(rows, vocab, waits_run_out):
+    """Rows that are split over CTAs, which wait for one another's sums and columns."""
+    x = torch.randn(rows, vocab, device=DEV)
+    tok = torch.zeros(rows, dtype=torch.int32, device=DEV)
+    lp, ent, stats, ids, tlp, res = vec(rows), vec(rows), vec(2 * rows), vec(5 * rows, torch.int32), vec(5 * rows), B.new_result()
+    call = lambda: B.dct_lm_logprobs_fwd(x, rows, vocab, vocab, 1.0, tok, 5, lp, ent, stats, ids, tlp, res)
+    call()
+    assert B.read_result(res).status == B.DCT_ERR_TIMEOUT
+    for t in (lp[:rows], ent[:rows], tlp[:5 * rows]):
+        assert bool(t.isnan().all())
+    B.dct_debug_configure()
+    call()
+    assert B.read_result(res).status == B.DCT_OK
+    want = torch.log_softmax(x.double(), 1)
+    assert torch.allclose(lp[:rows].double(), want[:, 0], atol=1e-4) and torch.equal(ids[:5 * rows].view(rows, 5).long(), want.topk(5, 1).indices)
