@@ -710,6 +710,8 @@ def _buf(t: Optional[torch.Tensor], dtype, name: str, count: int):
 
 def _span(rows: int, d: int, ld: int) -> int:
     """Elements from the first to one past the last of ``rows`` rows, ``ld`` apart, of which the first ``d`` count."""
+    if (rows | d | ld) >> 32:          # negative, too: the library would take it for a large unsigned number
+        raise ValueError(f"{rows} rows of {d} columns at a stride of {ld}: not 32-bit unsigned numbers")
     return (rows - 1) * ld + d if rows >= 1 and ld >= d else 0
 
 
