@@ -322,7 +322,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         // log Z = z_max + log_total; the streamed columns' share p_streamed of the student's distribution (1 unless kTail)
         const float z_streamed = __fmul_rn(student.xmax, a.by.inv_t);
         float z_max = z_streamed, log_total = logf(student.s) + beyond_max(student.xmax, a.by.inv_t, z_streamed);
-        float log_streamed = 0.0f, q_rest = 0.0f, log_norm = 0.0f;
+        float log_streamed = 0.0f, q_rest = 0.0f, t_max = 0.0f, log_norm = 0.0f;
         if (kTail) {
             const float log_s = log_total;
             z_max = fmaxf(z_streamed, named.xmax);
@@ -332,7 +332,8 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
             log_streamed = (z_streamed - z_max) + (log_s - log_total);
             q_rest = q_sum > 1.0f ? 0.0f : 1.0f - q_sum;
         } else {
-            log_norm = teacher.xmax + logf(teacher.s);
+            t_max = teacher.xmax;                          // (apart from the sum's logarithm, which a common offset would round away)
+            log_norm = logf(teacher.s);
         }
         const bool broken = log_total != log_total || nan_flag || gave_up;
         const bool nothing = (!broken && z_max == minus_inf()) || no_teacher;
@@ -341,7 +342,7 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         auto log_p = [&](uint32_t i) {                     // (as less_max: a row without a number is not asked for its log p)
             return (far ? __fadd_rn(__fmul_rn(logit(i), a.by.inv_t), -z_max) : fmaf(logit(i), a.by.inv_t, -z_max)) - log_total;
         };
-        auto log_q = [&](uint32_t i) { return t_s[i] - log_norm; };
+        auto log_q = [&](uint32_t i) { return (t_s[i] - t_max) - log_norm; };
 
         if (a.loss_out && rank == 0) {
             float loss = 0.0f;

@@ -278,3 +278,16 @@ def test_logprobs_whose_waits_run_out(rows, vocab, waits_run_out):
     assert B.read_result(res).status == B.DCT_OK
     want = torch.log_softmax(x.double(), 1)
     assert torch.allclose(lp[:rows].double(), want[:, 0], atol=1e-4) and torch.equal(ids[:5 * rows].view(rows, 5).long(), want.topk(5, 1).indices)
+
+
+@pytest.mark.parametrize("dtype,rows,vocab,top", [("f32", 300, 1000, 16), ("bf16", 40, 32768, 64), ("f32", 5, 50021, 40)])
+@pytest.mark.parametrize("offset", [0.0, -300.0, 8192.0, 65536.0])
+def test_distill_from_teacher_values_with_an_offset(dtype, rows, vocab, top, offset):
+    """A common offset of a row's teacher values (logits instead of log-probabilities) changes nothing, and costs no accuracy where
+    fp32 holds the values: multiples of 2^-6 here."""
+    x, _ = logits(rows, vocab, 91, DT[dtype])
+    gen = torch.Generator().manual_seed(17)
+    ids = torch.stack([torch.randperm(vocab, generator=gen)[:top] for _ in range(rows)]).to(torch.int32)
+    ids[0, 1] = ids[0, 0]
+    t = (torch.randn(rows, top, generator=gen) * 128).round() / 64 + offset
+    check_distill(x, 1.0, ids, t, False, None, vocab, 0, DT[dtype])
