@@ -51,7 +51,7 @@ class Student:
         self.share = torch.full((rows,), 1.0 / rows, device=device)         # the loss is the mean over the rows
         self.k = max(1, int(n * density))
         self.idx, self.val, self.tau = new(self.k, dt=torch.int32), new(self.k), new(1)
-        self.sent, self.status = B.new_result(device), B.new_result(device)
+        self.sent, self.status, self.applied = (B.new_result(device) for _ in range(3))      # compression, distillation, decompression
         self.norm_ws = B.new_workspace(B.dct_layer_norm_bwd_workspace_bytes(rows, d), device)
         self.send_ws = B.new_workspace(B.dct_dp_select_compress_workspace_bytes(n), device)
 
@@ -87,7 +87,7 @@ class Student:
         n = self.params.numel()
         B.dct_dp_select_compress(self.grads, self.residual, n, self.k, self.tau, self.idx, self.val, self.k, self.sent,
                                  self.send_ws)
-        B.dct_dp_decompress(self.idx, self.val, self.sent, self.k, self.update, n, False, self.status)
+        B.dct_dp_decompress(self.idx, self.val, self.sent, self.k, self.update, n, False, self.applied)
         self.params.sub_(self.update, alpha=self.lr)
         return StepResult(self.loss, self.sent, grad_hidden)
 

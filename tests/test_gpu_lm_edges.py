@@ -291,3 +291,19 @@ def test_distill_from_teacher_values_with_an_offset(dtype, rows, vocab, top, off
     ids[0, 1] = ids[0, 0]
     t = (torch.randn(rows, top, generator=gen) * 128).round() / 64 + offset
     check_distill(x, 1.0, ids, t, False, None, vocab, 0, DT[dtype])
+
+
+def test_a_step_keeps_what_each_of_its_calls_reports():
+    """A teacher's column outside the vocabulary is in the step's status when the step is over."""
+    from paper_2010_08899_b200.student import Student
+    s = Student(64, 301, 8, keep=64, top=4, density=1.0, dtype=torch.float32)
+    teach = s.teach
+
+    def teach_badly(teacher):
+        teach(teacher)
+        s.ids[3] = 301
+
+    s.teach = teach_badly
+    r = s.step(torch.randn(8, 64, device=DEV), torch.randn(8, 301, device=DEV))
+    assert B.read_result(s.status).status == B.DCT_ERR_BAD_MASK
+    assert B.read_result(r.sent).status == B.DCT_OK and B.read_result(s.applied).status == B.DCT_OK
