@@ -861,7 +861,7 @@ norm_param_join_kernel(const float* __restrict__ parts, uint32_t num, uint32_t d
 
 template <typename T, typename P>
 __global__ void __launch_bounds__(kNormThreads)
-norm_fwd_kernel(const T* __restrict__ x, uint32_t rows, uint32_t d, uint32_t ld, const P* __restrict__ weight,
+norm_fwd_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* __restrict__ weight,
                 const P* __restrict__ bias, float eps, T* y, uint32_t ld_y, float* __restrict__ mean_out,
                 float* __restrict__ rstd_out) {
     __shared__ float scratch[32];
@@ -877,10 +877,20 @@ norm_fwd_kernel(const T* __restrict__ x, uint32_t rows, uint32_t d, uint32_t ld,
         }
         const float rstd = 1.0f / sqrtf(cta_join<SumOp>(sq, scratch) / static_cast<float>(d) + eps);
         T* yr = y + static_cast<size_t>(row) * ld_y;
-        for (uint32_t j = threadIdx.x; j < d; j += kNormThreads) {
+        auto result = [&](float x_j, uint32_t j) {
             const float w = weight ? to_f32(weight[j]) : 1.0f, b = bias ? to_f32(bias[j]) : 0.0f;
-            yr[j] = from_f32<T>(fmaf((to_f32(xr[j]) - mean) * rstd, w, b));
+            return from_f32<T>(fmaf((x_j - mean) * rstd, w, b));
+        };
+        // (y may be x, so a load cannot be moved over a store: eight elements at a time, 129 us for 2048 rows of 32768 bf16; one by one 172)
+        uint32_t j = threadIdx.x;
+        for (; j + 7 * kNormThreads < d; j += 8 * kNormThreads) {
+            T out[8];
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) out[k] = result(to_f32(xr[j + k * kNormThreads]), j + k * kNormThreads);
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) yr[j + k * kNormThreads] = out[k];
         }
+        for (; j < d; j += kNormThreads) yr[j] = result(to_f32(xr[j]), j);
         if (threadIdx.x == 0) {
             if (mean_out) mean_out[row] = mean;
             if (rstd_out) rstd_out[row] = rstd;
