@@ -229,28 +229,28 @@ template <typename T> __device__ __forceinline__ uint4 pack_unit(const uint64_t 
 
 // Forward: y = (x - mu) r w + b.  The row is read once into registers; the variance is the mean square of the deviations from the
 // mean, a second sum over registers (a difference of squares would lose it where the mean is large against the deviation).
-template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits>
-__global__ void __launch_bounds__(kThreads)
+// Here a CTA to a row, for rows whose ring and parameters would not fit a CTA's shared memory.
+constexpr uint32_t kUnitsThreads = 512u;
+template <typename T, typename P>
+__global__ void __launch_bounds__(kUnitsThreads)
 norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* __restrict__ weight,
                       const P* __restrict__ bias, float eps, T* y, uint32_t ld_y, float* __restrict__ mean_out,
                       float* __restrict__ rstd_out) {
-    constexpr uint32_t E = Unit<T>::kElems, kGroups = kGroup ? kThreads / kGroup : 1;
-    extern __shared__ __align__(16) uint4 images[];
+    constexpr uint32_t E = Unit<T>::kElems, kUnits = 4;
+    extern __shared__ __align__(16) uint4 images[];        // two of an unaligned y
     __shared__ float slots[128];
-    const uint32_t lane = kGroup ? threadIdx.x % 32 : threadIdx.x, group = kGroup ? threadIdx.x / 32 : 0, units = (d + E - 1) / E;
-    uint4* image = images + group * 2 * (units + 2);
+    const uint32_t lane = threadIdx.x, units = (d + E - 1) / E;
     const bool vec_w = vector_params(weight), vec_b = vector_params(bias), whole = d % E == 0;
     uint32_t turn = 0;
-    for (uint64_t row = static_cast<uint64_t>(blockIdx.x) * kGroups + group; row < rows;
-         row += static_cast<uint64_t>(gridDim.x) * kGroups) {
+    for (uint64_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const NormRow<T> in(x + row * ld, d);
         uint4 raw[kUnits];
-        load_units<kGroup, kUnits, false>(raw, lane, units, in.off, in.pieces, [&](uint32_t p) { return ld_unit(in.base + p); });
+        load_units<0, kUnits, false>(raw, lane, units, in.off, in.pieces, [&](uint32_t p) { return ld_unit(in.base + p); });
         uint64_t v[kUnits][E / 2];
         uint64_t sum = 0;
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
-            const uint32_t u = lane + i * group_size<kGroup>();
+            const uint32_t u = lane + i * group_size<0>();
             unit_pairs<T>(raw[i], u < units ? d - u * E : 0u, 0.0f, v[i]);
 #pragma unroll
             for (uint32_t q = 0; q < E / 2; ++q) sum = add2(sum, v[i][q]);
@@ -258,13 +258,13 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
         float s0, s1;
         unpack2(sum, s0, s1);
         float total = __fadd_rn(s0, s1);
-        group_sum<kGroup>(total, slots, turn++);
+        group_sum<0>(total, slots, turn++);
         const float mean = total / static_cast<float>(d);
         const uint64_t minus_mean = pack2(-mean, -mean);
         uint64_t squares = 0;
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
-            const uint32_t u = lane + i * group_size<kGroup>(), left = u < units ? d - u * E : 0u;
+            const uint32_t u = lane + i * group_size<0>(), left = u < units ? d - u * E : 0u;
 #pragma unroll
             for (uint32_t q = 0; q < E / 2; ++q) v[i][q] = add2(v[i][q], minus_mean);
             if (left < E) {                        // what is past the end does not deviate
@@ -280,19 +280,19 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
         }
         unpack2(squares, s0, s1);
         float deviation = __fadd_rn(s0, s1);
-        group_sum<kGroup>(deviation, slots, turn++);
+        group_sum<0>(deviation, slots, turn++);
         const float rstd = 1.0f / sqrtf(deviation / static_cast<float>(d) + eps);
         const uint64_t by_rstd = pack2(rstd, rstd);
-        RowWriter<T, kGroup, false> out(y + row * ld_y, d, image, units + 2, turn / 2);
+        RowWriter<T, 0, false> out(y + row * ld_y, d, images, units + 2, turn / 2);
 #pragma unroll
         for (uint32_t i = 0; i < kUnits; ++i) {
-            const uint32_t col = (lane + i * group_size<kGroup>()) * E;
+            const uint32_t col = (lane + i * group_size<0>()) * E;
             uint64_t w[E / 2], b[E / 2];
             param_pairs<P, E>(weight, vec_w && whole, vec_w, col, d, 1.0f, w);
             param_pairs<P, E>(bias, vec_b && whole, vec_b, col, d, 0.0f, b);
 #pragma unroll
             for (uint32_t q = 0; q < E / 2; ++q) v[i][q] = fma2(mul2(v[i][q], by_rstd), w[q], b[q]);
-            out.put(lane + i * group_size<kGroup>(), pack_unit<T>(v[i]));
+            out.put(lane + i * group_size<0>(), pack_unit<T>(v[i]));
         }
         out.finish(lane);
         if (lane == 0) {
@@ -300,7 +300,7 @@ norm_fwd_units_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const 
             if (rstd_out) rstd_out[row] = rstd;
         }
     }
-    RowWriter<T, kGroup, false>::drain(lane);
+    RowWriter<T, 0, false>::drain(lane);
 }
 
 // Narrow rows: a unit to a lane and 32 / kLanes rows to a warp, four such sets of rows at a time.  With a warp to a row the work
@@ -957,20 +957,17 @@ uint32_t norm_parts(uint32_t rows, uint32_t d) {
     return rows < most ? (rows ? rows : 1) : most;
 }
 
-template <typename T, typename P, uint32_t kGroup, uint32_t kThreads, uint32_t kUnits>
+template <typename T, typename P>
 dct_status_t launch_fwd_units(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P* weight, const P* bias, float eps, T* y,
                               uint32_t ld_y, float* mean_out, float* rstd_out, cudaStream_t stream) {
-    constexpr uint32_t kGroups = kGroup ? kThreads / kGroup : 1, E = Unit<T>::kElems;
-    const uint32_t threads = kGroup ? kThreads : warps_for((d + E - 1) / E, kUnits) * 32;
-    auto kernel = norm_fwd_units_kernel<T, P, kGroup, kThreads, kUnits>;
+    const uint32_t units = (d + Unit<T>::kElems - 1) / Unit<T>::kElems, threads = warps_for(units, 4) * 32;
+    auto kernel = norm_fwd_units_kernel<T, P>;
     // an image only if some row of y does not start on a boundary
-    const size_t smem = on_boundaries(y, rows, ld_y, sizeof(T)) ? 0 : static_cast<size_t>(kGroups) * 2 * ((d + E - 1) / E + 2) * 16;
+    const size_t smem = on_boundaries(y, rows, ld_y, sizeof(T)) ? 0 : 2 * static_cast<size_t>(units + 2) * 16;
     static SharedLimit allowed;
     const dct_status_t allowed_st = allow_shared(kernel, smem, allowed);
     if (allowed_st != DCT_OK) return allowed_st;
-    const uint64_t ctas = (static_cast<uint64_t>(rows) + kGroups - 1) / kGroups;
-    kernel<<<static_cast<uint32_t>(ctas < (1u << 30) ? ctas : 1u << 30), threads, smem, stream>>>(
-        x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out);
+    kernel<<<rows < 1u << 30 ? rows : 1u << 30, threads, smem, stream>>>(x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out);
     DCT_CUDA_TRY(cudaGetLastError());
     return DCT_OK;
 }
@@ -1036,7 +1033,7 @@ dct_status_t launch_norm_fwd(const void* x_, uint32_t rows, uint32_t d, uint32_t
     if (units <= 2048) {
         // (the ring and both arrays of parameters fit an SM's shared memory unless fp32 parameters come with bf16 rows)
         if constexpr (sizeof(P) <= sizeof(T)) return go(launch_fwd_ring<T, P, 0, 512, 4>);
-        else return go(launch_fwd_units<T, P, 0, 512, 4>);
+        else return go(launch_fwd_units<T, P>);
     }
     const uint32_t grid = rows < 4096u ? rows : 4096u;
     norm_fwd_kernel<T, P><<<grid, kNormThreads, 0, stream>>>(x, rows, d, ld, weight, bias, eps, y, ld_y, mean_out, rstd_out);
