@@ -689,7 +689,8 @@ typedef enum {
  *           loss = sum_k q_k (log q_k - log p_{i_k}) + q_r (log q_r - log p_r);
  *           dloss/dz_j = p_j - sum_{k: i_k = j} q_k for a column some slot names, p_j (1 - q_r / p_r) for the others
  *   grad_logits_j = grad_loss * inv_temperature * dloss/dz_j
- * (q log q = 0 at q = 0; a slot with q = 0 adds nothing; the q_r term is left out where p_r = 0.)
+ * (q log q = 0 at q = 0; a slot with q = 0 adds nothing; the q_r term is left out where p_r = 0.  There, and where the slots sum to more
+ * than 1, the named columns' gradient is still p_j - q_j, which is not the derivative of the loss that is left.)
  *
  *   teacher_ids       [rows, top] int32, any order.  A negative id is an empty slot.  A column named by several
  *                     slots has the sum of their q.

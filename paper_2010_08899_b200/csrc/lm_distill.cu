@@ -41,10 +41,11 @@ __device__ __forceinline__ void add_value(RowPart& p, float v) {
 //   RENORM: gradient of a column 2^y (scale / S), a named one's less its q scale;
 //   TAIL:   of a column that is not named 2^y (p_r - q_r) scale / S, with p_r the streamed columns' share of the whole: the
 //           factor p_j (1 - q_r / p_r) without the quotient, which overflows where the remainder is tiny.
-// What bounds it: instructions.  An element takes two powers of two and some 16 instructions of its thread in all, at 24 warps to an SM
-// since the rows take the shared memory; reading and writing 2^27 bf16 logits alone would take 82 us.  4096 rows of 32768 bf16, 64
-// slots: 111 us (4.8 TB/s; every logit is read from DRAM once), fp32 206 us (5.2); 1024 rows of 131072 bf16, 128 slots and the
-// remainder: 142 us (3.8 TB/s).
+// What bounds it: instructions and the latencies between them, 2.2 a cycle of 4 at the 24 warps to an SM that the rows' shared memory and 80
+// registers leave.  An element takes two powers of two (the special function unit is at 57 %) and 15.7 instructions of its thread in all, of which 12.6 are
+// the two readings and the rest is the row's joins, logarithms and slots; with the remainder 19.5.  Reading and writing 2^27 bf16 logits alone would
+// take 82 us.  4096 rows of 32768 bf16, 64 slots: 111 us (4.8 TB/s; every logit is read from DRAM once), fp32 182 us (5.9); 1024 rows of 131072 bf16,
+// 128 slots and the remainder: 140 us (3.8 TB/s).
 constexpr uint32_t kChunkUnits = 128u, kChunkBytes = 16u * kChunkUnits;
 constexpr uint32_t kMaxChunksPerWarp = 16u;
 // shared memory of a CTA that a staged slice may take: three CTAs to an SM.  (With one, loading twice is faster: 256 rows of 262144
@@ -421,7 +422,8 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
                 const uint64_t by_c = pack2(a.by.c, a.by.c), shift = pack2(-ref, -ref), by_factor = pack2(factor, factor);
                 write_chunks([&](uint64_t x) { return mul2(powers(fma2(x, by_c, shift)), by_factor); });
             } else {                                       // (or none but -inf)
-                // (rare: one unit after the other, to keep it out of the other rows' registers)
+                // (rare: one unit after the other, which leaves the other rows' registers alone: 4096 rows of 32768 fp32 182 us, with a third loop
+                // like the others 194)
                 const float less = z_streamed == minus_inf() ? 0.0f : -z_streamed;
                 for (uint32_t k = warp; u0 + k * kChunkUnits < u1; k += kWarps) {
 #pragma unroll 1

@@ -6,9 +6,9 @@
 //   up to 2048   a CTA to a row (bf16 backward up to 1024)             } rows through a ring of bulk copies
 //   beyond       a CTA to a row that is read again for every sum (norm_fwd_kernel, norm_bwd_kernel, norm_param_parts_kernel);
 //                bf16 rows of 1025 to 2048 units with fp32 parameters go forward in registers without a ring (norm_fwd_units_kernel)
-// Memory bound: 2 and 3 times the matrix cross the bus.  16384 rows of 4096 bf16: forward 46 us (5.9 TB/s), backward 67 us with
-// the parameters' gradients (6.0 TB/s) and 62 us without; fp32 forward 89 us (6.0), backward 122 us (6.6).  Rows off the
-// 16-byte boundaries are bound by instructions: 16384 rows of 4095 bf16 72 and 100 us.
+// Memory bound: 2 and 3 times the matrix cross the bus.  In a replayed graph (a call of its own adds the launch, 5 us), 16384 rows of 4096 bf16:
+// forward 45.5 us (5.9 TB/s), backward 67 us with the parameters' gradients (6.0 TB/s) and 62 us without; fp32 forward 90 us (6.0), backward
+// 122 us (6.6).  Rows off the 16-byte boundaries are bound by instructions: 16384 rows of 4095 bf16 72 and 99 us.
 #include "lm_rows.cuh"
 
 namespace dct {
