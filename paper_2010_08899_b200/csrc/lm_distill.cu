@@ -474,9 +474,10 @@ lm_distill_kernel(const T* logits, T* grad, const DistillArgs a) {
         if (!more) break;
         row_id += clusters;
     }
+    if (kStaged && stuck && lane == 0) copies_settle();
     if (kCluster) {                                        // nobody pushes to a CTA that is gone
         cluster_barrier();
-        if (join_stuck) __nanosleep(1000000u);
+        if (join_stuck) copies_settle();
     }
 }
 

@@ -507,7 +507,7 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
     }
     if (kCluster) {                       // nobody pushes to a CTA that is gone
         cluster_wait();
-        if (stuck) __nanosleep(1000000u);
+        if (stuck) copies_settle();
     }
 }
 

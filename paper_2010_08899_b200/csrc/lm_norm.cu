@@ -523,20 +523,16 @@ template <typename P, uint32_t kE> struct ParamImage {
 struct RingWaits {
     uint32_t gave_up, stuck;
     __device__ __forceinline__ bool is_stuck() const { return *const_cast<const volatile uint32_t*>(&stuck); }
-    // false: what lies in the slot is not to be used
-    __device__ __forceinline__ bool row_is_here(uint64_t* full, uint32_t phase, uint32_t spin_limit) {
+    // false: what lies in the slot is not to be used.  (A thread that knows of a copy that did not come never looks at a barrier
+    // again, its limit is 0 from then on: the phase after the one that is due would seem to be over.)
+    __device__ __forceinline__ bool row_is_here(uint64_t* full, uint32_t phase, uint32_t& spin_limit) {
         if (mbar_wait_bounded(full, phase, spin_limit, &gave_up)) return true;
         *const_cast<volatile uint32_t*>(&gave_up) = 1;
         if (!is_stuck() && !mbar_drain(full, phase)) *const_cast<volatile uint32_t*>(&stuck) = 1;
+        if (is_stuck()) spin_limit = 0;
         return false;
     }
 };
-// Before the shared memory of a CTA that is stuck is given up or used for something else: by the thread that asked for the
-// copies, in whichever phase they are.
-template <uint32_t kRows> static __device__ __noinline__ void drain_ring(uint64_t* full) {
-    for (uint32_t i = 0; i < 2 * kRows; ++i) mbar_drain(&full[i / 2], i & 1u);
-}
-
 // CTAs of the forward kernel an SM's registers are asked to hold
 template <uint32_t kThreads, uint32_t kUnits> constexpr uint32_t fwd_ctas() { return (kUnits == 4 ? 512 : 1024) / kThreads; }
 
@@ -653,7 +649,7 @@ norm_fwd_ring_kernel(const T* x, uint32_t rows, uint32_t d, uint32_t ld, const P
         }
     }
     RowWriter<T, kGroup, kWhole>::drain(lane);
-    if (lane == 0 && waits.is_stuck()) drain_ring<kFwdRing>(full[group]);
+    if (lane == 0 && waits.is_stuck()) copies_settle();
 }
 
 // Backward: dx = r (g - mean(g) - h mean(g h)) with g = dy w, h = (x - mu) r; dweight = sum dy h, dbias = sum dy.
@@ -774,7 +770,7 @@ norm_bwd_units_kernel(const T* dy, uint32_t ld_dy, const T* x, uint32_t rows, ui
         }
     }
     RowWriter<T, kGroup, kWhole>::drain(lane);
-    if (lane == 0 && waits.is_stuck()) drain_ring<kRing>(full[group]);
+    if (lane == 0 && waits.is_stuck()) copies_settle();
     if (!parts) return;
     __syncthreads();                                       // every copy has arrived and been used, a wait that ran out is known
     // the CTA's partial sums: dweight, then dbias, `width` apart (a wait that ran out: NaN)

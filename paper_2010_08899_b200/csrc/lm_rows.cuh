@@ -450,6 +450,17 @@ __device__ __forceinline__ bool mbar_drain(uint64_t* bar, uint32_t parity) {
     return false;
 }
 
+// A second by the clock, before shared memory is given up or used for something else, for copies that may be on their way after one did not come.
+static __device__ __noinline__ void copies_settle() {
+    uint64_t start, now;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(start));
+    for (uint32_t i = 0; i < 1u << 20; ++i) {
+        __nanosleep(1000u);
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+        if (now - start > 1000000000ull) break;
+    }
+}
+
 // Clusters of CTAs -------------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
