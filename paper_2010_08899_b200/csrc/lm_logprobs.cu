@@ -415,6 +415,14 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
         const RowPart mine = sums.part<true>(warp_max(fmaxf(max0, max1)), a.by.c);
         if (lane == 0) sh.warp_part[turn][warp] = mine;
         __syncthreads();
+        // a row that is far off (the same for the whole CTA) is summed again, by all warps
+        const float x_slice = warp_max(sh.warp_part[turn][lane & (kWarps - 1)].xmax);
+        if (x_slice > minus_inf() && far_off(__fmul_rn(x_slice, a.by.inv_t))) {
+            const RowPart share = far_part(row, u0 + warp * 32, kThreads, u1, x_slice, a.by, [](uint32_t, uint32_t) { return true; });
+            __syncthreads();                                         // (the parts' largest have been read)
+            if (lane == 0) sh.warp_part[turn][warp] = share;
+            __syncthreads();
+        }
 
         float x_tok = 0.0f;
         if (tid == kThreads - 32 && tok >= 0 && static_cast<uint32_t>(tok) < a.vocab) x_tok = to_f32(xr[tok]);
@@ -432,8 +440,6 @@ lm_logprobs_kernel(const T* __restrict__ logits, const LogProbArgs a) {
         if (warp == kWarps - 1) {
             RowPart all = sh.warp_part[turn][lane & (kWarps - 1)];
             all.join_lanes<kWarps, true>(a.by.c);
-            if (all.xmax > minus_inf() && far_off(__fmul_rn(all.xmax, a.by.inv_t)))
-                all = far_part(row, u0, 32, u1, all.xmax, a.by, [](uint32_t, uint32_t) { return true; });
             if (kCluster) {
                 if (lane < ctas) push_remote(remote_smem(&pushed[rank], lane), all.xmax, all.s, all.st, 0.0f, remote_smem(&joined, lane));
             } else if (lane == 0) {
@@ -551,7 +557,8 @@ lm_logprobs_bwd_kernel(const T* logits, T* grad, const LogProbBwdArgs q) {
         const float a = asked ? q.grad_logprob[row_id] : 0.0f;
         const float c = q.grad_entropy ? q.grad_entropy[row_id] : 0.0f, h = q.grad_entropy ? q.entropy[row_id] : 0.0f;
         const uint32_t tok_at = asked ? static_cast<uint32_t>(tok) + row.lead : 0xFFFFFFFFu;
-        // z - m as the forward call forms it: the product with 1 / T by the fma, or (rows far off) rounded before it; the other factor is 1
+        // z - m as the forward call forms it: the product with 1 / T by the fma, or (rows far off) rounded before it; the other factor
+        // is 1 (and known only here: a product and a sum of pairs would come out as one fma again)
         const float before = far_off(ref) ? q.inv_t : 1.0f, within = far_off(ref) ? 1.0f : q.inv_t;
         const uint64_t first_scale = pack2(before, before), then_scale = pack2(within, within);
         const uint64_t scale = pack2(q.inv_t, q.inv_t), shift = pack2(-ref, -ref), less = pack2(-logsum, -logsum);
