@@ -713,6 +713,102 @@ DCT_API dct_status_t dct_lm_distill(
     const float* grad_loss, float* loss_out, void* grad_logits, uint32_t ld_grad,
     dct_result_t* result, dct_stream_t stream);
 
+/* ------------------------------------------------------------------------- *
+ * A Transformer stage whose activations are held in 8 bits: checkpoints, the
+ * matrix product of such matrices, and the gated feed-forward block.
+ * (The paper compresses what crosses a split; it prescribes nothing for these.)
+ * ------------------------------------------------------------------------- */
+
+/*
+ * A matrix [rows, cols] in 8 bits: e4m3 codes (4 bits of exponent, 3 of fraction, largest 448, 0x7F / 0xFF NaN) and one power of two
+ * for every 128 columns of a row (the last block of a row may be shorter):  value = code * 2^(byte - 127).
+ *   codes   [rows, ld] bytes, 16-byte aligned, ld >= cols and a multiple of 16; bytes behind a row's last column are not
+ *           written and count for nothing (they may be read together with the last ones), so matrices may lie side by side in wider rows.
+ *   scales  dct_act8_scale_bytes(rows, cols) bytes, 16-byte aligned.  The byte of row r and block b lies at
+ *             ((b / 4) * ceil(rows / 128) + r / 128) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4,
+ *           the order in which the tensor cores take them; bytes of rows and blocks that are not there are not looked at.
+ * rows and cols are at most DCT_ACT8_MAX_DIM; where one is 0 there is nothing to read or write, and the pointers may be NULL.
+ *
+ * Writing: with a = the largest magnitude of a block, e is the smallest integer >= -127 with a <= 448 * 2^e; its byte is e + 127 (a
+ * block of zeros: 0) and its codes are x * 2^-e rounded to nearest, ties to even.  A value is off by at most 2^-4 of itself, or, below
+ * 2^(e-6), by at most 2^(e-10).  A block with a NaN or an infinity becomes NaN throughout (byte 255).  (What would
+ * round to 2^128, beyond fp32, takes the code below.)
+ * The powers make the transpose exact but for values more than 2^13 below the largest of their new block.
+ */
+typedef struct {
+  void* codes;
+  void* scales;
+  uint32_t rows, cols, ld;
+  uint32_t reserved;   /* 0 */
+} dct_act8_t;
+
+#define DCT_ACT8_MAX_DIM (1u << 28)
+
+/* Bytes of the scales of a [rows, cols] matrix (0 if a size is 0 or too large). */
+DCT_API size_t dct_act8_scale_bytes(uint32_t rows, uint32_t cols);
+
+/*
+ * dct_act8_pack -- a matrix into 8 bits: x into `out` (blocks of 128 along x's rows), into `out_t` (x transposed, [cols, rows], blocks
+ * along x's columns, as the gradient of weights needs it), or both from one reading.
+ *   x        [rows, ld] fp32 or bf16; only the first `cols` columns of a row count.  Any stride and address.
+ *   out, out_t  HOST descriptors of the outputs, each may be NULL, not both.
+ * No output may overlap x or another output.
+ */
+DCT_API dct_status_t dct_act8_pack(
+    const void* x, dct_dtype_t dtype, uint32_t rows, uint32_t cols, uint32_t ld,
+    const dct_act8_t* out, const dct_act8_t* out_t, dct_stream_t stream);
+
+/* dct_act8_unpack -- the values of `a`, rounded to dtype (bf16 holds each exactly that is not below its range), into y [rows, ld_y]. */
+DCT_API dct_status_t dct_act8_unpack(
+    const dct_act8_t* a, void* y, dct_dtype_t dtype, uint32_t ld_y, dct_stream_t stream);
+
+/* dct_act8_transpose -- the values of `a` written as out_t [cols, rows]: what dct_act8_pack would write of them. */
+DCT_API dct_status_t dct_act8_transpose(const dct_act8_t* a, const dct_act8_t* out_t, dct_stream_t stream);
+
+/*
+ * dct_gemm8 -- the product of matrices in 8 bits: C = A B^T, or C = A B^T + A2 B2^T, added to what C holds if `accumulate` is not 0.
+ *   a, b     [m, k] and [n, k].   a2, b2  [m, k2] and [n, k2], or both NULL.  k may be 0 where a has 0 columns (rows of a
+ *            batch that has none): that product is zero.
+ *   c        [m, ld_c] fp32 or bf16; the first n columns of each row are written.  Any stride and address; it may not overlap the inputs.
+ * Products and sums are fp32 (the order of a sum is fixed for given sizes), rounded once to C's type.
+ * Should a bounded wait give up (not seen in practice), the tile concerned becomes NaN.
+ */
+DCT_API dct_status_t dct_gemm8(
+    const dct_act8_t* a, const dct_act8_t* b, const dct_act8_t* a2, const dct_act8_t* b2,
+    void* c, dct_dtype_t dtype, uint32_t ld_c, int accumulate, dct_stream_t stream);
+
+typedef enum {
+  DCT_ACT_SILU = 0, /* act(g) = g / (1 + exp(-g)) */
+  DCT_ACT_GELU = 1  /* act(g) = g / (1 + exp(-2 sqrt(2/pi) (g + 0.044715 g^3))): GELU in its tanh form */
+} dct_activation_t;
+
+/*
+ * dct_gated8_fwd -- the first half of a gated feed-forward block in one kernel: with gate g = x Wg^T and up u = x Wu^T,
+ *   h = act(g) * u.
+ *   x                [rows, d].   w_gate, w_up  [f, d].
+ *   h                [rows, f] in 8 bits, or NULL.     h_dense  [rows, ld_h] fp32 or bf16, or NULL.  One of them must be given.
+ *   gate, up         [rows, f]: g and u in 8 bits, what dct_gated8_bwd takes.  Both or neither (serving) may be NULL.
+ * g, u and h are fp32 throughout and rounded once into each output.  Outputs may not overlap inputs or one another.
+ */
+DCT_API dct_status_t dct_gated8_fwd(
+    const dct_act8_t* x, const dct_act8_t* w_gate, const dct_act8_t* w_up, dct_activation_t activation,
+    const dct_act8_t* h, void* h_dense, dct_dtype_t dtype, uint32_t ld_h,
+    const dct_act8_t* gate, const dct_act8_t* up, dct_stream_t stream);
+
+/*
+ * dct_gated8_bwd -- from the gradient at h and what the forward call kept:
+ *   dgate = dh * u * act'(g),   dup = dh * act(g),   and the product again, h = act(g) * u,
+ * each rounded once from fp32 into 8 bits, in the forms the products after it take.
+ *   dh               [rows, ld_dh] fp32 or bf16 (NULL if only h_t is asked for).
+ *   dgate, dup       [rows, f], for the gradient at x: dgate Wg + dup Wu.
+ *   dgate_t, dup_t, h_t  [f, rows], for the gradients of the three weights.  Each output may be NULL, not all of them.
+ * Outputs may not overlap inputs or one another.
+ */
+DCT_API dct_status_t dct_gated8_bwd(
+    const void* dh, dct_dtype_t dtype, uint32_t ld_dh, const dct_act8_t* gate, const dct_act8_t* up, dct_activation_t activation,
+    const dct_act8_t* dgate, const dct_act8_t* dup, const dct_act8_t* dgate_t, const dct_act8_t* dup_t, const dct_act8_t* h_t,
+    dct_stream_t stream);
+
 /*
  * TEST-ONLY knobs, exported for the library's own test-suite and not part of the production interface: two
  * process-wide words (atomics) that every later call reads once.  A build with -DDCT_NO_TEST_HOOKS turns the

@@ -20,6 +20,7 @@ DCT_OK, DCT_ERR_INVALID_ARG, DCT_ERR_WORKSPACE, DCT_ERR_UNSUPPORTED = 0, 1, 2, 3
 DCT_ERR_CUDA, DCT_ERR_CAPACITY, DCT_ERR_TIMEOUT, DCT_ERR_BAD_MASK = 4, 5, 6, 7
 DCT_F32, DCT_BF16 = 0, 1
 DCT_DISTILL_RENORM, DCT_DISTILL_TAIL = 0, 1
+DCT_ACT_SILU, DCT_ACT_GELU = 0, 1
 
 RESULT_BYTES = 40          # sizeof(dct_result_t)
 
@@ -41,6 +42,7 @@ EXPORTED_SYMBOLS = (
     "dct_threshold_select_shard_sampled_pass", "dct_threshold_select_shard_sampled_advance",
     "dct_layer_norm_fwd", "dct_layer_norm_bwd", "dct_layer_norm_bwd_workspace_bytes",
     "dct_lm_logprobs_fwd", "dct_lm_logprobs_bwd", "dct_lm_distill",
+    "dct_act8_scale_bytes", "dct_act8_pack", "dct_act8_unpack", "dct_act8_transpose", "dct_gemm8", "dct_gated8_fwd", "dct_gated8_bwd",
 )
 
 _vp, _u64, _u32, _sz, _int = ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_size_t, ctypes.c_int
@@ -148,6 +150,20 @@ def lib() -> ctypes.CDLL:
     L.dct_lm_logprobs_bwd.argtypes = [_vp, _int, _u32, _u32, _u32, _f32, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _vp]
     L.dct_lm_distill.restype = _int
     L.dct_lm_distill.argtypes = [_vp, _int, _u32, _u32, _u32, _f32, _vp, _vp, _u32, _int, _vp, _vp, _vp, _u32, _vp, _vp]
+    L.dct_act8_scale_bytes.restype = _sz
+    L.dct_act8_scale_bytes.argtypes = [_u32, _u32]
+    L.dct_act8_pack.restype = _int
+    L.dct_act8_pack.argtypes = [_vp, _int, _u32, _u32, _u32, _vp, _vp, _vp]
+    L.dct_act8_unpack.restype = _int
+    L.dct_act8_unpack.argtypes = [_vp, _vp, _int, _u32, _vp]
+    L.dct_act8_transpose.restype = _int
+    L.dct_act8_transpose.argtypes = [_vp, _vp, _vp]
+    L.dct_gemm8.restype = _int
+    L.dct_gemm8.argtypes = [_vp, _vp, _vp, _vp, _vp, _int, _u32, _int, _vp]
+    L.dct_gated8_fwd.restype = _int
+    L.dct_gated8_fwd.argtypes = [_vp, _vp, _vp, _int, _vp, _vp, _int, _u32, _vp, _vp, _vp]
+    L.dct_gated8_bwd.restype = _int
+    L.dct_gated8_bwd.argtypes = [_vp, _int, _u32, _vp, _vp, _int, _vp, _vp, _vp, _vp, _vp, _vp]
     L.dct_debug_configure.restype = None
     L.dct_debug_configure.argtypes = [_u32, _u32]
     _lib = L
@@ -777,3 +793,125 @@ def dct_lm_distill(logits, rows, vocab, ld, inv_temperature, teacher_ids, teache
         _buf(grad_logits, dt, "grad_logits", _span(rows, vocab, ld_grad)), ld_grad,
         _buf(result, torch.int64, "result", RESULT_BYTES // 8), _stream(stream))
     _check("dct_lm_distill", status)
+
+
+# --------------------------------------------------------------------------------------------
+# matrices in 8 bits: checkpoints, products, the gated feed-forward block
+# --------------------------------------------------------------------------------------------
+
+DCT_ACT8_MAX_DIM = 1 << 28
+
+
+class _Act8(ctypes.Structure):             # dct_act8_t
+    _fields_ = [("codes", _vp), ("scales", _vp), ("rows", _u32), ("cols", _u32), ("ld", _u32), ("reserved", _u32)]
+
+
+class Act8:
+    """A matrix [rows, cols] in 8 bits: its buffers and the descriptor the calls take.  ``codes`` is [at least rows, at least cols]
+    uint8 (or float8_e4m3fn) with unit column stride and a row stride that is a multiple of 16 (columns of a wider buffer will do);
+    ``scales`` holds dct_act8_scale_bytes(rows, cols) uint8."""
+
+    __slots__ = ("codes", "scales", "rows", "cols", "ld", "device", "_struct", "_at")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int):
+        if not (0 <= rows <= DCT_ACT8_MAX_DIM and 0 <= cols <= DCT_ACT8_MAX_DIM):
+            raise ValueError(f"{rows} rows of {cols} columns: at most {DCT_ACT8_MAX_DIM} of either")
+        if codes.dtype not in (torch.uint8, torch.float8_e4m3fn) or scales.dtype != torch.uint8:
+            raise TypeError(f"codes and scales: expected uint8, got {codes.dtype} and {scales.dtype}")
+        if not codes.is_cuda or scales.device != codes.device:
+            raise ValueError("codes and scales: must be CUDA tensors of one device")
+        if codes.dim() != 2 or not scales.is_contiguous():
+            raise ValueError("codes: must have two dimensions; scales: must be contiguous")
+        ld = (cols + 15) // 16 * 16
+        if rows and cols:
+            if codes.shape[0] < rows or codes.shape[1] < cols or (codes.shape[1] > 1 and codes.stride(1) != 1):
+                raise ValueError(f"codes: {tuple(codes.shape)} at strides {codes.stride()} cannot hold [{rows}, {cols}]")
+            if rows > 1:
+                ld = codes.stride(0)
+            if ld < cols or ld % 16 or ld >> 32:
+                raise ValueError(f"codes: a row stride of {ld}, which is no multiple of 16 of at least {cols}")
+            if scales.numel() < lib().dct_act8_scale_bytes(rows, cols):
+                raise ValueError("scales: smaller than dct_act8_scale_bytes(rows, cols)")
+        self.codes, self.scales, self.rows, self.cols, self.ld, self.device = codes, scales, rows, cols, ld, codes.device.index
+        self._struct = _Act8(codes.data_ptr(), scales.data_ptr(), rows, cols, ld, 0)
+        self._at = ctypes.addressof(self._struct)
+
+
+def act8(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int) -> Act8:
+    """A matrix in 8 bits in buffers of the caller's."""
+    return Act8(codes, scales, rows, cols)
+
+
+def new_act8(rows: int, cols: int, device="cuda") -> Act8:
+    """A matrix in 8 bits in new buffers; its contents are undefined."""
+    codes = torch.empty(rows, (cols + 15) // 16 * 16, dtype=torch.uint8, device=device)
+    return Act8(codes, torch.empty(lib().dct_act8_scale_bytes(rows, cols), dtype=torch.uint8, device=device), rows, cols)
+
+
+def _held(m: Optional[Act8], name: str, device: int):
+    """The address of a descriptor (None if absent) whose buffers lie on the device the call runs on."""
+    if m is None:
+        return None
+    if m.device != device:
+        raise ValueError(f"{name}: on device {m.device}, the current one is {device}")
+    return m._at
+
+
+def _here(t: Optional[torch.Tensor], dtype, name: str, count: int, device: int):
+    at = _buf(t, dtype, name, count)
+    if at is not None and t.get_device() != device:
+        raise ValueError(f"{name}: on device {t.get_device()}, the current one is {device}")
+    return at
+
+
+def _current_device() -> int:
+    return _device() if _device is not None else torch.cuda.current_device()
+
+
+def dct_act8_scale_bytes(rows: int, cols: int) -> int:
+    return lib().dct_act8_scale_bytes(rows, cols)
+
+
+def dct_act8_pack(x, rows, cols, ld, out=None, out_t=None, stream=None) -> None:
+    code, dev = _dtype_code(x), _current_device()
+    status = lib().dct_act8_pack(_here(x, x.dtype, "x", _span(rows, cols, ld), dev), code, rows, cols, ld, _held(out, "out", dev),
+                                 _held(out_t, "out_t", dev), _stream(stream))
+    _check("dct_act8_pack", status)
+
+
+def dct_act8_unpack(a, y, ld_y, stream=None) -> None:
+    code, dev = _dtype_code(y), _current_device()
+    status = lib().dct_act8_unpack(_held(a, "a", dev), _here(y, y.dtype, "y", _span(a.rows, a.cols, ld_y), dev), code, ld_y,
+                                   _stream(stream))
+    _check("dct_act8_unpack", status)
+
+
+def dct_act8_transpose(a, out_t, stream=None) -> None:
+    dev = _current_device()
+    _check("dct_act8_transpose", lib().dct_act8_transpose(_held(a, "a", dev), _held(out_t, "out_t", dev), _stream(stream)))
+
+
+def dct_gemm8(a, b, c, ld_c, a2=None, b2=None, accumulate=False, stream=None) -> None:
+    code, dev = _dtype_code(c), _current_device()
+    status = lib().dct_gemm8(_held(a, "a", dev), _held(b, "b", dev), _held(a2, "a2", dev), _held(b2, "b2", dev),
+                             _here(c, c.dtype, "c", _span(a.rows, b.rows, ld_c), dev), code, ld_c, 1 if accumulate else 0,
+                             _stream(stream))
+    _check("dct_gemm8", status)
+
+
+def dct_gated8_fwd(x, w_gate, w_up, activation, h=None, h_dense=None, ld_h=0, gate=None, up=None, stream=None) -> None:
+    dev = _current_device()
+    code, dt = (DCT_BF16, None) if h_dense is None else (_dtype_code(h_dense), h_dense.dtype)
+    status = lib().dct_gated8_fwd(_held(x, "x", dev), _held(w_gate, "w_gate", dev), _held(w_up, "w_up", dev), activation,
+                                  _held(h, "h", dev), _here(h_dense, dt, "h_dense", _span(x.rows, w_gate.rows, ld_h), dev), code, ld_h,
+                                  _held(gate, "gate", dev), _held(up, "up", dev), _stream(stream))
+    _check("dct_gated8_fwd", status)
+
+
+def dct_gated8_bwd(dh, ld_dh, gate, up, activation, dgate=None, dup=None, dgate_t=None, dup_t=None, h_t=None, stream=None) -> None:
+    dev = _current_device()
+    code, dt = (DCT_BF16, None) if dh is None else (_dtype_code(dh), dh.dtype)
+    status = lib().dct_gated8_bwd(_here(dh, dt, "dh", _span(gate.rows, gate.cols, ld_dh), dev), code, ld_dh, _held(gate, "gate", dev),
+                                  _held(up, "up", dev), activation, _held(dgate, "dgate", dev), _held(dup, "dup", dev),
+                                  _held(dgate_t, "dgate_t", dev), _held(dup_t, "dup_t", dev), _held(h_t, "h_t", dev), _stream(stream))
+    _check("dct_gated8_bwd", status)

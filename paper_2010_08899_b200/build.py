@@ -13,8 +13,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdct_b200.so")
 SOURCES = ["mp_pack.cu", "mp_pack_span.cu", "mp_pack_f32_wide.cu", "mp_pack_f32.cu", "mp_pack_narrow.cu", "dp_compress.cu", "threshold_select.cu", "threshold_select_batched.cu", "threshold_select_sharded.cu", "decompress.cu", "diagnostics.cu",
-           "dp_select_compress.cu", "lm_norm.cu", "lm_logprobs.cu", "lm_distill.cu", "abi.cu"]          # the slowest to compile first
-HEADERS = [os.path.join(CSRC, h) for h in ("common.cuh", "row_select.cuh", "mp_warp.cuh", "dp_chain.cuh", "lm_rows.cuh", "launch_words.h")] + \
+           "dp_select_compress.cu", "lm_norm.cu", "lm_logprobs.cu", "lm_distill.cu", "gemm8.cu", "act8.cu", "abi.cu"]          # the slowest to compile first
+HEADERS = [os.path.join(CSRC, h) for h in ("common.cuh", "row_select.cuh", "mp_warp.cuh", "dp_chain.cuh", "lm_rows.cuh", "act8.cuh", "launch_words.h")] + \
           [os.path.join(ROOT, "include", "dct.h")]
 
 NVCC_FLAGS = [

@@ -1,0 +1,158 @@
+// Matrices in 8 bits: e4m3 codes with a power of two for every 128 columns of a row (the layout is described in dct.h), shared by the
+// checkpoint kernels and the products.
+#pragma once
+#include <cuda_fp8.h>
+
+#include "lm_rows.cuh"
+
+namespace dct {
+
+constexpr uint32_t kAct8Block = 128;            // columns that share a power
+constexpr uint32_t kAct8ScaleTile = 512;        // bytes of the scales of 128 rows and four blocks
+
+struct Act8 {
+    uint8_t* codes;
+    uint8_t* scales;
+    uint32_t rows, cols, ld;
+    uint32_t row_tiles;          // ceil(rows / 128)
+};
+
+__host__ __device__ __forceinline__ uint32_t ceil_div(uint32_t a, uint32_t b) { return a / b + (a % b != 0); }
+
+__device__ __forceinline__ size_t act8_scale_offset(uint32_t row_tiles, uint32_t row, uint32_t block) {
+    return (static_cast<size_t>(block >> 2) * row_tiles + (row >> 7)) * kAct8ScaleTile + (row & 31u) * 16u + ((row >> 5) & 3u) * 4u + (block & 3u);
+}
+
+// |x| as an integer: ordered as the magnitudes, infinities above every number and NaN above those
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// The byte e + 127 of a block whose largest magnitude has these bits: 448 = 1.75 2^8, so e is the exponent less 8, one more if the fraction is
+// beyond 1.75 (adding 0x1FFFFF carries into the exponent exactly then).  Infinities and NaN: 255.
+__device__ __forceinline__ uint32_t act8_byte(uint32_t largest) {
+    if (largest >= 0x7F800000u) return 255u;
+    const uint32_t e = (largest + 0x1FFFFFu) >> 23;
+    return e > 8u ? e - 8u : 0u;
+}
+// 2^-e (NaN for byte 255) and 2^e
+__device__ __forceinline__ float act8_inverse(uint32_t byte) { return __uint_as_float(byte == 255u ? 0x7FC00000u : (254u - byte) << 23); }
+__device__ __forceinline__ float act8_power(uint32_t byte) {
+    return __uint_as_float(byte == 0u ? 0x00400000u : byte == 255u ? 0x7FC00000u : byte << 23);
+}
+
+// two values to e4m3, to nearest with ties to even, NaN to NaN; lo in the low byte
+__device__ __forceinline__ uint32_t act8_codes2(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t act8_codes4(float a, float b, float c, float d) { return act8_codes2(a, b) | act8_codes2(c, d) << 16; }
+// Four codes of a block with this byte: with the largest power (byte 247), 256 is beyond fp32, and 240 takes its place.
+__device__ __forceinline__ uint32_t act8_finite4(uint32_t codes, uint32_t byte) {
+    return byte == 247u ? __vminu4(codes & 0x7F7F7F7Fu, 0x77777777u) | (codes & 0x80808080u) : codes;
+}
+__device__ __forceinline__ void act8_values2(uint32_t two, float& lo, float& hi) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(two)));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    lo = f.x;
+    hi = f.y;
+}
+
+// p + c for a c that is never quite 0: where the sum is p all the same, the number next to p, away from 0 if `up`.  Products of codes have so
+// few digits that many lie exactly halfway between two codes; a share just below 1 must put them on the right side.
+__device__ __forceinline__ float beside(float p, float c, bool up) {
+    const float s = __fadd_rn(p, c);
+    const bool stuck = s == p && p != 0.0f && fabsf(p) < __uint_as_float(0x7F800000u);
+    return stuck ? __uint_as_float(__float_as_uint(p) + (up ? 1u : 0xFFFFFFFFu)) : s;
+}
+
+// act(g) = g share, share = sigmoid(y).  SILU: y = g; GELU: y = 2 sqrt(2/pi) (g + 0.044715 g^3).  With q = sigmoid(-|y|) the share is q
+// below 0 and 1 - q above, where the products take q as a small correction.
+struct Gate {
+    float g, q, dy;              // dy: the derivative of y
+    __device__ __forceinline__ Gate(float g_, bool gelu) : g(g_), dy(1.0f) {
+        constexpr float kA = 1.5957691216057308f, kB = 0.044715f;
+        float y = g;
+        if (gelu) {
+            const float g2 = __fmul_rn(g, g);
+            y = __fmul_rn(__fmul_rn(kA, g), fmaf(kB, g2, 1.0f));
+            dy = __fmul_rn(kA, fmaf(3.0f * kB, g2, 1.0f));
+        }
+        const float t = exp2_fast(__fmul_rn(-fabsf(y), kLog2E));
+        q = __fdividef(t, __fadd_rn(1.0f, t));
+    }
+    // act(g) x
+    __device__ __forceinline__ float times(float x) const {
+        const float p = __fmul_rn(x, g), low = __fmul_rn(x, __fmul_rn(g, q));
+        return g < 0.0f ? low : beside(p, -low, false);
+    }
+    // act'(g) p
+    __device__ __forceinline__ float slope_times(float p) const {
+        const float gq = __fmul_rn(g, q), more = fmaf(__fadd_rn(g, -gq), dy, -1.0f);
+        const float below = fmaf(__fmul_rn(gq, __fadd_rn(1.0f, -q)), dy, q);
+        return g < 0.0f ? __fmul_rn(p, q == 0.0f ? 0.0f : below) : q == 0.0f ? beside(p, 0.0f, more > 0.0f) : beside(p, __fmul_rn(p, __fmul_rn(q, more)), more > 0.0f);
+    }
+};
+
+// Host side -------------------------------------------------------------------------------------------------------
+
+inline size_t act8_scale_bytes(uint32_t rows, uint32_t cols) {
+    return static_cast<size_t>(ceil_div(rows, 128)) * ceil_div(cols, 512) * kAct8ScaleTile;
+}
+// whether a descriptor can be used as it stands; an empty matrix needs no buffers
+inline bool usable(const dct_act8_t* m) {
+    if (m->rows > DCT_ACT8_MAX_DIM || m->cols > DCT_ACT8_MAX_DIM) return false;
+    if (m->rows == 0 || m->cols == 0) return true;
+    return m->codes && m->scales && aligned_to(m->codes, 16) && aligned_to(m->scales, 16) && m->ld >= m->cols && m->ld % 16 == 0;
+}
+inline Act8 device_view(const dct_act8_t* m) {
+    if (!m) return Act8{nullptr, nullptr, 0, 0, 0, 0};
+    return Act8{static_cast<uint8_t*>(m->codes), static_cast<uint8_t*>(m->scales), m->rows, m->cols, m->ld, ceil_div(m->rows, 128)};
+}
+
+// The buffers of a call: what is written may overlap nothing else.  Rows of one matrix may lie between those of another, side by
+// side in wider rows, as long as they share no byte.
+class Buffers {
+public:
+    void read(const void* p, uint32_t rows, size_t width, size_t stride) { add(p, rows, width, stride, false); }
+    void write(const void* p, uint32_t rows, size_t width, size_t stride) { add(p, rows, width, stride, true); }
+    void read(const dct_act8_t* m) { add(m, false); }
+    void write(const dct_act8_t* m) { add(m, true); }
+    bool clash() const {
+        for (int i = 0; i < n_; ++i)
+            for (int j = 0; j < i; ++j)
+                if ((b_[i].written || b_[j].written) && meet(b_[i], b_[j])) return true;
+        return false;
+    }
+
+private:
+    struct Part {
+        uintptr_t at;
+        size_t rows, width, stride;
+        bool written;
+        size_t span() const { return (rows - 1) * stride + width; }
+    };
+    static bool meet(const Part& a, const Part& b) {
+        if (!(a.at < b.at + b.span() && b.at < a.at + a.span())) return false;
+        // of one stride: side by side if, modulo the stride, one starts where the other has ended
+        if (a.stride == b.stride) {
+            const uintptr_t up = (b.at - a.at) % a.stride, s = a.stride;
+            const uintptr_t apart = b.at >= a.at ? up : (s - (a.at - b.at) % s) % s;
+            if (apart >= a.width && apart + b.width <= s) return false;
+        }
+        return true;
+    }
+    void add(const void* p, uint32_t rows, size_t width, size_t stride, bool written) {
+        if (p && rows && width) b_[n_++] = Part{reinterpret_cast<uintptr_t>(p), rows, width, stride, written};
+    }
+    void add(const dct_act8_t* m, bool written) {
+        if (!m || m->rows == 0 || m->cols == 0) return;
+        add(m->codes, m->rows, m->cols, m->ld, written);
+        const size_t s = act8_scale_bytes(m->rows, m->cols);
+        add(m->scales, 1, s, s, written);
+    }
+    Part b_[24];
+    int n_ = 0;
+};
+
+}  // namespace dct
