@@ -1,88 +1,762 @@
-// Products of matrices in 8 bits, and the gated feed-forward block's first half.
+// Products of matrices in 8 bits, and the gated feed-forward block's first half, on the tensor cores.
+//
+// D = P Q^T with 128 rows of P to the lanes of tensor memory and up to 256 rows of Q to its columns, 128 of depth to a stage of shared memory.
+// The powers enter the tensor cores with the codes (block-scaled products): one byte for a row's 128 of depth, four depths to the word that a
+// scale tile holds for a row, so that 512 bytes per 128 rows serve four stages.  Sums stay in fp32 in tensor memory from the first
+// depth to the last.
+//
+//   wide:  P are C's rows, Q its columns.  A thread has one row of the tile.
+//   few:   rows of C are too few to fill 128 lanes: P are the columns (the weights), Q the rows.  A thread has one column of the tile.
+//   gated, wide:  Q are 128 rows of the gate's weights and the same 128 of up's: a thread has its row's g and u of a whole block.
+//   gated, few:   two P tiles, gate and up, with the same Q, into two accumulators.
+// Where tiles are too few for the device, a cluster of CTAs shares one: each sums a part of the depth, sends every other its columns of the
+// result, and adds up its own columns in the order of the parts.
+#include <cuda.h>
+
 #include "act8.cuh"
 
 namespace dct {
 namespace {
 
-constexpr uint32_t kThreads = 256, kRows = 64, kCols = 128, kDepth = 32;
+constexpr uint32_t kThreads = 320, kEpilogueWarps = 8, kProducerWarp = 8, kProductWarp = 9;
+constexpr uint32_t kDepth = 128;                 // bytes of a row in a stage: one swizzled line of shared memory
+constexpr uint32_t kTileBytes = 128 * kDepth;
+constexpr uint32_t kScaleBuffers = 8;            // of tensor memory, each for one load of scale tiles
+constexpr uint32_t kMaxSplit = 8;
+constexpr uint32_t kLost = 0x7FC00000u;
 
-struct Pair {
-    Act8 a, b;
+constexpr uint32_t power_of_two(uint32_t n) { return n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
+
+template <uint32_t kQ_, bool kFew_, bool kGated_, uint32_t kStages_, bool kSplit_> struct Shape {
+    static constexpr uint32_t kQ = kQ_, kStages = kStages_;
+    static constexpr bool kFew = kFew_, kGated = kGated_, kSplit = kSplit_;
+    static constexpr uint32_t kAcc = kGated && kFew ? 2 : 1;                    // accumulators, each with its P tile
+    static constexpr uint32_t kStageBytes = kAcc * kTileBytes + kQ * kDepth;
+    static constexpr uint32_t kScaleTilesQ = kQ > 128 ? 2 : 1, kScaleTiles = kAcc + kScaleTilesQ;
+    static constexpr uint32_t kScaleBytes = kScaleTiles * kAct8ScaleTile;
+    static constexpr uint32_t kAccCols = kAcc * kQ, kScaleCols = 4 * kScaleTiles;
+    static constexpr uint32_t kTmemCols = power_of_two(kAccCols + kScaleBuffers * kScaleCols);
+    // e4m3 times e4m3, powers as bytes of exponents, 128 by kQ; which byte of a scale word counts goes to bits 4 and 29
+    static constexpr uint32_t kProduct = (kQ >> 3) << 17 | 1u << 23 | (128u >> 4) << 24;
+    static constexpr uint32_t kReceiveBytes = kSplit ? kAcc * kQ * 128 * 4 : 0;
+    static constexpr uint32_t kTurnBytes = kFew ? 0 : kEpilogueWarps * 32 * 17 * 4;      // unaligned rows leave through here
+    static constexpr uint32_t kSharedBytes = 1024 + kStages * (kStageBytes + kScaleBytes) + kReceiveBytes + kTurnBytes;
+    static_assert(kStages <= kScaleBuffers, "a buffer of scales is written anew only after the products that read it");
+    static_assert(kSharedBytes + 4096 <= 232448, "shared memory of a CTA");
 };
 
-__device__ __forceinline__ float value_at(const Act8& m, uint32_t row, uint32_t col) {
-    if (row >= m.rows || col >= m.cols) return 0.0f;
-    float lo, hi;
-    act8_values2(m.codes[static_cast<size_t>(row) * m.ld + col], lo, hi);
-    return __fmul_rn(lo, act8_power(m.scales[act8_scale_offset(m.row_tiles, row, col >> 7)]));
+struct Scales {
+    const uint8_t* at;
+    uint32_t row_tiles;
+};
+
+struct alignas(64) Task {
+    CUtensorMap p[2], q[2];         // plain: of the two products; gated: gate and up where there are two
+    Scales sp[2], sq[2];
+    uint32_t depths[2];             // stages of each product
+    uint32_t p_rows, q_rows;        // of P and Q
+    uint32_t tiles_p, tiles_q;
+    uint32_t split;
+    uint32_t limit;                 // of a bounded wait
+    void* c;
+    uint32_t ld_c;
+    bool bf16, accumulate, aligned, gelu;
+    Act8 h, gate, up;
+};
+
+// ---- tensor memory, tensor cores, tensor copies ----
+
+__device__ __forceinline__ void tmem_alloc(uint32_t* where, uint32_t cols) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(where)), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t cols) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(cols));
+}
+__device__ __forceinline__ void tmem_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// arrives at the barrier once all tensor-core work of this thread so far is done
+__device__ __forceinline__ void tensor_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+// a scale tile (32 rows of 16 bytes) to four columns, once for each 32 lanes
+__device__ __forceinline__ void scales_to_tmem(uint32_t tmem, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void block_scaled_product(uint32_t d, uint64_t p, uint64_t q, uint32_t idesc, uint32_t sp, uint32_t sq, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred a;\n\tsetp.ne.u32 a, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], a;\n\t}"
+        ::"r"(d), "l"(p), "l"(q), "r"(idesc), "r"(sp), "r"(sq), "r"(static_cast<uint32_t>(add)) : "memory");
+}
+__device__ __forceinline__ void tmem_load32(float* v, uint32_t at) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,"
+        "%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(at));
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_load16(float* v, uint32_t at) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(at));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+template <uint32_t kN> __device__ __forceinline__ void tmem_load(float* v, uint32_t at) {
+    if constexpr (kN == 16) {
+        tmem_load16(v, at);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < kN; i += 32) tmem_load32(v + i, at + i);
+    }
+}
+// what was loaded may be used from here on
+template <uint32_t kN> __device__ __forceinline__ void tmem_loaded(float* v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (uint32_t i = 0; i < kN; ++i) asm volatile("" : "+f"(v[i]));
 }
 
-// acc += the tile's part of A B^T; a thread has rows 4 rg .. and columns 8 cx ..
-__device__ void multiply(float (&acc)[4][8], const Act8& a, const Act8& b, uint32_t row0, uint32_t col0) {
-    __shared__ float sa[kDepth][kRows + 1], sb[kDepth][kCols + 1];
-    const uint32_t cx = threadIdx.x & 15u, rg = threadIdx.x >> 4;
-    for (uint32_t k0 = 0; k0 < a.cols; k0 += kDepth) {
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < kRows * kDepth; i += kThreads) sa[i % kDepth][i / kDepth] = value_at(a, row0 + i / kDepth, k0 + i % kDepth);
-        for (uint32_t i = threadIdx.x; i < kCols * kDepth; i += kThreads) sb[i % kDepth][i / kDepth] = value_at(b, col0 + i / kDepth, k0 + i % kDepth);
-        __syncthreads();
-        for (uint32_t k = 0; k < kDepth; ++k) {
+__device__ __forceinline__ void tile_load(void* smem, const CUtensorMap* map, uint32_t x, uint32_t y, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(smem_addr(smem)), "l"(map), "r"(x), "r"(y), "r"(smem_addr(bar)) : "memory");
+}
+
+// Descriptors of shared memory.  Tiles: rows of 128 bytes, swizzled by 128 bytes, groups of eight rows 1024 bytes apart; 32 of depth further is 32 bytes
+// further.  Scale tiles: not swizzled, groups of eight rows (of 16 bytes) 128 bytes apart.
+__device__ __forceinline__ uint64_t tile_desc(const void* smem) {
+    return static_cast<uint64_t>((smem_addr(smem) & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ uint64_t scale_desc(const void* smem) {
+    return static_cast<uint64_t>((smem_addr(smem) & 0x3FFFFu) >> 4) | (8ull << 32) | (1ull << 46);
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t peer_address(uint32_t smem, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void st_peer(uint32_t at, float x) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory"); }
+
+// ---- what is written ----
+
+__device__ __forceinline__ void st32(void* p, const uint32_t (&w)[8]) {           // 32 bytes, a whole sector
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
+                 "r"(w[6]), "r"(w[7]) : "memory");
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// One element, added to what is there if asked for
+template <typename T> __device__ __forceinline__ void put(T* to, float x, bool accumulate) {
+    *to = from_f32<T>(accumulate ? __fadd_rn(to_f32(*to), x) : x);
+}
+// kN (a multiple of 8) neighbouring elements of a row, the first `count` of which are there.  aligned: `to` is on a 32-byte boundary (16 for
+// eight bf16).
+template <typename T, uint32_t kN> __device__ __forceinline__ void put_row(T* to, const float* v, uint32_t count, bool accumulate) {
+    constexpr uint32_t E = sizeof(T) == 4 ? 8 : kN >= 16 ? 16 : 8;
 #pragma unroll
-            for (uint32_t r = 0; r < 4; ++r)
+    for (uint32_t j = 0; j < kN; j += E) {
+        if (j + E <= count) {
+            float x[E];
 #pragma unroll
-                for (uint32_t c = 0; c < 8; ++c) acc[r][c] = fmaf(sa[k][rg * 4 + r], sb[k][cx * 8 + c], acc[r][c]);
+            for (uint32_t i = 0; i < E; ++i) x[i] = accumulate ? __fadd_rn(to_f32(to[j + i]), v[j + i]) : v[j + i];
+            if constexpr (sizeof(T) == 4) {
+                uint32_t w[8];
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) w[i] = __float_as_uint(x[i]);
+                st32(to + j, w);
+            } else if constexpr (E == 16) {
+                uint32_t w[8];
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+                st32(to + j, w);
+            } else {
+                st_unit(to + j, make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])));
+            }
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < E; ++i)
+                if (j + i < count) put(to + j + i, v[j + i], accumulate);
         }
     }
 }
-
-template <typename T>
-__global__ void __launch_bounds__(kThreads) gemm8_kernel(const Pair one, const Pair two, T* c, uint32_t m, uint32_t n, uint32_t ld_c, bool accumulate) {
-    const uint32_t row0 = blockIdx.y * kRows, col0 = blockIdx.x * kCols;
-    float acc[4][8] = {};
-    multiply(acc, one.a, one.b, row0, col0);
-    if (two.a.codes) multiply(acc, two.a, two.b, row0, col0);
-    const uint32_t cx = threadIdx.x & 15u, rg = threadIdx.x >> 4;
-    for (uint32_t r = 0; r < 4; ++r)
-        for (uint32_t k = 0; k < 8; ++k) {
-            const uint32_t row = row0 + rg * 4 + r, col = col0 + cx * 8 + k;
-            if (row >= m || col >= n) continue;
-            T* to = c + static_cast<size_t>(row) * ld_c + col;
-            *to = from_f32<T>(accumulate ? __fadd_rn(to_f32(*to), acc[r][k]) : acc[r][k]);
+// The same for 32 rows of a warp that start on no boundary: turned in shared memory, so that neighbouring lanes store neighbouring elements.
+template <typename T, uint32_t kN>
+__device__ __forceinline__ void put_rows_turned(T* c, uint32_t ld, uint32_t row0, uint32_t rows, const float* v, uint32_t col0, uint32_t cols,
+                                                bool accumulate, float* turn) {
+    constexpr uint32_t W = kN < 16 ? kN : 16;
+    const uint32_t lane = lane_id();
+#pragma unroll
+    for (uint32_t j = 0; j < kN; j += W) {
+        __syncwarp();
+#pragma unroll
+        for (uint32_t i = 0; i < W; ++i) turn[lane * 17 + i] = v[j + i];
+        __syncwarp();
+        const uint32_t col = col0 + j + lane % W;
+        if (col < cols) {
+#pragma unroll 4
+            for (uint32_t r = lane / W; r < 32 && row0 + r < rows; r += 32 / W)
+                put(c + static_cast<size_t>(row0 + r) * ld + col, turn[r * 17 + lane % W], accumulate);
         }
+    }
 }
-
-__device__ void hold(const float (&v)[8], const Act8& out, uint32_t row, uint32_t col) {
+template <uint32_t kN>
+__device__ __forceinline__ void put_dense(const Task& task, uint32_t row0, uint32_t rows, const float* v, uint32_t col0, uint32_t cols, float* turn) {
+    if (task.aligned) {
+        const uint32_t row = row0 + lane_id();
+        if (row >= rows || col0 >= cols) return;
+        const size_t at = static_cast<size_t>(row) * task.ld_c + col0;
+        if (task.bf16)
+            put_row<__nv_bfloat16, kN>(static_cast<__nv_bfloat16*>(task.c) + at, v, cols - col0, task.accumulate);
+        else
+            put_row<float, kN>(static_cast<float*>(task.c) + at, v, cols - col0, task.accumulate);
+    } else if (task.bf16) {
+        put_rows_turned<__nv_bfloat16, kN>(static_cast<__nv_bfloat16*>(task.c), task.ld_c, row0, rows, v, col0, cols, task.accumulate, turn);
+    } else {
+        put_rows_turned<float, kN>(static_cast<float*>(task.c), task.ld_c, row0, rows, v, col0, cols, task.accumulate, turn);
+    }
+}
+__device__ __forceinline__ void put_one(const Task& task, uint32_t row, uint32_t col, float x) {
+    const size_t at = static_cast<size_t>(row) * task.ld_c + col;
+    if (task.bf16)
+        put(static_cast<__nv_bfloat16*>(task.c) + at, x, task.accumulate);
+    else
+        put(static_cast<float*>(task.c) + at, x, task.accumulate);
+}
+// 64 neighbouring values of a row as codes, the first `count` of which are there
+__device__ __forceinline__ void hold64(const Act8& out, uint32_t row, uint32_t col, const float* v, uint32_t count, uint32_t byte) {
+    const float inverse = act8_inverse(byte);
+    uint8_t* to = out.codes + static_cast<size_t>(row) * out.ld + col;
+#pragma unroll
+    for (uint32_t j = 0; j < 64; j += 16) {
+        uint32_t w[4];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const float* x = v + j + 4 * i;
+            w[i] = act8_finite4(act8_codes4(__fmul_rn(x[0], inverse), __fmul_rn(x[1], inverse), __fmul_rn(x[2], inverse), __fmul_rn(x[3], inverse)), byte);
+        }
+        if (j + 16 <= count) {
+            st_unit(to + j, make_uint4(w[0], w[1], w[2], w[3]));
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i)
+                if (j + i < count) to[j + i] = static_cast<uint8_t>(w[i / 4] >> (8 * (i % 4)));
+        }
+    }
+}
+__device__ __forceinline__ uint32_t largest64(const float* v) {
     uint32_t m = 0;
-    for (uint32_t k = 0; k < 8; ++k) m = max(m, col + k < out.cols ? magnitude(v[k]) : 0u);
-    for (uint32_t o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-    if (row >= out.rows) return;
-    const uint32_t byte = act8_byte(m);
-    for (uint32_t k = 0; k < 8; ++k)
-        if (col + k < out.cols) out.codes[static_cast<size_t>(row) * out.ld + col + k] = static_cast<uint8_t>(act8_finite4(act8_codes2(__fmul_rn(v[k], act8_inverse(byte)), 0.0f), byte));
-    if (col % 128 == 0) out.scales[act8_scale_offset(out.row_tiles, row, col >> 7)] = static_cast<uint8_t>(byte);
+#pragma unroll
+    for (uint32_t j = 0; j < 64; ++j) m = max(m, magnitude(v[j]));
+    return m;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) gated8_kernel(const Act8 x, const Act8 w_gate, const Act8 w_up, bool gelu, const Act8 h, T* dense,
-                                                          uint32_t ld_h, const Act8 gate, const Act8 up) {
-    const uint32_t row0 = blockIdx.y * kRows, col0 = blockIdx.x * kCols;
-    float g[4][8] = {}, u[4][8] = {};
-    multiply(g, x, w_gate, row0, col0);
-    multiply(u, x, w_up, row0, col0);
-    const uint32_t cx = threadIdx.x & 15u, rg = threadIdx.x >> 4;
-    for (uint32_t r = 0; r < 4; ++r) {
-        const uint32_t row = row0 + rg * 4 + r, col = col0 + cx * 8;
-        float v[8];
-        for (uint32_t k = 0; k < 8; ++k) v[k] = Gate(g[r][k], gelu).times(u[r][k]);
-        if (gate.codes) {
-            hold(g[r], gate, row, col);
-            hold(u[r], up, row, col);
+// ---- the kernel ----
+
+struct Tile {
+    uint32_t p, q;
+};
+// Tiles in bands of eight P tiles, Q outermost within a band: what runs at a time reads few different rows of either.
+__device__ __forceinline__ Tile tile_at(const Task& task, uint32_t t) {
+    const uint32_t band = t / (8 * task.tiles_q), first = band * 8, in = t - band * 8 * task.tiles_q, height = min(8u, task.tiles_p - first);
+    return Tile{first + in % height, in / height};
+}
+
+template <typename S> struct Shared {
+    uint64_t full[S::kStages], empty[S::kStages], done, free, drained;
+    uint32_t tmem, stop;
+    uint32_t largest[S::kGated ? (S::kFew ? 2 * 3 * (S::kQ / 2) * 4 : 3 * 2 * 128) : 1];
+};
+
+// A few rows' g and u of one column each: the first `count` of the rows row0 .. .  The block of a row is the 128 lanes of a warp group.
+template <typename S, uint32_t kN>
+__device__ __forceinline__ void finish_few_gated(const Task& task, Shared<S>& sh, float (&g)[kN], float (&u)[kN], uint32_t count, uint32_t row0,
+                                                 uint32_t col, uint32_t group, uint32_t quarter, bool ok) {
+    const uint32_t f = task.p_rows, rows = task.q_rows;
+    float h[kN];
+    uint32_t* largest = sh.largest + group * (3 * kN * 4);
+#pragma unroll
+    for (uint32_t j = 0; j < kN; ++j) {
+        // (beyond the last column the powers are anything: what stands there is no number)
+        g[j] = !ok ? __uint_as_float(kLost) : col < f ? g[j] : 0.0f;
+        u[j] = col < f ? u[j] : 0.0f;
+        h[j] = Gate(g[j], task.gelu).times(u[j]);
+        if (j < count) {
+            const uint32_t mg = __reduce_max_sync(0xFFFFFFFFu, magnitude(g[j])), mu = __reduce_max_sync(0xFFFFFFFFu, magnitude(u[j])),
+                           mh = __reduce_max_sync(0xFFFFFFFFu, magnitude(h[j]));
+            if (lane_id() == 0) {
+                largest[j * 4 + quarter] = mg;
+                largest[(kN + j) * 4 + quarter] = mu;
+                largest[(2 * kN + j) * 4 + quarter] = mh;
+            }
         }
-        if (h.codes) hold(v, h, row, col);
-        if (dense && row < x.rows)
-            for (uint32_t k = 0; k < 8; ++k)
-                if (col + k < w_gate.rows) dense[static_cast<size_t>(row) * ld_h + col + k] = from_f32<T>(v[k]);
     }
+    named_barrier_sync(1 + group, 128);
+    const auto hold = [&](const Act8& m, uint32_t which, uint32_t j, float x) {
+        const uint32_t* l = largest + (which * kN + j) * 4;
+        const uint32_t byte = act8_byte(max(max(l[0], l[1]), max(l[2], l[3])));
+        const uint32_t row = row0 + j;
+        m.codes[static_cast<size_t>(row) * m.ld + col] = static_cast<uint8_t>(act8_finite4(act8_codes2(__fmul_rn(x, act8_inverse(byte)), 0.0f), byte));
+        if ((col & 127u) == 0) m.scales[act8_scale_offset(m.row_tiles, row, col >> 7)] = static_cast<uint8_t>(byte);
+    };
+#pragma unroll
+    for (uint32_t j = 0; j < kN; ++j) {
+        if (j >= count || row0 + j >= rows || col >= f) continue;
+        if (task.gate.codes) {
+            hold(task.gate, 0, j, g[j]);
+            hold(task.up, 1, j, u[j]);
+        }
+        if (task.h.codes) hold(task.h, 2, j, h[j]);
+        if (task.c) put_one(task, row0 + j, col, h[j]);
+    }
+    named_barrier_sync(1 + group, 128);          // before the next tile's are written
+}
+
+template <typename S>
+__global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_constant__ Task task) {
+    extern __shared__ uint8_t raw[];
+    __shared__ Shared<S> sh;
+    uint8_t* tiles = raw + ((1024u - (smem_addr(raw) & 1023u)) & 1023u);
+    uint8_t* scales = tiles + S::kStages * S::kStageBytes;
+    float* receive = reinterpret_cast<float*>(scales + S::kStages * S::kScaleBytes);
+    float* turns = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(receive) + S::kReceiveBytes);
+
+    const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
+    const uint32_t split = S::kSplit ? task.split : 1u, rank = split > 1 ? cluster_rank() : 0u;
+    const uint32_t all = task.depths[0] + task.depths[1];
+    const uint32_t begin = static_cast<uint32_t>(static_cast<uint64_t>(all) * rank / split);
+    const uint32_t end = static_cast<uint32_t>(static_cast<uint64_t>(all) * (rank + 1) / split);
+    const uint32_t tile0 = blockIdx.x / split, step = gridDim.x / split, tile_count = task.tiles_p * task.tiles_q;
+
+    if (threadIdx.x == 0) {
+        for (uint32_t i = 0; i < S::kStages; ++i) {
+            mbar_init(&sh.full[i], 1);
+            mbar_init(&sh.empty[i], 1);
+        }
+        mbar_init(&sh.done, 1);
+        mbar_init(&sh.free, kEpilogueWarps);
+        mbar_init(&sh.drained, 1);
+        sh.stop = 0;
+        mbar_init_fence();
+    }
+    if (warp == kProductWarp) tmem_alloc(&sh.tmem, S::kTmemCols);
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    if (split > 1) cluster_arrive();             // (waited for before anything is sent to a peer)
+    const uint32_t tmem = sh.tmem;
+    const volatile uint32_t* stop = &sh.stop;
+    const auto give_up = [&] { *const_cast<volatile uint32_t*>(&sh.stop) = 1u; };
+
+    if (warp == kProducerWarp) {
+        if (lane == 0) {
+            uint32_t stage = 0, phase = 0, issued = 0;
+            bool ok = true;
+            for (uint32_t t = tile0; ok && t < tile_count; t += step) {
+                const Tile at = tile_at(task, t);
+                for (uint32_t it = begin; it < end; ++it) {
+                    if (!mbar_wait_bounded(&sh.empty[stage], phase ^ 1u, task.limit, stop)) {
+                        ok = false;
+                        give_up();
+                        break;
+                    }
+                    const uint32_t second = !S::kGated && it >= task.depths[0] ? 1u : 0u, kb = second ? it - task.depths[0] : it;
+                    const bool with_scales = it == begin || (kb & 3u) == 0;
+                    uint8_t* tile = tiles + stage * S::kStageBytes;
+                    uint8_t* sc = scales + stage * S::kScaleBytes;
+                    uint64_t* bar = &sh.full[stage];
+                    const bool two = S::kScaleTilesQ == 2 && (S::kGated || 2 * at.q + 1 < task.sq[second].row_tiles);
+                    mbar_arrive_expect_tx(bar, S::kStageBytes + (with_scales ? (S::kAcc + 1 + two) * kAct8ScaleTile : 0));
+#pragma unroll
+                    for (uint32_t i = 0; i < S::kAcc; ++i) tile_load(tile + i * kTileBytes, &task.p[S::kAcc == 2 ? i : second], kb * kDepth, at.p * 128u, bar);
+                    uint8_t* q = tile + S::kAcc * kTileBytes;
+                    if constexpr (S::kGated && !S::kFew) {
+                        tile_load(q, &task.q[0], kb * kDepth, at.q * 128u, bar);
+                        tile_load(q + kTileBytes, &task.q[1], kb * kDepth, at.q * 128u, bar);
+                    } else {
+                        tile_load(q, &task.q[second], kb * kDepth, at.q * S::kQ, bar);
+                    }
+                    if (with_scales) {
+                        const auto scale_tile = [&](const Scales& s, uint32_t row_tile) {
+                            return s.at + (static_cast<size_t>(kb >> 2) * s.row_tiles + row_tile) * kAct8ScaleTile;
+                        };
+#pragma unroll
+                        for (uint32_t i = 0; i < S::kAcc; ++i)
+                            bulk_load(sc + i * kAct8ScaleTile, scale_tile(task.sp[S::kAcc == 2 ? i : second], at.p), kAct8ScaleTile, bar);
+                        sc += S::kAcc * kAct8ScaleTile;
+                        if constexpr (S::kGated && !S::kFew) {
+                            bulk_load(sc, scale_tile(task.sq[0], at.q), kAct8ScaleTile, bar);
+                            bulk_load(sc + kAct8ScaleTile, scale_tile(task.sq[1], at.q), kAct8ScaleTile, bar);
+                        } else if constexpr (S::kQ >= 128) {
+                            bulk_load(sc, scale_tile(task.sq[second], at.q * (S::kQ / 128)), kAct8ScaleTile, bar);
+                            if (two) bulk_load(sc + kAct8ScaleTile, scale_tile(task.sq[second], at.q * 2 + 1), kAct8ScaleTile, bar);
+                        } else {
+                            bulk_load(sc, scale_tile(task.sq[second], 0), kAct8ScaleTile, bar);       // (there is one Q tile, at row 0)
+                        }
+                    }
+                    ++issued;
+                    if (++stage == S::kStages) stage = 0, phase ^= 1u;
+                }
+            }
+            if (!ok) {             // what is in flight lands before the CTA ends
+                for (uint32_t i = min(issued, S::kStages); i > 0; --i) {
+                    const uint32_t n = issued - i;
+                    for (uint32_t k = 0; k < task.limit && !mbar_try_wait(&sh.full[n % S::kStages], (n / S::kStages) & 1u); ++k) {}
+                }
+            }
+        }
+    } else if (warp == kProductWarp) {
+        if (lane == 0) {
+            uint32_t stage = 0, phase = 0, free_phase = 1, buffer = 0;
+            bool ok = true;
+            for (uint32_t t = tile0; ok && t < tile_count; t += step) {
+                ok = mbar_wait_bounded(&sh.free, free_phase, task.limit, stop);
+                free_phase ^= 1u;
+                tmem_after_sync();
+                for (uint32_t it = begin; ok && it < end; ++it) {
+                    ok = mbar_wait_bounded(&sh.full[stage], phase, task.limit, stop);
+                    if (!ok) break;
+                    tmem_after_sync();
+                    const uint32_t kb = !S::kGated && it >= task.depths[0] ? it - task.depths[0] : it;
+                    if (it == begin || (kb & 3u) == 0) {
+                        buffer = (buffer + 1u) % kScaleBuffers;
+                        const uint64_t from = scale_desc(scales + stage * S::kScaleBytes);
+#pragma unroll
+                        for (uint32_t i = 0; i < S::kScaleTiles; ++i)
+                            scales_to_tmem(tmem + S::kAccCols + buffer * S::kScaleCols + 4 * i, from + i * (kAct8ScaleTile >> 4));
+                    }
+                    const uint32_t idesc = S::kProduct | (kb & 3u) << 4 | (kb & 3u) << 29;
+                    const uint32_t sf = tmem + S::kAccCols + buffer * S::kScaleCols;
+                    const uint64_t p = tile_desc(tiles + stage * S::kStageBytes), q = p + S::kAcc * (kTileBytes >> 4);
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k)
+#pragma unroll
+                        for (uint32_t i = 0; i < S::kAcc; ++i)
+                            block_scaled_product(tmem + i * S::kQ, p + i * (kTileBytes >> 4) + 2 * k, q + 2 * k, idesc, sf + 4 * i, sf + 4 * S::kAcc,
+                                                 it != begin || k != 0);
+                    tensor_commit(&sh.empty[stage]);
+                    if (++stage == S::kStages) stage = 0, phase ^= 1u;
+                }
+                if (ok) tensor_commit(&sh.done);
+            }
+            if (!ok) {
+                give_up();
+                tensor_commit(&sh.drained);
+                for (uint32_t k = 0; k < task.limit && !mbar_try_wait(&sh.drained, 0); ++k) {}
+            }
+        }
+    } else {
+        const uint32_t group = warp >> 2, row_lane = (warp & 3u) * 32u + lane, lanes = tmem + ((warp & 3u) << 21);
+        float* turn = S::kFew ? nullptr : turns + warp * (32 * 17);
+        uint32_t done_phase = 0;
+        bool ok = true;
+        for (uint32_t t = tile0; t < tile_count; t += step) {
+            const Tile at = tile_at(task, t);
+            if (ok && !mbar_wait_bounded(&sh.done, done_phase, task.limit, stop)) {
+                ok = false;
+                give_up();
+            }
+            done_phase ^= 1u;
+            tmem_after_sync();
+            const uint32_t p0 = at.p * 128u, q0 = at.q * (S::kGated && !S::kFew ? 128u : S::kQ);
+            const auto accumulator_read = [&] {
+                tmem_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.free);
+            };
+            if (split > 1) {
+                // this part's columns to the CTAs that add them up
+                const uint32_t slice = S::kQ / split;
+                cluster_wait();
+#pragma unroll
+                for (uint32_t a = 0; a < S::kAcc; ++a) {
+                    float v[S::kQ / 2];
+                    tmem_load<S::kQ / 2>(v, lanes + a * S::kQ + group * (S::kQ / 2));
+                    tmem_loaded<S::kQ / 2>(v);
+#pragma unroll
+                    for (uint32_t j = 0; j < S::kQ / 2; ++j) {
+                        const uint32_t col = group * (S::kQ / 2) + j, to = col / slice;
+                        st_peer(peer_address(smem_addr(receive + ((rank * S::kAcc + a) * slice + col % slice) * 128u + row_lane), to),
+                                ok ? v[j] : __uint_as_float(kLost));
+                    }
+                }
+                break;             // (one tile to a cluster)
+            }
+            if constexpr (S::kFew && !S::kGated) {
+                float v[S::kQ / 2];
+                tmem_load<S::kQ / 2>(v, lanes + group * (S::kQ / 2));
+                tmem_loaded<S::kQ / 2>(v);
+                accumulator_read();
+#pragma unroll
+                for (uint32_t j = 0; j < S::kQ / 2; ++j) {
+                    const uint32_t row = q0 + group * (S::kQ / 2) + j;
+                    if (row < task.q_rows && p0 + row_lane < task.p_rows) put_one(task, row, p0 + row_lane, ok ? v[j] : __uint_as_float(kLost));
+                }
+            } else if constexpr (!S::kGated) {
+                float v[S::kQ / 2];
+                tmem_load<S::kQ / 2>(v, lanes + group * (S::kQ / 2));
+                tmem_loaded<S::kQ / 2>(v);
+                accumulator_read();
+                if (!ok) {
+#pragma unroll
+                    for (uint32_t j = 0; j < S::kQ / 2; ++j) v[j] = __uint_as_float(kLost);
+                }
+                put_dense<S::kQ / 2>(task, p0 + (warp & 3u) * 32u, task.p_rows, v, q0 + group * (S::kQ / 2), task.q_rows, turn);
+            } else if constexpr (!S::kFew) {
+                float g[64], u[64];
+                tmem_load<64>(g, lanes + group * 64);
+                tmem_load<64>(u, lanes + 128 + group * 64);
+                tmem_loaded<64>(g);
+                tmem_loaded<64>(u);
+                accumulator_read();
+                const uint32_t row = p0 + row_lane, col = q0 + group * 64, count = col < task.q_rows ? task.q_rows - col : 0;
+#pragma unroll
+                for (uint32_t j = 0; j < 64; ++j) {
+                    // (beyond the last column the powers are anything: what stands there is no number)
+                    g[j] = !ok ? __uint_as_float(kLost) : j < count ? g[j] : 0.0f;
+                    u[j] = j < count ? u[j] : 0.0f;
+                }
+                const bool writes = row < task.p_rows && count > 0;
+                // the largest of the other 64 columns comes from the other warp group
+                const auto join = [&](uint32_t which, uint32_t m) { sh.largest[(which * 2 + group) * 128 + row_lane] = m; };
+                const auto joined = [&](uint32_t which) { return max(sh.largest[which * 256 + row_lane], sh.largest[which * 256 + 128 + row_lane]); };
+                const auto scale = [&](const Act8& m, uint32_t byte) {
+                    if (writes && group == 0) m.scales[act8_scale_offset(m.row_tiles, row, at.q)] = static_cast<uint8_t>(byte);
+                };
+                if (task.gate.codes) {
+                    join(0, largest64(g));
+                    join(1, largest64(u));
+                    named_barrier_sync(1, kEpilogueWarps * 32);
+                    const uint32_t bg = act8_byte(joined(0)), bu = act8_byte(joined(1));
+                    if (writes) {
+                        hold64(task.gate, row, col, g, count, bg);
+                        hold64(task.up, row, col, u, count, bu);
+                    }
+                    scale(task.gate, bg);
+                    scale(task.up, bu);
+                }
+#pragma unroll
+                for (uint32_t j = 0; j < 64; ++j) g[j] = Gate(g[j], task.gelu).times(u[j]);
+                if (task.h.codes) {
+                    join(2, largest64(g));
+                    named_barrier_sync(1, kEpilogueWarps * 32);
+                    const uint32_t bh = act8_byte(joined(2));
+                    if (writes) hold64(task.h, row, col, g, count, bh);
+                    scale(task.h, bh);
+                }
+                if (task.h.codes || task.gate.codes) named_barrier_sync(1, kEpilogueWarps * 32);          // before the next tile's are written
+                if (task.c) put_dense<64>(task, p0 + (warp & 3u) * 32u, task.p_rows, g, col, task.q_rows, turn);
+            }
+            if constexpr (S::kGated && S::kFew) {
+                float g[S::kQ / 2], u[S::kQ / 2];
+                tmem_load<S::kQ / 2>(g, lanes + group * (S::kQ / 2));
+                tmem_load<S::kQ / 2>(u, lanes + S::kQ + group * (S::kQ / 2));
+                tmem_loaded<S::kQ / 2>(g);
+                tmem_loaded<S::kQ / 2>(u);
+                accumulator_read();
+                finish_few_gated<S>(task, sh, g, u, S::kQ / 2, q0 + group * (S::kQ / 2), p0 + row_lane, group, warp & 3u, ok);
+            }
+        }
+    }
+    __syncwarp();
+    if (split > 1) {
+        // every thread of the cluster meets here; then each CTA adds up its own columns
+        if (warp >= kEpilogueWarps) cluster_wait();
+        cluster_arrive();
+        cluster_wait();
+        if (warp < kEpilogueWarps) {
+            const Tile at = tile_at(task, tile0);
+            const uint32_t group = warp >> 2, row_lane = (warp & 3u) * 32u + lane, slice = S::kQ / split, half = slice / 2;
+            const uint32_t p0 = at.p * 128u, q0 = at.q * S::kQ + rank * slice + group * half;
+            const auto sum = [&](uint32_t a, uint32_t j) {
+                float s = receive[(a * slice + group * half + j) * 128u + row_lane];
+                for (uint32_t k = 1; k < split; ++k) s = __fadd_rn(s, receive[((k * S::kAcc + a) * slice + group * half + j) * 128u + row_lane]);
+                return s;
+            };
+            if constexpr (S::kGated) {
+                float g[S::kQ / 2], u[S::kQ / 2];
+#pragma unroll
+                for (uint32_t j = 0; j < S::kQ / 2; ++j) {
+                    g[j] = j < half ? sum(0, j) : 0.0f;
+                    u[j] = j < half ? sum(1, j) : 0.0f;
+                }
+                finish_few_gated<S>(task, sh, g, u, half, q0, p0 + row_lane, group, warp & 3u, true);
+            } else if constexpr (S::kFew) {
+                for (uint32_t j = 0; j < half; ++j)
+                    if (q0 + j < task.q_rows && p0 + row_lane < task.p_rows) put_one(task, q0 + j, p0 + row_lane, sum(0, j));
+            } else {
+                float* turn = turns + warp * (32 * 17);
+                for (uint32_t j = 0; j < half; j += 8) {
+                    float v[8];
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) v[i] = sum(0, j + i);
+                    put_dense<8>(task, p0 + (warp & 3u) * 32u, task.p_rows, v, q0 + j, task.q_rows, turn);
+                }
+            }
+        }
+    }
+    tmem_before_sync();
+    __syncthreads();
+    if (warp == kProductWarp) {
+        tmem_after_sync();
+        tmem_free(tmem, S::kTmemCols);
+    }
+}
+
+// ---- host ----
+
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                            const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+dct_status_t encoder(Encode* out) {
+    static std::atomic<Encode> kept{nullptr};
+    Encode e = kept.load(std::memory_order_acquire);
+    if (!e) {
+        void* found = nullptr;
+        cudaDriverEntryPointQueryResult how = cudaDriverEntryPointSymbolNotFound;
+        DCT_CUDA_TRY(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &found, 12000, cudaEnableDefault, &how));
+        if (how != cudaDriverEntryPointSuccess || !found) return DCT_ERR_UNSUPPORTED;
+        e = reinterpret_cast<Encode>(found);
+        kept.store(e, std::memory_order_release);
+    }
+    *out = e;
+    return DCT_OK;
+}
+
+// codes in boxes of 128 bytes by `rows` rows; zeros outside the matrix
+dct_status_t encode(Encode e, CUtensorMap* map, const dct_act8_t* m, uint32_t rows) {
+    const cuuint64_t size[2] = {m->cols, m->rows}, stride[1] = {m->ld};
+    const cuuint32_t box[2] = {kDepth, rows}, unit[2] = {1, 1};
+    const CUresult r = e(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, m->codes, size, stride, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? DCT_OK : DCT_ERR_INVALID_ARG;
+}
+Scales scales_of(const dct_act8_t* m) { return Scales{static_cast<const uint8_t*>(m->scales), ceil_div(m->rows, 128)}; }
+
+// How many CTAs share a tile's depth: as many as leave each at least four stages, as long as all clusters run at once.
+template <typename S> dct_status_t split_of(uint64_t tiles, uint32_t depths, uint32_t* split) {
+    static ClusterCounts counts;
+    *split = 1;
+    for (uint32_t s = 2; S::kSplit && s <= kMaxSplit && depths >= 4 * s; s *= 2) {
+        uint32_t at_once = 0;
+        const dct_status_t st = clusters_at_once(product8_kernel<S>, kThreads, s, S::kSharedBytes, counts, &at_once);
+        if (st != DCT_OK) return st;
+        if (tiles > at_once) break;
+        *split = s;
+    }
+    return DCT_OK;
+}
+
+template <typename S> dct_status_t launch(Task& task, uint32_t sms, cudaStream_t stream) {
+    static SharedLimit allowed;
+    dct_status_t st = allow_shared(product8_kernel<S>, S::kSharedBytes, allowed);
+    if (st != DCT_OK) return st;
+    const uint64_t tiles = static_cast<uint64_t>(task.tiles_p) * task.tiles_q;
+    if (tiles > 0x3FFFFFFFull) return DCT_ERR_UNSUPPORTED;
+    if ((st = split_of<S>(tiles, task.depths[0] + task.depths[1], &task.split)) != DCT_OK) return st;
+    if (task.split > 1) {
+        DCT_CUDA_TRY(launch_clusters(product8_kernel<S>, static_cast<unsigned>(tiles) * task.split, kThreads, task.split, S::kSharedBytes, stream, task));
+    } else {
+        product8_kernel<S><<<static_cast<unsigned>(tiles < sms ? tiles : sms), kThreads, S::kSharedBytes, stream>>>(task);
+        DCT_CUDA_TRY(cudaGetLastError());
+    }
+    return DCT_OK;
+}
+
+using Wide256 = Shape<256, false, false, 4, false>;
+using Wide128 = Shape<128, false, false, 4, true>;
+using Few32 = Shape<32, true, false, 8, true>;
+using Few64 = Shape<64, true, false, 7, true>;
+using GatedWide = Shape<256, false, true, 4, false>;
+using GatedFew32 = Shape<32, true, true, 5, true>;
+using GatedFew64 = Shape<64, true, true, 3, true>;
+
+dct_status_t product(const dct_act8_t* const (&a)[2], const dct_act8_t* const (&b)[2], void* c, dct_dtype_t dtype, uint32_t ld_c, bool accumulate,
+                     cudaStream_t stream) {
+    Encode e = nullptr;
+    dct_status_t st = encoder(&e);
+    if (st != DCT_OK) return st;
+    const int sms = sm_count();
+    if (sms <= 0) return DCT_ERR_CUDA;
+    const uint32_t m = a[0]->rows, n = b[0]->rows, count = a[1] ? 2 : 1;
+    Task task = {};
+    task.limit = debug_config().spin_limit;
+    task.c = c;
+    task.ld_c = ld_c;
+    task.bf16 = dtype == DCT_BF16;
+    task.accumulate = accumulate;
+    task.aligned = aligned_to(c, 32) && static_cast<size_t>(ld_c) * element_size(dtype) % 32 == 0;
+    // Up to 64 rows: the columns take the lanes.  Else tiles of 128 x 256, or of 128 x 128 where those are too few to go round twice.
+    const bool few = m <= 64;
+    const uint64_t wide_tiles = static_cast<uint64_t>(ceil_div(m, 128)) * ceil_div(n, 256);
+    const uint32_t q = few ? (m <= 32 ? 32 : 64) : wide_tiles >= 2ull * sms ? 256 : 128;
+    for (uint32_t i = 0; i < count; ++i) {
+        const dct_act8_t *p_side = few ? b[i] : a[i], *q_side = few ? a[i] : b[i];
+        if ((st = encode(e, &task.p[i], p_side, 128)) != DCT_OK || (st = encode(e, &task.q[i], q_side, q)) != DCT_OK) return st;
+        task.sp[i] = scales_of(p_side);
+        task.sq[i] = scales_of(q_side);
+        task.depths[i] = ceil_div(a[i]->cols, kDepth);
+    }
+    task.p_rows = few ? n : m;
+    task.q_rows = few ? m : n;
+    task.tiles_p = ceil_div(task.p_rows, 128);
+    task.tiles_q = ceil_div(task.q_rows, q);
+    return q == 32 ? launch<Few32>(task, sms, stream) : q == 64 ? launch<Few64>(task, sms, stream)
+         : q == 128 ? launch<Wide128>(task, sms, stream) : launch<Wide256>(task, sms, stream);
+}
+
+dct_status_t gated(const dct_act8_t* x, const dct_act8_t* w_gate, const dct_act8_t* w_up, bool gelu, const dct_act8_t* h, void* h_dense, dct_dtype_t dtype,
+                   uint32_t ld_h, const dct_act8_t* gate, const dct_act8_t* up, cudaStream_t stream) {
+    Encode e = nullptr;
+    dct_status_t st = encoder(&e);
+    if (st != DCT_OK) return st;
+    const int sms = sm_count();
+    if (sms <= 0) return DCT_ERR_CUDA;
+    const uint32_t rows = x->rows, f = w_gate->rows;
+    Task task = {};
+    task.limit = debug_config().spin_limit;
+    task.c = h_dense;
+    task.ld_c = ld_h;
+    task.bf16 = dtype == DCT_BF16;
+    task.aligned = aligned_to(h_dense, 32) && static_cast<size_t>(ld_h) * element_size(dtype) % 32 == 0;
+    task.gelu = gelu;
+    task.h = device_view(h);
+    task.gate = device_view(gate);
+    task.up = device_view(up);
+    task.depths[0] = ceil_div(x->cols, kDepth);
+    const bool few = rows <= 64;
+    const uint32_t q = rows <= 32 ? 32 : 64;
+    CUtensorMap* weights = few ? task.p : task.q;
+    Scales* weight_scales = few ? task.sp : task.sq;
+    if ((st = encode(e, weights, w_gate, 128)) != DCT_OK || (st = encode(e, weights + 1, w_up, 128)) != DCT_OK ||
+        (st = encode(e, few ? task.q : task.p, x, few ? q : 128)) != DCT_OK)
+        return st;
+    weight_scales[0] = scales_of(w_gate);
+    weight_scales[1] = scales_of(w_up);
+    (few ? task.sq : task.sp)[0] = scales_of(x);
+    task.p_rows = few ? f : rows;
+    task.q_rows = few ? rows : f;
+    task.tiles_p = ceil_div(task.p_rows, 128);
+    task.tiles_q = few ? 1 : ceil_div(f, 128);
+    return !few ? launch<GatedWide>(task, sms, stream) : q == 32 ? launch<GatedFew32>(task, sms, stream) : launch<GatedFew64>(task, sms, stream);
 }
 
 }  // namespace
@@ -107,16 +781,18 @@ extern "C" dct_status_t dct_gemm8(const dct_act8_t* a, const dct_act8_t* b, cons
     all.read(a2);
     all.read(b2);
     if (all.clash()) return DCT_ERR_INVALID_ARG;
-    const dim3 grid(ceil_div(n, kCols), ceil_div(m, kRows));
-    if (grid.y > 65535u) return DCT_ERR_UNSUPPORTED;
+    const dct_act8_t *as[2] = {a, a2}, *bs[2] = {b, b2};
+    if (a2 && a2->cols == 0) as[1] = bs[1] = nullptr;
+    if (a->cols == 0) {
+        as[0] = as[1], bs[0] = bs[1];
+        as[1] = bs[1] = nullptr;
+    }
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    const Pair one{device_view(a), device_view(b)}, two{device_view(a2), device_view(b2)};
-    if (dtype == DCT_F32)
-        gemm8_kernel<<<grid, kThreads, 0, stream>>>(one, two, static_cast<float*>(c), m, n, ld_c, accumulate != 0);
-    else
-        gemm8_kernel<<<grid, kThreads, 0, stream>>>(one, two, static_cast<__nv_bfloat16*>(c), m, n, ld_c, accumulate != 0);
-    DCT_CUDA_TRY(cudaGetLastError());
-    return DCT_OK;
+    if (!as[0]) {             // no depth: the product is zero
+        if (!accumulate) DCT_CUDA_TRY(cudaMemset2DAsync(c, ld_c * es, 0, n * es, m, stream));
+        return DCT_OK;
+    }
+    return product(as, bs, c, dtype, ld_c, accumulate != 0, stream);
 }
 
 extern "C" dct_status_t dct_gated8_fwd(const dct_act8_t* x, const dct_act8_t* w_gate, const dct_act8_t* w_up, dct_activation_t activation,
@@ -126,7 +802,7 @@ extern "C" dct_status_t dct_gated8_fwd(const dct_act8_t* x, const dct_act8_t* w_
     if (!x || !w_gate || !w_up || !usable(x) || !usable(w_gate) || !usable(w_up)) return DCT_ERR_INVALID_ARG;
     const uint32_t rows = x->rows, d = x->cols, f = w_gate->rows;
     const auto is = [](const dct_act8_t* m, uint32_t r, uint32_t c) { return usable(m) && m->rows == r && m->cols == c; };
-    if (w_gate->cols != d || !is(w_up, f, d) || (!h && !h_dense) || (gate == nullptr) != (up == nullptr) || (h && !is(h, rows, f)) ||
+    if (d == 0 || w_gate->cols != d || !is(w_up, f, d) || (!h && !h_dense) || (gate == nullptr) != (up == nullptr) || (h && !is(h, rows, f)) ||
         (gate && (!is(gate, rows, f) || !is(up, rows, f))))
         return DCT_ERR_INVALID_ARG;
     const size_t es = element_size(dtype);
@@ -141,15 +817,5 @@ extern "C" dct_status_t dct_gated8_fwd(const dct_act8_t* x, const dct_act8_t* w_
     all.write(gate);
     all.write(up);
     if (all.clash()) return DCT_ERR_INVALID_ARG;
-    const dim3 grid(ceil_div(f, kCols), ceil_div(rows, kRows));
-    if (grid.y > 65535u) return DCT_ERR_UNSUPPORTED;
-    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    if (dtype == DCT_F32)
-        gated8_kernel<<<grid, kThreads, 0, stream>>>(device_view(x), device_view(w_gate), device_view(w_up), activation == DCT_ACT_GELU,
-            device_view(h), static_cast<float*>(h_dense), ld_h, device_view(gate), device_view(up));
-    else
-        gated8_kernel<<<grid, kThreads, 0, stream>>>(device_view(x), device_view(w_gate), device_view(w_up), activation == DCT_ACT_GELU,
-            device_view(h), static_cast<__nv_bfloat16*>(h_dense), ld_h, device_view(gate), device_view(up));
-    DCT_CUDA_TRY(cudaGetLastError());
-    return DCT_OK;
+    return gated(x, w_gate, w_up, activation == DCT_ACT_GELU, h, h_dense, dtype, ld_h, gate, up, static_cast<cudaStream_t>(stream_));
 }

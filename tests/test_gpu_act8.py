@@ -205,6 +205,24 @@ def test_product(m, n, k, dtype):
         assert np.linalg.norm(got - want) <= (1e-5 + HALF[dtype]) * np.linalg.norm(want)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", [(2400, 4200, 900), (300, 40000, 260), (60, 20000, 300), (128, 300, 20000), (4100, 520, 8200)])
+def test_product_of_many_tiles_or_great_depth(m, n, k, dtype):
+    """More tiles than the device has SMs, and depths that several CTAs share; compared in 64 bits on the device."""
+    a, b = matrix(m, k, 1), matrix(n, k, 2)
+    va, vb = torch.from_numpy(o.values(a)).to(DEV), torch.from_numpy(o.values(b)).to(DEV)
+    want, size = va @ vb.T, va.abs() @ vb.abs().T
+    c = torch.empty(m, n, dtype=dtype, device=DEV)
+    pa, pb = put(a), put(b)
+    B.dct_gemm8(pa, pb, c, n)
+    off = (c.double() - want).abs()
+    assert bool((off <= (k + 2) * 2.0 ** -23 * size * (1 + HALF[dtype]) + HALF[dtype] * want.abs()).all())
+    assert float(off.norm() / want.norm()) <= 1e-5 + HALF[dtype]
+    again = torch.empty_like(c)
+    B.dct_gemm8(pa, pb, again, n)
+    assert torch.equal(c, again)
+
+
 @pytest.mark.parametrize("m,n,k,k2", [(1, 100, 64, 700), (20, 300, 513, 129), (70, 200, 1, 1), (150, 300, 640, 1100), (260, 520, 1300, 2)])
 def test_two_products_added_to_what_is_there(m, n, k, k2):
     a, b, a2, b2 = matrix(m, k, 1), matrix(n, k, 2), matrix(m, k2, 3), matrix(n, k2, 4)
@@ -268,7 +286,7 @@ def test_product_of_far_apart_powers():
 
 # ---- the gated block ----
 
-GATED = [(1, 128, 64), (3, 700, 130), (16, 512, 1000), (40, 300, 129), (64, 96, 257), (100, 1, 1), (130, 256, 384), (300, 640, 520)]
+GATED = [(2, 200, 20000), (900, 130, 2500), (1, 128, 64), (3, 700, 130), (16, 512, 1000), (40, 300, 129), (64, 96, 257), (100, 1, 1), (130, 256, 384), (300, 640, 520), (9, 2100, 300)]
 
 
 def near_held(got: o.Held, want, off):
