@@ -1,242 +1,352 @@
 // Checkpoints in 8 bits: written from fp32 or bf16 by rows and / or transposed, read back, transposed; and the backward pass of the gated
 // block, which reads two of them and writes up to five.
 //
-// A CTA takes tiles of 128 x 128 elements, so that both a row's block and, in the transpose, a column's block are its own.  A thread holds a
-// patch of eight rows and eight columns in registers: sixteen neighbouring lanes hold a row's block, and the thread's own eight bytes of a
-// column are contiguous in the transpose.  The largest magnitude of a row's block is a maximum over sixteen lanes; that of a column's block
-// goes through shared memory, as do the transposed codes, which leave it as whole rows of 128 bytes.
+// All but the reading back work on tiles of 128 x 128 elements, so that both a row's block and, in the transpose, a column's block are the tile's
+// own.  A CTA goes from tile to tile; tensor copies bring the next tile's inputs into shared memory while this one is worked on.  A warp has eight
+// rows of the tile, a lane four columns of them: a row's largest magnitude is one reduction over the warp, a column's goes through shared
+// memory, and a lane's eight codes of a column lie next to each other in the transpose, which leaves shared memory as rows of 128 bytes.
 #include "act8.cuh"
 
 namespace dct {
 namespace {
 
-constexpr uint32_t kTileThreads = 256;
-constexpr uint32_t kPatch = 8;
+constexpr uint32_t kTileThreads = 512, kWarps = kTileThreads / 32;
+constexpr uint32_t kR = 8, kC = 4;                   // a lane's rows and columns
+constexpr uint32_t kTurnedBytes = 128 * 128;         // a plane's transposed codes
 
-struct Place {
-    uint32_t row0, col0;         // of the tile
-    uint32_t row, col;           // of the thread's patch
-    uint32_t cx, rg;             // the patch's number among the columns and the rows
-};
-__device__ __forceinline__ Place place_of(uint32_t tile_row, uint32_t tile_col) {
-    const uint32_t lane = threadIdx.x & 31u, cx = lane & 15u, rg = (threadIdx.x >> 5) * 2u + (lane >> 4);
-    return Place{tile_row * 128u, tile_col * 128u, tile_row * 128u + rg * kPatch, tile_col * 128u + cx * kPatch, cx, rg};
-}
-
-struct TileShared {
-    uint32_t largest[8][128];          // per warp and column, then row 0: the columns' bytes
-    uint8_t codes[128 * 128];          // transposed: [column][row], groups of eight rows exchanged by column
+struct TileTask {
+    CUtensorMap map[3];
+    Act8 held[2];                // inputs in 8 bits (their scales)
+    const void* x;               // a dense input whose rows start on no boundary
+    uint32_t ld_x;
+    bool direct, gelu;           // direct: x is not fetched by tensor copies (or is not there)
+    uint32_t rows, cols, tiles_r, tiles_c;
+    uint32_t limit;
+    Act8 by_rows[2], turned[3];  // outputs by plane
 };
 
-// The patch's rows as blocks of 128 columns
-__device__ __forceinline__ void write_rows(const float (&v)[kPatch][kPatch], const Act8& out, const Place& at) {
-    const uint32_t block = at.col0 >> 7;
+// Four neighbouring elements
+template <typename T> __device__ __forceinline__ void four(float (&v)[kC], const T* p);
+template <> __device__ __forceinline__ void four(float (&v)[kC], const float* p) {
+    const float4 w = *reinterpret_cast<const float4*>(p);
+    v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
+}
+template <> __device__ __forceinline__ void four(float (&v)[kC], const __nv_bfloat16* p) {
+    const uint2 w = *reinterpret_cast<const uint2*>(p);
+    v[0] = __uint_as_float(w.x << 16), v[1] = __uint_as_float(w.x & 0xFFFF0000u), v[2] = __uint_as_float(w.y << 16), v[3] = __uint_as_float(w.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void four(float (&v)[kC], uint32_t codes, float power) {
+    act8_values2(codes & 0xFFFFu, v[0], v[1]);
+    act8_values2(codes >> 16, v[2], v[3]);
 #pragma unroll
-    for (uint32_t r = 0; r < kPatch; ++r) {
-        uint32_t m = 0;
-#pragma unroll
-        for (uint32_t c = 0; c < kPatch; ++c) m = max(m, magnitude(v[r][c]));
-#pragma unroll
-        for (uint32_t o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-        const uint32_t byte = act8_byte(m), row = at.row + r;
-        if (row >= out.rows) continue;
-        const float inverse = act8_inverse(byte);
-        uint2 q;
-        q.x = act8_codes4(__fmul_rn(v[r][0], inverse), __fmul_rn(v[r][1], inverse), __fmul_rn(v[r][2], inverse), __fmul_rn(v[r][3], inverse));
-        q.y = act8_codes4(__fmul_rn(v[r][4], inverse), __fmul_rn(v[r][5], inverse), __fmul_rn(v[r][6], inverse), __fmul_rn(v[r][7], inverse));
-        q = make_uint2(act8_finite4(q.x, byte), act8_finite4(q.y, byte));
-        uint8_t* to = out.codes + static_cast<size_t>(row) * out.ld + at.col;
-        if (at.col + kPatch <= out.cols) {
-            *reinterpret_cast<uint2*>(to) = q;
-        } else {
-            for (uint32_t c = 0; at.col + c < out.cols; ++c) to[c] = static_cast<uint8_t>((c < 4 ? q.x >> (8 * c) : q.y >> (8 * c - 32)));
-        }
-        if (at.cx == 0) out.scales[act8_scale_offset(out.row_tiles, row, block)] = static_cast<uint8_t>(byte);
-    }
+    for (uint32_t c = 0; c < kC; ++c) v[c] = __fmul_rn(v[c], power);
 }
 
-// The patch's columns as blocks of 128 rows of the transpose
-__device__ __forceinline__ void write_columns(const float (&v)[kPatch][kPatch], const Act8& out, const Place& at, TileShared& sh) {
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
-    __syncthreads();                 // the last plane's readers are done
+// A dense tile whose rows start on no boundary, into the place a tensor copy would have put it: every warp its own rows, neighbouring lanes
+// neighbouring elements, zeros outside.
+template <typename T>
+__device__ __forceinline__ void fetch_rows(T* tile, const TileTask& task, uint32_t row0, uint32_t col0) {
+    const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
+    const T* x = static_cast<const T*>(task.x);
 #pragma unroll
-    for (uint32_t c = 0; c < kPatch; ++c) {
-        uint32_t m = 0;
+    for (uint32_t r = 0; r < kR; ++r) {
+        const uint32_t row = row0 + warp * kR + r;
+        const T* from = x + static_cast<size_t>(row) * task.ld_x + col0;
+        T* to = tile + (warp * kR + r) * 128u;
 #pragma unroll
-        for (uint32_t r = 0; r < kPatch; ++r) m = max(m, magnitude(v[r][c]));
-        m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
-        if (lane < 16) sh.largest[warp][at.cx * kPatch + c] = m;
-    }
-    __syncthreads();
-    if (threadIdx.x < 128) {
-        uint32_t m = 0;
-#pragma unroll
-        for (uint32_t w = 0; w < 8; ++w) m = max(m, sh.largest[w][threadIdx.x]);
-        const uint32_t byte = act8_byte(m), row = at.col0 + threadIdx.x;
-        if (row < out.rows) out.scales[act8_scale_offset(out.row_tiles, row, at.row0 >> 7)] = static_cast<uint8_t>(byte);
-        sh.largest[0][threadIdx.x] = byte;
-    }
-    __syncthreads();
-#pragma unroll
-    for (uint32_t c = 0; c < kPatch; ++c) {
-        const uint32_t byte = sh.largest[0][at.cx * kPatch + c];
-        const float inverse = act8_inverse(byte);
-        uint2 q;
-        q.x = act8_codes4(__fmul_rn(v[0][c], inverse), __fmul_rn(v[1][c], inverse), __fmul_rn(v[2][c], inverse), __fmul_rn(v[3][c], inverse));
-        q.y = act8_codes4(__fmul_rn(v[4][c], inverse), __fmul_rn(v[5][c], inverse), __fmul_rn(v[6][c], inverse), __fmul_rn(v[7][c], inverse));
-        q = make_uint2(act8_finite4(q.x, byte), act8_finite4(q.y, byte));
-        // (a half-warp's sixteen patches write sixteen different groups: no two to the same bank)
-        *reinterpret_cast<uint2*>(sh.codes + (at.cx * kPatch + c) * 128u + ((at.rg ^ at.cx) << 3)) = q;
-    }
-    __syncthreads();
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-        const uint32_t c = i * 16u + (threadIdx.x >> 4), group = threadIdx.x & 15u;
-        const uint32_t row = at.col0 + c, col = at.row0 + group * 8u;           // of the transpose
-        if (row >= out.rows || col >= out.cols) continue;
-        const uint2 q = *reinterpret_cast<const uint2*>(sh.codes + c * 128u + ((group ^ (c >> 3)) << 3));
-        uint8_t* to = out.codes + static_cast<size_t>(row) * out.ld + col;
-        if (col + 8 <= out.cols) {
-            *reinterpret_cast<uint2*>(to) = q;
-        } else {
-            for (uint32_t k = 0; col + k < out.cols; ++k) to[k] = static_cast<uint8_t>((k < 4 ? q.x >> (8 * k) : q.y >> (8 * k - 32)));
+        for (uint32_t k = 0; k < 4; ++k) {
+            const uint32_t c = lane + 32u * k;
+            to[c] = row < task.rows && col0 + c < task.cols ? from[c] : from_f32<T>(0.0f);
         }
     }
+    __syncwarp();
 }
 
-// A dense matrix: eight elements of one row, zeros outside.  aligned: rows start on 16-byte boundaries.
+// What a tile's planes are made of.  load(): the lane's patch of each plane; power: of the lane's row (lane & 7) of each held input.
 template <typename T> struct Dense {
-    const T* x;
-    uint32_t rows, cols, ld;
-    bool aligned;
-    __device__ __forceinline__ void load(float (&v)[kPatch], uint32_t row, uint32_t col) const {
-        const T* p = x + static_cast<size_t>(row) * ld + col;
-        if (row < rows && aligned && col + kPatch <= cols) {
-            constexpr uint32_t E = Unit<T>::kElems;
+    static constexpr uint32_t kPlanes = 1, kHeld = 0, kDenseBytes = 128 * 128 * sizeof(T), kCtas = sizeof(T) == 4 ? 1 : 2;
+    using Element = T;
+    __device__ static __forceinline__ void load(float (&v)[1][kR][kC], const uint8_t* stage, const float*, bool) {
+        const T* from = reinterpret_cast<const T*>(stage) + (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
 #pragma unroll
-            for (uint32_t u = 0; u < kPatch / E; ++u) {
-                const uint4 w = ld_unit(reinterpret_cast<const uint4*>(p) + u);
-#pragma unroll
-                for (uint32_t i = 0; i < E; ++i) v[u * E + i] = Unit<T>::get(w, i);
-            }
-        } else {
-#pragma unroll
-            for (uint32_t i = 0; i < kPatch; ++i) v[i] = row < rows && col + i < cols ? to_f32(p[i]) : 0.0f;
-        }
+        for (uint32_t r = 0; r < kR; ++r) four<T>(v[0][r], from + r * 128);
     }
 };
-
-// Eight values of a row of a matrix in 8 bits, zeros outside.  (Rows start on 16-byte boundaries and are as long as a multiple of 16, so
-// the eight codes can be read together wherever one of them counts.)
-__device__ __forceinline__ uint2 act8_load(const Act8& m, uint32_t row, uint32_t col) {
-    if (row >= m.rows || col >= m.cols) return make_uint2(0, 0);
-    uint2 q = *reinterpret_cast<const uint2*>(m.codes + static_cast<size_t>(row) * m.ld + col);
-    if (col + kPatch > m.cols) {
-        const uint32_t n = m.cols - col;          // 1 to 7
-        q.x = n >= 4 ? q.x : q.x & ((1u << 8 * n) - 1u);
-        q.y = n <= 4 ? 0u : q.y & ((1u << (8 * n - 32)) - 1u);
-    }
-    return q;
-}
-__device__ __forceinline__ float act8_power_at(const Act8& m, uint32_t row, uint32_t col) {
-    return row < m.rows && col < m.cols ? act8_power(m.scales[act8_scale_offset(m.row_tiles, row, col >> 7)]) : 0.0f;
-}
-__device__ __forceinline__ void act8_values(float (&v)[kPatch], const uint2& q, float power) {
-#pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) {
-        const uint32_t w = i < 2 ? q.x : q.y;
-        float lo, hi;
-        act8_values2(i & 1 ? w >> 16 : w & 0xFFFFu, lo, hi);
-        v[2 * i] = __fmul_rn(lo, power);
-        v[2 * i + 1] = __fmul_rn(hi, power);
-    }
-}
-
 struct Held {
-    Act8 a;
-    __device__ __forceinline__ void load(float (&v)[kPatch], uint32_t row, uint32_t col) const {
-        act8_values(v, act8_load(a, row, col), act8_power_at(a, row, col));
+    static constexpr uint32_t kPlanes = 1, kHeld = 1, kDenseBytes = 0, kCtas = 2;
+    using Element = float;
+    __device__ static __forceinline__ void load(float (&v)[1][kR][kC], const uint8_t* stage, const float* power, bool) {
+        const uint8_t* from = stage + (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
+#pragma unroll
+        for (uint32_t r = 0; r < kR; ++r) four(v[0][r], *reinterpret_cast<const uint32_t*>(from + r * 128), __shfl_sync(0xFFFFFFFFu, power[0], r));
+    }
+};
+// dh, gate and up; the planes are dgate, dup and h
+template <typename T> struct Gated {
+    static constexpr uint32_t kPlanes = 3, kHeld = 2, kDenseBytes = 128 * 128 * sizeof(T), kCtas = 1;
+    using Element = T;
+    __device__ static __forceinline__ void load(float (&v)[3][kR][kC], const uint8_t* stage, const float* power, bool gelu) {
+        const uint32_t at = (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
+#pragma unroll
+        for (uint32_t r = 0; r < kR; ++r) {
+            float d[kC], g[kC], u[kC];
+            four<T>(d, reinterpret_cast<const T*>(stage) + at + r * 128);
+            four(g, *reinterpret_cast<const uint32_t*>(stage + kDenseBytes + at + r * 128), __shfl_sync(0xFFFFFFFFu, power[0], r));
+            four(u, *reinterpret_cast<const uint32_t*>(stage + kDenseBytes + 128 * 128 + at + r * 128), __shfl_sync(0xFFFFFFFFu, power[1], r));
+#pragma unroll
+            for (uint32_t c = 0; c < kC; ++c) {
+                const Gate a(g[c], gelu);
+                v[0][r][c] = __fmul_rn(__fmul_rn(d[c], u[c]), a.slope);
+                v[1][r][c] = __fmul_rn(d[c], a.value);
+                v[2][r][c] = __fmul_rn(a.value, u[c]);
+            }
+        }
     }
 };
 
-template <typename Source>
-__global__ void __launch_bounds__(kTileThreads, 2) act8_write_kernel(const Source source, const Act8 out, const Act8 out_t) {
-    __shared__ TileShared sh;
-    const Place at = place_of(blockIdx.y, blockIdx.x);
-    float v[kPatch][kPatch];
-#pragma unroll
-    for (uint32_t r = 0; r < kPatch; ++r) source.load(v[r], at.row + r, at.col);
-    if (out.codes) write_rows(v, out, at);
-    if (out_t.codes) write_columns(v, out_t, at, sh);
+template <typename S> struct TileShape {
+    static constexpr uint32_t kStageBytes = S::kDenseBytes + S::kHeld * 128 * 128;
+    static constexpr uint32_t kLargestBytes = S::kPlanes * kWarps * 128 * 4;
+    static constexpr uint32_t kSharedBytes = 128 + 2 * kStageBytes + kLargestBytes;
+    static_assert(kStageBytes >= S::kPlanes * kTurnedBytes, "the transposed codes take the place of a tile's inputs");
+};
+
+__device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d, float inverse, uint32_t byte) {
+    return act8_finite4(act8_codes4(__fmul_rn(a, inverse), __fmul_rn(b, inverse), __fmul_rn(c, inverse), __fmul_rn(d, inverse)), byte);
 }
 
+// A lane's patch of a plane by rows
+__device__ __forceinline__ void write_rows(const float (&v)[kR][kC], const Act8& out, uint32_t row0, uint32_t col0) {
+    const uint32_t lane = lane_id(), col = col0 + lane * kC;
+#pragma unroll
+    for (uint32_t r = 0; r < kR; ++r) {
+        const uint32_t m = max(max(magnitude(v[r][0]), magnitude(v[r][1])), max(magnitude(v[r][2]), magnitude(v[r][3])));
+        const uint32_t byte = act8_byte(__reduce_max_sync(0xFFFFFFFFu, m)), row = row0 + r;
+        if (row >= out.rows) break;
+        const uint32_t q = codes_of(v[r][0], v[r][1], v[r][2], v[r][3], act8_inverse(byte), byte);
+        uint8_t* to = out.codes + static_cast<size_t>(row) * out.ld + col;
+        if (col + kC <= out.cols) {
+            *reinterpret_cast<uint32_t*>(to) = q;
+        } else {
+            for (uint32_t c = 0; col + c < out.cols; ++c) to[c] = static_cast<uint8_t>(q >> (8 * c));
+        }
+        if (lane == r) out.scales[act8_scale_offset(out.row_tiles, row, col0 >> 7)] = static_cast<uint8_t>(byte);
+    }
+}
+
+template <typename S>
+__global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const __grid_constant__ TileTask task) {
+    using Shape = TileShape<S>;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t arrived[2];
+    __shared__ alignas(16) uint32_t bytes[S::kPlanes][128];
+    __shared__ uint32_t stop;
+    uint8_t* stages = raw + ((128u - (smem_addr(raw) & 127u)) & 127u);
+    uint32_t* largest = reinterpret_cast<uint32_t*>(stages + 2 * Shape::kStageBytes);       // [plane][warp][column]
+    const uint32_t warp = threadIdx.x >> 5, lane = lane_id(), tiles = task.tiles_r * task.tiles_c;
+    const bool copied = S::kHeld != 0 || !task.direct;
+    if (threadIdx.x == 0) {
+        mbar_init(&arrived[0], 1);
+        mbar_init(&arrived[1], 1);
+        stop = 0;
+        mbar_init_fence();
+    }
+    const auto fetch = [&](uint32_t t, uint32_t s) {
+        const uint32_t x = t % task.tiles_c * 128u, y = t / task.tiles_c * 128u;
+        uint8_t* to = stages + s * Shape::kStageBytes;
+        const bool dense = S::kDenseBytes != 0 && !task.direct;
+        mbar_arrive_expect_tx(&arrived[s], (dense ? S::kDenseBytes : 0u) + S::kHeld * 128 * 128);
+        if (dense) tile_load(to, &task.map[0], x, y, &arrived[s]);
+#pragma unroll
+        for (uint32_t i = 0; i < S::kHeld; ++i) tile_load(to + S::kDenseBytes + i * 128 * 128, &task.map[1 + i], x, y, &arrived[s]);
+    };
+    if (threadIdx.x == 0 && copied && blockIdx.x < tiles) fetch(blockIdx.x, 0);
+    __syncthreads();
+    uint32_t s = 0, phase = 0;
+    bool ok = true;
+    for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+        const uint32_t col0 = t % task.tiles_c * 128u, row0 = t / task.tiles_c * 128u;
+        if (threadIdx.x == 0 && copied && ok && t + gridDim.x < tiles) fetch(t + gridDim.x, s ^ 1u);
+        uint8_t* stage = stages + s * Shape::kStageBytes;
+        // the powers of the warp's rows: lane r has row r's
+        float power[S::kHeld + 1];
+#pragma unroll
+        for (uint32_t i = 0; i < S::kHeld; ++i) {
+            const uint32_t row = row0 + warp * kR + (lane & 7u);
+            power[i] = row < task.rows ? act8_power(task.held[i].scales[act8_scale_offset(task.held[i].row_tiles, row, col0 >> 7)]) : 0.0f;
+        }
+        if (S::kDenseBytes != 0 && task.direct && task.x) fetch_rows(reinterpret_cast<typename S::Element*>(stage), task, row0, col0);
+        if (copied && ok && !mbar_wait_bounded(&arrived[s], phase, task.limit, &stop)) {
+            ok = false;
+            *const_cast<volatile uint32_t*>(&stop) = 1u;
+            if (threadIdx.x == 0) {             // what is still on its way lands before anything else happens here
+                for (uint32_t n = 0; n < task.limit && !mbar_try_wait(&arrived[s], phase); ++n) {}
+                for (uint32_t n = 0; t + gridDim.x < tiles && n < task.limit && !mbar_try_wait(&arrived[s ^ 1u], phase ^ s); ++n) {}
+            }
+        }
+        float v[S::kPlanes][kR][kC];
+        S::load(v, stage, power, task.gelu);
+        if (!ok) {
+#pragma unroll
+            for (uint32_t p = 0; p < S::kPlanes; ++p)
+#pragma unroll
+                for (uint32_t r = 0; r < kR; ++r) v[p][r][0] = __uint_as_float(0x7FC00000u);
+        }
+        bool any_turned = false;
+#pragma unroll
+        for (uint32_t p = 0; p < S::kPlanes; ++p) {
+            if (p < 2 && task.by_rows[p].codes) write_rows(v[p], task.by_rows[p], row0 + warp * kR, col0);
+            if (!task.turned[p].codes) continue;
+            any_turned = true;
+            uint32_t m[kC] = {};
+#pragma unroll
+            for (uint32_t r = 0; r < kR; ++r)
+#pragma unroll
+                for (uint32_t c = 0; c < kC; ++c) m[c] = max(m[c], magnitude(v[p][r][c]));
+            *reinterpret_cast<uint4*>(largest + (p * kWarps + warp) * 128u + lane * kC) = make_uint4(m[0], m[1], m[2], m[3]);
+        }
+        __syncthreads();
+        if (any_turned) {
+            if (threadIdx.x < S::kPlanes * 128u) {
+                const uint32_t p = threadIdx.x >> 7, c = threadIdx.x & 127u;
+                if (task.turned[p].codes) {
+                    uint32_t m = 0;
+#pragma unroll
+                    for (uint32_t w = 0; w < kWarps; ++w) m = max(m, largest[(p * kWarps + w) * 128u + c]);
+                    const uint32_t byte = act8_byte(m);
+                    bytes[p][c] = byte;
+                    if (col0 + c < task.cols) task.turned[p].scales[act8_scale_offset(task.turned[p].row_tiles, col0 + c, row0 >> 7)] = static_cast<uint8_t>(byte);
+                }
+            }
+            __syncthreads();
+            // (a half-warp's sixteen lanes write sixteen different groups: no two to the same bank)
+#pragma unroll
+            for (uint32_t p = 0; p < S::kPlanes; ++p) {
+                if (!task.turned[p].codes) continue;
+                const uint4 b = *reinterpret_cast<const uint4*>(&bytes[p][lane * kC]);
+                uint8_t* to = stage + p * kTurnedBytes + ((warp ^ (lane & 15u)) << 3);
+#pragma unroll
+                for (uint32_t c = 0; c < kC; ++c) {
+                    const uint32_t byte = c == 0 ? b.x : c == 1 ? b.y : c == 2 ? b.z : b.w;
+                    const float inverse = act8_inverse(byte);
+                    *reinterpret_cast<uint2*>(to + (lane * kC + c) * 128u) =
+                        make_uint2(codes_of(v[p][0][c], v[p][1][c], v[p][2][c], v[p][3][c], inverse, byte),
+                                   codes_of(v[p][4][c], v[p][5][c], v[p][6][c], v[p][7][c], inverse, byte));
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (uint32_t p = 0; p < S::kPlanes; ++p) {
+                const Act8& out = task.turned[p];
+                if (!out.codes) continue;
+#pragma unroll
+                for (uint32_t i = 0; i < 128u * 8u / kTileThreads; ++i) {
+                    const uint32_t c = i * (kTileThreads / 8u) + (threadIdx.x >> 3), pair = threadIdx.x & 7u, key = (c >> 2) & 15u;
+                    const uint32_t row = col0 + c, col = row0 + pair * 16u;           // of the transpose
+                    if (row >= out.rows || col >= out.cols) continue;
+                    uint4 q = *reinterpret_cast<const uint4*>(stage + p * kTurnedBytes + c * 128u + (((2u * pair) ^ (key & 14u)) << 3));
+                    if (key & 1u) q = make_uint4(q.z, q.w, q.x, q.y);
+                    uint8_t* to = out.codes + static_cast<size_t>(row) * out.ld + col;
+                    if (col + 16 <= out.cols) {
+                        st_unit(to, q);
+                    } else {
+                        for (uint32_t k = 0; col + k < out.cols; ++k)
+                            to[k] = static_cast<uint8_t>((k < 8 ? (k < 4 ? q.x : q.y) : (k < 12 ? q.z : q.w)) >> (8 * (k & 3u)));
+                    }
+                }
+            }
+        }
+        fence_proxy_async_smem();            // this stage is written by copies again
+        __syncthreads();
+        if (!copied) continue;
+        s ^= 1u;
+        if (s == 0) phase ^= 1u;
+    }
+}
+
+// Reading back: a warp has eight rows of 128 columns, a lane four of them.  Rows of y that start on no boundary are stored with neighbouring lanes at
+// neighbouring elements.
 template <typename T>
-__global__ void __launch_bounds__(kTileThreads) act8_unpack_kernel(const Act8 a, T* y, const uint32_t ld_y, const bool aligned) {
-    const Place at = place_of(blockIdx.y, blockIdx.x);
+__global__ void __launch_bounds__(256) act8_unpack_kernel(const Act8 a, T* y, const uint32_t ld_y, const uint32_t tiles_c, const bool aligned) {
+    __shared__ T turn[8][128];
+    const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
+    const uint32_t row0 = blockIdx.x / tiles_c * 64u + warp * kR, col0 = blockIdx.x % tiles_c * 128u, col = col0 + lane * kC;
+    const uint8_t* from = a.codes + static_cast<size_t>(row0) * a.ld + col;
+    const uint8_t* scales = a.scales + act8_scale_offset(a.row_tiles, row0, col0 >> 7);        // (eight rows of a scale tile are 16 bytes apart)
+    uint32_t q[kR];
+    float power = 0.0f;
+    if (row0 + (lane & 7u) < a.rows) power = act8_power(scales[(lane & 7u) * 16u]);
 #pragma unroll
-    for (uint32_t r = 0; r < kPatch; ++r) {
-        const uint32_t row = at.row + r;
-        if (row >= a.rows || at.col >= a.cols) continue;
-        float v[kPatch];
-        act8_values(v, act8_load(a, row, at.col), act8_power_at(a, row, at.col));
-        T* to = y + static_cast<size_t>(row) * ld_y + at.col;
-        if (aligned && at.col + kPatch <= a.cols) {
-            constexpr uint32_t E = Unit<T>::kElems;
+    for (uint32_t r = 0; r < kR; ++r) q[r] = row0 + r < a.rows && col < a.cols ? *reinterpret_cast<const uint32_t*>(from + static_cast<size_t>(r) * a.ld) : 0u;
 #pragma unroll
-            for (uint32_t u = 0; u < kPatch / E; ++u) {
-                float g[E];
-#pragma unroll
-                for (uint32_t i = 0; i < E; ++i) g[i] = v[u * E + i];
-                st_unit(to + u * E, Unit<T>::pack(g));
+    for (uint32_t r = 0; r < kR; ++r) {
+        float v[kC];
+        four(v, q[r], __shfl_sync(0xFFFFFFFFu, power, r));
+        if (row0 + r >= a.rows) break;
+        T* to = y + static_cast<size_t>(row0 + r) * ld_y + col0;
+        if (aligned && col0 + 128 <= a.cols) {
+            if constexpr (sizeof(T) == 4) {
+                st_unit(to + lane * kC, Unit<float>::pack(v));
+            } else {
+                const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
+                *reinterpret_cast<uint2*>(to + lane * kC) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
             }
         } else {
+            __syncwarp();
 #pragma unroll
-            for (uint32_t i = 0; i < kPatch; ++i)
-                if (at.col + i < a.cols) to[i] = from_f32<T>(v[i]);
+            for (uint32_t c = 0; c < kC; ++c) turn[warp][lane * kC + c] = from_f32<T>(v[c]);
+            __syncwarp();
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k)
+                if (col0 + lane + 32u * k < a.cols) to[lane + 32u * k] = turn[warp][lane + 32u * k];
         }
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kTileThreads, 1)
-gated_bwd_kernel(const Dense<T> dh, const Act8 gate, const Act8 up, const bool gelu, const Act8 dgate, const Act8 dup,
-                 const Act8 dgate_t, const Act8 dup_t, const Act8 h_t) {
-    __shared__ TileShared sh;
-    const Place at = place_of(blockIdx.y, blockIdx.x);
-    const bool want_gate = dgate.codes || dgate_t.codes, want_up = dup.codes || dup_t.codes;
-    float v[kPatch][kPatch];
-    for (uint32_t plane = 0; plane < 3; ++plane) {
-        if (plane == 0 ? !want_gate : plane == 1 ? !want_up : h_t.codes == nullptr) continue;
-#pragma unroll
-        for (uint32_t r = 0; r < kPatch; ++r) {
-            float g[kPatch], u[kPatch], d[kPatch];
-            act8_values(g, act8_load(gate, at.row + r, at.col), act8_power_at(gate, at.row + r, at.col));
-            if (plane != 1) act8_values(u, act8_load(up, at.row + r, at.col), act8_power_at(up, at.row + r, at.col));
-            if (plane != 2) dh.load(d, at.row + r, at.col);
-#pragma unroll
-            for (uint32_t c = 0; c < kPatch; ++c) {
-                const Gate a(g[c], gelu);
-                v[r][c] = plane == 0 ? a.slope_times(__fmul_rn(d[c], u[c])) : a.times(plane == 1 ? d[c] : u[c]);
-            }
-        }
-        if (plane == 0 && dgate.codes) write_rows(v, dgate, at);
-        if (plane == 1 && dup.codes) write_rows(v, dup, at);
-        const Act8& turned = plane == 0 ? dgate_t : plane == 1 ? dup_t : h_t;
-        if (turned.codes) write_columns(v, turned, at, sh);
-    }
-}
-
-// the grid of 128 x 128 tiles; false if it is beyond what one launch takes
-bool tile_grid(uint32_t rows, uint32_t cols, dim3* grid) {
-    *grid = dim3(ceil_div(cols, 128), ceil_div(rows, 128));
-    return grid->y <= 65535u;
-}
+// ---- host ----
 
 template <typename T> bool unit_rows(const void* p, uint32_t ld) {
     return aligned_to(p, 16) && static_cast<size_t>(ld) * sizeof(T) % 16 == 0;
 }
-template <typename T> Dense<T> dense(const void* x, uint32_t rows, uint32_t cols, uint32_t ld) {
-    return Dense<T>{static_cast<const T*>(x), rows, cols, ld, unit_rows<T>(x, ld)};
+template <typename T> constexpr CUtensorMapDataType tensor_type() {
+    return sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+}
+
+// Tiles of [rows, cols] over as many CTAs as the device holds at once
+template <typename S>
+dct_status_t launch_tiles(TileTask& task, uint32_t rows, uint32_t cols, const void* x, uint32_t ld_x, const dct_act8_t* held0, const dct_act8_t* held1,
+                          cudaStream_t stream) {
+    using T = typename S::Element;
+    static SharedLimit allowed;
+    dct_status_t st = allow_shared(act8_tile_kernel<S>, TileShape<S>::kSharedBytes, allowed);
+    if (st != DCT_OK) return st;
+    const int sms = sm_count();
+    if (sms <= 0) return DCT_ERR_CUDA;
+    task.rows = rows;
+    task.cols = cols;
+    task.tiles_r = ceil_div(rows, 128);
+    task.tiles_c = ceil_div(cols, 128);
+    task.limit = debug_config().spin_limit;
+    const uint64_t tiles = static_cast<uint64_t>(task.tiles_r) * task.tiles_c;
+    if (tiles > 0x7FFFFFFFull - 4096) return DCT_ERR_UNSUPPORTED;
+    TensorEncoder e = nullptr;
+    if ((st = tensor_encoder(&e)) != DCT_OK) return st;
+    if (S::kDenseBytes != 0) {
+        task.x = x;
+        task.ld_x = ld_x;
+        task.direct = !x || !unit_rows<T>(x, ld_x);
+        if (!task.direct && (st = tensor_map(e, &task.map[0], tensor_type<T>(), sizeof(T), x, rows, cols, ld_x, 128, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != DCT_OK)
+            return st;
+    }
+    const dct_act8_t* held[2] = {held0, held1};
+    for (uint32_t i = 0; i < S::kHeld; ++i) {
+        task.held[i] = device_view(held[i]);
+        if ((st = tensor_map(e, &task.map[1 + i], held[i], 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != DCT_OK) return st;
+    }
+    const uint64_t at_once = static_cast<uint64_t>(sms) * S::kCtas;
+    act8_tile_kernel<S><<<static_cast<unsigned>(tiles < at_once ? tiles : at_once), kTileThreads, TileShape<S>::kSharedBytes, stream>>>(task);
+    DCT_CUDA_TRY(cudaGetLastError());
+    return DCT_OK;
 }
 
 bool sized(const dct_act8_t* m, uint32_t rows, uint32_t cols) { return m->rows == rows && m->cols == cols && usable(m); }
@@ -264,15 +374,12 @@ extern "C" dct_status_t dct_act8_pack(const void* x, dct_dtype_t dtype, uint32_t
     all.write(out);
     all.write(out_t);
     if (all.clash()) return DCT_ERR_INVALID_ARG;
-    dim3 grid;
-    if (!tile_grid(rows, cols, &grid)) return DCT_ERR_UNSUPPORTED;
+    TileTask task = {};
+    task.by_rows[0] = device_view(out);
+    task.turned[0] = device_view(out_t);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    if (dtype == DCT_F32)
-        act8_write_kernel<<<grid, kTileThreads, 0, stream>>>(dense<float>(x, rows, cols, ld), device_view(out), device_view(out_t));
-    else
-        act8_write_kernel<<<grid, kTileThreads, 0, stream>>>(dense<__nv_bfloat16>(x, rows, cols, ld), device_view(out), device_view(out_t));
-    DCT_CUDA_TRY(cudaGetLastError());
-    return DCT_OK;
+    return dtype == DCT_F32 ? launch_tiles<Dense<float>>(task, rows, cols, x, ld, nullptr, nullptr, stream)
+                            : launch_tiles<Dense<__nv_bfloat16>>(task, rows, cols, x, ld, nullptr, nullptr, stream);
 }
 
 extern "C" dct_status_t dct_act8_unpack(const dct_act8_t* a, void* y, dct_dtype_t dtype, uint32_t ld_y, dct_stream_t stream_) {
@@ -285,14 +392,15 @@ extern "C" dct_status_t dct_act8_unpack(const dct_act8_t* a, void* y, dct_dtype_
     all.read(a);
     all.write(y, a->rows, a->cols * es, ld_y * es);
     if (all.clash()) return DCT_ERR_INVALID_ARG;
-    dim3 grid;
-    if (!tile_grid(a->rows, a->cols, &grid)) return DCT_ERR_UNSUPPORTED;
+    const uint32_t tiles_c = ceil_div(a->cols, 128);
+    const uint64_t tiles = static_cast<uint64_t>(ceil_div(a->rows, 64)) * tiles_c;
+    if (tiles > 0x7FFFFFFFull) return DCT_ERR_UNSUPPORTED;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const unsigned grid = static_cast<unsigned>(tiles);
     if (dtype == DCT_F32)
-        act8_unpack_kernel<<<grid, kTileThreads, 0, stream>>>(device_view(a), static_cast<float*>(y), ld_y, unit_rows<float>(y, ld_y));
+        act8_unpack_kernel<<<grid, 256, 0, stream>>>(device_view(a), static_cast<float*>(y), ld_y, tiles_c, unit_rows<float>(y, ld_y));
     else
-        act8_unpack_kernel<<<grid, kTileThreads, 0, stream>>>(device_view(a), static_cast<__nv_bfloat16*>(y), ld_y,
-                                                              unit_rows<__nv_bfloat16>(y, ld_y));
+        act8_unpack_kernel<<<grid, 256, 0, stream>>>(device_view(a), static_cast<__nv_bfloat16*>(y), ld_y, tiles_c, unit_rows<__nv_bfloat16>(y, ld_y));
     DCT_CUDA_TRY(cudaGetLastError());
     return DCT_OK;
 }
@@ -304,11 +412,9 @@ extern "C" dct_status_t dct_act8_transpose(const dct_act8_t* a, const dct_act8_t
     all.read(a);
     all.write(out_t);
     if (all.clash()) return DCT_ERR_INVALID_ARG;
-    dim3 grid;
-    if (!tile_grid(a->rows, a->cols, &grid)) return DCT_ERR_UNSUPPORTED;
-    act8_write_kernel<<<grid, kTileThreads, 0, static_cast<cudaStream_t>(stream_)>>>(Held{device_view(a)}, device_view(nullptr), device_view(out_t));
-    DCT_CUDA_TRY(cudaGetLastError());
-    return DCT_OK;
+    TileTask task = {};
+    task.turned[0] = device_view(out_t);
+    return launch_tiles<Held>(task, a->rows, a->cols, nullptr, 0, a, nullptr, static_cast<cudaStream_t>(stream_));
 }
 
 extern "C" dct_status_t dct_gated8_bwd(const void* dh, dct_dtype_t dtype, uint32_t ld_dh, const dct_act8_t* gate, const dct_act8_t* up,
@@ -335,16 +441,15 @@ extern "C" dct_status_t dct_gated8_bwd(const void* dh, dct_dtype_t dtype, uint32
     all.read(up);
     for (const dct_act8_t* m : outs) all.write(m);
     if (all.clash()) return DCT_ERR_INVALID_ARG;
-    dim3 grid;
-    if (!tile_grid(rows, f, &grid)) return DCT_ERR_UNSUPPORTED;
+    TileTask task = {};
+    task.by_rows[0] = device_view(dgate);
+    task.by_rows[1] = device_view(dup);
+    task.turned[0] = device_view(dgate_t);
+    task.turned[1] = device_view(dup_t);
+    task.turned[2] = device_view(h_t);
+    task.gelu = activation == DCT_ACT_GELU;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    const bool gelu = activation == DCT_ACT_GELU;
-    if (dtype == DCT_F32)
-        gated_bwd_kernel<<<grid, kTileThreads, 0, stream>>>(dense<float>(dh, rows, f, ld_dh), device_view(gate), device_view(up), gelu,
-            device_view(dgate), device_view(dup), device_view(dgate_t), device_view(dup_t), device_view(h_t));
-    else
-        gated_bwd_kernel<<<grid, kTileThreads, 0, stream>>>(dense<__nv_bfloat16>(dh, rows, f, ld_dh), device_view(gate), device_view(up), gelu,
-            device_view(dgate), device_view(dup), device_view(dgate_t), device_view(dup_t), device_view(h_t));
-    DCT_CUDA_TRY(cudaGetLastError());
-    return DCT_OK;
+    // (h alone asks for no dh)
+    return dtype == DCT_F32 && gradients ? launch_tiles<Gated<float>>(task, rows, f, dh, ld_dh, gate, up, stream)
+                                         : launch_tiles<Gated<__nv_bfloat16>>(task, rows, f, gradients ? dh : nullptr, ld_dh, gate, up, stream);
 }

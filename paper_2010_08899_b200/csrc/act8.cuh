@@ -3,6 +3,8 @@
 #pragma once
 #include <cuda_fp8.h>
 
+#include <cuda.h>
+
 #include "lm_rows.cuh"
 
 namespace dct {
@@ -58,39 +60,35 @@ __device__ __forceinline__ void act8_values2(uint32_t two, float& lo, float& hi)
     hi = f.y;
 }
 
-// p + c for a c that is never quite 0: where the sum is p all the same, the number next to p, away from 0 if `up`.  Products of codes have so
-// few digits that many lie exactly halfway between two codes; a share just below 1 must put them on the right side.
-__device__ __forceinline__ float beside(float p, float c, bool up) {
-    const float s = __fadd_rn(p, c);
-    const bool stuck = s == p && p != 0.0f && fabsf(p) < __uint_as_float(0x7F800000u);
-    return stuck ? __uint_as_float(__float_as_uint(p) + (up ? 1u : 0xFFFFFFFFu)) : s;
+__device__ __forceinline__ void tile_load(void* smem, const CUtensorMap* map, uint32_t x, uint32_t y, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(smem_addr(smem)), "l"(map), "r"(x), "r"(y), "r"(smem_addr(bar)) : "memory");
 }
 
-// act(g) = g share, share = sigmoid(y).  SILU: y = g; GELU: y = 2 sqrt(2/pi) (g + 0.044715 g^3).  With q = sigmoid(-|y|) the share is q
-// below 0 and 1 - q above, where the products take q as a small correction.
+// act(g) = g share, share = sigmoid(y), and its derivative.  SILU: y = g; GELU: y = 2 sqrt(2/pi) (g + 0.044715 g^3).  With q = sigmoid(-|y|) the
+// share is q below 0 and 1 - q above.  Products of codes have so few digits that many lie exactly halfway between two codes, and
+// a share just below 1 must put them on the right side: where act(g) would round to g, it is the number next to it, and a slope that would
+// round to 1 is next to 1 on its own side.  (x act(g) is then off x g by more than half a step unless x g is a power of two, which is no such halfway case.)
 struct Gate {
-    float g, q, dy;              // dy: the derivative of y
-    __device__ __forceinline__ Gate(float g_, bool gelu) : g(g_), dy(1.0f) {
+    float value, slope;
+    __device__ __forceinline__ Gate(float g, bool gelu) {
         constexpr float kA = 1.5957691216057308f, kB = 0.044715f;
-        float y = g;
+        float y = g, dy = 1.0f;
         if (gelu) {
             const float g2 = __fmul_rn(g, g);
             y = __fmul_rn(__fmul_rn(kA, g), fmaf(kB, g2, 1.0f));
             dy = __fmul_rn(kA, fmaf(3.0f * kB, g2, 1.0f));
         }
-        const float t = exp2_fast(__fmul_rn(-fabsf(y), kLog2E));
-        q = __fdividef(t, __fadd_rn(1.0f, t));
-    }
-    // act(g) x
-    __device__ __forceinline__ float times(float x) const {
-        const float p = __fmul_rn(x, g), low = __fmul_rn(x, __fmul_rn(g, q));
-        return g < 0.0f ? low : beside(p, -low, false);
-    }
-    // act'(g) p
-    __device__ __forceinline__ float slope_times(float p) const {
-        const float gq = __fmul_rn(g, q), more = fmaf(__fadd_rn(g, -gq), dy, -1.0f);
-        const float below = fmaf(__fmul_rn(gq, __fadd_rn(1.0f, -q)), dy, q);
-        return g < 0.0f ? __fmul_rn(p, q == 0.0f ? 0.0f : below) : q == 0.0f ? beside(p, 0.0f, more > 0.0f) : beside(p, __fmul_rn(p, __fmul_rn(q, more)), more > 0.0f);
+        const float t = exp2_fast(__fmul_rn(fabsf(y), -kLog2E)), r = __fdividef(1.0f, __fadd_rn(1.0f, t)), q = __fmul_rn(t, r), gq = __fmul_rn(g, q);
+        if (g < 0.0f) {
+            value = gq;
+            slope = t == 0.0f ? 0.0f : fmaf(__fmul_rn(gq, r), dy, q);
+        } else {
+            const float less = __fadd_rn(g, -gq), more = fmaf(less, dy, -1.0f);
+            value = less == g && g > 0.0f && g <= 3.4028234e38f ? __uint_as_float(__float_as_uint(g) - 1u) : less;
+            slope = t == 0.0f ? 1.0f : fmaf(q, more, 1.0f);
+            if (slope == 1.0f) slope = more > 0.0f ? 1.0f + 0x1p-23f : 1.0f - 0x1p-24f;
+        }
     }
 };
 
@@ -108,6 +106,39 @@ inline bool usable(const dct_act8_t* m) {
 inline Act8 device_view(const dct_act8_t* m) {
     if (!m) return Act8{nullptr, nullptr, 0, 0, 0, 0};
     return Act8{static_cast<uint8_t*>(m->codes), static_cast<uint8_t*>(m->scales), m->rows, m->cols, m->ld, ceil_div(m->rows, 128)};
+}
+
+// Descriptors of tensor copies -----------------------------------------------------------------------------------
+
+using TensorEncoder = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// the driver's function that makes them (looked up once)
+inline dct_status_t tensor_encoder(TensorEncoder* out) {
+    static std::atomic<TensorEncoder> kept{nullptr};
+    TensorEncoder e = kept.load(std::memory_order_acquire);
+    if (!e) {
+        void* found = nullptr;
+        cudaDriverEntryPointQueryResult how = cudaDriverEntryPointSymbolNotFound;
+        DCT_CUDA_TRY(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &found, 12000, cudaEnableDefault, &how));
+        if (how != cudaDriverEntryPointSuccess || !found) return DCT_ERR_UNSUPPORTED;
+        e = reinterpret_cast<TensorEncoder>(found);
+        kept.store(e, std::memory_order_release);
+    }
+    *out = e;
+    return DCT_OK;
+}
+// boxes of `box_cols` by `box_rows` of a row-major matrix on 16-byte boundaries; zeros outside it
+inline dct_status_t tensor_map(TensorEncoder e, CUtensorMap* map, CUtensorMapDataType type, size_t es, const void* p, uint32_t rows, uint32_t cols,
+                               uint32_t ld, uint32_t box_rows, uint32_t box_cols, CUtensorMapSwizzle swizzle) {
+    const cuuint64_t size[2] = {cols, rows}, stride[1] = {static_cast<cuuint64_t>(ld) * es};
+    const cuuint32_t box[2] = {box_cols, box_rows}, unit[2] = {1, 1};
+    const CUresult r = e(map, type, 2, const_cast<void*>(p), size, stride, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? DCT_OK : DCT_ERR_INVALID_ARG;
+}
+inline dct_status_t tensor_map(TensorEncoder e, CUtensorMap* map, const dct_act8_t* m, uint32_t box_rows, CUtensorMapSwizzle swizzle) {
+    return tensor_map(e, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, m->codes, m->rows, m->cols, m->ld, box_rows, 128, swizzle);
 }
 
 // The buffers of a call: what is written may overlap nothing else.  Rows of one matrix may lie between those of another, side by

@@ -11,8 +11,6 @@
 //   gated, few:   two P tiles, gate and up, with the same Q, into two accumulators.
 // Where tiles are too few for the device, a cluster of CTAs shares one: each sums a part of the depth, sends every other its columns of the
 // result, and adds up its own columns in the order of the parts.
-#include <cuda.h>
-
 #include "act8.cuh"
 
 namespace dct {
@@ -124,11 +122,6 @@ template <uint32_t kN> __device__ __forceinline__ void tmem_loaded(float* v) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
     for (uint32_t i = 0; i < kN; ++i) asm volatile("" : "+f"(v[i]));
-}
-
-__device__ __forceinline__ void tile_load(void* smem, const CUtensorMap* map, uint32_t x, uint32_t y, uint64_t* bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(smem_addr(smem)), "l"(map), "r"(x), "r"(y), "r"(smem_addr(bar)) : "memory");
 }
 
 // Descriptors of shared memory.  Tiles: rows of 128 bytes, swizzled by 128 bytes, groups of eight rows 1024 bytes apart; 32 of depth further is 32 bytes
@@ -298,7 +291,7 @@ __device__ __forceinline__ void finish_few_gated(const Task& task, Shared<S>& sh
         // (beyond the last column the powers are anything: what stands there is no number)
         g[j] = !ok ? __uint_as_float(kLost) : col < f ? g[j] : 0.0f;
         u[j] = col < f ? u[j] : 0.0f;
-        h[j] = Gate(g[j], task.gelu).times(u[j]);
+        h[j] = __fmul_rn(Gate(g[j], task.gelu).value, u[j]);
         if (j < count) {
             const uint32_t mg = __reduce_max_sync(0xFFFFFFFFu, magnitude(g[j])), mu = __reduce_max_sync(0xFFFFFFFFu, magnitude(u[j])),
                            mh = __reduce_max_sync(0xFFFFFFFFu, magnitude(h[j]));
@@ -554,7 +547,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                     scale(task.up, bu);
                 }
 #pragma unroll
-                for (uint32_t j = 0; j < 64; ++j) g[j] = Gate(g[j], task.gelu).times(u[j]);
+                for (uint32_t j = 0; j < 64; ++j) g[j] = __fmul_rn(Gate(g[j], task.gelu).value, u[j]);
                 if (task.h.codes) {
                     join(2, largest64(g));
                     named_barrier_sync(1, kEpilogueWarps * 32);
@@ -623,31 +616,9 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
 
 // ---- host ----
 
-using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                            const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-dct_status_t encoder(Encode* out) {
-    static std::atomic<Encode> kept{nullptr};
-    Encode e = kept.load(std::memory_order_acquire);
-    if (!e) {
-        void* found = nullptr;
-        cudaDriverEntryPointQueryResult how = cudaDriverEntryPointSymbolNotFound;
-        DCT_CUDA_TRY(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &found, 12000, cudaEnableDefault, &how));
-        if (how != cudaDriverEntryPointSuccess || !found) return DCT_ERR_UNSUPPORTED;
-        e = reinterpret_cast<Encode>(found);
-        kept.store(e, std::memory_order_release);
-    }
-    *out = e;
-    return DCT_OK;
-}
-
-// codes in boxes of 128 bytes by `rows` rows; zeros outside the matrix
-dct_status_t encode(Encode e, CUtensorMap* map, const dct_act8_t* m, uint32_t rows) {
-    const cuuint64_t size[2] = {m->cols, m->rows}, stride[1] = {m->ld};
-    const cuuint32_t box[2] = {kDepth, rows}, unit[2] = {1, 1};
-    const CUresult r = e(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, m->codes, size, stride, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? DCT_OK : DCT_ERR_INVALID_ARG;
+// codes in boxes of 128 bytes by `rows` rows
+dct_status_t encode(TensorEncoder e, CUtensorMap* map, const dct_act8_t* m, uint32_t rows) {
+    return tensor_map(e, map, m, rows, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 Scales scales_of(const dct_act8_t* m) { return Scales{static_cast<const uint8_t*>(m->scales), ceil_div(m->rows, 128)}; }
 
@@ -691,8 +662,8 @@ using GatedFew64 = Shape<64, true, true, 3, true>;
 
 dct_status_t product(const dct_act8_t* const (&a)[2], const dct_act8_t* const (&b)[2], void* c, dct_dtype_t dtype, uint32_t ld_c, bool accumulate,
                      cudaStream_t stream) {
-    Encode e = nullptr;
-    dct_status_t st = encoder(&e);
+    TensorEncoder e = nullptr;
+    dct_status_t st = tensor_encoder(&e);
     if (st != DCT_OK) return st;
     const int sms = sm_count();
     if (sms <= 0) return DCT_ERR_CUDA;
@@ -725,8 +696,8 @@ dct_status_t product(const dct_act8_t* const (&a)[2], const dct_act8_t* const (&
 
 dct_status_t gated(const dct_act8_t* x, const dct_act8_t* w_gate, const dct_act8_t* w_up, bool gelu, const dct_act8_t* h, void* h_dense, dct_dtype_t dtype,
                    uint32_t ld_h, const dct_act8_t* gate, const dct_act8_t* up, cudaStream_t stream) {
-    Encode e = nullptr;
-    dct_status_t st = encoder(&e);
+    TensorEncoder e = nullptr;
+    dct_status_t st = tensor_encoder(&e);
     if (st != DCT_OK) return st;
     const int sms = sm_count();
     if (sms <= 0) return DCT_ERR_CUDA;
