@@ -19,7 +19,7 @@ struct TileTask {
     Act8 held[2];                // inputs in 8 bits (their scales)
     const void* x;               // a dense input whose rows start on no boundary
     uint32_t ld_x;
-    bool direct, gelu;           // direct: x is not fetched by tensor copies (or is not there)
+    bool direct;                 // direct: x is not fetched by tensor copies (or is not there)
     uint32_t rows, cols, tiles_r, tiles_c;
     uint32_t limit;
     Act8 by_rows[2], turned[3];  // outputs by plane
@@ -38,8 +38,9 @@ template <> __device__ __forceinline__ void four(float (&v)[kC], const __nv_bflo
 __device__ __forceinline__ void four(float (&v)[kC], uint32_t codes, float power) {
     act8_values2(codes & 0xFFFFu, v[0], v[1]);
     act8_values2(codes >> 16, v[2], v[3]);
-#pragma unroll
-    for (uint32_t c = 0; c < kC; ++c) v[c] = __fmul_rn(v[c], power);
+    const uint64_t by = pack2(power, power);
+    unpack2(mul2(pack2(v[0], v[1]), by), v[0], v[1]);
+    unpack2(mul2(pack2(v[2], v[3]), by), v[2], v[3]);
 }
 
 // A dense tile whose rows start on no boundary, into the place a tensor copy would have put it: every warp its own rows, neighbouring lanes
@@ -66,7 +67,7 @@ __device__ __forceinline__ void fetch_rows(T* tile, const TileTask& task, uint32
 template <typename T> struct Dense {
     static constexpr uint32_t kPlanes = 1, kHeld = 0, kDenseBytes = 128 * 128 * sizeof(T), kCtas = sizeof(T) == 4 ? 1 : 2;
     using Element = T;
-    __device__ static __forceinline__ void load(float (&v)[1][kR][kC], const uint8_t* stage, const float*, bool) {
+    __device__ static __forceinline__ void load(float (&v)[1][kR][kC], const uint8_t* stage, const float*) {
         const T* from = reinterpret_cast<const T*>(stage) + (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
 #pragma unroll
         for (uint32_t r = 0; r < kR; ++r) four<T>(v[0][r], from + r * 128);
@@ -75,17 +76,17 @@ template <typename T> struct Dense {
 struct Held {
     static constexpr uint32_t kPlanes = 1, kHeld = 1, kDenseBytes = 0, kCtas = 2;
     using Element = float;
-    __device__ static __forceinline__ void load(float (&v)[1][kR][kC], const uint8_t* stage, const float* power, bool) {
+    __device__ static __forceinline__ void load(float (&v)[1][kR][kC], const uint8_t* stage, const float* power) {
         const uint8_t* from = stage + (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
 #pragma unroll
         for (uint32_t r = 0; r < kR; ++r) four(v[0][r], *reinterpret_cast<const uint32_t*>(from + r * 128), __shfl_sync(0xFFFFFFFFu, power[0], r));
     }
 };
 // dh, gate and up; the planes are dgate, dup and h
-template <typename T> struct Gated {
+template <typename T, bool kGelu> struct Gated {
     static constexpr uint32_t kPlanes = 3, kHeld = 2, kDenseBytes = 128 * 128 * sizeof(T), kCtas = 1;
     using Element = T;
-    __device__ static __forceinline__ void load(float (&v)[3][kR][kC], const uint8_t* stage, const float* power, bool gelu) {
+    __device__ static __forceinline__ void load(float (&v)[3][kR][kC], const uint8_t* stage, const float* power) {
         const uint32_t at = (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
 #pragma unroll
         for (uint32_t r = 0; r < kR; ++r) {
@@ -94,11 +95,12 @@ template <typename T> struct Gated {
             four(g, *reinterpret_cast<const uint32_t*>(stage + kDenseBytes + at + r * 128), __shfl_sync(0xFFFFFFFFu, power[0], r));
             four(u, *reinterpret_cast<const uint32_t*>(stage + kDenseBytes + 128 * 128 + at + r * 128), __shfl_sync(0xFFFFFFFFu, power[1], r));
 #pragma unroll
-            for (uint32_t c = 0; c < kC; ++c) {
-                const Gate a(g[c], gelu);
-                v[0][r][c] = __fmul_rn(__fmul_rn(d[c], u[c]), a.slope);
-                v[1][r][c] = __fmul_rn(d[c], a.value);
-                v[2][r][c] = __fmul_rn(a.value, u[c]);
+            for (uint32_t c = 0; c < kC; c += 2) {
+                const uint64_t d2 = pack2(d[c], d[c + 1]), u2 = pack2(u[c], u[c + 1]);
+                const Gate2 a = gate2<true, kGelu>(g[c], g[c + 1]);
+                unpack2(mul2(mul2(d2, u2), a.slope), v[0][r][c], v[0][r][c + 1]);
+                unpack2(mul2(d2, a.value), v[1][r][c], v[1][r][c + 1]);
+                unpack2(mul2(u2, a.value), v[2][r][c], v[2][r][c + 1]);
             }
         }
     }
@@ -111,26 +113,48 @@ template <typename S> struct TileShape {
     static_assert(kStageBytes >= S::kPlanes * kTurnedBytes, "the transposed codes take the place of a tile's inputs");
 };
 
-__device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d, float inverse, uint32_t byte) {
-    return act8_finite4(act8_codes4(__fmul_rn(a, inverse), __fmul_rn(b, inverse), __fmul_rn(c, inverse), __fmul_rn(d, inverse)), byte);
-}
-
-// A lane's patch of a plane by rows
-__device__ __forceinline__ void write_rows(const float (&v)[kR][kC], const Act8& out, uint32_t row0, uint32_t col0) {
+// A lane's patch of a plane by rows: eight reductions under way at once, and row r's byte and power worked out by lane r alone.  whole: the tile
+// lies inside the matrix.
+__device__ __forceinline__ void write_rows(const float (&v)[kR][kC], const Act8& out, uint32_t row0, uint32_t col0, bool whole) {
     const uint32_t lane = lane_id(), col = col0 + lane * kC;
+    float m[kR], mine = 0.0f;
+#pragma unroll
+    for (uint32_t r = 0; r < kR; ++r) m[r] = warp_largest(largest3(largest3(v[r][0], v[r][1], v[r][2]), v[r][3], 0.0f));
+#pragma unroll
+    for (uint32_t r = 0; r < kR; ++r) mine = lane == r ? m[r] : mine;
+    const uint32_t byte = act8_byte(magnitude(mine));
+    const float inverse = act8_inverse(byte);
+    const bool huge = __any_sync(0xFFFFFFFFu, byte == 247u);
+    if (lane < kR && row0 + lane < out.rows)
+        out.scales[act8_scale_offset(out.row_tiles, row0, col0 >> 7) + lane * 16u] = static_cast<uint8_t>(byte);
+    uint32_t q[kR];
 #pragma unroll
     for (uint32_t r = 0; r < kR; ++r) {
-        const uint32_t m = max(max(magnitude(v[r][0]), magnitude(v[r][1])), max(magnitude(v[r][2]), magnitude(v[r][3])));
-        const uint32_t byte = act8_byte(__reduce_max_sync(0xFFFFFFFFu, m)), row = row0 + r;
-        if (row >= out.rows) break;
-        const uint32_t q = codes_of(v[r][0], v[r][1], v[r][2], v[r][3], act8_inverse(byte), byte);
-        uint8_t* to = out.codes + static_cast<size_t>(row) * out.ld + col;
-        if (col + kC <= out.cols) {
-            *reinterpret_cast<uint32_t*>(to) = q;
-        } else {
-            for (uint32_t c = 0; col + c < out.cols; ++c) to[c] = static_cast<uint8_t>(q >> (8 * c));
+        const float f = __shfl_sync(0xFFFFFFFFu, inverse, r);
+        float a, b, c, d;
+        unpack2(mul2(pack2(v[r][0], v[r][1]), pack2(f, f)), a, b);
+        unpack2(mul2(pack2(v[r][2], v[r][3]), pack2(f, f)), c, d);
+        q[r] = act8_codes4(a, b, c, d);
+    }
+    if (huge) {
+#pragma unroll
+        for (uint32_t r = 0; r < kR; ++r) q[r] = act8_finite4(q[r], __shfl_sync(0xFFFFFFFFu, byte, r));
+    }
+    uint8_t* to = out.codes + static_cast<size_t>(row0) * out.ld + col;
+    if (whole) {
+#pragma unroll
+        for (uint32_t r = 0; r < kR; ++r) *reinterpret_cast<uint32_t*>(to + static_cast<size_t>(r) * out.ld) = q[r];
+    } else {
+#pragma unroll
+        for (uint32_t r = 0; r < kR; ++r) {
+            if (row0 + r >= out.rows) break;
+            if (col + kC <= out.cols) {
+                *reinterpret_cast<uint32_t*>(to) = q[r];
+            } else {
+                for (uint32_t c = 0; col + c < out.cols; ++c) to[c] = static_cast<uint8_t>(q[r] >> (8 * c));
+            }
+            to += out.ld;
         }
-        if (lane == r) out.scales[act8_scale_offset(out.row_tiles, row, col0 >> 7)] = static_cast<uint8_t>(byte);
     }
 }
 
@@ -142,7 +166,7 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
     __shared__ alignas(16) uint32_t bytes[S::kPlanes][128];
     __shared__ uint32_t stop;
     uint8_t* stages = raw + ((128u - (smem_addr(raw) & 127u)) & 127u);
-    uint32_t* largest = reinterpret_cast<uint32_t*>(stages + 2 * Shape::kStageBytes);       // [plane][warp][column]
+    float* largest = reinterpret_cast<float*>(stages + 2 * Shape::kStageBytes);       // [plane][warp][column]
     const uint32_t warp = threadIdx.x >> 5, lane = lane_id(), tiles = task.tiles_r * task.tiles_c;
     const bool copied = S::kHeld != 0 || !task.direct;
     if (threadIdx.x == 0) {
@@ -157,8 +181,8 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
         const bool dense = S::kDenseBytes != 0 && !task.direct;
         mbar_arrive_expect_tx(&arrived[s], (dense ? S::kDenseBytes : 0u) + S::kHeld * 128 * 128);
         if (dense) tile_load(to, &task.map[0], x, y, &arrived[s]);
-#pragma unroll
-        for (uint32_t i = 0; i < S::kHeld; ++i) tile_load(to + S::kDenseBytes + i * 128 * 128, &task.map[1 + i], x, y, &arrived[s]);
+        if constexpr (S::kHeld >= 1) tile_load(to + S::kDenseBytes, &task.map[1], x, y, &arrived[s]);
+        if constexpr (S::kHeld >= 2) tile_load(to + S::kDenseBytes + 128 * 128, &task.map[2], x, y, &arrived[s]);
     };
     if (threadIdx.x == 0 && copied && blockIdx.x < tiles) fetch(blockIdx.x, 0);
     __syncthreads();
@@ -166,15 +190,17 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
     bool ok = true;
     for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
         const uint32_t col0 = t % task.tiles_c * 128u, row0 = t / task.tiles_c * 128u;
+        const bool whole = row0 + 128 <= task.rows && col0 + 128 <= task.cols;
         if (threadIdx.x == 0 && copied && ok && t + gridDim.x < tiles) fetch(t + gridDim.x, s ^ 1u);
         uint8_t* stage = stages + s * Shape::kStageBytes;
         // the powers of the warp's rows: lane r has row r's
-        float power[S::kHeld + 1];
-#pragma unroll
-        for (uint32_t i = 0; i < S::kHeld; ++i) {
+        float power[2] = {};
+        const auto power_of = [&](const Act8& m) {
             const uint32_t row = row0 + warp * kR + (lane & 7u);
-            power[i] = row < task.rows ? act8_power(task.held[i].scales[act8_scale_offset(task.held[i].row_tiles, row, col0 >> 7)]) : 0.0f;
-        }
+            return row < task.rows ? act8_power(m.scales[act8_scale_offset(m.row_tiles, row, col0 >> 7)]) : 0.0f;
+        };
+        if constexpr (S::kHeld >= 1) power[0] = power_of(task.held[0]);
+        if constexpr (S::kHeld >= 2) power[1] = power_of(task.held[1]);
         if (S::kDenseBytes != 0 && task.direct && task.x) fetch_rows(reinterpret_cast<typename S::Element*>(stage), task, row0, col0);
         if (copied && ok && !mbar_wait_bounded(&arrived[s], phase, task.limit, &stop)) {
             ok = false;
@@ -185,7 +211,7 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
             }
         }
         float v[S::kPlanes][kR][kC];
-        S::load(v, stage, power, task.gelu);
+        S::load(v, stage, power);
         if (!ok) {
 #pragma unroll
             for (uint32_t p = 0; p < S::kPlanes; ++p)
@@ -195,25 +221,25 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
         bool any_turned = false;
 #pragma unroll
         for (uint32_t p = 0; p < S::kPlanes; ++p) {
-            if (p < 2 && task.by_rows[p].codes) write_rows(v[p], task.by_rows[p], row0 + warp * kR, col0);
+            if (p < 2 && task.by_rows[p].codes) write_rows(v[p], task.by_rows[p], row0 + warp * kR, col0, whole);
             if (!task.turned[p].codes) continue;
             any_turned = true;
-            uint32_t m[kC] = {};
+            float m[kC] = {};
 #pragma unroll
-            for (uint32_t r = 0; r < kR; ++r)
+            for (uint32_t r = 0; r < kR; r += 2)
 #pragma unroll
-                for (uint32_t c = 0; c < kC; ++c) m[c] = max(m[c], magnitude(v[p][r][c]));
-            *reinterpret_cast<uint4*>(largest + (p * kWarps + warp) * 128u + lane * kC) = make_uint4(m[0], m[1], m[2], m[3]);
+                for (uint32_t c = 0; c < kC; ++c) m[c] = largest3(m[c], v[p][r][c], v[p][r + 1][c]);
+            *reinterpret_cast<float4*>(largest + (p * kWarps + warp) * 128u + lane * kC) = make_float4(m[0], m[1], m[2], m[3]);
         }
         __syncthreads();
         if (any_turned) {
             if (threadIdx.x < S::kPlanes * 128u) {
                 const uint32_t p = threadIdx.x >> 7, c = threadIdx.x & 127u;
                 if (task.turned[p].codes) {
-                    uint32_t m = 0;
+                    float m = 0.0f;
 #pragma unroll
-                    for (uint32_t w = 0; w < kWarps; ++w) m = max(m, largest[(p * kWarps + w) * 128u + c]);
-                    const uint32_t byte = act8_byte(m);
+                    for (uint32_t w = 0; w < kWarps; w += 2) m = largest3(m, largest[(p * kWarps + w) * 128u + c], largest[(p * kWarps + w + 1) * 128u + c]);
+                    const uint32_t byte = act8_byte(magnitude(m));
                     bytes[p][c] = byte;
                     if (col0 + c < task.cols) task.turned[p].scales[act8_scale_offset(task.turned[p].row_tiles, col0 + c, row0 >> 7)] = static_cast<uint8_t>(byte);
                 }
@@ -224,14 +250,23 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
             for (uint32_t p = 0; p < S::kPlanes; ++p) {
                 if (!task.turned[p].codes) continue;
                 const uint4 b = *reinterpret_cast<const uint4*>(&bytes[p][lane * kC]);
+                const uint64_t f01 = pack2(act8_inverse(b.x), act8_inverse(b.y)), f23 = pack2(act8_inverse(b.z), act8_inverse(b.w));
+                const bool huge = b.x == 247u || b.y == 247u || b.z == 247u || b.w == 247u;
+                float x[kR][kC];
+#pragma unroll
+                for (uint32_t r = 0; r < kR; ++r) {
+                    unpack2(mul2(pack2(v[p][r][0], v[p][r][1]), f01), x[r][0], x[r][1]);
+                    unpack2(mul2(pack2(v[p][r][2], v[p][r][3]), f23), x[r][2], x[r][3]);
+                }
                 uint8_t* to = stage + p * kTurnedBytes + ((warp ^ (lane & 15u)) << 3);
 #pragma unroll
                 for (uint32_t c = 0; c < kC; ++c) {
-                    const uint32_t byte = c == 0 ? b.x : c == 1 ? b.y : c == 2 ? b.z : b.w;
-                    const float inverse = act8_inverse(byte);
-                    *reinterpret_cast<uint2*>(to + (lane * kC + c) * 128u) =
-                        make_uint2(codes_of(v[p][0][c], v[p][1][c], v[p][2][c], v[p][3][c], inverse, byte),
-                                   codes_of(v[p][4][c], v[p][5][c], v[p][6][c], v[p][7][c], inverse, byte));
+                    uint2 q = make_uint2(act8_codes4(x[0][c], x[1][c], x[2][c], x[3][c]), act8_codes4(x[4][c], x[5][c], x[6][c], x[7][c]));
+                    if (huge) {
+                        const uint32_t byte = c == 0 ? b.x : c == 1 ? b.y : c == 2 ? b.z : b.w;
+                        q = make_uint2(act8_finite4(q.x, byte), act8_finite4(q.y, byte));
+                    }
+                    *reinterpret_cast<uint2*>(to + (lane * kC + c) * 128u) = q;
                 }
             }
             __syncthreads();
@@ -243,11 +278,11 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
                 for (uint32_t i = 0; i < 128u * 8u / kTileThreads; ++i) {
                     const uint32_t c = i * (kTileThreads / 8u) + (threadIdx.x >> 3), pair = threadIdx.x & 7u, key = (c >> 2) & 15u;
                     const uint32_t row = col0 + c, col = row0 + pair * 16u;           // of the transpose
-                    if (row >= out.rows || col >= out.cols) continue;
+                    if (!whole && (row >= out.rows || col >= out.cols)) continue;
                     uint4 q = *reinterpret_cast<const uint4*>(stage + p * kTurnedBytes + c * 128u + (((2u * pair) ^ (key & 14u)) << 3));
                     if (key & 1u) q = make_uint4(q.z, q.w, q.x, q.y);
                     uint8_t* to = out.codes + static_cast<size_t>(row) * out.ld + col;
-                    if (col + 16 <= out.cols) {
+                    if (whole || col + 16 <= out.cols) {
                         st_unit(to, q);
                     } else {
                         for (uint32_t k = 0; col + k < out.cols; ++k)
@@ -338,11 +373,10 @@ dct_status_t launch_tiles(TileTask& task, uint32_t rows, uint32_t cols, const vo
         if (!task.direct && (st = tensor_map(e, &task.map[0], tensor_type<T>(), sizeof(T), x, rows, cols, ld_x, 128, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != DCT_OK)
             return st;
     }
-    const dct_act8_t* held[2] = {held0, held1};
-    for (uint32_t i = 0; i < S::kHeld; ++i) {
-        task.held[i] = device_view(held[i]);
-        if ((st = tensor_map(e, &task.map[1 + i], held[i], 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != DCT_OK) return st;
-    }
+    task.held[0] = device_view(held0);
+    task.held[1] = device_view(held1);
+    if (held0 && (st = tensor_map(e, &task.map[1], held0, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != DCT_OK) return st;
+    if (held1 && (st = tensor_map(e, &task.map[2], held1, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != DCT_OK) return st;
     const uint64_t at_once = static_cast<uint64_t>(sms) * S::kCtas;
     act8_tile_kernel<S><<<static_cast<unsigned>(tiles < at_once ? tiles : at_once), kTileThreads, TileShape<S>::kSharedBytes, stream>>>(task);
     DCT_CUDA_TRY(cudaGetLastError());
@@ -447,9 +481,10 @@ extern "C" dct_status_t dct_gated8_bwd(const void* dh, dct_dtype_t dtype, uint32
     task.turned[0] = device_view(dgate_t);
     task.turned[1] = device_view(dup_t);
     task.turned[2] = device_view(h_t);
-    task.gelu = activation == DCT_ACT_GELU;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     // (h alone asks for no dh)
-    return dtype == DCT_F32 && gradients ? launch_tiles<Gated<float>>(task, rows, f, dh, ld_dh, gate, up, stream)
-                                         : launch_tiles<Gated<__nv_bfloat16>>(task, rows, f, gradients ? dh : nullptr, ld_dh, gate, up, stream);
+    const bool gelu = activation == DCT_ACT_GELU;
+    auto launch = dtype == DCT_F32 && gradients ? (gelu ? launch_tiles<Gated<float, true>> : launch_tiles<Gated<float, false>>)
+                                                : (gelu ? launch_tiles<Gated<__nv_bfloat16, true>> : launch_tiles<Gated<__nv_bfloat16, false>>);
+    return launch(task, rows, f, gradients ? dh : nullptr, ld_dh, gate, up, stream);
 }

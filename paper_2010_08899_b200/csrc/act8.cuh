@@ -65,32 +65,76 @@ __device__ __forceinline__ void tile_load(void* smem, const CUtensorMap* map, ui
                  ::"r"(smem_addr(smem)), "l"(map), "r"(x), "r"(y), "r"(smem_addr(bar)) : "memory");
 }
 
-// act(g) = g share, share = sigmoid(y), and its derivative.  SILU: y = g; GELU: y = 2 sqrt(2/pi) (g + 0.044715 g^3).  With q = sigmoid(-|y|) the
-// share is q below 0 and 1 - q above.  Products of codes have so few digits that many lie exactly halfway between two codes, and
-// a share just below 1 must put them on the right side: where act(g) would round to g, it is the number next to it, and a slope that would
-// round to 1 is next to 1 on its own side.  (x act(g) is then off x g by more than half a step unless x g is a power of two, which is no such halfway case.)
-struct Gate {
-    float value, slope;
-    __device__ __forceinline__ Gate(float g, bool gelu) {
-        constexpr float kA = 1.5957691216057308f, kB = 0.044715f;
-        float y = g, dy = 1.0f;
-        if (gelu) {
-            const float g2 = __fmul_rn(g, g);
-            y = __fmul_rn(__fmul_rn(kA, g), fmaf(kB, g2, 1.0f));
-            dy = __fmul_rn(kA, fmaf(3.0f * kB, g2, 1.0f));
-        }
-        const float t = exp2_fast(__fmul_rn(fabsf(y), -kLog2E)), r = __fdividef(1.0f, __fadd_rn(1.0f, t)), q = __fmul_rn(t, r), gq = __fmul_rn(g, q);
-        if (g < 0.0f) {
-            value = gq;
-            slope = t == 0.0f ? 0.0f : fmaf(__fmul_rn(gq, r), dy, q);
-        } else {
-            const float less = __fadd_rn(g, -gq), more = fmaf(less, dy, -1.0f);
-            value = less == g && g > 0.0f && g <= 3.4028234e38f ? __uint_as_float(__float_as_uint(g) - 1u) : less;
-            slope = t == 0.0f ? 1.0f : fmaf(q, more, 1.0f);
-            if (slope == 1.0f) slope = more > 0.0f ? 1.0f + 0x1p-23f : 1.0f - 0x1p-24f;
-        }
-    }
+// the largest of three magnitudes, NaN if one is
+__device__ __forceinline__ float largest3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// the largest over the warp of values without a sign, NaN if one is
+__device__ __forceinline__ float warp_largest(float x) {
+    float r;
+    asm("redux.sync.max.NaN.f32 %0, %1, 0xFFFFFFFF;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2_rz(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2_ru(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rp.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float reciprocal_fast(float x) {           // within 1 ulp
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// act(g) = g share, share = sigmoid(y), and its derivative, for two g.  SILU: y = g; GELU: y = 2 sqrt(2/pi) (g + 0.044715 g^3).  With
+// t = exp(-|y|), r = 1 / (1 + t) and q = t r = sigmoid(-|y|) the share is q below 0 and 1 - q = r above:
+//   below 0: act = g q, act' = q + g q r y';    above: act = g - g q, act' = 1 + q (act y' - 1).
+// Products of codes have so few digits that many lie exactly halfway between two codes, and a share just below 1 must put them on the right
+// side: t is kept above 0 there, g - g q is rounded towards 0, so that it is not g, and act' (above 1 wherever q is small) up, so that it is not 1.
+// (x act(g) is then off x g by more than half a step unless x g is a power of two, which is no such halfway case.)
+struct Gate2 {
+    uint64_t value, slope;
 };
+template <bool kSlope, bool kGelu> __device__ __forceinline__ Gate2 gate2(float g0, float g1) {
+    constexpr float kA = 1.5957691216057308f, kB = 0.044715f, kLeast = 0x1p-100f;
+    float y0 = g0, y1 = g1;
+    const uint64_t g = pack2(g0, g1), one = pack2(1.0f, 1.0f), minus = pack2(-1.0f, -1.0f);
+    uint64_t dy = one;
+    if constexpr (kGelu) {
+        // (beyond 100 the share is 0 or 1, and g^3 stays a number)
+        const uint64_t c = pack2(fminf(fmaxf(g0, -100.0f), 100.0f), fminf(fmaxf(g1, -100.0f), 100.0f)), c2 = mul2(c, c);
+        unpack2(mul2(mul2(c, pack2(kA, kA)), fma2(c2, pack2(kB, kB), one)), y0, y1);
+        if (kSlope) dy = fma2(c2, pack2(3.0f * kA * kB, 3.0f * kA * kB), pack2(kA, kA));
+    }
+    const bool low0 = g0 < 0.0f, low1 = g1 < 0.0f;
+    float t0 = exp2_fast(__fmul_rn(fabsf(y0), -kLog2E)), t1 = exp2_fast(__fmul_rn(fabsf(y1), -kLog2E));
+    t0 = low0 ? t0 : fmaxf(t0, kLeast);
+    t1 = low1 ? t1 : fmaxf(t1, kLeast);
+    const uint64_t t = pack2(t0, t1);
+    float d0, d1;
+    unpack2(add2(t, one), d0, d1);
+    const uint64_t r = pack2(reciprocal_fast(d0), reciprocal_fast(d1)), q = mul2(t, r), gq = mul2(g, q);
+    const uint64_t less = add2_rz(g, mul2(gq, minus));
+    float a0, a1, b0, b1;
+    unpack2(gq, a0, a1);
+    unpack2(less, b0, b1);
+    Gate2 gate;
+    gate.value = pack2(low0 ? a0 : b0, low1 ? a1 : b1);
+    if (kSlope) {
+        const uint64_t below = fma2(mul2(gq, r), dy, q), above = fma2_ru(q, fma2(less, dy, minus), one);
+        unpack2(below, a0, a1);
+        unpack2(above, b0, b1);
+        gate.slope = pack2(low0 ? a0 : b0, low1 ? a1 : b1);
+    }
+    return gate;
+}
 
 // Host side -------------------------------------------------------------------------------------------------------
 

@@ -256,10 +256,10 @@ __device__ __forceinline__ void hold64(const Act8& out, uint32_t row, uint32_t c
     }
 }
 __device__ __forceinline__ uint32_t largest64(const float* v) {
-    uint32_t m = 0;
+    float m = 0.0f;
 #pragma unroll
-    for (uint32_t j = 0; j < 64; ++j) m = max(m, magnitude(v[j]));
-    return m;
+    for (uint32_t j = 0; j < 64; j += 2) m = largest3(m, v[j], v[j + 1]);
+    return magnitude(m);
 }
 
 // ---- the kernel ----
@@ -279,6 +279,15 @@ template <typename S> struct Shared {
     uint32_t largest[S::kGated ? (S::kFew ? 2 * 3 * (S::kQ / 2) * 4 : 3 * 2 * 128) : 1];
 };
 
+// h = act(g) u
+template <bool kGelu, uint32_t kN> __device__ __forceinline__ void gate_times(float* h, const float* g, const float* u) {
+#pragma unroll
+    for (uint32_t j = 0; j < kN; j += 2) {
+        const Gate2 a = gate2<false, kGelu>(g[j], g[j + 1]);
+        unpack2(mul2(a.value, pack2(u[j], u[j + 1])), h[j], h[j + 1]);
+    }
+}
+
 // A few rows' g and u of one column each: the first `count` of the rows row0 .. .  The block of a row is the 128 lanes of a warp group.
 template <typename S, uint32_t kN>
 __device__ __forceinline__ void finish_few_gated(const Task& task, Shared<S>& sh, float (&g)[kN], float (&u)[kN], uint32_t count, uint32_t row0,
@@ -291,7 +300,13 @@ __device__ __forceinline__ void finish_few_gated(const Task& task, Shared<S>& sh
         // (beyond the last column the powers are anything: what stands there is no number)
         g[j] = !ok ? __uint_as_float(kLost) : col < f ? g[j] : 0.0f;
         u[j] = col < f ? u[j] : 0.0f;
-        h[j] = __fmul_rn(Gate(g[j], task.gelu).value, u[j]);
+    }
+    if (task.gelu)
+        gate_times<true, kN>(h, g, u);
+    else
+        gate_times<false, kN>(h, g, u);
+#pragma unroll
+    for (uint32_t j = 0; j < kN; ++j) {
         if (j < count) {
             const uint32_t mg = __reduce_max_sync(0xFFFFFFFFu, magnitude(g[j])), mu = __reduce_max_sync(0xFFFFFFFFu, magnitude(u[j])),
                            mh = __reduce_max_sync(0xFFFFFFFFu, magnitude(h[j]));
@@ -546,8 +561,10 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                     scale(task.gate, bg);
                     scale(task.up, bu);
                 }
-#pragma unroll
-                for (uint32_t j = 0; j < 64; ++j) g[j] = __fmul_rn(Gate(g[j], task.gelu).value, u[j]);
+                if (task.gelu)
+                    gate_times<true, 64>(g, g, u);
+                else
+                    gate_times<false, 64>(g, g, u);
                 if (task.h.codes) {
                     join(2, largest64(g));
                     named_barrier_sync(1, kEpilogueWarps * 32);
