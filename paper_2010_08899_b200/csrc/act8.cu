@@ -3,15 +3,15 @@
 //
 // All but the reading back work on tiles of 128 x 128 elements, so that both a row's block and, in the transpose, a column's block are the tile's
 // own.  A CTA goes from tile to tile; tensor copies bring the next tile's inputs into shared memory while this one is worked on.  A warp has eight
-// rows of the tile, a lane four columns of them: a row's largest magnitude is one reduction over the warp, a column's goes through shared
-// memory, and a lane's eight codes of a column lie next to each other in the transpose, which leaves shared memory as rows of 128 bytes.
+// (or four) rows of the tile, a lane four columns of them: a row's largest magnitude is one reduction over the warp, a column's goes through shared
+// memory, and a lane's codes of a column lie next to each other in the transpose, which leaves shared memory as rows of 128 bytes.
 #include "act8.cuh"
 
 namespace dct {
 namespace {
 
-constexpr uint32_t kTileThreads = 512, kWarps = kTileThreads / 32;
-constexpr uint32_t kR = 8, kC = 4;                   // a lane's rows and columns
+constexpr uint32_t kC = 4;                           // a lane's columns
+constexpr uint32_t kUnpackRows = 8;                  // a lane's rows when reading back
 constexpr uint32_t kTurnedBytes = 128 * 128;         // a plane's transposed codes
 
 struct TileTask {
@@ -45,7 +45,7 @@ __device__ __forceinline__ void four(float (&v)[kC], uint32_t codes, float power
 
 // A dense tile whose rows start on no boundary, into the place a tensor copy would have put it: every warp its own rows, neighbouring lanes
 // neighbouring elements, zeros outside.
-template <typename T>
+template <typename T, uint32_t kR>
 __device__ __forceinline__ void fetch_rows(T* tile, const TileTask& task, uint32_t row0, uint32_t col0) {
     const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
     const T* x = static_cast<const T*>(task.x);
@@ -63,9 +63,10 @@ __device__ __forceinline__ void fetch_rows(T* tile, const TileTask& task, uint32
     __syncwarp();
 }
 
-// What a tile's planes are made of.  load(): the lane's patch of each plane; power: of the lane's row (lane & 7) of each held input.
+// What a tile's planes are made of.  kR: a lane's rows.  load(): the lane's patch of each plane; power: of the lane's row (lane % kR) of each held
+// input.
 template <typename T> struct Dense {
-    static constexpr uint32_t kPlanes = 1, kHeld = 0, kDenseBytes = 128 * 128 * sizeof(T), kCtas = sizeof(T) == 4 ? 1 : 2;
+    static constexpr uint32_t kR = 8, kPlanes = 1, kHeld = 0, kDenseBytes = 128 * 128 * sizeof(T), kCtas = sizeof(T) == 4 ? 1 : 2;
     using Element = T;
     __device__ static __forceinline__ void load(float (&v)[1][kR][kC], const uint8_t* stage, const float*) {
         const T* from = reinterpret_cast<const T*>(stage) + (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
@@ -74,7 +75,7 @@ template <typename T> struct Dense {
     }
 };
 struct Held {
-    static constexpr uint32_t kPlanes = 1, kHeld = 1, kDenseBytes = 0, kCtas = 2;
+    static constexpr uint32_t kR = 8, kPlanes = 1, kHeld = 1, kDenseBytes = 0, kCtas = 2;
     using Element = float;
     __device__ static __forceinline__ void load(float (&v)[1][kR][kC], const uint8_t* stage, const float* power) {
         const uint8_t* from = stage + (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
@@ -82,9 +83,10 @@ struct Held {
         for (uint32_t r = 0; r < kR; ++r) four(v[0][r], *reinterpret_cast<const uint32_t*>(from + r * 128), __shfl_sync(0xFFFFFFFFu, power[0], r));
     }
 };
-// dh, gate and up; the planes are dgate, dup and h
+// dh, gate and up; the planes are dgate, dup and h.  Three planes of eight rows leave an SM 16 warps, of four rows 32 (8192 x 8192: XX against YY us);
+// fp32 tiles leave no room for the maxima of 32 warps.
 template <typename T, bool kGelu> struct Gated {
-    static constexpr uint32_t kPlanes = 3, kHeld = 2, kDenseBytes = 128 * 128 * sizeof(T), kCtas = 1;
+    static constexpr uint32_t kR = sizeof(T) == 4 ? 8 : 4, kPlanes = 3, kHeld = 2, kDenseBytes = 128 * 128 * sizeof(T), kCtas = 1;
     using Element = T;
     __device__ static __forceinline__ void load(float (&v)[3][kR][kC], const uint8_t* stage, const float* power) {
         const uint32_t at = (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
@@ -108,13 +110,15 @@ template <typename T, bool kGelu> struct Gated {
 
 template <typename S> struct TileShape {
     static constexpr uint32_t kStageBytes = S::kDenseBytes + S::kHeld * 128 * 128;
+    static constexpr uint32_t kWarps = 128 / S::kR, kThreads = kWarps * 32;
     static constexpr uint32_t kLargestBytes = S::kPlanes * kWarps * 128 * 4;
     static constexpr uint32_t kSharedBytes = 128 + 2 * kStageBytes + kLargestBytes;
     static_assert(kStageBytes >= S::kPlanes * kTurnedBytes, "the transposed codes take the place of a tile's inputs");
 };
 
-// A lane's patch of a plane by rows: eight reductions under way at once, and row r's byte and power worked out by lane r alone.  whole: the tile
+// A lane's patch of a plane by rows: all its reductions under way at once, and row r's byte and power worked out by lane r alone.  whole: the tile
 // lies inside the matrix.
+template <uint32_t kR>
 __device__ __forceinline__ void write_rows(const float (&v)[kR][kC], const Act8& out, uint32_t row0, uint32_t col0, bool whole) {
     const uint32_t lane = lane_id(), col = col0 + lane * kC;
     float m[kR], mine = 0.0f;
@@ -159,8 +163,9 @@ __device__ __forceinline__ void write_rows(const float (&v)[kR][kC], const Act8&
 }
 
 template <typename S>
-__global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const __grid_constant__ TileTask task) {
+__global__ void __launch_bounds__(TileShape<S>::kThreads, S::kCtas) act8_tile_kernel(const __grid_constant__ TileTask task) {
     using Shape = TileShape<S>;
+    constexpr uint32_t kR = S::kR, kWarps = Shape::kWarps, kTileThreads = Shape::kThreads;
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t arrived[2];
     __shared__ alignas(16) uint32_t bytes[S::kPlanes][128];
@@ -186,6 +191,14 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
     };
     if (threadIdx.x == 0 && copied && blockIdx.x < tiles) fetch(blockIdx.x, 0);
     __syncthreads();
+    uint32_t byte0 = 0, byte1 = 0;
+    const auto next_bytes = [&](uint32_t t) {
+        const uint32_t row = t / task.tiles_c * 128u + warp * kR + lane % kR, block = t % task.tiles_c;
+        const auto byte_of = [&](const Act8& m) -> uint32_t { return row < task.rows ? m.scales[act8_scale_offset(m.row_tiles, row, block)] : 0u; };
+        if constexpr (S::kHeld >= 1) byte0 = byte_of(task.held[0]);
+        if constexpr (S::kHeld >= 2) byte1 = byte_of(task.held[1]);
+    };
+    next_bytes(blockIdx.x);
     uint32_t s = 0, phase = 0;
     bool ok = true;
     for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
@@ -193,15 +206,10 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
         const bool whole = row0 + 128 <= task.rows && col0 + 128 <= task.cols;
         if (threadIdx.x == 0 && copied && ok && t + gridDim.x < tiles) fetch(t + gridDim.x, s ^ 1u);
         uint8_t* stage = stages + s * Shape::kStageBytes;
-        // the powers of the warp's rows: lane r has row r's
-        float power[2] = {};
-        const auto power_of = [&](const Act8& m) {
-            const uint32_t row = row0 + warp * kR + (lane & 7u);
-            return row < task.rows ? act8_power(m.scales[act8_scale_offset(m.row_tiles, row, col0 >> 7)]) : 0.0f;
-        };
-        if constexpr (S::kHeld >= 1) power[0] = power_of(task.held[0]);
-        if constexpr (S::kHeld >= 2) power[1] = power_of(task.held[1]);
-        if (S::kDenseBytes != 0 && task.direct && task.x) fetch_rows(reinterpret_cast<typename S::Element*>(stage), task, row0, col0);
+        // the powers of the warp's rows (lane r has row r's) were asked for a tile ago; the next tile's are now
+        const float power[2] = {act8_power(byte0), act8_power(byte1)};
+        if (t + gridDim.x < tiles) next_bytes(t + gridDim.x);
+        if (S::kDenseBytes != 0 && task.direct && task.x) fetch_rows<typename S::Element, kR>(reinterpret_cast<typename S::Element*>(stage), task, row0, col0);
         if (copied && ok && !mbar_wait_bounded(&arrived[s], phase, task.limit, &stop)) {
             ok = false;
             *const_cast<volatile uint32_t*>(&stop) = 1u;
@@ -245,7 +253,7 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
                 }
             }
             __syncthreads();
-            // (a half-warp's sixteen lanes write sixteen different groups: no two to the same bank)
+            // (neighbouring lanes write different groups of a column's codes: no two to the same bank at a time)
 #pragma unroll
             for (uint32_t p = 0; p < S::kPlanes; ++p) {
                 if (!task.turned[p].codes) continue;
@@ -258,15 +266,20 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
                     unpack2(mul2(pack2(v[p][r][0], v[p][r][1]), f01), x[r][0], x[r][1]);
                     unpack2(mul2(pack2(v[p][r][2], v[p][r][3]), f23), x[r][2], x[r][3]);
                 }
-                uint8_t* to = stage + p * kTurnedBytes + ((warp ^ (lane & 15u)) << 3);
+                uint8_t* to = stage + p * kTurnedBytes + (warp ^ (lane % kWarps)) * kR;
 #pragma unroll
                 for (uint32_t c = 0; c < kC; ++c) {
-                    uint2 q = make_uint2(act8_codes4(x[0][c], x[1][c], x[2][c], x[3][c]), act8_codes4(x[4][c], x[5][c], x[6][c], x[7][c]));
-                    if (huge) {
-                        const uint32_t byte = c == 0 ? b.x : c == 1 ? b.y : c == 2 ? b.z : b.w;
-                        q = make_uint2(act8_finite4(q.x, byte), act8_finite4(q.y, byte));
+                    const uint32_t byte = c == 0 ? b.x : c == 1 ? b.y : c == 2 ? b.z : b.w;
+                    uint32_t q[kR / 4];
+#pragma unroll
+                    for (uint32_t i = 0; i < kR / 4; ++i) {
+                        q[i] = act8_codes4(x[4 * i][c], x[4 * i + 1][c], x[4 * i + 2][c], x[4 * i + 3][c]);
+                        if (huge) q[i] = act8_finite4(q[i], byte);
                     }
-                    *reinterpret_cast<uint2*>(to + (lane * kC + c) * 128u) = q;
+                    if constexpr (kR == 8)
+                        *reinterpret_cast<uint2*>(to + (lane * kC + c) * 128u) = make_uint2(q[0], q[1]);
+                    else
+                        *reinterpret_cast<uint32_t*>(to + (lane * kC + c) * 128u) = q[0];
                 }
             }
             __syncthreads();
@@ -276,11 +289,18 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
                 if (!out.codes) continue;
 #pragma unroll
                 for (uint32_t i = 0; i < 128u * 8u / kTileThreads; ++i) {
-                    const uint32_t c = i * (kTileThreads / 8u) + (threadIdx.x >> 3), pair = threadIdx.x & 7u, key = (c >> 2) & 15u;
-                    const uint32_t row = col0 + c, col = row0 + pair * 16u;           // of the transpose
+                    const uint32_t c = i * (kTileThreads / 8u) + (threadIdx.x >> 3), part = threadIdx.x & 7u, key = (c >> 2) % kWarps;
+                    const uint32_t row = col0 + c, col = row0 + part * 16u;           // of the transpose
                     if (!whole && (row >= out.rows || col >= out.cols)) continue;
-                    uint4 q = *reinterpret_cast<const uint4*>(stage + p * kTurnedBytes + c * 128u + (((2u * pair) ^ (key & 14u)) << 3));
-                    if (key & 1u) q = make_uint4(q.z, q.w, q.x, q.y);
+                    // sixteen codes are 16 / kR groups, exchanged among themselves by the key's low bits
+                    constexpr uint32_t kGroups = 16 / kR;
+                    uint4 q = *reinterpret_cast<const uint4*>(stage + p * kTurnedBytes + c * 128u + ((part * kGroups) ^ (key & ~(kGroups - 1u))) * kR);
+                    if constexpr (kR == 8) {
+                        if (key & 1u) q = make_uint4(q.z, q.w, q.x, q.y);
+                    } else {
+                        if (key & 1u) q = make_uint4(q.y, q.x, q.w, q.z);
+                        if (key & 2u) q = make_uint4(q.z, q.w, q.x, q.y);
+                    }
                     uint8_t* to = out.codes + static_cast<size_t>(row) * out.ld + col;
                     if (whole || col + 16 <= out.cols) {
                         st_unit(to, q);
@@ -303,6 +323,7 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
 // neighbouring elements.
 template <typename T>
 __global__ void __launch_bounds__(256) act8_unpack_kernel(const Act8 a, T* y, const uint32_t ld_y, const uint32_t tiles_c, const bool aligned) {
+    constexpr uint32_t kR = kUnpackRows;
     __shared__ T turn[8][128];
     const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
     const uint32_t row0 = blockIdx.x / tiles_c * 64u + warp * kR, col0 = blockIdx.x % tiles_c * 128u, col = col0 + lane * kC;
@@ -378,7 +399,7 @@ dct_status_t launch_tiles(TileTask& task, uint32_t rows, uint32_t cols, const vo
     if (held0 && (st = tensor_map(e, &task.map[1], held0, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != DCT_OK) return st;
     if (held1 && (st = tensor_map(e, &task.map[2], held1, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != DCT_OK) return st;
     const uint64_t at_once = static_cast<uint64_t>(sms) * S::kCtas;
-    act8_tile_kernel<S><<<static_cast<unsigned>(tiles < at_once ? tiles : at_once), kTileThreads, TileShape<S>::kSharedBytes, stream>>>(task);
+    act8_tile_kernel<S><<<static_cast<unsigned>(tiles < at_once ? tiles : at_once), TileShape<S>::kThreads, TileShape<S>::kSharedBytes, stream>>>(task);
     DCT_CUDA_TRY(cudaGetLastError());
     return DCT_OK;
 }

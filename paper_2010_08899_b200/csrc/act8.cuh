@@ -77,9 +77,9 @@ __device__ __forceinline__ float warp_largest(float x) {
     asm("redux.sync.max.NaN.f32 %0, %1, 0xFFFFFFFF;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ uint64_t add2_rz(uint64_t a, uint64_t b) {
+__device__ __forceinline__ uint64_t fma2_rz(uint64_t a, uint64_t b, uint64_t c) {
     uint64_t r;
-    asm("add.rz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    asm("fma.rz.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
 __device__ __forceinline__ uint64_t fma2_ru(uint64_t a, uint64_t b, uint64_t c) {
@@ -97,13 +97,13 @@ __device__ __forceinline__ float reciprocal_fast(float x) {           // within 
 // t = exp(-|y|), r = 1 / (1 + t) and q = t r = sigmoid(-|y|) the share is q below 0 and 1 - q = r above:
 //   below 0: act = g q, act' = q + g q r y';    above: act = g - g q, act' = 1 + q (act y' - 1).
 // Products of codes have so few digits that many lie exactly halfway between two codes, and a share just below 1 must put them on the right
-// side: t is kept above 0 there, g - g q is rounded towards 0, so that it is not g, and act' (above 1 wherever q is small) up, so that it is not 1.
+// side: t is kept above 0, g - g q is rounded towards 0, so that it is not g, and act' (above 1 wherever q is small) up, so that it is not 1.
 // (x act(g) is then off x g by more than half a step unless x g is a power of two, which is no such halfway case.)
 struct Gate2 {
     uint64_t value, slope;
 };
 template <bool kSlope, bool kGelu> __device__ __forceinline__ Gate2 gate2(float g0, float g1) {
-    constexpr float kA = 1.5957691216057308f, kB = 0.044715f, kLeast = 0x1p-100f;
+    constexpr float kA = 1.5957691216057308f, kB = 0.044715f, kLeast = 0x1p-126f;
     float y0 = g0, y1 = g1;
     const uint64_t g = pack2(g0, g1), one = pack2(1.0f, 1.0f), minus = pack2(-1.0f, -1.0f);
     uint64_t dy = one;
@@ -114,14 +114,11 @@ template <bool kSlope, bool kGelu> __device__ __forceinline__ Gate2 gate2(float 
         if (kSlope) dy = fma2(c2, pack2(3.0f * kA * kB, 3.0f * kA * kB), pack2(kA, kA));
     }
     const bool low0 = g0 < 0.0f, low1 = g1 < 0.0f;
-    float t0 = exp2_fast(__fmul_rn(fabsf(y0), -kLog2E)), t1 = exp2_fast(__fmul_rn(fabsf(y1), -kLog2E));
-    t0 = low0 ? t0 : fmaxf(t0, kLeast);
-    t1 = low1 ? t1 : fmaxf(t1, kLeast);
-    const uint64_t t = pack2(t0, t1);
+    const uint64_t t = pack2(fmaxf(exp2_fast(__fmul_rn(fabsf(y0), -kLog2E)), kLeast), fmaxf(exp2_fast(__fmul_rn(fabsf(y1), -kLog2E)), kLeast));
     float d0, d1;
     unpack2(add2(t, one), d0, d1);
     const uint64_t r = pack2(reciprocal_fast(d0), reciprocal_fast(d1)), q = mul2(t, r), gq = mul2(g, q);
-    const uint64_t less = add2_rz(g, mul2(gq, minus));
+    const uint64_t less = fma2_rz(gq, minus, g);
     float a0, a1, b0, b1;
     unpack2(gq, a0, a1);
     unpack2(less, b0, b1);
