@@ -3,15 +3,15 @@
 //
 // All but the reading back work on tiles of 128 x 128 elements, so that both a row's block and, in the transpose, a column's block are the tile's
 // own.  A CTA goes from tile to tile; tensor copies bring the next tile's inputs into shared memory while this one is worked on.  A warp has eight
-// (or four) rows of the tile, a lane four columns of them: a row's largest magnitude is one reduction over the warp, a column's goes through shared
+// rows of the tile, a lane four columns of them: a row's largest magnitude is one reduction over the warp, a column's goes through shared
 // memory, and a lane's codes of a column lie next to each other in the transpose, which leaves shared memory as rows of 128 bytes.
 #include "act8.cuh"
 
 namespace dct {
 namespace {
 
-constexpr uint32_t kC = 4;                           // a lane's columns
-constexpr uint32_t kUnpackRows = 8;                  // a lane's rows when reading back
+constexpr uint32_t kTileThreads = 512, kWarps = kTileThreads / 32;
+constexpr uint32_t kR = 8, kC = 4;                   // a lane's rows and columns
 constexpr uint32_t kTurnedBytes = 128 * 128;         // a plane's transposed codes
 
 struct TileTask {
@@ -45,7 +45,7 @@ __device__ __forceinline__ void four(float (&v)[kC], uint32_t codes, float power
 
 // A dense tile whose rows start on no boundary, into the place a tensor copy would have put it: every warp its own rows, neighbouring lanes
 // neighbouring elements, zeros outside.
-template <typename T, uint32_t kR>
+template <typename T>
 __device__ __forceinline__ void fetch_rows(T* tile, const TileTask& task, uint32_t row0, uint32_t col0) {
     const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
     const T* x = static_cast<const T*>(task.x);
@@ -63,10 +63,9 @@ __device__ __forceinline__ void fetch_rows(T* tile, const TileTask& task, uint32
     __syncwarp();
 }
 
-// What a tile's planes are made of.  kR: a lane's rows.  load(): the lane's patch of each plane; power: of the lane's row (lane % kR) of each held
-// input.
+// What a tile's planes are made of.  load(): the lane's patch of each plane; power: of the lane's row (lane % 8) of each held input.
 template <typename T> struct Dense {
-    static constexpr uint32_t kR = 8, kPlanes = 1, kHeld = 0, kDenseBytes = 128 * 128 * sizeof(T), kCtas = sizeof(T) == 4 ? 1 : 2;
+    static constexpr uint32_t kPlanes = 1, kHeld = 0, kDenseBytes = 128 * 128 * sizeof(T), kCtas = sizeof(T) == 4 ? 1 : 2;
     using Element = T;
     __device__ static __forceinline__ void load(float (&v)[1][kR][kC], const uint8_t* stage, const float*) {
         const T* from = reinterpret_cast<const T*>(stage) + (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
@@ -75,7 +74,7 @@ template <typename T> struct Dense {
     }
 };
 struct Held {
-    static constexpr uint32_t kR = 8, kPlanes = 1, kHeld = 1, kDenseBytes = 0, kCtas = 2;
+    static constexpr uint32_t kPlanes = 1, kHeld = 1, kDenseBytes = 0, kCtas = 2;
     using Element = float;
     __device__ static __forceinline__ void load(float (&v)[1][kR][kC], const uint8_t* stage, const float* power) {
         const uint8_t* from = stage + (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
@@ -83,10 +82,9 @@ struct Held {
         for (uint32_t r = 0; r < kR; ++r) four(v[0][r], *reinterpret_cast<const uint32_t*>(from + r * 128), __shfl_sync(0xFFFFFFFFu, power[0], r));
     }
 };
-// dh, gate and up; the planes are dgate, dup and h.  Three planes of eight rows leave an SM 16 warps, of four rows 32 (8192 x 8192: XX against YY us);
-// fp32 tiles leave no room for the maxima of 32 warps.
+// dh, gate and up; the planes are dgate, dup and h
 template <typename T, bool kGelu> struct Gated {
-    static constexpr uint32_t kR = sizeof(T) == 4 ? 8 : 4, kPlanes = 3, kHeld = 2, kDenseBytes = 128 * 128 * sizeof(T), kCtas = 1;
+    static constexpr uint32_t kPlanes = 3, kHeld = 2, kDenseBytes = 128 * 128 * sizeof(T), kCtas = 1;
     using Element = T;
     __device__ static __forceinline__ void load(float (&v)[3][kR][kC], const uint8_t* stage, const float* power) {
         const uint32_t at = (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
@@ -110,17 +108,16 @@ template <typename T, bool kGelu> struct Gated {
 
 template <typename S> struct TileShape {
     static constexpr uint32_t kStageBytes = S::kDenseBytes + S::kHeld * 128 * 128;
-    static constexpr uint32_t kWarps = 128 / S::kR, kThreads = kWarps * 32;
     static constexpr uint32_t kLargestBytes = S::kPlanes * kWarps * 128 * 4;
     static constexpr uint32_t kSharedBytes = 128 + 2 * kStageBytes + kLargestBytes;
     static_assert(kStageBytes >= S::kPlanes * kTurnedBytes, "the transposed codes take the place of a tile's inputs");
 };
 
-// A lane's patch of a plane by rows: all its reductions under way at once, and row r's byte and power worked out by lane r alone.  whole: the tile
-// lies inside the matrix.
-template <uint32_t kR>
-__device__ __forceinline__ void write_rows(const float (&v)[kR][kC], const Act8& out, uint32_t row0, uint32_t col0, bool whole) {
-    const uint32_t lane = lane_id(), col = col0 + lane * kC;
+// A lane's patch of a plane by rows: all its reductions under way at once, and row r's byte and power worked out by lane r alone.  kWhole: the
+// tile lies inside the matrix.
+template <bool kWhole>
+__device__ __forceinline__ void write_rows(const float (&v)[kR][kC], const Act8& out, uint32_t tile_r, uint32_t tile_c) {
+    const uint32_t warp = threadIdx.x >> 5, lane = lane_id(), row = tile_r * 128u + warp * kR, col = tile_c * 128u + lane * kC;
     float m[kR], mine = 0.0f;
 #pragma unroll
     for (uint32_t r = 0; r < kR; ++r) m[r] = warp_largest(largest3(largest3(v[r][0], v[r][1], v[r][2]), v[r][3], 0.0f));
@@ -128,9 +125,8 @@ __device__ __forceinline__ void write_rows(const float (&v)[kR][kC], const Act8&
     for (uint32_t r = 0; r < kR; ++r) mine = lane == r ? m[r] : mine;
     const uint32_t byte = act8_byte(magnitude(mine));
     const float inverse = act8_inverse(byte);
-    const bool huge = __any_sync(0xFFFFFFFFu, byte == 247u);
-    if (lane < kR && row0 + lane < out.rows)
-        out.scales[act8_scale_offset(out.row_tiles, row0, col0 >> 7) + lane * 16u] = static_cast<uint8_t>(byte);
+    if (lane < kR && (kWhole || row + lane < out.rows))
+        out.scales[act8_scale_tile(out.row_tiles, tile_r, tile_c) + act8_scale_row(warp * kR + lane)] = static_cast<uint8_t>(byte);
     uint32_t q[kR];
 #pragma unroll
     for (uint32_t r = 0; r < kR; ++r) {
@@ -140,48 +136,96 @@ __device__ __forceinline__ void write_rows(const float (&v)[kR][kC], const Act8&
         unpack2(mul2(pack2(v[r][2], v[r][3]), pack2(f, f)), c, d);
         q[r] = act8_codes4(a, b, c, d);
     }
-    if (huge) {
+    if (__any_sync(0xFFFFFFFFu, byte == 247u)) {
 #pragma unroll
         for (uint32_t r = 0; r < kR; ++r) q[r] = act8_finite4(q[r], __shfl_sync(0xFFFFFFFFu, byte, r));
     }
-    uint8_t* to = out.codes + static_cast<size_t>(row0) * out.ld + col;
-    if (whole) {
+    uint8_t* to = out.codes + static_cast<size_t>(row) * out.ld + col;
 #pragma unroll
-        for (uint32_t r = 0; r < kR; ++r) *reinterpret_cast<uint32_t*>(to + static_cast<size_t>(r) * out.ld) = q[r];
-    } else {
-#pragma unroll
-        for (uint32_t r = 0; r < kR; ++r) {
-            if (row0 + r >= out.rows) break;
-            if (col + kC <= out.cols) {
-                *reinterpret_cast<uint32_t*>(to) = q[r];
-            } else {
-                for (uint32_t c = 0; col + c < out.cols; ++c) to[c] = static_cast<uint8_t>(q[r] >> (8 * c));
-            }
-            to += out.ld;
+    for (uint32_t r = 0; r < kR; ++r) {
+        if (kWhole || (row + r < out.rows && col + kC <= out.cols)) {
+            *reinterpret_cast<uint32_t*>(to) = q[r];
+        } else if (row + r < out.rows) {
+            for (uint32_t c = 0; col + c < out.cols; ++c) to[c] = static_cast<uint8_t>(q[r] >> (8 * c));
         }
+        to += out.ld;
+    }
+}
+
+// A lane's columns of its warp's eight rows: the magnitudes' maxima, for the columns' blocks
+__device__ __forceinline__ void note_columns(const float (&v)[kR][kC], float* largest) {
+    float m[kC] = {};
+#pragma unroll
+    for (uint32_t r = 0; r < kR; r += 2)
+#pragma unroll
+        for (uint32_t c = 0; c < kC; ++c) m[c] = largest3(m[c], v[r][c], v[r + 1][c]);
+    *reinterpret_cast<float4*>(largest + (threadIdx.x >> 5) * 128u + lane_id() * kC) = make_float4(m[0], m[1], m[2], m[3]);
+}
+// The patch's columns as codes, eight of a column together, to where the columns lie as rows.  (Neighbouring lanes write different groups of
+// a column's codes: no two to the same bank at a time.)
+__device__ __forceinline__ void turn_columns(const float (&v)[kR][kC], const uint32_t* bytes, uint8_t* turned) {
+    const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
+    const uint4 b = *reinterpret_cast<const uint4*>(bytes + lane * kC);
+    const uint64_t f01 = pack2(act8_inverse(b.x), act8_inverse(b.y)), f23 = pack2(act8_inverse(b.z), act8_inverse(b.w));
+    const bool huge = __any_sync(0xFFFFFFFFu, b.x == 247u || b.y == 247u || b.z == 247u || b.w == 247u);
+    float x[kR][kC];
+#pragma unroll
+    for (uint32_t r = 0; r < kR; ++r) {
+        unpack2(mul2(pack2(v[r][0], v[r][1]), f01), x[r][0], x[r][1]);
+        unpack2(mul2(pack2(v[r][2], v[r][3]), f23), x[r][2], x[r][3]);
+    }
+    uint8_t* to = turned + ((warp ^ (lane & 15u)) << 3) + lane * (kC * 128u);
+#pragma unroll
+    for (uint32_t c = 0; c < kC; ++c) {
+        uint2 q = make_uint2(act8_codes4(x[0][c], x[1][c], x[2][c], x[3][c]), act8_codes4(x[4][c], x[5][c], x[6][c], x[7][c]));
+        if (huge) {
+            const uint32_t byte = c == 0 ? b.x : c == 1 ? b.y : c == 2 ? b.z : b.w;
+            q = make_uint2(act8_finite4(q.x, byte), act8_finite4(q.y, byte));
+        }
+        *reinterpret_cast<uint2*>(to + c * 128u) = q;
+    }
+}
+// The turned tile to the transpose, sixteen codes at a time
+template <bool kWhole>
+__device__ __forceinline__ void write_turned(const uint8_t* turned, const Act8& out, uint32_t tile_r, uint32_t tile_c) {
+    const uint32_t c0 = threadIdx.x >> 3, pair = threadIdx.x & 7u, row0 = tile_c * 128u + c0, col = tile_r * 128u + pair * 16u;           // of the transpose
+    uint8_t* to = out.codes + static_cast<size_t>(row0) * out.ld + col;
+#pragma unroll
+    for (uint32_t i = 0; i < 128u * 8u / kTileThreads; ++i) {
+        const uint32_t c = c0 + i * (kTileThreads / 8u), key = (c >> 2) & 15u;
+        if (!kWhole && (tile_c * 128u + c >= out.rows || col >= out.cols)) break;
+        uint4 q = *reinterpret_cast<const uint4*>(turned + c * 128u + (((2u * pair) ^ (key & 14u)) << 3));
+        if (key & 1u) q = make_uint4(q.z, q.w, q.x, q.y);
+        if (kWhole || col + 16 <= out.cols) {
+            st_unit(to, q);
+        } else {
+            for (uint32_t k = 0; col + k < out.cols; ++k)
+                to[k] = static_cast<uint8_t>((k < 8 ? (k < 4 ? q.x : q.y) : (k < 12 ? q.z : q.w)) >> (8 * (k & 3u)));
+        }
+        to += static_cast<size_t>(out.ld) * (kTileThreads / 8u);
     }
 }
 
 template <typename S>
-__global__ void __launch_bounds__(TileShape<S>::kThreads, S::kCtas) act8_tile_kernel(const __grid_constant__ TileTask task) {
+__global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const __grid_constant__ TileTask task) {
     using Shape = TileShape<S>;
-    constexpr uint32_t kR = S::kR, kWarps = Shape::kWarps, kTileThreads = Shape::kThreads;
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t arrived[2];
     __shared__ alignas(16) uint32_t bytes[S::kPlanes][128];
     __shared__ uint32_t stop;
     uint8_t* stages = raw + ((128u - (smem_addr(raw) & 127u)) & 127u);
     float* largest = reinterpret_cast<float*>(stages + 2 * Shape::kStageBytes);       // [plane][warp][column]
-    const uint32_t warp = threadIdx.x >> 5, lane = lane_id(), tiles = task.tiles_r * task.tiles_c;
+    const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
     const bool copied = S::kHeld != 0 || !task.direct;
+    chain_release_next();
     if (threadIdx.x == 0) {
         mbar_init(&arrived[0], 1);
         mbar_init(&arrived[1], 1);
         stop = 0;
         mbar_init_fence();
     }
-    const auto fetch = [&](uint32_t t, uint32_t s) {
-        const uint32_t x = t % task.tiles_c * 128u, y = t / task.tiles_c * 128u;
+    const auto fetch = [&](uint32_t tile_r, uint32_t tile_c, uint32_t s) {
+        const uint32_t x = tile_c * 128u, y = tile_r * 128u;
         uint8_t* to = stages + s * Shape::kStageBytes;
         const bool dense = S::kDenseBytes != 0 && !task.direct;
         mbar_arrive_expect_tx(&arrived[s], (dense ? S::kDenseBytes : 0u) + S::kHeld * 128 * 128);
@@ -189,33 +233,38 @@ __global__ void __launch_bounds__(TileShape<S>::kThreads, S::kCtas) act8_tile_ke
         if constexpr (S::kHeld >= 1) tile_load(to + S::kDenseBytes, &task.map[1], x, y, &arrived[s]);
         if constexpr (S::kHeld >= 2) tile_load(to + S::kDenseBytes + 128 * 128, &task.map[2], x, y, &arrived[s]);
     };
-    if (threadIdx.x == 0 && copied && blockIdx.x < tiles) fetch(blockIdx.x, 0);
-    __syncthreads();
+    // the bytes of the powers of the warp's rows: lane r has row r's
     uint32_t byte0 = 0, byte1 = 0;
-    const auto next_bytes = [&](uint32_t t) {
-        const uint32_t row = t / task.tiles_c * 128u + warp * kR + lane % kR, block = t % task.tiles_c;
-        const auto byte_of = [&](const Act8& m) -> uint32_t { return row < task.rows ? m.scales[act8_scale_offset(m.row_tiles, row, block)] : 0u; };
-        if constexpr (S::kHeld >= 1) byte0 = byte_of(task.held[0]);
-        if constexpr (S::kHeld >= 2) byte1 = byte_of(task.held[1]);
+    const auto ask_bytes = [&](uint32_t tile_r, uint32_t tile_c) {
+        const uint32_t in = warp * kR + lane % kR;
+        const bool there = tile_r * 128u + in < task.rows;
+        if constexpr (S::kHeld >= 1) byte0 = there ? task.held[0].scales[act8_scale_tile(task.tiles_r, tile_r, tile_c) + act8_scale_row(in)] : 0u;
+        if constexpr (S::kHeld >= 2) byte1 = there ? task.held[1].scales[act8_scale_tile(task.tiles_r, tile_r, tile_c) + act8_scale_row(in)] : 0u;
     };
-    next_bytes(blockIdx.x);
+    const uint32_t step_r = gridDim.x / task.tiles_c, step_c = gridDim.x % task.tiles_c;
+    uint32_t tile_r = blockIdx.x / task.tiles_c, tile_c = blockIdx.x % task.tiles_c;          // (there are at least as many tiles as CTAs)
+    chain_wait_previous();
+    if (threadIdx.x == 0 && copied) fetch(tile_r, tile_c, 0);
+    ask_bytes(tile_r, tile_c);
+    __syncthreads();
     uint32_t s = 0, phase = 0;
     bool ok = true;
-    for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-        const uint32_t col0 = t % task.tiles_c * 128u, row0 = t / task.tiles_c * 128u;
-        const bool whole = row0 + 128 <= task.rows && col0 + 128 <= task.cols;
-        if (threadIdx.x == 0 && copied && ok && t + gridDim.x < tiles) fetch(t + gridDim.x, s ^ 1u);
+    while (tile_r < task.tiles_r) {
+        uint32_t next_r = tile_r + step_r, next_c = tile_c + step_c;
+        if (next_c >= task.tiles_c) next_c -= task.tiles_c, ++next_r;
+        const bool more = next_r < task.tiles_r;
+        if (threadIdx.x == 0 && copied && ok && more) fetch(next_r, next_c, s ^ 1u);
         uint8_t* stage = stages + s * Shape::kStageBytes;
-        // the powers of the warp's rows (lane r has row r's) were asked for a tile ago; the next tile's are now
-        const float power[2] = {act8_power(byte0), act8_power(byte1)};
-        if (t + gridDim.x < tiles) next_bytes(t + gridDim.x);
-        if (S::kDenseBytes != 0 && task.direct && task.x) fetch_rows<typename S::Element, kR>(reinterpret_cast<typename S::Element*>(stage), task, row0, col0);
+        const float power[2] = {act8_power(byte0), act8_power(byte1)};       // asked for a tile ago
+        if (more) ask_bytes(next_r, next_c);
+        if (S::kDenseBytes != 0 && task.direct && task.x)
+            fetch_rows(reinterpret_cast<typename S::Element*>(stage), task, tile_r * 128u, tile_c * 128u);
         if (copied && ok && !mbar_wait_bounded(&arrived[s], phase, task.limit, &stop)) {
             ok = false;
             *const_cast<volatile uint32_t*>(&stop) = 1u;
             if (threadIdx.x == 0) {             // what is still on its way lands before anything else happens here
                 for (uint32_t n = 0; n < task.limit && !mbar_try_wait(&arrived[s], phase); ++n) {}
-                for (uint32_t n = 0; t + gridDim.x < tiles && n < task.limit && !mbar_try_wait(&arrived[s ^ 1u], phase ^ s); ++n) {}
+                for (uint32_t n = 0; more && n < task.limit && !mbar_try_wait(&arrived[s ^ 1u], phase ^ s); ++n) {}
             }
         }
         float v[S::kPlanes][kR][kC];
@@ -224,95 +273,56 @@ __global__ void __launch_bounds__(TileShape<S>::kThreads, S::kCtas) act8_tile_ke
 #pragma unroll
             for (uint32_t p = 0; p < S::kPlanes; ++p)
 #pragma unroll
-                for (uint32_t r = 0; r < kR; ++r) v[p][r][0] = __uint_as_float(0x7FC00000u);
+                for (uint32_t r = 0; r < kR; ++r) v[p][r][0] = v[p][r][1] = v[p][r][2] = v[p][r][3] = __uint_as_float(0x7FC00000u);
         }
+        const bool whole = (tile_r + 1) * 128u <= task.rows && (tile_c + 1) * 128u <= task.cols;
         bool any_turned = false;
 #pragma unroll
         for (uint32_t p = 0; p < S::kPlanes; ++p) {
-            if (p < 2 && task.by_rows[p].codes) write_rows(v[p], task.by_rows[p], row0 + warp * kR, col0, whole);
-            if (!task.turned[p].codes) continue;
-            any_turned = true;
-            float m[kC] = {};
-#pragma unroll
-            for (uint32_t r = 0; r < kR; r += 2)
-#pragma unroll
-                for (uint32_t c = 0; c < kC; ++c) m[c] = largest3(m[c], v[p][r][c], v[p][r + 1][c]);
-            *reinterpret_cast<float4*>(largest + (p * kWarps + warp) * 128u + lane * kC) = make_float4(m[0], m[1], m[2], m[3]);
+            if (p < 2 && task.by_rows[p].codes) {
+                if (whole)
+                    write_rows<true>(v[p], task.by_rows[p], tile_r, tile_c);
+                else
+                    write_rows<false>(v[p], task.by_rows[p], tile_r, tile_c);
+            }
+            if (task.turned[p].codes) {
+                any_turned = true;
+                note_columns(v[p], largest + p * (kWarps * 128));
+            }
         }
         __syncthreads();
         if (any_turned) {
             if (threadIdx.x < S::kPlanes * 128u) {
                 const uint32_t p = threadIdx.x >> 7, c = threadIdx.x & 127u;
-                if (task.turned[p].codes) {
+                const Act8& out = S::kPlanes == 1 ? task.turned[0] : task.turned[p];
+                if (out.codes) {
                     float m = 0.0f;
 #pragma unroll
                     for (uint32_t w = 0; w < kWarps; w += 2) m = largest3(m, largest[(p * kWarps + w) * 128u + c], largest[(p * kWarps + w + 1) * 128u + c]);
                     const uint32_t byte = act8_byte(magnitude(m));
                     bytes[p][c] = byte;
-                    if (col0 + c < task.cols) task.turned[p].scales[act8_scale_offset(task.turned[p].row_tiles, col0 + c, row0 >> 7)] = static_cast<uint8_t>(byte);
+                    if (whole || tile_c * 128u + c < task.cols)
+                        out.scales[act8_scale_tile(task.tiles_c, tile_c, tile_r) + act8_scale_row(c)] = static_cast<uint8_t>(byte);
                 }
             }
             __syncthreads();
-            // (neighbouring lanes write different groups of a column's codes: no two to the same bank at a time)
+#pragma unroll
+            for (uint32_t p = 0; p < S::kPlanes; ++p)
+                if (task.turned[p].codes) turn_columns(v[p], bytes[p], stage + p * kTurnedBytes);
+            __syncthreads();
 #pragma unroll
             for (uint32_t p = 0; p < S::kPlanes; ++p) {
                 if (!task.turned[p].codes) continue;
-                const uint4 b = *reinterpret_cast<const uint4*>(&bytes[p][lane * kC]);
-                const uint64_t f01 = pack2(act8_inverse(b.x), act8_inverse(b.y)), f23 = pack2(act8_inverse(b.z), act8_inverse(b.w));
-                const bool huge = b.x == 247u || b.y == 247u || b.z == 247u || b.w == 247u;
-                float x[kR][kC];
-#pragma unroll
-                for (uint32_t r = 0; r < kR; ++r) {
-                    unpack2(mul2(pack2(v[p][r][0], v[p][r][1]), f01), x[r][0], x[r][1]);
-                    unpack2(mul2(pack2(v[p][r][2], v[p][r][3]), f23), x[r][2], x[r][3]);
-                }
-                uint8_t* to = stage + p * kTurnedBytes + (warp ^ (lane % kWarps)) * kR;
-#pragma unroll
-                for (uint32_t c = 0; c < kC; ++c) {
-                    const uint32_t byte = c == 0 ? b.x : c == 1 ? b.y : c == 2 ? b.z : b.w;
-                    uint32_t q[kR / 4];
-#pragma unroll
-                    for (uint32_t i = 0; i < kR / 4; ++i) {
-                        q[i] = act8_codes4(x[4 * i][c], x[4 * i + 1][c], x[4 * i + 2][c], x[4 * i + 3][c]);
-                        if (huge) q[i] = act8_finite4(q[i], byte);
-                    }
-                    if constexpr (kR == 8)
-                        *reinterpret_cast<uint2*>(to + (lane * kC + c) * 128u) = make_uint2(q[0], q[1]);
-                    else
-                        *reinterpret_cast<uint32_t*>(to + (lane * kC + c) * 128u) = q[0];
-                }
-            }
-            __syncthreads();
-#pragma unroll
-            for (uint32_t p = 0; p < S::kPlanes; ++p) {
-                const Act8& out = task.turned[p];
-                if (!out.codes) continue;
-#pragma unroll
-                for (uint32_t i = 0; i < 128u * 8u / kTileThreads; ++i) {
-                    const uint32_t c = i * (kTileThreads / 8u) + (threadIdx.x >> 3), part = threadIdx.x & 7u, key = (c >> 2) % kWarps;
-                    const uint32_t row = col0 + c, col = row0 + part * 16u;           // of the transpose
-                    if (!whole && (row >= out.rows || col >= out.cols)) continue;
-                    // sixteen codes are 16 / kR groups, exchanged among themselves by the key's low bits
-                    constexpr uint32_t kGroups = 16 / kR;
-                    uint4 q = *reinterpret_cast<const uint4*>(stage + p * kTurnedBytes + c * 128u + ((part * kGroups) ^ (key & ~(kGroups - 1u))) * kR);
-                    if constexpr (kR == 8) {
-                        if (key & 1u) q = make_uint4(q.z, q.w, q.x, q.y);
-                    } else {
-                        if (key & 1u) q = make_uint4(q.y, q.x, q.w, q.z);
-                        if (key & 2u) q = make_uint4(q.z, q.w, q.x, q.y);
-                    }
-                    uint8_t* to = out.codes + static_cast<size_t>(row) * out.ld + col;
-                    if (whole || col + 16 <= out.cols) {
-                        st_unit(to, q);
-                    } else {
-                        for (uint32_t k = 0; col + k < out.cols; ++k)
-                            to[k] = static_cast<uint8_t>((k < 8 ? (k < 4 ? q.x : q.y) : (k < 12 ? q.z : q.w)) >> (8 * (k & 3u)));
-                    }
-                }
+                if (whole)
+                    write_turned<true>(stage + p * kTurnedBytes, task.turned[p], tile_r, tile_c);
+                else
+                    write_turned<false>(stage + p * kTurnedBytes, task.turned[p], tile_r, tile_c);
             }
         }
         fence_proxy_async_smem();            // this stage is written by copies again
         __syncthreads();
+        tile_r = next_r;
+        tile_c = next_c;
         if (!copied) continue;
         s ^= 1u;
         if (s == 0) phase ^= 1u;
@@ -323,8 +333,9 @@ __global__ void __launch_bounds__(TileShape<S>::kThreads, S::kCtas) act8_tile_ke
 // neighbouring elements.
 template <typename T>
 __global__ void __launch_bounds__(256) act8_unpack_kernel(const Act8 a, T* y, const uint32_t ld_y, const uint32_t tiles_c, const bool aligned) {
-    constexpr uint32_t kR = kUnpackRows;
     __shared__ T turn[8][128];
+    chain_release_next();
+    chain_wait_previous();
     const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
     const uint32_t row0 = blockIdx.x / tiles_c * 64u + warp * kR, col0 = blockIdx.x % tiles_c * 128u, col = col0 + lane * kC;
     const uint8_t* from = a.codes + static_cast<size_t>(row0) * a.ld + col;
@@ -399,8 +410,8 @@ dct_status_t launch_tiles(TileTask& task, uint32_t rows, uint32_t cols, const vo
     if (held0 && (st = tensor_map(e, &task.map[1], held0, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != DCT_OK) return st;
     if (held1 && (st = tensor_map(e, &task.map[2], held1, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != DCT_OK) return st;
     const uint64_t at_once = static_cast<uint64_t>(sms) * S::kCtas;
-    act8_tile_kernel<S><<<static_cast<unsigned>(tiles < at_once ? tiles : at_once), TileShape<S>::kThreads, TileShape<S>::kSharedBytes, stream>>>(task);
-    DCT_CUDA_TRY(cudaGetLastError());
+    DCT_CUDA_TRY(launch_chained_smem(act8_tile_kernel<S>, static_cast<unsigned>(tiles < at_once ? tiles : at_once), kTileThreads,
+                                     TileShape<S>::kSharedBytes, stream, task));
     return DCT_OK;
 }
 
@@ -453,10 +464,11 @@ extern "C" dct_status_t dct_act8_unpack(const dct_act8_t* a, void* y, dct_dtype_
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     const unsigned grid = static_cast<unsigned>(tiles);
     if (dtype == DCT_F32)
-        act8_unpack_kernel<<<grid, 256, 0, stream>>>(device_view(a), static_cast<float*>(y), ld_y, tiles_c, unit_rows<float>(y, ld_y));
+        DCT_CUDA_TRY(launch_chained(act8_unpack_kernel<float>, grid, 256, stream, device_view(a), static_cast<float*>(y), ld_y, tiles_c,
+                                    unit_rows<float>(y, ld_y)));
     else
-        act8_unpack_kernel<<<grid, 256, 0, stream>>>(device_view(a), static_cast<__nv_bfloat16*>(y), ld_y, tiles_c, unit_rows<__nv_bfloat16>(y, ld_y));
-    DCT_CUDA_TRY(cudaGetLastError());
+        DCT_CUDA_TRY(launch_chained(act8_unpack_kernel<__nv_bfloat16>, grid, 256, stream, device_view(a), static_cast<__nv_bfloat16*>(y), ld_y, tiles_c,
+                                    unit_rows<__nv_bfloat16>(y, ld_y)));
     return DCT_OK;
 }
 

@@ -25,6 +25,12 @@ __device__ __forceinline__ size_t act8_scale_offset(uint32_t row_tiles, uint32_t
     return (static_cast<size_t>(block >> 2) * row_tiles + (row >> 7)) * kAct8ScaleTile + (row & 31u) * 16u + ((row >> 5) & 3u) * 4u + (block & 3u);
 }
 
+// The same, of a row of a scale tile and of the tile
+__device__ __forceinline__ uint32_t act8_scale_row(uint32_t row) { return (row & 31u) * 16u + ((row >> 5) & 3u) * 4u; }
+__device__ __forceinline__ size_t act8_scale_tile(uint32_t row_tiles, uint32_t row_tile, uint32_t block) {
+    return (static_cast<size_t>(block >> 2) * row_tiles + row_tile) * kAct8ScaleTile + (block & 3u);
+}
+
 // |x| as an integer: ordered as the magnitudes, infinities above every number and NaN above those
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
@@ -147,6 +153,27 @@ inline bool usable(const dct_act8_t* m) {
 inline Act8 device_view(const dct_act8_t* m) {
     if (!m) return Act8{nullptr, nullptr, 0, 0, 0, 0};
     return Act8{static_cast<uint8_t*>(m->codes), static_cast<uint8_t*>(m->scales), m->rows, m->cols, m->ld, ceil_div(m->rows, 128)};
+}
+
+// launches `kernel` in clusters of `cluster` CTAs as a programmatic dependent of the kernel before it on the stream
+template <typename... Params, typename... Args>
+cudaError_t launch_chained_clusters(void (*kernel)(Params...), unsigned grid, unsigned block, unsigned cluster, size_t smem, cudaStream_t stream,
+                                    const Args&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute how[2] = {};
+    how[0].id = cudaLaunchAttributeClusterDimension;
+    how[0].val.clusterDim.x = cluster;
+    how[0].val.clusterDim.y = 1;
+    how[0].val.clusterDim.z = 1;
+    how[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    how[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = how;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
 }
 
 // Descriptors of tensor copies -----------------------------------------------------------------------------------

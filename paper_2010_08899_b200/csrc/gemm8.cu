@@ -307,7 +307,7 @@ __device__ __forceinline__ void finish_few_gated(const Task& task, Shared<S>& sh
         gate_times<false, kN>(h, g, u);
 #pragma unroll
     for (uint32_t j = 0; j < kN; ++j) {
-        if (j < count) {
+        if (j < count && row0 + j < rows) {
             const uint32_t mg = __reduce_max_sync(0xFFFFFFFFu, magnitude(g[j])), mu = __reduce_max_sync(0xFFFFFFFFu, magnitude(u[j])),
                            mh = __reduce_max_sync(0xFFFFFFFFu, magnitude(h[j]));
             if (lane_id() == 0) {
@@ -354,21 +354,67 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
     const uint32_t end = static_cast<uint32_t>(static_cast<uint64_t>(all) * (rank + 1) / split);
     const uint32_t tile0 = blockIdx.x / split, step = gridDim.x / split, tile_count = task.tiles_p * task.tiles_q;
 
-    if (threadIdx.x == 0) {
-        for (uint32_t i = 0; i < S::kStages; ++i) {
-            mbar_init(&sh.full[i], 1);
-            mbar_init(&sh.empty[i], 1);
+    // one stage of the product: the codes of 128 of depth, and, every fourth time and the first, the scale tiles of 512
+    const auto load_stage = [&](const Tile& at, uint32_t it, uint32_t stage) {
+        const uint32_t second = !S::kGated && it >= task.depths[0] ? 1u : 0u, kb = second ? it - task.depths[0] : it;
+        const bool with_scales = it == begin || (kb & 3u) == 0;
+        uint8_t* tile = tiles + stage * S::kStageBytes;
+        uint8_t* sc = scales + stage * S::kScaleBytes;
+        uint64_t* bar = &sh.full[stage];
+        const bool two = S::kScaleTilesQ == 2 && (S::kGated || 2 * at.q + 1 < task.sq[second].row_tiles);
+        mbar_arrive_expect_tx(bar, S::kStageBytes + (with_scales ? (S::kAcc + 1 + two) * kAct8ScaleTile : 0));
+#pragma unroll
+        for (uint32_t i = 0; i < S::kAcc; ++i) tile_load(tile + i * kTileBytes, &task.p[S::kAcc == 2 ? i : second], kb * kDepth, at.p * 128u, bar);
+        uint8_t* q = tile + S::kAcc * kTileBytes;
+        if constexpr (S::kGated && !S::kFew) {
+            tile_load(q, &task.q[0], kb * kDepth, at.q * 128u, bar);
+            tile_load(q + kTileBytes, &task.q[1], kb * kDepth, at.q * 128u, bar);
+        } else {
+            tile_load(q, &task.q[second], kb * kDepth, at.q * S::kQ, bar);
         }
-        mbar_init(&sh.done, 1);
-        mbar_init(&sh.free, kEpilogueWarps);
-        mbar_init(&sh.drained, 1);
-        sh.stop = 0;
+        if (with_scales) {
+            const auto scale_tile = [&](const Scales& s, uint32_t row_tile) {
+                return s.at + (static_cast<size_t>(kb >> 2) * s.row_tiles + row_tile) * kAct8ScaleTile;
+            };
+#pragma unroll
+            for (uint32_t i = 0; i < S::kAcc; ++i)
+                bulk_load(sc + i * kAct8ScaleTile, scale_tile(task.sp[S::kAcc == 2 ? i : second], at.p), kAct8ScaleTile, bar);
+            sc += S::kAcc * kAct8ScaleTile;
+            if constexpr (S::kGated && !S::kFew) {
+                bulk_load(sc, scale_tile(task.sq[0], at.q), kAct8ScaleTile, bar);
+                bulk_load(sc + kAct8ScaleTile, scale_tile(task.sq[1], at.q), kAct8ScaleTile, bar);
+            } else if constexpr (S::kQ >= 128) {
+                bulk_load(sc, scale_tile(task.sq[second], at.q * (S::kQ / 128)), kAct8ScaleTile, bar);
+                if (two) bulk_load(sc + kAct8ScaleTile, scale_tile(task.sq[second], at.q * 2 + 1), kAct8ScaleTile, bar);
+            } else {
+                bulk_load(sc, scale_tile(task.sq[second], 0), kAct8ScaleTile, bar);       // (there is one Q tile, at row 0)
+            }
+        }
+    };
+    chain_release_next();
+    const uint32_t primed = min(S::kStages, end - begin);             // stages of the first tile that are asked for before anything else
+    if (warp == kProducerWarp) {
+        // a lane to a stage: their descriptors and addresses are worked out side by side
+        if (lane < S::kStages) {
+            mbar_init(&sh.full[lane], 1);
+            mbar_init(&sh.empty[lane], 1);
+        }
+        if (lane == 0) {
+            mbar_init(&sh.done, 1);
+            mbar_init(&sh.free, kEpilogueWarps);
+            mbar_init(&sh.drained, 1);
+            sh.stop = 0;
+        }
         mbar_init_fence();
+        __syncwarp();
+        chain_wait_previous();
+        if (lane < primed) load_stage(tile_at(task, tile0), begin + lane, lane);
     }
     if (warp == kProductWarp) tmem_alloc(&sh.tmem, S::kTmemCols);
     tmem_before_sync();
     __syncthreads();
     tmem_after_sync();
+    chain_wait_previous();
     if (split > 1) cluster_arrive();             // (waited for before anything is sent to a peer)
     const uint32_t tmem = sh.tmem;
     const volatile uint32_t* stop = &sh.stop;
@@ -376,50 +422,17 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
 
     if (warp == kProducerWarp) {
         if (lane == 0) {
-            uint32_t stage = 0, phase = 0, issued = 0;
+            uint32_t stage = primed % S::kStages, phase = primed / S::kStages, issued = primed;
             bool ok = true;
             for (uint32_t t = tile0; ok && t < tile_count; t += step) {
                 const Tile at = tile_at(task, t);
-                for (uint32_t it = begin; it < end; ++it) {
+                for (uint32_t it = t == tile0 ? begin + primed : begin; it < end; ++it) {
                     if (!mbar_wait_bounded(&sh.empty[stage], phase ^ 1u, task.limit, stop)) {
                         ok = false;
                         give_up();
                         break;
                     }
-                    const uint32_t second = !S::kGated && it >= task.depths[0] ? 1u : 0u, kb = second ? it - task.depths[0] : it;
-                    const bool with_scales = it == begin || (kb & 3u) == 0;
-                    uint8_t* tile = tiles + stage * S::kStageBytes;
-                    uint8_t* sc = scales + stage * S::kScaleBytes;
-                    uint64_t* bar = &sh.full[stage];
-                    const bool two = S::kScaleTilesQ == 2 && (S::kGated || 2 * at.q + 1 < task.sq[second].row_tiles);
-                    mbar_arrive_expect_tx(bar, S::kStageBytes + (with_scales ? (S::kAcc + 1 + two) * kAct8ScaleTile : 0));
-#pragma unroll
-                    for (uint32_t i = 0; i < S::kAcc; ++i) tile_load(tile + i * kTileBytes, &task.p[S::kAcc == 2 ? i : second], kb * kDepth, at.p * 128u, bar);
-                    uint8_t* q = tile + S::kAcc * kTileBytes;
-                    if constexpr (S::kGated && !S::kFew) {
-                        tile_load(q, &task.q[0], kb * kDepth, at.q * 128u, bar);
-                        tile_load(q + kTileBytes, &task.q[1], kb * kDepth, at.q * 128u, bar);
-                    } else {
-                        tile_load(q, &task.q[second], kb * kDepth, at.q * S::kQ, bar);
-                    }
-                    if (with_scales) {
-                        const auto scale_tile = [&](const Scales& s, uint32_t row_tile) {
-                            return s.at + (static_cast<size_t>(kb >> 2) * s.row_tiles + row_tile) * kAct8ScaleTile;
-                        };
-#pragma unroll
-                        for (uint32_t i = 0; i < S::kAcc; ++i)
-                            bulk_load(sc + i * kAct8ScaleTile, scale_tile(task.sp[S::kAcc == 2 ? i : second], at.p), kAct8ScaleTile, bar);
-                        sc += S::kAcc * kAct8ScaleTile;
-                        if constexpr (S::kGated && !S::kFew) {
-                            bulk_load(sc, scale_tile(task.sq[0], at.q), kAct8ScaleTile, bar);
-                            bulk_load(sc + kAct8ScaleTile, scale_tile(task.sq[1], at.q), kAct8ScaleTile, bar);
-                        } else if constexpr (S::kQ >= 128) {
-                            bulk_load(sc, scale_tile(task.sq[second], at.q * (S::kQ / 128)), kAct8ScaleTile, bar);
-                            if (two) bulk_load(sc + kAct8ScaleTile, scale_tile(task.sq[second], at.q * 2 + 1), kAct8ScaleTile, bar);
-                        } else {
-                            bulk_load(sc, scale_tile(task.sq[second], 0), kAct8ScaleTile, bar);       // (there is one Q tile, at row 0)
-                        }
-                    }
+                    load_stage(at, it, stage);
                     ++issued;
                     if (++stage == S::kStages) stage = 0, phase ^= 1u;
                 }
@@ -492,7 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
             };
             if (split > 1) {
                 // this part's columns to the CTAs that add them up
-                const uint32_t slice = S::kQ / split;
+                const uint32_t shift = __ffs(S::kQ / split) - 1u, slice = 1u << shift, columns = task.q_rows - at.q * S::kQ;
                 cluster_wait();
 #pragma unroll
                 for (uint32_t a = 0; a < S::kAcc; ++a) {
@@ -501,9 +514,10 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                     tmem_loaded<S::kQ / 2>(v);
 #pragma unroll
                     for (uint32_t j = 0; j < S::kQ / 2; ++j) {
-                        const uint32_t col = group * (S::kQ / 2) + j, to = col / slice;
-                        st_peer(peer_address(smem_addr(receive + ((rank * S::kAcc + a) * slice + col % slice) * 128u + row_lane), to),
-                                ok ? v[j] : __uint_as_float(kLost));
+                        const uint32_t col = group * (S::kQ / 2) + j, to = col >> shift;
+                        if (col < columns)
+                            st_peer(peer_address(smem_addr(receive + ((rank * S::kAcc + a) * slice + (col & (slice - 1u))) * 128u + row_lane), to),
+                                    ok ? v[j] : __uint_as_float(kLost));
                     }
                 }
                 break;             // (one tile to a cluster)
@@ -605,13 +619,14 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                 float g[S::kQ / 2], u[S::kQ / 2];
 #pragma unroll
                 for (uint32_t j = 0; j < S::kQ / 2; ++j) {
-                    g[j] = j < half ? sum(0, j) : 0.0f;
-                    u[j] = j < half ? sum(1, j) : 0.0f;
+                    const bool there = j < half && q0 + j < task.q_rows;
+                    g[j] = there ? sum(0, j) : 0.0f;
+                    u[j] = there ? sum(1, j) : 0.0f;
                 }
                 finish_few_gated<S>(task, sh, g, u, half, q0, p0 + row_lane, group, warp & 3u, true);
             } else if constexpr (S::kFew) {
-                for (uint32_t j = 0; j < half; ++j)
-                    if (q0 + j < task.q_rows && p0 + row_lane < task.p_rows) put_one(task, q0 + j, p0 + row_lane, sum(0, j));
+                for (uint32_t j = 0; j < half && q0 + j < task.q_rows; ++j)
+                    if (p0 + row_lane < task.p_rows) put_one(task, q0 + j, p0 + row_lane, sum(0, j));
             } else {
                 float* turn = turns + warp * (32 * 17);
                 for (uint32_t j = 0; j < half; j += 8) {
@@ -661,10 +676,9 @@ template <typename S> dct_status_t launch(Task& task, uint32_t sms, cudaStream_t
     if (tiles > 0x3FFFFFFFull) return DCT_ERR_UNSUPPORTED;
     if ((st = split_of<S>(tiles, task.depths[0] + task.depths[1], &task.split)) != DCT_OK) return st;
     if (task.split > 1) {
-        DCT_CUDA_TRY(launch_clusters(product8_kernel<S>, static_cast<unsigned>(tiles) * task.split, kThreads, task.split, S::kSharedBytes, stream, task));
+        DCT_CUDA_TRY(launch_chained_clusters(product8_kernel<S>, static_cast<unsigned>(tiles) * task.split, kThreads, task.split, S::kSharedBytes, stream, task));
     } else {
-        product8_kernel<S><<<static_cast<unsigned>(tiles < sms ? tiles : sms), kThreads, S::kSharedBytes, stream>>>(task);
-        DCT_CUDA_TRY(cudaGetLastError());
+        DCT_CUDA_TRY(launch_chained_smem(product8_kernel<S>, static_cast<unsigned>(tiles < sms ? tiles : sms), kThreads, S::kSharedBytes, stream, task));
     }
     return DCT_OK;
 }
