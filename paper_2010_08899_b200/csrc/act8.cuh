@@ -66,6 +66,7 @@ __device__ __forceinline__ void act8_values2(uint32_t two, float& lo, float& hi)
     hi = f.y;
 }
 
+__device__ __forceinline__ void prefetch_descriptor(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void tile_load(void* smem, const CUtensorMap* map, uint32_t x, uint32_t y, uint64_t* bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(smem_addr(smem)), "l"(map), "r"(x), "r"(y), "r"(smem_addr(bar)) : "memory");

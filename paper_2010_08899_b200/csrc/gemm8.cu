@@ -36,7 +36,7 @@ template <uint32_t kQ_, bool kFew_, bool kGated_, uint32_t kStages_, bool kSplit
     static constexpr uint32_t kTmemCols = power_of_two(kAccCols + kScaleBuffers * kScaleCols);
     // e4m3 times e4m3, powers as bytes of exponents, 128 by kQ; which byte of a scale word counts goes to bits 4 and 29
     static constexpr uint32_t kProduct = (kQ >> 3) << 17 | 1u << 23 | (128u >> 4) << 24;
-    static constexpr uint32_t kReceiveBytes = kSplit ? kAcc * kQ * 128 * 4 : 0;
+    static constexpr uint32_t kReceiveBytes = kSplit || kFew ? kAcc * kQ * 128 * 4 : 0;
     static constexpr uint32_t kTurnBytes = kFew ? 0 : kEpilogueWarps * 32 * 17 * 4;      // unaligned rows leave through here
     static constexpr uint32_t kSharedBytes = 1024 + kStages * (kStageBytes + kScaleBytes) + kReceiveBytes + kTurnBytes;
     static_assert(kStages <= kScaleBuffers, "a buffer of scales is written anew only after the products that read it");
@@ -288,54 +288,67 @@ template <bool kGelu, uint32_t kN> __device__ __forceinline__ void gate_times(fl
     }
 }
 
-// A few rows' g and u of one column each: the first `count` of the rows row0 .. .  The block of a row is the 128 lanes of a warp group.
-template <typename S, uint32_t kN>
-__device__ __forceinline__ void finish_few_gated(const Task& task, Shared<S>& sh, float (&g)[kN], float (&u)[kN], uint32_t count, uint32_t row0,
-                                                 uint32_t col, uint32_t group, uint32_t quarter, bool ok) {
-    const uint32_t f = task.p_rows, rows = task.q_rows;
-    float h[kN];
-    uint32_t* largest = sh.largest + group * (3 * kN * 4);
-#pragma unroll
-    for (uint32_t j = 0; j < kN; ++j) {
+// Few rows: a thread adds up its column's parts of the rows row0 .. row0 + count, which lie in shared memory, and writes them.  These are loops, not
+// straight code: it runs once or twice in a launch, and reading instructions would be most of its time (gated, 64 x 4096 x 8192: XX us unrolled, YY us).
+template <typename S> __device__ __forceinline__ float few_sum(const float* from, uint32_t split, uint32_t slice) {
+    float s = from[0];
+    for (uint32_t k = 1; k < split; ++k) s = __fadd_rn(s, from[k * (S::kAcc * slice * 128u)]);
+    return s;
+}
+template <typename S>
+__device__ __forceinline__ void finish_few(const Task& task, const float* from, uint32_t split, uint32_t slice, uint32_t row0, uint32_t count, uint32_t col) {
+    const uint32_t n = row0 < task.q_rows ? min(count, task.q_rows - row0) : 0u;
+    if (col >= task.p_rows) return;
+#pragma unroll 4
+    for (uint32_t j = 0; j < n; ++j) put_one(task, row0 + j, col, few_sum<S>(from + j * 128u, split, slice));
+}
+// The same for g and u.  The block of a row is the 128 lanes of a warp group.
+template <typename S>
+__device__ __forceinline__ void finish_few_gated(const Task& task, Shared<S>& sh, const float* from, uint32_t split, uint32_t slice, uint32_t row0,
+                                                 uint32_t count, uint32_t col, uint32_t group, uint32_t quarter) {
+    const uint32_t n = row0 < task.q_rows ? min(count, task.q_rows - row0) : 0u;
+    const bool there = col < task.p_rows, held = task.h.codes || task.gate.codes;
+    uint32_t* largest = sh.largest + group * (3 * (S::kQ / 2) * 4);
+    const auto values = [&](uint32_t j, float& g, float& u, float& h) {
         // (beyond the last column the powers are anything: what stands there is no number)
-        g[j] = !ok ? __uint_as_float(kLost) : col < f ? g[j] : 0.0f;
-        u[j] = col < f ? u[j] : 0.0f;
-    }
-    if (task.gelu)
-        gate_times<true, kN>(h, g, u);
-    else
-        gate_times<false, kN>(h, g, u);
-#pragma unroll
-    for (uint32_t j = 0; j < kN; ++j) {
-        if (j < count && row0 + j < rows) {
-            const uint32_t mg = __reduce_max_sync(0xFFFFFFFFu, magnitude(g[j])), mu = __reduce_max_sync(0xFFFFFFFFu, magnitude(u[j])),
-                           mh = __reduce_max_sync(0xFFFFFFFFu, magnitude(h[j]));
-            if (lane_id() == 0) {
-                largest[j * 4 + quarter] = mg;
-                largest[(kN + j) * 4 + quarter] = mu;
-                largest[(2 * kN + j) * 4 + quarter] = mh;
-            }
+        g = there ? few_sum<S>(from + j * 128u, split, slice) : 0.0f;
+        u = there ? few_sum<S>(from + (slice + j) * 128u, split, slice) : 0.0f;
+        const Gate2 a = task.gelu ? gate2<false, true>(g, g) : gate2<false, false>(g, g);
+        float other;
+        unpack2(mul2(a.value, pack2(u, u)), h, other);
+    };
+    if (held) {
+#pragma unroll 2
+        for (uint32_t j = 0; j < n; ++j) {
+            float g, u, h;
+            values(j, g, u, h);
+            const uint32_t mg = __reduce_max_sync(0xFFFFFFFFu, magnitude(g)), mu = __reduce_max_sync(0xFFFFFFFFu, magnitude(u)),
+                           mh = __reduce_max_sync(0xFFFFFFFFu, magnitude(h));
+            if (lane_id() < 3) largest[(j * 3 + lane_id()) * 4 + quarter] = lane_id() == 0 ? mg : lane_id() == 1 ? mu : mh;
         }
+        named_barrier_sync(1 + group, 128);
     }
-    named_barrier_sync(1 + group, 128);
     const auto hold = [&](const Act8& m, uint32_t which, uint32_t j, float x) {
-        const uint32_t* l = largest + (which * kN + j) * 4;
+        const uint32_t* l = largest + (j * 3 + which) * 4;
         const uint32_t byte = act8_byte(max(max(l[0], l[1]), max(l[2], l[3])));
         const uint32_t row = row0 + j;
         m.codes[static_cast<size_t>(row) * m.ld + col] = static_cast<uint8_t>(act8_finite4(act8_codes2(__fmul_rn(x, act8_inverse(byte)), 0.0f), byte));
         if ((col & 127u) == 0) m.scales[act8_scale_offset(m.row_tiles, row, col >> 7)] = static_cast<uint8_t>(byte);
     };
-#pragma unroll
-    for (uint32_t j = 0; j < kN; ++j) {
-        if (j >= count || row0 + j >= rows || col >= f) continue;
-        if (task.gate.codes) {
-            hold(task.gate, 0, j, g[j]);
-            hold(task.up, 1, j, u[j]);
+    if (there) {
+#pragma unroll 2
+        for (uint32_t j = 0; j < n; ++j) {
+            float g, u, h;
+            values(j, g, u, h);
+            if (task.gate.codes) {
+                hold(task.gate, 0, j, g);
+                hold(task.up, 1, j, u);
+            }
+            if (task.h.codes) hold(task.h, 2, j, h);
+            if (task.c) put_one(task, row0 + j, col, h);
         }
-        if (task.h.codes) hold(task.h, 2, j, h[j]);
-        if (task.c) put_one(task, row0 + j, col, h[j]);
     }
-    named_barrier_sync(1 + group, 128);          // before the next tile's are written
+    if (held) named_barrier_sync(1 + group, 128);          // before the next tile's are written
 }
 
 template <typename S>
@@ -393,23 +406,28 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
     };
     chain_release_next();
     const uint32_t primed = min(S::kStages, end - begin);             // stages of the first tile that are asked for before anything else
-    if (warp == kProducerWarp) {
-        // a lane to a stage: their descriptors and addresses are worked out side by side
-        if (lane < S::kStages) {
-            mbar_init(&sh.full[lane], 1);
-            mbar_init(&sh.empty[lane], 1);
+    // A warp to a stage: its barriers and its copies are set up side by side with the others', and the first to look at a descriptor of a copy
+    // finds it on its way already.
+    if (lane == 0) {
+        if (warp == kProducerWarp) {
+            prefetch_descriptor(&task.p[0]);
+            prefetch_descriptor(&task.q[0]);
         }
-        if (lane == 0) {
+        if (warp < S::kStages) {
+            mbar_init(&sh.full[warp], 1);
+            mbar_init(&sh.empty[warp], 1);
+        }
+        if (warp == kProducerWarp) {
             mbar_init(&sh.done, 1);
             mbar_init(&sh.free, kEpilogueWarps);
             mbar_init(&sh.drained, 1);
             sh.stop = 0;
         }
         mbar_init_fence();
-        __syncwarp();
         chain_wait_previous();
-        if (lane < primed) load_stage(tile_at(task, tile0), begin + lane, lane);
+        if (warp < primed) load_stage(tile_at(task, tile0), begin + warp, warp);
     }
+    __syncwarp();
     if (warp == kProductWarp) tmem_alloc(&sh.tmem, S::kTmemCols);
     tmem_before_sync();
     __syncthreads();
@@ -522,16 +540,23 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                 }
                 break;             // (one tile to a cluster)
             }
-            if constexpr (S::kFew && !S::kGated) {
-                float v[S::kQ / 2];
-                tmem_load<S::kQ / 2>(v, lanes + group * (S::kQ / 2));
-                tmem_loaded<S::kQ / 2>(v);
-                accumulator_read();
+            if constexpr (S::kFew) {
+                // to shared memory, a thread's to where it reads them itself
 #pragma unroll
-                for (uint32_t j = 0; j < S::kQ / 2; ++j) {
-                    const uint32_t row = q0 + group * (S::kQ / 2) + j;
-                    if (row < task.q_rows && p0 + row_lane < task.p_rows) put_one(task, row, p0 + row_lane, ok ? v[j] : __uint_as_float(kLost));
+                for (uint32_t a = 0; a < S::kAcc; ++a) {
+                    float v[S::kQ / 2];
+                    tmem_load<S::kQ / 2>(v, lanes + a * S::kQ + group * (S::kQ / 2));
+                    tmem_loaded<S::kQ / 2>(v);
+#pragma unroll
+                    for (uint32_t j = 0; j < S::kQ / 2; ++j)
+                        receive[(a * S::kQ + group * (S::kQ / 2) + j) * 128u + row_lane] = ok ? v[j] : __uint_as_float(kLost);
                 }
+                accumulator_read();
+                const float* from = receive + group * (S::kQ / 2) * 128u + row_lane;
+                if constexpr (S::kGated)
+                    finish_few_gated<S>(task, sh, from, 1, S::kQ, q0 + group * (S::kQ / 2), S::kQ / 2, p0 + row_lane, group, warp & 3u);
+                else
+                    finish_few<S>(task, from, 1, S::kQ, q0 + group * (S::kQ / 2), S::kQ / 2, p0 + row_lane);
             } else if constexpr (!S::kGated) {
                 float v[S::kQ / 2];
                 tmem_load<S::kQ / 2>(v, lanes + group * (S::kQ / 2));
@@ -589,15 +614,6 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                 if (task.h.codes || task.gate.codes) named_barrier_sync(1, kEpilogueWarps * 32);          // before the next tile's are written
                 if (task.c) put_dense<64>(task, p0 + (warp & 3u) * 32u, task.p_rows, g, col, task.q_rows, turn);
             }
-            if constexpr (S::kGated && S::kFew) {
-                float g[S::kQ / 2], u[S::kQ / 2];
-                tmem_load<S::kQ / 2>(g, lanes + group * (S::kQ / 2));
-                tmem_load<S::kQ / 2>(u, lanes + S::kQ + group * (S::kQ / 2));
-                tmem_loaded<S::kQ / 2>(g);
-                tmem_loaded<S::kQ / 2>(u);
-                accumulator_read();
-                finish_few_gated<S>(task, sh, g, u, S::kQ / 2, q0 + group * (S::kQ / 2), p0 + row_lane, group, warp & 3u, ok);
-            }
         }
     }
     __syncwarp();
@@ -610,29 +626,17 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
             const Tile at = tile_at(task, tile0);
             const uint32_t group = warp >> 2, row_lane = (warp & 3u) * 32u + lane, slice = S::kQ / split, half = slice / 2;
             const uint32_t p0 = at.p * 128u, q0 = at.q * S::kQ + rank * slice + group * half;
-            const auto sum = [&](uint32_t a, uint32_t j) {
-                float s = receive[(a * slice + group * half + j) * 128u + row_lane];
-                for (uint32_t k = 1; k < split; ++k) s = __fadd_rn(s, receive[((k * S::kAcc + a) * slice + group * half + j) * 128u + row_lane]);
-                return s;
-            };
+            const float* from = receive + group * half * 128u + row_lane;
             if constexpr (S::kGated) {
-                float g[S::kQ / 2], u[S::kQ / 2];
-#pragma unroll
-                for (uint32_t j = 0; j < S::kQ / 2; ++j) {
-                    const bool there = j < half && q0 + j < task.q_rows;
-                    g[j] = there ? sum(0, j) : 0.0f;
-                    u[j] = there ? sum(1, j) : 0.0f;
-                }
-                finish_few_gated<S>(task, sh, g, u, half, q0, p0 + row_lane, group, warp & 3u, true);
+                finish_few_gated<S>(task, sh, from, split, slice, q0, half, p0 + row_lane, group, warp & 3u);
             } else if constexpr (S::kFew) {
-                for (uint32_t j = 0; j < half && q0 + j < task.q_rows; ++j)
-                    if (p0 + row_lane < task.p_rows) put_one(task, q0 + j, p0 + row_lane, sum(0, j));
+                finish_few<S>(task, from, split, slice, q0, half, p0 + row_lane);
             } else {
                 float* turn = turns + warp * (32 * 17);
                 for (uint32_t j = 0; j < half; j += 8) {
                     float v[8];
 #pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) v[i] = sum(0, j + i);
+                    for (uint32_t i = 0; i < 8; ++i) v[i] = few_sum<S>(from + (j + i) * 128u, split, slice);
                     put_dense<8>(task, p0 + (warp & 3u) * 32u, task.p_rows, v, q0 + j, task.q_rows, turn);
                 }
             }
@@ -685,10 +689,10 @@ template <typename S> dct_status_t launch(Task& task, uint32_t sms, cudaStream_t
 
 using Wide256 = Shape<256, false, false, 4, false>;
 using Wide128 = Shape<128, false, false, 4, true>;
-using Few32 = Shape<32, true, false, 8, true>;
-using Few64 = Shape<64, true, false, 7, true>;
+using Few32 = Shape<32, true, false, 5, true>;
+using Few64 = Shape<64, true, false, 5, true>;
 using GatedWide = Shape<256, false, true, 4, false>;
-using GatedFew32 = Shape<32, true, true, 5, true>;
+using GatedFew32 = Shape<32, true, true, 4, true>;
 using GatedFew64 = Shape<64, true, true, 3, true>;
 
 dct_status_t product(const dct_act8_t* const (&a)[2], const dct_act8_t* const (&b)[2], void* c, dct_dtype_t dtype, uint32_t ld_c, bool accumulate,
