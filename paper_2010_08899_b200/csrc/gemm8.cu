@@ -5,12 +5,14 @@
 // scale tile holds for a row, so that 512 bytes per 128 rows serve four stages.  Sums stay in fp32 in tensor memory from the first
 // depth to the last.
 //
-//   wide:  P are C's rows, Q its columns.  A thread has one row of the tile.
-//   few:   rows of C are too few to fill 128 lanes: P are the columns (the weights), Q the rows.  A thread has one column of the tile.
-//   gated, wide:  Q are 128 rows of the gate's weights and the same 128 of up's: a thread has its row's g and u of a whole block.
-//   gated, few:   two P tiles, gate and up, with the same Q, into two accumulators.
-// Where tiles are too few for the device, a cluster of CTAs shares one: each sums a part of the depth, sends every other its columns of the
-// result, and adds up its own columns in the order of the parts.
+//   pairs: P are C's rows, Q its columns, 256 of each.  Two CTAs of neighbouring SMs work on the tile: each has 128 of the rows and all columns in
+//          its tensor memory, and reads its own rows and half the columns' codes, the other half being its neighbour's.
+//          Gated: Q are 128 rows of the gate's weights and the same 128 of up's, so that a thread, which has one row, has g and u of a whole block.
+//   wide:  128 rows and 128 columns, one CTA, for matrices of few tiles.
+//   few:   rows of C are too few to fill 128 lanes: P are the columns (the weights), Q the rows.  A thread has one column of the tile.  Gated:
+//          two P tiles, gate and up, with the same Q, into two accumulators.
+// Where tiles of the last two are too few for the device, a cluster of CTAs shares one: each sums a part of the depth, sends every other its columns
+// of the result, and adds up its own columns in the order of the parts.
 #include "act8.cuh"
 
 namespace dct {
@@ -25,20 +27,30 @@ constexpr uint32_t kLost = 0x7FC00000u;
 
 constexpr uint32_t power_of_two(uint32_t n) { return n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
 
-template <uint32_t kQ_, bool kFew_, bool kGated_, uint32_t kStages_, bool kSplit_> struct Shape {
+template <uint32_t kQ_, bool kFew_, bool kGated_, uint32_t kStages_> struct Shape {
     static constexpr uint32_t kQ = kQ_, kStages = kStages_;
-    static constexpr bool kFew = kFew_, kGated = kGated_, kSplit = kSplit_;
-    static constexpr uint32_t kAcc = kGated && kFew ? 2 : 1;                    // accumulators, each with its P tile
+    static constexpr bool kFew = kFew_, kGated = kGated_;
+    static constexpr uint32_t kAcc = kGated ? 2 : 1;                    // accumulators, each with its P tile
     static constexpr uint32_t kStageBytes = kAcc * kTileBytes + kQ * kDepth;
-    static constexpr uint32_t kScaleTilesQ = kQ > 128 ? 2 : 1, kScaleTiles = kAcc + kScaleTilesQ;
+    static constexpr uint32_t kScaleTiles = kAcc + 1;
     static constexpr uint32_t kScaleBytes = kScaleTiles * kAct8ScaleTile;
     static constexpr uint32_t kAccCols = kAcc * kQ, kScaleCols = 4 * kScaleTiles;
     static constexpr uint32_t kTmemCols = power_of_two(kAccCols + kScaleBuffers * kScaleCols);
     // e4m3 times e4m3, powers as bytes of exponents, 128 by kQ; which byte of a scale word counts goes to bits 4 and 29
     static constexpr uint32_t kProduct = (kQ >> 3) << 17 | 1u << 23 | (128u >> 4) << 24;
-    static constexpr uint32_t kReceiveBytes = kSplit || kFew ? kAcc * kQ * 128 * 4 : 0;
+    static constexpr uint32_t kReceiveBytes = kAcc * kQ * 128 * 4;
     static constexpr uint32_t kTurnBytes = kFew ? 0 : kEpilogueWarps * 32 * 17 * 4;      // unaligned rows leave through here
     static constexpr uint32_t kSharedBytes = 1024 + kStages * (kStageBytes + kScaleBytes) + kReceiveBytes + kTurnBytes;
+    static_assert(kStages <= kScaleBuffers, "a buffer of scales is written anew only after the products that read it");
+    static_assert(kSharedBytes + 4096 <= 232448, "shared memory of a CTA");
+};
+
+// Two CTAs to a tile of 256 x 256
+struct PairShape {
+    static constexpr uint32_t kStages = 6, kStageBytes = 2 * kTileBytes, kScaleTiles = 3, kScaleBytes = kScaleTiles * kAct8ScaleTile;
+    static constexpr uint32_t kAccCols = 256, kScaleCols = 4 * kScaleTiles, kTmemCols = power_of_two(kAccCols + kScaleBuffers * kScaleCols);
+    static constexpr uint32_t kProduct = (256u >> 3) << 17 | 1u << 23 | (256u >> 4) << 24;
+    static constexpr uint32_t kSharedBytes = 1024 + kStages * (kStageBytes + kScaleBytes) + kEpilogueWarps * 32 * 17 * 4;
     static_assert(kStages <= kScaleBuffers, "a buffer of scales is written anew only after the products that read it");
     static_assert(kSharedBytes + 4096 <= 232448, "shared memory of a CTA");
 };
@@ -50,6 +62,7 @@ struct Scales {
 
 struct alignas(64) Task {
     CUtensorMap p[2], q[2];         // plain: of the two products; gated: gate and up where there are two
+    CUtensorMap sp_map[2], sq_map[2];        // pairs: of the scale tiles
     Scales sp[2], sq[2];
     uint32_t depths[2];             // stages of each product
     uint32_t p_rows, q_rows;        // of P and Q
@@ -122,6 +135,49 @@ template <uint32_t kN> __device__ __forceinline__ void tmem_loaded(float* v) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
     for (uint32_t i = 0; i < kN; ++i) asm volatile("" : "+f"(v[i]));
+}
+
+// The same for a pair: commands come from the even CTA's thread and work on both CTAs' memories, at the same places; a copy may arrive at the even
+// CTA's barrier from either.
+__device__ __forceinline__ void pair_alloc(uint32_t* where, uint32_t cols) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(where)), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+}
+__device__ __forceinline__ void pair_free(uint32_t at, uint32_t cols) {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(cols));
+}
+__device__ __forceinline__ void pair_commit(uint64_t* bar) {            // arrives at both CTAs'
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(smem_addr(bar)), "h"(static_cast<uint16_t>(3)) : "memory");
+}
+__device__ __forceinline__ void pair_scales_to_tmem(uint32_t tmem, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void pair_product(uint32_t d, uint64_t p, uint64_t q, uint32_t idesc, uint32_t sp, uint32_t sq, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred a;\n\tsetp.ne.u32 a, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], a;\n\t}"
+        ::"r"(d), "l"(p), "l"(q), "r"(idesc), "r"(sp), "r"(sq), "r"(static_cast<uint32_t>(add)) : "memory");
+}
+__device__ __forceinline__ void pair_tile_load(void* smem, const CUtensorMap* map, uint32_t x, uint32_t y, uint32_t even_bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(smem_addr(smem)), "l"(map), "r"(x), "r"(y), "r"(even_bar) : "memory");
+}
+__device__ __forceinline__ bool wait_for_cluster(uint64_t* bar, uint32_t parity, uint32_t limit, const volatile uint32_t* stop) {       // as mbar_wait_bounded
+    for (uint32_t i = 0; i < limit; ++i) {
+        uint32_t there;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(there) : "r"(smem_addr(bar)), "r"(parity) : "memory");
+        if (there) return true;
+        if ((i & 63u) == 63u && *stop) return false;
+    }
+    return false;
+}
+__device__ __forceinline__ void arrive_at(uint32_t bar) {               // a barrier of any CTA of the cluster
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 // Descriptors of shared memory.  Tiles: rows of 128 bytes, swizzled by 128 bytes, groups of eight rows 1024 bytes apart; 32 of depth further is 32 bytes
@@ -276,7 +332,7 @@ __device__ __forceinline__ Tile tile_at(const Task& task, uint32_t t) {
 template <typename S> struct Shared {
     uint64_t full[S::kStages], empty[S::kStages], done, free, drained;
     uint32_t tmem, stop;
-    uint32_t largest[S::kGated ? (S::kFew ? 2 * 3 * (S::kQ / 2) * 4 : 3 * 2 * 128) : 1];
+    uint32_t largest[S::kGated ? 2 * 3 * (S::kQ / 2) * 4 : 1];
 };
 
 // h = act(g) u
@@ -286,6 +342,74 @@ template <bool kGelu, uint32_t kN> __device__ __forceinline__ void gate_times(fl
         const Gate2 a = gate2<false, kGelu>(g[j], g[j + 1]);
         unpack2(mul2(a.value, pack2(u[j], u[j + 1])), h[j], h[j + 1]);
     }
+}
+
+// A warp's 32 rows and kN columns of the accumulator, read at once so that the next tile's products may begin
+template <uint32_t kN, typename Read>
+__device__ __forceinline__ void finish_wide(const Task& task, uint32_t from, uint32_t row0, uint32_t col0, float* turn, bool ok, const Read& accumulator_read) {
+    const uint32_t group = threadIdx.x >> 7;
+    float v[kN];
+    tmem_load<kN>(v, from + group * kN);
+    tmem_loaded<kN>(v);
+    accumulator_read();
+    if (!ok) {
+#pragma unroll
+        for (uint32_t j = 0; j < kN; ++j) v[j] = __uint_as_float(kLost);
+    }
+    put_dense<kN>(task, row0, task.p_rows, v, col0, task.q_rows, turn);
+}
+// The same of a gated tile: 64 columns' g and u, columns 128 .. of the accumulator being up's.  The largest of the other 64 columns of the block
+// comes from the other warp group, through `shared`.
+template <typename Read>
+__device__ __forceinline__ void finish_wide_gated(const Task& task, uint32_t from, uint32_t row0, uint32_t block, uint32_t* shared, float* turn, bool ok,
+                                                  const Read& accumulator_read) {
+    const uint32_t group = threadIdx.x >> 7, row_lane = threadIdx.x & 127u;
+    float g[64], u[64];
+    tmem_load<64>(g, from + group * 64);
+    tmem_load<64>(u, from + 128 + group * 64);
+    tmem_loaded<64>(g);
+    tmem_loaded<64>(u);
+    accumulator_read();
+    const uint32_t row = row0 + lane_id(), col = block * 128u + group * 64u, count = col < task.q_rows ? task.q_rows - col : 0;
+    if (!ok || count < 64) {
+#pragma unroll
+        for (uint32_t j = 0; j < 64; ++j) {
+            // (beyond the last column the powers are anything: what stands there is no number)
+            g[j] = !ok ? __uint_as_float(kLost) : j < count ? g[j] : 0.0f;
+            u[j] = j < count ? u[j] : 0.0f;
+        }
+    }
+    const bool writes = row < task.p_rows && count > 0;
+    const auto join = [&](uint32_t which, uint32_t m) { shared[(which * 2 + group) * 128 + row_lane] = m; };
+    const auto joined = [&](uint32_t which) { return max(shared[which * 256 + row_lane], shared[which * 256 + 128 + row_lane]); };
+    const auto scale = [&](const Act8& m, uint32_t byte) {
+        if (writes && group == 0) m.scales[act8_scale_offset(m.row_tiles, row, block)] = static_cast<uint8_t>(byte);
+    };
+    if (task.gate.codes) {
+        join(0, largest64(g));
+        join(1, largest64(u));
+        named_barrier_sync(1, kEpilogueWarps * 32);
+        const uint32_t bg = act8_byte(joined(0)), bu = act8_byte(joined(1));
+        if (writes) {
+            hold64(task.gate, row, col, g, count, bg);
+            hold64(task.up, row, col, u, count, bu);
+        }
+        scale(task.gate, bg);
+        scale(task.up, bu);
+    }
+    if (task.gelu)
+        gate_times<true, 64>(g, g, u);
+    else
+        gate_times<false, 64>(g, g, u);
+    if (task.h.codes) {
+        join(2, largest64(g));
+        named_barrier_sync(1, kEpilogueWarps * 32);
+        const uint32_t bh = act8_byte(joined(2));
+        if (writes) hold64(task.h, row, col, g, count, bh);
+        scale(task.h, bh);
+    }
+    if (task.h.codes || task.gate.codes) named_barrier_sync(1, kEpilogueWarps * 32);          // before the next tile's are written
+    if (task.c) put_dense<64>(task, row0, task.p_rows, g, col, task.q_rows, turn);
 }
 
 // Few rows: a thread adds up its column's parts of the rows row0 .. row0 + count, which lie in shared memory, and writes them.  These are loops, not
@@ -361,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
     float* turns = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(receive) + S::kReceiveBytes);
 
     const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
-    const uint32_t split = S::kSplit ? task.split : 1u, rank = split > 1 ? cluster_rank() : 0u;
+    const uint32_t split = task.split, rank = split > 1 ? cluster_rank() : 0u;
     const uint32_t all = task.depths[0] + task.depths[1];
     const uint32_t begin = static_cast<uint32_t>(static_cast<uint64_t>(all) * rank / split);
     const uint32_t end = static_cast<uint32_t>(static_cast<uint64_t>(all) * (rank + 1) / split);
@@ -374,17 +498,10 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
         uint8_t* tile = tiles + stage * S::kStageBytes;
         uint8_t* sc = scales + stage * S::kScaleBytes;
         uint64_t* bar = &sh.full[stage];
-        const bool two = S::kScaleTilesQ == 2 && (S::kGated || 2 * at.q + 1 < task.sq[second].row_tiles);
-        mbar_arrive_expect_tx(bar, S::kStageBytes + (with_scales ? (S::kAcc + 1 + two) * kAct8ScaleTile : 0));
+        mbar_arrive_expect_tx(bar, S::kStageBytes + (with_scales ? S::kScaleBytes : 0));
 #pragma unroll
         for (uint32_t i = 0; i < S::kAcc; ++i) tile_load(tile + i * kTileBytes, &task.p[S::kAcc == 2 ? i : second], kb * kDepth, at.p * 128u, bar);
-        uint8_t* q = tile + S::kAcc * kTileBytes;
-        if constexpr (S::kGated && !S::kFew) {
-            tile_load(q, &task.q[0], kb * kDepth, at.q * 128u, bar);
-            tile_load(q + kTileBytes, &task.q[1], kb * kDepth, at.q * 128u, bar);
-        } else {
-            tile_load(q, &task.q[second], kb * kDepth, at.q * S::kQ, bar);
-        }
+        tile_load(tile + S::kAcc * kTileBytes, &task.q[second], kb * kDepth, at.q * S::kQ, bar);
         if (with_scales) {
             const auto scale_tile = [&](const Scales& s, uint32_t row_tile) {
                 return s.at + (static_cast<size_t>(kb >> 2) * s.row_tiles + row_tile) * kAct8ScaleTile;
@@ -392,16 +509,8 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
 #pragma unroll
             for (uint32_t i = 0; i < S::kAcc; ++i)
                 bulk_load(sc + i * kAct8ScaleTile, scale_tile(task.sp[S::kAcc == 2 ? i : second], at.p), kAct8ScaleTile, bar);
-            sc += S::kAcc * kAct8ScaleTile;
-            if constexpr (S::kGated && !S::kFew) {
-                bulk_load(sc, scale_tile(task.sq[0], at.q), kAct8ScaleTile, bar);
-                bulk_load(sc + kAct8ScaleTile, scale_tile(task.sq[1], at.q), kAct8ScaleTile, bar);
-            } else if constexpr (S::kQ >= 128) {
-                bulk_load(sc, scale_tile(task.sq[second], at.q * (S::kQ / 128)), kAct8ScaleTile, bar);
-                if (two) bulk_load(sc + kAct8ScaleTile, scale_tile(task.sq[second], at.q * 2 + 1), kAct8ScaleTile, bar);
-            } else {
-                bulk_load(sc, scale_tile(task.sq[second], 0), kAct8ScaleTile, bar);       // (there is one Q tile, at row 0)
-            }
+            // (of few rows there is one Q tile, at row 0)
+            bulk_load(sc + S::kAcc * kAct8ScaleTile, scale_tile(task.sq[second], S::kFew ? 0 : at.q), kAct8ScaleTile, bar);
         }
     };
     chain_release_next();
@@ -515,7 +624,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
             }
             done_phase ^= 1u;
             tmem_after_sync();
-            const uint32_t p0 = at.p * 128u, q0 = at.q * (S::kGated && !S::kFew ? 128u : S::kQ);
+            const uint32_t p0 = at.p * 128u, q0 = at.q * S::kQ;
             const auto accumulator_read = [&] {
                 tmem_before_sync();
                 __syncwarp();
@@ -557,62 +666,8 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                     finish_few_gated<S>(task, sh, from, 1, S::kQ, q0 + group * (S::kQ / 2), S::kQ / 2, p0 + row_lane, group, warp & 3u);
                 else
                     finish_few<S>(task, from, 1, S::kQ, q0 + group * (S::kQ / 2), S::kQ / 2, p0 + row_lane);
-            } else if constexpr (!S::kGated) {
-                float v[S::kQ / 2];
-                tmem_load<S::kQ / 2>(v, lanes + group * (S::kQ / 2));
-                tmem_loaded<S::kQ / 2>(v);
-                accumulator_read();
-                if (!ok) {
-#pragma unroll
-                    for (uint32_t j = 0; j < S::kQ / 2; ++j) v[j] = __uint_as_float(kLost);
-                }
-                put_dense<S::kQ / 2>(task, p0 + (warp & 3u) * 32u, task.p_rows, v, q0 + group * (S::kQ / 2), task.q_rows, turn);
-            } else if constexpr (!S::kFew) {
-                float g[64], u[64];
-                tmem_load<64>(g, lanes + group * 64);
-                tmem_load<64>(u, lanes + 128 + group * 64);
-                tmem_loaded<64>(g);
-                tmem_loaded<64>(u);
-                accumulator_read();
-                const uint32_t row = p0 + row_lane, col = q0 + group * 64, count = col < task.q_rows ? task.q_rows - col : 0;
-#pragma unroll
-                for (uint32_t j = 0; j < 64; ++j) {
-                    // (beyond the last column the powers are anything: what stands there is no number)
-                    g[j] = !ok ? __uint_as_float(kLost) : j < count ? g[j] : 0.0f;
-                    u[j] = j < count ? u[j] : 0.0f;
-                }
-                const bool writes = row < task.p_rows && count > 0;
-                // the largest of the other 64 columns comes from the other warp group
-                const auto join = [&](uint32_t which, uint32_t m) { sh.largest[(which * 2 + group) * 128 + row_lane] = m; };
-                const auto joined = [&](uint32_t which) { return max(sh.largest[which * 256 + row_lane], sh.largest[which * 256 + 128 + row_lane]); };
-                const auto scale = [&](const Act8& m, uint32_t byte) {
-                    if (writes && group == 0) m.scales[act8_scale_offset(m.row_tiles, row, at.q)] = static_cast<uint8_t>(byte);
-                };
-                if (task.gate.codes) {
-                    join(0, largest64(g));
-                    join(1, largest64(u));
-                    named_barrier_sync(1, kEpilogueWarps * 32);
-                    const uint32_t bg = act8_byte(joined(0)), bu = act8_byte(joined(1));
-                    if (writes) {
-                        hold64(task.gate, row, col, g, count, bg);
-                        hold64(task.up, row, col, u, count, bu);
-                    }
-                    scale(task.gate, bg);
-                    scale(task.up, bu);
-                }
-                if (task.gelu)
-                    gate_times<true, 64>(g, g, u);
-                else
-                    gate_times<false, 64>(g, g, u);
-                if (task.h.codes) {
-                    join(2, largest64(g));
-                    named_barrier_sync(1, kEpilogueWarps * 32);
-                    const uint32_t bh = act8_byte(joined(2));
-                    if (writes) hold64(task.h, row, col, g, count, bh);
-                    scale(task.h, bh);
-                }
-                if (task.h.codes || task.gate.codes) named_barrier_sync(1, kEpilogueWarps * 32);          // before the next tile's are written
-                if (task.c) put_dense<64>(task, p0 + (warp & 3u) * 32u, task.p_rows, g, col, task.q_rows, turn);
+            } else {
+                finish_wide<S::kQ / 2>(task, lanes, p0 + (warp & 3u) * 32u, q0 + group * (S::kQ / 2), turn, ok, accumulator_read);
             }
         }
     }
@@ -650,11 +705,173 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
     }
 }
 
+// ---- two CTAs to a tile ----
+
+template <bool kGated>
+__global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constant__ Task task) {
+    using S = PairShape;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t full[S::kStages], empty[S::kStages], done, free_again, drained;        // full, free_again, drained: the even CTA's count
+    __shared__ uint32_t tmem_at, stop_word, largest[kGated ? 3 * 2 * 128 : 1];
+    uint8_t* tiles = raw + ((1024u - (smem_addr(raw) & 1023u)) & 1023u);
+    uint8_t* scales = tiles + S::kStages * S::kStageBytes;
+    float* turns = reinterpret_cast<float*>(scales + S::kStages * S::kScaleBytes);
+
+    const uint32_t warp = threadIdx.x >> 5, lane = lane_id(), rank = cluster_rank();
+    const uint32_t depth = task.depths[0] + task.depths[1], tile0 = blockIdx.x / 2, step = gridDim.x / 2, tile_count = task.tiles_p * task.tiles_q;
+    const volatile uint32_t* stop = &stop_word;
+    const auto give_up = [&] { *const_cast<volatile uint32_t*>(&stop_word) = 1u; };
+    chain_release_next();
+    if (warp == kProducerWarp && lane == 0) {
+        prefetch_descriptor(&task.p[0]);
+        prefetch_descriptor(&task.q[0]);
+        for (uint32_t i = 0; i < S::kStages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        mbar_init(&done, 1);
+        mbar_init(&free_again, 2 * kEpilogueWarps);
+        mbar_init(&drained, 1);
+        stop_word = 0;
+        mbar_init_fence();
+    }
+    __syncwarp();
+    if (warp == kProductWarp) pair_alloc(&tmem_at, S::kTmemCols);
+    tmem_before_sync();
+    cluster_arrive();
+    cluster_wait();
+    tmem_after_sync();
+    chain_wait_previous();
+    const uint32_t tmem = tmem_at;
+
+    if (warp == kProducerWarp) {
+        if (lane == 0) {
+            // own rows of P, own half of Q's, and the scale tiles of own rows and of all of Q's
+            uint32_t stage = 0, phase = 0, issued = 0;
+            bool ok = true;
+            for (uint32_t t = tile0; ok && t < tile_count; t += step) {
+                const Tile at = tile_at(task, t);
+                for (uint32_t it = 0; it < depth; ++it) {
+                    if (!mbar_wait_bounded(&empty[stage], phase ^ 1u, task.limit, stop)) {
+                        ok = false;
+                        give_up();
+                        break;
+                    }
+                    const uint32_t second = !kGated && it >= task.depths[0] ? 1u : 0u, kb = second ? it - task.depths[0] : it;
+                    const bool with_scales = (kb & 3u) == 0;
+                    uint8_t* tile = tiles + stage * S::kStageBytes;
+                    const uint32_t bar = peer_address(smem_addr(&full[stage]), 0);
+                    if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * (S::kStageBytes + (with_scales ? S::kScaleBytes : 0)));
+                    pair_tile_load(tile, &task.p[second], kb * kDepth, at.p * 256u + rank * 128u, bar);
+                    if constexpr (kGated)
+                        pair_tile_load(tile + kTileBytes, &task.q[rank], kb * kDepth, at.q * 128u, bar);
+                    else
+                        pair_tile_load(tile + kTileBytes, &task.q[second], kb * kDepth, at.q * 256u + rank * 128u, bar);
+                    if (with_scales) {
+                        // (a tile of rows that are not there is another's, or zeros: it scales nothing that is written)
+                        uint8_t* sc = scales + stage * S::kScaleBytes;
+                        const uint32_t group = kb >> 2;
+                        pair_tile_load(sc, &task.sp_map[second], 0, group * task.sp[second].row_tiles + at.p * 2u + rank, bar);
+                        if constexpr (kGated) {
+                            pair_tile_load(sc + kAct8ScaleTile, &task.sq_map[0], 0, group * task.sq[0].row_tiles + at.q, bar);
+                            pair_tile_load(sc + 2 * kAct8ScaleTile, &task.sq_map[1], 0, group * task.sq[1].row_tiles + at.q, bar);
+                        } else {
+                            pair_tile_load(sc + kAct8ScaleTile, &task.sq_map[second], 0, group * task.sq[second].row_tiles + at.q * 2u, bar);
+                            pair_tile_load(sc + 2 * kAct8ScaleTile, &task.sq_map[second], 0, group * task.sq[second].row_tiles + at.q * 2u + 1u, bar);
+                        }
+                    }
+                    ++issued;
+                    if (++stage == S::kStages) stage = 0, phase ^= 1u;
+                }
+            }
+            if (!ok && rank == 0) {             // what is in flight lands before the CTAs end (they meet once more)
+                for (uint32_t i = min(issued, S::kStages); i > 0; --i) {
+                    const uint32_t n = issued - i;
+                    for (uint32_t k = 0; k < task.limit && !mbar_try_wait(&full[n % S::kStages], (n / S::kStages) & 1u); ++k) {}
+                }
+            }
+        }
+    } else if (warp == kProductWarp) {
+        if (lane == 0 && rank == 0) {
+            uint32_t stage = 0, phase = 0, free_phase = 1, buffer = 0;
+            bool ok = true;
+            for (uint32_t t = tile0; ok && t < tile_count; t += step) {
+                ok = wait_for_cluster(&free_again, free_phase, task.limit, stop);
+                free_phase ^= 1u;
+                tmem_after_sync();
+                for (uint32_t it = 0; ok && it < depth; ++it) {
+                    ok = mbar_wait_bounded(&full[stage], phase, task.limit, stop);
+                    if (!ok) break;
+                    tmem_after_sync();
+                    const uint32_t kb = !kGated && it >= task.depths[0] ? it - task.depths[0] : it;
+                    if ((kb & 3u) == 0) {
+                        buffer = (buffer + 1u) % kScaleBuffers;
+                        const uint64_t from = scale_desc(scales + stage * S::kScaleBytes);
+#pragma unroll
+                        for (uint32_t i = 0; i < S::kScaleTiles; ++i)
+                            pair_scales_to_tmem(tmem + S::kAccCols + buffer * S::kScaleCols + 4 * i, from + i * (kAct8ScaleTile >> 4));
+                    }
+                    const uint32_t idesc = S::kProduct | (kb & 3u) << 4 | (kb & 3u) << 29, sf = tmem + S::kAccCols + buffer * S::kScaleCols;
+                    const uint64_t p = tile_desc(tiles + stage * S::kStageBytes), q = p + (kTileBytes >> 4);
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) pair_product(tmem, p + 2 * k, q + 2 * k, idesc, sf, sf + 4, it != 0 || k != 0);
+                    pair_commit(&empty[stage]);
+                    if (++stage == S::kStages) stage = 0, phase ^= 1u;
+                }
+                if (ok) pair_commit(&done);
+            }
+            if (!ok) {
+                give_up();
+                pair_commit(&drained);
+                for (uint32_t k = 0; k < task.limit && !mbar_try_wait(&drained, 0); ++k) {}
+            }
+        }
+    } else {
+        const uint32_t group = warp >> 2, lanes = tmem + ((warp & 3u) << 21), free_bar = peer_address(smem_addr(&free_again), 0);
+        float* turn = turns + warp * (32 * 17);
+        uint32_t done_phase = 0;
+        bool ok = true;
+        for (uint32_t t = tile0; t < tile_count; t += step) {
+            const Tile at = tile_at(task, t);
+            if (ok && !mbar_wait_bounded(&done, done_phase, task.limit, stop)) {
+                ok = false;
+                give_up();
+            }
+            done_phase ^= 1u;
+            tmem_after_sync();
+            const uint32_t row0 = at.p * 256u + rank * 128u + (warp & 3u) * 32u;
+            const auto accumulator_read = [&] {
+                tmem_before_sync();
+                __syncwarp();
+                if (lane == 0) arrive_at(free_bar);
+            };
+            if constexpr (kGated)
+                finish_wide_gated(task, lanes, row0, at.q, largest, turn, ok, accumulator_read);
+            else
+                finish_wide<128>(task, lanes, row0, at.q * 256u + group * 128u, turn, ok, accumulator_read);
+        }
+    }
+    __syncwarp();
+    tmem_before_sync();
+    cluster_arrive();                // neither ends while the other may still signal it
+    cluster_wait();
+    if (warp == kProductWarp) {
+        tmem_after_sync();
+        pair_free(tmem, S::kTmemCols);
+    }
+}
+
 // ---- host ----
 
 // codes in boxes of 128 bytes by `rows` rows
 dct_status_t encode(TensorEncoder e, CUtensorMap* map, const dct_act8_t* m, uint32_t rows) {
     return tensor_map(e, map, m, rows, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+// scale tiles one by one
+dct_status_t encode_scales(TensorEncoder e, CUtensorMap* map, const dct_act8_t* m) {
+    const uint64_t tiles = act8_scale_bytes(m->rows, m->cols) / kAct8ScaleTile;
+    if (tiles > 0x7FFFFFFFull) return DCT_ERR_UNSUPPORTED;
+    return tensor_map(e, map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, m->scales, static_cast<uint32_t>(tiles), 128, 128, 1, 128, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 Scales scales_of(const dct_act8_t* m) { return Scales{static_cast<const uint8_t*>(m->scales), ceil_div(m->rows, 128)}; }
 
@@ -662,7 +879,7 @@ Scales scales_of(const dct_act8_t* m) { return Scales{static_cast<const uint8_t*
 template <typename S> dct_status_t split_of(uint64_t tiles, uint32_t depths, uint32_t* split) {
     static ClusterCounts counts;
     *split = 1;
-    for (uint32_t s = 2; S::kSplit && s <= kMaxSplit && depths >= 4 * s; s *= 2) {
+    for (uint32_t s = 2; s <= kMaxSplit && depths >= 4 * s; s *= 2) {
         uint32_t at_once = 0;
         const dct_status_t st = clusters_at_once(product8_kernel<S>, kThreads, s, S::kSharedBytes, counts, &at_once);
         if (st != DCT_OK) return st;
@@ -687,13 +904,26 @@ template <typename S> dct_status_t launch(Task& task, uint32_t sms, cudaStream_t
     return DCT_OK;
 }
 
-using Wide256 = Shape<256, false, false, 4, false>;
-using Wide128 = Shape<128, false, false, 4, true>;
-using Few32 = Shape<32, true, false, 5, true>;
-using Few64 = Shape<64, true, false, 5, true>;
-using GatedWide = Shape<256, false, true, 4, false>;
-using GatedFew32 = Shape<32, true, true, 4, true>;
-using GatedFew64 = Shape<64, true, true, 3, true>;
+// Pairs of CTAs; as many as the device holds, from tile to tile
+template <bool kGated> dct_status_t launch_pairs(Task& task, cudaStream_t stream) {
+    static SharedLimit allowed;
+    static ClusterCounts counts;
+    dct_status_t st = allow_shared(pair8_kernel<kGated>, PairShape::kSharedBytes, allowed);
+    if (st != DCT_OK) return st;
+    const uint64_t tiles = static_cast<uint64_t>(task.tiles_p) * task.tiles_q;
+    if (tiles > 0x3FFFFFFFull) return DCT_ERR_UNSUPPORTED;
+    uint32_t at_once = 0;
+    if ((st = clusters_at_once(pair8_kernel<kGated>, kThreads, 2, PairShape::kSharedBytes, counts, &at_once)) != DCT_OK) return st;
+    const unsigned pairs = static_cast<unsigned>(tiles < at_once ? tiles : at_once);
+    DCT_CUDA_TRY(launch_chained_clusters(pair8_kernel<kGated>, 2 * pairs, kThreads, 2, PairShape::kSharedBytes, stream, task));
+    return DCT_OK;
+}
+
+using Wide128 = Shape<128, false, false, 4>;
+using Few32 = Shape<32, true, false, 5>;
+using Few64 = Shape<64, true, false, 5>;
+using GatedFew32 = Shape<32, true, true, 4>;
+using GatedFew64 = Shape<64, true, true, 3>;
 
 dct_status_t product(const dct_act8_t* const (&a)[2], const dct_act8_t* const (&b)[2], void* c, dct_dtype_t dtype, uint32_t ld_c, bool accumulate,
                      cudaStream_t stream) {
@@ -710,23 +940,24 @@ dct_status_t product(const dct_act8_t* const (&a)[2], const dct_act8_t* const (&
     task.bf16 = dtype == DCT_BF16;
     task.accumulate = accumulate;
     task.aligned = aligned_to(c, 32) && static_cast<size_t>(ld_c) * element_size(dtype) % 32 == 0;
-    // Up to 64 rows: the columns take the lanes.  Else tiles of 128 x 256, or of 128 x 128 where those are too few to go round twice.
+    // Up to 64 rows: the columns take the lanes.  Else pairs of CTAs, or single ones where the pairs' tiles are too few to go round twice.
     const bool few = m <= 64;
-    const uint64_t wide_tiles = static_cast<uint64_t>(ceil_div(m, 128)) * ceil_div(n, 256);
-    const uint32_t q = few ? (m <= 32 ? 32 : 64) : wide_tiles >= 2ull * sms ? 256 : 128;
+    const bool pairs = static_cast<uint64_t>(ceil_div(m, 256)) * ceil_div(n, 256) >= static_cast<uint64_t>(sms);
+    const uint32_t q = few ? (m <= 32 ? 32 : 64) : pairs ? 256 : 128;
     for (uint32_t i = 0; i < count; ++i) {
         const dct_act8_t *p_side = few ? b[i] : a[i], *q_side = few ? a[i] : b[i];
-        if ((st = encode(e, &task.p[i], p_side, 128)) != DCT_OK || (st = encode(e, &task.q[i], q_side, q)) != DCT_OK) return st;
+        if ((st = encode(e, &task.p[i], p_side, 128)) != DCT_OK || (st = encode(e, &task.q[i], q_side, q < 128 ? q : 128)) != DCT_OK) return st;
+        if (q == 256 && ((st = encode_scales(e, &task.sp_map[i], p_side)) != DCT_OK || (st = encode_scales(e, &task.sq_map[i], q_side)) != DCT_OK)) return st;
         task.sp[i] = scales_of(p_side);
         task.sq[i] = scales_of(q_side);
         task.depths[i] = ceil_div(a[i]->cols, kDepth);
     }
     task.p_rows = few ? n : m;
     task.q_rows = few ? m : n;
-    task.tiles_p = ceil_div(task.p_rows, 128);
+    task.tiles_p = ceil_div(task.p_rows, q == 256 ? 256 : 128);
     task.tiles_q = ceil_div(task.q_rows, q);
     return q == 32 ? launch<Few32>(task, sms, stream) : q == 64 ? launch<Few64>(task, sms, stream)
-         : q == 128 ? launch<Wide128>(task, sms, stream) : launch<Wide256>(task, sms, stream);
+         : q == 128 ? launch<Wide128>(task, sms, stream) : launch_pairs<false>(task, stream);
 }
 
 dct_status_t gated(const dct_act8_t* x, const dct_act8_t* w_gate, const dct_act8_t* w_up, bool gelu, const dct_act8_t* h, void* h_dense, dct_dtype_t dtype,
@@ -758,11 +989,14 @@ dct_status_t gated(const dct_act8_t* x, const dct_act8_t* w_gate, const dct_act8
     weight_scales[0] = scales_of(w_gate);
     weight_scales[1] = scales_of(w_up);
     (few ? task.sq : task.sp)[0] = scales_of(x);
+    if (!few && ((st = encode_scales(e, &task.sp_map[0], x)) != DCT_OK || (st = encode_scales(e, &task.sq_map[0], w_gate)) != DCT_OK ||
+                 (st = encode_scales(e, &task.sq_map[1], w_up)) != DCT_OK))
+        return st;
     task.p_rows = few ? f : rows;
     task.q_rows = few ? rows : f;
-    task.tiles_p = ceil_div(task.p_rows, 128);
+    task.tiles_p = ceil_div(task.p_rows, few ? 128 : 256);
     task.tiles_q = few ? 1 : ceil_div(f, 128);
-    return !few ? launch<GatedWide>(task, sms, stream) : q == 32 ? launch<GatedFew32>(task, sms, stream) : launch<GatedFew64>(task, sms, stream);
+    return !few ? launch_pairs<true>(task, stream) : q == 32 ? launch<GatedFew32>(task, sms, stream) : launch<GatedFew64>(task, sms, stream);
 }
 
 }  // namespace
