@@ -202,6 +202,14 @@ __device__ __forceinline__ uint32_t peer_address(uint32_t smem, uint32_t rank) {
 }
 __device__ __forceinline__ void st_peer(uint32_t at, float x) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory"); }
 
+// The thread of a converged warp that issues its commands.  The loops around them run in all lanes, so that descriptors and addresses are the warp's,
+// not a lane's: worked out in one lane they held the commands up (8192 x 8192 x 4096 of zeros, where power does not count: 223 us, now 170; of numbers 246 and 217).
+__device__ __forceinline__ bool elected() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
+
 // ---- what is written ----
 
 __device__ __forceinline__ void st32(void* p, const uint32_t (&w)[8]) {           // 32 bytes, a whole sector
@@ -484,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
     float* receive = reinterpret_cast<float*>(scales + S::kStages * S::kScaleBytes);
     float* turns = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(receive) + S::kReceiveBytes);
 
-    const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
+    const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = lane_id();
     const uint32_t split = task.split, rank = split > 1 ? cluster_rank() : 0u;
     const uint32_t all = task.depths[0] + task.depths[1];
     const uint32_t begin = static_cast<uint32_t>(static_cast<uint64_t>(all) * rank / split);
@@ -543,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
     tmem_after_sync();
     chain_wait_previous();
     if (split > 1) cluster_arrive();             // (waited for before anything is sent to a peer)
-    const uint32_t tmem = sh.tmem;
+    const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, sh.tmem, 0);
     const volatile uint32_t* stop = &sh.stop;
     const auto give_up = [&] { *const_cast<volatile uint32_t*>(&sh.stop) = 1u; };
 
@@ -572,28 +580,27 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
             }
         }
     } else if (warp == kProductWarp) {
-        if (lane == 0) {
-            uint32_t stage = 0, phase = 0, free_phase = 1, buffer = 0;
-            bool ok = true;
-            for (uint32_t t = tile0; ok && t < tile_count; t += step) {
-                ok = mbar_wait_bounded(&sh.free, free_phase, task.limit, stop);
-                free_phase ^= 1u;
+        uint32_t stage = 0, phase = 0, free_phase = 1, buffer = 0;
+        bool ok = true;
+        for (uint32_t t = tile0; ok && t < tile_count; t += step) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sh.free, free_phase, task.limit, stop));
+            free_phase ^= 1u;
+            tmem_after_sync();
+            for (uint32_t it = begin; ok && it < end; ++it) {
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sh.full[stage], phase, task.limit, stop));
+                if (!ok) break;
                 tmem_after_sync();
-                for (uint32_t it = begin; ok && it < end; ++it) {
-                    ok = mbar_wait_bounded(&sh.full[stage], phase, task.limit, stop);
-                    if (!ok) break;
-                    tmem_after_sync();
-                    const uint32_t kb = !S::kGated && it >= task.depths[0] ? it - task.depths[0] : it;
-                    if (it == begin || (kb & 3u) == 0) {
-                        buffer = (buffer + 1u) % kScaleBuffers;
-                        const uint64_t from = scale_desc(scales + stage * S::kScaleBytes);
+                const uint32_t kb = !S::kGated && it >= task.depths[0] ? it - task.depths[0] : it;
+                const bool with_scales = it == begin || (kb & 3u) == 0;
+                if (with_scales) buffer = (buffer + 1u) % kScaleBuffers;
+                const uint32_t idesc = S::kProduct | (kb & 3u) << 4 | (kb & 3u) << 29, sf = tmem + S::kAccCols + buffer * S::kScaleCols;
+                const uint64_t from = scale_desc(scales + stage * S::kScaleBytes);
+                const uint64_t p = tile_desc(tiles + stage * S::kStageBytes), q = p + S::kAcc * (kTileBytes >> 4);
+                if (elected()) {
+                    if (with_scales) {
 #pragma unroll
-                        for (uint32_t i = 0; i < S::kScaleTiles; ++i)
-                            scales_to_tmem(tmem + S::kAccCols + buffer * S::kScaleCols + 4 * i, from + i * (kAct8ScaleTile >> 4));
+                        for (uint32_t i = 0; i < S::kScaleTiles; ++i) scales_to_tmem(sf + 4 * i, from + i * (kAct8ScaleTile >> 4));
                     }
-                    const uint32_t idesc = S::kProduct | (kb & 3u) << 4 | (kb & 3u) << 29;
-                    const uint32_t sf = tmem + S::kAccCols + buffer * S::kScaleCols;
-                    const uint64_t p = tile_desc(tiles + stage * S::kStageBytes), q = p + S::kAcc * (kTileBytes >> 4);
 #pragma unroll
                     for (uint32_t k = 0; k < 4; ++k)
 #pragma unroll
@@ -601,15 +608,16 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                             block_scaled_product(tmem + i * S::kQ, p + i * (kTileBytes >> 4) + 2 * k, q + 2 * k, idesc, sf + 4 * i, sf + 4 * S::kAcc,
                                                  it != begin || k != 0);
                     tensor_commit(&sh.empty[stage]);
-                    if (++stage == S::kStages) stage = 0, phase ^= 1u;
+                    if (it + 1 == end) tensor_commit(&sh.done);
                 }
-                if (ok) tensor_commit(&sh.done);
+                __syncwarp();
+                if (++stage == S::kStages) stage = 0, phase ^= 1u;
             }
-            if (!ok) {
-                give_up();
-                tensor_commit(&sh.drained);
-                for (uint32_t k = 0; k < task.limit && !mbar_try_wait(&sh.drained, 0); ++k) {}
-            }
+        }
+        if (!ok && elected()) {
+            give_up();
+            tensor_commit(&sh.drained);
+            for (uint32_t k = 0; k < task.limit && !mbar_try_wait(&sh.drained, 0); ++k) {}
         }
     } else {
         const uint32_t group = warp >> 2, row_lane = (warp & 3u) * 32u + lane, lanes = tmem + ((warp & 3u) << 21);
@@ -717,7 +725,7 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
     uint8_t* scales = tiles + S::kStages * S::kStageBytes;
     float* turns = reinterpret_cast<float*>(scales + S::kStages * S::kScaleBytes);
 
-    const uint32_t warp = threadIdx.x >> 5, lane = lane_id(), rank = cluster_rank();
+    const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = lane_id(), rank = cluster_rank();
     const uint32_t depth = task.depths[0] + task.depths[1], tile0 = blockIdx.x / 2, step = gridDim.x / 2, tile_count = task.tiles_p * task.tiles_q;
     const volatile uint32_t* stop = &stop_word;
     const auto give_up = [&] { *const_cast<volatile uint32_t*>(&stop_word) = 1u; };
@@ -742,7 +750,7 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
     cluster_wait();
     tmem_after_sync();
     chain_wait_previous();
-    const uint32_t tmem = tmem_at;
+    const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tmem_at, 0);
 
     if (warp == kProducerWarp) {
         if (lane == 0) {
@@ -792,35 +800,37 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
             }
         }
     } else if (warp == kProductWarp) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             uint32_t stage = 0, phase = 0, free_phase = 1, buffer = 0;
             bool ok = true;
             for (uint32_t t = tile0; ok && t < tile_count; t += step) {
-                ok = wait_for_cluster(&free_again, free_phase, task.limit, stop);
+                ok = __all_sync(0xFFFFFFFFu, wait_for_cluster(&free_again, free_phase, task.limit, stop));
                 free_phase ^= 1u;
                 tmem_after_sync();
                 for (uint32_t it = 0; ok && it < depth; ++it) {
-                    ok = mbar_wait_bounded(&full[stage], phase, task.limit, stop);
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&full[stage], phase, task.limit, stop));
                     if (!ok) break;
                     tmem_after_sync();
                     const uint32_t kb = !kGated && it >= task.depths[0] ? it - task.depths[0] : it;
-                    if ((kb & 3u) == 0) {
-                        buffer = (buffer + 1u) % kScaleBuffers;
-                        const uint64_t from = scale_desc(scales + stage * S::kScaleBytes);
-#pragma unroll
-                        for (uint32_t i = 0; i < S::kScaleTiles; ++i)
-                            pair_scales_to_tmem(tmem + S::kAccCols + buffer * S::kScaleCols + 4 * i, from + i * (kAct8ScaleTile >> 4));
-                    }
+                    if ((kb & 3u) == 0) buffer = (buffer + 1u) % kScaleBuffers;
                     const uint32_t idesc = S::kProduct | (kb & 3u) << 4 | (kb & 3u) << 29, sf = tmem + S::kAccCols + buffer * S::kScaleCols;
+                    const uint64_t from = scale_desc(scales + stage * S::kScaleBytes);
                     const uint64_t p = tile_desc(tiles + stage * S::kStageBytes), q = p + (kTileBytes >> 4);
+                    if (elected()) {
+                        if ((kb & 3u) == 0) {
 #pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) pair_product(tmem, p + 2 * k, q + 2 * k, idesc, sf, sf + 4, it != 0 || k != 0);
-                    pair_commit(&empty[stage]);
+                            for (uint32_t i = 0; i < S::kScaleTiles; ++i) pair_scales_to_tmem(sf + 4 * i, from + i * (kAct8ScaleTile >> 4));
+                        }
+#pragma unroll
+                        for (uint32_t k = 0; k < 4; ++k) pair_product(tmem, p + 2 * k, q + 2 * k, idesc, sf, sf + 4, it != 0 || k != 0);
+                        pair_commit(&empty[stage]);
+                        if (it + 1 == depth) pair_commit(&done);
+                    }
+                    __syncwarp();
                     if (++stage == S::kStages) stage = 0, phase ^= 1u;
                 }
-                if (ok) pair_commit(&done);
             }
-            if (!ok) {
+            if (!ok && elected()) {
                 give_up();
                 pair_commit(&drained);
                 for (uint32_t k = 0; k < task.limit && !mbar_try_wait(&drained, 0); ++k) {}
