@@ -950,9 +950,10 @@ dct_status_t product(const dct_act8_t* const (&a)[2], const dct_act8_t* const (&
     task.bf16 = dtype == DCT_BF16;
     task.accumulate = accumulate;
     task.aligned = aligned_to(c, 32) && static_cast<size_t>(ld_c) * element_size(dtype) % 32 == 0;
-    // Up to 64 rows: the columns take the lanes.  Else pairs of CTAs, or single ones where the pairs' tiles are too few to go round twice.
+    // Up to 64 rows: the columns take the lanes.  Else single CTAs with tiles of 128 x 128, as long as all run at once; a pair's stage brings four times the
+    // products for twice the codes and takes about as long (2048 x 4096 x 4096: 29 us in pairs, 45 by single CTAs).
     const bool few = m <= 64;
-    const bool pairs = static_cast<uint64_t>(ceil_div(m, 256)) * ceil_div(n, 256) >= static_cast<uint64_t>(sms);
+    const bool pairs = static_cast<uint64_t>(ceil_div(m, 128)) * ceil_div(n, 128) > static_cast<uint64_t>(sms);
     const uint32_t q = few ? (m <= 32 ? 32 : 64) : pairs ? 256 : 128;
     for (uint32_t i = 0; i < count; ++i) {
         const dct_act8_t *p_side = few ? b[i] : a[i], *q_side = few ? a[i] : b[i];
