@@ -843,8 +843,9 @@ def act8(codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int) -> Act
 
 
 def new_act8(rows: int, cols: int, device="cuda") -> Act8:
-    """A matrix in 8 bits in new buffers; its contents are undefined."""
-    codes = torch.empty(rows, (cols + 15) // 16 * 16, dtype=torch.uint8, device=device)
+    """A matrix in 8 bits in new buffers; its contents are undefined.  (Rows of more than a line of memory start on one.)"""
+    to = 128 if cols > 128 else 16
+    codes = torch.empty(rows, (cols + to - 1) // to * to, dtype=torch.uint8, device=device)
     return Act8(codes, torch.empty(lib().dct_act8_scale_bytes(rows, cols), dtype=torch.uint8, device=device), rows, cols)
 
 

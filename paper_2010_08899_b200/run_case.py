@@ -18,7 +18,13 @@ A small command-line driver for profiling and quick timing of a single kernel at
     python -m paper_2010_08899_b200.run_case logprobs --rows 4096 --d 32768 --k 64 --dtype bf16
     python -m paper_2010_08899_b200.run_case logprobs_bwd / distill / distill_tail            (same arguments)
     python -m paper_2010_08899_b200.run_case student_step --rows 1024 --d 512 --vocab 32768 --k 64
-                                                                 (a split student learns from a teacher: all of it together)
+                                                                 (a split student learns from a teacher: all of it together;
+                                                                  --ffn 2048 puts a gated feed-forward block with kept activations in
+                                                                  8 bits in front, and its and the projection's products in 8 bits)
+    python -m paper_2010_08899_b200.run_case act8_pack --rows 16384 --d 4096 --dtype bf16     (into 8 bits; act8_pack_both, act8_unpack,
+                                                                  act8_transpose)
+    python -m paper_2010_08899_b200.run_case gemm8 --rows 8192 --d 4096 --ffn 8192            (the product of [rows, d] and [ffn, d])
+    python -m paper_2010_08899_b200.run_case gated8_fwd / gated8_bwd --rows 8192 --d 4096 --ffn 8192
 
 It prints the mean device time per call (CUDA events) and the algorithmic GB/s.
 """
@@ -209,13 +215,53 @@ def lm_call(args, dev):
             2 * rows * d * es)
 
 
+def act8_call(args, dev):
+    """One call on matrices in 8 bits (--rows of --d features, --ffn inner ones) on three sets of inputs by turns, and the bytes
+    it cannot do without."""
+    rows, d, f = args.rows, args.d, args.ffn or 2 * args.d
+    dt = torch.float32 if args.dtype == "f32" else torch.bfloat16
+    es = 4 if args.dtype == "f32" else 2
+    three = range(3)
+
+    def held(rows, cols, seed):
+        a = B.new_act8(rows, cols, dev)
+        B.dct_act8_pack(inputs.mp_gradients(rows, cols, seed, dtype=torch.bfloat16, device=dev), rows, cols, cols, a)
+        return a
+
+    if args.entry in ("act8_pack", "act8_pack_both"):
+        x, both = [inputs.mp_gradients(rows, d, 560 + j, dtype=dt, device=dev) for j in three], args.entry == "act8_pack_both"
+        out, out_t = [B.new_act8(rows, d, dev) for _ in three], [B.new_act8(d, rows, dev) if both else None for _ in three]
+        return lambda i: B.dct_act8_pack(x[i % 3], rows, d, d, out[i % 3], out_t[i % 3]), rows * d * (es + 1 + both)
+    if args.entry in ("act8_unpack", "act8_transpose"):
+        a = [held(rows, d, 570 + j) for j in three]
+        if args.entry == "act8_transpose":
+            out_t = [B.new_act8(d, rows, dev) for _ in three]
+            return lambda i: B.dct_act8_transpose(a[i % 3], out_t[i % 3]), 2 * rows * d
+        y = [torch.empty(rows, d, dtype=dt, device=dev) for _ in three]
+        return lambda i: B.dct_act8_unpack(a[i % 3], y[i % 3], d), rows * d * (1 + es)
+    if args.entry == "gemm8":
+        a, b = [held(rows, d, 580 + j) for j in three], [held(f, d, 590 + j) for j in three]
+        c = [torch.empty(rows, f, dtype=dt, device=dev) for _ in three]
+        return lambda i: B.dct_gemm8(a[i % 3], b[i % 3], c[i % 3], f), rows * d + f * d + rows * f * es
+    gate, up = [held(rows, f, 600 + j) for j in three], [held(rows, f, 610 + j) for j in three]
+    if args.entry == "gated8_fwd":
+        x, wg, wu = ([held(n, d, seed + j) for j in three] for n, seed in ((rows, 620), (f, 630), (f, 640)))
+        h = [B.new_act8(rows, f, dev) for _ in three]
+        return (lambda i: B.dct_gated8_fwd(x[i % 3], wg[i % 3], wu[i % 3], B.DCT_ACT_SILU, h[i % 3], None, 0, gate[i % 3], up[i % 3]),
+                rows * d + 2 * f * d + 3 * rows * f)
+    dh = [inputs.mp_gradients(rows, f, 650 + j, dtype=dt, device=dev) for j in three]
+    out = [[B.new_act8(rows, f, dev), B.new_act8(rows, f, dev)] + [B.new_act8(f, rows, dev) for _ in range(3)] for _ in three]
+    return (lambda i: B.dct_gated8_bwd(dh[i % 3], f, gate[i % 3], up[i % 3], B.DCT_ACT_SILU, *out[i % 3])), rows * f * (es + 7)
+
+
 def student_step(args, dev, stream):
     """A student (layer norm, split with DCT-MP, projection) learns from a teacher's top log-probabilities, its gradient sent
     by DCT-DP: --iters steps on one batch of --rows rows of --d features and --vocab columns, --k slots per row."""
     from .student import Student
     rows, d, vocab, top = args.rows, args.d, args.vocab, args.k or 64
     dt = torch.float32 if args.dtype == "f32" else torch.bfloat16
-    s = Student(d, vocab, rows, keep=B.k_from_sparsity(d, 75, 100), top=top, dtype=dt, device=dev, lr=20.0)
+    s = Student(d, vocab, rows, keep=B.k_from_sparsity(d, 75, 100), top=top, dtype=dt, device=dev, lr=20.0, ffn=args.ffn,
+                eight_bit=args.ffn > 0)
     hidden = inputs.mp_gradients(rows, d, 551, dtype=dt, device=dev)
     teacher = inputs.lm_logits(rows, vocab, 552, dtype=dt, device=dev)
     tokens = teacher.argmax(1).to(torch.int32)
@@ -235,12 +281,14 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("entry", choices=["select", "compress", "select_compress", "compress_layers", "decompress", "mp_fwd", "mp_bwd", "mp_unpack",
                                      "select_multi", "threshold_mean", "mp_fwd_sweep", "dp_sweep", "receiver_sweep",
-                                     "norm_fwd", "norm_bwd", "logprobs", "logprobs_bwd", "distill", "distill_tail", "student_step"])
+                                     "norm_fwd", "norm_bwd", "logprobs", "logprobs_bwd", "distill", "distill_tail", "student_step", "act8_pack", "act8_pack_both",
+                                     "act8_unpack", "act8_transpose", "gemm8", "gated8_fwd", "gated8_bwd"])
     ap.add_argument("--n", type=int, default=1 << 28)
     ap.add_argument("--k", type=int, default=0, help="survivor target (default: 0.01 %% of n, or 5 %% of d)")
     ap.add_argument("--rows", type=int, default=16384)
     ap.add_argument("--d", type=int, default=4096)
     ap.add_argument("--vocab", type=int, default=32768, help="student_step: columns of the logits")
+    ap.add_argument("--ffn", type=int, default=0, help="inner features of the feed-forward block (default: none for student_step, 2 d else)")
     ap.add_argument("--dtype", choices=["f32", "bf16"], default="bf16")
     ap.add_argument("--dist", choices=["mixture", "gaussian", "dlrm"], default="mixture")
     ap.add_argument("--iters", type=int, default=3)
@@ -403,6 +451,8 @@ def main():
                 nbytes = 4 * n + 8 * count       # clear the dense vector, read the packed pairs
     elif args.entry in ("norm_fwd", "norm_bwd", "logprobs", "logprobs_bwd", "distill", "distill_tail"):
         call, nbytes = lm_call(args, dev)
+    elif args.entry.startswith(("act8", "gemm8", "gated8")):
+        call, nbytes = act8_call(args, dev)
     else:
         rows, d = args.rows, args.d
         k = args.k or B.k_from_sparsity(d, 95, 100)

@@ -6,8 +6,11 @@ packing of DCT and the operators next to it run together, as they would be used.
     and back: the gradient at y through the same mask, the layer norm's gradients, and every parameter's gradient
     (one flat fp32 vector) through DCT-DP with error feedback at threshold life-span 1, applied by plain SGD.
 
+With ``ffn`` a gated feed-forward block stands in front of the layer norm, added to its input.  Between its forward and its backward pass it
+keeps its input, gate and up in 8 bits, and all of its products are of matrices in 8 bits; with ``eight_bit`` those of the projection are, too.
+
 The worker that holds the layer norm sends ``(cols, vals)``, the teacher sends ``(ids, log-probs)``, the trainer sends
-``(idx, val)``: the three messages of the step are the packed ones.  The projection is a library matrix product.
+``(idx, val)``: the three messages of the step are the packed ones.  Without ``eight_bit`` the projection is a library matrix product.
 """
 from __future__ import annotations
 
@@ -24,26 +27,91 @@ class StepResult(NamedTuple):
     grad_hidden: torch.Tensor   # [rows, d]: what goes back to the layer below
 
 
+class FeedForward:
+    """The gated feed-forward block (act(x gate^T) * x up^T) down^T of ``d`` features and ``f`` inner ones, in 8 bits.  ``params`` and
+    ``grads`` are flat fp32 vectors of 3 f d elements: gate [f, d], up [f, d], down [d, f]."""
+
+    def __init__(self, d: int, f: int, rows: int, params: torch.Tensor, grads: torch.Tensor, activation: int = B.DCT_ACT_SILU,
+                 dtype=torch.bfloat16, device="cuda"):
+        self.d, self.f, self.rows, self.activation = d, f, rows, activation
+        shapes = ((f, d), (f, d), (d, f))
+        self.gate, self.up, self.down = (params[i * f * d:(i + 1) * f * d].view(shape) for i, shape in enumerate(shapes))
+        self.grad_gate, self.grad_up, self.grad_down = (grads[i * f * d:(i + 1) * f * d].view(shape) for i, shape in enumerate(shapes))
+        new8 = lambda *size: B.new_act8(*size, device)
+        # the weights as the products take them, by rows and transposed
+        self.gate8, self.up8, self.down8 = new8(f, d), new8(f, d), new8(d, f)
+        self.gate8_t, self.up8_t, self.down8_t = new8(d, f), new8(d, f), new8(f, d)
+        # kept from the forward pass to the backward pass
+        self.x8, self.kept_gate, self.kept_up = new8(rows, d), new8(rows, f), new8(rows, f)
+        self.h8, self.y = new8(rows, f), torch.empty(rows, d, dtype=dtype, device=device)
+        # of the backward pass
+        self.x8_t, self.h8_t, self.dy8, self.dy8_t = new8(d, rows), new8(f, rows), new8(rows, d), new8(d, rows)
+        self.dgate8, self.dup8, self.dgate8_t, self.dup8_t = new8(rows, f), new8(rows, f), new8(f, rows), new8(f, rows)
+        self.dh, self.dx = torch.empty(rows, f, dtype=dtype, device=device), torch.empty(rows, d, dtype=dtype, device=device)
+
+    def load(self) -> None:
+        """The parameters into 8 bits: after every change of theirs."""
+        d, f = self.d, self.f
+        B.dct_act8_pack(self.gate, f, d, d, self.gate8, self.gate8_t)
+        B.dct_act8_pack(self.up, f, d, d, self.up8, self.up8_t)
+        B.dct_act8_pack(self.down, d, f, f, self.down8, self.down8_t)
+
+    def forward(self, x: torch.Tensor, keep: bool = True) -> torch.Tensor:
+        rows, d = self.rows, self.d
+        B.dct_act8_pack(x, rows, d, d, self.x8)
+        kept = (self.kept_gate, self.kept_up) if keep else (None, None)
+        B.dct_gated8_fwd(self.x8, self.gate8, self.up8, self.activation, self.h8, None, 0, *kept)
+        B.dct_gemm8(self.h8, self.down8, self.y, d)
+        return self.y
+
+    def backward(self, dy: torch.Tensor) -> torch.Tensor:
+        """The gradient at the last forward pass's input, from that at its output; the weights' gradients go to ``grads``."""
+        rows, d, f = self.rows, self.d, self.f
+        B.dct_act8_pack(dy, rows, d, d, self.dy8, self.dy8_t)
+        B.dct_gemm8(self.dy8, self.down8_t, self.dh, f)
+        B.dct_gated8_bwd(self.dh, f, self.kept_gate, self.kept_up, self.activation, self.dgate8, self.dup8, self.dgate8_t, self.dup8_t,
+                         self.h8_t)
+        B.dct_act8_transpose(self.x8, self.x8_t)
+        B.dct_gemm8(self.dgate8, self.gate8_t, self.dx, d, self.dup8, self.up8_t)
+        B.dct_gemm8(self.dgate8_t, self.x8_t, self.grad_gate, d)
+        B.dct_gemm8(self.dup8_t, self.x8_t, self.grad_up, d)
+        B.dct_gemm8(self.dy8_t, self.h8_t, self.grad_down, f)
+        return self.dx
+
+
 class Student:
     """Layer norm and projection of ``d`` features to ``vocab`` columns.  The parameters are one flat fp32 vector
-    (norm weight, norm bias, projection [vocab, d]); activations have type ``dtype``."""
+    (norm weight, norm bias, projection [vocab, d], then the feed-forward block's if ``ffn`` > 0); activations have type ``dtype``."""
 
     def __init__(self, d: int, vocab: int, rows: int, keep: int, top: int, density: float = 0.05, tail: bool = True,
-                 temperature: float = 1.0, lr: float = 0.5, dtype=torch.bfloat16, device="cuda", seed: int = 0):
+                 temperature: float = 1.0, lr: float = 0.5, dtype=torch.bfloat16, device="cuda", seed: int = 0, ffn: int = 0,
+                 eight_bit: bool = False):
         self.d, self.vocab, self.rows, self.keep, self.top, self.lr = d, vocab, rows, keep, top, lr
         self.mode = B.DCT_DISTILL_TAIL if tail else B.DCT_DISTILL_RENORM
         self.inv_t = 1.0 / temperature
         gen = torch.Generator(device=device)
         gen.manual_seed(seed)
-        n = 2 * d + vocab * d
+        head = 2 * d + vocab * d
+        n = head + 3 * ffn * d
         new = lambda *shape, dt=torch.float32: torch.empty(*shape, dtype=dt, device=device)
         self.params = torch.zeros(n, device=device)
         self.weight, self.bias = self.params[:d], self.params[d:2 * d]
-        self.projection = self.params[2 * d:].view(vocab, d)
+        self.projection = self.params[2 * d:head].view(vocab, d)
         self.weight.fill_(1.0)
         self.projection.copy_(torch.randn(vocab, d, generator=gen, device=device) * d ** -0.5)
+        if ffn:
+            self.params[head:].copy_(torch.randn(3 * ffn * d, generator=gen, device=device))
+            self.params[head:head + 2 * ffn * d].mul_(d ** -0.5)
+            self.params[head + 2 * ffn * d:].mul_(ffn ** -0.5)
         self.grads, self.residual, self.update = torch.zeros(n, device=device), torch.zeros(n, device=device), torch.zeros(n, device=device)
+        self.grad_projection = self.grads[2 * d:head].view(vocab, d)
+        self.block = FeedForward(d, ffn, rows, self.params[head:], self.grads[head:], dtype=dtype, device=device) if ffn else None
+        self.eight_bit, self.loaded = eight_bit, False             # loaded: the forms of the parameters that products take are up to date
         # what a step needs, laid out once
+        if eight_bit:
+            self.projection8, self.projection8_t = B.new_act8(vocab, d, device), B.new_act8(d, vocab, device)
+            self.y8, self.y8_t, self.scores = B.new_act8(rows, d, device), B.new_act8(d, rows, device), new(rows, vocab, dt=dtype)
+            self.dscores8, self.dscores8_t, self.grad_y = B.new_act8(rows, vocab, device), B.new_act8(vocab, rows, device), new(rows, d, dt=dtype)
         self.y, self.y_kept, self.g_kept = new(rows, d, dt=dtype), new(rows, d, dt=dtype), new(rows, d, dt=dtype)
         self.mean, self.rstd, self.loss = new(rows), new(rows), new(rows)
         self.cols, self.vals, self.gvals = new(rows * keep, dt=torch.int16), new(rows * keep, dt=dtype), new(rows * keep, dt=dtype)
@@ -55,12 +123,29 @@ class Student:
         self.norm_ws = B.new_workspace(B.dct_layer_norm_bwd_workspace_bytes(rows, d), device)
         self.send_ws = B.new_workspace(B.dct_dp_select_compress_workspace_bytes(n), device)
 
-    def logits(self, hidden: torch.Tensor) -> torch.Tensor:
+    def load(self) -> None:
+        """The parameters in the forms the products take."""
+        if self.block:
+            self.block.load()
+        if self.eight_bit:
+            B.dct_act8_pack(self.projection, self.vocab, self.d, self.d, self.projection8, self.projection8_t)
+        self.loaded = True
+
+    def logits(self, hidden: torch.Tensor, training: bool = False) -> torch.Tensor:
         """The student's logits, with the activations that cross the split packed to ``keep`` per row."""
         rows, d = self.rows, self.d
+        if not self.loaded:
+            self.load()
+        if self.block:
+            hidden = hidden + self.block.forward(hidden, keep=training)
+        self.hidden = hidden if training else None             # what the layer norm's backward pass takes
         B.dct_layer_norm_fwd(hidden, rows, d, d, self.weight, self.bias, 1e-5, self.y, d, self.mean, self.rstd)
         B.dct_mp_topk_pack_fwd(self.y, rows, d, d, self.keep, self.cols, self.vals)
         B.dct_mp_unpack(self.cols, self.vals, rows, d, d, self.keep, self.y_kept)
+        if self.eight_bit:
+            B.dct_act8_pack(self.y_kept, rows, d, d, self.y8)
+            B.dct_gemm8(self.y8, self.projection8, self.scores, self.vocab)
+            return self.scores
         return self.y_kept @ self.projection.to(self.y.dtype).t()
 
     def teach(self, teacher_logits: torch.Tensor) -> None:
@@ -71,24 +156,34 @@ class Student:
     def step(self, hidden: torch.Tensor, teacher_logits: torch.Tensor) -> StepResult:
         rows, d, vocab = self.rows, self.d, self.vocab
         self.teach(teacher_logits)
-        logits = self.logits(hidden)
+        logits = self.logits(hidden, training=True)
         # loss, and the gradient in the place of the logits
         B.dct_lm_distill(logits, rows, vocab, vocab, self.inv_t, self.ids, self.logprobs, self.top, self.mode, self.share,
                          self.loss, logits, vocab, self.status)
-        torch.mm(logits.t().float(), self.y_kept.float(), out=self.grads[2 * d:].view(vocab, d))
-        grad_y = logits @ self.projection.to(logits.dtype)
+        if self.eight_bit:
+            B.dct_act8_pack(logits, rows, vocab, vocab, self.dscores8, self.dscores8_t)
+            B.dct_act8_transpose(self.y8, self.y8_t)
+            B.dct_gemm8(self.dscores8_t, self.y8_t, self.grad_projection, d)
+            B.dct_gemm8(self.dscores8, self.projection8_t, self.grad_y, d)
+            grad_y = self.grad_y
+        else:
+            torch.mm(logits.t().float(), self.y_kept.float(), out=self.grad_projection)
+            grad_y = logits @ self.projection.to(logits.dtype)
         # back over the split through the mask of the forward pass
         B.dct_mp_pack_bwd(grad_y, rows, d, d, self.keep, self.cols, self.gvals)
         B.dct_mp_unpack(self.cols, self.gvals, rows, d, d, self.keep, self.g_kept)
         grad_hidden = torch.empty_like(hidden)
-        B.dct_layer_norm_bwd(self.g_kept, d, hidden, rows, d, d, self.weight, self.mean, self.rstd, grad_hidden, d,
+        B.dct_layer_norm_bwd(self.g_kept, d, self.hidden, rows, d, d, self.weight, self.mean, self.rstd, grad_hidden, d,
                              self.grads[:d], self.grads[d:2 * d], self.norm_ws)
+        if self.block:
+            grad_hidden += self.block.backward(grad_hidden)
         # the trainer's message, and the update it carries
         n = self.params.numel()
         B.dct_dp_select_compress(self.grads, self.residual, n, self.k, self.tau, self.idx, self.val, self.k, self.sent,
                                  self.send_ws)
         B.dct_dp_decompress(self.idx, self.val, self.sent, self.k, self.update, n, False, self.applied)
         self.params.sub_(self.update, alpha=self.lr)
+        self.loaded = False
         return StepResult(self.loss, self.sent, grad_hidden)
 
     def score(self, hidden: torch.Tensor, tokens: torch.Tensor, alternatives: int = 0):
