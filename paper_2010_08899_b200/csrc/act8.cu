@@ -64,8 +64,10 @@ __device__ __forceinline__ void fetch_rows(T* tile, const TileTask& task, uint32
 }
 
 // What a tile's planes are made of.  load(): the lane's patch of each plane; power: of the lane's row (lane % 8) of each held input.
-template <typename T> struct Dense {
-    static constexpr uint32_t kPlanes = 1, kHeld = 0, kDenseBytes = 128 * 128 * sizeof(T), kCtas = sizeof(T) == 4 ? 1 : 2;
+// kDirect: rows that start on no boundary are fetched element by element.  That is not done ahead, so two CTAs to an SM take turns (2047 x 5003
+// fp32: 13 us, with one 16); fp32 tiles that are fetched ahead leave room for one, which then has all the registers.
+template <typename T, bool kDirect> struct Dense {
+    static constexpr uint32_t kPlanes = 1, kHeld = 0, kDenseBytes = 128 * 128 * sizeof(T), kCtas = sizeof(T) == 4 && !kDirect ? 1 : 2;
     using Element = T;
     __device__ static __forceinline__ void load(float (&v)[1][kR][kC], const uint8_t* stage, const float*) {
         const T* from = reinterpret_cast<const T*>(stage) + (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
@@ -109,7 +111,7 @@ template <typename T, bool kGelu> struct Gated {
 template <typename S> struct TileShape {
     static constexpr uint32_t kStageBytes = S::kDenseBytes + S::kHeld * 128 * 128;
     static constexpr uint32_t kLargestBytes = S::kPlanes * kWarps * 128 * 4;
-    static constexpr uint32_t kSharedBytes = 128 + 2 * kStageBytes + kLargestBytes;
+    static constexpr uint32_t shared_bytes(uint32_t stages) { return 128 + stages * kStageBytes + kLargestBytes; }
     static_assert(kStageBytes >= S::kPlanes * kTurnedBytes, "the transposed codes take the place of a tile's inputs");
 };
 
@@ -214,9 +216,9 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
     __shared__ alignas(16) uint32_t bytes[S::kPlanes][128];
     __shared__ uint32_t stop;
     uint8_t* stages = raw + ((128u - (smem_addr(raw) & 127u)) & 127u);
-    float* largest = reinterpret_cast<float*>(stages + 2 * Shape::kStageBytes);       // [plane][warp][column]
-    const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
     const bool copied = S::kHeld != 0 || !task.direct;
+    float* largest = reinterpret_cast<float*>(stages + (copied ? 2 : 1) * Shape::kStageBytes);       // [plane][warp][column]
+    const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
     chain_release_next();
     if (threadIdx.x == 0) {
         mbar_init(&arrived[0], 1);
@@ -385,7 +387,10 @@ dct_status_t launch_tiles(TileTask& task, uint32_t rows, uint32_t cols, const vo
                           cudaStream_t stream) {
     using T = typename S::Element;
     static SharedLimit allowed;
-    dct_status_t st = allow_shared(act8_tile_kernel<S>, TileShape<S>::kSharedBytes, allowed);
+    // (a matrix fetched element by element is not fetched ahead: one stage, and more CTAs to an SM instead)
+    const bool ahead = S::kHeld != 0 || unit_rows<T>(x, ld_x);
+    const uint32_t shared = TileShape<S>::shared_bytes(ahead ? 2 : 1);
+    dct_status_t st = allow_shared(act8_tile_kernel<S>, shared, allowed);
     if (st != DCT_OK) return st;
     const int sms = sm_count();
     if (sms <= 0) return DCT_ERR_CUDA;
@@ -401,7 +406,7 @@ dct_status_t launch_tiles(TileTask& task, uint32_t rows, uint32_t cols, const vo
     if (S::kDenseBytes != 0) {
         task.x = x;
         task.ld_x = ld_x;
-        task.direct = !x || !unit_rows<T>(x, ld_x);
+        task.direct = !x || !unit_rows<T>(x, ld_x);         // (as the kernel was chosen)
         if (!task.direct && (st = tensor_map(e, &task.map[0], tensor_type<T>(), sizeof(T), x, rows, cols, ld_x, 128, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != DCT_OK)
             return st;
     }
@@ -409,9 +414,10 @@ dct_status_t launch_tiles(TileTask& task, uint32_t rows, uint32_t cols, const vo
     task.held[1] = device_view(held1);
     if (held0 && (st = tensor_map(e, &task.map[1], held0, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != DCT_OK) return st;
     if (held1 && (st = tensor_map(e, &task.map[2], held1, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != DCT_OK) return st;
-    const uint64_t at_once = static_cast<uint64_t>(sms) * S::kCtas;
+    // as many CTAs as an SM has room for
+    const uint64_t at_once = static_cast<uint64_t>(sms) * (S::kCtas * (shared + 2048) <= 228 * 1024 ? S::kCtas : 1);
     DCT_CUDA_TRY(launch_chained_smem(act8_tile_kernel<S>, static_cast<unsigned>(tiles < at_once ? tiles : at_once), kTileThreads,
-                                     TileShape<S>::kSharedBytes, stream, task));
+                                     shared, stream, task));
     return DCT_OK;
 }
 
@@ -444,8 +450,9 @@ extern "C" dct_status_t dct_act8_pack(const void* x, dct_dtype_t dtype, uint32_t
     task.by_rows[0] = device_view(out);
     task.turned[0] = device_view(out_t);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    return dtype == DCT_F32 ? launch_tiles<Dense<float>>(task, rows, cols, x, ld, nullptr, nullptr, stream)
-                            : launch_tiles<Dense<__nv_bfloat16>>(task, rows, cols, x, ld, nullptr, nullptr, stream);
+    auto launch = dtype == DCT_F32 ? (unit_rows<float>(x, ld) ? launch_tiles<Dense<float, false>> : launch_tiles<Dense<float, true>>)
+                : unit_rows<__nv_bfloat16>(x, ld) ? launch_tiles<Dense<__nv_bfloat16, false>> : launch_tiles<Dense<__nv_bfloat16, true>>;
+    return launch(task, rows, cols, x, ld, nullptr, nullptr, stream);
 }
 
 extern "C" dct_status_t dct_act8_unpack(const dct_act8_t* a, void* y, dct_dtype_t dtype, uint32_t ld_y, dct_stream_t stream_) {

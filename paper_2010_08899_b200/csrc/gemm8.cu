@@ -200,6 +200,9 @@ __device__ __forceinline__ uint32_t peer_address(uint32_t smem, uint32_t rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem), "r"(rank));
     return r;
 }
+__device__ __forceinline__ void st_peer4(uint32_t at, float a, float b, float c, float d) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
+}
 __device__ __forceinline__ void st_peer(uint32_t at, float x) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory"); }
 
 // The thread of a converged warp that issues its commands.  The loops around them run in all lanes, so that descriptors and addresses are the warp's,
@@ -418,6 +421,30 @@ __device__ __forceinline__ void finish_wide_gated(const Task& task, uint32_t fro
     }
     if (task.h.codes || task.gate.codes) named_barrier_sync(1, kEpilogueWarps * 32);          // before the next tile's are written
     if (task.c) put_dense<64>(task, row0, task.p_rows, g, col, task.q_rows, turn);
+}
+
+// A split tile of 128 x 128: a part's share of a CTA's columns lies in its shared memory by rows, groups of four columns exchanged by row, so that eight
+// neighbouring rows' groups are in eight different places.
+__device__ __forceinline__ uint32_t split_place(uint32_t part, uint32_t row, uint32_t group, uint32_t groups) {       // in groups
+    return (part * 128u + row) * groups + (group ^ (groups >= 8 ? row & 7u : row >> 1 & 3u));
+}
+// The columns of one of kSplit CTAs, of which a warp group has half: the parts are added up in their order.
+template <uint32_t kSplit>
+__device__ __forceinline__ void finish_split(const Task& task, const float* receive, uint32_t row0, uint32_t col0, float* turn) {
+    constexpr uint32_t kN = 128 / kSplit / 2, kGroups = 128 / kSplit / 4;
+    const uint32_t half = threadIdx.x >> 7, row = threadIdx.x & 127u;
+    float v[kN];
+#pragma unroll
+    for (uint32_t k = 0; k < kSplit; ++k)
+#pragma unroll
+        for (uint32_t i = 0; i < kN / 4; ++i) {
+            const float4 x = reinterpret_cast<const float4*>(receive)[split_place(k, row, half * (kN / 4) + i, kGroups)];
+            v[4 * i] = k == 0 ? x.x : __fadd_rn(v[4 * i], x.x);
+            v[4 * i + 1] = k == 0 ? x.y : __fadd_rn(v[4 * i + 1], x.y);
+            v[4 * i + 2] = k == 0 ? x.z : __fadd_rn(v[4 * i + 2], x.z);
+            v[4 * i + 3] = k == 0 ? x.w : __fadd_rn(v[4 * i + 3], x.w);
+        }
+    put_dense<kN>(task, row0, task.p_rows, v, col0 + half * kN, task.q_rows, turn);
 }
 
 // Few rows: a thread adds up its column's parts of the rows row0 .. row0 + count, which lie in shared memory, and writes them.  These are loops, not
@@ -642,17 +669,33 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                 // this part's columns to the CTAs that add them up
                 const uint32_t shift = __ffs(S::kQ / split) - 1u, slice = 1u << shift, columns = task.q_rows - at.q * S::kQ;
                 cluster_wait();
-#pragma unroll
-                for (uint32_t a = 0; a < S::kAcc; ++a) {
+                if constexpr (!S::kFew) {
                     float v[S::kQ / 2];
-                    tmem_load<S::kQ / 2>(v, lanes + a * S::kQ + group * (S::kQ / 2));
+                    tmem_load<S::kQ / 2>(v, lanes + group * (S::kQ / 2));
                     tmem_loaded<S::kQ / 2>(v);
+                    if (!ok) {
 #pragma unroll
-                    for (uint32_t j = 0; j < S::kQ / 2; ++j) {
-                        const uint32_t col = group * (S::kQ / 2) + j, to = col >> shift;
-                        if (col < columns)
-                            st_peer(peer_address(smem_addr(receive + ((rank * S::kAcc + a) * slice + (col & (slice - 1u))) * 128u + row_lane), to),
-                                    ok ? v[j] : __uint_as_float(kLost));
+                        for (uint32_t j = 0; j < S::kQ / 2; ++j) v[j] = __uint_as_float(kLost);
+                    }
+#pragma unroll
+                    for (uint32_t j = 0; j < S::kQ / 2; j += 4) {
+                        const uint32_t col = group * (S::kQ / 2) + j;
+                        const uint32_t at = smem_addr(receive) + 16u * split_place(rank, row_lane, (col & (slice - 1u)) >> 2, slice >> 2);
+                        if (col < columns) st_peer4(peer_address(at, col >> shift), v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    }
+                } else {
+#pragma unroll
+                    for (uint32_t a = 0; a < S::kAcc; ++a) {
+                        float v[S::kQ / 2];
+                        tmem_load<S::kQ / 2>(v, lanes + a * S::kQ + group * (S::kQ / 2));
+                        tmem_loaded<S::kQ / 2>(v);
+#pragma unroll
+                        for (uint32_t j = 0; j < S::kQ / 2; ++j) {
+                            const uint32_t col = group * (S::kQ / 2) + j, to = col >> shift;
+                            if (col < columns)
+                                st_peer(peer_address(smem_addr(receive + ((rank * S::kAcc + a) * slice + (col & (slice - 1u))) * 128u + row_lane), to),
+                                        ok ? v[j] : __uint_as_float(kLost));
+                        }
                     }
                 }
                 break;             // (one tile to a cluster)
@@ -696,12 +739,13 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                 finish_few<S>(task, from, split, slice, q0, half, p0 + row_lane);
             } else {
                 float* turn = turns + warp * (32 * 17);
-                for (uint32_t j = 0; j < half; j += 8) {
-                    float v[8];
-#pragma unroll
-                    for (uint32_t i = 0; i < 8; ++i) v[i] = few_sum<S>(from + (j + i) * 128u, split, slice);
-                    put_dense<8>(task, p0 + (warp & 3u) * 32u, task.p_rows, v, q0 + j, task.q_rows, turn);
-                }
+                const uint32_t row0 = p0 + (warp & 3u) * 32u, col0 = at.q * S::kQ + rank * slice;
+                if (split == 2)
+                    finish_split<2>(task, receive, row0, col0, turn);
+                else if (split == 4)
+                    finish_split<4>(task, receive, row0, col0, turn);
+                else
+                    finish_split<8>(task, receive, row0, col0, turn);
             }
         }
     }
