@@ -25,22 +25,31 @@ struct TileTask {
     Act8 by_rows[2], turned[3];  // outputs by plane
 };
 
-// Four neighbouring elements
-template <typename T> __device__ __forceinline__ void four(float (&v)[kC], const T* p);
-template <> __device__ __forceinline__ void four(float (&v)[kC], const float* p) {
+// Four neighbouring elements as two pairs of fp32; a patch is kept as pairs, which is how most instructions take it
+struct Four {
+    uint64_t lo, hi;
+    __device__ __forceinline__ float at(uint32_t c) const {
+        float a, b;
+        unpack2(c < 2 ? lo : hi, a, b);
+        return c & 1u ? b : a;
+    }
+    __device__ __forceinline__ Four times(uint64_t f01, uint64_t f23) const { return Four{mul2(lo, f01), mul2(hi, f23)}; }
+};
+template <typename T> __device__ __forceinline__ Four four(const T* p);
+template <> __device__ __forceinline__ Four four(const float* p) {
     const float4 w = *reinterpret_cast<const float4*>(p);
-    v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
+    return Four{pack2(w.x, w.y), pack2(w.z, w.w)};
 }
-template <> __device__ __forceinline__ void four(float (&v)[kC], const __nv_bfloat16* p) {
+template <> __device__ __forceinline__ Four four(const __nv_bfloat16* p) {
     const uint2 w = *reinterpret_cast<const uint2*>(p);
-    v[0] = __uint_as_float(w.x << 16), v[1] = __uint_as_float(w.x & 0xFFFF0000u), v[2] = __uint_as_float(w.y << 16), v[3] = __uint_as_float(w.y & 0xFFFF0000u);
+    return Four{pack2(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u)), pack2(__uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u))};
 }
-__device__ __forceinline__ void four(float (&v)[kC], uint32_t codes, float power) {
-    act8_values2(codes & 0xFFFFu, v[0], v[1]);
-    act8_values2(codes >> 16, v[2], v[3]);
+__device__ __forceinline__ Four four(uint32_t codes, float power) {
+    float a, b, c, d;
+    act8_values2(codes & 0xFFFFu, a, b);
+    act8_values2(codes >> 16, c, d);
     const uint64_t by = pack2(power, power);
-    unpack2(mul2(pack2(v[0], v[1]), by), v[0], v[1]);
-    unpack2(mul2(pack2(v[2], v[3]), by), v[2], v[3]);
+    return Four{mul2(pack2(a, b), by), mul2(pack2(c, d), by)};
 }
 
 // A dense tile whose rows start on no boundary, into the place a tensor copy would have put it: every warp its own rows, neighbouring lanes
@@ -69,41 +78,36 @@ __device__ __forceinline__ void fetch_rows(T* tile, const TileTask& task, uint32
 template <typename T, bool kDirect> struct Dense {
     static constexpr uint32_t kPlanes = 1, kHeld = 0, kDenseBytes = 128 * 128 * sizeof(T), kCtas = sizeof(T) == 4 && !kDirect ? 1 : 2;
     using Element = T;
-    __device__ static __forceinline__ void load(float (&v)[1][kR][kC], const uint8_t* stage, const float*) {
+    __device__ static __forceinline__ void load(Four (&v)[1][kR], const uint8_t* stage, const float*) {
         const T* from = reinterpret_cast<const T*>(stage) + (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
 #pragma unroll
-        for (uint32_t r = 0; r < kR; ++r) four<T>(v[0][r], from + r * 128);
+        for (uint32_t r = 0; r < kR; ++r) v[0][r] = four<T>(from + r * 128);
     }
 };
 struct Held {
     static constexpr uint32_t kPlanes = 1, kHeld = 1, kDenseBytes = 0, kCtas = 2;
     using Element = float;
-    __device__ static __forceinline__ void load(float (&v)[1][kR][kC], const uint8_t* stage, const float* power) {
+    __device__ static __forceinline__ void load(Four (&v)[1][kR], const uint8_t* stage, const float* power) {
         const uint8_t* from = stage + (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
 #pragma unroll
-        for (uint32_t r = 0; r < kR; ++r) four(v[0][r], *reinterpret_cast<const uint32_t*>(from + r * 128), __shfl_sync(0xFFFFFFFFu, power[0], r));
+        for (uint32_t r = 0; r < kR; ++r) v[0][r] = four(*reinterpret_cast<const uint32_t*>(from + r * 128), __shfl_sync(0xFFFFFFFFu, power[0], r));
     }
 };
 // dh, gate and up; the planes are dgate, dup and h
 template <typename T, bool kGelu> struct Gated {
     static constexpr uint32_t kPlanes = 3, kHeld = 2, kDenseBytes = 128 * 128 * sizeof(T), kCtas = 1;
     using Element = T;
-    __device__ static __forceinline__ void load(float (&v)[3][kR][kC], const uint8_t* stage, const float* power) {
+    __device__ static __forceinline__ void load(Four (&v)[3][kR], const uint8_t* stage, const float* power) {
         const uint32_t at = (threadIdx.x >> 5) * (kR * 128) + lane_id() * kC;
 #pragma unroll
         for (uint32_t r = 0; r < kR; ++r) {
-            float d[kC], g[kC], u[kC];
-            four<T>(d, reinterpret_cast<const T*>(stage) + at + r * 128);
-            four(g, *reinterpret_cast<const uint32_t*>(stage + kDenseBytes + at + r * 128), __shfl_sync(0xFFFFFFFFu, power[0], r));
-            four(u, *reinterpret_cast<const uint32_t*>(stage + kDenseBytes + 128 * 128 + at + r * 128), __shfl_sync(0xFFFFFFFFu, power[1], r));
-#pragma unroll
-            for (uint32_t c = 0; c < kC; c += 2) {
-                const uint64_t d2 = pack2(d[c], d[c + 1]), u2 = pack2(u[c], u[c + 1]);
-                const Gate2 a = gate2<true, kGelu>(g[c], g[c + 1]);
-                unpack2(mul2(mul2(d2, u2), a.slope), v[0][r][c], v[0][r][c + 1]);
-                unpack2(mul2(d2, a.value), v[1][r][c], v[1][r][c + 1]);
-                unpack2(mul2(u2, a.value), v[2][r][c], v[2][r][c + 1]);
-            }
+            const Four d = four<T>(reinterpret_cast<const T*>(stage) + at + r * 128);
+            const Four g = four(*reinterpret_cast<const uint32_t*>(stage + kDenseBytes + at + r * 128), __shfl_sync(0xFFFFFFFFu, power[0], r));
+            const Four u = four(*reinterpret_cast<const uint32_t*>(stage + kDenseBytes + 128 * 128 + at + r * 128), __shfl_sync(0xFFFFFFFFu, power[1], r));
+            const Gate2 a = gate2<true, kGelu>(g.lo), b = gate2<true, kGelu>(g.hi);
+            v[0][r] = Four{mul2(mul2(d.lo, u.lo), a.slope), mul2(mul2(d.hi, u.hi), b.slope)};
+            v[1][r] = d.times(a.value, b.value);
+            v[2][r] = u.times(a.value, b.value);
         }
     }
 };
@@ -118,11 +122,11 @@ template <typename S> struct TileShape {
 // A lane's patch of a plane by rows: all its reductions under way at once, and row r's byte and power worked out by lane r alone.  kWhole: the
 // tile lies inside the matrix.
 template <bool kWhole>
-__device__ __forceinline__ void write_rows(const float (&v)[kR][kC], const Act8& out, uint32_t tile_r, uint32_t tile_c) {
+__device__ __forceinline__ void write_rows(const Four (&v)[kR], const Act8& out, uint32_t tile_r, uint32_t tile_c) {
     const uint32_t warp = threadIdx.x >> 5, lane = lane_id(), row = tile_r * 128u + warp * kR, col = tile_c * 128u + lane * kC;
     float m[kR], mine = 0.0f;
 #pragma unroll
-    for (uint32_t r = 0; r < kR; ++r) m[r] = warp_largest(largest3(largest3(v[r][0], v[r][1], v[r][2]), v[r][3], 0.0f));
+    for (uint32_t r = 0; r < kR; ++r) m[r] = warp_largest(largest3(largest3(v[r].at(0), v[r].at(1), v[r].at(2)), v[r].at(3), 0.0f));
 #pragma unroll
     for (uint32_t r = 0; r < kR; ++r) mine = lane == r ? m[r] : mine;
     const uint32_t byte = act8_byte(magnitude(mine));
@@ -133,10 +137,8 @@ __device__ __forceinline__ void write_rows(const float (&v)[kR][kC], const Act8&
 #pragma unroll
     for (uint32_t r = 0; r < kR; ++r) {
         const float f = __shfl_sync(0xFFFFFFFFu, inverse, r);
-        float a, b, c, d;
-        unpack2(mul2(pack2(v[r][0], v[r][1]), pack2(f, f)), a, b);
-        unpack2(mul2(pack2(v[r][2], v[r][3]), pack2(f, f)), c, d);
-        q[r] = act8_codes4(a, b, c, d);
+        const Four x = v[r].times(pack2(f, f), pack2(f, f));
+        q[r] = act8_codes4(x.at(0), x.at(1), x.at(2), x.at(3));
     }
     if (__any_sync(0xFFFFFFFFu, byte == 247u)) {
 #pragma unroll
@@ -155,33 +157,29 @@ __device__ __forceinline__ void write_rows(const float (&v)[kR][kC], const Act8&
 }
 
 // A lane's columns of its warp's eight rows: the magnitudes' maxima, for the columns' blocks
-__device__ __forceinline__ void note_columns(const float (&v)[kR][kC], float* largest) {
+__device__ __forceinline__ void note_columns(const Four (&v)[kR], float* largest) {
     float m[kC] = {};
 #pragma unroll
     for (uint32_t r = 0; r < kR; r += 2)
 #pragma unroll
-        for (uint32_t c = 0; c < kC; ++c) m[c] = largest3(m[c], v[r][c], v[r + 1][c]);
+        for (uint32_t c = 0; c < kC; ++c) m[c] = largest3(m[c], v[r].at(c), v[r + 1].at(c));
     *reinterpret_cast<float4*>(largest + (threadIdx.x >> 5) * 128u + lane_id() * kC) = make_float4(m[0], m[1], m[2], m[3]);
 }
 // The patch's columns as codes, eight of a column together, to where the columns lie as rows.  (Neighbouring lanes write different groups of
 // a column's codes: no two to the same bank at a time.)
-__device__ __forceinline__ void turn_columns(const float (&v)[kR][kC], const uint32_t* bytes, uint8_t* turned) {
+__device__ __forceinline__ void turn_columns(const Four (&v)[kR], const float* inverses, bool huge, uint8_t* turned) {
     const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
-    const uint4 b = *reinterpret_cast<const uint4*>(bytes + lane * kC);
-    const uint64_t f01 = pack2(act8_inverse(b.x), act8_inverse(b.y)), f23 = pack2(act8_inverse(b.z), act8_inverse(b.w));
-    const bool huge = __any_sync(0xFFFFFFFFu, b.x == 247u || b.y == 247u || b.z == 247u || b.w == 247u);
-    float x[kR][kC];
+    const float4 f = *reinterpret_cast<const float4*>(inverses + lane * kC);
+    const uint64_t f01 = pack2(f.x, f.y), f23 = pack2(f.z, f.w);
+    Four x[kR];
 #pragma unroll
-    for (uint32_t r = 0; r < kR; ++r) {
-        unpack2(mul2(pack2(v[r][0], v[r][1]), f01), x[r][0], x[r][1]);
-        unpack2(mul2(pack2(v[r][2], v[r][3]), f23), x[r][2], x[r][3]);
-    }
+    for (uint32_t r = 0; r < kR; ++r) x[r] = v[r].times(f01, f23);
     uint8_t* to = turned + ((warp ^ (lane & 15u)) << 3) + lane * (kC * 128u);
 #pragma unroll
     for (uint32_t c = 0; c < kC; ++c) {
-        uint2 q = make_uint2(act8_codes4(x[0][c], x[1][c], x[2][c], x[3][c]), act8_codes4(x[4][c], x[5][c], x[6][c], x[7][c]));
+        uint2 q = make_uint2(act8_codes4(x[0].at(c), x[1].at(c), x[2].at(c), x[3].at(c)), act8_codes4(x[4].at(c), x[5].at(c), x[6].at(c), x[7].at(c)));
         if (huge) {
-            const uint32_t byte = c == 0 ? b.x : c == 1 ? b.y : c == 2 ? b.z : b.w;
+            const uint32_t byte = inverses[lane * kC + c] == 0x1p-120f ? 247u : 0u;
             q = make_uint2(act8_finite4(q.x, byte), act8_finite4(q.y, byte));
         }
         *reinterpret_cast<uint2*>(to + c * 128u) = q;
@@ -213,8 +211,8 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
     using Shape = TileShape<S>;
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t arrived[2];
-    __shared__ alignas(16) uint32_t bytes[S::kPlanes][128];
-    __shared__ uint32_t stop;
+    __shared__ alignas(16) float inverses[S::kPlanes][128];
+    __shared__ uint32_t stop, huge[S::kPlanes][4];          // huge: whether a column of a warp's 32 has the largest power there is
     uint8_t* stages = raw + ((128u - (smem_addr(raw) & 127u)) & 127u);
     const bool copied = S::kHeld != 0 || !task.direct;
     float* largest = reinterpret_cast<float*>(stages + (copied ? 2 : 1) * Shape::kStageBytes);       // [plane][warp][column]
@@ -269,13 +267,13 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
                 for (uint32_t n = 0; more && n < task.limit && !mbar_try_wait(&arrived[s ^ 1u], phase ^ s); ++n) {}
             }
         }
-        float v[S::kPlanes][kR][kC];
+        Four v[S::kPlanes][kR];
         S::load(v, stage, power);
         if (!ok) {
 #pragma unroll
             for (uint32_t p = 0; p < S::kPlanes; ++p)
 #pragma unroll
-                for (uint32_t r = 0; r < kR; ++r) v[p][r][0] = v[p][r][1] = v[p][r][2] = v[p][r][3] = __uint_as_float(0x7FC00000u);
+                for (uint32_t r = 0; r < kR; ++r) v[p][r].lo = v[p][r].hi = 0x7FC000007FC00000ull;
         }
         const bool whole = (tile_r + 1) * 128u <= task.rows && (tile_c + 1) * 128u <= task.cols;
         bool any_turned = false;
@@ -302,7 +300,10 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
 #pragma unroll
                     for (uint32_t w = 0; w < kWarps; w += 2) m = largest3(m, largest[(p * kWarps + w) * 128u + c], largest[(p * kWarps + w + 1) * 128u + c]);
                     const uint32_t byte = act8_byte(magnitude(m));
-                    bytes[p][c] = byte;
+                    inverses[p][c] = act8_inverse(byte);
+                    if (lane == 0) huge[p][c >> 5] = 0;
+                    __syncwarp();
+                    if (byte == 247u) huge[p][c >> 5] = 1;
                     if (whole || tile_c * 128u + c < task.cols)
                         out.scales[act8_scale_tile(task.tiles_c, tile_c, tile_r) + act8_scale_row(c)] = static_cast<uint8_t>(byte);
                 }
@@ -310,7 +311,7 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
             __syncthreads();
 #pragma unroll
             for (uint32_t p = 0; p < S::kPlanes; ++p)
-                if (task.turned[p].codes) turn_columns(v[p], bytes[p], stage + p * kTurnedBytes);
+                if (task.turned[p].codes) turn_columns(v[p], inverses[p], (huge[p][0] | huge[p][1] | huge[p][2] | huge[p][3]) != 0, stage + p * kTurnedBytes);
             __syncthreads();
 #pragma unroll
             for (uint32_t p = 0; p < S::kPlanes; ++p) {
@@ -349,8 +350,8 @@ __global__ void __launch_bounds__(256) act8_unpack_kernel(const Act8 a, T* y, co
     for (uint32_t r = 0; r < kR; ++r) q[r] = row0 + r < a.rows && col < a.cols ? *reinterpret_cast<const uint32_t*>(from + static_cast<size_t>(r) * a.ld) : 0u;
 #pragma unroll
     for (uint32_t r = 0; r < kR; ++r) {
-        float v[kC];
-        four(v, q[r], __shfl_sync(0xFFFFFFFFu, power, r));
+        const Four held = four(q[r], __shfl_sync(0xFFFFFFFFu, power, r));
+        const float v[kC] = {held.at(0), held.at(1), held.at(2), held.at(3)};
         if (row0 + r >= a.rows) break;
         T* to = y + static_cast<size_t>(row0 + r) * ld_y + col0;
         if (aligned && col0 + 128 <= a.cols) {

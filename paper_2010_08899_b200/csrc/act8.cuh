@@ -109,10 +109,12 @@ __device__ __forceinline__ float reciprocal_fast(float x) {           // within 
 struct Gate2 {
     uint64_t value, slope;
 };
-template <bool kSlope, bool kGelu> __device__ __forceinline__ Gate2 gate2(float g0, float g1) {
+template <bool kSlope, bool kGelu> __device__ __forceinline__ Gate2 gate2(uint64_t g) {
     constexpr float kA = 1.5957691216057308f, kB = 0.044715f, kLeast = 0x1p-126f;
+    float g0, g1;
+    unpack2(g, g0, g1);
     float y0 = g0, y1 = g1;
-    const uint64_t g = pack2(g0, g1), one = pack2(1.0f, 1.0f), minus = pack2(-1.0f, -1.0f);
+    const uint64_t one = pack2(1.0f, 1.0f), minus = pack2(-1.0f, -1.0f);
     uint64_t dy = one;
     if constexpr (kGelu) {
         // (beyond 100 the share is 0 or 1, and g^3 stays a number)

@@ -24,6 +24,9 @@ constexpr uint32_t kTileBytes = 128 * kDepth;
 constexpr uint32_t kScaleBuffers = 8;            // of tensor memory, each for one load of scale tiles
 constexpr uint32_t kMaxSplit = 8;
 constexpr uint32_t kLost = 0x7FC00000u;
+// Sums that end in fp32 leave the tensor cores every 4096 of depth and are added up in registers: the tensor cores cut what does not fit an
+// accumulator, and that error grows with the depth in one sum (2-norm over 16384 of depth: 1.5e-6 in one, 3.8e-7 in four; 8192 x 4096 x 16384: 393 and 409 us).
+constexpr uint32_t kSumDepths = 32;
 
 constexpr uint32_t power_of_two(uint32_t n) { return n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
 
@@ -68,6 +71,7 @@ struct alignas(64) Task {
     uint32_t p_rows, q_rows;        // of P and Q
     uint32_t tiles_p, tiles_q;
     uint32_t split;
+    uint32_t sum;                   // stages to a sum (the pieces of a depth in one accumulator)
     uint32_t limit;                 // of a bounded wait
     void* c;
     uint32_t ld_c;
@@ -350,24 +354,36 @@ template <typename S> struct Shared {
 template <bool kGelu, uint32_t kN> __device__ __forceinline__ void gate_times(float* h, const float* g, const float* u) {
 #pragma unroll
     for (uint32_t j = 0; j < kN; j += 2) {
-        const Gate2 a = gate2<false, kGelu>(g[j], g[j + 1]);
+        const Gate2 a = gate2<false, kGelu>(pack2(g[j], g[j + 1]));
         unpack2(mul2(a.value, pack2(u[j], u[j + 1])), h[j], h[j + 1]);
     }
 }
 
-// A warp's 32 rows and kN columns of the accumulator, read at once so that the next tile's products may begin
-template <uint32_t kN, typename Read>
-__device__ __forceinline__ void finish_wide(const Task& task, uint32_t from, uint32_t row0, uint32_t col0, float* turn, bool ok, const Read& accumulator_read) {
-    const uint32_t group = threadIdx.x >> 7;
-    float v[kN];
-    tmem_load<kN>(v, from + group * kN);
+// A warp's 32 rows and kN columns of the accumulator, piece by piece; each is read at once, so that the next products may begin.
+// arrived(): the piece is there; read(): it has been read.
+template <uint32_t kN, typename Arrived, typename Read>
+__device__ __forceinline__ bool add_up(float (&v)[kN], uint32_t from, uint32_t pieces, const Arrived& arrived, const Read& read) {
+    bool ok = arrived();
+    tmem_load<kN>(v, from);
     tmem_loaded<kN>(v);
-    accumulator_read();
+    read();
+    for (uint32_t p = 1; p < pieces; ++p) {
+        ok = arrived();
+#pragma unroll
+        for (uint32_t j = 0; j < kN; j += 16) {
+            float x[16];
+            tmem_load<16>(x, from + j);
+            tmem_loaded<16>(x);
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) v[j + i] = __fadd_rn(v[j + i], x[i]);
+        }
+        read();
+    }
     if (!ok) {
 #pragma unroll
         for (uint32_t j = 0; j < kN; ++j) v[j] = __uint_as_float(kLost);
     }
-    put_dense<kN>(task, row0, task.p_rows, v, col0, task.q_rows, turn);
+    return ok;
 }
 // The same of a gated tile: 64 columns' g and u, columns 128 .. of the accumulator being up's.  The largest of the other 64 columns of the block
 // comes from the other warp group, through `shared`.
@@ -472,7 +488,7 @@ __device__ __forceinline__ void finish_few_gated(const Task& task, Shared<S>& sh
         // (beyond the last column the powers are anything: what stands there is no number)
         g = there ? few_sum<S>(from + j * 128u, split, slice) : 0.0f;
         u = there ? few_sum<S>(from + (slice + j) * 128u, split, slice) : 0.0f;
-        const Gate2 a = task.gelu ? gate2<false, true>(g, g) : gate2<false, false>(g, g);
+        const Gate2 a = task.gelu ? gate2<false, true>(pack2(g, g)) : gate2<false, false>(pack2(g, g));
         float other;
         unpack2(mul2(a.value, pack2(u, u)), h, other);
     };
@@ -610,10 +626,16 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
         uint32_t stage = 0, phase = 0, free_phase = 1, buffer = 0;
         bool ok = true;
         for (uint32_t t = tile0; ok && t < tile_count; t += step) {
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sh.free, free_phase, task.limit, stop));
-            free_phase ^= 1u;
-            tmem_after_sync();
+            uint32_t left = 0;             // stages of the present sum
             for (uint32_t it = begin; ok && it < end; ++it) {
+                const bool fresh = left == 0;
+                if (fresh) {
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sh.free, free_phase, task.limit, stop));
+                    if (!ok) break;
+                    free_phase ^= 1u;
+                    left = min(task.sum, end - it);
+                }
+                --left;
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sh.full[stage], phase, task.limit, stop));
                 if (!ok) break;
                 tmem_after_sync();
@@ -633,9 +655,9 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
 #pragma unroll
                         for (uint32_t i = 0; i < S::kAcc; ++i)
                             block_scaled_product(tmem + i * S::kQ, p + i * (kTileBytes >> 4) + 2 * k, q + 2 * k, idesc, sf + 4 * i, sf + 4 * S::kAcc,
-                                                 it != begin || k != 0);
+                                                 !fresh || k != 0);
                     tensor_commit(&sh.empty[stage]);
-                    if (it + 1 == end) tensor_commit(&sh.done);
+                    if (left == 0) tensor_commit(&sh.done);
                 }
                 __syncwarp();
                 if (++stage == S::kStages) stage = 0, phase ^= 1u;
@@ -649,16 +671,21 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
     } else {
         const uint32_t group = warp >> 2, row_lane = (warp & 3u) * 32u + lane, lanes = tmem + ((warp & 3u) << 21);
         float* turn = S::kFew ? nullptr : turns + warp * (32 * 17);
+        const uint32_t pieces = ceil_div(end - begin, task.sum);
         uint32_t done_phase = 0;
         bool ok = true;
         for (uint32_t t = tile0; t < tile_count; t += step) {
             const Tile at = tile_at(task, t);
-            if (ok && !mbar_wait_bounded(&sh.done, done_phase, task.limit, stop)) {
-                ok = false;
-                give_up();
-            }
-            done_phase ^= 1u;
-            tmem_after_sync();
+            const auto arrived = [&] {
+                if (ok && !mbar_wait_bounded(&sh.done, done_phase, task.limit, stop)) {
+                    ok = false;
+                    give_up();
+                }
+                done_phase ^= 1u;
+                tmem_after_sync();
+                return ok;
+            };
+            if (S::kFew) arrived();
             const uint32_t p0 = at.p * 128u, q0 = at.q * S::kQ;
             const auto accumulator_read = [&] {
                 tmem_before_sync();
@@ -671,12 +698,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                 cluster_wait();
                 if constexpr (!S::kFew) {
                     float v[S::kQ / 2];
-                    tmem_load<S::kQ / 2>(v, lanes + group * (S::kQ / 2));
-                    tmem_loaded<S::kQ / 2>(v);
-                    if (!ok) {
-#pragma unroll
-                        for (uint32_t j = 0; j < S::kQ / 2; ++j) v[j] = __uint_as_float(kLost);
-                    }
+                    add_up(v, lanes + group * (S::kQ / 2), pieces, arrived, accumulator_read);
 #pragma unroll
                     for (uint32_t j = 0; j < S::kQ / 2; j += 4) {
                         const uint32_t col = group * (S::kQ / 2) + j;
@@ -718,7 +740,9 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                 else
                     finish_few<S>(task, from, 1, S::kQ, q0 + group * (S::kQ / 2), S::kQ / 2, p0 + row_lane);
             } else {
-                finish_wide<S::kQ / 2>(task, lanes, p0 + (warp & 3u) * 32u, q0 + group * (S::kQ / 2), turn, ok, accumulator_read);
+                float v[S::kQ / 2];
+                add_up(v, lanes + group * (S::kQ / 2), pieces, arrived, accumulator_read);
+                put_dense<S::kQ / 2>(task, p0 + (warp & 3u) * 32u, task.p_rows, v, q0 + group * (S::kQ / 2), task.q_rows, turn);
             }
         }
     }
@@ -848,10 +872,16 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
             uint32_t stage = 0, phase = 0, free_phase = 1, buffer = 0;
             bool ok = true;
             for (uint32_t t = tile0; ok && t < tile_count; t += step) {
-                ok = __all_sync(0xFFFFFFFFu, wait_for_cluster(&free_again, free_phase, task.limit, stop));
-                free_phase ^= 1u;
-                tmem_after_sync();
+                uint32_t left = 0;             // stages of the present sum
                 for (uint32_t it = 0; ok && it < depth; ++it) {
+                    const bool fresh = left == 0;
+                    if (fresh) {
+                        ok = __all_sync(0xFFFFFFFFu, wait_for_cluster(&free_again, free_phase, task.limit, stop));
+                        if (!ok) break;
+                        free_phase ^= 1u;
+                        left = min(task.sum, depth - it);
+                    }
+                    --left;
                     ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&full[stage], phase, task.limit, stop));
                     if (!ok) break;
                     tmem_after_sync();
@@ -866,9 +896,9 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
                             for (uint32_t i = 0; i < S::kScaleTiles; ++i) pair_scales_to_tmem(sf + 4 * i, from + i * (kAct8ScaleTile >> 4));
                         }
 #pragma unroll
-                        for (uint32_t k = 0; k < 4; ++k) pair_product(tmem, p + 2 * k, q + 2 * k, idesc, sf, sf + 4, it != 0 || k != 0);
+                        for (uint32_t k = 0; k < 4; ++k) pair_product(tmem, p + 2 * k, q + 2 * k, idesc, sf, sf + 4, !fresh || k != 0);
                         pair_commit(&empty[stage]);
-                        if (it + 1 == depth) pair_commit(&done);
+                        if (left == 0) pair_commit(&done);
                     }
                     __syncwarp();
                     if (++stage == S::kStages) stage = 0, phase ^= 1u;
@@ -882,27 +912,35 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
         }
     } else {
         const uint32_t group = warp >> 2, lanes = tmem + ((warp & 3u) << 21), free_bar = peer_address(smem_addr(&free_again), 0);
+        const uint32_t pieces = ceil_div(depth, task.sum);
         float* turn = turns + warp * (32 * 17);
         uint32_t done_phase = 0;
         bool ok = true;
         for (uint32_t t = tile0; t < tile_count; t += step) {
             const Tile at = tile_at(task, t);
-            if (ok && !mbar_wait_bounded(&done, done_phase, task.limit, stop)) {
-                ok = false;
-                give_up();
-            }
-            done_phase ^= 1u;
-            tmem_after_sync();
+            const auto arrived = [&] {
+                if (ok && !mbar_wait_bounded(&done, done_phase, task.limit, stop)) {
+                    ok = false;
+                    give_up();
+                }
+                done_phase ^= 1u;
+                tmem_after_sync();
+                return ok;
+            };
             const uint32_t row0 = at.p * 256u + rank * 128u + (warp & 3u) * 32u;
             const auto accumulator_read = [&] {
                 tmem_before_sync();
                 __syncwarp();
                 if (lane == 0) arrive_at(free_bar);
             };
-            if constexpr (kGated)
+            if constexpr (kGated) {
+                arrived();
                 finish_wide_gated(task, lanes, row0, at.q, largest, turn, ok, accumulator_read);
-            else
-                finish_wide<128>(task, lanes, row0, at.q * 256u + group * 128u, turn, ok, accumulator_read);
+            } else {
+                float v[128];
+                add_up(v, lanes + group * 128u, pieces, arrived, accumulator_read);
+                put_dense<128>(task, row0, task.p_rows, v, at.q * 256u + group * 128u, task.q_rows, turn);
+            }
         }
     }
     __syncwarp();
@@ -993,6 +1031,7 @@ dct_status_t product(const dct_act8_t* const (&a)[2], const dct_act8_t* const (&
     task.ld_c = ld_c;
     task.bf16 = dtype == DCT_BF16;
     task.accumulate = accumulate;
+    task.sum = dtype == DCT_F32 && m > 64 ? kSumDepths : 0xFFFFFFFFu;
     task.aligned = aligned_to(c, 32) && static_cast<size_t>(ld_c) * element_size(dtype) % 32 == 0;
     // Up to 64 rows: the columns take the lanes.  Else single CTAs with tiles of 128 x 128, as long as all run at once; a pair's stage brings four times the
     // products for twice the codes and takes about as long (2048 x 4096 x 4096: 29 us in pairs, 45 by single CTAs).
@@ -1030,6 +1069,7 @@ dct_status_t gated(const dct_act8_t* x, const dct_act8_t* w_gate, const dct_act8
     task.bf16 = dtype == DCT_BF16;
     task.aligned = aligned_to(h_dense, 32) && static_cast<size_t>(ld_h) * element_size(dtype) % 32 == 0;
     task.gelu = gelu;
+    task.sum = 0xFFFFFFFFu;
     task.h = device_view(h);
     task.gate = device_view(gate);
     task.up = device_view(up);
