@@ -263,8 +263,8 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
             ok = false;
             *const_cast<volatile uint32_t*>(&stop) = 1u;
             if (threadIdx.x == 0) {             // what is still on its way lands before anything else happens here
-                for (uint32_t n = 0; n < task.limit && !mbar_try_wait(&arrived[s], phase); ++n) {}
-                for (uint32_t n = 0; more && n < task.limit && !mbar_try_wait(&arrived[s ^ 1u], phase ^ s); ++n) {}
+                for (uint32_t n = 0; n < (1u << 21) && !mbar_try_wait(&arrived[s], phase); ++n) {}
+                for (uint32_t n = 0; more && n < (1u << 21) && !mbar_try_wait(&arrived[s ^ 1u], phase ^ s); ++n) {}
             }
         }
         Four v[S::kPlanes][kR];

@@ -184,6 +184,11 @@ __device__ __forceinline__ void arrive_at(uint32_t bar) {               // a bar
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// The last wait of a CTA, for what the hardware still does for it.  Its limit is its own: far longer than any copy or product takes.
+__device__ __forceinline__ void wait_landed(uint64_t* bar, uint32_t parity) {
+    for (uint32_t k = 0; k < (1u << 21) && !mbar_try_wait(bar, parity); ++k) {}
+}
+
 // Descriptors of shared memory.  Tiles: rows of 128 bytes, swizzled by 128 bytes, groups of eight rows 1024 bytes apart; 32 of depth further is 32 bytes
 // further.  Scale tiles: not swizzled, groups of eight rows (of 16 bytes) 128 bytes apart.
 __device__ __forceinline__ uint64_t tile_desc(const void* smem) {
@@ -615,12 +620,8 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                     if (++stage == S::kStages) stage = 0, phase ^= 1u;
                 }
             }
-            if (!ok) {             // what is in flight lands before the CTA ends
-                for (uint32_t i = min(issued, S::kStages); i > 0; --i) {
-                    const uint32_t n = issued - i;
-                    for (uint32_t k = 0; k < task.limit && !mbar_try_wait(&sh.full[n % S::kStages], (n / S::kStages) & 1u); ++k) {}
-                }
-            }
+            // What was asked for lands before the CTA ends.  (As a rule it has: it was multiplied.  If a wait anywhere gave up, it need not.)
+            for (uint32_t i = min(issued, S::kStages); i > 0; --i) wait_landed(&sh.full[(issued - i) % S::kStages], (issued - i) / S::kStages & 1u);
         }
     } else if (warp == kProductWarp) {
         uint32_t stage = 0, phase = 0, free_phase = 1, buffer = 0;
@@ -663,11 +664,12 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                 if (++stage == S::kStages) stage = 0, phase ^= 1u;
             }
         }
-        if (!ok && elected()) {
-            give_up();
+        if (elected()) {             // the same of products
+            if (!ok) give_up();
             tensor_commit(&sh.drained);
-            for (uint32_t k = 0; k < task.limit && !mbar_try_wait(&sh.drained, 0); ++k) {}
+            wait_landed(&sh.drained, 0);
         }
+        __syncwarp();
     } else {
         const uint32_t group = warp >> 2, row_lane = (warp & 3u) * 32u + lane, lanes = tmem + ((warp & 3u) << 21);
         float* turn = S::kFew ? nullptr : turns + warp * (32 * 17);
@@ -677,7 +679,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
         for (uint32_t t = tile0; t < tile_count; t += step) {
             const Tile at = tile_at(task, t);
             const auto arrived = [&] {
-                if (ok && !mbar_wait_bounded(&sh.done, done_phase, task.limit, stop)) {
+                if (ok && !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sh.done, done_phase, task.limit, stop))) {
                     ok = false;
                     give_up();
                 }
@@ -687,10 +689,11 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
             };
             if (S::kFew) arrived();
             const uint32_t p0 = at.p * 128u, q0 = at.q * S::kQ;
+            // (a warp that gave up lets nothing be overwritten any more: others may still be reading)
             const auto accumulator_read = [&] {
                 tmem_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.free);
+                if (lane == 0 && ok) mbar_arrive(&sh.free);
             };
             if (split > 1) {
                 // this part's columns to the CTAs that add them up
@@ -860,11 +863,12 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
                     if (++stage == S::kStages) stage = 0, phase ^= 1u;
                 }
             }
-            if (!ok && rank == 0) {             // what is in flight lands before the CTAs end (they meet once more)
-                for (uint32_t i = min(issued, S::kStages); i > 0; --i) {
-                    const uint32_t n = issued - i;
-                    for (uint32_t k = 0; k < task.limit && !mbar_try_wait(&full[n % S::kStages], (n / S::kStages) & 1u); ++k) {}
-                }
+            // What was asked for lands before the CTAs end, who meet once more.  (As a rule it has: it was multiplied.)  The barriers are the even CTA's; if the
+            // odd one gave up, the even one may not have counted its last copies, and it gives them time.
+            if (rank == 0) {
+                for (uint32_t i = min(issued, S::kStages); i > 0; --i) wait_landed(&full[(issued - i) % S::kStages], (issued - i) / S::kStages & 1u);
+            } else if (!ok) {
+                for (uint32_t i = 0; i < 1000; ++i) __nanosleep(1000);
             }
         }
     } else if (warp == kProductWarp) {
@@ -904,11 +908,12 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
                     if (++stage == S::kStages) stage = 0, phase ^= 1u;
                 }
             }
-            if (!ok && elected()) {
-                give_up();
+            if (elected()) {             // the same of products
+                if (!ok) give_up();
                 pair_commit(&drained);
-                for (uint32_t k = 0; k < task.limit && !mbar_try_wait(&drained, 0); ++k) {}
+                wait_landed(&drained, 0);
             }
+            __syncwarp();
         }
     } else {
         const uint32_t group = warp >> 2, lanes = tmem + ((warp & 3u) << 21), free_bar = peer_address(smem_addr(&free_again), 0);
@@ -919,7 +924,7 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
         for (uint32_t t = tile0; t < tile_count; t += step) {
             const Tile at = tile_at(task, t);
             const auto arrived = [&] {
-                if (ok && !mbar_wait_bounded(&done, done_phase, task.limit, stop)) {
+                if (ok && !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&done, done_phase, task.limit, stop))) {
                     ok = false;
                     give_up();
                 }
@@ -931,7 +936,7 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
             const auto accumulator_read = [&] {
                 tmem_before_sync();
                 __syncwarp();
-                if (lane == 0) arrive_at(free_bar);
+                if (lane == 0 && ok) arrive_at(free_bar);          // (a warp that gave up lets nothing be overwritten any more)
             };
             if constexpr (kGated) {
                 arrived();

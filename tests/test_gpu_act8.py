@@ -487,3 +487,110 @@ def test_rows_whose_offset_passes_32_bits():
     B.dct_gemm8(small, w, e, 96)
     assert not c[:-last].any()
     assert bool(((c[-last:] - e).abs() <= 1e-4 * e.abs().amax()).all())
+
+
+# ---- waits that run out, several threads, a first call inside a capture ----
+
+def test_waits_that_run_out_lose_values_and_nothing_else():
+    """With a limit of one look at a barrier most waits give up: what is written is then right or NaN, every call ends, and the next one (with
+    the usual limit) is right."""
+    x, w = rows_of(300, 700, torch.bfloat16, 1), rows_of(400, 700, torch.float32, 2)
+    dh = rows_of(300, 400, torch.bfloat16, 3)
+    big = rows_of(4000, 300, torch.bfloat16, 4)
+
+    def calls():
+        out = {}
+        a, t, b = B.new_act8(300, 700), B.new_act8(700, 300), B.new_act8(400, 700)
+        B.dct_act8_pack(x, 300, 700, 700, a, t)
+        B.dct_act8_pack(w, 400, 700, 700, b)
+        g = put(matrix(4000, 300, 5))
+        turned = B.new_act8(300, 4000)
+        B.dct_act8_transpose(g, turned)
+        few, mid, pairs = (torch.empty(*size, device=DEV) for size in ((9, 400), (300, 400), (4000, 2600)))
+        p, q = put(matrix(300, 700, 6)), put(matrix(400, 700, 7))
+        B.dct_gemm8(put(matrix(9, 700, 8)), q, few, 400)
+        B.dct_gemm8(p, q, mid, 400)
+        B.dct_gemm8(g, put(matrix(2600, 300, 9)), pairs, 2600)
+        wide, narrow = torch.empty(300, 400, device=DEV), torch.empty(9, 400, device=DEV)
+        B.dct_gated8_fwd(p, q, put(matrix(400, 700, 10)), B.DCT_ACT_SILU, None, wide, 400)
+        B.dct_gated8_fwd(put(matrix(9, 700, 8)), q, put(matrix(400, 700, 10)), B.DCT_ACT_SILU, None, narrow, 400)
+        dg = B.new_act8(400, 300)
+        kept = put(matrix(300, 400, 11))
+        B.dct_gated8_bwd(dh, 400, kept, kept, B.DCT_ACT_SILU, dgate_t=dg)
+        for name, m in (("a", a), ("t", t), ("turned", turned), ("dg", dg)):
+            out[name] = torch.empty(m.rows, m.cols, device=DEV)
+            B.dct_act8_unpack(m, out[name], m.cols)
+        out.update(few=few, mid=mid, pairs=pairs, wide=wide, narrow=narrow)
+        torch.cuda.synchronize()
+        return out
+
+    want = calls()
+    try:
+        B.dct_debug_configure(1, 0)
+        for _ in range(3):
+            got = calls()
+            for name, v in got.items():
+                assert bool((torch.isnan(v) | (v == want[name])).all()), name
+    finally:
+        B.dct_debug_configure()
+    for name, v in calls().items():
+        assert torch.equal(v, want[name]), name
+
+
+def test_several_threads_call_at_once():
+    import threading
+    a, b = matrix(200, 600, 1), matrix(300, 600, 2)
+    pa, pb = put(a), put(b)
+    want = torch.empty(200, 300, device=DEV)
+    B.dct_gemm8(pa, pb, want, 300)
+    torch.cuda.synchronize()
+    out, errors = [torch.empty_like(want) for _ in range(4)], []
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            for _ in range(50):
+                out[i].fill_(-1.0)
+                stream.wait_stream(torch.cuda.current_stream())
+                B.dct_gemm8(pa, pb, out[i], 300, stream=stream)
+                stream.synchronize()
+                if not torch.equal(out[i], want):
+                    errors.append(i)
+        except Exception as e:           # (an exception in a thread would only be printed)
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2010_08899_b200 import binding as B
+x = torch.randn(70, 256, device="cuda").bfloat16()
+a, t, c, h = B.new_act8(70, 256), B.new_act8(256, 70), torch.empty(70, 70, device="cuda"), torch.empty(70, 70, device="cuda")
+few, f = B.new_act8(5, 256), torch.empty(5, 70, device="cuda")
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    B.dct_act8_pack(x, 70, 256, 256, a, t)
+    B.dct_act8_pack(x, 5, 256, 256, few)
+    B.dct_gemm8(a, a, c, 70)
+    B.dct_gemm8(few, a, f, 70)
+    B.dct_gated8_fwd(a, a, a, B.DCT_ACT_SILU, None, h, 70)
+graph.replay()
+torch.cuda.synchronize()
+y = torch.empty(70, 256, device="cuda")
+B.dct_act8_unpack(a, y, 256)
+want = (y.double() @ y.double().T)
+assert (c.double() - want).abs().max() <= 1e-4 * want.abs().max()
+assert torch.equal(f, c[:5]) or (f - c[:5]).abs().max() <= 1e-4 * want.abs().max()
+assert torch.isfinite(h).all()
+"""
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
