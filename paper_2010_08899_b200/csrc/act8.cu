@@ -2,7 +2,7 @@
 // block, which reads two of them and writes up to five.
 //
 // All but the reading back work on tiles of 128 x 128 elements, so that both a row's block and, in the transpose, a column's block are the tile's
-// own.  A CTA goes from tile to tile; tensor copies bring the next tile's inputs into shared memory while this one is worked on.  A warp has eight
+// own.  A CTA goes from tile to tile; tensor copies bring the next tiles' inputs into shared memory while this one is worked on.  A warp has eight
 // rows of the tile, a lane four columns of them: a row's largest magnitude is one reduction over the warp, a column's goes through shared
 // memory, and a lane's codes of a column lie next to each other in the transpose, which leaves shared memory as rows of 128 bytes.
 #include "act8.cuh"
@@ -116,6 +116,11 @@ template <typename S> struct TileShape {
     static constexpr uint32_t kStageBytes = S::kDenseBytes + S::kHeld * 128 * 128;
     static constexpr uint32_t kLargestBytes = S::kPlanes * kWarps * 128 * 4;
     static constexpr uint32_t shared_bytes(uint32_t stages) { return 128 + stages * kStageBytes + kLargestBytes; }
+    // Two stages: a tile's copies are asked for when the one before it begins, and a barrier ends each tile.  Three: two tiles ahead, after a tile's
+    // first barrier, and warps go on to the next tile without one.  The transpose alone gains (16384 x 4096: 37.4 -> 35.0 us); the others' tiles are
+    // larger, and the gated ones have no registers for a second place (8192 x 8192: 187 us with two, 221 with three).
+    static constexpr uint32_t kStages = S::kDenseBytes == 0 ? 3 : 2;
+    static constexpr bool kDeep = kStages == 3;
     static_assert(kStageBytes >= S::kPlanes * kTurnedBytes, "the transposed codes take the place of a tile's inputs");
 };
 
@@ -210,17 +215,16 @@ template <typename S>
 __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const __grid_constant__ TileTask task) {
     using Shape = TileShape<S>;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t arrived[2];
+    __shared__ uint64_t arrived[Shape::kStages];
     __shared__ alignas(16) float inverses[S::kPlanes][128];
     __shared__ uint32_t stop, huge[S::kPlanes][4];          // huge: whether a column of a warp's 32 has the largest power there is
     uint8_t* stages = raw + ((128u - (smem_addr(raw) & 127u)) & 127u);
     const bool copied = S::kHeld != 0 || !task.direct;
-    float* largest = reinterpret_cast<float*>(stages + (copied ? 2 : 1) * Shape::kStageBytes);       // [plane][warp][column]
+    float* largest = reinterpret_cast<float*>(stages + (copied ? Shape::kStages : 1) * Shape::kStageBytes);       // [plane][warp][column]
     const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
     chain_release_next();
     if (threadIdx.x == 0) {
-        mbar_init(&arrived[0], 1);
-        mbar_init(&arrived[1], 1);
+        for (uint32_t i = 0; i < Shape::kStages; ++i) mbar_init(&arrived[i], 1);
         stop = 0;
         mbar_init_fence();
     }
@@ -242,18 +246,29 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
         if constexpr (S::kHeld >= 2) byte1 = there ? task.held[1].scales[act8_scale_tile(task.tiles_r, tile_r, tile_c) + act8_scale_row(in)] : 0u;
     };
     const uint32_t step_r = gridDim.x / task.tiles_c, step_c = gridDim.x % task.tiles_c;
+    const auto advance = [&](uint32_t& r, uint32_t& c) {
+        r += step_r;
+        c += step_c;
+        if (c >= task.tiles_c) c -= task.tiles_c, ++r;
+    };
     uint32_t tile_r = blockIdx.x / task.tiles_c, tile_c = blockIdx.x % task.tiles_c;          // (there are at least as many tiles as CTAs)
+    uint32_t ahead_r = tile_r, ahead_c = tile_c;                                              // deep: the next tile to ask for
     chain_wait_previous();
     if (threadIdx.x == 0 && copied) fetch(tile_r, tile_c, 0);
+    if constexpr (Shape::kDeep) {
+        advance(ahead_r, ahead_c);
+        if (threadIdx.x == 0 && copied && ahead_r < task.tiles_r) fetch(ahead_r, ahead_c, 1);
+        advance(ahead_r, ahead_c);
+    }
     ask_bytes(tile_r, tile_c);
     __syncthreads();
     uint32_t s = 0, phase = 0;
     bool ok = true;
     while (tile_r < task.tiles_r) {
-        uint32_t next_r = tile_r + step_r, next_c = tile_c + step_c;
-        if (next_c >= task.tiles_c) next_c -= task.tiles_c, ++next_r;
+        uint32_t next_r = tile_r, next_c = tile_c;
+        advance(next_r, next_c);
         const bool more = next_r < task.tiles_r;
-        if (threadIdx.x == 0 && copied && ok && more) fetch(next_r, next_c, s ^ 1u);
+        if (!Shape::kDeep && threadIdx.x == 0 && copied && ok && more) fetch(next_r, next_c, s ^ 1u);
         uint8_t* stage = stages + s * Shape::kStageBytes;
         const float power[2] = {act8_power(byte0), act8_power(byte1)};       // asked for a tile ago
         if (more) ask_bytes(next_r, next_c);
@@ -262,9 +277,10 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
         if (copied && ok && !mbar_wait_bounded(&arrived[s], phase, task.limit, &stop)) {
             ok = false;
             *const_cast<volatile uint32_t*>(&stop) = 1u;
-            if (threadIdx.x == 0) {             // what is still on its way lands before anything else happens here
+            if (threadIdx.x == 0) {             // what is still on its way, this tile's and the next one's, lands before anything else happens here
                 for (uint32_t n = 0; n < (1u << 21) && !mbar_try_wait(&arrived[s], phase); ++n) {}
-                for (uint32_t n = 0; more && n < (1u << 21) && !mbar_try_wait(&arrived[s ^ 1u], phase ^ s); ++n) {}
+                const uint32_t then = s + 1 == Shape::kStages ? 0u : s + 1;
+                for (uint32_t n = 0; more && n < (1u << 21) && !mbar_try_wait(&arrived[then], phase ^ (then == 0)); ++n) {}
             }
         }
         Four v[S::kPlanes][kR];
@@ -290,7 +306,12 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
                 note_columns(v[p], largest + p * (kWarps * 128));
             }
         }
+        if (Shape::kDeep) fence_proxy_async_smem();            // what this thread did in the last tile's stage comes before the copies into it
         __syncthreads();
+        if constexpr (Shape::kDeep) {
+            if (threadIdx.x == 0 && copied && ok && ahead_r < task.tiles_r) fetch(ahead_r, ahead_c, s == 0 ? Shape::kStages - 1 : s - 1);
+            advance(ahead_r, ahead_c);
+        }
         if (any_turned) {
             if (threadIdx.x < S::kPlanes * 128u) {
                 const uint32_t p = threadIdx.x >> 7, c = threadIdx.x & 127u;
@@ -322,13 +343,14 @@ __global__ void __launch_bounds__(kTileThreads, S::kCtas) act8_tile_kernel(const
                     write_turned<false>(stage + p * kTurnedBytes, task.turned[p], tile_r, tile_c);
             }
         }
-        fence_proxy_async_smem();            // this stage is written by copies again
-        __syncthreads();
+        if constexpr (!Shape::kDeep) {         // (deep: what the next tile writes before its first barrier, nobody reads any more)
+            fence_proxy_async_smem();
+            __syncthreads();
+        }
         tile_r = next_r;
         tile_c = next_c;
         if (!copied) continue;
-        s ^= 1u;
-        if (s == 0) phase ^= 1u;
+        if (++s == Shape::kStages) s = 0, phase ^= 1u;
     }
 }
 
@@ -390,7 +412,7 @@ dct_status_t launch_tiles(TileTask& task, uint32_t rows, uint32_t cols, const vo
     static SharedLimit allowed;
     // (a matrix fetched element by element is not fetched ahead: one stage, and more CTAs to an SM instead)
     const bool ahead = S::kHeld != 0 || unit_rows<T>(x, ld_x);
-    const uint32_t shared = TileShape<S>::shared_bytes(ahead ? 2 : 1);
+    const uint32_t shared = TileShape<S>::shared_bytes(ahead ? TileShape<S>::kStages : 1);
     dct_status_t st = allow_shared(act8_tile_kernel<S>, shared, allowed);
     if (st != DCT_OK) return st;
     const int sms = sm_count();
