@@ -30,6 +30,18 @@ def test_oracle_codes_are_those_of_e4m3():
     assert (largest <= power).all() and ((largest > power / 2) | (o.hold(y).bytes == 0)).all()
 
 
+def test_oracle_activations_against_known_values_and_differences():
+    """SILU is g sigmoid(g); GELU in its tanh form is torch's; the slopes are differences of the values."""
+    g = np.linspace(-9, 9, 721)
+    t = torch.from_numpy(g)
+    assert np.allclose(o.activation(g, False)[0], torch.nn.functional.silu(t).numpy(), rtol=1e-12, atol=1e-15)
+    assert np.allclose(o.activation(g, True)[0], torch.nn.functional.gelu(t, approximate="tanh").numpy(), rtol=1e-9, atol=1e-12)
+    for gelu in (False, True):
+        # a value of up to 9 from four roundings is off by 4 * 9 * 2^-53 = 4e-15, the difference of two by twice that over 2e-6: 4e-9
+        slope = (o.activation(g + 1e-6, gelu)[0] - o.activation(g - 1e-6, gelu)[0]) / 2e-6
+        assert np.allclose(o.activation(g, gelu)[1], slope, rtol=0, atol=4e-9)
+
+
 def test_scale_bytes():
     assert B.dct_act8_scale_bytes(1, 1) == 512 and B.dct_act8_scale_bytes(128, 512) == 512
     assert B.dct_act8_scale_bytes(129, 513) == 4 * 512 and B.dct_act8_scale_bytes(0, 5) == 0 and B.dct_act8_scale_bytes(5, 0) == 0
