@@ -26,7 +26,8 @@ constexpr uint32_t kMaxSplit = 8;
 constexpr uint32_t kLost = 0x7FC00000u;
 // Sums that end in fp32 leave the tensor cores every 4096 of depth and are added up in registers: the tensor cores cut what does not fit an
 // accumulator, and that error grows with the depth in one sum (2-norm over 16384 of depth: 1.5e-6 in one, 3.8e-7 in four; 8192 x 4096 x 16384: 393 and 409 us).
-constexpr uint32_t kSumDepths = 32;
+// What goes into 8 bits does so every 2048: a last digit decides between two codes now and then.
+constexpr uint32_t kSumDepths = 32, kSumDepthsHeld = 16;
 
 constexpr uint32_t power_of_two(uint32_t n) { return n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
 
@@ -364,23 +365,30 @@ template <bool kGelu, uint32_t kN> __device__ __forceinline__ void gate_times(fl
     }
 }
 
-// A warp's 32 rows and kN columns of the accumulator, piece by piece; each is read at once, so that the next products may begin.
-// arrived(): the piece is there; read(): it has been read.
-template <uint32_t kN, typename Arrived, typename Read>
-__device__ __forceinline__ bool add_up(float (&v)[kN], uint32_t from, uint32_t pieces, const Arrived& arrived, const Read& read) {
+// A warp's 32 rows of the accumulator, piece by piece; each is read at once, so that the next products may begin.  kN columns from `from`, to v; with
+// kTwo as many from `from2`, to w.  arrived(): the piece is there; read(): it has been read.
+template <uint32_t kN, bool kTwo, typename Arrived, typename Read>
+__device__ __forceinline__ bool add_up(float (&v)[kN], uint32_t from, float* w, uint32_t from2, uint32_t pieces, const Arrived& arrived, const Read& read) {
     bool ok = arrived();
     tmem_load<kN>(v, from);
+    if constexpr (kTwo) tmem_load<kN>(w, from2);
     tmem_loaded<kN>(v);
+    if constexpr (kTwo) tmem_loaded<kN>(w);
     read();
     for (uint32_t p = 1; p < pieces; ++p) {
         ok = arrived();
 #pragma unroll
-        for (uint32_t j = 0; j < kN; j += 16) {
+        for (uint32_t j = 0; j < (kTwo ? 2 : 1) * kN; j += 16) {
             float x[16];
-            tmem_load<16>(x, from + j);
+            tmem_load<16>(x, j < kN ? from + j : from2 + j - kN);
             tmem_loaded<16>(x);
 #pragma unroll
-            for (uint32_t i = 0; i < 16; ++i) v[j + i] = __fadd_rn(v[j + i], x[i]);
+            for (uint32_t i = 0; i < 16; ++i) {
+                if (j < kN)
+                    v[j + i] = __fadd_rn(v[j + i], x[i]);
+                else
+                    w[j - kN + i] = __fadd_rn(w[j - kN + i], x[i]);
+            }
         }
         read();
     }
@@ -392,16 +400,12 @@ __device__ __forceinline__ bool add_up(float (&v)[kN], uint32_t from, uint32_t p
 }
 // The same of a gated tile: 64 columns' g and u, columns 128 .. of the accumulator being up's.  The largest of the other 64 columns of the block
 // comes from the other warp group, through `shared`.
-template <typename Read>
-__device__ __forceinline__ void finish_wide_gated(const Task& task, uint32_t from, uint32_t row0, uint32_t block, uint32_t* shared, float* turn, bool ok,
-                                                  const Read& accumulator_read) {
+template <typename Arrived, typename Read>
+__device__ __forceinline__ void finish_wide_gated(const Task& task, uint32_t from, uint32_t row0, uint32_t block, uint32_t pieces, uint32_t* shared, float* turn,
+                                                  const Arrived& arrived, const Read& accumulator_read) {
     const uint32_t group = threadIdx.x >> 7, row_lane = threadIdx.x & 127u;
     float g[64], u[64];
-    tmem_load<64>(g, from + group * 64);
-    tmem_load<64>(u, from + 128 + group * 64);
-    tmem_loaded<64>(g);
-    tmem_loaded<64>(u);
-    accumulator_read();
+    const bool ok = add_up<64, true>(g, from + group * 64, u, from + 128 + group * 64, pieces, arrived, accumulator_read);
     const uint32_t row = row0 + lane_id(), col = block * 128u + group * 64u, count = col < task.q_rows ? task.q_rows - col : 0;
     if (!ok || count < 64) {
 #pragma unroll
@@ -701,7 +705,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                 cluster_wait();
                 if constexpr (!S::kFew) {
                     float v[S::kQ / 2];
-                    add_up(v, lanes + group * (S::kQ / 2), pieces, arrived, accumulator_read);
+                    add_up<S::kQ / 2, false>(v, lanes + group * (S::kQ / 2), nullptr, 0, pieces, arrived, accumulator_read);
 #pragma unroll
                     for (uint32_t j = 0; j < S::kQ / 2; j += 4) {
                         const uint32_t col = group * (S::kQ / 2) + j;
@@ -744,7 +748,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                     finish_few<S>(task, from, 1, S::kQ, q0 + group * (S::kQ / 2), S::kQ / 2, p0 + row_lane);
             } else {
                 float v[S::kQ / 2];
-                add_up(v, lanes + group * (S::kQ / 2), pieces, arrived, accumulator_read);
+                add_up<S::kQ / 2, false>(v, lanes + group * (S::kQ / 2), nullptr, 0, pieces, arrived, accumulator_read);
                 put_dense<S::kQ / 2>(task, p0 + (warp & 3u) * 32u, task.p_rows, v, q0 + group * (S::kQ / 2), task.q_rows, turn);
             }
         }
@@ -939,11 +943,10 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
                 if (lane == 0 && ok) arrive_at(free_bar);          // (a warp that gave up lets nothing be overwritten any more)
             };
             if constexpr (kGated) {
-                arrived();
-                finish_wide_gated(task, lanes, row0, at.q, largest, turn, ok, accumulator_read);
+                finish_wide_gated(task, lanes, row0, at.q, pieces, largest, turn, arrived, accumulator_read);
             } else {
                 float v[128];
-                add_up(v, lanes + group * 128u, pieces, arrived, accumulator_read);
+                add_up<128, false>(v, lanes + group * 128u, nullptr, 0, pieces, arrived, accumulator_read);
                 put_dense<128>(task, row0, task.p_rows, v, at.q * 256u + group * 128u, task.q_rows, turn);
             }
         }
@@ -1074,7 +1077,7 @@ dct_status_t gated(const dct_act8_t* x, const dct_act8_t* w_gate, const dct_act8
     task.bf16 = dtype == DCT_BF16;
     task.aligned = aligned_to(h_dense, 32) && static_cast<size_t>(ld_h) * element_size(dtype) % 32 == 0;
     task.gelu = gelu;
-    task.sum = 0xFFFFFFFFu;
+    task.sum = rows > 64 && (h || gate) ? kSumDepthsHeld : 0xFFFFFFFFu;
     task.h = device_view(h);
     task.gate = device_view(gate);
     task.up = device_view(up);
