@@ -155,6 +155,9 @@ __device__ __forceinline__ void pair_commit(uint64_t* bar) {            // arriv
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(smem_addr(bar)), "h"(static_cast<uint16_t>(3)) : "memory");
 }
+__device__ __forceinline__ void pair_commit_here(uint64_t* bar) {       // at its own
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
 __device__ __forceinline__ void pair_scales_to_tmem(uint32_t tmem, uint64_t desc) {
     asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
@@ -367,7 +370,7 @@ template <bool kGelu, uint32_t kN> __device__ __forceinline__ void gate_times(fl
 
 // A warp's 32 rows of the accumulator, piece by piece; each is read at once, so that the next products may begin.  kN columns from `from`, to v; with
 // kTwo as many from `from2`, to w.  arrived(): the piece is there; read(): it has been read.
-template <uint32_t kN, bool kTwo, typename Arrived, typename Read>
+template <uint32_t kN, bool kTwo, bool kPieces, typename Arrived, typename Read>
 __device__ __forceinline__ bool add_up(float (&v)[kN], uint32_t from, float* w, uint32_t from2, uint32_t pieces, const Arrived& arrived, const Read& read) {
     bool ok = arrived();
     tmem_load<kN>(v, from);
@@ -375,7 +378,7 @@ __device__ __forceinline__ bool add_up(float (&v)[kN], uint32_t from, float* w, 
     tmem_loaded<kN>(v);
     if constexpr (kTwo) tmem_loaded<kN>(w);
     read();
-    for (uint32_t p = 1; p < pieces; ++p) {
+    for (uint32_t p = 1; kPieces && p < pieces; ++p) {
         ok = arrived();
 #pragma unroll
         for (uint32_t j = 0; j < (kTwo ? 2 : 1) * kN; j += 16) {
@@ -400,12 +403,12 @@ __device__ __forceinline__ bool add_up(float (&v)[kN], uint32_t from, float* w, 
 }
 // The same of a gated tile: 64 columns' g and u, columns 128 .. of the accumulator being up's.  The largest of the other 64 columns of the block
 // comes from the other warp group, through `shared`.
-template <typename Arrived, typename Read>
+template <bool kPieces, typename Arrived, typename Read>
 __device__ __forceinline__ void finish_wide_gated(const Task& task, uint32_t from, uint32_t row0, uint32_t block, uint32_t pieces, uint32_t* shared, float* turn,
                                                   const Arrived& arrived, const Read& accumulator_read) {
     const uint32_t group = threadIdx.x >> 7, row_lane = threadIdx.x & 127u;
     float g[64], u[64];
-    const bool ok = add_up<64, true>(g, from + group * 64, u, from + 128 + group * 64, pieces, arrived, accumulator_read);
+    const bool ok = add_up<64, true, kPieces>(g, from + group * 64, u, from + 128 + group * 64, pieces, arrived, accumulator_read);
     const uint32_t row = row0 + lane_id(), col = block * 128u + group * 64u, count = col < task.q_rows ? task.q_rows - col : 0;
     if (!ok || count < 64) {
 #pragma unroll
@@ -628,7 +631,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
             for (uint32_t i = min(issued, S::kStages); i > 0; --i) wait_landed(&sh.full[(issued - i) % S::kStages], (issued - i) / S::kStages & 1u);
         }
     } else if (warp == kProductWarp) {
-        uint32_t stage = 0, phase = 0, free_phase = 1, buffer = 0;
+        uint32_t stage = 0, phase = 0, free_phase = 1, buffer = 0, sums = 0;
         bool ok = true;
         for (uint32_t t = tile0; ok && t < tile_count; t += step) {
             uint32_t left = 0;             // stages of the present sum
@@ -639,6 +642,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                     if (!ok) break;
                     free_phase ^= 1u;
                     left = min(task.sum, end - it);
+                    ++sums;
                 }
                 --left;
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sh.full[stage], phase, task.limit, stop));
@@ -668,10 +672,15 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                 if (++stage == S::kStages) stage = 0, phase ^= 1u;
             }
         }
-        if (elected()) {             // the same of products
-            if (!ok) give_up();
-            tensor_commit(&sh.drained);
-            wait_landed(&sh.drained, 0);
+        // the same of products: the last sum's barrier says so, or one of its own where there was none
+        if (elected()) {
+            if (ok) {
+                wait_landed(&sh.done, sums - 1u & 1u);
+            } else {
+                give_up();
+                tensor_commit(&sh.drained);
+                wait_landed(&sh.drained, 0);
+            }
         }
         __syncwarp();
     } else {
@@ -705,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                 cluster_wait();
                 if constexpr (!S::kFew) {
                     float v[S::kQ / 2];
-                    add_up<S::kQ / 2, false>(v, lanes + group * (S::kQ / 2), nullptr, 0, pieces, arrived, accumulator_read);
+                    add_up<S::kQ / 2, false, true>(v, lanes + group * (S::kQ / 2), nullptr, 0, pieces, arrived, accumulator_read);
 #pragma unroll
                     for (uint32_t j = 0; j < S::kQ / 2; j += 4) {
                         const uint32_t col = group * (S::kQ / 2) + j;
@@ -748,7 +757,7 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
                     finish_few<S>(task, from, 1, S::kQ, q0 + group * (S::kQ / 2), S::kQ / 2, p0 + row_lane);
             } else {
                 float v[S::kQ / 2];
-                add_up<S::kQ / 2, false>(v, lanes + group * (S::kQ / 2), nullptr, 0, pieces, arrived, accumulator_read);
+                add_up<S::kQ / 2, false, true>(v, lanes + group * (S::kQ / 2), nullptr, 0, pieces, arrived, accumulator_read);
                 put_dense<S::kQ / 2>(task, p0 + (warp & 3u) * 32u, task.p_rows, v, q0 + group * (S::kQ / 2), task.q_rows, turn);
             }
         }
@@ -790,7 +799,8 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
 
 // ---- two CTAs to a tile ----
 
-template <bool kGated>
+// kPieces: a tile's sum may leave the tensor cores several times.
+template <bool kGated, bool kPieces>
 __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constant__ Task task) {
     using S = PairShape;
     extern __shared__ uint8_t raw[];
@@ -877,7 +887,7 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
         }
     } else if (warp == kProductWarp) {
         if (rank == 0) {
-            uint32_t stage = 0, phase = 0, free_phase = 1, buffer = 0;
+            uint32_t stage = 0, phase = 0, free_phase = 1, buffer = 0, sums = 0;
             bool ok = true;
             for (uint32_t t = tile0; ok && t < tile_count; t += step) {
                 uint32_t left = 0;             // stages of the present sum
@@ -887,7 +897,8 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
                         ok = __all_sync(0xFFFFFFFFu, wait_for_cluster(&free_again, free_phase, task.limit, stop));
                         if (!ok) break;
                         free_phase ^= 1u;
-                        left = min(task.sum, depth - it);
+                        left = kPieces ? min(task.sum, depth - it) : depth;
+                        ++sums;
                     }
                     --left;
                     ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&full[stage], phase, task.limit, stop));
@@ -912,10 +923,15 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
                     if (++stage == S::kStages) stage = 0, phase ^= 1u;
                 }
             }
-            if (elected()) {             // the same of products
-                if (!ok) give_up();
-                pair_commit(&drained);
-                wait_landed(&drained, 0);
+            // the same of products: the last sum's barrier says so, or one of its own where there was none
+            if (elected()) {
+                if (ok) {
+                    wait_landed(&done, sums - 1u & 1u);
+                } else {
+                    give_up();
+                    pair_commit_here(&drained);
+                    wait_landed(&drained, 0);
+                }
             }
             __syncwarp();
         }
@@ -943,10 +959,10 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
                 if (lane == 0 && ok) arrive_at(free_bar);          // (a warp that gave up lets nothing be overwritten any more)
             };
             if constexpr (kGated) {
-                finish_wide_gated(task, lanes, row0, at.q, pieces, largest, turn, arrived, accumulator_read);
+                finish_wide_gated<kPieces>(task, lanes, row0, at.q, pieces, largest, turn, arrived, accumulator_read);
             } else {
                 float v[128];
-                add_up<128, false>(v, lanes + group * 128u, nullptr, 0, pieces, arrived, accumulator_read);
+                add_up<128, false, kPieces>(v, lanes + group * 128u, nullptr, 0, pieces, arrived, accumulator_read);
                 put_dense<128>(task, row0, task.p_rows, v, at.q * 256u + group * 128u, task.q_rows, turn);
             }
         }
@@ -1005,17 +1021,17 @@ template <typename S> dct_status_t launch(Task& task, uint32_t sms, cudaStream_t
 }
 
 // Pairs of CTAs; as many as the device holds, from tile to tile
-template <bool kGated> dct_status_t launch_pairs(Task& task, cudaStream_t stream) {
+template <bool kGated, bool kPieces> dct_status_t launch_pairs(Task& task, cudaStream_t stream) {
     static SharedLimit allowed;
     static ClusterCounts counts;
-    dct_status_t st = allow_shared(pair8_kernel<kGated>, PairShape::kSharedBytes, allowed);
+    dct_status_t st = allow_shared(pair8_kernel<kGated, kPieces>, PairShape::kSharedBytes, allowed);
     if (st != DCT_OK) return st;
     const uint64_t tiles = static_cast<uint64_t>(task.tiles_p) * task.tiles_q;
     if (tiles > 0x3FFFFFFFull) return DCT_ERR_UNSUPPORTED;
     uint32_t at_once = 0;
-    if ((st = clusters_at_once(pair8_kernel<kGated>, kThreads, 2, PairShape::kSharedBytes, counts, &at_once)) != DCT_OK) return st;
+    if ((st = clusters_at_once(pair8_kernel<kGated, kPieces>, kThreads, 2, PairShape::kSharedBytes, counts, &at_once)) != DCT_OK) return st;
     const unsigned pairs = static_cast<unsigned>(tiles < at_once ? tiles : at_once);
-    DCT_CUDA_TRY(launch_chained_clusters(pair8_kernel<kGated>, 2 * pairs, kThreads, 2, PairShape::kSharedBytes, stream, task));
+    DCT_CUDA_TRY(launch_chained_clusters(pair8_kernel<kGated, kPieces>, 2 * pairs, kThreads, 2, PairShape::kSharedBytes, stream, task));
     return DCT_OK;
 }
 
@@ -1059,7 +1075,7 @@ dct_status_t product(const dct_act8_t* const (&a)[2], const dct_act8_t* const (&
     task.tiles_p = ceil_div(task.p_rows, q == 256 ? 256 : 128);
     task.tiles_q = ceil_div(task.q_rows, q);
     return q == 32 ? launch<Few32>(task, sms, stream) : q == 64 ? launch<Few64>(task, sms, stream)
-         : q == 128 ? launch<Wide128>(task, sms, stream) : launch_pairs<false>(task, stream);
+         : q == 128 ? launch<Wide128>(task, sms, stream) : task.sum < task.depths[0] + task.depths[1] ? launch_pairs<false, true>(task, stream) : launch_pairs<false, false>(task, stream);
 }
 
 dct_status_t gated(const dct_act8_t* x, const dct_act8_t* w_gate, const dct_act8_t* w_up, bool gelu, const dct_act8_t* h, void* h_dense, dct_dtype_t dtype,
@@ -1099,7 +1115,7 @@ dct_status_t gated(const dct_act8_t* x, const dct_act8_t* w_gate, const dct_act8
     task.q_rows = few ? rows : f;
     task.tiles_p = ceil_div(task.p_rows, few ? 128 : 256);
     task.tiles_q = few ? 1 : ceil_div(f, 128);
-    return !few ? launch_pairs<true>(task, stream) : q == 32 ? launch<GatedFew32>(task, sms, stream) : launch<GatedFew64>(task, sms, stream);
+    return !few ? (task.sum < task.depths[0] ? launch_pairs<true, true>(task, stream) : launch_pairs<true, false>(task, stream)) : q == 32 ? launch<GatedFew32>(task, sms, stream) : launch<GatedFew64>(task, sms, stream);
 }
 
 }  // namespace
