@@ -734,6 +734,8 @@ DCT_API dct_status_t dct_lm_distill(
  * 2^(e-6), by at most 2^(e-10).  A block with a NaN or an infinity becomes NaN throughout (byte 255).  (What would
  * round to 2^128, beyond fp32, takes the code below.)
  * The powers make the transpose exact but for values more than 2^13 below the largest of their new block.
+ * The calls below keep no state and need no workspace; sums run in a fixed order, so equal inputs give equal bits.  Should a bounded wait for the
+ * hardware give up (not seen in practice), what depends on it becomes NaN.
  */
 typedef struct {
   void* codes;
@@ -770,8 +772,8 @@ DCT_API dct_status_t dct_act8_transpose(const dct_act8_t* a, const dct_act8_t* o
  *   a, b     [m, k] and [n, k].   a2, b2  [m, k2] and [n, k2], or both NULL.  k may be 0 where a has 0 columns (rows of a
  *            batch that has none): that product is zero.
  *   c        [m, ld_c] fp32 or bf16; the first n columns of each row are written.  Any stride and address; it may not overlap the inputs.
- * Products and sums are fp32 (the order of a sum is fixed for given sizes), rounded once to C's type.
- * Should a bounded wait give up (not seen in practice), the tile concerned becomes NaN.
+ * Products and sums are fp32, rounded once to C's type; with more than 64 rows, sums into fp32 are added up from pieces of 4096 of depth.
+ * Any shape works; rows of the matrices that start on 128-byte boundaries and C on 32-byte ones are the fast case.
  */
 DCT_API dct_status_t dct_gemm8(
     const dct_act8_t* a, const dct_act8_t* b, const dct_act8_t* a2, const dct_act8_t* b2,
@@ -788,7 +790,7 @@ typedef enum {
  *   x                [rows, d].   w_gate, w_up  [f, d].
  *   h                [rows, f] in 8 bits, or NULL.     h_dense  [rows, ld_h] fp32 or bf16, or NULL.  One of them must be given.
  *   gate, up         [rows, f]: g and u in 8 bits, what dct_gated8_bwd takes.  Both or neither (serving) may be NULL.
- * g, u and h are fp32 throughout and rounded once into each output.  Outputs may not overlap inputs or one another.
+ * 1 <= d.  g, u and h are fp32 throughout and rounded once into each output.  Outputs may not overlap inputs or one another.
  */
 DCT_API dct_status_t dct_gated8_fwd(
     const dct_act8_t* x, const dct_act8_t* w_gate, const dct_act8_t* w_up, dct_activation_t activation,

@@ -538,6 +538,9 @@ __device__ __forceinline__ void finish_few_gated(const Task& task, Shared<S>& sh
     if (held) named_barrier_sync(1 + group, 128);          // before the next tile's are written
 }
 
+// One CTA, or a part of a cluster's tile.  Warps 0 to 7 finish tiles, warp 8 asks for copies, warp 9 for products.  Few rows are bound by reading the
+// weights: 5 TB/s in small calls (16 x 8192 x 4096: 12 us, of them 7.5 reading, 2.5 joining), 6.2 between the ends of long ones; gated, 4 x 4096 x 8192: 17 us.
+// Tiles of 128 x 128 by their codes from L2, 12 TB/s: 256 x 8192 x 4096 16 us.
 template <typename S>
 __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_constant__ Task task) {
     extern __shared__ uint8_t raw[];
@@ -799,7 +802,9 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
 
 // ---- two CTAs to a tile ----
 
-// kPieces: a tile's sum may leave the tensor cores several times.
+// The same warps.  8192 x 8192 x 4096: 201 to 210 us (2.6 to 2.7 PFLOP/s, tensor cores 62 to 70 % of the time) single, 238 to 249 over and over, where the
+// device's power is the bound; of zeros 167 (3.3 PFLOP/s), where the codes from L2 are, 14 TB/s: 670 cycles a stage of 512.  128 by 256 by single CTAs
+// would read half as much again.  Six stages of 32 KB and a CTA.  kPieces: a tile's sum may leave the tensor cores several times.
 template <bool kGated, bool kPieces>
 __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constant__ Task task) {
     using S = PairShape;
