@@ -237,6 +237,27 @@ def test_two_products_added_to_what_is_there(m, n, k, k2):
             assert (np.abs(f64(c) - want) <= product_bound(va, vb, dtype, want, np.abs(before))).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k,k2", [(2300, 4300, 4200, 130), (2560, 4352, 100, 9000), (2300, 4300, 1, 1)])
+def test_two_products_of_many_tiles(m, n, k, k2, dtype):
+    """The same over pairs of CTAs, whose sums into fp32 come in pieces that the second product may begin in; C starts on no boundary."""
+    a, b, a2, b2 = matrix(m, k, 1), matrix(n, k, 2), matrix(m, k2, 3), matrix(n, k2, 4)
+    on = lambda h: torch.from_numpy(o.values(h)).to(DEV)
+    va, vb = torch.cat([on(a), on(a2)], 1), torch.cat([on(b), on(b2)], 1)
+    product, size = va @ vb.T, va.abs() @ vb.abs().T
+    pa, pb, pa2, pb2 = put(a), put(b), put(a2), put(b2)
+    for pad, offset, accumulate in ((0, 0, True), (3, 1, True), (3, 1, False)):
+        buf = torch.randn(m * (n + pad) + offset + 8, generator=gen(5), device=DEV).to(dtype)
+        before = buf.clone()
+        c = buf[offset:offset + m * (n + pad)].view(m, n + pad)
+        was = before[offset:offset + m * (n + pad)].view(m, n + pad)[:, :n].double() * accumulate
+        B.dct_gemm8(pa, pb, c, n + pad, pa2, pb2, accumulate)
+        want, terms = product + was, k + k2 + 3
+        off = (c[:, :n].double() - want).abs()
+        assert bool((off <= terms * 2.0 ** -23 * (size + was.abs()) * (1 + HALF[dtype]) + HALF[dtype] * want.abs()).all())
+        assert torch.equal(c[:, n:], before[offset:offset + m * (n + pad)].view(m, n + pad)[:, n:]) and torch.equal(buf[-8:], before[-8:])
+
+
 @pytest.mark.parametrize("m,n", [(5, 300), (200, 300)])
 def test_product_without_depth(m, n):
     """The gradient of weights from a batch of no rows: zeros, or what was there."""
