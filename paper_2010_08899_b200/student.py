@@ -106,7 +106,7 @@ class Student:
         self.grads, self.residual, self.update = torch.zeros(n, device=device), torch.zeros(n, device=device), torch.zeros(n, device=device)
         self.grad_projection = self.grads[2 * d:head].view(vocab, d)
         self.block = FeedForward(d, ffn, rows, self.params[head:], self.grads[head:], dtype=dtype, device=device) if ffn else None
-        self.eight_bit, self.loaded = eight_bit, False             # loaded: the forms of the parameters that products take are up to date
+        self.eight_bit = eight_bit
         # what a step needs, laid out once
         if eight_bit:
             self.projection8, self.projection8_t = B.new_act8(vocab, d, device), B.new_act8(d, vocab, device)
@@ -122,6 +122,7 @@ class Student:
         self.sent, self.status, self.applied = (B.new_result(device) for _ in range(3))      # compression, distillation, decompression
         self.norm_ws = B.new_workspace(B.dct_layer_norm_bwd_workspace_bytes(rows, d), device)
         self.send_ws = B.new_workspace(B.dct_dp_select_compress_workspace_bytes(n), device)
+        self.load()
 
     def load(self) -> None:
         """The parameters in the forms the products take."""
@@ -129,12 +130,12 @@ class Student:
             self.block.load()
         if self.eight_bit:
             B.dct_act8_pack(self.projection, self.vocab, self.d, self.d, self.projection8, self.projection8_t)
-        self.loaded = True
 
-    def logits(self, hidden: torch.Tensor, training: bool = False) -> torch.Tensor:
-        """The student's logits, with the activations that cross the split packed to ``keep`` per row."""
+    def logits(self, hidden: torch.Tensor, training: bool = False, reload: bool = True) -> torch.Tensor:
+        """The student's logits, with the activations that cross the split packed to ``keep`` per row.  ``reload=False``: the parameters
+        are what they were at the last load() (serving)."""
         rows, d = self.rows, self.d
-        if not self.loaded:
+        if reload:
             self.load()
         if self.block:
             hidden = hidden + self.block.forward(hidden, keep=training)
@@ -183,16 +184,15 @@ class Student:
                                  self.send_ws)
         B.dct_dp_decompress(self.idx, self.val, self.sent, self.k, self.update, n, False, self.applied)
         self.params.sub_(self.update, alpha=self.lr)
-        self.loaded = False
         return StepResult(self.loss, self.sent, grad_hidden)
 
-    def score(self, hidden: torch.Tensor, tokens: torch.Tensor, alternatives: int = 0):
+    def score(self, hidden: torch.Tensor, tokens: torch.Tensor, alternatives: int = 0, reload: bool = True):
         """Log-probabilities of ``tokens`` (int32, negative: none), entropies and, if asked for, the best alternatives of
-        every row: what serving the student returns."""
+        every row: what serving the student returns.  ``reload`` as for logits()."""
         rows, vocab = self.rows, self.vocab
         dev = hidden.device
         lp, ent = torch.empty(rows, device=dev), torch.empty(rows, device=dev)
         ids: Optional[torch.Tensor] = torch.empty(rows, alternatives, dtype=torch.int32, device=dev) if alternatives else None
         lps = torch.empty(rows, alternatives, device=dev) if alternatives else None
-        B.dct_lm_logprobs_fwd(self.logits(hidden), rows, vocab, vocab, 1.0, tokens, alternatives, lp, ent, None, ids, lps)
+        B.dct_lm_logprobs_fwd(self.logits(hidden, reload=reload), rows, vocab, vocab, 1.0, tokens, alternatives, lp, ent, None, ids, lps)
         return lp, ent, ids, lps

@@ -149,3 +149,40 @@ def test_the_block_captured_forward_and_backward():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(y, block.forward(x))
+
+
+def student_in_8_bits(seed=4):
+    from paper_2010_08899_b200.student import Student
+    rows, d, vocab, ffn = 24, 96, 701, 160
+    s = Student(d, vocab, rows, keep=d, top=12, density=1.0, tail=False, lr=0.25, seed=seed, ffn=ffn, eight_bit=True)
+    return s, inputs.mp_gradients(rows, d, 1, device=DEV).bfloat16(), inputs.lm_logits(rows, vocab, 2, device=DEV).bfloat16()
+
+
+def test_parameters_changed_between_two_calls():
+    s, hidden, _ = student_in_8_bits()
+    other, _, _ = student_in_8_bits(seed=5)
+    s.logits(hidden)
+    s.params.copy_(other.params)
+    assert torch.equal(s.logits(hidden), other.logits(hidden))
+    # serving that changes nothing need not read the parameters again
+    assert torch.equal(s.logits(hidden, reload=False), other.logits(hidden))
+
+
+def test_a_captured_step_trains_the_parameters_it_finds():
+    s, hidden, teacher = student_in_8_bits()
+    eager, _, _ = student_in_8_bits()
+    for _ in range(3):
+        eager.step(hidden, teacher)
+    start = s.params.clone()
+    s.step(hidden, teacher)
+    s.params.copy_(start)
+    s.residual.zero_()
+    s.logits(hidden)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.step(hidden, teacher)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(s.params, eager.params)
+    assert torch.equal(s.logits(hidden), eager.logits(hidden))
