@@ -44,6 +44,7 @@ class FeedForward:
         # kept from the forward pass to the backward pass
         self.x8, self.kept_gate, self.kept_up = new8(rows, d), new8(rows, f), new8(rows, f)
         self.h8, self.y = new8(rows, f), torch.empty(rows, d, dtype=dtype, device=device)
+        self.kept = False
         # of the backward pass
         self.x8_t, self.h8_t, self.dy8, self.dy8_t = new8(d, rows), new8(f, rows), new8(rows, d), new8(d, rows)
         self.dgate8, self.dup8, self.dgate8_t, self.dup8_t = new8(rows, f), new8(rows, f), new8(f, rows), new8(f, rows)
@@ -60,12 +61,15 @@ class FeedForward:
         rows, d = self.rows, self.d
         B.dct_act8_pack(x, rows, d, d, self.x8)
         kept = (self.kept_gate, self.kept_up) if keep else (None, None)
+        self.kept = keep
         B.dct_gated8_fwd(self.x8, self.gate8, self.up8, self.activation, self.h8, None, 0, *kept)
         B.dct_gemm8(self.h8, self.down8, self.y, d)
         return self.y
 
     def backward(self, dy: torch.Tensor) -> torch.Tensor:
         """The gradient at the last forward pass's input, from that at its output; the weights' gradients go to ``grads``."""
+        if not self.kept:
+            raise RuntimeError("backward: the last forward pass kept nothing")
         rows, d, f = self.rows, self.d, self.f
         B.dct_act8_pack(dy, rows, d, d, self.dy8, self.dy8_t)
         B.dct_gemm8(self.dy8, self.down8_t, self.dh, f)

@@ -186,3 +186,22 @@ def test_a_captured_step_trains_the_parameters_it_finds():
     torch.cuda.synchronize()
     assert torch.equal(s.params, eager.params)
     assert torch.equal(s.logits(hidden), eager.logits(hidden))
+
+
+def test_no_gradients_of_a_pass_that_kept_nothing():
+    from paper_2010_08899_b200.student import FeedForward
+    rows, d, f = 20, 64, 128
+    g = torch.Generator(device=DEV).manual_seed(11)
+    params, grads = torch.randn(3 * f * d, generator=g, device=DEV) * d ** -0.5, torch.zeros(3 * f * d, device=DEV)
+    block = FeedForward(d, f, rows, params, grads)
+    block.load()
+    x = torch.randn(rows, d, generator=g, device=DEV).bfloat16()
+    with pytest.raises(RuntimeError, match="kept nothing"):
+        block.backward(x)
+    want = block.forward(x).clone()
+    block.backward(x)
+    block.forward(x, keep=False)
+    with pytest.raises(RuntimeError, match="kept nothing"):
+        block.backward(x)
+    assert torch.equal(block.forward(x), want)
+    block.backward(x)
