@@ -1153,7 +1153,13 @@ extern "C" dct_status_t dct_gemm8(const dct_act8_t* a, const dct_act8_t* b, cons
     }
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     if (!as[0]) {             // no depth: the product is zero
-        if (!accumulate) DCT_CUDA_TRY(cudaMemset2DAsync(c, ld_c * es, 0, n * es, m, stream));
+        if (accumulate) return DCT_OK;
+        const size_t pitch = ld_c * es;
+        if (pitch <= 0x7FFFFFFFu) {
+            DCT_CUDA_TRY(cudaMemset2DAsync(c, pitch, 0, n * es, m, stream));
+        } else {             // no pitch the driver takes; such rows are few
+            for (uint32_t i = 0; i < m; ++i) DCT_CUDA_TRY(cudaMemsetAsync(static_cast<uint8_t*>(c) + i * pitch, 0, n * es, stream));
+        }
         return DCT_OK;
     }
     return product(as, bs, c, dtype, ld_c, accumulate != 0, stream);

@@ -258,6 +258,16 @@ def test_two_products_of_many_tiles(m, n, k, k2, dtype):
         assert torch.equal(c[:, n:], before[offset:offset + m * (n + pad)].view(m, n + pad)[:, n:]) and torch.equal(buf[-8:], before[-8:])
 
 
+def test_product_without_depth_into_far_rows():
+    """Rows of C more than 2 GiB apart."""
+    n, ld = 300, (1 << 30) + 24
+    a, b = B.new_act8(3, 0), B.new_act8(n, 0)
+    c = torch.full((2 * ld + n + 8,), 2.0, dtype=torch.bfloat16, device=DEV)
+    B.dct_gemm8(a, b, c, ld)
+    for r in range(3):
+        assert float(c[r * ld:r * ld + n].abs().max()) == 0.0 and float(c[r * ld + n:r * ld + n + 8].min()) == 2.0
+
+
 @pytest.mark.parametrize("m,n", [(5, 300), (200, 300)])
 def test_product_without_depth(m, n):
     """The gradient of weights from a batch of no rows: zeros, or what was there."""
