@@ -67,10 +67,12 @@ struct Scales {
 struct alignas(64) Task {
     CUtensorMap p[2], q[2];         // plain: of the two products; gated: gate and up where there are two
     CUtensorMap sp_map[2], sq_map[2];        // pairs: of the scale tiles
+    CUtensorMap q_part[2];          // pairs: Q, in boxes for a quarter of a tile's columns
     Scales sp[2], sq[2];
     uint32_t depths[2];             // stages of each product
     uint32_t p_rows, q_rows;        // of P and Q
     uint32_t tiles_p, tiles_q;
+    uint32_t whole;                 // pairs: the tiles from `whole` on are done in quarters
     uint32_t split;
     uint32_t sum;                   // stages to a sum (the pieces of a depth in one accumulator)
     uint32_t limit;                 // of a bounded wait
@@ -351,6 +353,18 @@ struct Tile {
 __device__ __forceinline__ Tile tile_at(const Task& task, uint32_t t) {
     const uint32_t band = t / (8 * task.tiles_q), first = band * 8, in = t - band * 8 * task.tiles_q, height = min(8u, task.tiles_p - first);
     return Tile{first + in % height, in / height};
+}
+
+// What a pair does at a time: a tile of 256 columns, or with kParts perhaps a quarter of one, 64 columns
+struct PairTile {
+    uint32_t p, q, quarter;
+    bool whole;
+};
+template <bool kParts> __device__ __forceinline__ PairTile pair_tile_at(const Task& task, uint32_t t) {
+    const bool whole = !kParts || t < task.whole;
+    const uint32_t i = whole ? 0u : t - task.whole;
+    const Tile at = tile_at(task, whole ? t : task.whole + i / 4u);
+    return PairTile{at.p, at.q, i % 4u, whole};
 }
 
 template <typename S> struct Shared {
@@ -805,7 +819,8 @@ __global__ void __launch_bounds__(kThreads, 1) product8_kernel(const __grid_cons
 // The same warps.  8192 x 8192 x 4096: 201 to 210 us (2.6 to 2.7 PFLOP/s, tensor cores 62 to 70 % of the time) single, 238 to 249 over and over, where the
 // device's power is the bound; of zeros 167 (3.3 PFLOP/s), where the codes from L2 are, 14 TB/s: 670 cycles a stage of 512.  128 by 256 by single CTAs
 // would read half as much again.  Six stages of 32 KB and a CTA.  kPieces: a tile's sum may leave the tensor cores several times.
-template <bool kGated, bool kPieces>
+// kParts: a last round of few tiles is done in quarters of their columns.
+template <bool kGated, bool kPieces, bool kParts>
 __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constant__ Task task) {
     using S = PairShape;
     extern __shared__ uint8_t raw[];
@@ -816,7 +831,8 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
     float* turns = reinterpret_cast<float*>(scales + S::kStages * S::kScaleBytes);
 
     const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = lane_id(), rank = cluster_rank();
-    const uint32_t depth = task.depths[0] + task.depths[1], tile0 = blockIdx.x / 2, step = gridDim.x / 2, tile_count = task.tiles_p * task.tiles_q;
+    const uint32_t depth = task.depths[0] + task.depths[1], tile0 = blockIdx.x / 2, step = gridDim.x / 2;
+    const uint32_t tiles_all = task.tiles_p * task.tiles_q, tile_count = kParts ? 4 * tiles_all - 3 * task.whole : tiles_all;
     const volatile uint32_t* stop = &stop_word;
     const auto give_up = [&] { *const_cast<volatile uint32_t*>(&stop_word) = 1u; };
     chain_release_next();
@@ -848,7 +864,10 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
             uint32_t stage = 0, phase = 0, issued = 0;
             bool ok = true;
             for (uint32_t t = tile0; ok && t < tile_count; t += step) {
-                const Tile at = tile_at(task, t);
+                const PairTile at = pair_tile_at<kParts>(task, t);
+                const CUtensorMap* q_map = kGated ? &task.q[rank] : at.whole ? task.q : task.q_part;
+                const uint32_t q_row = kGated ? at.q * 128u : at.q * 256u + at.quarter * 64u + rank * (at.whole ? 128u : 32u);
+                const uint32_t stage_bytes = kTileBytes + (at.whole ? 128u : 32u) * kDepth;
                 for (uint32_t it = 0; it < depth; ++it) {
                     if (!mbar_wait_bounded(&empty[stage], phase ^ 1u, task.limit, stop)) {
                         ok = false;
@@ -859,12 +878,9 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
                     const bool with_scales = (kb & 3u) == 0;
                     uint8_t* tile = tiles + stage * S::kStageBytes;
                     const uint32_t bar = peer_address(smem_addr(&full[stage]), 0);
-                    if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * (S::kStageBytes + (with_scales ? S::kScaleBytes : 0)));
+                    if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * (stage_bytes + (with_scales ? S::kScaleBytes : 0)));
                     pair_tile_load(tile, &task.p[second], kb * kDepth, at.p * 256u + rank * 128u, bar);
-                    if constexpr (kGated)
-                        pair_tile_load(tile + kTileBytes, &task.q[rank], kb * kDepth, at.q * 128u, bar);
-                    else
-                        pair_tile_load(tile + kTileBytes, &task.q[second], kb * kDepth, at.q * 256u + rank * 128u, bar);
+                    pair_tile_load(tile + kTileBytes, q_map + second, kb * kDepth, q_row, bar);
                     if (with_scales) {
                         // (a tile of rows that are not there is another's, or zeros: it scales nothing that is written)
                         uint8_t* sc = scales + stage * S::kScaleBytes;
@@ -895,6 +911,7 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
             uint32_t stage = 0, phase = 0, free_phase = 1, buffer = 0, sums = 0;
             bool ok = true;
             for (uint32_t t = tile0; ok && t < tile_count; t += step) {
+                const PairTile at = pair_tile_at<kParts>(task, t);
                 uint32_t left = 0;             // stages of the present sum
                 for (uint32_t it = 0; ok && it < depth; ++it) {
                     const bool fresh = left == 0;
@@ -919,8 +936,15 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
 #pragma unroll
                             for (uint32_t i = 0; i < S::kScaleTiles; ++i) pair_scales_to_tmem(sf + 4 * i, from + i * (kAct8ScaleTile >> 4));
                         }
+                        if (at.whole) {
 #pragma unroll
-                        for (uint32_t k = 0; k < 4; ++k) pair_product(tmem, p + 2 * k, q + 2 * k, idesc, sf, sf + 4, !fresh || k != 0);
+                            for (uint32_t k = 0; k < 4; ++k) pair_product(tmem, p + 2 * k, q + 2 * k, idesc, sf, sf + 4, !fresh || k != 0);
+                        } else {
+                            // a quarter's columns go to the accumulator's first 64; their powers are two columns of tensor memory
+                            const uint32_t narrow = idesc - ((256u - 64u) >> 3 << 17), powers = 2 * at.quarter;
+#pragma unroll
+                            for (uint32_t k = 0; k < 4; ++k) pair_product(tmem, p + 2 * k, q + 2 * k, narrow, sf, sf + 4 + powers, !fresh || k != 0);
+                        }
                         pair_commit(&empty[stage]);
                         if (left == 0) pair_commit(&done);
                     }
@@ -947,7 +971,7 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
         uint32_t done_phase = 0;
         bool ok = true;
         for (uint32_t t = tile0; t < tile_count; t += step) {
-            const Tile at = tile_at(task, t);
+            const PairTile at = pair_tile_at<kParts>(task, t);
             const auto arrived = [&] {
                 if (ok && !__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&done, done_phase, task.limit, stop))) {
                     ok = false;
@@ -966,9 +990,15 @@ __global__ void __launch_bounds__(kThreads, 1) pair8_kernel(const __grid_constan
             if constexpr (kGated) {
                 finish_wide_gated<kPieces>(task, lanes, row0, at.q, pieces, largest, turn, arrived, accumulator_read);
             } else {
-                float v[128];
-                add_up<128, false, kPieces>(v, lanes + group * 128u, nullptr, 0, pieces, arrived, accumulator_read);
-                put_dense<128>(task, row0, task.p_rows, v, at.q * 256u + group * 128u, task.q_rows, turn);
+                if (at.whole) {
+                    float v[128];
+                    add_up<128, false, kPieces>(v, lanes + group * 128u, nullptr, 0, pieces, arrived, accumulator_read);
+                    put_dense<128>(task, row0, task.p_rows, v, at.q * 256u + group * 128u, task.q_rows, turn);
+                } else {
+                    float v[32];
+                    add_up<32, false, kPieces>(v, lanes + group * 32u, nullptr, 0, pieces, arrived, accumulator_read);
+                    put_dense<32>(task, row0, task.p_rows, v, at.q * 256u + at.quarter * 64u + group * 32u, task.q_rows, turn);
+                }
             }
         }
     }
@@ -1026,17 +1056,31 @@ template <typename S> dct_status_t launch(Task& task, uint32_t sms, cudaStream_t
 }
 
 // Pairs of CTAs; as many as the device holds, from tile to tile
-template <bool kGated, bool kPieces> dct_status_t launch_pairs(Task& task, cudaStream_t stream) {
+template <bool kGated, bool kPieces, bool kParts = false>
+dct_status_t launch_pairs(TensorEncoder e, Task& task, const dct_act8_t* const (&q_side)[2], cudaStream_t stream) {
     static SharedLimit allowed;
     static ClusterCounts counts;
-    dct_status_t st = allow_shared(pair8_kernel<kGated, kPieces>, PairShape::kSharedBytes, allowed);
+    const auto kernel = pair8_kernel<kGated, kPieces, kParts>;
+    dct_status_t st = allow_shared(kernel, PairShape::kSharedBytes, allowed);
     if (st != DCT_OK) return st;
-    const uint64_t tiles = static_cast<uint64_t>(task.tiles_p) * task.tiles_q;
-    if (tiles > 0x3FFFFFFFull) return DCT_ERR_UNSUPPORTED;
+    uint64_t items = static_cast<uint64_t>(task.tiles_p) * task.tiles_q;
+    if (items > 0x3FFFFFFFull) return DCT_ERR_UNSUPPORTED;
     uint32_t at_once = 0;
-    if ((st = clusters_at_once(pair8_kernel<kGated, kPieces>, kThreads, 2, PairShape::kSharedBytes, counts, &at_once)) != DCT_OK) return st;
-    const unsigned pairs = static_cast<unsigned>(tiles < at_once ? tiles : at_once);
-    DCT_CUDA_TRY(launch_chained_clusters(pair8_kernel<kGated, kPieces>, 2 * pairs, kThreads, 2, PairShape::kSharedBytes, stream, task));
+    if ((st = clusters_at_once(kernel, kThreads, 2, PairShape::kSharedBytes, counts, &at_once)) != DCT_OK) return st;
+    // A round of few tiles lasts as long as a full one: if quarters of them all run at once, they are what is done (a quarter reads five eighths of a
+    // tile's codes; 1023 x 5003 x 2007 in fp32, 80 tiles for 74 pairs: 22.4 us, so 19.0).  By halves nothing was gained (4096 x 4096 x 4096, 34 left over: 55.2 and 56 us).
+    const uint32_t rest = static_cast<uint32_t>(items % at_once);
+    if constexpr (!kGated && !kParts) {
+        if (rest > 0 && 4ull * rest <= at_once) return launch_pairs<kGated, kPieces, true>(e, task, q_side, stream);
+    }
+    if constexpr (kParts) {
+        task.whole = static_cast<uint32_t>(items) - rest;
+        items = task.whole + 4ull * rest;
+        for (int i = 0; i < 2; ++i)
+            if (q_side[i] && (st = encode(e, &task.q_part[i], q_side[i], 32)) != DCT_OK) return st;
+    }
+    const unsigned pairs = static_cast<unsigned>(items < at_once ? items : at_once);
+    DCT_CUDA_TRY(launch_chained_clusters(kernel, 2 * pairs, kThreads, 2, PairShape::kSharedBytes, stream, task));
     return DCT_OK;
 }
 
@@ -1079,8 +1123,8 @@ dct_status_t product(const dct_act8_t* const (&a)[2], const dct_act8_t* const (&
     task.q_rows = few ? m : n;
     task.tiles_p = ceil_div(task.p_rows, q == 256 ? 256 : 128);
     task.tiles_q = ceil_div(task.q_rows, q);
-    return q == 32 ? launch<Few32>(task, sms, stream) : q == 64 ? launch<Few64>(task, sms, stream)
-         : q == 128 ? launch<Wide128>(task, sms, stream) : task.sum < task.depths[0] + task.depths[1] ? launch_pairs<false, true>(task, stream) : launch_pairs<false, false>(task, stream);
+    return q == 32 ? launch<Few32>(task, sms, stream) : q == 64 ? launch<Few64>(task, sms, stream) : q == 128 ? launch<Wide128>(task, sms, stream)
+         : task.sum < task.depths[0] + task.depths[1] ? launch_pairs<false, true>(e, task, b, stream) : launch_pairs<false, false>(e, task, b, stream);
 }
 
 dct_status_t gated(const dct_act8_t* x, const dct_act8_t* w_gate, const dct_act8_t* w_up, bool gelu, const dct_act8_t* h, void* h_dense, dct_dtype_t dtype,
@@ -1120,7 +1164,8 @@ dct_status_t gated(const dct_act8_t* x, const dct_act8_t* w_gate, const dct_act8
     task.q_rows = few ? rows : f;
     task.tiles_p = ceil_div(task.p_rows, few ? 128 : 256);
     task.tiles_q = few ? 1 : ceil_div(f, 128);
-    return !few ? (task.sum < task.depths[0] ? launch_pairs<true, true>(task, stream) : launch_pairs<true, false>(task, stream)) : q == 32 ? launch<GatedFew32>(task, sms, stream) : launch<GatedFew64>(task, sms, stream);
+    const dct_act8_t* const none[2] = {};
+    return !few ? (task.sum < task.depths[0] ? launch_pairs<true, true>(e, task, none, stream) : launch_pairs<true, false>(e, task, none, stream)) : q == 32 ? launch<GatedFew32>(task, sms, stream) : launch<GatedFew64>(task, sms, stream);
 }
 
 }  // namespace
