@@ -44,7 +44,7 @@ class FeedForward:
         # kept from the forward pass to the backward pass
         self.x8, self.kept_gate, self.kept_up = new8(rows, d), new8(rows, f), new8(rows, f)
         self.h8, self.y = new8(rows, f), torch.empty(rows, d, dtype=dtype, device=device)
-        self.kept = False
+        self.loaded, self.kept = False, False
         # of the backward pass
         self.x8_t, self.h8_t, self.dy8, self.dy8_t = new8(d, rows), new8(f, rows), new8(rows, d), new8(d, rows)
         self.dgate8, self.dup8, self.dgate8_t, self.dup8_t = new8(rows, f), new8(rows, f), new8(f, rows), new8(f, rows)
@@ -56,9 +56,14 @@ class FeedForward:
         B.dct_act8_pack(self.gate, f, d, d, self.gate8, self.gate8_t)
         B.dct_act8_pack(self.up, f, d, d, self.up8, self.up8_t)
         B.dct_act8_pack(self.down, d, f, f, self.down8, self.down8_t)
+        self.loaded = True
 
     def forward(self, x: torch.Tensor, keep: bool = True) -> torch.Tensor:
         rows, d = self.rows, self.d
+        if not self.loaded:
+            raise RuntimeError("forward: load() has not been called")
+        if x.shape != (rows, d):
+            raise ValueError(f"x: expected {(rows, d)}, got {tuple(x.shape)}")
         B.dct_act8_pack(x, rows, d, d, self.x8)
         kept = (self.kept_gate, self.kept_up) if keep else (None, None)
         self.kept = keep
@@ -71,6 +76,8 @@ class FeedForward:
         if not self.kept:
             raise RuntimeError("backward: the last forward pass kept nothing")
         rows, d, f = self.rows, self.d, self.f
+        if dy.shape != (rows, d):
+            raise ValueError(f"dy: expected {(rows, d)}, got {tuple(dy.shape)}")
         B.dct_act8_pack(dy, rows, d, d, self.dy8, self.dy8_t)
         B.dct_gemm8(self.dy8, self.down8_t, self.dh, f)
         B.dct_gated8_bwd(self.dh, f, self.kept_gate, self.kept_up, self.activation, self.dgate8, self.dup8, self.dgate8_t, self.dup8_t,

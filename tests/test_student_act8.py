@@ -205,3 +205,23 @@ def test_no_gradients_of_a_pass_that_kept_nothing():
         block.backward(x)
     assert torch.equal(block.forward(x), want)
     block.backward(x)
+
+
+def test_the_block_refuses_other_shapes_and_parameters_it_never_loaded():
+    from paper_2010_08899_b200.student import FeedForward
+    rows, d, f = 20, 64, 128
+    g = torch.Generator(device=DEV).manual_seed(12)
+    params, grads = torch.randn(3 * f * d, generator=g, device=DEV) * d ** -0.5, torch.zeros(3 * f * d, device=DEV)
+    block = FeedForward(d, f, rows, params, grads)
+    x = torch.randn(rows, d, generator=g, device=DEV).bfloat16()
+    with pytest.raises(RuntimeError, match="load"):
+        block.forward(x)
+    block.load()
+    want = [block.forward(x).clone(), block.backward(x).clone()]
+    for shape in ((rows, 2 * d), (2 * rows, d), (d, rows), (1, rows, d)):
+        other = torch.zeros(shape, device=DEV, dtype=torch.bfloat16)
+        with pytest.raises(ValueError, match="x: expected"):
+            block.forward(other)
+        with pytest.raises(ValueError, match="dy: expected"):
+            block.backward(other)
+    assert torch.equal(block.forward(x), want[0]) and torch.equal(block.backward(x), want[1])
