@@ -27,6 +27,8 @@ constexpr uint32_t kLost = 0x7FC00000u;
 // Sums that end in fp32 leave the tensor cores every 4096 of depth and are added up in registers: the tensor cores cut what does not fit an
 // accumulator, and that error grows with the depth in one sum (2-norm over 16384 of depth: 1.5e-6 in one, 3.8e-7 in four; 8192 x 4096 x 16384: 393 and 409 us).
 // What goes into 8 bits does so every 2048: a last digit decides between two codes now and then.
+// (8192 x 4096 x 8192 kept, gate's 2-norm from 64 bits, mean of two seeds, and time: 1.05e-4 and 443 us; every 1024 0.91e-4 and 509, every 512 0.78e-4 and
+// 666, since the tensor cores wait while an accumulator is read; sums in plain fp32 0.83e-4.)
 constexpr uint32_t kSumDepths = 32, kSumDepthsHeld = 16;
 
 constexpr uint32_t power_of_two(uint32_t n) { return n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
